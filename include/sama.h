@@ -19,7 +19,8 @@
  *     or keeps caller memory.  Structs (sama_adam_t, sama_mlp_t and the dims
  *     array) are HOST memory, read during the call only.
  *   - Arrays are fp32, contiguous.  Pointers need 4-byte alignment; 16-byte
- *     alignment selects the vectorised kernels (same results).
+ *     alignment selects the vectorised kernels (same results).  (The text-model
+ *     operators also take 16-bit types, see sama_dtype: alignment to the element.)
  *   - The flat parameter vector is W1, b1, W2, b2, ..., W_l stored
  *     [d_l][d_{l-1}] row-major; the batch X is [B][d_0] row-major; labels are
  *     int32 in [0, d_L).
@@ -59,6 +60,7 @@ typedef enum sama_status {
 enum {
     SAMA_DEV_DEGENERATE_NORM = 1, /* ||p|| was 0 or not finite: eps_fd = 0, theta+- = theta, metagrad = 0 */
     SAMA_DEV_BAD_LABEL = 2,       /* a label outside [0, d_L): that sample's metagrad is 0 */
+    SAMA_DEV_BAD_INDEX = 8,       /* a token id outside [0, vocab): its output row is 0, it adds to no gradient */
     SAMA_DEV_TIMEOUT = 4          /* a bounded wait inside a kernel expired; outputs of that call are invalid, and the
                                      context's arrival counters may be left non-zero: destroy and recreate it */
 };
@@ -244,6 +246,31 @@ int sama_biasreg_step(sama_ctx* ctx, int32_t d, int32_t n_val, const float* Xv, 
                       const sama_adam_t* adam, float alpha, float* g_meta_out, float* p_out, float* w_plus,
                       float* w_minus, float* metagrad_out, void* stream);
 
+/* ---- Operators of text models -----------------------------------------------------------------------------
+ * The base models of the paper's text experiments are token encoders; these operators compute such a model's
+ * features and gradients next to the step: their gradients, clipped into one flat fp32 vector, are the g_base or
+ * g_meta of sama_adapt and sama_step.  They need a context (any sama_create will do, mlp may be NULL) for its
+ * status word and for a workspace that is allocated on first use and grows with the largest call (cudaMalloc;
+ * synchronises the stream).  A stream capture must therefore be preceded by a call of at least its sizes, and a
+ * captured graph must not be replayed after a larger call has made the workspace grow. */
+typedef enum sama_dtype { SAMA_F32 = 0, SAMA_BF16 = 1, SAMA_F16 = 2 } sama_dtype;
+
+/* Token embedding: out[t][:] = scale * table[ids[t]][:], computed in fp32 and rounded once.
+ * table: [vocab][d], out: [n_tokens][d], both of type `dtype`; ids: int32 [n_tokens].  0 <= n_tokens <= 2^30,
+ * 1 <= vocab < 2^31 - 1, d >= 1.  An id outside [0, vocab) sets SAMA_DEV_BAD_INDEX and its row of out is 0. */
+int sama_embed(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t vocab, int32_t d, const void* table,
+               const int32_t* ids, float scale, void* out, void* stream);
+
+/* Its gradient: grad[v][:] = scale * sum over {t : ids[t] = v} of d_out[t][:], summed in fp32 in a fixed order
+ * (bitwise reproducible).  d_out: [n_tokens][d] of type `dtype`; grad: [vocab][d] of type `grad_dtype`, which is
+ * `dtype` or SAMA_F32.  accumulate = 0: every row of grad is written (0 where no token is); 1: the sum is added to
+ * the rows that have tokens, the others are left alone (a table shared with another layer, or several
+ * micro-batches).  skip_id: an id that gets no gradient (padding), or a negative number for none; an id outside
+ * [0, vocab) sets SAMA_DEV_BAD_INDEX and is left out.  grad must not overlap the inputs. */
+int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t vocab, int32_t d, const int32_t* ids,
+                    const void* d_out, float scale, int32_t skip_id, int32_t grad_dtype, int32_t accumulate,
+                    void* grad, void* stream);
+
 /* sama_step (Fig. 2) for callers whose data lives in HOST memory: every
  * pointer below is a host pointer (pinned memory makes the copies
  * asynchronous).  Copies the inputs to staging buffers owned by the context
@@ -331,7 +358,9 @@ enum {
     SAMA_K_REWEIGHT_FD = 11,  /* central difference of the shared reweighting network's gradient (Eq. 5, Sec. 4.1) */
     SAMA_K_BIASREG_GRAD = 12, /* direct gradient of the biased-regression meta objective (Appendix E) */
     SAMA_K_BIASREG_FD = 13,   /* central difference for the biased-regression base objective */
-    SAMA_K_FUSED_SWEEP = 14   /* adaptation + norm + perturbation + operand split in one launch (small models) */
+    SAMA_K_FUSED_SWEEP = 14,  /* adaptation + norm + perturbation + operand split in one launch (small models) */
+    SAMA_K_EMBED = 15,        /* token embedding */
+    SAMA_K_EMBED_GRAD = 16    /* its gradient: sort, sums, joins */
 };
 typedef struct sama_kernel_time_t {
     int32_t kind;     /* SAMA_K_* */

@@ -27,7 +27,9 @@ lib = C.CDLL(LIB_PATH)
 SAMA_OK = 0
 SAMA_ERR_NULL, SAMA_ERR_ALIGN, SAMA_ERR_SIZE, SAMA_ERR_PARAM = -1, -2, -3, -4
 SAMA_ERR_OVERLAP, SAMA_ERR_CUDA, SAMA_ERR_NOMEM, SAMA_ERR_UNSUPPORTED = -5, -6, -7, -8
-SAMA_DEV_DEGENERATE_NORM, SAMA_DEV_BAD_LABEL, SAMA_DEV_TIMEOUT = 1, 2, 4
+SAMA_DEV_DEGENERATE_NORM, SAMA_DEV_BAD_LABEL, SAMA_DEV_TIMEOUT, SAMA_DEV_BAD_INDEX = 1, 2, 4, 8
+SAMA_F32, SAMA_BF16, SAMA_F16 = 0, 1, 2
+DTYPES = {"f32": SAMA_F32, "bf16": SAMA_BF16, "f16": SAMA_F16}
 
 
 class SamaError(RuntimeError):
@@ -48,7 +50,8 @@ class sama_kernel_time_t(C.Structure):
 
 KERNEL_KINDS = {0: "adapt_sumsq", 1: "sumsq", 2: "perturb", 3: "gemm_ffma", 4: "ce_fd", 5: "split_tf32",
                 6: "gemm_tf32x3", 7: "head_ce_fd", 8: "perturb_split", 9: "meta_gemm", 10: "meta_aux",
-                11: "reweight_fd", 12: "biasreg_grad", 13: "biasreg_fd", 14: "fused_sweep"}
+                11: "reweight_fd", 12: "biasreg_grad", 13: "biasreg_fd", 14: "fused_sweep", 15: "embed",
+                16: "embed_grad"}
 
 
 class sama_mlp_t(C.Structure):
@@ -106,6 +109,9 @@ lib.sama_biasreg_step.argtypes = [_vp, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp,
 lib.sama_meta_grad.argtypes = [_vp, C.POINTER(sama_mlp_t), _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp]
 lib.sama_step_host.argtypes = [_vp, C.POINTER(sama_mlp_t), C.c_int64, _vp, _vp, _vp, _vp, _vp,
                                C.POINTER(sama_adam_t), C.c_float, _vp, _vp, _vp, C.c_int32, _vp, _vp, _vp, _vp]
+lib.sama_embed.argtypes = [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, C.c_float, _vp, _vp]
+lib.sama_embed_grad.argtypes = [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, C.c_float, C.c_int32, C.c_int32,
+                                C.c_int32, _vp, _vp]
 lib.sama_ctx_sumsq.argtypes = [_vp]
 lib.sama_ctx_sumsq.restype = _vp
 lib.sama_ctx_eps_fd.argtypes = [_vp]
@@ -131,6 +137,25 @@ def _ptr(x) -> Optional[int]:
         return None
     if isinstance(x, int):
         return x
+    return x.data_ptr()
+
+
+_torch_dtypes = {}
+
+
+def _dense(x, dtype: int, count: int, where: str) -> Optional[int]:
+    """Address of an operand of the text-model operators, which take several types: a tensor has to be contiguous, of
+    the type that the call names (ids: "i32") and hold at least ``count`` elements.  Ints and None pass through."""
+    if x is None or isinstance(x, int):
+        return x
+    if not _torch_dtypes:
+        import torch
+        _torch_dtypes.update({SAMA_F32: torch.float32, SAMA_BF16: torch.bfloat16, SAMA_F16: torch.float16,
+                              "i32": torch.int32})
+    if x.dtype is not _torch_dtypes.get(dtype) or not x.is_contiguous():
+        raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is not contiguous or not of the type the call names" % where)
+    if x.numel() < count:
+        raise SamaError(SAMA_ERR_SIZE, where)
     return x.data_ptr()
 
 
@@ -253,6 +278,21 @@ def sama_biasreg_step(ctx, d, n_val, Xv, yv, w, lam, beta, m, s, g_base, adam: A
 def sama_meta_grad(ctx, mlp: MLP, theta, X_meta, y_meta, B, g_meta_out, loss_out=None, stream=None) -> int:
     return _check(lib.sama_meta_grad(ctx, mlp.c(), _ptr(theta), _ptr(X_meta), _ptr(y_meta), int(B),
                                      _ptr(g_meta_out), _ptr(loss_out), _stream(stream)), "sama_meta_grad")
+
+
+def sama_embed(ctx, dtype, n_tokens, vocab, d, table, ids, scale, out, stream=None) -> int:
+    w = "sama_embed"
+    return _check(lib.sama_embed(ctx, dtype, n_tokens, vocab, d, _dense(table, dtype, vocab * d, w),
+                                 _dense(ids, "i32", n_tokens, w), scale, _dense(out, dtype, n_tokens * d, w),
+                                 _stream(stream)), w)
+
+
+def sama_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, grad_dtype, accumulate, grad,
+                    stream=None) -> int:
+    w = "sama_embed_grad"
+    return _check(lib.sama_embed_grad(ctx, dtype, n_tokens, vocab, d, _dense(ids, "i32", n_tokens, w),
+                                      _dense(d_out, dtype, n_tokens * d, w), scale, skip_id, grad_dtype, accumulate,
+                                      _dense(grad, grad_dtype, vocab * d, w), _stream(stream)), w)
 
 
 def sama_step_host(ctx, mlp: MLP, n, theta_host, m_host, s_host, g_base_host, g_meta_host, adam: Adam, alpha,

@@ -460,6 +460,7 @@ int sama_destroy(sama_ctx* ctx) {
     cudaFree(ctx->mg_ws);
     cudaFree(ctx->mg_tc);
     cudaFree(ctx->stage);
+    cudaFree(ctx->op_ws);
     cudaFree(ctx->pm_small);
     cudaFree(ctx->pm_scratch);
     cudaFree(ctx->rw_partials);

@@ -120,6 +120,8 @@ struct sama_ctx {
     size_t br_partials_doubles;
     float* stage;                  // device: staging of the host entry point (allocated on first use)
     size_t stage_bytes;
+    void* op_ws;                   // device: workspace of the text-model operators (allocated on first use, grows)
+    size_t op_ws_bytes;
     sama::Profiler* prof;          // host
 };
 
@@ -310,5 +312,13 @@ size_t meta_grad_tc_floats(const sama_mlp_t* mlp, int64_t B);
 SplitLayout make_split_layout(const sama_mlp_t* mlp);  // sama_api.cu
 cudaError_t run_meta_grad(sama_ctx* ctx, const sama_mlp_t* mlp, const float* theta, const float* X, const int32_t* y,
                           int32_t B, float* g_out, float* loss_out, cudaStream_t st);
+
+// embed.cu : token embedding and its gradient
+cudaError_t launch_embed(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* table, const int32_t* ids,
+                         float scale, void* out, cudaStream_t st);
+size_t embed_grad_workspace(int64_t n, int64_t vocab, int d);
+cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const int32_t* ids,
+                              const void* dout, float scale, int32_t skip_id, int grad_dtype, int accumulate, void* grad,
+                              void* ws, cudaStream_t st);
 
 }  // namespace sama

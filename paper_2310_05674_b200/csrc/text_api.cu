@@ -1,0 +1,81 @@
+// Host side of the text-model operators: argument checks, workspace, launch sequencing.
+#include <cmath>
+
+#include "api_util.h"
+#include "num_types.h"
+#include "sama_internal.h"
+
+using namespace sama;
+
+namespace {
+
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+
+// The operators' workspace, at least `bytes` large.  Growing it waits for the work that may still use the old one.
+int need_workspace(sama_ctx* ctx, size_t bytes, cudaStream_t st) {
+    if (ctx->op_ws_bytes >= bytes) return SAMA_OK;
+    SAMA_CUDA(ctx, cudaStreamSynchronize(st));
+    cudaFree(ctx->op_ws);
+    ctx->op_ws = nullptr;
+    ctx->op_ws_bytes = 0;
+    if (cudaMalloc(&ctx->op_ws, bytes) != cudaSuccess) { cudaGetLastError(); return SAMA_ERR_NOMEM; }
+    ctx->op_ws_bytes = bytes;
+    return SAMA_OK;
+}
+
+// n_tokens * d and vocab * d elements of at most 4 bytes stay far from the end of 64 bits
+bool embed_sizes_ok(int64_t n_tokens, int64_t vocab, int32_t d) {
+    return n_tokens >= 0 && n_tokens <= kMaxTokens && vocab >= 1 && vocab < 0x7fffffff && d >= 1;
+}
+
+}  // namespace
+
+extern "C" {
+
+int sama_embed(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t vocab, int32_t d, const void* table,
+               const int32_t* ids, float scale, void* out, void* stream) {
+    if (!ctx || !table) return SAMA_ERR_NULL;
+    if (!embed_sizes_ok(n_tokens, vocab, d)) return SAMA_ERR_SIZE;
+    if (n_tokens > 0 && (!ids || !out)) return SAMA_ERR_NULL;
+    if (!dtype_valid(dtype) || !std::isfinite(scale)) return SAMA_ERR_PARAM;
+    const size_t es = dtype_size(dtype);
+    if (!aligned(table, es) || !aligned(out, es) || !aligned(ids, 4)) return SAMA_ERR_ALIGN;
+    const size_t ob = (size_t)n_tokens * d * es;
+    if (overlaps(out, ob, table, (size_t)vocab * d * es) || overlaps(out, ob, ids, (size_t)n_tokens * 4))
+        return SAMA_ERR_OVERLAP;
+    if (n_tokens == 0) return SAMA_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SAMA_ERR_CUDA;
+    SAMA_CUDA(ctx, launch_embed(ctx, dtype, n_tokens, vocab, d, table, ids, scale, out, (cudaStream_t)stream));
+    return SAMA_OK;
+}
+
+int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t vocab, int32_t d, const int32_t* ids,
+                    const void* d_out, float scale, int32_t skip_id, int32_t grad_dtype, int32_t accumulate,
+                    void* grad, void* stream) {
+    if (!ctx || !grad) return SAMA_ERR_NULL;
+    if (!embed_sizes_ok(n_tokens, vocab, d)) return SAMA_ERR_SIZE;
+    if (n_tokens > 0 && (!ids || !d_out)) return SAMA_ERR_NULL;
+    if (!dtype_valid(dtype) || (grad_dtype != dtype && grad_dtype != SAMA_F32) || !std::isfinite(scale) ||
+        (accumulate != 0 && accumulate != 1))
+        return SAMA_ERR_PARAM;
+    const size_t es = dtype_size(dtype), gs = dtype_size(grad_dtype);
+    if (!aligned(d_out, es) || !aligned(grad, gs) || !aligned(ids, 4)) return SAMA_ERR_ALIGN;
+    const size_t gb = (size_t)vocab * d * gs;
+    if (overlaps(grad, gb, d_out, (size_t)n_tokens * d * es) || overlaps(grad, gb, ids, (size_t)n_tokens * 4))
+        return SAMA_ERR_OVERLAP;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SAMA_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (n_tokens == 0) {
+        if (!accumulate) SAMA_CUDA(ctx, cudaMemsetAsync(grad, 0, gb, st));
+        return SAMA_OK;
+    }
+    const int rc = need_workspace(ctx, embed_grad_workspace(n_tokens, vocab, d), st);
+    if (rc != SAMA_OK) return rc;
+    SAMA_CUDA(ctx, launch_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, grad_dtype, accumulate,
+                                     grad, ctx->op_ws, st));
+    return SAMA_OK;
+}
+
+}  // extern "C"
