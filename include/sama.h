@@ -61,6 +61,7 @@ enum {
     SAMA_DEV_DEGENERATE_NORM = 1, /* ||p|| was 0 or not finite: eps_fd = 0, theta+- = theta, metagrad = 0 */
     SAMA_DEV_BAD_LABEL = 2,       /* a label outside [0, d_L): that sample's metagrad is 0 */
     SAMA_DEV_BAD_INDEX = 8,       /* a token id outside [0, vocab): its output row is 0, it adds to no gradient */
+    SAMA_DEV_NONFINITE_GRAD = 16, /* the norm of sama_clip_grads was not finite: every output is 0 */
     SAMA_DEV_TIMEOUT = 4          /* a bounded wait inside a kernel expired; outputs of that call are invalid, and the
                                      context's arrival counters may be left non-zero: destroy and recreate it */
 };
@@ -271,6 +272,27 @@ int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t voca
                     const void* d_out, float scale, int32_t skip_id, int32_t grad_dtype, int32_t accumulate,
                     void* grad, void* stream);
 
+/* One tensor of sama_clip_grads: n contiguous elements. */
+typedef struct sama_tensor_t {
+    const void* in;     /* device, type dtype */
+    void* out;          /* device, type out_dtype; == in (same type) to scale in place; NULL: counted in the norm only */
+    int64_t n;
+    int32_t dtype;      /* sama_dtype */
+    int32_t out_dtype;
+} sama_tensor_t;
+
+/* Global gradient norm over many tensors, and clipping:
+ *   norm = sqrt(sum over all tensors and elements of in^2),   c = min(1, max_norm / norm),   out = c * in,
+ * the squares summed in double in a fixed order (bitwise reproducible), each product in fp32 and rounded once.
+ * tensors (HOST, read during the call only): n_tensors of them, at most 65536; types may differ from tensor to tensor
+ * and from in to out, so the outs may be consecutive slices of the one flat fp32 vector that sama_adapt takes as
+ * g_base or g_meta.  An out may be its own in, and must overlap no other tensor of the call (the caller's to see to:
+ * only the pair itself is checked).  max_norm > 0; INFINITY never clips.  norm_out: one float on the device, or NULL.
+ * A tensor that is scaled in place is not written when c = 1.  If a gradient is not finite: SAMA_DEV_NONFINITE_GRAD is set, norm_out is infinite or NaN, and
+ * every out is 0: a step that changes nothing. */
+int sama_clip_grads(sama_ctx* ctx, const sama_tensor_t* tensors, int32_t n_tensors, float max_norm, float* norm_out,
+                    void* stream);
+
 /* sama_step (Fig. 2) for callers whose data lives in HOST memory: every
  * pointer below is a host pointer (pinned memory makes the copies
  * asynchronous).  Copies the inputs to staging buffers owned by the context
@@ -360,7 +382,8 @@ enum {
     SAMA_K_BIASREG_FD = 13,   /* central difference for the biased-regression base objective */
     SAMA_K_FUSED_SWEEP = 14,  /* adaptation + norm + perturbation + operand split in one launch (small models) */
     SAMA_K_EMBED = 15,        /* token embedding */
-    SAMA_K_EMBED_GRAD = 16    /* its gradient: sort, sums, joins */
+    SAMA_K_EMBED_GRAD = 16,   /* its gradient: sort, sums, joins */
+    SAMA_K_CLIP = 17          /* global gradient norm and clipping */
 };
 typedef struct sama_kernel_time_t {
     int32_t kind;     /* SAMA_K_* */

@@ -27,7 +27,8 @@ lib = C.CDLL(LIB_PATH)
 SAMA_OK = 0
 SAMA_ERR_NULL, SAMA_ERR_ALIGN, SAMA_ERR_SIZE, SAMA_ERR_PARAM = -1, -2, -3, -4
 SAMA_ERR_OVERLAP, SAMA_ERR_CUDA, SAMA_ERR_NOMEM, SAMA_ERR_UNSUPPORTED = -5, -6, -7, -8
-SAMA_DEV_DEGENERATE_NORM, SAMA_DEV_BAD_LABEL, SAMA_DEV_TIMEOUT, SAMA_DEV_BAD_INDEX = 1, 2, 4, 8
+SAMA_DEV_DEGENERATE_NORM, SAMA_DEV_BAD_LABEL, SAMA_DEV_TIMEOUT = 1, 2, 4
+SAMA_DEV_BAD_INDEX, SAMA_DEV_NONFINITE_GRAD = 8, 16
 SAMA_F32, SAMA_BF16, SAMA_F16 = 0, 1, 2
 DTYPES = {"f32": SAMA_F32, "bf16": SAMA_BF16, "f16": SAMA_F16}
 
@@ -51,11 +52,15 @@ class sama_kernel_time_t(C.Structure):
 KERNEL_KINDS = {0: "adapt_sumsq", 1: "sumsq", 2: "perturb", 3: "gemm_ffma", 4: "ce_fd", 5: "split_tf32",
                 6: "gemm_tf32x3", 7: "head_ce_fd", 8: "perturb_split", 9: "meta_gemm", 10: "meta_aux",
                 11: "reweight_fd", 12: "biasreg_grad", 13: "biasreg_fd", 14: "fused_sweep", 15: "embed",
-                16: "embed_grad"}
+                16: "embed_grad", 17: "clip"}
 
 
 class sama_mlp_t(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("dims", C.POINTER(C.c_int32))]
+
+
+class sama_tensor_t(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32)]
 
 
 @dataclass
@@ -86,6 +91,26 @@ class MLP:
         return C.byref(self._c)
 
 
+class TensorList:
+    """Host description of the tensors of one sama_clip_grads call, kept by a program whose gradients stay where they
+    are.  ``outs``: one tensor per input (the input itself: in place; None: counted in the norm only), or None for all
+    in place.  Holds references, so the addresses stay valid."""
+
+    def __init__(self, ins: Sequence, outs: Optional[Sequence] = None):
+        self.ins, self.outs = list(ins), list(ins if outs is None else outs)
+        if len(self.ins) != len(self.outs):
+            raise SamaError(SAMA_ERR_SIZE, "TensorList")
+        self._arr = (sama_tensor_t * max(1, len(self.ins)))()
+        for e, x, y in zip(self._arr, self.ins, self.outs):
+            e.n, e.dtype = x.numel(), _dtype_of(x)
+            e.in_ = _dense(x, e.dtype, 0, "TensorList")
+            e.out_dtype = e.dtype if y is None else _dtype_of(y)
+            e.out = None if y is None else _dense(y, e.out_dtype, e.n, "TensorList")
+
+    def c(self):
+        return self._arr
+
+
 _vp = C.c_void_p
 lib.sama_create.argtypes = [C.POINTER(_vp), C.c_int, C.c_int64, C.c_int32, C.POINTER(sama_mlp_t)]
 lib.sama_destroy.argtypes = [_vp]
@@ -112,6 +137,7 @@ lib.sama_step_host.argtypes = [_vp, C.POINTER(sama_mlp_t), C.c_int64, _vp, _vp, 
 lib.sama_embed.argtypes = [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, C.c_float, _vp, _vp]
 lib.sama_embed_grad.argtypes = [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, C.c_float, C.c_int32, C.c_int32,
                                 C.c_int32, _vp, _vp]
+lib.sama_clip_grads.argtypes = [_vp, C.POINTER(sama_tensor_t), C.c_int32, C.c_float, _vp, _vp]
 lib.sama_ctx_sumsq.argtypes = [_vp]
 lib.sama_ctx_sumsq.restype = _vp
 lib.sama_ctx_eps_fd.argtypes = [_vp]
@@ -143,15 +169,27 @@ def _ptr(x) -> Optional[int]:
 _torch_dtypes = {}
 
 
+def _fill_dtypes():
+    import torch
+    _torch_dtypes.update({SAMA_F32: torch.float32, SAMA_BF16: torch.bfloat16, SAMA_F16: torch.float16, "i32": torch.int32})
+
+
+def _dtype_of(x) -> int:
+    if not _torch_dtypes:
+        _fill_dtypes()
+    for k in (SAMA_F32, SAMA_BF16, SAMA_F16):
+        if _torch_dtypes[k] is x.dtype:
+            return k
+    raise SamaError(SAMA_ERR_PARAM, "a tensor is of type %s" % x.dtype)
+
+
 def _dense(x, dtype: int, count: int, where: str) -> Optional[int]:
     """Address of an operand of the text-model operators, which take several types: a tensor has to be contiguous, of
     the type that the call names (ids: "i32") and hold at least ``count`` elements.  Ints and None pass through."""
     if x is None or isinstance(x, int):
         return x
     if not _torch_dtypes:
-        import torch
-        _torch_dtypes.update({SAMA_F32: torch.float32, SAMA_BF16: torch.bfloat16, SAMA_F16: torch.float16,
-                              "i32": torch.int32})
+        _fill_dtypes()
     if x.dtype is not _torch_dtypes.get(dtype) or not x.is_contiguous():
         raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is not contiguous or not of the type the call names" % where)
     if x.numel() < count:
@@ -293,6 +331,12 @@ def sama_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, 
     return _check(lib.sama_embed_grad(ctx, dtype, n_tokens, vocab, d, _dense(ids, "i32", n_tokens, w),
                                       _dense(d_out, dtype, n_tokens * d, w), scale, skip_id, grad_dtype, accumulate,
                                       _dense(grad, grad_dtype, vocab * d, w), _stream(stream)), w)
+
+
+def sama_clip_grads(ctx, tensors: TensorList, max_norm, norm_out=None, stream=None) -> int:
+    w = "sama_clip_grads"
+    return _check(lib.sama_clip_grads(ctx, tensors.c(), len(tensors.ins), max_norm, _dense(norm_out, SAMA_F32, 1, w),
+                                      _stream(stream)), w)
 
 
 def sama_step_host(ctx, mlp: MLP, n, theta_host, m_host, s_host, g_base_host, g_meta_host, adam: Adam, alpha,

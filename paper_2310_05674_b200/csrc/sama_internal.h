@@ -15,6 +15,11 @@ constexpr int kTcFlags = 1024;      // arrival counters of the tensor-core kerne
 constexpr int kMaxReweightHidden = 256;  // widest hidden layer of the shared reweighting network
 constexpr int kMaxReweightBlocks = 512;  // upper bound on the grid of its reduction
 
+// What the norm of sama_clip_grads leaves for the scaling.
+struct ClipState {
+    double factor;         // min(1, max_norm / norm); 0: the norm is not finite, zeros are written
+};
+
 // Device scalars owned by a context.
 struct DeviceScalars {
     double sumsq;          // sum p^2 of the last adapt
@@ -22,6 +27,7 @@ struct DeviceScalars {
     int32_t status;        // OR of SAMA_DEV_* bits
     unsigned int counter;  // arrival counter of the last-block-done reductions and of the fused sweep's grid barrier (returns to 0)
     unsigned int departed; // blocks that have left the fused sweep's grid barrier (returns to 0)
+    ClipState clip;
 };
 
 // Host-precomputed constants of the Adam adaptation matrix (Appendix C).
@@ -320,5 +326,9 @@ size_t embed_grad_workspace(int64_t n, int64_t vocab, int d);
 cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const int32_t* ids,
                               const void* dout, float scale, int32_t skip_id, int grad_dtype, int accumulate, void* grad,
                               void* ws, cudaStream_t st);
+
+// clip_grads.cu : global gradient norm and clipping
+cudaError_t launch_clip_grads(sama_ctx* ctx, const sama_tensor_t* t, int n, float max_norm, float* norm_out,
+                              cudaStream_t st);
 
 }  // namespace sama

@@ -78,4 +78,28 @@ int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t voca
     return SAMA_OK;
 }
 
+int sama_clip_grads(sama_ctx* ctx, const sama_tensor_t* tensors, int32_t n_tensors, float max_norm, float* norm_out,
+                    void* stream) {
+    if (!ctx || (n_tensors > 0 && !tensors)) return SAMA_ERR_NULL;
+    if (n_tensors < 0 || n_tensors > 65536) return SAMA_ERR_SIZE;
+    if (!(max_norm > 0.f)) return SAMA_ERR_PARAM;
+    if (!aligned(norm_out, 4)) return SAMA_ERR_ALIGN;
+    for (int i = 0; i < n_tensors; ++i) {
+        const sama_tensor_t& t = tensors[i];
+        if (t.n < 0 || t.n > ((int64_t)1 << 40)) return SAMA_ERR_SIZE;
+        if (t.n > 0 && !t.in) return SAMA_ERR_NULL;
+        if (!dtype_valid(t.dtype) || (t.out && !dtype_valid(t.out_dtype))) return SAMA_ERR_PARAM;
+        const size_t es = dtype_size(t.dtype), os = dtype_size(t.out_dtype);
+        if (!aligned(t.in, es) || !aligned(t.out, os)) return SAMA_ERR_ALIGN;
+        const size_t ib = (size_t)t.n * es, ob = (size_t)t.n * os;
+        const bool in_place = t.out == t.in && t.out_dtype == t.dtype;
+        if ((!in_place && overlaps(t.out, ob, t.in, ib)) || overlaps(norm_out, 4, t.in, ib) || overlaps(norm_out, 4, t.out, ob))
+            return SAMA_ERR_OVERLAP;
+    }
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SAMA_ERR_CUDA;
+    SAMA_CUDA(ctx, launch_clip_grads(ctx, tensors, n_tensors, max_norm, norm_out, (cudaStream_t)stream));
+    return SAMA_OK;
+}
+
 }  // extern "C"
