@@ -272,6 +272,27 @@ int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t voca
                     const void* d_out, float scale, int32_t skip_id, int32_t grad_dtype, int32_t accumulate,
                     void* grad, void* stream);
 
+/* Gated feed-forward block (no biases; `act` is a of the gate):
+ *   G = X Wg^T,   U = X Wu^T,   H = a(G) * U (elementwise),   Y = H Wd^T
+ * x, y: [n_tokens][d]; w_gate, w_up: [f][d]; w_down: [d][f], row-major, all of type `dtype` (SAMA_BF16 or SAMA_F16).
+ * gate_out, up_out: [n_tokens][f], G and U as the backward pass wants them, or both NULL.  Products are summed in fp32;
+ * H is rounded to `dtype` in between.  0 <= n_tokens <= 2^24, 1 <= d, f <= 2^20, any of them odd; 16-byte aligned
+ * operands with d and f multiples of 8 are read in place, others are first copied to the workspace.
+ * Outputs must not overlap the inputs or one another.
+ *
+ * sama_gated_ffn_grad, given the gradient dy of Y, G and U:
+ *   dH = dY Wd,  dG = dH * U * a'(G),  dU = dH * a(G),
+ *   dx = dG Wg + dU Wu,  dw_gate = dG^T X,  dw_up = dU^T X,  dw_down = dY^T H
+ * each of type `dtype`; an output that is NULL is not computed.  a' of the ReLU at 0 is 0.  With n_tokens = 0 the
+ * weight gradients are zeros. */
+enum { SAMA_ACT_SILU = 0, SAMA_ACT_GELU = 1, SAMA_ACT_GELU_TANH = 2, SAMA_ACT_RELU = 3 };
+int sama_gated_ffn(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tokens, int32_t d, int32_t f, const void* x,
+                   const void* w_gate, const void* w_up, const void* w_down, void* y, void* gate_out, void* up_out,
+                   void* stream);
+int sama_gated_ffn_grad(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tokens, int32_t d, int32_t f, const void* x,
+                        const void* w_gate, const void* w_up, const void* w_down, const void* gate, const void* up,
+                        const void* dy, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* stream);
+
 /* One tensor of sama_clip_grads: n contiguous elements. */
 typedef struct sama_tensor_t {
     const void* in;     /* device, type dtype */
@@ -383,7 +404,8 @@ enum {
     SAMA_K_FUSED_SWEEP = 14,  /* adaptation + norm + perturbation + operand split in one launch (small models) */
     SAMA_K_EMBED = 15,        /* token embedding */
     SAMA_K_EMBED_GRAD = 16,   /* its gradient: sort, sums, joins */
-    SAMA_K_CLIP = 17          /* global gradient norm and clipping */
+    SAMA_K_CLIP = 17,         /* global gradient norm and clipping */
+    SAMA_K_FFN = 18           /* gated feed-forward block; layer: 0 gate-up, 1 down, 2 d-hidden, 3 d-input, 4 d-weights */
 };
 typedef struct sama_kernel_time_t {
     int32_t kind;     /* SAMA_K_* */

@@ -31,6 +31,8 @@ SAMA_DEV_DEGENERATE_NORM, SAMA_DEV_BAD_LABEL, SAMA_DEV_TIMEOUT = 1, 2, 4
 SAMA_DEV_BAD_INDEX, SAMA_DEV_NONFINITE_GRAD = 8, 16
 SAMA_F32, SAMA_BF16, SAMA_F16 = 0, 1, 2
 DTYPES = {"f32": SAMA_F32, "bf16": SAMA_BF16, "f16": SAMA_F16}
+SAMA_ACT_SILU, SAMA_ACT_GELU, SAMA_ACT_GELU_TANH, SAMA_ACT_RELU = 0, 1, 2, 3
+ACTS = {"silu": SAMA_ACT_SILU, "gelu": SAMA_ACT_GELU, "gelu_tanh": SAMA_ACT_GELU_TANH, "relu": SAMA_ACT_RELU}
 
 
 class SamaError(RuntimeError):
@@ -52,7 +54,7 @@ class sama_kernel_time_t(C.Structure):
 KERNEL_KINDS = {0: "adapt_sumsq", 1: "sumsq", 2: "perturb", 3: "gemm_ffma", 4: "ce_fd", 5: "split_tf32",
                 6: "gemm_tf32x3", 7: "head_ce_fd", 8: "perturb_split", 9: "meta_gemm", 10: "meta_aux",
                 11: "reweight_fd", 12: "biasreg_grad", 13: "biasreg_fd", 14: "fused_sweep", 15: "embed",
-                16: "embed_grad", 17: "clip"}
+                16: "embed_grad", 17: "clip", 18: "ffn"}
 
 
 class sama_mlp_t(C.Structure):
@@ -137,6 +139,8 @@ lib.sama_step_host.argtypes = [_vp, C.POINTER(sama_mlp_t), C.c_int64, _vp, _vp, 
 lib.sama_embed.argtypes = [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, C.c_float, _vp, _vp]
 lib.sama_embed_grad.argtypes = [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32, _vp, _vp, C.c_float, C.c_int32, C.c_int32,
                                 C.c_int32, _vp, _vp]
+lib.sama_gated_ffn.argtypes = [_vp, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int32] + [_vp] * 8
+lib.sama_gated_ffn_grad.argtypes = [_vp, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int32] + [_vp] * 12
 lib.sama_clip_grads.argtypes = [_vp, C.POINTER(sama_tensor_t), C.c_int32, C.c_float, _vp, _vp]
 lib.sama_ctx_sumsq.argtypes = [_vp]
 lib.sama_ctx_sumsq.restype = _vp
@@ -331,6 +335,27 @@ def sama_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, 
     return _check(lib.sama_embed_grad(ctx, dtype, n_tokens, vocab, d, _dense(ids, "i32", n_tokens, w),
                                       _dense(d_out, dtype, n_tokens * d, w), scale, skip_id, grad_dtype, accumulate,
                                       _dense(grad, grad_dtype, vocab * d, w), _stream(stream)), w)
+
+
+def sama_gated_ffn(ctx, dtype, act, n_tokens, d, f, x, w_gate, w_up, w_down, y, gate_out=None, up_out=None,
+                   stream=None) -> int:
+    w = "sama_gated_ffn"
+    return _check(lib.sama_gated_ffn(ctx, dtype, act, n_tokens, d, f, _dense(x, dtype, n_tokens * d, w),
+                                     _dense(w_gate, dtype, f * d, w), _dense(w_up, dtype, f * d, w),
+                                     _dense(w_down, dtype, d * f, w), _dense(y, dtype, n_tokens * d, w),
+                                     _dense(gate_out, dtype, n_tokens * f, w), _dense(up_out, dtype, n_tokens * f, w),
+                                     _stream(stream)), w)
+
+
+def sama_gated_ffn_grad(ctx, dtype, act, n_tokens, d, f, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up,
+                        dw_down, stream=None) -> int:
+    w = "sama_gated_ffn_grad"
+    t, h, m = n_tokens * d, n_tokens * f, d * f
+    return _check(lib.sama_gated_ffn_grad(ctx, dtype, act, n_tokens, d, f, _dense(x, dtype, t, w),
+                                          _dense(w_gate, dtype, m, w), _dense(w_up, dtype, m, w),
+                                          _dense(w_down, dtype, m, w), _dense(gate, dtype, h, w), _dense(up, dtype, h, w),
+                                          _dense(dy, dtype, t, w), _dense(dx, dtype, t, w), _dense(dw_gate, dtype, m, w),
+                                          _dense(dw_up, dtype, m, w), _dense(dw_down, dtype, m, w), _stream(stream)), w)
 
 
 def sama_clip_grads(ctx, tensors: TensorList, max_norm, norm_out=None, stream=None) -> int:

@@ -1,0 +1,731 @@
+// Gated feed-forward block and its backward pass on the 5th-generation tensor cores, bf16 or fp16 operands, fp32 sums.
+//
+//   G = X Wg^T,  U = X Wu^T,  H = a(G) * U,  Y = H Wd^T
+//   dH = dY Wd,  dG = dH * U * a'(G),  dU = dH * a(G)
+//   dX = dG Wg + dU Wu,  dWg = dG^T X,  dWu = dU^T X,  dWd = dY^T H
+//
+// Five launches of one persistent kernel template, two forward and three backward:
+//   gate-up   both projections of a tile of X in one pass: the tile of the right operand is half rows of Wg and half the
+//             same rows of Wu, so one accumulator holds G and U of the same features side by side and the epilogue forms
+//             H from registers.  G and U are stored only if a backward pass will want them.
+//   down      Y = H Wd^T
+//   d-hidden  dH = dY Wd, whose epilogue reads G and U and leaves dG, dU and H (formed again rather than kept)
+//   d-input   dX as one product over the concatenated contraction (dG, dU) x (Wg, Wu)
+//   d-weights the three weight gradients as one launch over the tiles of all three
+// H, dG and dU are rounded to the operands' type between launches, as any operand of a 16-bit product has to be; every
+// sum stays in fp32 until its one rounding on the way out.
+//
+// Operands are read as they lie in memory: where the contraction runs along a matrix's rows, the tile is loaded and
+// described to the tensor core "MN-major" instead of being transposed by a pass of its own.
+//
+// Roles of the 10 warps: warp 0 copies (TMA, 128-byte swizzle, six 32 KB stages), warp 1 issues products, warps 2..9
+// read finished accumulators and store them through a shared-memory transpose while the next tile is multiplied (two
+// accumulators in tensor memory).  A CTA pair works on a 256 x 256 tile with cta_group::2 products; shapes with too few
+// of those take 128 x 128 tiles on single CTAs.  Every wait is bounded: one that expires raises SAMA_DEV_TIMEOUT, stops
+// the CTA's work, lets its copies land and exits.
+#include <type_traits>
+
+#include "num_types.h"
+#include "sama_internal.h"
+#include "tc_ptx.h"
+
+namespace sama {
+
+namespace {
+
+constexpr int BM = 128;         // rows of a CTA's share of the output tile
+constexpr int BK = 64;          // contraction per stage: one 128-byte row of 16-bit values
+constexpr int STAGES = 6;
+constexpr int OPERAND = BM * BK * 2;              // bytes of either operand's share of a stage
+constexpr int STAGE = 2 * OPERAND;
+constexpr int EPI = 8;          // epilogue warps
+constexpr int THREADS = 64 + 32 * EPI;
+constexpr int STAGING = 4096;   // bytes per epilogue warp
+constexpr int SMEM = STAGES * STAGE + EPI * STAGING + 256 + 1024;
+
+enum Mode { GATE_UP, PLAIN, D_HIDDEN };
+
+struct Problem {
+    CUtensorMap a[2], b[2];     // [1]: the second part of the contraction, or (gate-up) the second right operand
+    int M, N;                   // rows and columns of the output (gate-up: features)
+    int num_kb, kb_first;       // k-blocks, and how many of them the first maps cover
+    int tiles_m, tiles_n, item0;
+    void* out[3];
+    const void* in[2];          // d-hidden: G and U
+    int64_t ldo[3], ldi;
+    int cols[3];                // columns of out[i] that may be written
+    int vec_out, vec_in;        // bit i: out[i] (G and U) can be accessed in aligned 16-byte groups
+};
+template <int G>
+struct alignas(64) Params {
+    Problem p[G];
+    int n_items, group_m, act;
+    int32_t* status;
+};
+
+// ---------------------------------------------------------------- PTX for 16-bit products
+
+// D (fp32) += A B^T, 16 of the contraction per instruction.
+__device__ __forceinline__ void umma16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Instruction descriptor: fp32 accumulator (bit 4), operand type (bits 7 and 10: 0 fp16, 1 bf16; both the same),
+// operands stored MN-major (bits 15, 16), N / 8 (bit 17), M / 16 (bit 24).
+__host__ __device__ constexpr uint32_t idesc16(bool bf16, bool a_mn, bool b_mn, int m, int n) {
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+// Shared-memory descriptor of an MN-major tile with the 128-byte swizzle: rows of the contraction are 64 consecutive
+// elements of M (or N), 128 bytes; 8 rows make a swizzle block of 1024 bytes (the stride offset); the next 64 elements
+// of M lie BK rows further on (the leading offset).
+__device__ __forceinline__ uint64_t make_desc_mn(uint32_t saddr) {
+    return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)((BK * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+// Into this CTA's shared memory, counted on the leader's barrier.
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t leader_bar, int x, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst), "l"(map), "r"(leader_bar), "r"(x), "r"(y) : "memory");
+}
+
+// ---------------------------------------------------------------- activations
+
+// a(x), and with GRAD its derivative.
+template <bool GRAD>
+__device__ __forceinline__ float2 activate(int act, float x) {
+    if (act == SAMA_ACT_SILU) {
+        const float s = __fdividef(1.f, 1.f + __expf(-x));   // exp overflows to infinity for x < -88: s = 0, as it should
+        return make_float2(x * s, GRAD ? s * fmaf(x, 1.f - s, 1.f) : 0.f);
+    }
+    if (act == SAMA_ACT_RELU) return make_float2(x > 0.f ? x : (x != x ? x : 0.f), x > 0.f ? 1.f : 0.f);
+    if (act == SAMA_ACT_GELU) {
+        const float p = 0.5f * erfcf(-0.70710678f * x);      // the normal distribution function, accurate in both tails
+        return make_float2(x * p, GRAD ? fmaf(x * 0.39894228f, __expf(-0.5f * x * x), p) : 0.f);
+    }
+    // gelu_tanh: 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
+    const float z2 = 1.59576912f * x * fmaf(0.044715f * x, x, 1.f);
+    const float p = __fdividef(1.f, 1.f + __expf(-z2));
+    return make_float2(x * p, GRAD ? fmaf(x * p * (1.f - p), 1.59576912f * fmaf(0.134145f * x, x, 1.f), p) : 0.f);
+}
+
+// ---------------------------------------------------------------- stores
+
+// Writes a block of 32 rows x CU columns that a warp holds as packed pairs, one row per lane, in whole row segments:
+// through `stg` with 16-byte chunks permuted by row, so that neither side has bank conflicts.
+template <typename T, int CU>
+__device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, T* dst, int64_t ld, int row0, int rows,
+                                           int col0, int cols, bool vec, int lane) {
+    constexpr int LPR = CU / 8;  // 16-byte chunks of a row
+    auto at = [](int r, int c) { return r * LPR + (c ^ (LPR == 8 ? (r & 7) : ((r >> 1) & 3))); };
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < LPR; ++c)
+        stg[at(lane, c)] = make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+    __syncwarp();
+    if (vec) {
+        const int c = lane % LPR;
+        if (col0 + 8 * c < cols) {   // (a vector destination has whole groups of eight columns)
+#pragma unroll
+            for (int i = 0; i < LPR; ++i) {
+                const int r = lane / LPR + i * (32 / LPR);
+                if (r < rows) *reinterpret_cast<uint4*>(dst + (int64_t)(row0 + r) * ld + col0 + 8 * c) = stg[at(r, c)];
+            }
+        }
+    } else {
+        // rows that start anywhere: neighbouring lanes take neighbouring elements
+        const T* s = reinterpret_cast<const T*>(stg);
+#pragma unroll 4
+        for (int r = 0; r < 32; ++r)
+            if (r < rows)
+#pragma unroll
+                for (int j = 0; j < CU / 32; ++j) {
+                    const int c = lane + 32 * j;
+                    if (col0 + c < cols) dst[(int64_t)(row0 + r) * ld + col0 + c] = s[at(r, c >> 3) * 8 + (c & 7)];
+                }
+    }
+}
+
+// Eight consecutive values of a row, zeros beyond `cols`.
+template <typename T>
+__device__ __forceinline__ uint4 load8(const T* p, int col, int cols, bool vec) {
+    if (vec) return __ldg(reinterpret_cast<const uint4*>(p + col));
+    uint32_t r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = col + 2 * j < cols ? *reinterpret_cast<const uint16_t*>(p + col + 2 * j) : 0;
+        const uint32_t hi = col + 2 * j + 1 < cols ? *reinterpret_cast<const uint16_t*>(p + col + 2 * j + 1) : 0;
+        r[j] = lo | (hi << 16);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+// ---------------------------------------------------------------- the kernel
+
+template <typename T, int MODE, bool PAIR, bool A_MN, bool B_MN, int G>
+__global__ void __launch_bounds__(THREADS, 1)
+ffn_kernel(const __grid_constant__ Params<G> P) {
+    constexpr int BN = PAIR ? 256 : 128;                // accumulator columns
+    constexpr int TN = MODE == GATE_UP ? BN / 2 : BN;   // output columns (features) of a tile
+    constexpr int TM = PAIR ? 2 * BM : BM;
+    constexpr uint32_t IDESC = idesc16(std::is_same<T, __nv_bfloat16>::value, A_MN, B_MN, TM, BN);
+    constexpr uint32_t TMEM_COLS = 2 * BN;
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;       // swizzled tiles need 1024-byte alignment
+    const uint32_t staging = base + STAGES * STAGE;
+    const uint32_t bars = staging + EPI * STAGING;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
+    auto acc_full_bar = [&](int b) { return bars + 8u * (2 * STAGES + b); };
+    auto acc_empty_bar = [&](int b) { return bars + 8u * (2 * STAGES + 2 + b); };
+    const uint32_t tmem_slot = bars + 8u * (2 * STAGES + 4);
+    volatile uint32_t* tmem_ptr_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_slot - raw));
+    volatile uint32_t* abort_flag = tmem_ptr_slot + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
+    const int unit = (int)blockIdx.x / (PAIR ? 2 : 1), n_units = (int)gridDim.x / (PAIR ? 2 : 1);
+
+    // Work item -> problem and tile.  Items that run together cover group_m row tiles of a few column tiles, so that
+    // one wave's operands come out of L2.
+    auto locate = [&](int item, int& tm, int& tn) -> const Problem& {
+        int g = 0;
+#pragma unroll
+        for (int i = 1; i < G; ++i)
+            if (item >= P.p[i].item0) g = i;
+        const Problem& q = P.p[g];
+        const int t = item - q.item0, per_group = P.group_m * q.tiles_n, group = t / per_group, rem = t - group * per_group;
+        const int first = group * P.group_m, size = min(P.group_m, q.tiles_m - first);
+        tm = first + rem % size;
+        tn = rem / size;
+        return q;
+    };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full_bar(b), 1);
+            mbar_init(acc_empty_bar(b), EPI * (PAIR ? 2 : 1));
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if (PAIR) tmem_alloc_pair(tmem_slot, TMEM_COLS); else tmem_alloc(tmem_slot, TMEM_COLS);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync();  // the other CTA's barriers exist before anything is signalled on them
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_ptr_slot;
+    pdl_trigger();
+    pdl_wait();
+
+    auto raise_timeout = [&]() {
+        *abort_flag = 1;
+        atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
+    };
+
+    if (warp == 0) {
+        // ---------------------------------------------------------- copies
+        if (lane == 0) {
+            int issued = 0, s = 0;
+            uint32_t empty_parity = 1;
+            bool ok = true;
+            for (int item = unit; ok && item < P.n_items; item += n_units) {
+                int tm, tn;
+                const Problem& q = locate(item, tm, tn);
+                const int m0 = tm * TM + (int)rank * BM;
+                const int n0 = tn * TN + (PAIR && MODE != GATE_UP ? (int)rank * BM : 0);
+                for (int kb = 0; kb < q.num_kb; ++kb) {
+                    if (issued >= STAGES && !mbar_wait(empty_bar(s), empty_parity, abort_flag)) { raise_timeout(); ok = false; break; }
+                    const uint32_t sa = base + s * STAGE, sb = sa + OPERAND;
+                    const int part = MODE != GATE_UP && kb >= q.kb_first;
+                    const int k0 = (kb - (part ? q.kb_first : 0)) * BK;
+                    const CUtensorMap* ma = &q.a[part];
+                    const CUtensorMap* mb = &q.b[MODE == GATE_UP ? (PAIR ? (int)rank : 0) : part];
+                    const uint32_t bar = PAIR ? (full_bar(s) & kPeerBitMask) : full_bar(s);
+                    if (!PAIR || rank == 0) mbar_expect_tx(full_bar(s), STAGE * (PAIR ? 2 : 1));
+                    auto load = [&](uint32_t dst, const CUtensorMap* map, int x, int y) {
+                        if (PAIR) tma_load_2d_pair(dst, map, bar, x, y); else tma_load_2d(dst, map, bar, x, y);
+                    };
+                    if (A_MN) {
+                        load(sa, ma, m0, k0);
+                        load(sa + OPERAND / 2, ma, m0 + 64, k0);
+                    } else {
+                        load(sa, ma, k0, m0);
+                    }
+                    if (B_MN) {
+                        load(sb, mb, n0, k0);
+                        load(sb + OPERAND / 2, mb, n0 + 64, k0);
+                    } else if (MODE == GATE_UP && !PAIR) {
+                        load(sb, &q.b[0], k0, n0);
+                        load(sb + OPERAND / 2, &q.b[1], k0, n0);
+                    } else {
+                        load(sb, mb, k0, n0);
+                    }
+                    ++issued;
+                    if (++s == STAGES) { s = 0; empty_parity ^= 1u; }
+                }
+            }
+            if (*abort_flag && rank == 0) {
+                // let the copies already issued land before the CTA's shared memory goes away
+                for (int i = (issued > STAGES ? issued - STAGES : 0); i < issued; ++i) mbar_wait(full_bar(i % STAGES), (i / STAGES) & 1);
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------------------------------------------------- products (the leader's, for a pair)
+        if (lane == 0 && rank == 0) {
+            int s = 0, t = 0;  // t counts tiles: accumulator t & 1
+            uint32_t full_parity = 0;
+            bool ok = true;
+            for (int item = unit; ok && item < P.n_items; item += n_units, ++t) {
+                int tm, tn;
+                const Problem& q = locate(item, tm, tn);
+                const int buf = t & 1;
+                if (t >= 2 && !mbar_wait(acc_empty_bar(buf), ((t >> 1) - 1) & 1, abort_flag)) { raise_timeout(); break; }
+                tc_fence_after();
+                const uint32_t acc = tmem_base + (uint32_t)buf * BN;
+                for (int kb = 0; kb < q.num_kb; ++kb) {
+                    if (!mbar_wait(full_bar(s), full_parity, abort_flag)) { raise_timeout(); ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sa = base + s * STAGE, sb = sa + OPERAND;
+                    const uint64_t da = A_MN ? make_desc_mn(sa) : make_desc(sa), db = B_MN ? make_desc_mn(sb) : make_desc(sb);
+#pragma unroll
+                    for (int k = 0; k < BK / 16; ++k) {
+                        // 16 of the contraction: 32 bytes along a K-major row, 16 rows of 128 bytes of an MN-major tile
+                        const uint64_t ka = (uint64_t)((A_MN ? k * 2048 : k * 32) >> 4), kbo = (uint64_t)((B_MN ? k * 2048 : k * 32) >> 4);
+                        if (PAIR) umma16_pair(acc, da + ka, db + kbo, IDESC, kb > 0 || k > 0);
+                        else umma16(acc, da + ka, db + kbo, IDESC, kb > 0 || k > 0);
+                    }
+                    if (PAIR) umma_commit_pair(empty_bar(s)); else umma_commit(empty_bar(s));
+                    if (++s == STAGES) { s = 0; full_parity ^= 1u; }
+                }
+                if (!ok) break;
+                if (PAIR) umma_commit_pair(acc_full_bar(buf)); else umma_commit(acc_full_bar(buf));
+            }
+        }
+    } else {
+        // ---------------------------------------------------------- epilogue
+        const int quarter = warp & 3;               // a warp may only touch TMEM lanes [32 quarter, 32 quarter + 32)
+        const int half = (warp - 2) >> 2;           // which half of the tile's columns
+        const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+        uint4* stg = reinterpret_cast<uint4*>(smem_raw + (staging - raw) + (warp - 2) * STAGING);
+        const int my_tiles = unit < P.n_items ? (P.n_items - unit + n_units - 1) / n_units : 0;
+        bool ok = true;
+        int t = 0;
+        for (int item = unit; item < P.n_items; item += n_units, ++t) {
+            int tm, tn;
+            const Problem& q = locate(item, tm, tn);
+            const int buf = t & 1;
+            const int row0 = tm * TM + (int)rank * BM + quarter * 32;
+            const int rows = min(32, q.M - row0);   // may be negative: nothing to store
+            const uint32_t acc = lane_addr + (uint32_t)buf * BN;
+            if (lane == 0) {
+                // the tile is complete when its barrier flips, or never if another role gave up
+                const long long t0 = clock64();
+                while (!mbar_try(acc_full_bar(buf), (t >> 1) & 1)) {
+                    if (*abort_flag) { ok = false; break; }
+                    if (clock64() - t0 > 2 * kWaitCycles) { raise_timeout(); ok = false; break; }
+                }
+            }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            if (!ok) break;
+            tc_fence_after();
+            // Hands the accumulator back.  (Not for the last two tiles: nobody waits for them, and no arrival may be
+            // on its way to the other CTA when that one exits.)
+            auto release = [&]() {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0 && t + 2 < my_tiles) {
+                    if (PAIR) mbar_arrive_cluster(acc_empty_bar(buf) & kPeerBitMask); else mbar_arrive(acc_empty_bar(buf));
+                }
+            };
+            if constexpr (MODE == GATE_UP) {
+                constexpr int CU = TN / 2;          // features per warp: 64 or 32
+                uint32_t pg[CU / 2], pu[CU / 2], ph[CU / 2];
+#pragma unroll
+                for (int c = 0; c < CU; c += 32) {
+                    float g[32], u[32];
+                    tmem_ld32(acc + half * CU + c, g);
+                    tmem_ld32(acc + TN + half * CU + c, u);
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        const float h0 = activate<false>(P.act, g[j]).x * u[j], h1 = activate<false>(P.act, g[j + 1]).x * u[j + 1];
+                        pg[(c + j) / 2] = pack2<T>(g[j], g[j + 1]);
+                        pu[(c + j) / 2] = pack2<T>(u[j], u[j + 1]);
+                        ph[(c + j) / 2] = pack2<T>(h0, h1);
+                    }
+                }
+                release();
+                const int col0 = tn * TN + half * CU;
+                if (q.out[0]) {
+                    store_rows<T, CU>(stg, pg, static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, col0, q.cols[0], q.vec_out & 1, lane);
+                    store_rows<T, CU>(stg, pu, static_cast<T*>(q.out[1]), q.ldo[1], row0, rows, col0, q.cols[1], q.vec_out & 2, lane);
+                }
+                store_rows<T, CU>(stg, ph, static_cast<T*>(q.out[2]), q.ldo[2], row0, rows, col0, q.cols[2], q.vec_out & 4, lane);
+            } else if constexpr (MODE == PLAIN) {
+#pragma unroll
+                for (int c = 0; c < TN / 2; c += 64) {
+                    uint32_t packed[32];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float v[32];
+                        tmem_ld32(acc + half * (TN / 2) + c + 32 * i, v);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) packed[16 * i + j / 2] = pack2<T>(v[j], v[j + 1]);
+                    }
+                    if (c + 64 >= TN / 2) release();
+                    store_rows<T, 64>(stg, packed, static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, tn * TN + half * (TN / 2) + c,
+                                      q.cols[0], q.vec_out & 1, lane);
+                }
+            } else {
+                // The block goes through shared memory in fp32, so that G and U are read, and dG, dU and H written,
+                // in row segments of 64 bytes: a lane handles eight columns of rows lane / 4 + 8 i.
+                float4* sf = reinterpret_cast<float4*>(stg);
+                const int c8 = lane & 3, r0 = lane >> 2;
+#pragma unroll 1
+                for (int c = 0; c < TN / 2; c += 32) {
+                    const int col = tn * TN + half * (TN / 2) + c + 8 * c8;
+                    uint4 vg[4], vu[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = r0 + 8 * i;
+                        vg[i] = vu[i] = make_uint4(0, 0, 0, 0);
+                        if (r < rows && col < q.N) {
+                            vg[i] = load8(static_cast<const T*>(q.in[0]) + (int64_t)(row0 + r) * q.ldi, col, q.N, q.vec_in & 1);
+                            vu[i] = load8(static_cast<const T*>(q.in[1]) + (int64_t)(row0 + r) * q.ldi, col, q.N, q.vec_in & 2);
+                        }
+                    }
+                    float v[32];
+                    tmem_ld32(acc + half * (TN / 2) + c, v);
+                    if (c + 32 >= TN / 2) release();
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        sf[lane * 8 + (k ^ (lane & 7))] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = r0 + 8 * i;
+                        if (r >= rows || col >= q.cols[0]) continue;
+                        const float4 d0 = sf[r * 8 + ((2 * c8) ^ (r & 7))], d1 = sf[r * 8 + ((2 * c8 + 1) ^ (r & 7))];
+                        const float dh[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
+                        const uint32_t wg[4] = {vg[i].x, vg[i].y, vg[i].z, vg[i].w}, wu[4] = {vu[i].x, vu[i].y, vu[i].z, vu[i].w};
+                        uint32_t og[4], ou[4], oh[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 g = unpack2<T>(wg[j]), u = unpack2<T>(wu[j]);
+                            const float2 a0 = activate<true>(P.act, g.x), a1 = activate<true>(P.act, g.y);
+                            og[j] = pack2<T>(dh[2 * j] * u.x * a0.y, dh[2 * j + 1] * u.y * a1.y);
+                            ou[j] = pack2<T>(dh[2 * j] * a0.x, dh[2 * j + 1] * a1.x);
+                            oh[j] = pack2<T>(a0.x * u.x, a1.x * u.y);
+                        }
+                        const int64_t at = (int64_t)(row0 + r) * q.ldo[0] + col;   // all three have the same layout
+                        *reinterpret_cast<uint4*>(static_cast<T*>(q.out[0]) + at) = make_uint4(og[0], og[1], og[2], og[3]);
+                        *reinterpret_cast<uint4*>(static_cast<T*>(q.out[1]) + at) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                        *reinterpret_cast<uint4*>(static_cast<T*>(q.out[2]) + at) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (PAIR) cluster_sync_relaxed();  // the leader's products use the other CTA's shared and tensor memory
+    if (warp == 1) {
+        tc_fence_after();
+        if (PAIR) tmem_dealloc_pair(tmem_base, TMEM_COLS); else tmem_dealloc(tmem_base, TMEM_COLS);
+    }
+}
+
+// Rows of `cols` values at any address -> rows of `ld` (a multiple of 8) at an aligned one: what TMA can read.
+template <typename T>
+__global__ void __launch_bounds__(256)
+align_rows_kernel(const T* __restrict__ src, int64_t rows, int cols, int ld, T* __restrict__ dst) {
+    pdl_trigger();
+    pdl_wait();
+    const int groups = ld / 8;
+    const int64_t total = rows * groups;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t r = i / groups;
+        const int c = (int)(i - r * groups) * 8;
+        *reinterpret_cast<uint4*>(dst + r * ld + c) = load8(src + r * cols, c, cols, false);
+    }
+}
+
+// ---------------------------------------------------------------- host side
+
+inline int up8(int x) { return (x + 7) & ~7; }
+inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+inline bool vec_rows(const void* p, int ld) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld % 8 == 0; }
+
+// A matrix of 16-bit values as TMA reads it.
+struct Matrix {
+    const void* p;
+    int64_t rows;
+    int cols, ld;
+};
+
+// Box of box_cols x box_rows; columns and rows beyond the matrix read as zero.
+bool make_map2(CUtensorMap* map, const Matrix& m, int dtype, int box_cols, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
+    cuuint64_t strides[1] = {(cuuint64_t)m.ld * 2};
+    cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    return fn(map, dtype == SAMA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+              const_cast<void*>(m.p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The tile of 128 rows (or columns, MN-major) that one CTA stages.
+bool operand_map(CUtensorMap* map, const Matrix& m, int dtype, bool mn_major, int rows = BM) {
+    return mn_major ? make_map2(map, m, dtype, 64, BK) : make_map2(map, m, dtype, BK, rows);
+}
+
+inline int blocks_of(int64_t x, int b) { return (int)((x + b - 1) / b); }
+
+template <typename T, int MODE, bool PAIR, bool A_MN, bool B_MN, int G>
+cudaError_t launch_ffn(sama_ctx* ctx, Params<G>& P, int kind, cudaStream_t st) {
+    auto* kernel = ffn_kernel<T, MODE, PAIR, A_MN, B_MN, G>;
+    const uint32_t bit = 1u << (4 * kind + (PAIR ? 2 : 0) + (std::is_same<T, __half>::value ? 1 : 0));
+    if (!(ctx->ffn_ready & bit)) {  // once per context: the opt-in to this much shared memory
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+        if (e != cudaSuccess) return e;
+        ctx->ffn_ready |= bit;
+    }
+    const int tm = PAIR ? 2 * BM : BM, tn = (PAIR ? 256 : 128) / (MODE == GATE_UP ? 2 : 1);
+    int items = 0;
+    for (int g = 0; g < G; ++g) {
+        Problem& q = P.p[g];
+        q.tiles_m = blocks_of(q.M, tm);
+        q.tiles_n = blocks_of(q.N, tn);
+        q.item0 = items;
+        items += q.tiles_m * q.tiles_n;
+    }
+    P.n_items = items;
+    P.group_m = 8;
+    P.status = &ctx->scalars->status;
+    const int max_units = PAIR ? ctx->ffn_pair_units : ctx->sm_count;
+    const int units = items < max_units ? items : max_units;
+    KernelScope scope(ctx, SAMA_K_FFN, kind, st);
+    return launch_clustered(PAIR ? 2 : 1, kernel, dim3(units * (PAIR ? 2 : 1)), dim3(THREADS), (size_t)SMEM, st, P);
+}
+
+// CTA pairs of the kernel that can be resident (asked once per context).
+cudaError_t find_pair_units(sama_ctx* ctx) {
+    auto* kernel = ffn_kernel<__nv_bfloat16, PLAIN, true, false, false, 1>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * (ctx->sm_count / 2));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if ((e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg)) != cudaSuccess) return e;
+    ctx->ffn_pair_units = clusters < ctx->sm_count / 2 ? clusters : ctx->sm_count / 2;
+    return ctx->ffn_pair_units > 0 ? cudaSuccess : cudaErrorLaunchOutOfResources;
+}
+
+// Pairs of CTAs where their tiles keep most of the machine busy, single CTAs otherwise.
+bool use_pairs(const sama_ctx* ctx, int64_t pair_tiles) { return pair_tiles * 4 >= (int64_t)ctx->ffn_pair_units * 3; }
+
+void set_output(Problem& q, int i, void* p, int ld, int cols) {
+    q.out[i] = p;
+    q.ldo[i] = ld;
+    q.cols[i] = cols;
+    if (vec_rows(p, ld) && cols % 8 == 0) q.vec_out |= 1 << i;
+}
+
+// What a call works on: operands as TMA can read them, copied to the workspace where they are not.
+template <typename T>
+struct Block {
+    sama_ctx* ctx;
+    const FfnShape& f;
+    uint8_t* ws;
+    cudaStream_t st;
+    int fp;               // leading dimension of the workspace's [tokens][f] matrices
+    cudaError_t err = cudaSuccess;
+
+    void* take(size_t elements) {
+        void* p = ws;
+        ws += up256(elements * 2);
+        return p;
+    }
+    Matrix readable(const void* p, int64_t rows, int cols) {
+        if (vec_rows(p, cols)) return {p, rows, cols, cols};
+        const int ld = up8(cols);
+        T* dst = static_cast<T*>(take((size_t)rows * ld));
+        int64_t blocks = (rows * (ld / 8) + 255) / 256;
+        if (blocks > 8 * ctx->sm_count) blocks = 8 * ctx->sm_count;
+        if (err == cudaSuccess) {
+            KernelScope scope(ctx, SAMA_K_FFN, -1, st);
+            err = launch_dependent(align_rows_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(p),
+                                   rows, cols, ld, dst);
+        }
+        return {dst, rows, cols, ld};
+    }
+    template <int MODE, bool A_MN, bool B_MN, int G>
+    void run(Params<G>& P, int kind, bool pair) {
+        if (err != cudaSuccess) return;
+        err = pair ? launch_ffn<T, MODE, true, A_MN, B_MN, G>(ctx, P, kind, st) : launch_ffn<T, MODE, false, A_MN, B_MN, G>(ctx, P, kind, st);
+    }
+    void check(bool ok) {
+        if (!ok && err == cudaSuccess) err = cudaErrorInvalidValue;
+    }
+
+    void forward(const void* x, const void* wg, const void* wu, const void* wd, void* y, void* gate, void* up) {
+        const int M = (int)f.n_tokens, d = f.d, n = f.f;
+        void* h = take((size_t)M * fp);
+        const Matrix mx = readable(x, M, d), mg = readable(wg, n, d), mu = readable(wu, n, d), md = readable(wd, d, n);
+        {
+            Params<1> P = {};
+            Problem& q = P.p[0];
+            const bool pair = use_pairs(ctx, (int64_t)blocks_of(M, 2 * BM) * blocks_of(n, 128));
+            check(operand_map(&q.a[0], mx, f.dtype, false) && operand_map(&q.b[0], mg, f.dtype, false, pair ? 128 : 64) &&
+                  operand_map(&q.b[1], mu, f.dtype, false, pair ? 128 : 64));
+            q.M = M;
+            q.N = n;
+            q.num_kb = q.kb_first = blocks_of(d, BK);
+            set_output(q, 0, gate, n, n);
+            set_output(q, 1, up, n, n);
+            set_output(q, 2, h, fp, fp);
+            P.act = f.act;
+            run<GATE_UP, false, false, 1>(P, 0, pair);
+        }
+        Params<1> P = {};
+        Problem& q = P.p[0];
+        check(operand_map(&q.a[0], {h, M, n, fp}, f.dtype, false) && operand_map(&q.b[0], md, f.dtype, false));
+        q.M = M;
+        q.N = d;
+        q.num_kb = q.kb_first = blocks_of(n, BK);
+        set_output(q, 0, y, d, d);
+        run<PLAIN, false, false, 1>(P, 1, use_pairs(ctx, (int64_t)blocks_of(M, 2 * BM) * blocks_of(d, 256)));
+    }
+
+    void backward(const void* x, const void* wg, const void* wu, const void* wd, const void* gate, const void* up,
+                  const void* dy, void* dx, void* dwg, void* dwu, void* dwd) {
+        const int M = (int)f.n_tokens, d = f.d, n = f.f;
+        void* dg = take((size_t)M * fp);
+        void* du = take((size_t)M * fp);
+        void* h = take((size_t)M * fp);
+        const Matrix my = readable(dy, M, d), md = readable(wd, d, n);
+        {
+            Params<1> P = {};
+            Problem& q = P.p[0];
+            check(operand_map(&q.a[0], my, f.dtype, false) && operand_map(&q.b[0], md, f.dtype, true));
+            q.M = M;
+            q.N = n;
+            q.num_kb = q.kb_first = blocks_of(d, BK);
+            void* outs[3] = {dg, du, h};
+            for (int i = 0; i < 3; ++i) set_output(q, i, outs[i], fp, fp);
+            q.in[0] = gate;
+            q.in[1] = up;
+            q.ldi = n;
+            q.vec_in = (vec_rows(gate, n) ? 1 : 0) | (vec_rows(up, n) ? 2 : 0);
+            P.act = f.act;
+            run<D_HIDDEN, false, true, 1>(P, 2, use_pairs(ctx, (int64_t)blocks_of(M, 2 * BM) * blocks_of(n, 256)));
+        }
+        const Matrix mdg = {dg, M, n, fp}, mdu = {du, M, n, fp}, mh = {h, M, n, fp};
+        if (dx) {
+            const Matrix mg = readable(wg, n, d), mu = readable(wu, n, d);
+            Params<1> P = {};
+            Problem& q = P.p[0];
+            check(operand_map(&q.a[0], mdg, f.dtype, false) && operand_map(&q.a[1], mdu, f.dtype, false) &&
+                  operand_map(&q.b[0], mg, f.dtype, true) && operand_map(&q.b[1], mu, f.dtype, true));
+            q.M = M;
+            q.N = d;
+            q.kb_first = blocks_of(n, BK);
+            q.num_kb = 2 * q.kb_first;
+            set_output(q, 0, dx, d, d);
+            run<PLAIN, false, true, 1>(P, 3, use_pairs(ctx, (int64_t)blocks_of(M, 2 * BM) * blocks_of(d, 256)));
+        }
+        if (!dwg && !dwu && !dwd) return;
+        const Matrix mx = (dwg || dwu) ? readable(x, M, d) : my;
+        Params<3> P = {};
+        struct { const Matrix* a; const Matrix* b; void* out; int rows, cols; } w[3] = {
+            {&mdg, &mx, dwg, n, d}, {&mdu, &mx, dwu, n, d}, {&my, &mh, dwd, d, n}};
+        int64_t tiles = 0;
+        for (int i = 0; i < 3; ++i) {
+            Problem& q = P.p[i];
+            check(operand_map(&q.a[0], *w[i].a, f.dtype, true) && operand_map(&q.b[0], *w[i].b, f.dtype, true));
+            q.M = w[i].out ? w[i].rows : 0;   // a gradient that is not wanted has no tiles
+            q.N = w[i].cols;
+            q.num_kb = q.kb_first = blocks_of(M, BK);
+            set_output(q, 0, w[i].out, w[i].cols, w[i].cols);
+            tiles += (int64_t)blocks_of(q.M, 2 * BM) * blocks_of(q.N, 256);
+        }
+        run<PLAIN, true, true, 3>(P, 4, use_pairs(ctx, tiles));
+    }
+};
+
+}  // namespace
+
+// `copies`: some operand starts at an odd address or has rows that do.
+size_t ffn_workspace(const FfnShape& f, bool grad, bool copies) {
+    const size_t M = (size_t)f.n_tokens, dp = up8(f.d), fp = up8(f.f);
+    size_t b = (grad ? 3 : 1) * up256(M * fp * 2);
+    if (copies) b += 2 * up256(M * dp * 2) + 2 * up256((size_t)f.f * dp * 2) + up256((size_t)f.d * fp * 2);
+    return b;
+}
+
+cudaError_t launch_ffn_forward(sama_ctx* ctx, const FfnShape& f, const void* x, const void* wg, const void* wu,
+                               const void* wd, void* y, void* gate, void* up, void* ws, cudaStream_t st) {
+    if (ctx->ffn_pair_units == 0) {
+        const cudaError_t e = find_pair_units(ctx);
+        if (e != cudaSuccess) return e;
+    }
+    if (f.dtype == SAMA_BF16) {
+        Block<__nv_bfloat16> b{ctx, f, static_cast<uint8_t*>(ws), st, up8(f.f)};
+        b.forward(x, wg, wu, wd, y, gate, up);
+        return b.err;
+    }
+    Block<__half> b{ctx, f, static_cast<uint8_t*>(ws), st, up8(f.f)};
+    b.forward(x, wg, wu, wd, y, gate, up);
+    return b.err;
+}
+
+cudaError_t launch_ffn_backward(sama_ctx* ctx, const FfnShape& f, const void* x, const void* wg, const void* wu,
+                                const void* wd, const void* gate, const void* up, const void* dy, void* dx, void* dwg,
+                                void* dwu, void* dwd, void* ws, cudaStream_t st) {
+    if (ctx->ffn_pair_units == 0) {
+        const cudaError_t e = find_pair_units(ctx);
+        if (e != cudaSuccess) return e;
+    }
+    if (f.dtype == SAMA_BF16) {
+        Block<__nv_bfloat16> b{ctx, f, static_cast<uint8_t*>(ws), st, up8(f.f)};
+        b.backward(x, wg, wu, wd, gate, up, dy, dx, dwg, dwu, dwd);
+        return b.err;
+    }
+    Block<__half> b{ctx, f, static_cast<uint8_t*>(ws), st, up8(f.f)};
+    b.backward(x, wg, wu, wd, gate, up, dy, dx, dwg, dwu, dwd);
+    return b.err;
+}
+
+}  // namespace sama

@@ -128,6 +128,8 @@ struct sama_ctx {
     size_t stage_bytes;
     void* op_ws;                   // device: workspace of the text-model operators (allocated on first use, grows)
     size_t op_ws_bytes;
+    uint32_t ffn_ready;            // kernels of gated_ffn.cu whose shared-memory size is set on this device
+    int ffn_pair_units;            // CTA pairs of them that can be resident (0: not yet asked)
     sama::Profiler* prof;          // host
 };
 
@@ -330,5 +332,17 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
 // clip_grads.cu : global gradient norm and clipping
 cudaError_t launch_clip_grads(sama_ctx* ctx, const sama_tensor_t* t, int n, float max_norm, float* norm_out,
                               cudaStream_t st);
+
+// gated_ffn.cu : gated feed-forward block
+struct FfnShape {
+    int64_t n_tokens;
+    int32_t d, f, dtype, act;
+};
+size_t ffn_workspace(const FfnShape& f, bool grad, bool copies);
+cudaError_t launch_ffn_forward(sama_ctx* ctx, const FfnShape& f, const void* x, const void* wg, const void* wu,
+                               const void* wd, void* y, void* gate, void* up, void* ws, cudaStream_t st);
+cudaError_t launch_ffn_backward(sama_ctx* ctx, const FfnShape& f, const void* x, const void* wg, const void* wu,
+                                const void* wd, const void* gate, const void* up, const void* dy, void* dx, void* dwg,
+                                void* dwu, void* dwd, void* ws, cudaStream_t st);
 
 }  // namespace sama

@@ -28,6 +28,32 @@ bool embed_sizes_ok(int64_t n_tokens, int64_t vocab, int32_t d) {
     return n_tokens >= 0 && n_tokens <= kMaxTokens && vocab >= 1 && vocab < 0x7fffffff && d >= 1;
 }
 
+struct Span {
+    const void* p;
+    size_t bytes;
+};
+
+// Checks shared by the block's two directions: `ins` are all required, `outs` may be NULL; no output overlaps anything.
+int check_ffn(const FfnShape& s, const Span* ins, int n_in, const Span* outs, int n_out, bool* copies) {
+    if (s.n_tokens < 0 || s.n_tokens > ((int64_t)1 << 24) || s.d < 1 || s.d > (1 << 20) || s.f < 1 || s.f > (1 << 20))
+        return SAMA_ERR_SIZE;
+    if ((s.dtype != SAMA_BF16 && s.dtype != SAMA_F16) || s.act < SAMA_ACT_SILU || s.act > SAMA_ACT_RELU) return SAMA_ERR_PARAM;
+    *copies = s.d % 8 != 0 || s.f % 8 != 0;
+    for (int i = 0; i < n_in; ++i) {
+        if (!ins[i].p && ins[i].bytes > 0) return SAMA_ERR_NULL;
+        if (!aligned(ins[i].p, 2)) return SAMA_ERR_ALIGN;
+        if (!aligned(ins[i].p, 16)) *copies = true;
+    }
+    for (int i = 0; i < n_out; ++i) {
+        if (!aligned(outs[i].p, 2)) return SAMA_ERR_ALIGN;
+        for (int j = 0; j < n_in; ++j)
+            if (overlaps(outs[i].p, outs[i].bytes, ins[j].p, ins[j].bytes)) return SAMA_ERR_OVERLAP;
+        for (int j = 0; j < i; ++j)
+            if (overlaps(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes)) return SAMA_ERR_OVERLAP;
+    }
+    return SAMA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -99,6 +125,52 @@ int sama_clip_grads(sama_ctx* ctx, const sama_tensor_t* tensors, int32_t n_tenso
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SAMA_ERR_CUDA;
     SAMA_CUDA(ctx, launch_clip_grads(ctx, tensors, n_tensors, max_norm, norm_out, (cudaStream_t)stream));
+    return SAMA_OK;
+}
+
+int sama_gated_ffn(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tokens, int32_t d, int32_t f, const void* x,
+                   const void* w_gate, const void* w_up, const void* w_down, void* y, void* gate_out, void* up_out,
+                   void* stream) {
+    if (!ctx) return SAMA_ERR_NULL;
+    const FfnShape s{n_tokens, d, f, dtype, act};
+    const size_t t = (size_t)n_tokens * d * 2, h = (size_t)n_tokens * f * 2, w = (size_t)d * f * 2;
+    const Span ins[4] = {{x, t}, {w_gate, w}, {w_up, w}, {w_down, w}}, outs[3] = {{y, t}, {gate_out, h}, {up_out, h}};
+    bool copies = false;
+    int rc = check_ffn(s, ins, 4, outs, 3, &copies);
+    if (rc != SAMA_OK) return rc;
+    if (n_tokens == 0) return SAMA_OK;
+    if (!y || (gate_out == nullptr) != (up_out == nullptr)) return SAMA_ERR_NULL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SAMA_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = need_workspace(ctx, ffn_workspace(s, false, copies), st)) != SAMA_OK) return rc;
+    SAMA_CUDA(ctx, launch_ffn_forward(ctx, s, x, w_gate, w_up, w_down, y, gate_out, up_out, ctx->op_ws, st));
+    return SAMA_OK;
+}
+
+int sama_gated_ffn_grad(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tokens, int32_t d, int32_t f, const void* x,
+                        const void* w_gate, const void* w_up, const void* w_down, const void* gate, const void* up,
+                        const void* dy, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* stream) {
+    if (!ctx) return SAMA_ERR_NULL;
+    const FfnShape s{n_tokens, d, f, dtype, act};
+    const size_t t = (size_t)n_tokens * d * 2, h = (size_t)n_tokens * f * 2, w = (size_t)d * f * 2;
+    const Span ins[7] = {{x, t}, {w_gate, w}, {w_up, w}, {w_down, w}, {gate, h}, {up, h}, {dy, t}};
+    const Span outs[4] = {{dx, t}, {dw_gate, w}, {dw_up, w}, {dw_down, w}};
+    bool copies = false;
+    int rc = check_ffn(s, ins, 7, outs, 4, &copies);
+    if (rc != SAMA_OK) return rc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SAMA_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (n_tokens == 0) {
+        void* dw[3] = {dw_gate, dw_up, dw_down};
+        for (void* p : dw)
+            if (p) SAMA_CUDA(ctx, cudaMemsetAsync(p, 0, w, st));
+        return SAMA_OK;
+    }
+    if ((rc = need_workspace(ctx, ffn_workspace(s, true, copies), st)) != SAMA_OK) return rc;
+    SAMA_CUDA(ctx, launch_ffn_backward(ctx, s, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down,
+                                       ctx->op_ws, st));
     return SAMA_OK;
 }
 
