@@ -8,15 +8,15 @@
 // makes up most of a text costs no more than any other; and a run is always added up in token order, piece by piece,
 // so the result does not depend on scheduling (there is no floating-point atomic).
 //
-// Three launches:
-//   embed_sort   : one cluster of 8 CTAs sorts (id, position) by 8-bit digits, least significant first.  Counts are
-//                  exchanged through distributed shared memory, so the passes need only cluster barriers.  Ids outside
-//                  the vocabulary and the skipped id become the key `vocab`, which sorts behind all others.  It also
-//                  leaves one bit per row of dE that has a token.
-//   embed_reduce : workers of one CTA's threads each add up `piece` consecutive entries of the list.  A run that
-//                  lies inside a piece is written out; the parts of runs that cross pieces go to the workspace in fp32.
-//                  Further blocks write zeros to the rows without a token.
-//   embed_join   : adds the parts of the runs that cross pieces, in order.
+// Two launches:
+//   embed_sort   : one cluster of 8 CTAs sorts (id, position) by digits of up to 10 bits, least significant first.
+//                  Counts are exchanged through distributed shared memory, so the passes need only cluster barriers.
+//                  Ids outside the vocabulary and the skipped id become the key `vocab`, which sorts behind all others.
+//                  Meanwhile the other CTAs write zeros to the rows of dE that have no token: each takes a range of
+//                  rows and finds out by reading all ids.
+//   embed_reduce : a warp adds up one piece of the list for 32 threads' columns.  A run that lies inside a piece is
+//                  written out; the parts of a run that crosses pieces go to the workspace in fp32, and the warp that
+//                  finishes the last part adds them all up, in the order of the list.
 #include "num_types.h"
 #include "sama_internal.h"
 
@@ -28,39 +28,51 @@ namespace {
 
 constexpr int kEmbedThreads = 256;
 
-// VE consecutive columns per thread; `tpr` threads (a power of two) share a row.
-template <typename T, int VE>
+// VE consecutive columns per thread; `tpr` threads (a power of two) share a row, a thread takes ROWS of them at a time.
+template <typename T, int VE, int ROWS>
 __global__ void __launch_bounds__(kEmbedThreads)
 embed_kernel(int64_t n_tokens, int64_t vocab, int d, int tpr, const T* __restrict__ table,
              const int32_t* __restrict__ ids, float scale, T* __restrict__ out, int32_t* status) {
     pdl_trigger();
     pdl_wait();
     const int rows = kEmbedThreads / tpr, tx = threadIdx.x & (tpr - 1);
-    const int64_t t = (int64_t)blockIdx.x * rows + threadIdx.x / tpr;
-    if (t >= n_tokens) return;
-    const int32_t id = ids[t];
-    const bool good = id >= 0 && id < vocab;
-    if (!good && tx == 0) atomicOr(status, (int)SAMA_DEV_BAD_INDEX);
-    const T* src = table + (good ? (int64_t)id : 0) * d;
-    T* dst = out + t * d;
-    for (int c = tx * VE; c < d; c += tpr * VE) {
-        float v[VE];
-        load_n<T, VE, true>(src + c, v);  // rows of frequent tokens are read again and again
+    const int64_t t0 = (int64_t)blockIdx.x * rows * ROWS + threadIdx.x / tpr;
+    int32_t id[ROWS];
+    bool good[ROWS];
 #pragma unroll
-        for (int i = 0; i < VE; ++i) v[i] = good ? v[i] * scale : 0.f;
-        store_n<T, VE>(dst + c, v);
+    for (int r = 0; r < ROWS; ++r) {
+        const int64_t t = t0 + (int64_t)r * rows;
+        id[r] = t < n_tokens ? ids[t] : 0;
+        good[r] = id[r] >= 0 && id[r] < vocab;
+        if (!good[r] && tx == 0) atomicOr(status, (int)SAMA_DEV_BAD_INDEX);
+    }
+    for (int c = tx * VE; c < d; c += tpr * VE) {
+        float v[ROWS][VE];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)  // (rows of frequent tokens are read again and again)
+            load_n<T, VE, true>(table + (good[r] ? (int64_t)id[r] : 0) * d + c, v[r]);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const int64_t t = t0 + (int64_t)r * rows;
+            if (t >= n_tokens) continue;
+#pragma unroll
+            for (int i = 0; i < VE; ++i) v[r][i] = good[r] ? v[r][i] * scale : 0.f;
+            store_n<T, VE>(out + t * d + c, v[r]);
+        }
     }
 }
 
 // ------------------------------------------------------------------ sort
 
-constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256;
+constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBins = 1024;
+constexpr int kFillRows = 1 << 19;  // rows whose presence one CTA tracks at a time
 
 struct SortSmem {
-    uint32_t hist[kSortWarps][kDigits];  // counts, then next output positions, of every warp's share
-    uint32_t total[kDigits];             // this CTA's counts (read by the other CTAs)
-    uint32_t warp_sum[8];
+    uint32_t hist[kSortWarps][kMaxBins];  // counts, then next output positions, of every warp's share
+    uint32_t total[kMaxBins];             // this CTA's counts (read by the other CTAs)
+    uint32_t warp_sum[kSortWarps];
 };
+static_assert(sizeof(SortSmem) >= kFillRows / 8, "the map of present rows takes the same shared memory");
 
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -73,47 +85,105 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(const uint32_t* p, uint32_t c
     return v;
 }
 
-// ids -> `passes` stable counting passes over (key, position), buf[0] and buf[1] in turn (pass p writes buf[p & 1]).
-// present: bit v of the row map (cleared here), or null.
+struct SortArgs {
+    const int32_t* ids;
+    int2* buf[2];       // lists of (key, position); pass p writes buf[p & 1]
+    int2* span;         // [vocab]: begin and end of each present row's run in the sorted list
+    int* arrived;       // [parts]: zeroed for embed_reduce
+    uint8_t* grad;      // rows to be zeroed where no token is, or null
+    int64_t row_bytes;
+    int n, parts, passes, bits;
+    int32_t vocab, skip_id;
+    int32_t* status;
+};
+
+// Zeros to this CTA's share of the rows that have no token.
+__device__ void fill_absent_rows(const SortArgs& a, uint32_t* present, int cta, int n_ctas) {
+    const int64_t per = (a.vocab + n_ctas - 1) / n_ctas;
+    const int64_t first = cta * per, stop = min((int64_t)a.vocab, first + per);
+    const int64_t low = a.row_bytes | (int64_t)reinterpret_cast<uintptr_t>(a.grad);   // alignment of every row
+    for (int64_t r0 = first; r0 < stop; r0 += kFillRows) {
+        const int rows = (int)min((int64_t)kFillRows, stop - r0);
+        for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) present[i] = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.n; i += 4 * kSortThreads) {
+            int32_t id[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) id[u] = i + u * kSortThreads < a.n ? a.ids[i + u * kSortThreads] : -1;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int64_t r = (int64_t)id[u] - r0;
+                if (r >= 0 && r < rows && id[u] != a.skip_id) {
+                    uint32_t* w = present + (r >> 5);
+                    const uint32_t bit = 1u << (r & 31);
+                    if (!(*w & bit)) atomicOr(w, bit);
+                }
+            }
+        }
+        __syncthreads();
+        for (int r = threadIdx.x >> 5; r < rows; r += kSortWarps) {
+            if (present[r >> 5] >> (r & 31) & 1u) continue;
+            uint8_t* g = a.grad + (r0 + r) * a.row_bytes;
+            if ((low & 15) == 0) {
+                for (int64_t b = (threadIdx.x & 31) * 16; b < a.row_bytes; b += 512)
+                    *reinterpret_cast<uint4*>(g + b) = make_uint4(0, 0, 0, 0);
+            } else if ((low & 3) == 0) {
+                for (int64_t b = (threadIdx.x & 31) * 4; b < a.row_bytes; b += 128) *reinterpret_cast<uint32_t*>(g + b) = 0;
+            } else {
+                for (int64_t b = (threadIdx.x & 31) * 2; b < a.row_bytes; b += 64) *reinterpret_cast<uint16_t*>(g + b) = 0;
+            }
+        }
+        __syncthreads();
+    }
+}
+
 __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads)
-embed_sort_kernel(int n, int32_t vocab, int32_t skip_id, int passes, const int32_t* __restrict__ ids, int2* buf0,
-                  int2* buf1, uint32_t* present, int32_t* status) {
+embed_sort_kernel(const __grid_constant__ SortArgs a) {
     extern __shared__ uint8_t sort_raw[];
     SortSmem& sm = *reinterpret_cast<SortSmem*>(sort_raw);
+    pdl_trigger();
+    pdl_wait();
+    if (blockIdx.x >= kSortCtas) {
+        fill_absent_rows(a, reinterpret_cast<uint32_t*>(sort_raw), blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
+        return;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = blockIdx.x;
+    const int n = a.n, bins = 1 << a.bits;
     const int per_cta = ((n + kSortCtas - 1) / kSortCtas + 31) & ~31;
     const int per_warp = ((per_cta + kSortWarps - 1) / kSortWarps + 31) & ~31;
     const int64_t cta_end = min((int64_t)n, (int64_t)(rank + 1) * per_cta);
     const int64_t begin = (int64_t)rank * per_cta + (int64_t)warp * per_warp;
     const int64_t end = min(cta_end, begin + per_warp);
-    pdl_trigger();
-    pdl_wait();
-    if (present)
-        for (int64_t w = (int64_t)rank * kSortThreads + threadIdx.x; w < ((int64_t)vocab + 31) / 32; w += kSortCtas * kSortThreads)
-            present[w] = 0;
-    for (int p = 0; p < passes; ++p) {
-        const int2* src = (p & 1) ? buf0 : buf1;
-        int2* dst = (p & 1) ? buf1 : buf0;
+    constexpr int U = 4;  // elements in flight per thread
+    for (int i = (int)rank * kSortThreads + threadIdx.x; i < a.parts; i += kSortCtas * kSortThreads) a.arrived[i] = 0;
+    for (int p = 0; p < a.passes; ++p) {
+        const int2* src = a.buf[(p & 1) ^ 1];
+        int2* dst = a.buf[p & 1];
+        const int shift = a.bits * p;
         auto fetch = [&](int64_t i) -> int2 {
+            if (i >= end) return make_int2(-1, 0);   // (beyond this warp's share)
             if (p > 0) return __ldcg(src + i);
-            const int32_t id = ids[i];
-            const bool good = id >= 0 && id < vocab;
-            if (!good) atomicOr(status, (int)SAMA_DEV_BAD_INDEX);
-            return make_int2(good && id != skip_id ? id : vocab, (int)i);
+            const int32_t id = a.ids[i];
+            const bool good = id >= 0 && id < a.vocab;
+            if (!good) atomicOr(a.status, (int)SAMA_DEV_BAD_INDEX);
+            return make_int2(good && id != a.skip_id ? id : a.vocab, (int)i);
         };
-        for (int b = lane; b < kDigits; b += 32) sm.hist[warp][b] = 0;
+        for (int b = lane; b < bins; b += 32) sm.hist[warp][b] = 0;
         __syncwarp();
-        for (int64_t i = begin + lane; i - lane < end; i += 32) {
-            const bool on = i < end;
-            const uint32_t digit = on ? ((uint32_t)fetch(i).x >> (8 * p)) & 255u : 256u;
-            const uint32_t same = __match_any_sync(0xffffffffu, digit);
-            if (on && lane == __ffs(same) - 1) sm.hist[warp][digit] += __popc(same);
-            __syncwarp();
+        for (int64_t i = begin + lane; i - lane < end; i += 32 * U) {
+            int2 e[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) e[u] = fetch(i + 32 * u);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (e[u].x >= 0) atomicAdd(&sm.hist[warp][((uint32_t)e[u].x >> shift) & (bins - 1)], 1u);
         }
         __syncthreads();
+        // thread b owns bin b
         uint32_t mine = 0;
-        if (threadIdx.x < kDigits) {
+        if (threadIdx.x < bins) {
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w) {
                 const uint32_t c = sm.hist[w][threadIdx.x];
                 sm.hist[w][threadIdx.x] = mine;
@@ -122,51 +192,59 @@ embed_sort_kernel(int n, int32_t vocab, int32_t skip_id, int passes, const int32
             sm.total[threadIdx.x] = mine;
         }
         cluster_barrier();
-        uint32_t before = 0, all = 0, incl = 0;
-        if (threadIdx.x < kDigits) {
-            for (uint32_t c = 0; c < kSortCtas; ++c) {
-                const uint32_t v = ld_cluster_u32(&sm.total[threadIdx.x], c);
-                if (c < rank) before += v;
-                all += v;
-            }
-            incl = all;
+        uint32_t before = 0, all = 0;
+        if (threadIdx.x < bins) {
+            uint32_t v[kSortCtas];
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += v;
+            for (uint32_t c = 0; c < kSortCtas; ++c) v[c] = ld_cluster_u32(&sm.total[threadIdx.x], c);
+#pragma unroll
+            for (uint32_t c = 0; c < kSortCtas; ++c) {
+                if (c < rank) before += v[c];
+                all += v[c];
             }
-            if (lane == 31) sm.warp_sum[warp] = incl;
         }
+        uint32_t incl = all;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) sm.warp_sum[warp] = incl;
         __syncthreads();
-        if (threadIdx.x < kDigits) {
+        if (threadIdx.x < bins) {
             uint32_t base = incl - all + before;
             for (int w = 0; w < warp; ++w) base += sm.warp_sum[w];
+#pragma unroll 8
             for (int w = 0; w < kSortWarps; ++w) sm.hist[w][threadIdx.x] += base;
         }
         __syncthreads();
-        for (int64_t i = begin + lane; i - lane < end; i += 32) {
-            const bool on = i < end;
-            int2 e = make_int2(0, 0);
-            if (on) e = fetch(i);
-            const uint32_t digit = on ? ((uint32_t)e.x >> (8 * p)) & 255u : 256u;
-            const uint32_t same = __match_any_sync(0xffffffffu, digit);
-            uint32_t at = 0;
-            if (on) at = sm.hist[warp][digit] + __popc(same & ((1u << lane) - 1u));
-            __syncwarp();
-            if (on) {
-                dst[at] = e;
-                if (lane == __ffs(same) - 1) sm.hist[warp][digit] += __popc(same);
+        for (int64_t i = begin + lane; i - lane < end; i += 32 * U) {
+            int2 e[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) e[u] = fetch(i + 32 * u);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool on = e[u].x >= 0;
+                const uint32_t digit = on ? ((uint32_t)e[u].x >> shift) & (bins - 1) : 0xffffffffu;
+                const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                uint32_t at = 0;
+                if (on) at = sm.hist[warp][digit] + __popc(same & ((1u << lane) - 1u));
+                __syncwarp();
+                if (on) {
+                    dst[at] = e[u];
+                    if (lane == __ffs(same) - 1) sm.hist[warp][digit] += __popc(same);
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
         cluster_barrier();  // the pass is complete: every CTA may read all of dst, and total may be rewritten
     }
-    if (present) {
-        const int2* fin = ((passes - 1) & 1) ? buf1 : buf0;
-        for (int64_t i = begin + lane; i < end; i += 32) {
-            const int32_t key = __ldcg(fin + i).x;
-            if (key < vocab && (i == 0 || __ldcg(fin + i - 1).x != key)) atomicOr(present + (key >> 5), 1u << (key & 31));
-        }
+    const int2* list = a.buf[(a.passes - 1) & 1];
+    for (int64_t i = begin + lane; i < end; i += 32) {
+        const int32_t key = __ldcg(list + i).x;
+        if (key >= a.vocab) continue;
+        if (i == 0 || __ldcg(list + i - 1).x != key) a.span[key].x = (int)i;
+        if (i == n - 1 || __ldcg(list + i + 1).x != key) a.span[key].y = (int)i + 1;
     }
 }
 
@@ -174,13 +252,14 @@ embed_sort_kernel(int n, int32_t vocab, int32_t skip_id, int passes, const int32
 
 struct ReduceArgs {
     const int2* list;         // sorted (id, position)
-    const uint32_t* present;  // row map
+    const int2* span;         // each present row's run
     const void* dout;
     void* grad;
-    float* head;              // [pieces][d]: the part of a run that began in an earlier piece
+    float* head;              // [pieces][d]: the part, in this piece, of a run that began in an earlier one
     float* tail;              // [pieces][d]: the first part of a run that goes on in the next piece
+    int* arrived;             // [pieces][slabs], by the piece a run begins in: parts that are stored
     int n, vocab, d;
-    int piece, pieces, tpr, reduce_blocks, fill_blocks;
+    int piece, pieces, slabs;
     int accumulate;
     float scale;
 };
@@ -200,102 +279,124 @@ __device__ __forceinline__ void put_row(const ReduceArgs& a, int row, int c, con
     store_n<TG, VE>(g, v);
 }
 
+// The thread's VE values as they lie in memory: 16 bytes, or one value.
+template <typename T, int VE> struct Raw {
+    uint4 r;
+    __device__ __forceinline__ void load(const T* p) { r = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void add_to(float* acc) const {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 4) {
+                acc[j] += __uint_as_float(w[j]);
+            } else {
+                const float2 f = unpack2<T>(w[j]);
+                acc[2 * j] += f.x;
+                acc[2 * j + 1] += f.y;
+            }
+        }
+    }
+};
+template <typename T> struct Raw<T, 1> {
+    T r;
+    __device__ __forceinline__ void load(const T* p) { r = *p; }
+    __device__ __forceinline__ void add_to(float* acc) const { acc[0] += to_float(r); }
+};
+
+// VE fp32 values that another warp of this launch has stored.
+template <int VE>
+__device__ __forceinline__ void load_part(const float* p, float* v) {
+    if constexpr (VE == 1) {
+        v[0] = __ldcg(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VE / 4; ++i) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(p) + i);
+            v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+        }
+    }
+}
+
+// One warp: piece k of the list, columns [32 VE slab, 32 VE (slab + 1)).
 template <typename T, typename TG, int VE>
 __global__ void __launch_bounds__(kEmbedThreads)
 embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int U = 4;  // rows in flight per thread
-    const T* dout = static_cast<const T*>(a.dout);
-    if ((int)blockIdx.x >= a.reduce_blocks) {
-        // rows without a token: one warp per word of the row map
-        const int warps = kEmbedThreads / 32, lane = threadIdx.x & 31;
-        const int words = (a.vocab + 31) / 32;
-        float z[VE];
-#pragma unroll
-        for (int i = 0; i < VE; ++i) z[i] = 0.f;
-        for (int w = ((int)blockIdx.x - a.reduce_blocks) * warps + (threadIdx.x >> 5); w < words; w += a.fill_blocks * warps) {
-            uint32_t absent = ~a.present[w];
-            if (w == words - 1 && (a.vocab & 31)) absent &= (1u << (a.vocab & 31)) - 1u;
-            while (absent) {
-                const int r = __ffs(absent) - 1;
-                absent &= absent - 1;
-                TG* g = static_cast<TG*>(a.grad) + ((int64_t)w * 32 + r) * a.d;
-                for (int c = lane * VE; c < a.d; c += 32 * VE) store_n<TG, VE>(g + c, z);
-            }
-        }
-        return;
-    }
-    const int tx = threadIdx.x & (a.tpr - 1);
-    const int k = blockIdx.x * (kEmbedThreads / a.tpr) + threadIdx.x / a.tpr;
+    constexpr int U = 8;  // rows in flight per thread
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5);
+    const int k = (int)(unit / a.slabs), slab = (int)(unit - (int64_t)k * a.slabs);
     if (k >= a.pieces) return;
     const int i0 = k * a.piece, i1 = min(a.n, i0 + a.piece);
-    const int first = a.list[i0].x;
-    const bool open_head = i0 > 0 && a.list[i0 - 1].x == first;
-    for (int c = tx * VE; c < a.d; c += a.tpr * VE) {
-        int key = first;
-        bool from_head = open_head;
-        float acc[VE];
+    const int c = (slab * 32 + lane) * VE;
+    const bool on = c < a.d;   // (the other lanes of the last slab go along for the warp's sake)
+    const T* dout = static_cast<const T*>(a.dout) + (on ? c : 0);
+    int key = a.list[i0].x;
+    bool open_head = i0 > 0 && a.list[i0 - 1].x == key;
+    float acc[VE];
 #pragma unroll
-        for (int i = 0; i < VE; ++i) acc[i] = 0.f;
-        for (int i = i0; i < i1 && key < a.vocab; i += U) {
-            int2 e[U];
-            float v[U][VE];
+    for (int j = 0; j < VE; ++j) acc[j] = 0.f;
+
+    // The current run has no more entries in this piece.
+    auto finish = [&](bool goes_on) {
+        if (!open_head && !goes_on) {
+            if (on) put_row<TG, VE>(a, key, c, acc);
+            return;
+        }
+        if (on) store_n<float, VE>((open_head ? a.head : a.tail) + (int64_t)k * a.d + c, acc);
+        const int2 run = a.span[key];
+        const int k0 = run.x / a.piece, k1 = (run.y - 1) / a.piece;
+        __threadfence();
+        __syncwarp();
+        int before = 0;
+        if (lane == 0) before = atomicAdd(a.arrived + (int64_t)k0 * a.slabs + slab, 1);
+        before = __shfl_sync(0xffffffffu, before, 0);
+        if (before != k1 - k0) return;
+        __threadfence();   // all parts are in place: add them up
+        if (!on) return;
+        float sum[VE], v[4][VE];
+        load_part<VE>(a.tail + (int64_t)k0 * a.d + c, sum);
+        for (int j = k0 + 1; j <= k1; j += 4) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (j + u <= k1) load_part<VE>(a.head + (int64_t)(j + u) * a.d + c, v[u]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (j + u <= k1)
+#pragma unroll
+                    for (int q = 0; q < VE; ++q) sum[q] += v[u][q];
+        }
+        put_row<TG, VE>(a, key, c, sum);
+    };
+
+    for (int ib = i0; ib < i1 && key < a.vocab; ib += 32) {
+        const int2 mine = ib + lane < i1 ? a.list[ib + lane] : make_int2(a.vocab, 0);   // 32 entries, one per lane
+        const int count = min(32, i1 - ib);
+        for (int b = 0; b < count && key < a.vocab; b += U) {
+            Raw<T, VE> v[U];
+            int id[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                e[u] = i + u < i1 ? a.list[i + u] : make_int2(a.vocab, 0);
-                if (e[u].x < a.vocab) load_n<T, VE>(dout + (int64_t)e[u].y * a.d + c, v[u]);
+                id[u] = __shfl_sync(0xffffffffu, mine.x, b + u);
+                const int pos = __shfl_sync(0xffffffffu, mine.y, b + u);
+                if (id[u] < a.vocab) v[u].load(dout + (int64_t)pos * a.d);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (i + u >= i1) break;
-                if (e[u].x != key) {
-                    if (from_head) store_n<float, VE>(a.head + (int64_t)k * a.d + c, acc);
-                    else put_row<TG, VE>(a, key, c, acc);
-                    from_head = false;
-                    key = e[u].x;
+                if (b + u >= count || key >= a.vocab) continue;
+                if (id[u] != key) {
+                    finish(false);
+                    open_head = false;
+                    key = id[u];
 #pragma unroll
                     for (int j = 0; j < VE; ++j) acc[j] = 0.f;
                 }
-                if (key >= a.vocab) break;
-#pragma unroll
-                for (int j = 0; j < VE; ++j) acc[j] += v[u][j];
+                if (key < a.vocab) v[u].add_to(acc);
             }
         }
-        if (key < a.vocab) {
-            if (from_head) store_n<float, VE>(a.head + (int64_t)k * a.d + c, acc);
-            else if (i1 < a.n && a.list[i1].x == key) store_n<float, VE>(a.tail + (int64_t)k * a.d + c, acc);
-            else put_row<TG, VE>(a, key, c, acc);
-        }
     }
-}
-
-// One worker per piece in which a run begins that does not end there.
-template <typename TG, int VE>
-__global__ void __launch_bounds__(kEmbedThreads)
-embed_join_kernel(const __grid_constant__ ReduceArgs a) {
-    pdl_trigger();
-    pdl_wait();
-    const int tx = threadIdx.x & (a.tpr - 1);
-    const int k = blockIdx.x * (kEmbedThreads / a.tpr) + threadIdx.x / a.tpr;
-    if (k >= a.pieces - 1) return;
-    const int i1 = (k + 1) * a.piece;
-    const int key = a.list[i1 - 1].x;
-    if (key >= a.vocab || a.list[i1].x != key) return;
-    const int i0 = k * a.piece;
-    if (i0 > 0 && a.list[i0].x == key && a.list[i0 - 1].x == key) return;  // began earlier
-    int last = k + 1;                                                       // the piece the run ends in
-    while ((last + 1) * (int64_t)a.piece < a.n && a.list[(last + 1) * a.piece].x == key) ++last;
-    for (int c = tx * VE; c < a.d; c += a.tpr * VE) {
-        float acc[VE], v[VE];
-        load_n<float, VE>(a.tail + (int64_t)k * a.d + c, acc);
-        for (int j = k + 1; j <= last; ++j) {
-            load_n<float, VE>(a.head + (int64_t)j * a.d + c, v);
-#pragma unroll
-            for (int i = 0; i < VE; ++i) acc[i] += v[i];
-        }
-        put_row<TG, VE>(a, key, c, acc);
-    }
+    if (key < a.vocab) finish(i1 < a.n && a.list[i1].x == key);
 }
 
 int threads_per_row(int d, int ve) {
@@ -310,35 +411,54 @@ cudaError_t embed_typed(sama_ctx* ctx, int64_t n, int64_t vocab, int d, const vo
     constexpr int VE = 16 / sizeof(T);
     const bool vec = d % VE == 0 && ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
     const int tpr = threads_per_row(d, vec ? VE : 1), rows = kEmbedThreads / tpr;
-    const dim3 grid((unsigned)((n + rows - 1) / rows));
+    // four rows per thread once that still leaves every SM its full number of threads
+    const bool deep = n * tpr >= (int64_t)ctx->sm_count * 2048 * 4;
+    const int64_t per_block = (int64_t)rows * (deep ? 4 : 1);
     KernelScope scope(ctx, SAMA_K_EMBED, -1, st);
-    auto* kernel = vec ? embed_kernel<T, VE> : embed_kernel<T, 1>;
-    return launch_dependent(kernel, grid, dim3(kEmbedThreads), 0, st, n, vocab, d, tpr, static_cast<const T*>(table), ids,
-                            scale, static_cast<T*>(out), &ctx->scalars->status);
+    auto* kernel = vec ? (deep ? embed_kernel<T, VE, 4> : embed_kernel<T, VE, 1>) : (deep ? embed_kernel<T, 1, 4> : embed_kernel<T, 1, 1>);
+    return launch_dependent(kernel, dim3((unsigned)((n + per_block - 1) / per_block)), dim3(kEmbedThreads), 0, st, n, vocab,
+                            d, tpr, static_cast<const T*>(table), ids, scale, static_cast<T*>(out), &ctx->scalars->status);
 }
 
-constexpr int kPiece = 32;
-
-template <typename T, typename TG>
-cudaError_t reduce_typed(sama_ctx* ctx, ReduceArgs a, cudaStream_t st) {
-    constexpr int VE = 16 / (sizeof(T) < sizeof(TG) ? sizeof(T) : sizeof(TG));
-    const bool vec = a.d % VE == 0 && ((reinterpret_cast<uintptr_t>(a.dout) | reinterpret_cast<uintptr_t>(a.grad)) & 15u) == 0;
-    a.tpr = threads_per_row(a.d, vec ? VE : 1);
-    const int workers = kEmbedThreads / a.tpr;
-    a.reduce_blocks = (a.pieces + workers - 1) / workers;
-    a.fill_blocks = a.accumulate ? 0 : 2 * ctx->sm_count;
-    {
-        KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
-        auto* kernel = vec ? embed_reduce_kernel<T, TG, VE> : embed_reduce_kernel<T, TG, 1>;
-        const cudaError_t e = launch_dependent(kernel, dim3(a.reduce_blocks + a.fill_blocks), dim3(kEmbedThreads), 0, st, a);
-        if (e != cudaSuccess) return e;
-    }
-    KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
-    auto* kernel = vec ? embed_join_kernel<TG, VE> : embed_join_kernel<TG, 1>;
-    return launch_dependent(kernel, dim3(a.reduce_blocks), dim3(kEmbedThreads), 0, st, a);
+// Entries per piece: as many as still give every SM 16 warps, 8 to 64.
+int piece_of(const sama_ctx* ctx, int64_t n, int slabs) {
+    int piece = 64;
+    while (piece > 8 && (n + piece - 1) / piece * slabs < (int64_t)ctx->sm_count * 16) piece /= 2;
+    return piece;
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct GradPlan {
+    bool vec;
+    int ve, slabs, piece, pieces;
+    size_t list, span, arrived, parts;  // bytes
+    size_t total() const { return 2 * list + span + arrived + 2 * parts; }
+};
+GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout, int grad_dtype,
+                   const void* grad) {
+    GradPlan g;
+    const int ve = 16 / (int)dtype_size(dtype);
+    g.vec = d % ve == 0 && ((reinterpret_cast<uintptr_t>(dout) | reinterpret_cast<uintptr_t>(grad)) & 15u) == 0;
+    g.ve = g.vec ? ve : 1;
+    g.slabs = (d + 32 * g.ve - 1) / (32 * g.ve);
+    g.piece = piece_of(ctx, n, g.slabs);
+    g.pieces = (int)((n + g.piece - 1) / g.piece);
+    g.list = up256(sizeof(int2) * (size_t)n);
+    g.span = up256(sizeof(int2) * (size_t)vocab);
+    g.arrived = up256(sizeof(int) * (size_t)g.pieces * g.slabs);
+    g.parts = up256(sizeof(float) * (size_t)g.pieces * d);
+    return g;
+}
+
+template <typename T, typename TG>
+cudaError_t reduce_typed(sama_ctx* ctx, const ReduceArgs& a, bool vec, cudaStream_t st) {
+    constexpr int VE = 16 / sizeof(T);
+    KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
+    auto* kernel = vec ? embed_reduce_kernel<T, TG, VE> : embed_reduce_kernel<T, TG, 1>;
+    const int64_t units = (int64_t)a.pieces * a.slabs, per = kEmbedThreads / 32;
+    return launch_dependent(kernel, dim3((unsigned)((units + per - 1) / per)), dim3(kEmbedThreads), 0, st, a);
+}
 
 }  // namespace
 
@@ -349,52 +469,68 @@ cudaError_t launch_embed(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int
     return embed_typed<__half>(ctx, n, vocab, d, table, ids, scale, out, st);
 }
 
-// Workspace: two lists of (id, position), the row map, and two parts per piece.
-size_t embed_grad_workspace(int64_t n, int64_t vocab, int d) {
-    const size_t pieces = ((size_t)n + kPiece - 1) / kPiece;
-    return 2 * up256(sizeof(int2) * (size_t)n) + up256((size_t)(vocab + 31) / 32 * 4) + 2 * up256(pieces * (size_t)d * 4);
+// Workspace: two lists of (id, position), the rows' runs, arrival counters, and two parts per piece.
+size_t embed_grad_workspace(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout,
+                            int grad_dtype, const void* grad) {
+    return make_plan(ctx, dtype, n, vocab, d, dout, grad_dtype, grad).total();
 }
 
 cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const int32_t* ids,
                               const void* dout, float scale, int32_t skip_id, int grad_dtype, int accumulate, void* grad,
                               void* ws, cudaStream_t st) {
+    const GradPlan g = make_plan(ctx, dtype, n, vocab, d, dout, grad_dtype, grad);
     uint8_t* w = static_cast<uint8_t*>(ws);
-    int2* buf[2];
-    for (int i = 0; i < 2; ++i) {
-        buf[i] = reinterpret_cast<int2*>(w);
-        w += up256(sizeof(int2) * (size_t)n);
+    SortArgs s;
+    s.ids = ids;
+    s.buf[0] = reinterpret_cast<int2*>(w);
+    s.buf[1] = reinterpret_cast<int2*>(w + g.list);
+    s.span = reinterpret_cast<int2*>(w + 2 * g.list);
+    s.arrived = reinterpret_cast<int*>(w + 2 * g.list + g.span);
+    s.grad = accumulate ? nullptr : static_cast<uint8_t*>(grad);
+    s.row_bytes = (int64_t)d * dtype_size(grad_dtype);
+    s.n = (int)n;
+    s.parts = g.pieces * g.slabs;
+    int bits = 1;   // of the largest key, which is `vocab` itself
+    while ((vocab >> bits) != 0) ++bits;
+    s.passes = (bits + 9) / 10;
+    s.bits = (bits + s.passes - 1) / s.passes;
+    s.vocab = (int32_t)vocab;
+    s.skip_id = skip_id;
+    s.status = &ctx->scalars->status;
+    if (!ctx->embed_ready) {
+        const cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortSmem));
+        if (e != cudaSuccess) return e;
+        ctx->embed_ready = 1;
     }
-    uint32_t* present = reinterpret_cast<uint32_t*>(w);
-    w += up256((size_t)(vocab + 31) / 32 * 4);
-    ReduceArgs a;
-    a.piece = kPiece;
-    a.pieces = (int)((n + a.piece - 1) / a.piece);
-    a.head = reinterpret_cast<float*>(w);
-    a.tail = reinterpret_cast<float*>(w + up256((size_t)a.pieces * d * 4));
-    int passes = 1;  // 8 bits each; the largest key is `vocab` itself
-    while (passes < 4 && (vocab >> (8 * passes)) != 0) ++passes;
     {
-        KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
         // (the cluster shape is part of the kernel's declaration)
-        const cudaError_t e = launch_dependent(embed_sort_kernel, dim3(kSortCtas), dim3(kSortThreads), sizeof(SortSmem), st,
-                                               (int)n, (int32_t)vocab, skip_id, passes, ids, buf[0], buf[1],
-                                               accumulate ? (uint32_t*)nullptr : present, &ctx->scalars->status);
+        const int ctas = accumulate ? kSortCtas : (ctx->sm_count / kSortCtas) * kSortCtas;
+        KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
+        const cudaError_t e = launch_dependent(embed_sort_kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortSmem), st, s);
         if (e != cudaSuccess) return e;
     }
-    a.list = buf[(passes - 1) & 1];
-    a.present = present;
+    ReduceArgs a;
+    a.list = s.buf[(s.passes - 1) & 1];
+    a.span = s.span;
     a.dout = dout;
     a.grad = grad;
+    a.head = reinterpret_cast<float*>(w + 2 * g.list + g.span + g.arrived);
+    a.tail = reinterpret_cast<float*>(w + 2 * g.list + g.span + g.arrived + g.parts);
+    a.arrived = s.arrived;
     a.n = (int)n;
     a.vocab = (int)vocab;
     a.d = d;
+    a.piece = g.piece;
+    a.pieces = g.pieces;
+    a.slabs = g.slabs;
     a.accumulate = accumulate;
     a.scale = scale;
     const bool wide = grad_dtype == SAMA_F32;
-    if (dtype == SAMA_F32) return reduce_typed<float, float>(ctx, a, st);
+    if (dtype == SAMA_F32) return reduce_typed<float, float>(ctx, a, g.vec, st);
     if (dtype == SAMA_BF16)
-        return wide ? reduce_typed<__nv_bfloat16, float>(ctx, a, st) : reduce_typed<__nv_bfloat16, __nv_bfloat16>(ctx, a, st);
-    return wide ? reduce_typed<__half, float>(ctx, a, st) : reduce_typed<__half, __half>(ctx, a, st);
+        return wide ? reduce_typed<__nv_bfloat16, float>(ctx, a, g.vec, st)
+                    : reduce_typed<__nv_bfloat16, __nv_bfloat16>(ctx, a, g.vec, st);
+    return wide ? reduce_typed<__half, float>(ctx, a, g.vec, st) : reduce_typed<__half, __half>(ctx, a, g.vec, st);
 }
 
 }  // namespace sama

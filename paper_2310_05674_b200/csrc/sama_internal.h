@@ -128,6 +128,7 @@ struct sama_ctx {
     size_t stage_bytes;
     void* op_ws;                   // device: workspace of the text-model operators (allocated on first use, grows)
     size_t op_ws_bytes;
+    int embed_ready;               // the sort's shared-memory size is set on this device
     uint32_t ffn_ready;            // kernels of gated_ffn.cu whose shared-memory size is set on this device
     int ffn_pair_units;            // CTA pairs of them that can be resident (0: not yet asked)
     sama::Profiler* prof;          // host
@@ -324,7 +325,8 @@ cudaError_t run_meta_grad(sama_ctx* ctx, const sama_mlp_t* mlp, const float* the
 // embed.cu : token embedding and its gradient
 cudaError_t launch_embed(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* table, const int32_t* ids,
                          float scale, void* out, cudaStream_t st);
-size_t embed_grad_workspace(int64_t n, int64_t vocab, int d);
+size_t embed_grad_workspace(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout,
+                            int grad_dtype, const void* grad);
 cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const int32_t* ids,
                               const void* dout, float scale, int32_t skip_id, int grad_dtype, int accumulate, void* grad,
                               void* ws, cudaStream_t st);
