@@ -9,14 +9,14 @@
 // so the result does not depend on scheduling (there is no floating-point atomic).
 //
 // Two launches:
-//   embed_sort   : one cluster of 8 CTAs sorts (id, position) by digits of up to 10 bits, least significant first.
+//   embed_sort   : one cluster of 16 CTAs sorts (id, position) by digits of up to 10 bits, least significant first.
 //                  Counts are exchanged through distributed shared memory, so the passes need only cluster barriers.
 //                  Ids outside the vocabulary and the skipped id become the key `vocab`, which sorts behind all others.
 //                  Meanwhile the other CTAs write zeros to the rows of dE that have no token: each takes a range of
 //                  rows and finds out by reading all ids.
 //   embed_reduce : a warp adds up one piece of the list for 32 threads' columns.  A run that lies inside a piece is
-//                  written out; the parts of a run that crosses pieces go to the workspace in fp32, and the warp that
-//                  finishes the last part adds them all up, in the order of the list.
+//                  written out; the parts of a run that crosses pieces go to the workspace in fp32, and the warps that
+//                  finish last add them up, in the order of the list.
 #include "num_types.h"
 #include "sama_internal.h"
 
@@ -64,7 +64,7 @@ embed_kernel(int64_t n_tokens, int64_t vocab, int d, int tpr, const T* __restric
 
 // ------------------------------------------------------------------ sort
 
-constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBins = 1024;
+constexpr int kSortCtas = 16, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBins = 1024;
 constexpr int kFillRows = 1 << 19;  // rows whose presence one CTA tracks at a time
 
 struct SortSmem {
@@ -89,10 +89,10 @@ struct SortArgs {
     const int32_t* ids;
     int2* buf[2];       // lists of (key, position); pass p writes buf[p & 1]
     int2* span;         // [vocab]: begin and end of each present row's run in the sorted list
-    int* arrived;       // [parts]: zeroed for embed_reduce
+    int* arrived;       // [counters]: zeroed for embed_reduce
     uint8_t* grad;      // rows to be zeroed where no token is, or null
     int64_t row_bytes;
-    int n, parts, passes, bits;
+    int n, counters, passes, bits;
     int32_t vocab, skip_id;
     int32_t* status;
 };
@@ -106,20 +106,31 @@ __device__ void fill_absent_rows(const SortArgs& a, uint32_t* present, int cta, 
         const int rows = (int)min((int64_t)kFillRows, stop - r0);
         for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) present[i] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < a.n; i += 4 * kSortThreads) {
-            int32_t id[4];
+        auto mark = [&](int32_t id) {
+            const int64_t r = (int64_t)id - r0;
+            if (r < 0 || r >= rows || id == a.skip_id) return;
+            uint32_t* w = present + (r >> 5);
+            const uint32_t bit = 1u << (r & 31);
+            if (!(*w & bit)) atomicOr(w, bit);
+        };
+        // 16 ids per thread at a time where their address allows, the rest one by one
+        const bool quads = (reinterpret_cast<uintptr_t>(a.ids) & 15u) == 0;
+        const int n4 = quads ? a.n / 4 : 0;
+        for (int i = threadIdx.x; i < n4; i += 4 * kSortThreads) {
+            int4 id[4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) id[u] = i + u * kSortThreads < a.n ? a.ids[i + u * kSortThreads] : -1;
+            for (int u = 0; u < 4; ++u)
+                id[u] = i + u * kSortThreads < n4 ? __ldg(reinterpret_cast<const int4*>(a.ids) + i + u * kSortThreads) : make_int4(-1, -1, -1, -1);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int64_t r = (int64_t)id[u] - r0;
-                if (r >= 0 && r < rows && id[u] != a.skip_id) {
-                    uint32_t* w = present + (r >> 5);
-                    const uint32_t bit = 1u << (r & 31);
-                    if (!(*w & bit)) atomicOr(w, bit);
-                }
+                mark(id[u].x);
+                mark(id[u].y);
+                mark(id[u].z);
+                mark(id[u].w);
             }
         }
+#pragma unroll 4
+        for (int i = 4 * n4 + threadIdx.x; i < a.n; i += kSortThreads) mark(a.ids[i]);
         __syncthreads();
         for (int r = threadIdx.x >> 5; r < rows; r += kSortWarps) {
             if (present[r >> 5] >> (r & 31) & 1u) continue;
@@ -137,7 +148,8 @@ __device__ void fill_absent_rows(const SortArgs& a, uint32_t* present, int cta, 
     }
 }
 
-__global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads)
+// Launched in clusters of kSortCtas.
+__global__ void __launch_bounds__(kSortThreads)
 embed_sort_kernel(const __grid_constant__ SortArgs a) {
     extern __shared__ uint8_t sort_raw[];
     SortSmem& sm = *reinterpret_cast<SortSmem*>(sort_raw);
@@ -155,8 +167,9 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
     const int64_t cta_end = min((int64_t)n, (int64_t)(rank + 1) * per_cta);
     const int64_t begin = (int64_t)rank * per_cta + (int64_t)warp * per_warp;
     const int64_t end = min(cta_end, begin + per_warp);
-    constexpr int U = 4;  // elements in flight per thread
-    for (int i = (int)rank * kSortThreads + threadIdx.x; i < a.parts; i += kSortCtas * kSortThreads) a.arrived[i] = 0;
+    constexpr int U = 8;  // elements in flight per thread
+    const bool once = per_warp <= 32 * U;  // a thread's elements stay in registers between the two sweeps of a pass
+    for (int i = (int)rank * kSortThreads + threadIdx.x; i < a.counters; i += kSortCtas * kSortThreads) a.arrived[i] = 0;
     for (int p = 0; p < a.passes; ++p) {
         const int2* src = a.buf[(p & 1) ^ 1];
         int2* dst = a.buf[p & 1];
@@ -171,8 +184,8 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
         };
         for (int b = lane; b < bins; b += 32) sm.hist[warp][b] = 0;
         __syncwarp();
+        int2 e[U];
         for (int64_t i = begin + lane; i - lane < end; i += 32 * U) {
-            int2 e[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) e[u] = fetch(i + 32 * u);
 #pragma unroll
@@ -219,11 +232,13 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
         }
         __syncthreads();
         for (int64_t i = begin + lane; i - lane < end; i += 32 * U) {
-            int2 e[U];
+            if (!once) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) e[u] = fetch(i + 32 * u);
+                for (int u = 0; u < U; ++u) e[u] = fetch(i + 32 * u);
+            }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (i - lane + 32 * u >= end) break;
                 const bool on = e[u].x >= 0;
                 const uint32_t digit = on ? ((uint32_t)e[u].x >> shift) & (bins - 1) : 0xffffffffu;
                 const uint32_t same = __match_any_sync(0xffffffffu, digit);
@@ -240,15 +255,30 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
         cluster_barrier();  // the pass is complete: every CTA may read all of dst, and total may be rewritten
     }
     const int2* list = a.buf[(a.passes - 1) & 1];
-    for (int64_t i = begin + lane; i < end; i += 32) {
-        const int32_t key = __ldcg(list + i).x;
-        if (key >= a.vocab) continue;
-        if (i == 0 || __ldcg(list + i - 1).x != key) a.span[key].x = (int)i;
-        if (i == n - 1 || __ldcg(list + i + 1).x != key) a.span[key].y = (int)i + 1;
+    for (int64_t i = begin + lane; i - lane < end; i += 32 * U) {
+        int32_t key[U], edge[U];   // edge: the neighbour beyond the warp's 32 entries, for the first and the last lane
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t j = i + 32 * u, k = lane == 0 ? j - 1 : j + 1;
+            key[u] = j < n ? __ldcg(list + j).x : a.vocab;
+            edge[u] = (lane == 0 || lane == 31) && k >= 0 && k < n ? __ldcg(list + k).x : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t j = i + 32 * u;
+            int32_t prev = __shfl_up_sync(0xffffffffu, key[u], 1), next = __shfl_down_sync(0xffffffffu, key[u], 1);
+            if (lane == 0) prev = edge[u];
+            if (lane == 31) next = edge[u];
+            if (j >= end || key[u] >= a.vocab) continue;
+            if (prev != key[u]) a.span[key[u]].x = (int)j;
+            if (next != key[u]) a.span[key[u]].y = (int)j + 1;
+        }
     }
 }
 
 // ------------------------------------------------------------------ reduction
+
+constexpr int kJoin = 32;     // pieces per group of the join
 
 struct ReduceArgs {
     const int2* list;         // sorted (id, position)
@@ -257,7 +287,7 @@ struct ReduceArgs {
     void* grad;
     float* head;              // [pieces][d]: the part, in this piece, of a run that began in an earlier one
     float* tail;              // [pieces][d]: the first part of a run that goes on in the next piece
-    int* arrived;             // [pieces][slabs], by the piece a run begins in: parts that are stored
+    int* arrived;             // counters of stored parts: [pieces][slabs] twice, then [groups][slabs]
     int n, vocab, d;
     int piece, pieces, slabs;
     int accumulate;
@@ -317,9 +347,68 @@ __device__ __forceinline__ void load_part(const float* p, float* v) {
     }
 }
 
+// Adds the parts at base + (first + step j) d, j = 0 .. count - 1, to sum, in this order.
+template <int VE>
+__device__ __forceinline__ void add_parts(const float* base, int64_t first, int64_t step, int count, float* sum) {
+    constexpr int U = VE == 8 ? 4 : 8;  // (more would set the whole kernel's register count)
+    for (int j = 0; j < count; j += U) {
+        float v[U][VE];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (j + u < count) load_part<VE>(base + first + (j + u) * step, v[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (j + u < count)
+#pragma unroll
+                for (int q = 0; q < VE; ++q) sum[q] += v[u][q];
+    }
+}
+
+// Whether this warp is the last of `parts` to get here with its part stored.
+__device__ __forceinline__ bool last_to_arrive(int* counter, int parts, int lane) {
+    __threadfence();
+    __syncwarp();
+    int before = 0;
+    if (lane == 0) before = atomicAdd(counter, 1);
+    before = __shfl_sync(0xffffffffu, before, 0);
+    if (before != parts - 1) return false;
+    __threadfence();
+    return true;
+}
+
+// This warp has stored its part, in piece k, of a run over pieces k0 .. k1.  The parts are joined in groups of kJoin
+// pieces, then the groups: the last to store a part adds up its group, the last to store a group's sum (in the place of
+// its first part) adds up the groups.
+template <typename TG, int VE>
+__device__ __forceinline__ void join_run(const ReduceArgs& a, int key, int k, int slab, int lane) {
+    const int c = (slab * 32 + lane) * VE;
+    const bool on = c < a.d;
+    const int2 run = a.span[key];
+    const int k0 = run.x / a.piece, k1 = (run.y - 1) / a.piece;
+    const int g = k / kJoin, g0 = k0 / kJoin, g1 = k1 / kJoin;
+    const int first = max(k0, g * kJoin), last = min(k1, g * kJoin + kJoin - 1);
+    const int64_t parts = (int64_t)a.pieces * a.slabs;
+    // counters: of the group a run begins in, by k0 (at most one such run per piece); of a later group, by the group
+    int* in_group = g == g0 ? a.arrived + (int64_t)k0 * a.slabs + slab : a.arrived + 2 * parts + (int64_t)g * a.slabs + slab;
+    if (!last_to_arrive(in_group, last - first + 1, lane)) return;
+    float sum[VE];
+    float* slot = (g == g0 ? a.tail : a.head) + (int64_t)first * a.d + (on ? c : 0);
+    const float* heads = a.head + (on ? c : 0);
+    load_part<VE>(slot, sum);
+    add_parts<VE>(heads, (int64_t)(first + 1) * a.d, a.d, last - first, sum);
+    if (g0 != g1) {
+        __syncwarp();
+        if (on) store_n<float, VE>(slot, sum);
+        if (!last_to_arrive(a.arrived + parts + (int64_t)k0 * a.slabs + slab, g1 - g0 + 1, lane)) return;
+        load_part<VE>(a.tail + (int64_t)k0 * a.d + (on ? c : 0), sum);
+        add_parts<VE>(heads, (int64_t)(g0 + 1) * kJoin * a.d, (int64_t)kJoin * a.d, g1 - g0, sum);
+    }
+    if (on) put_row<TG, VE>(a, key, c, sum);
+}
+
 // One warp: piece k of the list, columns [32 VE slab, 32 VE (slab + 1)).
 template <typename T, typename TG, int VE>
-__global__ void __launch_bounds__(kEmbedThreads)
+__global__ void __launch_bounds__(kEmbedThreads, 3)
 embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
     pdl_trigger();
     pdl_wait();
@@ -328,75 +417,66 @@ embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
     const int64_t unit = (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5);
     const int k = (int)(unit / a.slabs), slab = (int)(unit - (int64_t)k * a.slabs);
     if (k >= a.pieces) return;
-    const int i0 = k * a.piece, i1 = min(a.n, i0 + a.piece);
+    const int i0 = k * a.piece, count = min(a.n - i0, a.piece);
     const int c = (slab * 32 + lane) * VE;
     const bool on = c < a.d;   // (the other lanes of the last slab go along for the warp's sake)
     const T* dout = static_cast<const T*>(a.dout) + (on ? c : 0);
-    int key = a.list[i0].x;
-    bool open_head = i0 > 0 && a.list[i0 - 1].x == key;
+    // the piece's entries, two per lane
+    const int2 none = make_int2(a.vocab, 0);
+    const int2 low = lane < count ? a.list[i0 + lane] : none, high = lane + 32 < count ? a.list[i0 + lane + 32] : none;
+    const int before_key = i0 > 0 ? a.list[i0 - 1].x : -1, after_key = i0 + count < a.n ? a.list[i0 + count].x : -1;
+    const int first_key = __shfl_sync(0xffffffffu, low.x, 0);
+    const bool open_head = before_key == first_key && first_key < a.vocab;
+    int key = first_key;
+    bool in_head = open_head;   // the current run began in an earlier piece
     float acc[VE];
 #pragma unroll
     for (int j = 0; j < VE; ++j) acc[j] = 0.f;
 
-    // The current run has no more entries in this piece.
-    auto finish = [&](bool goes_on) {
-        if (!open_head && !goes_on) {
-            if (on) put_row<TG, VE>(a, key, c, acc);
-            return;
-        }
-        if (on) store_n<float, VE>((open_head ? a.head : a.tail) + (int64_t)k * a.d + c, acc);
-        const int2 run = a.span[key];
-        const int k0 = run.x / a.piece, k1 = (run.y - 1) / a.piece;
-        __threadfence();
-        __syncwarp();
-        int before = 0;
-        if (lane == 0) before = atomicAdd(a.arrived + (int64_t)k0 * a.slabs + slab, 1);
-        before = __shfl_sync(0xffffffffu, before, 0);
-        if (before != k1 - k0) return;
-        __threadfence();   // all parts are in place: add them up
-        if (!on) return;
-        float sum[VE], v[4][VE];
-        load_part<VE>(a.tail + (int64_t)k0 * a.d + c, sum);
-        for (int j = k0 + 1; j <= k1; j += 4) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (j + u <= k1) load_part<VE>(a.head + (int64_t)(j + u) * a.d + c, v[u]);
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (j + u <= k1)
-#pragma unroll
-                    for (int q = 0; q < VE; ++q) sum[q] += v[u][q];
-        }
-        put_row<TG, VE>(a, key, c, sum);
+    Raw<T, VE> v[U];
+    auto entry = [&](int i) {
+        const int2 e = i < 32 ? low : high;
+        return make_int2(__shfl_sync(0xffffffffu, e.x, i & 31), __shfl_sync(0xffffffffu, e.y, i & 31));
     };
-
-    for (int ib = i0; ib < i1 && key < a.vocab; ib += 32) {
-        const int2 mine = ib + lane < i1 ? a.list[ib + lane] : make_int2(a.vocab, 0);   // 32 entries, one per lane
-        const int count = min(32, i1 - ib);
-        for (int b = 0; b < count && key < a.vocab; b += U) {
-            Raw<T, VE> v[U];
-            int id[U];
+    auto fetch = [&](Raw<T, VE>& r, int i) {
+        if (i >= count) return;
+        const int2 e = entry(i);
+        if (e.x < a.vocab) r.load(dout + (int64_t)e.y * a.d);
+    };
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                id[u] = __shfl_sync(0xffffffffu, mine.x, b + u);
-                const int pos = __shfl_sync(0xffffffffu, mine.y, b + u);
-                if (id[u] < a.vocab) v[u].load(dout + (int64_t)pos * a.d);
-            }
+    for (int u = 0; u < U; ++u) fetch(v[u], u);
+    for (int b = 0; b < count && key < a.vocab; b += U) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (b + u >= count || key >= a.vocab) continue;
-                if (id[u] != key) {
-                    finish(false);
-                    open_head = false;
-                    key = id[u];
-#pragma unroll
-                    for (int j = 0; j < VE; ++j) acc[j] = 0.f;
+        for (int u = 0; u < U; ++u) {
+            if (b + u >= count) break;
+            const int id = entry(b + u).x;
+            if (id != key) {
+                if (on) {
+                    if (in_head) store_n<float, VE>(a.head + (int64_t)k * a.d + c, acc);
+                    else put_row<TG, VE>(a, key, c, acc);
                 }
-                if (key < a.vocab) v[u].add_to(acc);
+                in_head = false;
+                key = id;
+                if (key >= a.vocab) break;
+#pragma unroll
+                for (int j = 0; j < VE; ++j) acc[j] = 0.f;
             }
+            v[u].add_to(acc);
+            fetch(v[u], b + u + U);
         }
     }
-    if (key < a.vocab) finish(i1 < a.n && a.list[i1].x == key);
+    const bool open_tail = key < a.vocab && after_key == key;
+    if (on && key < a.vocab) {
+        if (in_head) store_n<float, VE>(a.head + (int64_t)k * a.d + c, acc);
+        else if (open_tail) store_n<float, VE>(a.tail + (int64_t)k * a.d + c, acc);
+        else put_row<TG, VE>(a, key, c, acc);
+    }
+    // the run that came in, and the one that goes on where that is another
+#pragma unroll 1
+    for (int j = 0; j < 2; ++j) {
+        const int run = j == 0 ? first_key : key;
+        if (j == 0 ? open_head : (open_tail && !in_head)) join_run<TG, VE>(a, run, k, slab, lane);
+    }
 }
 
 int threads_per_row(int d, int ve) {
@@ -431,7 +511,7 @@ inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct GradPlan {
     bool vec;
-    int ve, slabs, piece, pieces;
+    int ve, slabs, piece, pieces, counters;
     size_t list, span, arrived, parts;  // bytes
     size_t total() const { return 2 * list + span + arrived + 2 * parts; }
 };
@@ -446,7 +526,8 @@ GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int
     g.pieces = (int)((n + g.piece - 1) / g.piece);
     g.list = up256(sizeof(int2) * (size_t)n);
     g.span = up256(sizeof(int2) * (size_t)vocab);
-    g.arrived = up256(sizeof(int) * (size_t)g.pieces * g.slabs);
+    g.counters = (2 * g.pieces + (g.pieces + kJoin - 1) / kJoin) * g.slabs;
+    g.arrived = up256(sizeof(int) * (size_t)g.counters);
     g.parts = up256(sizeof(float) * (size_t)g.pieces * d);
     return g;
 }
@@ -489,7 +570,7 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
     s.grad = accumulate ? nullptr : static_cast<uint8_t*>(grad);
     s.row_bytes = (int64_t)d * dtype_size(grad_dtype);
     s.n = (int)n;
-    s.parts = g.pieces * g.slabs;
+    s.counters = g.counters;
     int bits = 1;   // of the largest key, which is `vocab` itself
     while ((vocab >> bits) != 0) ++bits;
     s.passes = (bits + 9) / 10;
@@ -498,15 +579,17 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
     s.skip_id = skip_id;
     s.status = &ctx->scalars->status;
     if (!ctx->embed_ready) {
-        const cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortSmem));
+        cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortSmem));
+        if (e != cudaSuccess) return e;
+        e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         ctx->embed_ready = 1;
     }
     {
-        // (the cluster shape is part of the kernel's declaration)
-        const int ctas = accumulate ? kSortCtas : (ctx->sm_count / kSortCtas) * kSortCtas;
+        // seven further clusters fill: one cluster of 16 fits into each of the 8 groups of SMs
+        const int ctas = accumulate ? kSortCtas : 8 * kSortCtas;
         KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
-        const cudaError_t e = launch_dependent(embed_sort_kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortSmem), st, s);
+        const cudaError_t e = launch_clustered(kSortCtas, embed_sort_kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortSmem), st, s);
         if (e != cudaSuccess) return e;
     }
     ReduceArgs a;
