@@ -13,10 +13,10 @@
 //                  Counts are exchanged through distributed shared memory, so the passes need only cluster barriers.
 //                  Ids outside the vocabulary and the skipped id become the key `vocab`, which sorts behind all others.
 //                  Meanwhile the other CTAs write zeros to the rows of dE that have no token: each takes a range of
-//                  rows and finds out by reading all ids.
+//                  rows and finds out by reading all ids.  They stop when the list is sorted.
 //   embed_reduce : a warp adds up one piece of the list for 32 threads' columns.  A run that lies inside a piece is
 //                  written out; the parts of a run that crosses pieces go to the workspace in fp32, and the warps that
-//                  finish last add them up, in the order of the list.
+//                  finish last add them up, in the order of the list.  The first blocks write the zeros still missing.
 #include "num_types.h"
 #include "sama_internal.h"
 
@@ -57,22 +57,49 @@ embed_kernel(int64_t n_tokens, int64_t vocab, int d, int tpr, const T* __restric
             if (t >= n_tokens) continue;
 #pragma unroll
             for (int i = 0; i < VE; ++i) v[r][i] = good[r] ? v[r][i] * scale : 0.f;
-            store_n<T, VE>(out + t * d + c, v[r]);
+            store_n<T, VE, true>(out + t * d + c, v[r]);  // (not to push the table out of L2)
         }
     }
 }
 
 // ------------------------------------------------------------------ sort
 
-constexpr int kSortCtas = 16, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBins = 1024;
-constexpr int kFillRows = 1 << 19;  // rows whose presence one CTA tracks at a time
+constexpr int kSortCtas = 16, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kMaxBits = 10, kMaxBins = 1 << kMaxBits;
+constexpr int kStage = 8192;        // elements of one CTA that fit its staging area
+// One cluster of 16 fits into each of the 8 groups of SMs: one sorts, the others zero.
+constexpr int kFillCtas = 7 * kSortCtas;
 
 struct SortSmem {
     uint32_t hist[kSortWarps][kMaxBins];  // counts, then next output positions, of every warp's share
     uint32_t total[kMaxBins];             // this CTA's counts (read by the other CTAs)
-    uint32_t warp_sum[kSortWarps];
+    uint32_t warp_sum[2][kSortWarps];
+    uint32_t shift_to[kMaxBins];          // from a place in `stage` to the place in the list, by digit
+    int2 stage[kStage];                   // this CTA's elements in the order of their digit
 };
-static_assert(sizeof(SortSmem) >= kFillRows / 8, "the map of present rows takes the same shared memory");
+static_assert(sizeof(SortSmem) <= 227 * 1024, "one CTA per SM");
+
+// Zeroing of absent rows: kFillCtas shares of the rows, in each share warp w of 32 takes rows w, w + 32, ...
+struct FillArgs {
+    uint8_t* grad;          // null: nothing is zeroed
+    int64_t row_bytes;
+    int64_t share;          // rows per share, a multiple of 32
+    uint32_t* present;      // one bit per row
+    int* progress;          // [kFillCtas][32]: rows of the share's warp that are done
+    int32_t vocab;
+};
+__device__ __forceinline__ bool zero_row_if_absent(const FillArgs& f, int64_t row, uint32_t present_word, int lane) {
+    if (present_word >> (row & 31) & 1u) return false;
+    uint8_t* g = f.grad + row * f.row_bytes;
+    const int64_t low = f.row_bytes | (int64_t)reinterpret_cast<uintptr_t>(f.grad);   // alignment of every row
+    if ((low & 15) == 0) {
+        for (int64_t b = lane * 16; b < f.row_bytes; b += 512) *reinterpret_cast<uint4*>(g + b) = make_uint4(0, 0, 0, 0);
+    } else if ((low & 3) == 0) {
+        for (int64_t b = lane * 4; b < f.row_bytes; b += 128) *reinterpret_cast<uint32_t*>(g + b) = 0;
+    } else {
+        for (int64_t b = lane * 2; b < f.row_bytes; b += 64) *reinterpret_cast<uint16_t*>(g + b) = 0;
+    }
+    return true;
+}
 
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -90,20 +117,23 @@ struct SortArgs {
     int2* buf[2];       // lists of (key, position); pass p writes buf[p & 1]
     int2* span;         // [vocab]: begin and end of each present row's run in the sorted list
     int* arrived;       // [counters]: zeroed for embed_reduce
-    uint8_t* grad;      // rows to be zeroed where no token is, or null
-    int64_t row_bytes;
+    FillArgs fill;
+    int* done;          // set to `epoch` once the list is sorted
+    int epoch;
     int n, counters, passes, bits;
     int32_t vocab, skip_id;
     int32_t* status;
 };
 
-// Zeros to this CTA's share of the rows that have no token.
-__device__ void fill_absent_rows(const SortArgs& a, uint32_t* present, int cta, int n_ctas) {
-    const int64_t per = (a.vocab + n_ctas - 1) / n_ctas;
-    const int64_t first = cta * per, stop = min((int64_t)a.vocab, first + per);
-    const int64_t low = a.row_bytes | (int64_t)reinterpret_cast<uintptr_t>(a.grad);   // alignment of every row
-    for (int64_t r0 = first; r0 < stop; r0 += kFillRows) {
-        const int rows = (int)min((int64_t)kFillRows, stop - r0);
+// Finds the rows of this CTA's share that have a token, and zeroes the others until the list is sorted.
+__device__ void fill_absent_rows(const SortArgs& a, uint8_t* smem, int cta) {
+    uint32_t* present = reinterpret_cast<uint32_t*>(smem);
+    constexpr int kTrack = 1 << 20;   // rows whose presence fits shared memory
+    const FillArgs& f = a.fill;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t first = cta * f.share, stop = min((int64_t)f.vocab, first + f.share);
+    for (int64_t r0 = first; r0 < stop; r0 += kTrack) {
+        const int rows = (int)min((int64_t)kTrack, stop - r0);
         for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) present[i] = 0;
         __syncthreads();
         auto mark = [&](int32_t id) {
@@ -132,20 +162,20 @@ __device__ void fill_absent_rows(const SortArgs& a, uint32_t* present, int cta, 
 #pragma unroll 4
         for (int i = 4 * n4 + threadIdx.x; i < a.n; i += kSortThreads) mark(a.ids[i]);
         __syncthreads();
-        for (int r = threadIdx.x >> 5; r < rows; r += kSortWarps) {
-            if (present[r >> 5] >> (r & 31) & 1u) continue;
-            uint8_t* g = a.grad + (r0 + r) * a.row_bytes;
-            if ((low & 15) == 0) {
-                for (int64_t b = (threadIdx.x & 31) * 16; b < a.row_bytes; b += 512)
-                    *reinterpret_cast<uint4*>(g + b) = make_uint4(0, 0, 0, 0);
-            } else if ((low & 3) == 0) {
-                for (int64_t b = (threadIdx.x & 31) * 4; b < a.row_bytes; b += 128) *reinterpret_cast<uint32_t*>(g + b) = 0;
-            } else {
-                for (int64_t b = (threadIdx.x & 31) * 2; b < a.row_bytes; b += 64) *reinterpret_cast<uint16_t*>(g + b) = 0;
-            }
-        }
+        for (int i = threadIdx.x; i < (rows + 31) / 32; i += kSortThreads) f.present[r0 / 32 + i] = present[i];
         __syncthreads();
     }
+    int64_t j = 0;
+    if (stop - first <= kTrack) {
+        // (a warp looks at the flag before every row; what it leaves, embed_reduce does)
+        for (; first + j * 32 + warp < stop; ++j) {
+            int seen = 0;
+            if (lane == 0) seen = *reinterpret_cast<volatile int*>(a.done);
+            if (__shfl_sync(0xffffffffu, seen, 0) == a.epoch) break;
+            zero_row_if_absent(f, first + j * 32 + warp, present[j], lane);
+        }
+    }
+    if (lane == 0) f.progress[cta * 32 + warp] = (int)j;
 }
 
 // Launched in clusters of kSortCtas.
@@ -156,7 +186,7 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
     pdl_trigger();
     pdl_wait();
     if (blockIdx.x >= kSortCtas) {
-        fill_absent_rows(a, reinterpret_cast<uint32_t*>(sort_raw), blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
+        fill_absent_rows(a, sort_raw, blockIdx.x - kSortCtas);
         return;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -164,28 +194,32 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
     const int n = a.n, bins = 1 << a.bits;
     const int per_cta = ((n + kSortCtas - 1) / kSortCtas + 31) & ~31;
     const int per_warp = ((per_cta + kSortWarps - 1) / kSortWarps + 31) & ~31;
-    const int64_t cta_end = min((int64_t)n, (int64_t)(rank + 1) * per_cta);
-    const int64_t begin = (int64_t)rank * per_cta + (int64_t)warp * per_warp;
-    const int64_t end = min(cta_end, begin + per_warp);
+    // (n <= 2^30, so that the rounded shares stay below 2^31)
+    const int cta_end = min(n, (int)(rank + 1) * per_cta);
+    const int begin = (int)rank * per_cta + warp * per_warp;
+    const int end = min(cta_end, begin + per_warp);
     constexpr int U = 8;  // elements in flight per thread
-    const bool once = per_warp <= 32 * U;  // a thread's elements stay in registers between the two sweeps of a pass
+    // Up to 32 U elements per warp stay in registers between the two sweeps of a pass, and go through shared memory in
+    // the order of their digit, so that they reach the list in runs rather than one sector each.
+    const bool once = per_warp <= 32 * U;
+    static_assert(kSortWarps * 32 * U <= kStage, "such a CTA's elements fit the stage");
     for (int i = (int)rank * kSortThreads + threadIdx.x; i < a.counters; i += kSortCtas * kSortThreads) a.arrived[i] = 0;
     for (int p = 0; p < a.passes; ++p) {
         const int2* src = a.buf[(p & 1) ^ 1];
         int2* dst = a.buf[p & 1];
         const int shift = a.bits * p;
-        auto fetch = [&](int64_t i) -> int2 {
+        auto fetch = [&](int i) -> int2 {
             if (i >= end) return make_int2(-1, 0);   // (beyond this warp's share)
             if (p > 0) return __ldcg(src + i);
             const int32_t id = a.ids[i];
             const bool good = id >= 0 && id < a.vocab;
             if (!good) atomicOr(a.status, (int)SAMA_DEV_BAD_INDEX);
-            return make_int2(good && id != a.skip_id ? id : a.vocab, (int)i);
+            return make_int2(good && id != a.skip_id ? id : a.vocab, i);
         };
         for (int b = lane; b < bins; b += 32) sm.hist[warp][b] = 0;
         __syncwarp();
         int2 e[U];
-        for (int64_t i = begin + lane; i - lane < end; i += 32 * U) {
+        for (int i = begin + lane; i - lane < end; i += 32 * U) {
 #pragma unroll
             for (int u = 0; u < U; ++u) e[u] = fetch(i + 32 * u);
 #pragma unroll
@@ -196,11 +230,13 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
         // thread b owns bin b
         uint32_t mine = 0;
         if (threadIdx.x < bins) {
-#pragma unroll 8
+            uint32_t c[kSortWarps];
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) c[w] = sm.hist[w][threadIdx.x];
+#pragma unroll
             for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t c = sm.hist[w][threadIdx.x];
                 sm.hist[w][threadIdx.x] = mine;
-                mine += c;
+                mine += c[w];
             }
             sm.total[threadIdx.x] = mine;
         }
@@ -216,22 +252,29 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
                 all += v[c];
             }
         }
-        uint32_t incl = all;
+        uint32_t incl = all, local = mine;   // inclusive sums over the bins: of the whole list, of this CTA's elements
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
+            const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o), x = __shfl_up_sync(0xffffffffu, local, o);
+            if (lane >= o) { incl += v; local += x; }
         }
-        if (lane == 31) sm.warp_sum[warp] = incl;
+        if (lane == 31) { sm.warp_sum[0][warp] = incl; sm.warp_sum[1][warp] = local; }
         __syncthreads();
+        // the sums of the warps before this one
+        const uint32_t past = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[0][lane] : 0u);
+        const uint32_t past_here = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[1][lane] : 0u);
         if (threadIdx.x < bins) {
-            uint32_t base = incl - all + before;
-            for (int w = 0; w < warp; ++w) base += sm.warp_sum[w];
-#pragma unroll 8
-            for (int w = 0; w < kSortWarps; ++w) sm.hist[w][threadIdx.x] += base;
+            const uint32_t base = past + incl - all + before, here = past_here + local - mine;
+            sm.shift_to[threadIdx.x] = base - here;
+            const uint32_t add = once ? here : base;
+            uint32_t c[kSortWarps];
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) c[w] = sm.hist[w][threadIdx.x];
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) sm.hist[w][threadIdx.x] = c[w] + add;
         }
         __syncthreads();
-        for (int64_t i = begin + lane; i - lane < end; i += 32 * U) {
+        for (int i = begin + lane; i - lane < end; i += 32 * U) {
             if (!once) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) e[u] = fetch(i + 32 * u);
@@ -240,38 +283,55 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
             for (int u = 0; u < U; ++u) {
                 if (i - lane + 32 * u >= end) break;
                 const bool on = e[u].x >= 0;
-                const uint32_t digit = on ? ((uint32_t)e[u].x >> shift) & (bins - 1) : 0xffffffffu;
-                const uint32_t same = __match_any_sync(0xffffffffu, digit);
+                const uint32_t digit = on ? ((uint32_t)e[u].x >> shift) & (bins - 1) : 0u;
+                // lanes with the same digit, one vote per bit (the instruction that matches whole values takes a step per
+                // distinct value: 200 cycles for a warp of different digits)
+                uint32_t same = __ballot_sync(0xffffffffu, on);
+#pragma unroll
+                for (int b = 0; b < kMaxBits; ++b) {   // (bits the digit does not have are 0 everywhere)
+                    const bool set = (digit & (1u << b)) != 0;
+                    same &= __ballot_sync(0xffffffffu, set) ^ (set ? 0u : 0xffffffffu);
+                }
                 uint32_t at = 0;
                 if (on) at = sm.hist[warp][digit] + __popc(same & ((1u << lane) - 1u));
                 __syncwarp();
                 if (on) {
-                    dst[at] = e[u];
+                    if (once) sm.stage[at] = e[u]; else dst[at] = e[u];
                     if (lane == __ffs(same) - 1) sm.hist[warp][digit] += __popc(same);
                 }
                 __syncwarp();
             }
         }
+        if (once) {
+            __syncthreads();
+            const int held = max(0, cta_end - (int)rank * per_cta);
+#pragma unroll 4
+            for (int i = threadIdx.x; i < held; i += kSortThreads) {
+                const int2 v = sm.stage[i];
+                dst[sm.shift_to[((uint32_t)v.x >> shift) & (bins - 1)] + i] = v;
+            }
+        }
         cluster_barrier();  // the pass is complete: every CTA may read all of dst, and total may be rewritten
     }
+    if (rank == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int*>(a.done) = a.epoch;
     const int2* list = a.buf[(a.passes - 1) & 1];
-    for (int64_t i = begin + lane; i - lane < end; i += 32 * U) {
+    for (int i = begin + lane; i - lane < end; i += 32 * U) {
         int32_t key[U], edge[U];   // edge: the neighbour beyond the warp's 32 entries, for the first and the last lane
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t j = i + 32 * u, k = lane == 0 ? j - 1 : j + 1;
+            const int j = i + 32 * u, k = lane == 0 ? j - 1 : j + 1;
             key[u] = j < n ? __ldcg(list + j).x : a.vocab;
             edge[u] = (lane == 0 || lane == 31) && k >= 0 && k < n ? __ldcg(list + k).x : -1;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t j = i + 32 * u;
+            const int j = i + 32 * u;
             int32_t prev = __shfl_up_sync(0xffffffffu, key[u], 1), next = __shfl_down_sync(0xffffffffu, key[u], 1);
             if (lane == 0) prev = edge[u];
             if (lane == 31) next = edge[u];
             if (j >= end || key[u] >= a.vocab) continue;
-            if (prev != key[u]) a.span[key[u]].x = (int)j;
-            if (next != key[u]) a.span[key[u]].y = (int)j + 1;
+            if (prev != key[u]) a.span[key[u]].x = j;
+            if (next != key[u]) a.span[key[u]].y = j + 1;
         }
     }
 }
@@ -290,6 +350,8 @@ struct ReduceArgs {
     int* arrived;             // counters of stored parts: [pieces][slabs] twice, then [groups][slabs]
     int n, vocab, d;
     int piece, pieces, slabs;
+    FillArgs fill;
+    int fill_blocks;          // the first blocks zero what embed_sort left
     int accumulate;
     float scale;
 };
@@ -414,7 +476,16 @@ embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
     pdl_wait();
     constexpr int U = 8;  // rows in flight per thread
     const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5);
+    if ((int)blockIdx.x < a.fill_blocks) {
+        const FillArgs& f = a.fill;
+        for (int w = (int)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5); w < kFillCtas * 32; w += a.fill_blocks * (kEmbedThreads / 32)) {
+            const int64_t first = (w / 32) * f.share, stop = min((int64_t)f.vocab, first + f.share);
+            for (int64_t row = first + (int64_t)f.progress[w] * 32 + w % 32; row < stop; row += 32)
+                zero_row_if_absent(f, row, f.present[row / 32], lane);
+        }
+        return;
+    }
+    const int64_t unit = (int64_t)(blockIdx.x - a.fill_blocks) * (kEmbedThreads / 32) + (threadIdx.x >> 5);
     const int k = (int)(unit / a.slabs), slab = (int)(unit - (int64_t)k * a.slabs);
     if (k >= a.pieces) return;
     const int i0 = k * a.piece, count = min(a.n - i0, a.piece);
@@ -512,8 +583,9 @@ inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 struct GradPlan {
     bool vec;
     int ve, slabs, piece, pieces, counters;
-    size_t list, span, arrived, parts;  // bytes
-    size_t total() const { return 2 * list + span + arrived + 2 * parts; }
+    int64_t share;
+    size_t list, span, arrived, present, progress, parts;  // bytes
+    size_t total() const { return 2 * list + span + arrived + present + progress + 2 * parts; }
 };
 GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout, int grad_dtype,
                    const void* grad) {
@@ -528,6 +600,9 @@ GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int
     g.span = up256(sizeof(int2) * (size_t)vocab);
     g.counters = (2 * g.pieces + (g.pieces + kJoin - 1) / kJoin) * g.slabs;
     g.arrived = up256(sizeof(int) * (size_t)g.counters);
+    g.share = ((vocab + kFillCtas - 1) / kFillCtas + 31) & ~(int64_t)31;
+    g.present = up256((size_t)(g.share / 32) * kFillCtas * 4);
+    g.progress = up256(sizeof(int) * kFillCtas * 32);
     g.parts = up256(sizeof(float) * (size_t)g.pieces * d);
     return g;
 }
@@ -538,7 +613,7 @@ cudaError_t reduce_typed(sama_ctx* ctx, const ReduceArgs& a, bool vec, cudaStrea
     KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
     auto* kernel = vec ? embed_reduce_kernel<T, TG, VE> : embed_reduce_kernel<T, TG, 1>;
     const int64_t units = (int64_t)a.pieces * a.slabs, per = kEmbedThreads / 32;
-    return launch_dependent(kernel, dim3((unsigned)((units + per - 1) / per)), dim3(kEmbedThreads), 0, st, a);
+    return launch_dependent(kernel, dim3((unsigned)(a.fill_blocks + (units + per - 1) / per)), dim3(kEmbedThreads), 0, st, a);
 }
 
 }  // namespace
@@ -561,19 +636,31 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
                               void* ws, cudaStream_t st) {
     const GradPlan g = make_plan(ctx, dtype, n, vocab, d, dout, grad_dtype, grad);
     uint8_t* w = static_cast<uint8_t*>(ws);
+    auto take = [&](size_t bytes) {
+        void* p = w;
+        w += bytes;
+        return p;
+    };
     SortArgs s;
     s.ids = ids;
-    s.buf[0] = reinterpret_cast<int2*>(w);
-    s.buf[1] = reinterpret_cast<int2*>(w + g.list);
-    s.span = reinterpret_cast<int2*>(w + 2 * g.list);
-    s.arrived = reinterpret_cast<int*>(w + 2 * g.list + g.span);
-    s.grad = accumulate ? nullptr : static_cast<uint8_t*>(grad);
-    s.row_bytes = (int64_t)d * dtype_size(grad_dtype);
+    s.buf[0] = static_cast<int2*>(take(g.list));
+    s.buf[1] = static_cast<int2*>(take(g.list));
+    s.span = static_cast<int2*>(take(g.span));
+    s.arrived = static_cast<int*>(take(g.arrived));
+    s.fill.present = static_cast<uint32_t*>(take(g.present));
+    s.fill.progress = static_cast<int*>(take(g.progress));
+    s.fill.grad = accumulate ? nullptr : static_cast<uint8_t*>(grad);
+    s.fill.row_bytes = (int64_t)d * dtype_size(grad_dtype);
+    s.fill.share = g.share;
+    s.fill.vocab = (int32_t)vocab;
+    s.done = &ctx->scalars->embed_done;
+    // (replays of a captured call find the flag already set: then embed_reduce writes all the zeros)
+    s.epoch = ++ctx->embed_epoch;
     s.n = (int)n;
     s.counters = g.counters;
     int bits = 1;   // of the largest key, which is `vocab` itself
     while ((vocab >> bits) != 0) ++bits;
-    s.passes = (bits + 9) / 10;
+    s.passes = (bits + kMaxBits - 1) / kMaxBits;
     s.bits = (bits + s.passes - 1) / s.passes;
     s.vocab = (int32_t)vocab;
     s.skip_id = skip_id;
@@ -586,8 +673,7 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
         ctx->embed_ready = 1;
     }
     {
-        // seven further clusters fill: one cluster of 16 fits into each of the 8 groups of SMs
-        const int ctas = accumulate ? kSortCtas : 8 * kSortCtas;
+        const int ctas = accumulate ? kSortCtas : kSortCtas + kFillCtas;
         KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
         const cudaError_t e = launch_clustered(kSortCtas, embed_sort_kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortSmem), st, s);
         if (e != cudaSuccess) return e;
@@ -597,8 +683,10 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
     a.span = s.span;
     a.dout = dout;
     a.grad = grad;
-    a.head = reinterpret_cast<float*>(w + 2 * g.list + g.span + g.arrived);
-    a.tail = reinterpret_cast<float*>(w + 2 * g.list + g.span + g.arrived + g.parts);
+    a.head = static_cast<float*>(take(g.parts));
+    a.tail = static_cast<float*>(take(g.parts));
+    a.fill = s.fill;
+    a.fill_blocks = accumulate ? 0 : ctx->sm_count;
     a.arrived = s.arrived;
     a.n = (int)n;
     a.vocab = (int)vocab;

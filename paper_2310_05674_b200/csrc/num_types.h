@@ -67,20 +67,26 @@ __device__ __forceinline__ void load_n(const T* p, float* v) {
         }
     }
 }
-template <typename T, int N>
+// PASS: data that should not displace what is in L2.
+template <typename T, int N, bool PASS = false>
 __device__ __forceinline__ void store_n(T* p, const float* v) {
     if constexpr (N == 1) {
         *p = from_float<T>(v[0]);
     } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i)
-            reinterpret_cast<float4*>(p)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        for (int i = 0; i < N / 4; ++i) {
+            const float4 x = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            float4* q = reinterpret_cast<float4*>(p) + i;
+            if (PASS) __stcs(q, x); else *q = x;
+        }
     } else {
 #pragma unroll
-        for (int i = 0; i < N / 8; ++i)
-            reinterpret_cast<uint4*>(p)[i] =
-                make_uint4(pack2<T>(v[8 * i], v[8 * i + 1]), pack2<T>(v[8 * i + 2], v[8 * i + 3]),
-                           pack2<T>(v[8 * i + 4], v[8 * i + 5]), pack2<T>(v[8 * i + 6], v[8 * i + 7]));
+        for (int i = 0; i < N / 8; ++i) {
+            const uint4 x = make_uint4(pack2<T>(v[8 * i], v[8 * i + 1]), pack2<T>(v[8 * i + 2], v[8 * i + 3]),
+                                       pack2<T>(v[8 * i + 4], v[8 * i + 5]), pack2<T>(v[8 * i + 6], v[8 * i + 7]));
+            uint4* q = reinterpret_cast<uint4*>(p) + i;
+            if (PASS) __stcs(q, x); else *q = x;
+        }
     }
 }
 #endif

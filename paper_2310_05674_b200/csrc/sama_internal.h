@@ -28,6 +28,7 @@ struct DeviceScalars {
     unsigned int counter;  // arrival counter of the last-block-done reductions and of the fused sweep's grid barrier (returns to 0)
     unsigned int departed; // blocks that have left the fused sweep's grid barrier (returns to 0)
     ClipState clip;
+    int embed_done;        // the call (by number) whose tokens the embedding gradient has sorted
 };
 
 // Host-precomputed constants of the Adam adaptation matrix (Appendix C).
@@ -129,6 +130,7 @@ struct sama_ctx {
     void* op_ws;                   // device: workspace of the text-model operators (allocated on first use, grows)
     size_t op_ws_bytes;
     int embed_ready;               // the sort's shared-memory size is set on this device
+    int embed_epoch;               // number of the last such call
     uint32_t ffn_ready;            // kernels of gated_ffn.cu whose shared-memory size is set on this device
     int ffn_pair_units;            // CTA pairs of them that can be resident (0: not yet asked)
     sama::Profiler* prof;          // host
