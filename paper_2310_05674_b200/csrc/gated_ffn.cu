@@ -15,6 +15,8 @@
 // H, dG and dU are rounded to the operands' type between launches, as any operand of a 16-bit product has to be; every
 // sum stays in fp32 until its one rounding on the way out.
 //
+// Up to 16 tokens go another way, see ffn_few_kernel.
+//
 // Operands are read as they lie in memory: where the contraction runs along a matrix's rows, the tile is loaded and
 // described to the tensor core "MN-major" instead of being transposed by a pass of its own.
 //
@@ -458,6 +460,124 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
     }
 }
 
+// ---------------------------------------------------------------- few tokens
+
+// Up to 16 tokens (a decode step): the products are bound by reading the weights once, 6 d f bytes, and a 128-row tile
+// would leave the tensor core mostly zeros to multiply and two thirds of the machine idle on Y = H Wd^T.  Here a block
+// takes 8 features (8 rows of Wg and of Wu, or of Wd) and its 8 warps share the contraction, so there are f / 8 and d / 8
+// blocks; weights go from memory straight to the registers of m16n8k16 products, 16 bytes per load.  (A thread's 8
+// consecutive k are used as the k-indices that the instruction wants from it; the tokens' operand is read with the same
+// permutation, so the sum is over the same products.)  The warps' partial sums are added in a fixed order.
+constexpr int kFewTokens = 16, kFewWarps = 8;
+
+struct FewArgs {
+    const void* x;        // [M][K], ld
+    const void* w[2];     // [N][K]
+    void* out[3];         // gate-up: G, U (or null) and H; down: Y
+    int64_t ldx, ldo[3];
+    int M, N, K, act;
+};
+
+__device__ __forceinline__ uint4 load_weights(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (std::is_same<T, __half>::value)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// VEC: rows of x and w are 16-byte aligned (K is then a multiple of 8).  WIDE: more than 8 tokens.
+template <typename T, bool GATE, bool VEC, bool WIDE>
+__global__ void __launch_bounds__(32 * kFewWarps, 32 / kFewWarps)
+ffn_few_kernel(const __grid_constant__ FewArgs a) {
+    constexpr int NT = GATE ? 2 : 1, U = 8 / NT;   // eight weight loads in flight per thread
+    __shared__ float red[kFewWarps][NT][kFewTokens][8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int n0 = blockIdx.x * 8;
+    // Steps of 32 of the contraction.  Gate-up: a warp takes a contiguous eighth of them.  Down: they are dealt out in runs
+    // of U, so that what the warps read at a time is contiguous.  (Each the faster way for its kernel, 1 token, 4096 x
+    // 8192: gate-up 25 us against 27 in runs, down 14 us against 16 in eighths.)
+    const int steps = (a.K + 31) / 32, mine = (steps + U * kFewWarps - 1) / (U * kFewWarps) * U;
+    auto step_of = [&](int i) { return GATE ? warp * mine + i : (i / U * kFewWarps + warp) * U + i % U; };
+    // rows beyond the matrix: some row that exists, its results are not stored
+    const T* w[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) w[j] = static_cast<const T*>(a.w[j]) + (int64_t)min(n0 + g, a.N - 1) * a.K;
+    const T* x0 = static_cast<const T*>(a.x) + (int64_t)min(g, a.M - 1) * a.ldx;
+    const T* x1 = static_cast<const T*>(a.x) + (int64_t)min(g + 8, a.M - 1) * a.ldx;
+    float acc[NT][4] = {};
+    uint4 v[U][NT];
+    auto fetch_step = [&](uint4 (&r)[NT], int i) {
+        const int k = step_of(i) * 32 + 8 * t;
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            r[j] = i >= mine || k >= a.K ? make_uint4(0, 0, 0, 0) : (VEC ? load_weights(w[j] + k) : load8(w[j], k, a.K, false));
+    };
+    auto fetch = [&]() {
+#pragma unroll
+        for (int u = 0; u < U; ++u) fetch_step(v[u], u);
+    };
+    if (GATE) {
+        // The dependent launch may read its weights before this kernel has ended, so it must not start before whatever
+        // wrote them has: wait first.
+        pdl_wait();
+        pdl_trigger();
+        fetch();
+    } else {
+        fetch();   // the weights were there before the gate-up kernel started; H was not
+        pdl_trigger();
+        pdl_wait();
+    }
+    for (int i = 0; i < mine; i += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = step_of(i + u) * 32 + 8 * t;
+            const bool in = k < a.K;
+            const uint4 zero = make_uint4(0, 0, 0, 0);
+            const uint4 p = in ? load8(x0, k, a.K, VEC) : zero, q = WIDE && in ? load8(x1, k, a.K, VEC) : zero;
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                mma16816<T>(acc[j], p.x, q.x, p.y, q.y, v[u][j].x, v[u][j].y);
+                mma16816<T>(acc[j], p.z, q.z, p.w, q.w, v[u][j].z, v[u][j].w);
+            }
+            fetch_step(v[u], i + u + U);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        *reinterpret_cast<float2*>(&red[warp][j][g][2 * t]) = make_float2(acc[j][0], acc[j][1]);
+        if (WIDE) *reinterpret_cast<float2*>(&red[warp][j][g + 8][2 * t]) = make_float2(acc[j][2], acc[j][3]);
+    }
+    __syncthreads();
+    const int m = threadIdx.x >> 3, f = threadIdx.x & 7;
+    static_assert(32 * kFewWarps >= 8 * kFewTokens, "a thread per output");
+    if (m >= a.M || n0 + f >= a.N) return;
+    float sum[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        sum[j] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kFewWarps; ++i) sum[j] += red[i][j][m][f];
+    }
+    auto put = [&](int i, float val) { static_cast<T*>(a.out[i])[m * a.ldo[i] + n0 + f] = from_float<T>(val); };
+    if (GATE) {
+        if (a.out[0]) {
+            put(0, sum[0]);
+            put(1, sum[NT - 1]);
+        }
+        put(2, activate<false>(a.act, sum[0]).x * sum[NT - 1]);
+    } else {
+        put(0, sum[0]);
+    }
+}
+
 // Rows of `cols` values at any address -> rows of `ld` (a multiple of 8) at an aligned one: what TMA can read.
 template <typename T>
 __global__ void __launch_bounds__(256)
@@ -600,9 +720,44 @@ struct Block {
         if (!ok && err == cudaSuccess) err = cudaErrorInvalidValue;
     }
 
+    template <bool GATE>
+    void run_few(const FewArgs& a, bool vec) {
+        if (err != cudaSuccess) return;
+        const bool wide = a.M > 8;
+        auto* kernel = vec ? (wide ? ffn_few_kernel<T, GATE, true, true> : ffn_few_kernel<T, GATE, true, false>)
+                           : (wide ? ffn_few_kernel<T, GATE, false, true> : ffn_few_kernel<T, GATE, false, false>);
+        KernelScope scope(ctx, SAMA_K_FFN, GATE ? 0 : 1, st);
+        err = launch_dependent(kernel, dim3(blocks_of(a.N, 8)), dim3(32 * kFewWarps), 0, st, a);
+    }
+
     void forward(const void* x, const void* wg, const void* wu, const void* wd, void* y, void* gate, void* up) {
         const int M = (int)f.n_tokens, d = f.d, n = f.f;
         void* h = take((size_t)M * fp);
+        if (M <= kFewTokens) {
+            FewArgs a = {};
+            a.x = x;
+            a.w[0] = wg;
+            a.w[1] = wu;
+            void* outs[3] = {gate, up, h};
+            for (int i = 0; i < 3; ++i) a.out[i] = outs[i], a.ldo[i] = i < 2 ? n : fp;
+            a.ldx = d;
+            a.M = M;
+            a.N = n;
+            a.K = d;
+            a.act = f.act;
+            run_few<true>(a, vec_rows(x, d) && vec_rows(wg, d) && vec_rows(wu, d));
+            FewArgs b = {};
+            b.x = h;
+            b.w[0] = b.w[1] = wd;
+            b.out[0] = y;
+            b.ldo[0] = d;
+            b.ldx = fp;
+            b.M = M;
+            b.N = d;
+            b.K = n;
+            run_few<false>(b, vec_rows(wd, n));
+            return;
+        }
         const Matrix mx = readable(x, M, d), mg = readable(wg, n, d), mu = readable(wu, n, d), md = readable(wd, d, n);
         {
             Params<1> P = {};
