@@ -108,21 +108,40 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
 // ---------------------------------------------------------------- activations
 
 // a(x), and with GRAD its derivative.
-template <bool GRAD>
-__device__ __forceinline__ float2 activate(int act, float x) {
-    if (act == SAMA_ACT_SILU) {
+template <int ACT, bool GRAD>
+__device__ __forceinline__ float2 activate(float x) {
+    if constexpr (ACT == SAMA_ACT_SILU) {
         const float s = __fdividef(1.f, 1.f + __expf(-x));   // exp overflows to infinity for x < -88: s = 0, as it should
         return make_float2(x * s, GRAD ? s * fmaf(x, 1.f - s, 1.f) : 0.f);
+    } else if constexpr (ACT == SAMA_ACT_RELU) {
+        return make_float2(x > 0.f ? x : (x != x ? x : 0.f), x > 0.f ? 1.f : 0.f);
+    } else if constexpr (ACT == SAMA_ACT_GELU) {
+        // The normal distribution function by Abramowitz and Stegun 7.1.26, absolute error 7.5e-8, whose exponential is
+        // the density's: p(-|x|) = poly(t) exp(-x^2 / 2) / 2 with t = 1 / (1 + 0.3275911 |x| / sqrt 2).
+        const float e = __expf(-0.5f * x * x);
+        const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(x), 1.f));
+        float q = fmaf(1.061405429f, t, -1.453152027f);
+        q = fmaf(q, t, 1.421413741f);
+        q = fmaf(q, t, -0.284496736f);
+        q = fmaf(q, t, 0.254829592f);
+        q *= 0.5f * t * e;
+        const float p = x > 0.f ? 1.f - q : q;
+        return make_float2(x * p, GRAD ? fmaf(x * 0.39894228f, e, p) : 0.f);
+    } else {
+        // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
+        const float z2 = 1.59576912f * x * fmaf(0.044715f * x, x, 1.f);
+        const float p = __fdividef(1.f, 1.f + __expf(-z2));
+        return make_float2(x * p, GRAD ? fmaf(x * p * (1.f - p), 1.59576912f * fmaf(0.134145f * x, x, 1.f), p) : 0.f);
     }
-    if (act == SAMA_ACT_RELU) return make_float2(x > 0.f ? x : (x != x ? x : 0.f), x > 0.f ? 1.f : 0.f);
-    if (act == SAMA_ACT_GELU) {
-        const float p = 0.5f * erfcf(-0.70710678f * x);      // the normal distribution function, accurate in both tails
-        return make_float2(x * p, GRAD ? fmaf(x * 0.39894228f, __expf(-0.5f * x * x), p) : 0.f);
-    }
-    // gelu_tanh: 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
-    const float z2 = 1.59576912f * x * fmaf(0.044715f * x, x, 1.f);
-    const float p = __fdividef(1.f, 1.f + __expf(-z2));
-    return make_float2(x * p, GRAD ? fmaf(x * p * (1.f - p), 1.59576912f * fmaf(0.134145f * x, x, 1.f), p) : 0.f);
+}
+
+// Runs fn with the activation as a constant, so that the choice is made once and not per element.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& fn) {
+    if (act == SAMA_ACT_SILU) fn(std::integral_constant<int, SAMA_ACT_SILU>());
+    else if (act == SAMA_ACT_GELU) fn(std::integral_constant<int, SAMA_ACT_GELU>());
+    else if (act == SAMA_ACT_GELU_TANH) fn(std::integral_constant<int, SAMA_ACT_GELU_TANH>());
+    else fn(std::integral_constant<int, SAMA_ACT_RELU>());
 }
 
 // ---------------------------------------------------------------- stores
@@ -372,11 +391,15 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                     tmem_ld32(acc + TN + half * CU + c, u);
 #pragma unroll
                     for (int j = 0; j < 32; j += 2) {
-                        const float h0 = activate<false>(P.act, g[j]).x * u[j], h1 = activate<false>(P.act, g[j + 1]).x * u[j + 1];
                         pg[(c + j) / 2] = pack2<T>(g[j], g[j + 1]);
                         pu[(c + j) / 2] = pack2<T>(u[j], u[j + 1]);
-                        ph[(c + j) / 2] = pack2<T>(h0, h1);
                     }
+                    with_act(P.act, [&](auto kind) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2)
+                            ph[(c + j) / 2] = pack2<T>(activate<decltype(kind)::value, false>(g[j]).x * u[j],
+                                                       activate<decltype(kind)::value, false>(g[j + 1]).x * u[j + 1]);
+                    });
                 }
                 release();
                 const int col0 = tn * TN + half * CU;
@@ -434,14 +457,16 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                         const float dh[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
                         const uint32_t wg[4] = {vg[i].x, vg[i].y, vg[i].z, vg[i].w}, wu[4] = {vu[i].x, vu[i].y, vu[i].z, vu[i].w};
                         uint32_t og[4], ou[4], oh[4];
+                        with_act(P.act, [&](auto kind) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float2 g = unpack2<T>(wg[j]), u = unpack2<T>(wu[j]);
-                            const float2 a0 = activate<true>(P.act, g.x), a1 = activate<true>(P.act, g.y);
-                            og[j] = pack2<T>(dh[2 * j] * u.x * a0.y, dh[2 * j + 1] * u.y * a1.y);
-                            ou[j] = pack2<T>(dh[2 * j] * a0.x, dh[2 * j + 1] * a1.x);
-                            oh[j] = pack2<T>(a0.x * u.x, a1.x * u.y);
-                        }
+                            for (int j = 0; j < 4; ++j) {
+                                const float2 g = unpack2<T>(wg[j]), u = unpack2<T>(wu[j]);
+                                const float2 a0 = activate<decltype(kind)::value, true>(g.x), a1 = activate<decltype(kind)::value, true>(g.y);
+                                og[j] = pack2<T>(dh[2 * j] * u.x * a0.y, dh[2 * j + 1] * u.y * a1.y);
+                                ou[j] = pack2<T>(dh[2 * j] * a0.x, dh[2 * j + 1] * a1.x);
+                                oh[j] = pack2<T>(a0.x * u.x, a1.x * u.y);
+                            }
+                        });
                         const int64_t at = (int64_t)(row0 + r) * q.ldo[0] + col;   // all three have the same layout
                         *reinterpret_cast<uint4*>(static_cast<T*>(q.out[0]) + at) = make_uint4(og[0], og[1], og[2], og[3]);
                         *reinterpret_cast<uint4*>(static_cast<T*>(q.out[1]) + at) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
@@ -572,7 +597,7 @@ ffn_few_kernel(const __grid_constant__ FewArgs a) {
             put(0, sum[0]);
             put(1, sum[NT - 1]);
         }
-        put(2, activate<false>(a.act, sum[0]).x * sum[NT - 1]);
+        with_act(a.act, [&](auto kind) { put(2, activate<decltype(kind)::value, false>(sum[0]).x * sum[NT - 1]); });
     } else {
         put(0, sum[0]);
     }
