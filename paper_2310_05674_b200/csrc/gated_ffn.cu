@@ -20,11 +20,12 @@
 // Operands are read as they lie in memory: where the contraction runs along a matrix's rows, the tile is loaded and
 // described to the tensor core "MN-major" instead of being transposed by a pass of its own.
 //
-// Roles of the 10 warps: warp 0 copies (TMA, 128-byte swizzle, six 32 KB stages), warp 1 issues products, warps 2..9
-// read finished accumulators and store them through a shared-memory transpose while the next tile is multiplied (two
-// accumulators in tensor memory).  A CTA pair works on a 256 x 256 tile with cta_group::2 products; shapes with too few
+// Roles of the 10 warps: warp 0 copies (TMA, 128-byte swizzle, 32 KB stages), warp 1 issues products, warps 2..9 read
+// finished accumulators, and store them through a shared-memory transpose while the next tile is
+// multiplied (two accumulators in tensor memory).  A CTA pair works on a 256 x 256 tile with cta_group::2 products; shapes with too few
 // of those take 128 x 128 tiles on single CTAs.  Every wait is bounded: one that expires raises SAMA_DEV_TIMEOUT, stops
 // the CTA's work, lets its copies land and exits.
+#include <cstdlib>
 #include <type_traits>
 
 #include "num_types.h"
@@ -37,15 +38,20 @@ namespace {
 
 constexpr int BM = 128;         // rows of a CTA's share of the output tile
 constexpr int BK = 64;          // contraction per stage: one 128-byte row of 16-bit values
-constexpr int STAGES = 6;
 constexpr int OPERAND = BM * BK * 2;              // bytes of either operand's share of a stage
 constexpr int STAGE = 2 * OPERAND;
 constexpr int EPI = 8;          // epilogue warps
 constexpr int THREADS = 64 + 32 * EPI;
-constexpr int STAGING = 4096;   // bytes per epilogue warp
-constexpr int SMEM = STAGES * STAGE + EPI * STAGING + 256 + 1024;
 
 enum Mode { GATE_UP, PLAIN, D_HIDDEN };
+
+// Staging of one epilogue warp: 32 rows of 64 columns, in 16 bits, or (d-hidden) in fp32.  Rows of 64 columns because the
+// load and store units take a cycle per 128-byte line: with steps of 16 columns the d-hidden epilogue of a pair's tile
+// was 25 % slower, although twice as many warps shared it.
+__host__ __device__ constexpr int staging_of(int mode) { return mode == D_HIDDEN ? 8192 : 4096; }
+__host__ __device__ constexpr int stages_of(int mode) { return mode == D_HIDDEN ? 5 : 6; }
+__host__ __device__ constexpr int smem_of(int mode) { return stages_of(mode) * STAGE + EPI * staging_of(mode) + 256 + 1024; }
+
 
 struct Problem {
     CUtensorMap a[2], b[2];     // [1]: the second part of the contraction, or (gate-up) the second right operand
@@ -61,7 +67,10 @@ struct Problem {
 template <int G>
 struct alignas(64) Params {
     Problem p[G];
-    int n_items, group_m, act;
+    // Tiles in the order of the work: `whole` of them, then the others in `split` parts of their contraction each.
+    int n_items, whole, split, group_m, act;
+    float4* parts;      // sums of split tiles: [split tile][part][CTA of the tile][epilogue warp][64 columns / 4][32 rows]
+    int* arrived;       // [split tile][CTA of the tile][epilogue warp]: parts stored, zero between launches
     int32_t* status;
 };
 
@@ -105,21 +114,68 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
         ::"r"(dst), "l"(map), "r"(leader_bar), "r"(x), "r"(y) : "memory");
 }
 
+// 16 accumulator columns of this warp's 32 rows, from and to tensor memory.
+__device__ __forceinline__ void tmem_ld16_nowait(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float* v) {
+    uint32_t r[16];
+    tmem_ld16_nowait(taddr, r);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_ld16x2(uint32_t a0, uint32_t a1, float* v0, float* v1) {
+    uint32_t r0[16], r1[16];
+    tmem_ld16_nowait(a0, r0);
+    tmem_ld16_nowait(a1, r1);
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) { v0[i] = __uint_as_float(r0[i]); v1[i] = __uint_as_float(r1[i]); }
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const float* v) {
+    uint32_t r[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr));
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
 // ---------------------------------------------------------------- activations
+
+// 2^x and 1 / x to two units in the last place; results below the normal range are 0.
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.44269504f;
 
 // a(x), and with GRAD its derivative.
 template <int ACT, bool GRAD>
 __device__ __forceinline__ float2 activate(float x) {
     if constexpr (ACT == SAMA_ACT_SILU) {
-        const float s = __fdividef(1.f, 1.f + __expf(-x));   // exp overflows to infinity for x < -88: s = 0, as it should
+        const float s = fast_rcp(1.f + fast_exp2(-kLog2e * x));   // the power overflows to infinity for x < -88: s = 0, as it should
         return make_float2(x * s, GRAD ? s * fmaf(x, 1.f - s, 1.f) : 0.f);
     } else if constexpr (ACT == SAMA_ACT_RELU) {
         return make_float2(x > 0.f ? x : (x != x ? x : 0.f), x > 0.f ? 1.f : 0.f);
     } else if constexpr (ACT == SAMA_ACT_GELU) {
         // The normal distribution function by Abramowitz and Stegun 7.1.26, absolute error 7.5e-8, whose exponential is
         // the density's: p(-|x|) = poly(t) exp(-x^2 / 2) / 2 with t = 1 / (1 + 0.3275911 |x| / sqrt 2).
-        const float e = __expf(-0.5f * x * x);
-        const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678f, fabsf(x), 1.f));
+        const float e = fast_exp2(-0.5f * kLog2e * x * x);
+        const float t = fast_rcp(fmaf(0.3275911f * 0.70710678f, fabsf(x), 1.f));
         float q = fmaf(1.061405429f, t, -1.453152027f);
         q = fmaf(q, t, 1.421413741f);
         q = fmaf(q, t, -0.284496736f);
@@ -130,7 +186,7 @@ __device__ __forceinline__ float2 activate(float x) {
     } else {
         // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
         const float z2 = 1.59576912f * x * fmaf(0.044715f * x, x, 1.f);
-        const float p = __fdividef(1.f, 1.f + __expf(-z2));
+        const float p = fast_rcp(1.f + fast_exp2(-kLog2e * z2));
         return make_float2(x * p, GRAD ? fmaf(x * p * (1.f - p), 1.59576912f * fmaf(0.134145f * x, x, 1.f), p) : 0.f);
     }
 }
@@ -153,6 +209,7 @@ __device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, T
                                            int col0, int cols, bool vec, int lane) {
     constexpr int LPR = CU / 8;  // 16-byte chunks of a row
     auto at = [](int r, int c) { return r * LPR + (c ^ (LPR == 8 ? (r & 7) : ((r >> 1) & 3))); };
+    static_assert(CU == 64 || CU == 32, "rows of 128 or 64 bytes");
     __syncwarp();
 #pragma unroll
     for (int c = 0; c < LPR; ++c)
@@ -171,13 +228,12 @@ __device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, T
         // rows that start anywhere: neighbouring lanes take neighbouring elements
         const T* s = reinterpret_cast<const T*>(stg);
 #pragma unroll 4
-        for (int r = 0; r < 32; ++r)
-            if (r < rows)
+        for (int r = 0; r < min(rows, 32); ++r)
 #pragma unroll
-                for (int j = 0; j < CU / 32; ++j) {
-                    const int c = lane + 32 * j;
-                    if (col0 + c < cols) dst[(int64_t)(row0 + r) * ld + col0 + c] = s[at(r, c >> 3) * 8 + (c & 7)];
-                }
+            for (int j = 0; j < CU / 32; ++j) {
+                const int c = lane + 32 * j;
+                if (col0 + c < cols) dst[(int64_t)(row0 + r) * ld + col0 + c] = s[at(r, c >> 3) * 8 + (c & 7)];
+            }
     }
 }
 
@@ -200,6 +256,7 @@ __device__ __forceinline__ uint4 load8(const T* p, int col, int cols, bool vec) 
 template <typename T, int MODE, bool PAIR, bool A_MN, bool B_MN, int G>
 __global__ void __launch_bounds__(THREADS, 1)
 ffn_kernel(const __grid_constant__ Params<G> P) {
+    constexpr int STAGES = stages_of(MODE), STAGING = staging_of(MODE);
     constexpr int BN = PAIR ? 256 : 128;                // accumulator columns
     constexpr int TN = MODE == GATE_UP ? BN / 2 : BN;   // output columns (features) of a tile
     constexpr int TM = PAIR ? 2 * BM : BM;
@@ -223,18 +280,33 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
     const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
     const int unit = (int)blockIdx.x / (PAIR ? 2 : 1), n_units = (int)gridDim.x / (PAIR ? 2 : 1);
 
-    // Work item -> problem and tile.  Items that run together cover group_m row tiles of a few column tiles, so that
-    // one wave's operands come out of L2.
-    auto locate = [&](int item, int& tm, int& tn) -> const Problem& {
+    // Work item -> problem, tile and range of k-blocks.  Tiles that run together cover group_m row tiles of a few column
+    // tiles, so that one wave's operands come out of L2.
+    struct Work { int tm, tn, kb0, kb1, part, split_tile; };   // split_tile < 0: a whole tile
+    auto locate = [&](int item, Work& w) -> const Problem& {
+        const int over = item - P.whole;
+        int tile = item;
+        w.split_tile = -1;
+        if (over >= 0) {
+            w.split_tile = over / P.split;
+            w.part = over - w.split_tile * P.split;
+            tile = P.whole + w.split_tile;
+        }
         int g = 0;
 #pragma unroll
         for (int i = 1; i < G; ++i)
-            if (item >= P.p[i].item0) g = i;
+            if (tile >= P.p[i].item0) g = i;
         const Problem& q = P.p[g];
-        const int t = item - q.item0, per_group = P.group_m * q.tiles_n, group = t / per_group, rem = t - group * per_group;
+        w.kb0 = 0;
+        w.kb1 = q.num_kb;
+        if (over >= 0) {
+            w.kb0 = (int)((int64_t)q.num_kb * w.part / P.split);
+            w.kb1 = (int)((int64_t)q.num_kb * (w.part + 1) / P.split);
+        }
+        const int t = tile - q.item0, per_group = P.group_m * q.tiles_n, group = t / per_group, rem = t - group * per_group;
         const int first = group * P.group_m, size = min(P.group_m, q.tiles_m - first);
-        tm = first + rem % size;
-        tn = rem / size;
+        w.tm = first + rem % size;
+        w.tn = rem / size;
         return q;
     };
 
@@ -273,11 +345,11 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
             uint32_t empty_parity = 1;
             bool ok = true;
             for (int item = unit; ok && item < P.n_items; item += n_units) {
-                int tm, tn;
-                const Problem& q = locate(item, tm, tn);
-                const int m0 = tm * TM + (int)rank * BM;
-                const int n0 = tn * TN + (PAIR && MODE != GATE_UP ? (int)rank * BM : 0);
-                for (int kb = 0; kb < q.num_kb; ++kb) {
+                Work w;
+                const Problem& q = locate(item, w);
+                const int m0 = w.tm * TM + (int)rank * BM;
+                const int n0 = w.tn * TN + (PAIR && MODE != GATE_UP ? (int)rank * BM : 0);
+                for (int kb = w.kb0; kb < w.kb1; ++kb) {
                     if (issued >= STAGES && !mbar_wait(empty_bar(s), empty_parity, abort_flag)) { raise_timeout(); ok = false; break; }
                     const uint32_t sa = base + s * STAGE, sb = sa + OPERAND;
                     const int part = MODE != GATE_UP && kb >= q.kb_first;
@@ -320,13 +392,13 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
             uint32_t full_parity = 0;
             bool ok = true;
             for (int item = unit; ok && item < P.n_items; item += n_units, ++t) {
-                int tm, tn;
-                const Problem& q = locate(item, tm, tn);
+                Work w;
+                locate(item, w);
                 const int buf = t & 1;
                 if (t >= 2 && !mbar_wait(acc_empty_bar(buf), ((t >> 1) - 1) & 1, abort_flag)) { raise_timeout(); break; }
                 tc_fence_after();
                 const uint32_t acc = tmem_base + (uint32_t)buf * BN;
-                for (int kb = 0; kb < q.num_kb; ++kb) {
+                for (int kb = w.kb0; kb < w.kb1; ++kb) {
                     if (!mbar_wait(full_bar(s), full_parity, abort_flag)) { raise_timeout(); ok = false; break; }
                     tc_fence_after();
                     const uint32_t sa = base + s * STAGE, sb = sa + OPERAND;
@@ -335,8 +407,8 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                     for (int k = 0; k < BK / 16; ++k) {
                         // 16 of the contraction: 32 bytes along a K-major row, 16 rows of 128 bytes of an MN-major tile
                         const uint64_t ka = (uint64_t)((A_MN ? k * 2048 : k * 32) >> 4), kbo = (uint64_t)((B_MN ? k * 2048 : k * 32) >> 4);
-                        if (PAIR) umma16_pair(acc, da + ka, db + kbo, IDESC, kb > 0 || k > 0);
-                        else umma16(acc, da + ka, db + kbo, IDESC, kb > 0 || k > 0);
+                        if (PAIR) umma16_pair(acc, da + ka, db + kbo, IDESC, kb > w.kb0 || k > 0);
+                        else umma16(acc, da + ka, db + kbo, IDESC, kb > w.kb0 || k > 0);
                     }
                     if (PAIR) umma_commit_pair(empty_bar(s)); else umma_commit(empty_bar(s));
                     if (++s == STAGES) { s = 0; full_parity ^= 1u; }
@@ -348,19 +420,38 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
     } else {
         // ---------------------------------------------------------- epilogue
         const int quarter = warp & 3;               // a warp may only touch TMEM lanes [32 quarter, 32 quarter + 32)
-        const int half = (warp - 2) >> 2;           // which half of the tile's columns
+        const int share = (warp - 2) >> 2;          // which CPW of the accumulator's columns (gate-up: half of G, half of U)
+        constexpr int CPW = BN / (EPI / 4), STEPS = CPW / 16;
         const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
         uint4* stg = reinterpret_cast<uint4*>(smem_raw + (staging - raw) + (warp - 2) * STAGING);
         const int my_tiles = unit < P.n_items ? (P.n_items - unit + n_units - 1) / n_units : 0;
         bool ok = true;
         int t = 0;
         for (int item = unit; item < P.n_items; item += n_units, ++t) {
-            int tm, tn;
-            const Problem& q = locate(item, tm, tn);
+            Work w;
+            const Problem& q = locate(item, w);
+            const int tn = w.tn;
             const int buf = t & 1;
-            const int row0 = tm * TM + (int)rank * BM + quarter * 32;
+            const int row0 = w.tm * TM + (int)rank * BM + quarter * 32;
             const int rows = min(32, q.M - row0);   // may be negative: nothing to store
             const uint32_t acc = lane_addr + (uint32_t)buf * BN;
+            // d-hidden: a lane handles eight columns of rows lane / 8 + 4 i.  It has G and U of four rows at a time in
+            // registers; those of the first four are on their way while the tile is still being multiplied.
+            const int c8 = lane & 7, r0 = lane >> 3;
+            uint4 vg[4], vu[4];
+            auto load_gu = [&](int i0, int col) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = r0 + 4 * (i0 + i);
+                    vg[i] = vu[i] = make_uint4(0, 0, 0, 0);
+                    if (r < rows && col < q.N) {
+                        vg[i] = load8(static_cast<const T*>(q.in[0]) + (int64_t)(row0 + r) * q.ldi, col, q.N, q.vec_in & 1);
+                        vu[i] = load8(static_cast<const T*>(q.in[1]) + (int64_t)(row0 + r) * q.ldi, col, q.N, q.vec_in & 2);
+                    }
+                }
+            };
+            const int dh_col = tn * TN + share * CPW + 8 * c8;
+            if (MODE == D_HIDDEN) load_gu(0, dh_col);
             if (lane == 0) {
                 // the tile is complete when its barrier flips, or never if another role gave up
                 const long long t0 = clock64();
@@ -381,97 +472,138 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                     if (PAIR) mbar_arrive_cluster(acc_empty_bar(buf) & kPeerBitMask); else mbar_arrive(acc_empty_bar(buf));
                 }
             };
-            if constexpr (MODE == GATE_UP) {
-                constexpr int CU = TN / 2;          // features per warp: 64 or 32
-                uint32_t pg[CU / 2], pu[CU / 2], ph[CU / 2];
+            // gate-up: half of the steps are columns of G, the others the same columns of U
+            auto column = [&](int step) {
+                return MODE == GATE_UP ? (step / (STEPS / 2)) * TN + share * (CPW / 2) + step % (STEPS / 2) * 16 : share * CPW + step * 16;
+            };
+            // A tile whose contraction is split: every part's warps leave their sums in the workspace; the one that finds
+            // all others there adds them up in the order of the parts (its own among them), puts the result back into
+            // tensor memory and goes on with it.
+            if (w.split_tile >= 0) {
+                constexpr int CTAS = PAIR ? 2 : 1, SLAB = STEPS * 4 * 32;
+                const int64_t stride = (int64_t)CTAS * EPI * SLAB;
+                float4* base = P.parts + (((int64_t)w.split_tile * P.split * CTAS + rank) * EPI + (warp - 2)) * SLAB + lane;
+#pragma unroll 1
+                for (int st = 0; st < STEPS; ++st) {
+                    float v[16];
+                    tmem_ld16(acc + column(st), v);
 #pragma unroll
-                for (int c = 0; c < CU; c += 32) {
-                    float g[32], u[32];
-                    tmem_ld32(acc + half * CU + c, g);
-                    tmem_ld32(acc + TN + half * CU + c, u);
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        pg[(c + j) / 2] = pack2<T>(g[j], g[j + 1]);
-                        pu[(c + j) / 2] = pack2<T>(u[j], u[j + 1]);
-                    }
-                    with_act(P.act, [&](auto kind) {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2)
-                            ph[(c + j) / 2] = pack2<T>(activate<decltype(kind)::value, false>(g[j]).x * u[j],
-                                                       activate<decltype(kind)::value, false>(g[j + 1]).x * u[j + 1]);
-                    });
+                    for (int k = 0; k < 4; ++k)
+                        __stcg(base + w.part * stride + (st * 4 + k) * 32, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
                 }
+                __threadfence();
+                __syncwarp();
+                int* counter = P.arrived + (w.split_tile * CTAS + (int)rank) * EPI + (warp - 2);
+                int before = 0;
+                if (lane == 0) before = atomicAdd(counter, 1);
+                before = __shfl_sync(0xffffffffu, before, 0);
+                if (before != P.split - 1) {
+                    release();
+                    continue;
+                }
+                if (lane == 0) *counter = 0;
+                __threadfence();
+#pragma unroll 1
+                for (int st = 0; st < STEPS; ++st) {
+                    float sum[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[j] = 0.f;
+#pragma unroll 2
+                    for (int p = 0; p < P.split; ++p)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float4 x = __ldcg(base + p * stride + (st * 4 + k) * 32);
+                            sum[4 * k] += x.x; sum[4 * k + 1] += x.y; sum[4 * k + 2] += x.z; sum[4 * k + 3] += x.w;
+                        }
+                    tmem_st16(acc + column(st), sum);
+                }
+            }
+            if constexpr (MODE == GATE_UP) {
+                constexpr int CU = CPW / 2;         // features per warp: 64 or 32
+                uint32_t pg[CU / 2], pu[CU / 2], ph[CU / 2];
+                with_act(P.act, [&](auto kind) {
+#pragma unroll
+                    for (int st = 0; st < STEPS / 2; ++st) {
+                        float g[16], u[16];
+                        tmem_ld16x2(acc + column(st), acc + column(st + STEPS / 2), g, u);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            pg[8 * st + j] = pack2<T>(g[2 * j], g[2 * j + 1]);
+                            pu[8 * st + j] = pack2<T>(u[2 * j], u[2 * j + 1]);
+                            ph[8 * st + j] = pack2<T>(activate<decltype(kind)::value, false>(g[2 * j]).x * u[2 * j],
+                                                      activate<decltype(kind)::value, false>(g[2 * j + 1]).x * u[2 * j + 1]);
+                        }
+                    }
+                });
                 release();
-                const int col0 = tn * TN + half * CU;
+                const int col0 = tn * TN + share * CU;
                 if (q.out[0]) {
                     store_rows<T, CU>(stg, pg, static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, col0, q.cols[0], q.vec_out & 1, lane);
                     store_rows<T, CU>(stg, pu, static_cast<T*>(q.out[1]), q.ldo[1], row0, rows, col0, q.cols[1], q.vec_out & 2, lane);
                 }
                 store_rows<T, CU>(stg, ph, static_cast<T*>(q.out[2]), q.ldo[2], row0, rows, col0, q.cols[2], q.vec_out & 4, lane);
             } else if constexpr (MODE == PLAIN) {
-#pragma unroll
-                for (int c = 0; c < TN / 2; c += 64) {
+#pragma unroll 1
+                for (int c = 0; c < CPW; c += 64) {
                     uint32_t packed[32];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         float v[32];
-                        tmem_ld32(acc + half * (TN / 2) + c + 32 * i, v);
+                        tmem_ld32(acc + share * CPW + c + 32 * i, v);
 #pragma unroll
-                        for (int j = 0; j < 32; j += 2) packed[16 * i + j / 2] = pack2<T>(v[j], v[j + 1]);
+                        for (int j = 0; j < 16; ++j) packed[16 * i + j] = pack2<T>(v[2 * j], v[2 * j + 1]);
                     }
-                    if (c + 64 >= TN / 2) release();
-                    store_rows<T, 64>(stg, packed, static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, tn * TN + half * (TN / 2) + c,
+                    if (c + 64 == CPW) release();
+                    store_rows<T, 64>(stg, packed, static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, tn * TN + share * CPW + c,
                                       q.cols[0], q.vec_out & 1, lane);
                 }
             } else {
-                // The block goes through shared memory in fp32, so that G and U are read, and dG, dU and H written,
-                // in row segments of 64 bytes: a lane handles eight columns of rows lane / 4 + 8 i.
-                float4* sf = reinterpret_cast<float4*>(stg);
-                const int c8 = lane & 3, r0 = lane >> 2;
+                // The block goes through shared memory in fp32, so that G and U are read, and dG, dU and H written, in
+                // row segments of 128 bytes.
+                float4* sf = reinterpret_cast<float4*>(stg);   // 32 rows of sixteen 16-byte chunks, permuted by row
+                auto at = [](int r, int c) { return r * 16 + (c ^ (r & 7)); };
 #pragma unroll 1
-                for (int c = 0; c < TN / 2; c += 32) {
-                    const int col = tn * TN + half * (TN / 2) + c + 8 * c8;
-                    uint4 vg[4], vu[4];
+                for (int c = 0; c < CPW; c += 64) {
+                    const int col = dh_col + c;
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = r0 + 8 * i;
-                        vg[i] = vu[i] = make_uint4(0, 0, 0, 0);
-                        if (r < rows && col < q.N) {
-                            vg[i] = load8(static_cast<const T*>(q.in[0]) + (int64_t)(row0 + r) * q.ldi, col, q.N, q.vec_in & 1);
-                            vu[i] = load8(static_cast<const T*>(q.in[1]) + (int64_t)(row0 + r) * q.ldi, col, q.N, q.vec_in & 2);
-                        }
+                    for (int i = 0; i < 2; ++i) {
+                        float v[32];
+                        tmem_ld32(acc + share * CPW + c + 32 * i, v);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) sf[at(lane, 8 * i + k)] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                     }
-                    float v[32];
-                    tmem_ld32(acc + half * (TN / 2) + c, v);
-                    if (c + 32 >= TN / 2) release();
+                    if (c + 64 == CPW) release();
                     __syncwarp();
+                    with_act(P.act, [&](auto kind) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        sf[lane * 8 + (k ^ (lane & 7))] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
-                    __syncwarp();
+                        for (int h = 0; h < 2; ++h) {
+                            const uint4 cg[4] = {vg[0], vg[1], vg[2], vg[3]}, cu[4] = {vu[0], vu[1], vu[2], vu[3]};
+                            if (h == 0) load_gu(4, col);
+                            else if (c + 64 < CPW) load_gu(0, col + 64);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = r0 + 8 * i;
-                        if (r >= rows || col >= q.cols[0]) continue;
-                        const float4 d0 = sf[r * 8 + ((2 * c8) ^ (r & 7))], d1 = sf[r * 8 + ((2 * c8 + 1) ^ (r & 7))];
-                        const float dh[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
-                        const uint32_t wg[4] = {vg[i].x, vg[i].y, vg[i].z, vg[i].w}, wu[4] = {vu[i].x, vu[i].y, vu[i].z, vu[i].w};
-                        uint32_t og[4], ou[4], oh[4];
-                        with_act(P.act, [&](auto kind) {
+                            for (int i = 0; i < 4; ++i) {
+                                const int r = r0 + 4 * (4 * h + i);
+                                if (r >= rows || col >= q.cols[0]) continue;
+                                const float4 d0 = sf[at(r, 2 * c8)], d1 = sf[at(r, 2 * c8 + 1)];
+                                const float dh[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
+                                const uint32_t wg[4] = {cg[i].x, cg[i].y, cg[i].z, cg[i].w}, wu[4] = {cu[i].x, cu[i].y, cu[i].z, cu[i].w};
+                                uint32_t og[4], ou[4], oh[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float2 g = unpack2<T>(wg[j]), u = unpack2<T>(wu[j]);
-                                const float2 a0 = activate<decltype(kind)::value, true>(g.x), a1 = activate<decltype(kind)::value, true>(g.y);
-                                og[j] = pack2<T>(dh[2 * j] * u.x * a0.y, dh[2 * j + 1] * u.y * a1.y);
-                                ou[j] = pack2<T>(dh[2 * j] * a0.x, dh[2 * j + 1] * a1.x);
-                                oh[j] = pack2<T>(a0.x * u.x, a1.x * u.y);
+                                for (int j = 0; j < 4; ++j) {
+                                    const float2 g = unpack2<T>(wg[j]), u = unpack2<T>(wu[j]);
+                                    const float2 a0 = activate<decltype(kind)::value, true>(g.x), a1 = activate<decltype(kind)::value, true>(g.y);
+                                    og[j] = pack2<T>(dh[2 * j] * u.x * a0.y, dh[2 * j + 1] * u.y * a1.y);
+                                    ou[j] = pack2<T>(dh[2 * j] * a0.x, dh[2 * j + 1] * a1.x);
+                                    oh[j] = pack2<T>(a0.x * u.x, a1.x * u.y);
+                                }
+                                const int64_t to = (int64_t)(row0 + r) * q.ldo[0] + col;   // all three have the same layout
+                                *reinterpret_cast<uint4*>(static_cast<T*>(q.out[0]) + to) = make_uint4(og[0], og[1], og[2], og[3]);
+                                *reinterpret_cast<uint4*>(static_cast<T*>(q.out[1]) + to) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
+                                *reinterpret_cast<uint4*>(static_cast<T*>(q.out[2]) + to) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
                             }
-                        });
-                        const int64_t at = (int64_t)(row0 + r) * q.ldo[0] + col;   // all three have the same layout
-                        *reinterpret_cast<uint4*>(static_cast<T*>(q.out[0]) + at) = make_uint4(og[0], og[1], og[2], og[3]);
-                        *reinterpret_cast<uint4*>(static_cast<T*>(q.out[1]) + at) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
-                        *reinterpret_cast<uint4*>(static_cast<T*>(q.out[2]) + at) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
-                    }
+                        }
+                    });
                 }
             }
         }
@@ -649,42 +781,54 @@ bool operand_map(CUtensorMap* map, const Matrix& m, int dtype, bool mn_major, in
 
 inline int blocks_of(int64_t x, int b) { return (int)((x + b - 1) / b); }
 
+// How a launch's tiles are worked on.
+struct TilePlan {
+    bool pair;
+    int whole, split;
+};
+constexpr int kMaxSplitTiles = 256, kMaxSplitParts = 512;   // of 128 x 128 values per CTA; twice as many per CTA of a pair
+
 template <typename T, int MODE, bool PAIR, bool A_MN, bool B_MN, int G>
-cudaError_t launch_ffn(sama_ctx* ctx, Params<G>& P, int kind, cudaStream_t st) {
+cudaError_t launch_ffn(sama_ctx* ctx, Params<G>& P, int kind, const TilePlan& plan, cudaStream_t st) {
     auto* kernel = ffn_kernel<T, MODE, PAIR, A_MN, B_MN, G>;
     const uint32_t bit = 1u << (4 * kind + (PAIR ? 2 : 0) + (std::is_same<T, __half>::value ? 1 : 0));
     if (!(ctx->ffn_ready & bit)) {  // once per context: the opt-in to this much shared memory
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(MODE));
         if (e != cudaSuccess) return e;
         ctx->ffn_ready |= bit;
     }
     const int tm = PAIR ? 2 * BM : BM, tn = (PAIR ? 256 : 128) / (MODE == GATE_UP ? 2 : 1);
-    int items = 0;
+    int tiles = 0;
     for (int g = 0; g < G; ++g) {
         Problem& q = P.p[g];
         q.tiles_m = blocks_of(q.M, tm);
         q.tiles_n = blocks_of(q.N, tn);
-        q.item0 = items;
-        items += q.tiles_m * q.tiles_n;
+        q.item0 = tiles;
+        tiles += q.tiles_m * q.tiles_n;
     }
-    P.n_items = items;
+    P.whole = plan.whole;
+    P.split = plan.split;
+    P.n_items = plan.whole + (tiles - plan.whole) * plan.split;
+    P.parts = reinterpret_cast<float4*>(ctx->ffn_parts);
+    P.arrived = ctx->ffn_arrived;
     P.group_m = 8;
     P.status = &ctx->scalars->status;
-    const int max_units = PAIR ? ctx->ffn_pair_units : ctx->sm_count;
+    const int max_units = PAIR ? ctx->ffn_pair_units : ctx->sm_count, items = P.n_items;
     const int units = items < max_units ? items : max_units;
     KernelScope scope(ctx, SAMA_K_FFN, kind, st);
-    return launch_clustered(PAIR ? 2 : 1, kernel, dim3(units * (PAIR ? 2 : 1)), dim3(THREADS), (size_t)SMEM, st, P);
+    return launch_clustered(PAIR ? 2 : 1, kernel, dim3(units * (PAIR ? 2 : 1)), dim3(THREADS), (size_t)smem_of(MODE), st, P);
 }
 
-// CTA pairs of the kernel that can be resident (asked once per context).
-cudaError_t find_pair_units(sama_ctx* ctx) {
+// Once per context: how many CTA pairs of the kernel can be resident, and the workspace of split tiles.
+cudaError_t prepare_ffn(sama_ctx* ctx) {
+    if (ctx->ffn_pair_units > 0) return cudaSuccess;
     auto* kernel = ffn_kernel<__nv_bfloat16, PLAIN, true, false, false, 1>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(PLAIN));
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (ctx->sm_count / 2));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = SMEM;
+    cfg.dynamicSmemBytes = smem_of(PLAIN);
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
@@ -694,12 +838,46 @@ cudaError_t find_pair_units(sama_ctx* ctx) {
     cfg.numAttrs = 1;
     int clusters = 0;
     if ((e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg)) != cudaSuccess) return e;
+    if (clusters < 1) return cudaErrorLaunchOutOfResources;
+    const size_t counters = sizeof(int) * kMaxSplitTiles * 2 * EPI;
+    if (!ctx->ffn_parts && (e = cudaMalloc(&ctx->ffn_parts, sizeof(float) * kMaxSplitParts * BM * 128)) != cudaSuccess) return e;
+    if (!ctx->ffn_arrived && (e = cudaMalloc(&ctx->ffn_arrived, counters)) != cudaSuccess) return e;
+    if ((e = cudaMemset(ctx->ffn_arrived, 0, counters)) != cudaSuccess || (e = cudaDeviceSynchronize()) != cudaSuccess) return e;
     ctx->ffn_pair_units = clusters < ctx->sm_count / 2 ? clusters : ctx->sm_count / 2;
-    return ctx->ffn_pair_units > 0 ? cudaSuccess : cudaErrorLaunchOutOfResources;
+    return cudaSuccess;
 }
 
-// Pairs of CTAs where their tiles keep most of the machine busy, single CTAs otherwise.
-bool use_pairs(const sama_ctx* ctx, int64_t pair_tiles) { return pair_tiles * 4 >= (int64_t)ctx->ffn_pair_units * 3; }
+// The fastest plan by estimate.  A launch's time is its rounds of tiles, each the longer of multiplying it and storing the
+// one before; a last round that would leave half of the units without a tile (or the only one) splits the contraction
+// of its tiles instead, which costs an exchange through L2.
+TilePlan plan_tiles(const sama_ctx* ctx, const Problem* p, int n, bool gate_up) {
+    static const char* force = getenv("FFN_PLAN");
+    TilePlan best = {false, 1 << 30, 1};
+    double best_cost = -1.0;
+    for (int pair = 0; pair < 2; ++pair) {
+        const int tm = pair ? 256 : 128, tn = (pair ? 256 : 128) / (gate_up ? 2 : 1), units = pair ? ctx->ffn_pair_units : ctx->sm_count;
+        const double t_kb = pair ? 0.28 : 0.16, t_store = pair ? 4.0 : 2.5, t_exchange = pair ? 4.0 : 2.5;
+        int64_t tiles = 0;
+        int least_kb = 1 << 30, most_kb = 0;
+        for (int i = 0; i < n; ++i) {
+            if (p[i].M == 0) continue;
+            tiles += (int64_t)blocks_of(p[i].M, tm) * blocks_of(p[i].N, tn);
+            least_kb = p[i].num_kb < least_kb ? p[i].num_kb : least_kb;
+            most_kb = p[i].num_kb > most_kb ? p[i].num_kb : most_kb;
+        }
+        const double t_tile = most_kb * t_kb > t_store ? most_kb * t_kb : t_store;
+        const int64_t rounds = tiles / units, rest = tiles - rounds * units;
+        for (int split = 1; split <= 8; ++split) {
+            if (split > 1 && (rest * split > units || rest > kMaxSplitTiles || rest * split * (pair ? 4 : 1) > kMaxSplitParts || least_kb < 4 * split || rest == 0)) break;
+            const double cost = rounds * t_tile + (rest ? most_kb * t_kb / split : 0.0) + t_store + (split > 1 ? t_exchange : 0.0);
+            if (force ? (force[0] - '0' == pair && force[1] - '0' == split) : (best_cost < 0.0 || cost < best_cost)) {
+                best_cost = cost;
+                best = {pair != 0, split > 1 ? (int)(rounds * units) : (int)tiles, split};
+            }
+        }
+    }
+    return best;
+}
 
 void set_output(Problem& q, int i, void* p, int ld, int cols) {
     q.out[i] = p;
@@ -737,9 +915,14 @@ struct Block {
         return {dst, rows, cols, ld};
     }
     template <int MODE, bool A_MN, bool B_MN, int G>
-    void run(Params<G>& P, int kind, bool pair) {
+    void run(Params<G>& P, int kind, const TilePlan& plan) {
         if (err != cudaSuccess) return;
-        err = pair ? launch_ffn<T, MODE, true, A_MN, B_MN, G>(ctx, P, kind, st) : launch_ffn<T, MODE, false, A_MN, B_MN, G>(ctx, P, kind, st);
+        err = plan.pair ? launch_ffn<T, MODE, true, A_MN, B_MN, G>(ctx, P, kind, plan, st)
+                        : launch_ffn<T, MODE, false, A_MN, B_MN, G>(ctx, P, kind, plan, st);
+    }
+    template <int MODE, bool A_MN, bool B_MN, int G>
+    void run(Params<G>& P, int kind) {
+        run<MODE, A_MN, B_MN, G>(P, kind, plan_tiles(ctx, P.p, G, MODE == GATE_UP));
     }
     void check(bool ok) {
         if (!ok && err == cudaSuccess) err = cudaErrorInvalidValue;
@@ -787,17 +970,17 @@ struct Block {
         {
             Params<1> P = {};
             Problem& q = P.p[0];
-            const bool pair = use_pairs(ctx, (int64_t)blocks_of(M, 2 * BM) * blocks_of(n, 128));
-            check(operand_map(&q.a[0], mx, f.dtype, false) && operand_map(&q.b[0], mg, f.dtype, false, pair ? 128 : 64) &&
-                  operand_map(&q.b[1], mu, f.dtype, false, pair ? 128 : 64));
             q.M = M;
             q.N = n;
             q.num_kb = q.kb_first = blocks_of(d, BK);
+            const TilePlan plan = plan_tiles(ctx, &q, 1, true);
+            check(operand_map(&q.a[0], mx, f.dtype, false) && operand_map(&q.b[0], mg, f.dtype, false, plan.pair ? 128 : 64) &&
+                  operand_map(&q.b[1], mu, f.dtype, false, plan.pair ? 128 : 64));
             set_output(q, 0, gate, n, n);
             set_output(q, 1, up, n, n);
             set_output(q, 2, h, fp, fp);
             P.act = f.act;
-            run<GATE_UP, false, false, 1>(P, 0, pair);
+            run<GATE_UP, false, false, 1>(P, 0, plan);
         }
         Params<1> P = {};
         Problem& q = P.p[0];
@@ -806,7 +989,7 @@ struct Block {
         q.N = d;
         q.num_kb = q.kb_first = blocks_of(n, BK);
         set_output(q, 0, y, d, d);
-        run<PLAIN, false, false, 1>(P, 1, use_pairs(ctx, (int64_t)blocks_of(M, 2 * BM) * blocks_of(d, 256)));
+        run<PLAIN, false, false, 1>(P, 1);
     }
 
     void backward(const void* x, const void* wg, const void* wu, const void* wd, const void* gate, const void* up,
@@ -830,7 +1013,7 @@ struct Block {
             q.ldi = n;
             q.vec_in = (vec_rows(gate, n) ? 1 : 0) | (vec_rows(up, n) ? 2 : 0);
             P.act = f.act;
-            run<D_HIDDEN, false, true, 1>(P, 2, use_pairs(ctx, (int64_t)blocks_of(M, 2 * BM) * blocks_of(n, 256)));
+            run<D_HIDDEN, false, true, 1>(P, 2);
         }
         const Matrix mdg = {dg, M, n, fp}, mdu = {du, M, n, fp}, mh = {h, M, n, fp};
         if (dx) {
@@ -844,14 +1027,13 @@ struct Block {
             q.kb_first = blocks_of(n, BK);
             q.num_kb = 2 * q.kb_first;
             set_output(q, 0, dx, d, d);
-            run<PLAIN, false, true, 1>(P, 3, use_pairs(ctx, (int64_t)blocks_of(M, 2 * BM) * blocks_of(d, 256)));
+            run<PLAIN, false, true, 1>(P, 3);
         }
         if (!dwg && !dwu && !dwd) return;
         const Matrix mx = (dwg || dwu) ? readable(x, M, d) : my;
         Params<3> P = {};
         struct { const Matrix* a; const Matrix* b; void* out; int rows, cols; } w[3] = {
             {&mdg, &mx, dwg, n, d}, {&mdu, &mx, dwu, n, d}, {&my, &mh, dwd, d, n}};
-        int64_t tiles = 0;
         for (int i = 0; i < 3; ++i) {
             Problem& q = P.p[i];
             check(operand_map(&q.a[0], *w[i].a, f.dtype, true) && operand_map(&q.b[0], *w[i].b, f.dtype, true));
@@ -859,9 +1041,8 @@ struct Block {
             q.N = w[i].cols;
             q.num_kb = q.kb_first = blocks_of(M, BK);
             set_output(q, 0, w[i].out, w[i].cols, w[i].cols);
-            tiles += (int64_t)blocks_of(q.M, 2 * BM) * blocks_of(q.N, 256);
         }
-        run<PLAIN, true, true, 3>(P, 4, use_pairs(ctx, tiles));
+        run<PLAIN, true, true, 3>(P, 4);
     }
 };
 
@@ -877,10 +1058,8 @@ size_t ffn_workspace(const FfnShape& f, bool grad, bool copies) {
 
 cudaError_t launch_ffn_forward(sama_ctx* ctx, const FfnShape& f, const void* x, const void* wg, const void* wu,
                                const void* wd, void* y, void* gate, void* up, void* ws, cudaStream_t st) {
-    if (ctx->ffn_pair_units == 0) {
-        const cudaError_t e = find_pair_units(ctx);
-        if (e != cudaSuccess) return e;
-    }
+    const cudaError_t e = prepare_ffn(ctx);
+    if (e != cudaSuccess) return e;
     if (f.dtype == SAMA_BF16) {
         Block<__nv_bfloat16> b{ctx, f, static_cast<uint8_t*>(ws), st, up8(f.f)};
         b.forward(x, wg, wu, wd, y, gate, up);
@@ -894,10 +1073,8 @@ cudaError_t launch_ffn_forward(sama_ctx* ctx, const FfnShape& f, const void* x, 
 cudaError_t launch_ffn_backward(sama_ctx* ctx, const FfnShape& f, const void* x, const void* wg, const void* wu,
                                 const void* wd, const void* gate, const void* up, const void* dy, void* dx, void* dwg,
                                 void* dwu, void* dwd, void* ws, cudaStream_t st) {
-    if (ctx->ffn_pair_units == 0) {
-        const cudaError_t e = find_pair_units(ctx);
-        if (e != cudaSuccess) return e;
-    }
+    const cudaError_t e = prepare_ffn(ctx);
+    if (e != cudaSuccess) return e;
     if (f.dtype == SAMA_BF16) {
         Block<__nv_bfloat16> b{ctx, f, static_cast<uint8_t*>(ws), st, up8(f.f)};
         b.backward(x, wg, wu, wd, gate, up, dy, dx, dwg, dwu, dwd);

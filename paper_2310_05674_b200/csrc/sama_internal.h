@@ -133,6 +133,8 @@ struct sama_ctx {
     int embed_epoch;               // number of the last such call
     uint32_t ffn_ready;            // kernels of gated_ffn.cu whose shared-memory size is set on this device
     int ffn_pair_units;            // CTA pairs of them that can be resident (0: not yet asked)
+    float* ffn_parts;              // device: sums of tiles whose contraction several CTAs share
+    int* ffn_arrived;              // device: arrival counters of such tiles, zero between launches
     sama::Profiler* prof;          // host
 };
 
