@@ -5,8 +5,14 @@
 // Bound by memory traffic.  The tensors' addresses, lengths and types travel in the kernel's parameters (no copy, no
 // plan on the device), and each block takes an equal, contiguous share of the elements of all tensors together, cut
 // into chunks that never cross a tensor.  Squares are summed in double: a square of any fp32 or bf16 value neither
-// overflows nor vanishes there, and the partial sums of the blocks are added in a fixed order.
+// overflows nor vanishes there, and the partial sums of the blocks are added in a fixed order.  (The conversion
+// instruction to double runs at four values per cycle and SM, a third of what bf16 gradients arrive at; integer
+// operations put the bits of a normal fp32 value where a double has them, see sum_group.)
+//
+// Two launches, norm and scaling; the second goes through each block's share backwards, so that what the first read last
+// comes out of L2.  Up to 2^20 elements, where launches are all that counts, one cluster of 16 CTAs does both.
 #include <cmath>
+#include <type_traits>
 
 #include "num_types.h"
 #include "sama_internal.h"
@@ -16,7 +22,10 @@ namespace sama {
 namespace {
 
 constexpr int kClipThreads = 256;
-constexpr int kGroup = 8;  // elements per thread and access: 16 bytes of a 16-bit type, 32 of fp32
+constexpr int kLane = 16;              // bytes per thread and access
+constexpr int kChunkUnit = 8 * 1024;   // chunks are multiples of this many elements: aligned shares for every type
+constexpr int kCapSmall = 112, kCapLarge = 960;  // tensors of one launch: 3.6 KB and 31 KB of parameters
+constexpr int kFewElements = 1 << 20, kFewCtas = 16, kFewThreads = 1024;
 
 struct ClipEntry {
     const void* in;
@@ -27,7 +36,7 @@ struct ClipEntry {
 };
 template <int CAP>
 struct ClipArgs {
-    int n_entries, n_chunks, chunk;   // chunk: elements, a multiple of kGroup * kClipThreads
+    int n_entries, n_chunks, chunk;   // chunk: elements, a multiple of kChunkUnit
     int n_partials, partial0;         // all launches' block partials, and where this launch's begin
     int last;                         // this launch adds them up
     float max_norm;
@@ -44,6 +53,7 @@ __device__ __forceinline__ double clip_warp_sum(double v) {
     return v;
 }
 // Sum over the block in a fixed order; valid in thread 0.
+template <int THREADS>
 __device__ __forceinline__ double clip_block_sum(double v, double* smem) {
     v = clip_warp_sum(v);
     __syncthreads();
@@ -51,7 +61,7 @@ __device__ __forceinline__ double clip_block_sum(double v, double* smem) {
     __syncthreads();
     double t = 0.0;
     if (threadIdx.x == 0)
-        for (int w = 0; w < kClipThreads / 32; ++w) t += smem[w];
+        for (int w = 0; w < THREADS / 32; ++w) t += smem[w];
     return t;
 }
 
@@ -66,97 +76,189 @@ __device__ __forceinline__ int entry_of(const ClipArgs<CAP>& a, int c) {
     return lo;
 }
 
+// A normal fp32 value's magnitude as a double: exponent re-biased, mantissa moved.  Zero and subnormal values come out
+// below 2^-126, infinities and NaN at 2^128 and above, where no finite value's does.
+__device__ __forceinline__ double magnitude(uint32_t bits) {
+    return __hiloint2double((int)(((bits & 0x7fffffffu) >> 3) + 0x38000000u), (int)(bits << 29));
+}
+// Adds the squares of 16 bytes of values to acc, and their bits (without the sign) to any.
 template <typename T>
-__device__ __forceinline__ double chunk_sumsq(const T* __restrict__ p, int n, bool vec) {
-    constexpr int U = 4;
-    double acc[2] = {0.0, 0.0};
-    if (vec) {
-        const int groups = n / kGroup;
-        for (int i = threadIdx.x; i < groups; i += U * kClipThreads) {
-            float v[U][kGroup];
+__device__ __forceinline__ void sum_group(const uint4& x, double* acc, uint32_t& any) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (i + u * kClipThreads < groups) {
-                    load_n<T, kGroup, true>(p + (int64_t)(i + u * kClipThreads) * kGroup, v[u]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < kGroup; ++j) v[u][j] = 0.f;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int j = 0; j < kGroup; ++j) acc[j & 1] = fma((double)v[u][j], (double)v[u][j], acc[j & 1]);
+    for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) {
+            const double m = magnitude(w[j]);
+            acc[j & 1] = fma(m, m, acc[j & 1]);
+            any |= w[j] & 0x7fffffffu;
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const float2 f = unpack2<T>(w[j]);   // (a subnormal fp16 value is a normal fp32 one)
+            const double m0 = magnitude(__float_as_uint(f.x)), m1 = magnitude(__float_as_uint(f.y));
+            acc[0] = fma(m0, m0, acc[0]);
+            acc[1] = fma(m1, m1, acc[1]);
+            any |= w[j] & 0x7fff7fffu;
+        } else {
+            // the low mantissa bits of a bf16 value are zero, so the double's low word is
+            const double m0 = __hiloint2double((int)(((w[j] & 0x7fffu) << 13) + 0x38000000u), 0);
+            const double m1 = __hiloint2double((int)(((w[j] & 0x7fff0000u) >> 3) + 0x38000000u), 0);
+            acc[0] = fma(m0, m0, acc[0]);
+            acc[1] = fma(m1, m1, acc[1]);
+            any |= w[j] & 0x7fff7fffu;
         }
     }
-    // the rest, or a tensor at an odd address: neighbouring threads take neighbouring elements
-    const int done = vec ? n / kGroup * kGroup : 0;
-    for (int i = done + threadIdx.x; i < n; i += kGroup * kClipThreads) {
-        float v[kGroup];
+}
+
+// This thread's share of a chunk: sum of squares of n elements, THREADS threads, neighbouring threads on neighbouring
+// 16 bytes (or elements, where the tensor starts at an odd address).
+template <typename T, int THREADS>
+__device__ __forceinline__ double chunk_sumsq(const T* __restrict__ p, int n, bool vec) {
+    constexpr int PER = kLane / sizeof(T), U = 4;
+    double sum = 0.0;
+    const int groups = vec ? n / PER : 0;
+    if (vec) {
+        double acc[2] = {0.0, 0.0};
+        uint32_t any = 0;
+        const uint4* q = reinterpret_cast<const uint4*>(p);
+#pragma unroll 1
+        for (int i = threadIdx.x; i < groups; i += U * THREADS) {
+            uint4 v[U];
 #pragma unroll
-        for (int u = 0; u < kGroup; ++u) v[u] = i + u * kClipThreads < n ? to_float(p[i + u * kClipThreads]) : 0.f;
+            for (int u = 0; u < U; ++u) v[u] = i + u * THREADS < groups ? __ldg(q + i + u * THREADS) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int u = 0; u < kGroup; ++u) acc[u & 1] = fma((double)v[u], (double)v[u], acc[u & 1]);
+            for (int u = 0; u < U; ++u) sum_group<T>(v[u], acc, any);
+        }
+        sum = acc[0] + acc[1];
+        // Values that are not finite (2^256 and above: at least 2^254 in a share), or so small that what zeros and
+        // subnormals add could count (below 2^-245 in a share): once more with the converting instruction.  A share of
+        // zeros is 0.
+        if (any == 0) {
+            sum = 0.0;
+        } else if (!(sum < 2.894802230932905e76) || sum < 6.525304467998525e-55) {
+            sum = 0.0;
+#pragma unroll 1
+            for (int i = threadIdx.x; i < groups; i += THREADS)
+#pragma unroll 1
+                for (int j = 0; j < PER; ++j) {
+                    const double x = (double)to_float(p[(int64_t)i * PER + j]);
+                    sum = fma(x, x, sum);
+                }
+        }
     }
-    return acc[0] + acc[1];
+    constexpr int W = 8;
+#pragma unroll 1
+    for (int i = groups * PER + threadIdx.x; i < n; i += W * THREADS) {
+        float v[W];
+#pragma unroll
+        for (int u = 0; u < W; ++u) v[u] = i + u * THREADS < n ? to_float(p[i + u * THREADS]) : 0.f;
+#pragma unroll
+        for (int u = 0; u < W; ++u) sum = fma((double)v[u], (double)v[u], sum);
+    }
+    return sum;
+}
+template <int THREADS>
+__device__ __forceinline__ double entry_sumsq(const ClipEntry& e, int64_t at, int n) {
+    if (e.dtype == SAMA_F32) return chunk_sumsq<float, THREADS>(static_cast<const float*>(e.in) + at, n, e.in_vec);
+    if (e.dtype == SAMA_BF16) return chunk_sumsq<__nv_bfloat16, THREADS>(static_cast<const __nv_bfloat16*>(e.in) + at, n, e.in_vec);
+    return chunk_sumsq<__half, THREADS>(static_cast<const __half*>(e.in) + at, n, e.in_vec);
+}
+
+// min(1, max_norm / norm), or 0 and the status bit for a norm that is not finite.
+__device__ __forceinline__ double clip_factor(double sum, float max_norm, float* norm_out, int32_t* status) {
+    const double norm = sqrt(sum);
+    if (norm_out) *norm_out = (float)norm;
+    if (!isfinite(norm)) {
+        atomicOr(status, (int)SAMA_DEV_NONFINITE_GRAD);
+        return 0.0;
+    }
+    return norm > (double)max_norm ? (double)max_norm / norm : 1.0;
 }
 
 // The factor.  Below 2^-100 it may leave fp32's normal range (a limit of 1e-30 on a norm of 1e38), where only double
-// still holds it.  0 marks a norm that is not finite: zeros are written whatever the gradients are.
+// still holds it; 0 marks a norm that is not finite, for which zeros are written whatever the gradients are.  Neither
+// is worth a fast path; `plain` is every other case.
 struct Factor {
     float f;
     double d;
-    bool in_double;
-    __device__ explicit Factor(double c) : f((float)c), d(c), in_double(c < 7.888609052210118e-31 && c != 0.0) {}
-    __device__ __forceinline__ float operator()(float x) const {
-        if (in_double) return (float)((double)x * d);
-        return f == 0.f ? 0.f : x * f;
-    }
+    bool plain;
+    __device__ explicit Factor(double c) : f((float)c), d(c), plain(c >= 7.888609052210118e-31) {}
+    __device__ __forceinline__ float slow(float x) const { return d == 0.0 ? 0.f : (float)((double)x * d); }
 };
 
-template <int N>
-__device__ __forceinline__ void store_as(int dtype, void* q, int64_t at, const float* v) {
-    if (dtype == SAMA_F32) store_n<float, N>(static_cast<float*>(q) + at, v);
-    else if (dtype == SAMA_BF16) store_n<__nv_bfloat16, N>(static_cast<__nv_bfloat16*>(q) + at, v);
-    else store_n<__half, N>(static_cast<__half*>(q) + at, v);
+// Four or eight consecutive values, 8 or 16 bytes: loads and stores that are both contiguous over a warp.
+template <typename T, int N>
+__device__ __forceinline__ void get_few(const T* p, float* v) {
+    if constexpr (sizeof(T) == 2 && N == 4) {
+        const uint2 x = __ldcs(reinterpret_cast<const uint2*>(p));
+        const float2 a = unpack2<T>(x.x), b = unpack2<T>(x.y);
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+    } else {
+        load_n<T, N>(p, v);
+    }
 }
-
-template <typename T>
-__device__ __forceinline__ void chunk_scale(const ClipEntry& e, int64_t at, int n, const Factor& by) {
-    constexpr int U = 4;
+template <typename T, int N>
+__device__ __forceinline__ void put_few(T* p, const float* v) {
+    if constexpr (sizeof(T) == 2 && N == 4) __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3])));
+    else store_n<T, N, true>(p, v);
+}
+template <typename T, typename TO, int THREADS>
+__device__ __forceinline__ void chunk_scale(const T* p, TO* q, int n, bool vec, Factor by) {
+    constexpr int PER = sizeof(T) == 2 && sizeof(TO) == 2 ? 8 : 4, U = 4;
+    if (!by.plain) {
+#pragma unroll 1
+        for (int i = threadIdx.x; i < n; i += THREADS) q[i] = from_float<TO>(by.slow(to_float(p[i])));
+        return;
+    }
+    const float f = by.f;
+    const int groups = vec ? n / PER : 0;
+    // (whole rounds without conditions, then what is left: conditions on every access cost hundreds of spilled bytes)
+    auto round = [&](auto count, int i) {
+        constexpr int R = decltype(count)::value;
+        float x[R][PER];
+#pragma unroll
+        for (int u = 0; u < R; ++u) get_few<T, PER>(p + (int64_t)(i + u * THREADS) * PER, x[u]);
+#pragma unroll
+        for (int u = 0; u < R; ++u) {
+#pragma unroll
+            for (int j = 0; j < PER; ++j) x[u][j] *= f;
+            put_few<TO, PER>(q + (int64_t)(i + u * THREADS) * PER, x[u]);
+        }
+    };
+    int i = threadIdx.x;
+#pragma unroll 1
+    for (; i + (U - 1) * THREADS < groups; i += U * THREADS) round(std::integral_constant<int, U>(), i);
+#pragma unroll 1
+    for (; i < groups; i += THREADS) round(std::integral_constant<int, 1>(), i);
+    constexpr int W = 8;
+    i = groups * PER + threadIdx.x;
+#pragma unroll 1
+    for (; i + (W - 1) * THREADS < n; i += W * THREADS) {
+        float v[W];
+#pragma unroll
+        for (int u = 0; u < W; ++u) v[u] = to_float(p[i + u * THREADS]);
+#pragma unroll
+        for (int u = 0; u < W; ++u) q[i + u * THREADS] = from_float<TO>(v[u] * f);
+    }
+#pragma unroll 1
+    for (; i < n; i += THREADS) q[i] = from_float<TO>(to_float(p[i]) * f);
+}
+template <typename T, int THREADS>
+__device__ __forceinline__ void scale_from(const ClipEntry& e, int64_t at, int n, const Factor& by) {
     const T* p = static_cast<const T*>(e.in) + at;
-    void* const q = e.out;
-    const int to = e.out_dtype;
-    const int groups = e.in_vec && e.out_vec ? n / kGroup : 0;
-    for (int i = threadIdx.x; i < groups; i += U * kClipThreads) {
-        float v[U][kGroup];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + u * kClipThreads < groups) load_n<T, kGroup>(p + (int64_t)(i + u * kClipThreads) * kGroup, v[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i + u * kClipThreads < groups) {
-#pragma unroll
-                for (int j = 0; j < kGroup; ++j) v[u][j] = by(v[u][j]);
-                store_as<kGroup>(to, q, at + (int64_t)(i + u * kClipThreads) * kGroup, v[u]);
-            }
-    }
-    for (int i = groups * kGroup + threadIdx.x; i < n; i += kGroup * kClipThreads) {
-        float v[kGroup];
-#pragma unroll
-        for (int u = 0; u < kGroup; ++u)
-            if (i + u * kClipThreads < n) v[u] = to_float(p[i + u * kClipThreads]);
-#pragma unroll
-        for (int u = 0; u < kGroup; ++u)
-            if (i + u * kClipThreads < n) {
-                v[u] = by(v[u]);
-                store_as<1>(to, q, at + i + u * kClipThreads, v + u);
-            }
-    }
+    const bool vec = e.in_vec && e.out_vec;
+    if (e.out_dtype == SAMA_F32) chunk_scale<T, float, THREADS>(p, static_cast<float*>(e.out) + at, n, vec, by);
+    else if (e.out_dtype == SAMA_BF16) chunk_scale<T, __nv_bfloat16, THREADS>(p, static_cast<__nv_bfloat16*>(e.out) + at, n, vec, by);
+    else chunk_scale<T, __half, THREADS>(p, static_cast<__half*>(e.out) + at, n, vec, by);
+}
+template <int THREADS>
+__device__ __forceinline__ void entry_scale(const ClipEntry& e, int64_t at, int n, const Factor& by) {
+    if (!e.out || (e.out == e.in && by.f == 1.f)) return;   // nothing to write
+    if (e.dtype == SAMA_F32) scale_from<float, THREADS>(e, at, n, by);
+    else if (e.dtype == SAMA_BF16) scale_from<__nv_bfloat16, THREADS>(e, at, n, by);
+    else scale_from<__half, THREADS>(e, at, n, by);
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(kClipThreads)
+__global__ void __launch_bounds__(kClipThreads, 4)
 grad_norm_kernel(const __grid_constant__ ClipArgs<CAP> a) {
     __shared__ double smem[kClipThreads / 32];
     __shared__ bool is_last;
@@ -171,13 +273,10 @@ grad_norm_kernel(const __grid_constant__ ClipArgs<CAP> a) {
             while (k + 1 < a.n_entries && a.e[k + 1].first_chunk <= c) ++k;
             const ClipEntry& e = a.e[k];
             const int64_t at = (int64_t)(c - e.first_chunk) * a.chunk;
-            const int n = (int)min((int64_t)a.chunk, e.n - at);
-            if (e.dtype == SAMA_F32) acc += chunk_sumsq(static_cast<const float*>(e.in) + at, n, e.in_vec);
-            else if (e.dtype == SAMA_BF16) acc += chunk_sumsq(static_cast<const __nv_bfloat16*>(e.in) + at, n, e.in_vec);
-            else acc += chunk_sumsq(static_cast<const __half*>(e.in) + at, n, e.in_vec);
+            acc += entry_sumsq<kClipThreads>(e, at, (int)min((int64_t)a.chunk, e.n - at));
         }
     }
-    const double total = clip_block_sum(acc, smem);
+    const double total = clip_block_sum<kClipThreads>(acc, smem);
     if (threadIdx.x == 0) {
         a.partials[a.partial0 + blockIdx.x] = total;
         __threadfence();
@@ -189,26 +288,15 @@ grad_norm_kernel(const __grid_constant__ ClipArgs<CAP> a) {
     double v = 0.0;
     if (a.last)
         for (int i = threadIdx.x; i < a.n_partials; i += kClipThreads) v += __ldcg(a.partials + i);
-    const double sum = clip_block_sum(v, smem);
+    const double sum = clip_block_sum<kClipThreads>(v, smem);
     if (threadIdx.x == 0) {
         a.sc->counter = 0u;
-        if (a.last) {
-            const double norm = sqrt(sum);
-            double c = 1.0;
-            if (!isfinite(norm)) {
-                c = 0.0;
-                atomicOr(&a.sc->status, (int)SAMA_DEV_NONFINITE_GRAD);
-            } else if (norm > (double)a.max_norm) {
-                c = (double)a.max_norm / norm;
-            }
-            a.state->factor = c;
-            if (a.norm_out) *a.norm_out = (float)norm;
-        }
+        if (a.last) a.state->factor = clip_factor(sum, a.max_norm, a.norm_out, &a.sc->status);
     }
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(kClipThreads)
+__global__ void __launch_bounds__(kClipThreads, 4)
 grad_scale_kernel(const __grid_constant__ ClipArgs<CAP> a) {
     pdl_trigger();
     pdl_wait();
@@ -216,21 +304,58 @@ grad_scale_kernel(const __grid_constant__ ClipArgs<CAP> a) {
     const int c0 = (int)((int64_t)a.n_chunks * blockIdx.x / gridDim.x);
     const int c1 = (int)((int64_t)a.n_chunks * (blockIdx.x + 1) / gridDim.x);
     if (c0 >= c1) return;
-    int k = entry_of(a, c0);
-    for (int c = c0; c < c1; ++c) {
-        while (k + 1 < a.n_entries && a.e[k + 1].first_chunk <= c) ++k;
+    int k = entry_of(a, c1 - 1);
+    for (int c = c1 - 1; c >= c0; --c) {
+        while (a.e[k].first_chunk > c) --k;
         const ClipEntry& e = a.e[k];
-        if (!e.out || (e.out == e.in && by.f == 1.f)) continue;  // nothing to write
         const int64_t at = (int64_t)(c - e.first_chunk) * a.chunk;
-        const int n = (int)min((int64_t)a.chunk, e.n - at);
-        if (e.dtype == SAMA_F32) chunk_scale<float>(e, at, n, by);
-        else if (e.dtype == SAMA_BF16) chunk_scale<__nv_bfloat16>(e, at, n, by);
-        else chunk_scale<__half>(e, at, n, by);
+        entry_scale<kClipThreads>(e, at, (int)min((int64_t)a.chunk, e.n - at), by);
     }
 }
 
-// One launch's worth of tensors.
-constexpr int kCapSmall = 112, kCapLarge = 960;  // 3.6 KB and 31 KB of parameters
+// Both in one cluster of kFewCtas CTAs: CTA r takes chunks r, r + kFewCtas, ...
+__global__ void __launch_bounds__(kFewThreads)
+grad_clip_few_kernel(const __grid_constant__ ClipArgs<kCapSmall> a) {
+    __shared__ double smem[kFewThreads / 32], total, factor;
+    pdl_trigger();
+    pdl_wait();
+    const uint32_t rank = blockIdx.x;
+    double acc = 0.0;
+    int k = 0;
+    for (int c = (int)rank; c < a.n_chunks; c += kFewCtas) {
+        while (k + 1 < a.n_entries && a.e[k + 1].first_chunk <= c) ++k;
+        const ClipEntry& e = a.e[k];
+        const int64_t at = (int64_t)(c - e.first_chunk) * a.chunk;
+        acc += entry_sumsq<kFewThreads>(e, at, (int)min((int64_t)a.chunk, e.n - at));
+    }
+    const double mine = clip_block_sum<kFewThreads>(acc, smem);
+    if (threadIdx.x == 0) total = mine;
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (threadIdx.x < 32) {
+        double v = 0.0;
+        if (threadIdx.x < kFewCtas) {
+            uint32_t addr;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"((uint32_t)__cvta_generic_to_shared(&total)), "r"(threadIdx.x));
+            asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+        }
+        v = clip_warp_sum(v);
+        if (threadIdx.x == 0) {
+            factor = clip_factor(v, a.max_norm, rank == 0 ? a.norm_out : nullptr, &a.sc->status);
+        }
+    }
+    // no CTA leaves before all have read its total
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const Factor by(factor);
+    k = 0;
+    for (int c = (int)rank; c < a.n_chunks; c += kFewCtas) {
+        while (k + 1 < a.n_entries && a.e[k + 1].first_chunk <= c) ++k;
+        const ClipEntry& e = a.e[k];
+        const int64_t at = (int64_t)(c - e.first_chunk) * a.chunk;
+        entry_scale<kFewThreads>(e, at, (int)min((int64_t)a.chunk, e.n - at), by);
+    }
+}
 
 template <int CAP>
 void fill(ClipArgs<CAP>& a, const sama_tensor_t* t, int first, int count, int chunk) {
@@ -257,11 +382,10 @@ template <int CAP>
 cudaError_t run_clip(sama_ctx* ctx, const sama_tensor_t* t, int n, int64_t total, bool any_out, float max_norm,
                      float* norm_out, ClipState* state, cudaStream_t st) {
     const int launches = n > 0 ? (n + CAP - 1) / CAP : 1;
-    const int64_t lanes = (int64_t)kClipThreads * kGroup;
-    // at most 2^31 chunks; enough of them for every block to get a share, few enough for a block's bookkeeping
-    int64_t chunk = total / ((int64_t)ctx->sm_count * 4 * 8) / lanes * lanes;
-    if (chunk < lanes) chunk = lanes;
-    if (chunk > 16 * lanes) chunk = 16 * lanes;
+    // enough chunks for every block to get an even share, few enough for a block's bookkeeping
+    int64_t chunk = total / ((int64_t)ctx->sm_count * 4 * 8) / kChunkUnit * kChunkUnit;
+    if (chunk < kChunkUnit) chunk = kChunkUnit;
+    if (chunk > 4 * kChunkUnit) chunk = 4 * kChunkUnit;
     int grid = ctx->sm_count * 4;
     if (grid > kMaxPartials / launches) grid = kMaxPartials / launches;
     ClipArgs<CAP> a;
@@ -295,6 +419,20 @@ cudaError_t launch_clip_grads(sama_ctx* ctx, const sama_tensor_t* t, int n, floa
         any_out = any_out || (t[i].out && t[i].n > 0);
     }
     ClipState* state = &ctx->scalars->clip;
+    if (n <= kCapSmall && total <= kFewElements) {
+        ClipArgs<kCapSmall> a;
+        fill(a, t, 0, n, 16 * kFewThreads);   // a chunk is one round of loads of a CTA
+        a.max_norm = max_norm;
+        a.norm_out = norm_out;
+        a.sc = ctx->scalars;
+        if (!ctx->clip_ready) {
+            const cudaError_t e = cudaFuncSetAttribute(grad_clip_few_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (e != cudaSuccess) return e;
+            ctx->clip_ready = 1;
+        }
+        KernelScope scope(ctx, SAMA_K_CLIP, -1, st);
+        return launch_clustered(kFewCtas, grad_clip_few_kernel, dim3(kFewCtas), dim3(kFewThreads), 0, st, a);
+    }
     if (n <= kCapSmall) return run_clip<kCapSmall>(ctx, t, n, total, any_out, max_norm, norm_out, state, st);
     return run_clip<kCapLarge>(ctx, t, n, total, any_out, max_norm, norm_out, state, st);
 }

@@ -131,6 +131,7 @@ struct sama_ctx {
     size_t op_ws_bytes;
     int embed_ready;               // the sort's shared-memory size is set on this device
     int embed_epoch;               // number of the last such call
+    int clip_ready;                // the small clipping kernel's cluster size is allowed on this device
     uint32_t ffn_ready;            // kernels of gated_ffn.cu whose shared-memory size is set on this device
     int ffn_pair_units;            // CTA pairs of them that can be resident (0: not yet asked)
     float* ffn_parts;              // device: sums of tiles whose contraction several CTAs share
