@@ -9,8 +9,8 @@
 // instruction to double runs at four values per cycle and SM, a third of what bf16 gradients arrive at; integer
 // operations put the bits of a normal fp32 value where a double has them, see sum_group.)
 //
-// Two launches, norm and scaling; the second goes through each block's share backwards, so that what the first read last
-// comes out of L2.  Up to 2^20 elements, where launches are all that counts, one cluster of 16 CTAs does both.
+// Two launches, norm and scaling; the second goes through each block's share backwards, in eight blocks, so that what the
+// first read last comes out of L2 and the stores of one block do not wait for another's loads.  Up to 2^20 elements, where launches are all that counts, one cluster of 16 CTAs does both.
 #include <cmath>
 #include <type_traits>
 
@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kClipThreads = 256;
 constexpr int kLane = 16;              // bytes per thread and access
+constexpr int kScaleParts = 8;
 constexpr int kChunkUnit = 8 * 1024;   // chunks are multiples of this many elements: aligned shares for every type
 constexpr int kCapSmall = 112, kCapLarge = 960;  // tensors of one launch: 3.6 KB and 31 KB of parameters
 constexpr int kFewElements = 1 << 20, kFewCtas = 16, kFewThreads = 1024;
@@ -202,7 +203,7 @@ __device__ __forceinline__ void put_few(T* p, const float* v) {
 }
 template <typename T, typename TO, int THREADS>
 __device__ __forceinline__ void chunk_scale(const T* p, TO* q, int n, bool vec, Factor by) {
-    constexpr int PER = sizeof(T) == 2 && sizeof(TO) == 2 ? 8 : 4, U = 4;
+    constexpr int PER = sizeof(T) == 2 && sizeof(TO) == 2 ? 8 : 4, U = 32 / PER;
     if (!by.plain) {
 #pragma unroll 1
         for (int i = threadIdx.x; i < n; i += THREADS) q[i] = from_float<TO>(by.slow(to_float(p[i])));
@@ -301,8 +302,10 @@ grad_scale_kernel(const __grid_constant__ ClipArgs<CAP> a) {
     pdl_trigger();
     pdl_wait();
     const Factor by(a.state->factor);
-    const int c0 = (int)((int64_t)a.n_chunks * blockIdx.x / gridDim.x);
-    const int c1 = (int)((int64_t)a.n_chunks * (blockIdx.x + 1) / gridDim.x);
+    // kScaleParts blocks for each of the norm's, the last parts of all shares first: those are in L2
+    const int shares = gridDim.x / kScaleParts, share = blockIdx.x % shares, part = kScaleParts - 1 - blockIdx.x / shares;
+    const int first = (int)((int64_t)a.n_chunks * share / shares), n = (int)((int64_t)a.n_chunks * (share + 1) / shares) - first;
+    const int c0 = first + (int)((int64_t)n * part / kScaleParts), c1 = first + (int)((int64_t)n * (part + 1) / kScaleParts);
     if (c0 >= c1) return;
     int k = entry_of(a, c1 - 1);
     for (int c = c1 - 1; c >= c0; --c) {
@@ -402,7 +405,7 @@ cudaError_t run_clip(sama_ctx* ctx, const sama_tensor_t* t, int n, int64_t total
             a.last = l == launches - 1;
             KernelScope scope(ctx, SAMA_K_CLIP, -1, st);
             const cudaError_t e = pass == 0 ? launch_dependent(grad_norm_kernel<CAP>, dim3(grid), dim3(kClipThreads), 0, st, a)
-                                            : launch_dependent(grad_scale_kernel<CAP>, dim3(grid), dim3(kClipThreads), 0, st, a);
+                                            : launch_dependent(grad_scale_kernel<CAP>, dim3(grid * kScaleParts), dim3(kClipThreads), 0, st, a);
             if (e != cudaSuccess) return e;
         }
     return cudaSuccess;
