@@ -226,14 +226,20 @@ __device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, T
         }
     } else {
         // rows that start anywhere: neighbouring lanes take neighbouring elements
-        const T* s = reinterpret_cast<const T*>(stg);
-#pragma unroll 4
-        for (int r = 0; r < min(rows, 32); ++r)
-#pragma unroll
-            for (int j = 0; j < CU / 32; ++j) {
-                const int c = lane + 32 * j;
-                if (col0 + c < cols) dst[(int64_t)(row0 + r) * ld + col0 + c] = s[at(r, c >> 3) * 8 + (c & 7)];
-            }
+        // (in pairs that start on a 4-byte boundary, which in a row of odd length every other row's first value does not)
+        const uint16_t* s = reinterpret_cast<const uint16_t*>(stg);
+        constexpr int ROWS = 64 / CU;               // rows at a time
+        const int j = lane % (CU / 2);
+        auto value = [&](int r, int c) { return (uint32_t)s[at(r, c >> 3) * 8 + (c & 7)]; };
+#pragma unroll 2
+        for (int r = lane / (CU / 2); r < min(rows, 32); r += ROWS) {
+            uint16_t* d = reinterpret_cast<uint16_t*>(dst) + (int64_t)(row0 + r) * ld + col0;
+            const int odd = (int)(reinterpret_cast<uintptr_t>(d) >> 1) & 1;
+            const int c = 2 * j + odd;
+            if (c + 1 < CU && col0 + c + 1 < cols) *reinterpret_cast<uint32_t*>(d + c) = value(r, c) | value(r, c + 1) << 16;
+            else if (c < CU && col0 + c < cols) d[c] = (uint16_t)value(r, c);
+            if (odd && j == 0 && col0 < cols) d[0] = (uint16_t)value(r, 0);
+        }
     }
 }
 
@@ -241,12 +247,27 @@ __device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, T
 template <typename T>
 __device__ __forceinline__ uint4 load8(const T* p, int col, int cols, bool vec) {
     if (vec) return __ldg(reinterpret_cast<const uint4*>(p + col));
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + col;
     uint32_t r[4];
+    if (col + 8 <= cols) {
+        if ((reinterpret_cast<uintptr_t>(q) & 2u) == 0) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t lo = col + 2 * j < cols ? *reinterpret_cast<const uint16_t*>(p + col + 2 * j) : 0;
-        const uint32_t hi = col + 2 * j + 1 < cols ? *reinterpret_cast<const uint16_t*>(p + col + 2 * j + 1) : 0;
-        r[j] = lo | (hi << 16);
+            for (int j = 0; j < 4; ++j) r[j] = __ldg(reinterpret_cast<const uint32_t*>(q) + j);
+        } else {   // the words around a value at an odd place, within the eight
+            uint32_t w[5];
+            w[0] = (uint32_t)__ldg(q) << 16;
+#pragma unroll
+            for (int j = 0; j < 3; ++j) w[j + 1] = __ldg(reinterpret_cast<const uint32_t*>(q + 1) + j);
+            w[4] = __ldg(q + 7);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = __funnelshift_r(w[j], w[j + 1], 16);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t lo = col + 2 * j < cols ? q[2 * j] : 0, hi = col + 2 * j + 1 < cols ? q[2 * j + 1] : 0;
+            r[j] = lo | (hi << 16);
+        }
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
@@ -735,18 +756,29 @@ ffn_few_kernel(const __grid_constant__ FewArgs a) {
     }
 }
 
-// Rows of `cols` values at any address -> rows of `ld` (a multiple of 8) at an aligned one: what TMA can read.
+// Rows of `cols` values at any address -> rows of `ld` (a multiple of 8) at an aligned one: what TMA can read.  All
+// matrices of a call in one launch.
+struct AlignJobs {
+    static constexpr int kMost = 5;
+    const void* src[kMost];
+    void* dst[kMost];
+    int64_t first[kMost + 1];   // 16-byte groups of the matrices before
+    int cols[kMost], ld[kMost];
+    int n;
+};
 template <typename T>
 __global__ void __launch_bounds__(256)
-align_rows_kernel(const T* __restrict__ src, int64_t rows, int cols, int ld, T* __restrict__ dst) {
+align_rows_kernel(const __grid_constant__ AlignJobs a) {
     pdl_trigger();
     pdl_wait();
-    const int groups = ld / 8;
-    const int64_t total = rows * groups;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t r = i / groups;
-        const int c = (int)(i - r * groups) * 8;
-        *reinterpret_cast<uint4*>(dst + r * ld + c) = load8(src + r * cols, c, cols, false);
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < a.first[a.n]; i += (int64_t)gridDim.x * blockDim.x) {
+        int k = 0;
+        while (i >= a.first[k + 1]) ++k;
+        const int groups = a.ld[k] / 8;
+        const int64_t at = i - a.first[k], r = at / groups;
+        const int c = (int)(at - r * groups) * 8;
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.dst[k]) + r * a.ld[k] + c) =
+            load8(static_cast<const T*>(a.src[k]) + r * a.cols[k], c, a.cols[k], false);
     }
 }
 
@@ -901,18 +933,24 @@ struct Block {
         ws += up256(elements * 2);
         return p;
     }
+    // The matrix itself, or the place of a copy that align() will make.
+    AlignJobs jobs = {};
     Matrix readable(const void* p, int64_t rows, int cols) {
         if (vec_rows(p, cols)) return {p, rows, cols, cols};
-        const int ld = up8(cols);
-        T* dst = static_cast<T*>(take((size_t)rows * ld));
-        int64_t blocks = (rows * (ld / 8) + 255) / 256;
-        if (blocks > 8 * ctx->sm_count) blocks = 8 * ctx->sm_count;
-        if (err == cudaSuccess) {
-            KernelScope scope(ctx, SAMA_K_FFN, -1, st);
-            err = launch_dependent(align_rows_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, static_cast<const T*>(p),
-                                   rows, cols, ld, dst);
-        }
-        return {dst, rows, cols, ld};
+        const int ld = up8(cols), k = jobs.n++;
+        jobs.src[k] = p;
+        jobs.dst[k] = take((size_t)rows * ld);
+        jobs.cols[k] = cols;
+        jobs.ld[k] = ld;
+        jobs.first[k + 1] = jobs.first[k] + rows * (ld / 8);
+        return {jobs.dst[k], rows, cols, ld};
+    }
+    void align() {
+        if (jobs.n == 0 || err != cudaSuccess) return;
+        int64_t blocks = (jobs.first[jobs.n] + 255) / 256;
+        if (blocks > 16 * ctx->sm_count) blocks = 16 * ctx->sm_count;
+        KernelScope scope(ctx, SAMA_K_FFN, -1, st);
+        err = launch_dependent(align_rows_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, st, jobs);
     }
     template <int MODE, bool A_MN, bool B_MN, int G>
     void run(Params<G>& P, int kind, const TilePlan& plan) {
@@ -967,6 +1005,7 @@ struct Block {
             return;
         }
         const Matrix mx = readable(x, M, d), mg = readable(wg, n, d), mu = readable(wu, n, d), md = readable(wd, d, n);
+        align();
         {
             Params<1> P = {};
             Problem& q = P.p[0];
@@ -998,7 +1037,10 @@ struct Block {
         void* dg = take((size_t)M * fp);
         void* du = take((size_t)M * fp);
         void* h = take((size_t)M * fp);
-        const Matrix my = readable(dy, M, d), md = readable(wd, d, n);
+        const Matrix my = readable(dy, M, d), md = readable(wd, d, n), none = {};
+        const Matrix mg = dx ? readable(wg, n, d) : none, mu = dx ? readable(wu, n, d) : none;
+        const Matrix mx = dwg || dwu ? readable(x, M, d) : my;
+        align();
         {
             Params<1> P = {};
             Problem& q = P.p[0];
@@ -1017,7 +1059,6 @@ struct Block {
         }
         const Matrix mdg = {dg, M, n, fp}, mdu = {du, M, n, fp}, mh = {h, M, n, fp};
         if (dx) {
-            const Matrix mg = readable(wg, n, d), mu = readable(wu, n, d);
             Params<1> P = {};
             Problem& q = P.p[0];
             check(operand_map(&q.a[0], mdg, f.dtype, false) && operand_map(&q.a[1], mdu, f.dtype, false) &&
@@ -1030,7 +1071,6 @@ struct Block {
             run<PLAIN, false, true, 1>(P, 3);
         }
         if (!dwg && !dwu && !dwd) return;
-        const Matrix mx = (dwg || dwu) ? readable(x, M, d) : my;
         Params<3> P = {};
         struct { const Matrix* a; const Matrix* b; void* out; int rows, cols; } w[3] = {
             {&mdg, &mx, dwg, n, d}, {&mdu, &mx, dwu, n, d}, {&my, &mh, dwd, d, n}};
