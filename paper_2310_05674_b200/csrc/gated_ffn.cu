@@ -59,10 +59,10 @@ struct Problem {
     int num_kb, kb_first;       // k-blocks, and how many of them the first maps cover
     int tiles_m, tiles_n, item0;
     void* out[3];
-    const void* in[2];          // d-hidden: G and U
-    int64_t ldo[3], ldi;
+    const void* in[2];          // d-hidden: G and U, rows of whole aligned 16-byte groups
+    int64_t ldo[3], ldi[2];
     int cols[3];                // columns of out[i] that may be written
-    int vec_out, vec_in;        // bit i: out[i] (G and U) can be accessed in aligned 16-byte groups
+    int vec_out;                // bit i: out[i] can be written in aligned 16-byte groups
 };
 template <int G>
 struct alignas(64) Params {
@@ -226,19 +226,34 @@ __device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, T
         }
     } else {
         // rows that start anywhere: neighbouring lanes take neighbouring elements
-        // (in pairs that start on a 4-byte boundary, which in a row of odd length every other row's first value does not)
-        const uint16_t* s = reinterpret_cast<const uint16_t*>(stg);
-        constexpr int ROWS = 64 / CU;               // rows at a time
-        const int j = lane % (CU / 2);
-        auto value = [&](int r, int c) { return (uint32_t)s[at(r, c >> 3) * 8 + (c & 7)]; };
+        // Four values per lane, stored as two words that start on a 4-byte boundary: in a row that starts between two
+        // words they begin one value further on, and the second takes its last value from the next lane.
+        constexpr int LANES = CU / 4, ROWS = 32 / LANES;   // of a row, at a time
+        const int k = lane % LANES;
+        const uint2* s = reinterpret_cast<const uint2*>(stg);
 #pragma unroll 2
-        for (int r = lane / (CU / 2); r < min(rows, 32); r += ROWS) {
+        for (int r = lane / LANES; r < 32; r += ROWS) {
+            const uint2 v = s[at(r, k >> 1) * 2 + (k & 1)];
+            const uint32_t next = __shfl_down_sync(0xffffffffu, v.x, 1);
+            if (r >= rows) continue;
             uint16_t* d = reinterpret_cast<uint16_t*>(dst) + (int64_t)(row0 + r) * ld + col0;
-            const int odd = (int)(reinterpret_cast<uintptr_t>(d) >> 1) & 1;
-            const int c = 2 * j + odd;
-            if (c + 1 < CU && col0 + c + 1 < cols) *reinterpret_cast<uint32_t*>(d + c) = value(r, c) | value(r, c + 1) << 16;
-            else if (c < CU && col0 + c < cols) d[c] = (uint16_t)value(r, c);
-            if (odd && j == 0 && col0 < cols) d[0] = (uint16_t)value(r, 0);
+            const int left = cols - col0 - 4 * k;            // values from this lane's first on
+            const bool odd = (reinterpret_cast<uintptr_t>(d) & 2u) != 0;
+            d += 4 * k;
+            if (left >= 5 || (left == 4 && !odd)) {
+                if (!odd) {
+                    reinterpret_cast<uint32_t*>(d)[0] = v.x;
+                    reinterpret_cast<uint32_t*>(d)[1] = v.y;
+                } else {
+                    if (k == 0) d[0] = (uint16_t)v.x;
+                    *reinterpret_cast<uint32_t*>(d + 1) = __funnelshift_r(v.x, v.y, 16);
+                    if (k + 1 < LANES) *reinterpret_cast<uint32_t*>(d + 3) = __funnelshift_r(v.y, next, 16);
+                    else d[3] = (uint16_t)(v.y >> 16);
+                }
+            } else {
+                const uint32_t w[2] = {v.x, v.y};
+                for (int j = odd && k > 0 ? 1 : 0; j < min(left, 4); ++j) d[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+            }
         }
     }
 }
@@ -466,8 +481,8 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                     const int r = r0 + 4 * (i0 + i);
                     vg[i] = vu[i] = make_uint4(0, 0, 0, 0);
                     if (r < rows && col < q.N) {
-                        vg[i] = load8(static_cast<const T*>(q.in[0]) + (int64_t)(row0 + r) * q.ldi, col, q.N, q.vec_in & 1);
-                        vu[i] = load8(static_cast<const T*>(q.in[1]) + (int64_t)(row0 + r) * q.ldi, col, q.N, q.vec_in & 2);
+                        vg[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(q.in[0]) + (row0 + r) * q.ldi[0] + col));
+                        vu[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(q.in[1]) + (row0 + r) * q.ldi[1] + col));
                     }
                 }
             };
@@ -526,16 +541,24 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                 __threadfence();
 #pragma unroll 1
                 for (int st = 0; st < STEPS; ++st) {
+                    // up to four parts' values on their way at a time
                     float sum[16];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) sum[j] = 0.f;
-#pragma unroll 2
-                    for (int p = 0; p < P.split; ++p)
+                    for (int p0 = 0; p0 < P.split; p0 += 4) {
+                        float4 x[4][4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const float4 x = __ldcg(base + p * stride + (st * 4 + k) * 32);
-                            sum[4 * k] += x.x; sum[4 * k + 1] += x.y; sum[4 * k + 2] += x.z; sum[4 * k + 3] += x.w;
-                        }
+                        for (int p = 0; p < 4; ++p)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                x[p][k] = p0 + p < P.split ? __ldcg(base + (p0 + p) * stride + (st * 4 + k) * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int p = 0; p < 4; ++p)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                sum[4 * k] += x[p][k].x; sum[4 * k + 1] += x[p][k].y; sum[4 * k + 2] += x[p][k].z; sum[4 * k + 3] += x[p][k].w;
+                            }
+                    }
                     tmem_st16(acc + column(st), sum);
                 }
             }
@@ -596,12 +619,13 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                     }
                     if (c + 64 == CPW) release();
                     __syncwarp();
-                    with_act(P.act, [&](auto kind) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const uint4 cg[4] = {vg[0], vg[1], vg[2], vg[3]}, cu[4] = {vu[0], vu[1], vu[2], vu[3]};
-                            if (h == 0) load_gu(4, col);
-                            else if (c + 64 < CPW) load_gu(0, col + 64);
+                    // (not unrolled: code that runs once per tile is fetched once per tile)
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 cg[4] = {vg[0], vg[1], vg[2], vg[3]}, cu[4] = {vu[0], vu[1], vu[2], vu[3]};
+                        if (h == 0) load_gu(4, col);
+                        else if (c + 64 < CPW) load_gu(0, col + 64);
+                        with_act(P.act, [&](auto kind) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const int r = r0 + 4 * (4 * h + i);
@@ -623,8 +647,8 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                                 *reinterpret_cast<uint4*>(static_cast<T*>(q.out[1]) + to) = make_uint4(ou[0], ou[1], ou[2], ou[3]);
                                 *reinterpret_cast<uint4*>(static_cast<T*>(q.out[2]) + to) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
                             }
-                        }
-                    });
+                        });
+                    }
                 }
             }
         }
@@ -759,10 +783,11 @@ ffn_few_kernel(const __grid_constant__ FewArgs a) {
 // Rows of `cols` values at any address -> rows of `ld` (a multiple of 8) at an aligned one: what TMA can read.  All
 // matrices of a call in one launch.
 struct AlignJobs {
-    static constexpr int kMost = 5;
+    static constexpr int kMost = 7;
     const void* src[kMost];
     void* dst[kMost];
     int64_t first[kMost + 1];   // 16-byte groups of the matrices before
+    uintptr_t end[kMost];       // where src ends
     int cols[kMost], ld[kMost];
     int n;
 };
@@ -775,10 +800,31 @@ align_rows_kernel(const __grid_constant__ AlignJobs a) {
         int k = 0;
         while (i >= a.first[k + 1]) ++k;
         const int groups = a.ld[k] / 8;
-        const int64_t at = i - a.first[k], r = at / groups;
+        const int64_t at = i - a.first[k];
+        const int64_t r = at >> 32 ? at / groups : (int64_t)((uint32_t)at / (uint32_t)groups);   // (the wide division costs 100 instructions)
         const int c = (int)(at - r * groups) * 8;
-        *reinterpret_cast<uint4*>(static_cast<T*>(a.dst[k]) + r * a.ld[k] + c) =
-            load8(static_cast<const T*>(a.src[k]) + r * a.cols[k], c, a.cols[k], false);
+        const T* row = static_cast<const T*>(a.src[k]) + r * a.cols[k];
+        const uintptr_t from = reinterpret_cast<uintptr_t>(row + c), block = from & ~(uintptr_t)15;
+        uint4 v;
+        if (c + 8 <= a.cols[k] && block >= reinterpret_cast<uintptr_t>(a.src[k]) && block + 32 <= a.end[k]) {
+            // eight values out of the two aligned 16-byte blocks they lie in, both within the matrix
+            const uint4 x = __ldg(reinterpret_cast<const uint4*>(block)), y = __ldg(reinterpret_cast<const uint4*>(block) + 1);
+            uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            const int shift = (int)(from & 15) >> 1;   // in values
+            if (shift & 4)
+#pragma unroll
+                for (int j = 0; j < 6; ++j) w[j] = w[j + 2];
+            if (shift & 2)
+#pragma unroll
+                for (int j = 0; j < 5; ++j) w[j] = w[j + 1];
+            if (shift & 1)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(w[j], w[j + 1], 16);
+            v = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            v = load8(row, c, a.cols[k], false);
+        }
+        *reinterpret_cast<uint4*>(static_cast<T*>(a.dst[k]) + r * a.ld[k] + c) = v;
     }
 }
 
@@ -840,7 +886,7 @@ cudaError_t launch_ffn(sama_ctx* ctx, Params<G>& P, int kind, const TilePlan& pl
     }
     P.whole = plan.whole;
     P.split = plan.split;
-    P.n_items = plan.whole + (tiles - plan.whole) * plan.split;
+    P.n_items = plan.split > 1 ? plan.whole + (tiles - plan.whole) * plan.split : tiles;
     P.parts = reinterpret_cast<float4*>(ctx->ffn_parts);
     P.arrived = ctx->ffn_arrived;
     P.group_m = 8;
@@ -882,13 +928,17 @@ cudaError_t prepare_ffn(sama_ctx* ctx) {
 // The fastest plan by estimate.  A launch's time is its rounds of tiles, each the longer of multiplying it and storing the
 // one before; a last round that would leave half of the units without a tile (or the only one) splits the contraction
 // of its tiles instead, which costs an exchange through L2.
-TilePlan plan_tiles(const sama_ctx* ctx, const Problem* p, int n, bool gate_up) {
+// (`tail`: a last round may be split while the others are not.)
+TilePlan plan_tiles(const sama_ctx* ctx, const Problem* p, int n, Mode mode, bool tail = true) {
     static const char* force = getenv("FFN_PLAN");
     TilePlan best = {false, 1 << 30, 1};
     double best_cost = -1.0;
     for (int pair = 0; pair < 2; ++pair) {
-        const int tm = pair ? 256 : 128, tn = (pair ? 256 : 128) / (gate_up ? 2 : 1), units = pair ? ctx->ffn_pair_units : ctx->sm_count;
-        const double t_kb = pair ? 0.28 : 0.16, t_store = pair ? 4.0 : 2.5, t_exchange = pair ? 4.0 : 2.5;
+        const int tm = pair ? 256 : 128, tn = (pair ? 256 : 128) / (mode == GATE_UP ? 2 : 1), units = pair ? ctx->ffn_pair_units : ctx->sm_count;
+        // microseconds, measured with a contraction of 64 (storing) and of 4096 (multiplying); a tile stores while the next
+        // one multiplies
+        const double t_exchange = 6.0;
+        const double t_store = mode == GATE_UP ? (pair ? 5.6 : 3.0) : mode == PLAIN ? (pair ? 3.5 : 2.0) : (pair ? 12.5 : 6.0);
         int64_t tiles = 0;
         int least_kb = 1 << 30, most_kb = 0;
         for (int i = 0; i < n; ++i) {
@@ -897,14 +947,16 @@ TilePlan plan_tiles(const sama_ctx* ctx, const Problem* p, int n, bool gate_up) 
             least_kb = p[i].num_kb < least_kb ? p[i].num_kb : least_kb;
             most_kb = p[i].num_kb > most_kb ? p[i].num_kb : most_kb;
         }
+        // (an SM takes in 64 bytes per cycle, all of them together less; pairs that run for long meet the power limit)
+        const double t_kb = pair ? (tiles > 2 * units ? 0.42 : 0.36) : (tiles > units / 2 ? 0.33 : 0.27);
         const double t_tile = most_kb * t_kb > t_store ? most_kb * t_kb : t_store;
         const int64_t rounds = tiles / units, rest = tiles - rounds * units;
         for (int split = 1; split <= 8; ++split) {
-            if (split > 1 && (rest * split > units || rest > kMaxSplitTiles || rest * split * (pair ? 4 : 1) > kMaxSplitParts || least_kb < 4 * split || rest == 0)) break;
+            if (split > 1 && (rest * split > units || rest > kMaxSplitTiles || rest * split * (pair ? 4 : 1) > kMaxSplitParts || least_kb < 4 * split || rest == 0 || (rounds > 0 && !tail))) break;
             const double cost = rounds * t_tile + (rest ? most_kb * t_kb / split : 0.0) + t_store + (split > 1 ? t_exchange : 0.0);
             if (force ? (force[0] - '0' == pair && force[1] - '0' == split) : (best_cost < 0.0 || cost < best_cost)) {
                 best_cost = cost;
-                best = {pair != 0, split > 1 ? (int)(rounds * units) : (int)tiles, split};
+                best = {pair != 0, split > 1 ? (int)(rounds * units) : 1 << 30, split};
             }
         }
     }
@@ -939,6 +991,7 @@ struct Block {
         if (vec_rows(p, cols)) return {p, rows, cols, cols};
         const int ld = up8(cols), k = jobs.n++;
         jobs.src[k] = p;
+        jobs.end[k] = reinterpret_cast<uintptr_t>(p) + (size_t)rows * cols * 2;
         jobs.dst[k] = take((size_t)rows * ld);
         jobs.cols[k] = cols;
         jobs.ld[k] = ld;
@@ -960,7 +1013,7 @@ struct Block {
     }
     template <int MODE, bool A_MN, bool B_MN, int G>
     void run(Params<G>& P, int kind) {
-        run<MODE, A_MN, B_MN, G>(P, kind, plan_tiles(ctx, P.p, G, MODE == GATE_UP));
+        run<MODE, A_MN, B_MN, G>(P, kind, plan_tiles(ctx, P.p, G, static_cast<Mode>(MODE)));
     }
     void check(bool ok) {
         if (!ok && err == cudaSuccess) err = cudaErrorInvalidValue;
@@ -1012,7 +1065,7 @@ struct Block {
             q.M = M;
             q.N = n;
             q.num_kb = q.kb_first = blocks_of(d, BK);
-            const TilePlan plan = plan_tiles(ctx, &q, 1, true);
+            const TilePlan plan = plan_tiles(ctx, &q, 1, GATE_UP);
             check(operand_map(&q.a[0], mx, f.dtype, false) && operand_map(&q.b[0], mg, f.dtype, false, plan.pair ? 128 : 64) &&
                   operand_map(&q.b[1], mu, f.dtype, false, plan.pair ? 128 : 64));
             set_output(q, 0, gate, n, n);
@@ -1040,6 +1093,7 @@ struct Block {
         const Matrix my = readable(dy, M, d), md = readable(wd, d, n), none = {};
         const Matrix mg = dx ? readable(wg, n, d) : none, mu = dx ? readable(wu, n, d) : none;
         const Matrix mx = dwg || dwu ? readable(x, M, d) : my;
+        const Matrix mgate = readable(gate, M, n), mup = readable(up, M, n);
         align();
         {
             Params<1> P = {};
@@ -1050,10 +1104,10 @@ struct Block {
             q.num_kb = q.kb_first = blocks_of(d, BK);
             void* outs[3] = {dg, du, h};
             for (int i = 0; i < 3; ++i) set_output(q, i, outs[i], fp, fp);
-            q.in[0] = gate;
-            q.in[1] = up;
-            q.ldi = n;
-            q.vec_in = (vec_rows(gate, n) ? 1 : 0) | (vec_rows(up, n) ? 2 : 0);
+            q.in[0] = mgate.p;
+            q.in[1] = mup.p;
+            q.ldi[0] = mgate.ld;
+            q.ldi[1] = mup.ld;
             P.act = f.act;
             run<D_HIDDEN, false, true, 1>(P, 2);
         }
@@ -1077,12 +1131,16 @@ struct Block {
         for (int i = 0; i < 3; ++i) {
             Problem& q = P.p[i];
             check(operand_map(&q.a[0], *w[i].a, f.dtype, true) && operand_map(&q.b[0], *w[i].b, f.dtype, true));
-            q.M = w[i].out ? w[i].rows : 0;   // a gradient that is not wanted has no tiles
+            q.M = w[i].rows;
             q.N = w[i].cols;
             q.num_kb = q.kb_first = blocks_of(M, BK);
             set_output(q, 0, w[i].out, w[i].cols, w[i].cols);
         }
-        run<PLAIN, true, true, 3>(P, 4);
+        // (planned for all three, so that a gradient's bits do not depend on which others are wanted)
+        const TilePlan plan = plan_tiles(ctx, P.p, 3, PLAIN, false);
+        for (int i = 0; i < 3; ++i)
+            if (!w[i].out) P.p[i].M = 0;   // no tiles
+        run<PLAIN, true, true, 3>(P, 4, plan);
     }
 };
 
@@ -1092,7 +1150,7 @@ struct Block {
 size_t ffn_workspace(const FfnShape& f, bool grad, bool copies) {
     const size_t M = (size_t)f.n_tokens, dp = up8(f.d), fp = up8(f.f);
     size_t b = (grad ? 3 : 1) * up256(M * fp * 2);
-    if (copies) b += 2 * up256(M * dp * 2) + 2 * up256((size_t)f.f * dp * 2) + up256((size_t)f.d * fp * 2);
+    if (copies) b += 2 * up256(M * dp * 2) + 2 * up256((size_t)f.f * dp * 2) + up256((size_t)f.d * fp * 2) + 2 * up256(M * fp * 2);
     return b;
 }
 
