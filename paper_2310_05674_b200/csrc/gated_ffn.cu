@@ -25,7 +25,6 @@
 // multiplied (two accumulators in tensor memory).  A CTA pair works on a 256 x 256 tile with cta_group::2 products; shapes with too few
 // of those take 128 x 128 tiles on single CTAs.  Every wait is bounded: one that expires raises SAMA_DEV_TIMEOUT, stops
 // the CTA's work, lets its copies land and exits.
-#include <cstdlib>
 #include <type_traits>
 
 #include "num_types.h"
@@ -48,9 +47,16 @@ enum Mode { GATE_UP, PLAIN, D_HIDDEN };
 // Staging of one epilogue warp: 32 rows of 64 columns, in 16 bits, or (d-hidden) in fp32.  Rows of 64 columns because the
 // load and store units take a cycle per 128-byte line: with steps of 16 columns the d-hidden epilogue of a pair's tile
 // was 25 % slower, although twice as many warps shared it.
-__host__ __device__ constexpr int staging_of(int mode) { return mode == D_HIDDEN ? 8192 : 4096; }
-__host__ __device__ constexpr int stages_of(int mode) { return mode == D_HIDDEN ? 5 : 6; }
-__host__ __device__ constexpr int smem_of(int mode) { return stages_of(mode) * STAGE + EPI * staging_of(mode) + 256 + 1024; }
+//
+// Units: a CTA pair on a 256 x 256 tile, a CTA on a 128 x 128 tile, or a cluster of 2, 4 or 8 CTAs on one 128 x 128 tile
+// whose contraction they share.  The latter exchange sums through distributed shared memory: a warp's 32 x 64 block of
+// the tile goes to the CTA that finishes it, which receives 64 KB in all and stages its output in the same place.
+enum Unit { SINGLE, PAIRED, SHARED };
+__host__ __device__ constexpr int staging_of(int mode, int unit) { return unit == SHARED || mode == D_HIDDEN ? 8192 : 4096; }
+__host__ __device__ constexpr int stages_of(int mode, int unit) { return unit == SHARED || mode == D_HIDDEN ? 5 : 6; }
+__host__ __device__ constexpr int smem_of(int mode, int unit) {
+    return stages_of(mode, unit) * STAGE + EPI * staging_of(mode, unit) + 256 + 1024;
+}
 
 
 struct Problem {
@@ -289,10 +295,11 @@ __device__ __forceinline__ uint4 load8(const T* p, int col, int cols, bool vec) 
 
 // ---------------------------------------------------------------- the kernel
 
-template <typename T, int MODE, bool PAIR, bool A_MN, bool B_MN, int G>
+template <typename T, int MODE, int UNIT, bool A_MN, bool B_MN, int G>
 __global__ void __launch_bounds__(THREADS, 1)
 ffn_kernel(const __grid_constant__ Params<G> P) {
-    constexpr int STAGES = stages_of(MODE), STAGING = staging_of(MODE);
+    constexpr bool PAIR = UNIT == PAIRED;
+    constexpr int STAGES = stages_of(MODE, UNIT), STAGING = staging_of(MODE, UNIT);
     constexpr int BN = PAIR ? 256 : 128;                // accumulator columns
     constexpr int TN = MODE == GATE_UP ? BN / 2 : BN;   // output columns (features) of a tile
     constexpr int TM = PAIR ? 2 * BM : BM;
@@ -363,7 +370,7 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
     }
     tc_fence_before();
     __syncthreads();
-    if (PAIR) cluster_sync();  // the other CTA's barriers exist before anything is signalled on them
+    if (UNIT != SINGLE) cluster_sync();  // the other CTAs run, and their barriers exist, before anything reaches them
     tc_fence_after();
     const uint32_t tmem_base = *tmem_ptr_slot;
     pdl_trigger();
@@ -421,6 +428,10 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                 for (int i = (issued > STAGES ? issued - STAGES : 0); i < issued; ++i) mbar_wait(full_bar(i % STAGES), (i / STAGES) & 1);
             }
         }
+        if (UNIT == SHARED) {
+            __syncwarp();
+            cluster_sync();
+        }
     } else if (warp == 1) {
         // ---------------------------------------------------------- products (the leader's, for a pair)
         if (lane == 0 && rank == 0) {
@@ -452,6 +463,10 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                 if (!ok) break;
                 if (PAIR) umma_commit_pair(acc_full_bar(buf)); else umma_commit(acc_full_bar(buf));
             }
+        }
+        if (UNIT == SHARED) {
+            __syncwarp();
+            cluster_sync();
         }
     } else {
         // ---------------------------------------------------------- epilogue
@@ -497,7 +512,10 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                 }
             }
             ok = __shfl_sync(0xffffffffu, ok, 0);
-            if (!ok) break;
+            if (!ok) {
+                if (UNIT == SHARED) cluster_sync();   // the other CTAs wait for this one there
+                break;
+            }
             tc_fence_after();
             // Hands the accumulator back.  (Not for the last two tiles: nobody waits for them, and no arrival may be
             // on its way to the other CTA when that one exits.)
@@ -512,10 +530,44 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
             auto column = [&](int step) {
                 return MODE == GATE_UP ? (step / (STEPS / 2)) * TN + share * (CPW / 2) + step % (STEPS / 2) * 16 : share * CPW + step * 16;
             };
+            if constexpr (UNIT == SHARED) {
+                // Block (quarter, share) of the tile goes to one CTA of the cluster, part by part; its warp there adds the
+                // parts in their order, puts the sums back into tensor memory and goes on with them.
+                const int block = quarter * 2 + share, per_cta = EPI / P.split;
+                const uint32_t owner = (uint32_t)(block / per_cta);
+                const uint32_t place = staging + (uint32_t)(block % per_cta) * P.split * 8192u + (uint32_t)lane * 16u;
+                const uint32_t there = map_to_rank(place + (uint32_t)w.part * 8192u, owner);
+#pragma unroll 1
+                for (int st = 0; st < STEPS; ++st) {
+                    float v[16];
+                    tmem_ld16(acc + column(st), v);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) st_cluster_f4(there + (uint32_t)(st * 4 + k) * 512u, v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                }
+                cluster_sync();
+                if (owner != (uint32_t)w.part) break;   // (one tile per cluster)
+                const float4* parts = reinterpret_cast<const float4*>(smem_raw + (place - raw));
+#pragma unroll 1
+                for (int st = 0; st < STEPS; ++st) {
+                    float sum[16];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[j] = 0.f;
+#pragma unroll 2
+                    for (int p = 0; p < P.split; ++p)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float4 x = parts[p * 512 + (st * 4 + k) * 32];
+                            sum[4 * k] += x.x; sum[4 * k + 1] += x.y; sum[4 * k + 2] += x.z; sum[4 * k + 3] += x.w;
+                        }
+                    tmem_st16(acc + column(st), sum);
+                }
+                // from here on the block's own place, which only this warp reads, is its staging area
+                stg = reinterpret_cast<uint4*>(smem_raw + (place - raw) - lane * 16);
+            }
             // A tile whose contraction is split: every part's warps leave their sums in the workspace; the one that finds
             // all others there adds them up in the order of the parts (its own among them), puts the result back into
             // tensor memory and goes on with it.
-            if (w.split_tile >= 0) {
+            if (UNIT != SHARED && w.split_tile >= 0) {
                 constexpr int CTAS = PAIR ? 2 : 1, SLAB = STEPS * 4 * 32;
                 const int64_t stride = (int64_t)CTAS * EPI * SLAB;
                 float4* base = P.parts + (((int64_t)w.split_tile * P.split * CTAS + rank) * EPI + (warp - 2)) * SLAB + lane;
@@ -861,17 +913,18 @@ inline int blocks_of(int64_t x, int b) { return (int)((x + b - 1) / b); }
 
 // How a launch's tiles are worked on.
 struct TilePlan {
-    bool pair;
+    Unit unit;
     int whole, split;
 };
 constexpr int kMaxSplitTiles = 256, kMaxSplitParts = 512;   // of 128 x 128 values per CTA; twice as many per CTA of a pair
 
-template <typename T, int MODE, bool PAIR, bool A_MN, bool B_MN, int G>
+template <typename T, int MODE, int UNIT, bool A_MN, bool B_MN, int G>
 cudaError_t launch_ffn(sama_ctx* ctx, Params<G>& P, int kind, const TilePlan& plan, cudaStream_t st) {
-    auto* kernel = ffn_kernel<T, MODE, PAIR, A_MN, B_MN, G>;
-    const uint32_t bit = 1u << (4 * kind + (PAIR ? 2 : 0) + (std::is_same<T, __half>::value ? 1 : 0));
+    constexpr bool PAIR = UNIT == PAIRED;
+    auto* kernel = ffn_kernel<T, MODE, UNIT, A_MN, B_MN, G>;
+    const uint32_t bit = 1u << (6 * kind + 2 * UNIT + (std::is_same<T, __half>::value ? 1 : 0));
     if (!(ctx->ffn_ready & bit)) {  // once per context: the opt-in to this much shared memory
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(MODE));
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(MODE, UNIT));
         if (e != cudaSuccess) return e;
         ctx->ffn_ready |= bit;
     }
@@ -892,31 +945,40 @@ cudaError_t launch_ffn(sama_ctx* ctx, Params<G>& P, int kind, const TilePlan& pl
     P.group_m = 8;
     P.status = &ctx->scalars->status;
     const int max_units = PAIR ? ctx->ffn_pair_units : ctx->sm_count, items = P.n_items;
-    const int units = items < max_units ? items : max_units;
+    const int units = UNIT == SHARED || items < max_units ? items : max_units;   // (shared: one tile per cluster)
     KernelScope scope(ctx, SAMA_K_FFN, kind, st);
-    return launch_clustered(PAIR ? 2 : 1, kernel, dim3(units * (PAIR ? 2 : 1)), dim3(THREADS), (size_t)smem_of(MODE), st, P);
+    return launch_clustered(PAIR ? 2 : UNIT == SHARED ? plan.split : 1, kernel, dim3(units * (PAIR ? 2 : 1)), dim3(THREADS),
+                            (size_t)smem_of(MODE, UNIT), st, P);
 }
 
-// Once per context: how many CTA pairs of the kernel can be resident, and the workspace of split tiles.
+// Once per context: how many CTA pairs and clusters of the kernel can be resident, and the workspace of split tiles.
 cudaError_t prepare_ffn(sama_ctx* ctx) {
     if (ctx->ffn_pair_units > 0) return cudaSuccess;
-    auto* kernel = ffn_kernel<__nv_bfloat16, PLAIN, true, false, false, 1>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(PLAIN));
+    auto* kernel = ffn_kernel<__nv_bfloat16, PLAIN, PAIRED, false, false, 1>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(PLAIN, PAIRED));
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * (ctx->sm_count / 2));
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = smem_of(PLAIN);
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    auto* sharing = ffn_kernel<__nv_bfloat16, PLAIN, SHARED, false, false, 1>;
+    e = cudaFuncSetAttribute(sharing, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_of(PLAIN, SHARED));
+    if (e != cudaSuccess) return e;
+    auto resident = [&](auto* k, int size, int smem, int* clusters) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(ctx->sm_count / size * size);
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = size;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaOccupancyMaxActiveClusters(clusters, k, &cfg);
+    };
     int clusters = 0;
-    if ((e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg)) != cudaSuccess) return e;
+    if ((e = resident(kernel, 2, smem_of(PLAIN, PAIRED), &clusters)) != cudaSuccess) return e;
     if (clusters < 1) return cudaErrorLaunchOutOfResources;
+    for (int i = 0; i < 3; ++i)
+        if ((e = resident(sharing, 2 << i, smem_of(PLAIN, SHARED), &ctx->ffn_clusters[i])) != cudaSuccess) return e;
     const size_t counters = sizeof(int) * kMaxSplitTiles * 2 * EPI;
     if (!ctx->ffn_parts && (e = cudaMalloc(&ctx->ffn_parts, sizeof(float) * kMaxSplitParts * BM * 128)) != cudaSuccess) return e;
     if (!ctx->ffn_arrived && (e = cudaMalloc(&ctx->ffn_arrived, counters)) != cudaSuccess) return e;
@@ -926,18 +988,18 @@ cudaError_t prepare_ffn(sama_ctx* ctx) {
 }
 
 // The fastest plan by estimate.  A launch's time is its rounds of tiles, each the longer of multiplying it and storing the
-// one before; a last round that would leave half of the units without a tile (or the only one) splits the contraction
-// of its tiles instead, which costs an exchange through L2.
+// one before.  A last round that would leave half of the pairs without a tile splits the contraction of its tiles instead,
+// which costs an exchange through L2; tiles too few for one round of CTAs are shared by clusters.
 // (`tail`: a last round may be split while the others are not.)
 TilePlan plan_tiles(const sama_ctx* ctx, const Problem* p, int n, Mode mode, bool tail = true) {
-    static const char* force = getenv("FFN_PLAN");
-    TilePlan best = {false, 1 << 30, 1};
+    TilePlan best = {SINGLE, 1 << 30, 1};
     double best_cost = -1.0;
-    for (int pair = 0; pair < 2; ++pair) {
+    for (int u = SINGLE; u <= SHARED; ++u) {
+        const bool pair = u == PAIRED;
         const int tm = pair ? 256 : 128, tn = (pair ? 256 : 128) / (mode == GATE_UP ? 2 : 1), units = pair ? ctx->ffn_pair_units : ctx->sm_count;
         // microseconds, measured with a contraction of 64 (storing) and of 4096 (multiplying); a tile stores while the next
         // one multiplies
-        const double t_exchange = 6.0;
+        const double t_exchange = pair ? 9.0 : 3.0;
         const double t_store = mode == GATE_UP ? (pair ? 5.6 : 3.0) : mode == PLAIN ? (pair ? 3.5 : 2.0) : (pair ? 12.5 : 6.0);
         int64_t tiles = 0;
         int least_kb = 1 << 30, most_kb = 0;
@@ -947,16 +1009,19 @@ TilePlan plan_tiles(const sama_ctx* ctx, const Problem* p, int n, Mode mode, boo
             least_kb = p[i].num_kb < least_kb ? p[i].num_kb : least_kb;
             most_kb = p[i].num_kb > most_kb ? p[i].num_kb : most_kb;
         }
-        // (an SM takes in 64 bytes per cycle, all of them together less; pairs that run for long meet the power limit)
-        const double t_kb = pair ? (tiles > 2 * units ? 0.42 : 0.36) : (tiles > units / 2 ? 0.33 : 0.27);
-        const double t_tile = most_kb * t_kb > t_store ? most_kb * t_kb : t_store;
         const int64_t rounds = tiles / units, rest = tiles - rounds * units;
-        for (int split = 1; split <= 8; ++split) {
-            if (split > 1 && (rest * split > units || rest > kMaxSplitTiles || rest * split * (pair ? 4 : 1) > kMaxSplitParts || least_kb < 4 * split || rest == 0 || (rounds > 0 && !tail))) break;
+        for (int split = u == SHARED ? 2 : 1; split <= 8; split = u == SHARED ? 2 * split : split + 1) {
+            if (u == SINGLE && split > 1) break;
+            if (split > 1 && (rest == 0 || rest * split > units || least_kb < 2 * split)) break;
+            if (pair && split > 1 && (rest > kMaxSplitTiles || rest * split * 4 > kMaxSplitParts || (rounds > 0 && !tail))) break;
+            if (u == SHARED && (rounds > 0 || tiles > ctx->ffn_clusters[split == 2 ? 0 : split == 4 ? 1 : 2])) break;
+            // (an SM takes in 64 bytes per cycle, all of them together less; pairs that run for long meet the power limit)
+            const double t_kb = pair ? (tiles > 2 * units ? 0.42 : 0.36) : (tiles * split > units / 2 ? 0.33 : 0.27);
+            const double t_tile = most_kb * t_kb > t_store ? most_kb * t_kb : t_store;
             const double cost = rounds * t_tile + (rest ? most_kb * t_kb / split : 0.0) + t_store + (split > 1 ? t_exchange : 0.0);
-            if (force ? (force[0] - '0' == pair && force[1] - '0' == split) : (best_cost < 0.0 || cost < best_cost)) {
+            if (best_cost < 0.0 || cost < best_cost) {
                 best_cost = cost;
-                best = {pair != 0, split > 1 ? (int)(rounds * units) : 1 << 30, split};
+                best = {static_cast<Unit>(u), split > 1 ? (int)(rounds * units) : 1 << 30, split};
             }
         }
     }
@@ -1008,8 +1073,9 @@ struct Block {
     template <int MODE, bool A_MN, bool B_MN, int G>
     void run(Params<G>& P, int kind, const TilePlan& plan) {
         if (err != cudaSuccess) return;
-        err = plan.pair ? launch_ffn<T, MODE, true, A_MN, B_MN, G>(ctx, P, kind, plan, st)
-                        : launch_ffn<T, MODE, false, A_MN, B_MN, G>(ctx, P, kind, plan, st);
+        err = plan.unit == PAIRED   ? launch_ffn<T, MODE, PAIRED, A_MN, B_MN, G>(ctx, P, kind, plan, st)
+              : plan.unit == SHARED ? launch_ffn<T, MODE, SHARED, A_MN, B_MN, G>(ctx, P, kind, plan, st)
+                                    : launch_ffn<T, MODE, SINGLE, A_MN, B_MN, G>(ctx, P, kind, plan, st);
     }
     template <int MODE, bool A_MN, bool B_MN, int G>
     void run(Params<G>& P, int kind) {
@@ -1066,8 +1132,8 @@ struct Block {
             q.N = n;
             q.num_kb = q.kb_first = blocks_of(d, BK);
             const TilePlan plan = plan_tiles(ctx, &q, 1, GATE_UP);
-            check(operand_map(&q.a[0], mx, f.dtype, false) && operand_map(&q.b[0], mg, f.dtype, false, plan.pair ? 128 : 64) &&
-                  operand_map(&q.b[1], mu, f.dtype, false, plan.pair ? 128 : 64));
+            check(operand_map(&q.a[0], mx, f.dtype, false) && operand_map(&q.b[0], mg, f.dtype, false, plan.unit == PAIRED ? 128 : 64) &&
+                  operand_map(&q.b[1], mu, f.dtype, false, plan.unit == PAIRED ? 128 : 64));
             set_output(q, 0, gate, n, n);
             set_output(q, 1, up, n, n);
             set_output(q, 2, h, fp, fp);

@@ -134,6 +134,7 @@ struct sama_ctx {
     int clip_ready;                // the small clipping kernel's cluster size is allowed on this device
     uint32_t ffn_ready;            // kernels of gated_ffn.cu whose shared-memory size is set on this device
     int ffn_pair_units;            // CTA pairs of them that can be resident (0: not yet asked)
+    int ffn_clusters[3];           // ... and clusters of 2, 4 and 8 CTAs
     float* ffn_parts;              // device: sums of tiles whose contraction several CTAs share
     int* ffn_arrived;              // device: arrival counters of such tiles, zero between launches
     sama::Profiler* prof;          // host
