@@ -17,6 +17,8 @@
 //   embed_reduce : a warp adds up one piece of the list for 32 threads' columns.  A run that lies inside a piece is
 //                  written out; the parts of a run that crosses pieces go to the workspace in fp32, and the warps that
 //                  finish last add them up, in the order of the list.  The first blocks write the zeros still missing.
+// Up to 2048 tokens, where launches and round trips are what counts, one launch: every CTA sorts all tokens for itself in
+// shared memory, then takes its share of the pieces and of the rows to be zeroed.
 #include "num_types.h"
 #include "sama_internal.h"
 
@@ -110,6 +112,26 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(const uint32_t* p, uint32_t c
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
     return v;
+}
+
+// The place of this lane's element among those of its digit: the warp's next places (`next`, by digit) are handed out in
+// the order of the lanes.  Lanes of one digit find each other with one vote per bit (the instruction that matches whole
+// values takes a step per distinct value, 200 cycles for a warp of different digits).
+template <int MOST>
+__device__ __forceinline__ uint32_t take_place(uint32_t* next, bool on, uint32_t digit, int bits, int lane) {
+    uint32_t same = __ballot_sync(0xffffffffu, on);
+#pragma unroll
+    for (int b = 0; b < MOST; ++b) {
+        if (b >= bits) break;
+        const bool set = (digit & (1u << b)) != 0;
+        same &= __ballot_sync(0xffffffffu, set) ^ (set ? 0u : 0xffffffffu);
+    }
+    uint32_t at = 0;
+    if (on) at = next[digit] + __popc(same & ((1u << lane) - 1u));
+    __syncwarp();
+    if (on && lane == __ffs(same) - 1) next[digit] += __popc(same);
+    __syncwarp();
+    return at;
 }
 
 struct SortArgs {
@@ -284,22 +306,9 @@ embed_sort_kernel(const __grid_constant__ SortArgs a) {
                 if (i - lane + 32 * u >= end) break;
                 const bool on = e[u].x >= 0;
                 const uint32_t digit = on ? ((uint32_t)e[u].x >> shift) & (bins - 1) : 0u;
-                // lanes with the same digit, one vote per bit (the instruction that matches whole values takes a step per
-                // distinct value: 200 cycles for a warp of different digits)
-                uint32_t same = __ballot_sync(0xffffffffu, on);
-#pragma unroll
-                for (int b = 0; b < kMaxBits; ++b) {   // (bits the digit does not have are 0 everywhere)
-                    const bool set = (digit & (1u << b)) != 0;
-                    same &= __ballot_sync(0xffffffffu, set) ^ (set ? 0u : 0xffffffffu);
-                }
-                uint32_t at = 0;
-                if (on) at = sm.hist[warp][digit] + __popc(same & ((1u << lane) - 1u));
-                __syncwarp();
-                if (on) {
-                    if (once) sm.stage[at] = e[u]; else dst[at] = e[u];
-                    if (lane == __ffs(same) - 1) sm.hist[warp][digit] += __popc(same);
-                }
-                __syncwarp();
+                const uint32_t at = take_place<kMaxBits>(sm.hist[warp], on, digit, a.bits, lane);
+                if (!on) continue;
+                if (once) sm.stage[at] = e[u]; else dst[at] = e[u];
             }
         }
         if (once) {
@@ -434,18 +443,41 @@ __device__ __forceinline__ bool last_to_arrive(int* counter, int parts, int lane
     if (lane == 0) before = atomicAdd(counter, 1);
     before = __shfl_sync(0xffffffffu, before, 0);
     if (before != parts - 1) return false;
+    if (lane == 0) *counter = 0;   // (embed_few's counters stay between calls)
     __threadfence();
     return true;
 }
 
+// The sorted list in global memory, with the rows' runs beside it, or in shared memory, where a run is quickly found.
+struct GlobalList {
+    const int2* list;
+    const int2* span;
+    __device__ __forceinline__ int2 at(int i) const { return list[i]; }
+    __device__ __forceinline__ int2 run(int key) const { return span[key]; }
+};
+struct SharedList {
+    const int2* list;
+    int n;
+    __device__ __forceinline__ int2 at(int i) const { return list[i]; }
+    __device__ __forceinline__ int first_not_below(int key) const {
+        int lo = 0, hi = n;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (list[mid].x < key) lo = mid + 1; else hi = mid;
+        }
+        return lo;
+    }
+    __device__ __forceinline__ int2 run(int key) const { return make_int2(first_not_below(key), first_not_below(key + 1)); }
+};
+
 // This warp has stored its part, in piece k, of a run over pieces k0 .. k1.  The parts are joined in groups of kJoin
 // pieces, then the groups: the last to store a part adds up its group, the last to store a group's sum (in the place of
 // its first part) adds up the groups.
-template <typename TG, int VE>
-__device__ __forceinline__ void join_run(const ReduceArgs& a, int key, int k, int slab, int lane) {
+template <typename TG, int VE, typename List>
+__device__ __forceinline__ void join_run(const ReduceArgs& a, const List& list, int key, int k, int slab, int lane) {
     const int c = (slab * 32 + lane) * VE;
     const bool on = c < a.d;
-    const int2 run = a.span[key];
+    const int2 run = list.run(key);
     const int k0 = run.x / a.piece, k1 = (run.y - 1) / a.piece;
     const int g = k / kJoin, g0 = k0 / kJoin, g1 = k1 / kJoin;
     const int first = max(k0, g * kJoin), last = min(k1, g * kJoin + kJoin - 1);
@@ -468,34 +500,17 @@ __device__ __forceinline__ void join_run(const ReduceArgs& a, int key, int k, in
     if (on) put_row<TG, VE>(a, key, c, sum);
 }
 
-// One warp: piece k of the list, columns [32 VE slab, 32 VE (slab + 1)).
-template <typename T, typename TG, int VE>
-__global__ void __launch_bounds__(kEmbedThreads, 3)
-embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
-    pdl_trigger();
-    pdl_wait();
-    constexpr int U = 8;  // rows in flight per thread
-    const int lane = threadIdx.x & 31;
-    if ((int)blockIdx.x < a.fill_blocks) {
-        const FillArgs& f = a.fill;
-        for (int w = (int)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5); w < kFillCtas * 32; w += a.fill_blocks * (kEmbedThreads / 32)) {
-            const int64_t first = (w / 32) * f.share, stop = min((int64_t)f.vocab, first + f.share);
-            for (int64_t row = first + (int64_t)f.progress[w] * 32 + w % 32; row < stop; row += 32)
-                zero_row_if_absent(f, row, f.present[row / 32], lane);
-        }
-        return;
-    }
-    const int64_t unit = (int64_t)(blockIdx.x - a.fill_blocks) * (kEmbedThreads / 32) + (threadIdx.x >> 5);
-    const int k = (int)(unit / a.slabs), slab = (int)(unit - (int64_t)k * a.slabs);
-    if (k >= a.pieces) return;
+// One warp: piece k of the list, columns [32 VE slab, 32 VE (slab + 1)), U rows in flight per thread.
+template <typename T, typename TG, int VE, int U, typename List>
+__device__ __forceinline__ void reduce_piece(const ReduceArgs& a, const List& list, int k, int slab, int lane) {
     const int i0 = k * a.piece, count = min(a.n - i0, a.piece);
     const int c = (slab * 32 + lane) * VE;
     const bool on = c < a.d;   // (the other lanes of the last slab go along for the warp's sake)
     const T* dout = static_cast<const T*>(a.dout) + (on ? c : 0);
     // the piece's entries, two per lane
     const int2 none = make_int2(a.vocab, 0);
-    const int2 low = lane < count ? a.list[i0 + lane] : none, high = lane + 32 < count ? a.list[i0 + lane + 32] : none;
-    const int before_key = i0 > 0 ? a.list[i0 - 1].x : -1, after_key = i0 + count < a.n ? a.list[i0 + count].x : -1;
+    const int2 low = lane < count ? list.at(i0 + lane) : none, high = lane + 32 < count ? list.at(i0 + lane + 32) : none;
+    const int before_key = i0 > 0 ? list.at(i0 - 1).x : -1, after_key = i0 + count < a.n ? list.at(i0 + count).x : -1;
     const int first_key = __shfl_sync(0xffffffffu, low.x, 0);
     const bool open_head = before_key == first_key && first_key < a.vocab;
     int key = first_key;
@@ -546,14 +561,169 @@ embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
 #pragma unroll 1
     for (int j = 0; j < 2; ++j) {
         const int run = j == 0 ? first_key : key;
-        if (j == 0 ? open_head : (open_tail && !in_head)) join_run<TG, VE>(a, run, k, slab, lane);
+        if (j == 0 ? open_head : (open_tail && !in_head)) join_run<TG, VE>(a, list, run, k, slab, lane);
     }
 }
 
+template <typename T, typename TG, int VE>
+__global__ void __launch_bounds__(kEmbedThreads, 3)
+embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    if ((int)blockIdx.x < a.fill_blocks) {
+        const FillArgs& f = a.fill;
+        for (int w = (int)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5); w < kFillCtas * 32; w += a.fill_blocks * (kEmbedThreads / 32)) {
+            const int64_t first = (w / 32) * f.share, stop = min((int64_t)f.vocab, first + f.share);
+            for (int64_t row = first + (int64_t)f.progress[w] * 32 + w % 32; row < stop; row += 32)
+                zero_row_if_absent(f, row, f.present[row / 32], lane);
+        }
+        return;
+    }
+    const int64_t unit = (int64_t)(blockIdx.x - a.fill_blocks) * (kEmbedThreads / 32) + (threadIdx.x >> 5);
+    const int k = (int)(unit / a.slabs), slab = (int)(unit - (int64_t)k * a.slabs);
+    // (single values: twice the rows, for half as many bytes in flight or less)
+    if (k < a.pieces) reduce_piece<T, TG, VE, VE == 1 ? 16 : 8>(a, GlobalList{a.list, a.span}, k, slab, lane);
+}
+
+// ------------------------------------------------------------------ few tokens
+
+// (512 threads: with 1024 the reduction's 64 registers spill a kilobyte)
+constexpr int kFewTokens = 2048, kFewThreads = 512, kFewWarps = kFewThreads / 32, kFewPer = kFewTokens / kFewThreads;
+constexpr int kFewBits = 9, kFewBins = 1 << kFewBits, kFewCounters = 1 << 16;
+constexpr int kFewShare = 1 << 18;   // rows whose presence a CTA can track
+struct FewSmem {
+    uint32_t hist[kFewWarps][kFewBins];
+    int2 list[2][kFewTokens];
+    uint32_t warp_sum[kFewWarps];
+    uint32_t present[kFewShare / 32];      // a bit per row of this CTA's share
+    int next_row;
+};
+
+struct FewArgs {
+    const int32_t* ids;
+    int passes, bits;
+    int32_t skip_id;
+    int64_t share;       // rows per CTA, a multiple of 32; 0: nothing is zeroed
+    int32_t* status;
+};
+
+template <typename T, typename TG, int VE>
+__global__ void __launch_bounds__(kFewThreads, 1)
+embed_few_kernel(const __grid_constant__ ReduceArgs a, const __grid_constant__ FewArgs f) {
+    extern __shared__ uint8_t few_raw[];
+    FewSmem& sm = *reinterpret_cast<FewSmem*>(few_raw);
+    static_assert(sizeof(FewSmem) <= 227 * 1024, "");
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = a.n, bins = 1 << f.bits;
+    pdl_trigger();
+    pdl_wait();
+    // The sort of embed_sort, on one CTA: a warp has up to kFewPer runs of 32 consecutive elements.
+    const int per_warp = ((n + kFewWarps - 1) / kFewWarps + 31) & ~31, begin = warp * per_warp, end = min(n, begin + per_warp);
+    int2 e[kFewPer];
+#pragma unroll
+    for (int u = 0; u < kFewPer; ++u) {
+        const int i = begin + 32 * u + lane;
+        e[u] = make_int2(-1, 0);
+        if (i < end) {
+            const int32_t id = f.ids[i];
+            const bool good = id >= 0 && id < a.vocab;
+            if (!good && blockIdx.x == 0) atomicOr(f.status, (int)SAMA_DEV_BAD_INDEX);
+            e[u] = make_int2(good && id != f.skip_id ? id : a.vocab, i);
+        }
+    }
+    // which rows of this CTA's share have a token
+    const int64_t first_row = blockIdx.x * f.share;
+    const int rows = (int)max((int64_t)0, min((int64_t)a.vocab, first_row + f.share) - first_row);
+    for (int i = threadIdx.x; i < (rows + 31) / 32; i += kFewThreads) sm.present[i] = 0;
+    if (threadIdx.x == 0) sm.next_row = 0;
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kFewPer; ++u) {
+        const int64_t r = (int64_t)e[u].x - first_row;
+        if (e[u].x >= 0 && r >= 0 && r < rows) atomicOr(sm.present + (r >> 5), 1u << (r & 31));
+    }
+    for (int p = 0; p < f.passes; ++p) {
+        const int shift = f.bits * p;
+        for (int b = lane; b < bins; b += 32) sm.hist[warp][b] = 0;
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < kFewPer; ++u)
+            if (e[u].x >= 0) atomicAdd(&sm.hist[warp][((uint32_t)e[u].x >> shift) & (bins - 1)], 1u);
+        __syncthreads();
+        uint32_t mine = 0;   // thread b owns bin b
+        if (threadIdx.x < bins) {
+            uint32_t c[kFewWarps];
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) c[w] = sm.hist[w][threadIdx.x];
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) mine += c[w];
+        }
+        uint32_t incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) sm.warp_sum[warp] = incl;
+        __syncthreads();
+        uint32_t at = __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[lane] : 0u) + incl - mine;
+        if (threadIdx.x < bins) {
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) {
+                const uint32_t c = sm.hist[w][threadIdx.x];
+                sm.hist[w][threadIdx.x] = at;
+                at += c;
+            }
+        }
+        __syncthreads();
+        int2* dst = sm.list[p & 1];
+#pragma unroll
+        for (int u = 0; u < kFewPer; ++u) {
+            if (begin + 32 * u >= end) break;
+            const bool on = e[u].x >= 0;
+            const uint32_t digit = on ? ((uint32_t)e[u].x >> shift) & (bins - 1) : 0u;
+            const uint32_t to = take_place<kFewBits>(sm.hist[warp], on, digit, f.bits, lane);
+            if (on) dst[to] = e[u];
+        }
+        __syncthreads();
+        if (p + 1 < f.passes) {
+#pragma unroll
+            for (int u = 0; u < kFewPer; ++u) {
+                const int i = begin + 32 * u + lane;
+                if (i < end) e[u] = dst[i];
+            }
+        }
+    }
+    const SharedList list{sm.list[(f.passes - 1) & 1], n};
+    // this CTA's share of the pieces, neighbouring ones on different CTAs
+    const int64_t units = (int64_t)a.pieces * a.slabs;
+    for (int64_t unit = (int64_t)warp * gridDim.x + blockIdx.x; unit < units; unit += (int64_t)kFewWarps * gridDim.x) {
+        const int k = (int)(unit / a.slabs), slab = (int)(unit - (int64_t)k * a.slabs);
+        reduce_piece<T, TG, VE, 4>(a, list, k, slab, lane);
+    }
+    // zeros to the rows without a token, by the warps that have no piece (any more)
+    for (;;) {
+        int r0 = 0;
+        if (lane == 0) r0 = atomicAdd(&sm.next_row, 4);
+        r0 = __shfl_sync(0xffffffffu, r0, 0);
+        if (r0 >= rows) break;
+        for (int r = r0; r < min(r0 + 4, rows); ++r) zero_row_if_absent(a.fill, first_row + r, sm.present[r >> 5], lane);
+    }
+}
+
+// Threads (a power of two, at most a block) that share a row of `chunks` vectors: the number that leaves the fewest idle in
+// the last round, the larger one of equals.
 int threads_per_row(int d, int ve) {
-    int t = 1;
-    while (t < kEmbedThreads && t * ve < d) t *= 2;
-    return t;
+    const int chunks = (d + ve - 1) / ve;
+    int best = 1;
+    int64_t least = (int64_t)1 << 62;
+    for (int t = 1; t <= kEmbedThreads && t < 2 * chunks; t *= 2) {
+        const int64_t rounds = (chunks + t - 1) / t;
+        // (a round more costs about as much as eight idle threads)
+        const int64_t cost = rounds * t + 8 * rounds;
+        if (cost <= least) { least = cost; best = t; }
+    }
+    return best;
 }
 
 template <typename T>
@@ -571,21 +741,21 @@ cudaError_t embed_typed(sama_ctx* ctx, int64_t n, int64_t vocab, int d, const vo
                             d, tpr, static_cast<const T*>(table), ids, scale, static_cast<T*>(out), &ctx->scalars->status);
 }
 
-// Entries per piece: as many as still give every SM 16 warps, 8 to 64.
+// Entries per piece: as many as still give every SM 24 warps, 8 to 64.
 int piece_of(const sama_ctx* ctx, int64_t n, int slabs) {
     int piece = 64;
-    while (piece > 8 && (n + piece - 1) / piece * slabs < (int64_t)ctx->sm_count * 16) piece /= 2;
+    while (piece > 8 && (n + piece - 1) / piece * slabs < (int64_t)ctx->sm_count * 24) piece /= 2;
     return piece;
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct GradPlan {
-    bool vec;
+    bool vec, few;
     int ve, slabs, piece, pieces, counters;
     int64_t share;
     size_t list, span, arrived, present, progress, parts;  // bytes
-    size_t total() const { return 2 * list + span + arrived + present + progress + 2 * parts; }
+    size_t total() const { return few ? 2 * parts : 2 * list + span + arrived + present + progress + 2 * parts; }
 };
 GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout, int grad_dtype,
                    const void* grad) {
@@ -599,6 +769,7 @@ GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int
     g.list = up256(sizeof(int2) * (size_t)n);
     g.span = up256(sizeof(int2) * (size_t)vocab);
     g.counters = (2 * g.pieces + (g.pieces + kJoin - 1) / kJoin) * g.slabs;
+    g.few = n <= kFewTokens && g.counters <= kFewCounters && vocab <= (int64_t)ctx->sm_count * (kFewShare / 2);
     g.arrived = up256(sizeof(int) * (size_t)g.counters);
     g.share = ((vocab + kFillCtas - 1) / kFillCtas + 31) & ~(int64_t)31;
     g.present = up256((size_t)(g.share / 32) * kFillCtas * 4);
@@ -608,12 +779,53 @@ GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int
 }
 
 template <typename T, typename TG>
-cudaError_t reduce_typed(sama_ctx* ctx, const ReduceArgs& a, bool vec, cudaStream_t st) {
-    constexpr int VE = 16 / sizeof(T);
-    KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
-    auto* kernel = vec ? embed_reduce_kernel<T, TG, VE> : embed_reduce_kernel<T, TG, 1>;
-    const int64_t units = (int64_t)a.pieces * a.slabs, per = kEmbedThreads / 32;
-    return launch_dependent(kernel, dim3((unsigned)(a.fill_blocks + (units + per - 1) / per)), dim3(kEmbedThreads), 0, st, a);
+struct ReduceLaunch {
+    static cudaError_t run(sama_ctx* ctx, const ReduceArgs& a, bool vec, cudaStream_t st) {
+        constexpr int VE = 16 / sizeof(T);
+        KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
+        auto* kernel = vec ? embed_reduce_kernel<T, TG, VE> : embed_reduce_kernel<T, TG, 1>;
+        const int64_t units = (int64_t)a.pieces * a.slabs, per = kEmbedThreads / 32;
+        return launch_dependent(kernel, dim3((unsigned)(a.fill_blocks + (units + per - 1) / per)), dim3(kEmbedThreads), 0, st, a);
+    }
+};
+template <typename T, typename TG>
+struct FewLaunch {
+    static cudaError_t run(sama_ctx* ctx, const ReduceArgs& a, const FewArgs& f, bool vec, int ctas, cudaStream_t st) {
+        constexpr int VE = 16 / sizeof(T);
+        KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
+        auto* kernel = vec ? embed_few_kernel<T, TG, VE> : embed_few_kernel<T, TG, 1>;
+        return launch_dependent(kernel, dim3((unsigned)ctas), dim3(kFewThreads), sizeof(FewSmem), st, a, f);
+    }
+    static cudaError_t prepare() {
+        constexpr int VE = 16 / sizeof(T);
+        const cudaError_t e = cudaFuncSetAttribute(embed_few_kernel<T, TG, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewSmem));
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_few_kernel<T, TG, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewSmem));
+    }
+};
+// Launch<type of dOut, type of the gradient>::run(args)
+template <template <typename, typename> class Launch, typename... Args>
+cudaError_t by_type(int dtype, int grad_dtype, Args&&... args) {
+    const bool wide = grad_dtype == SAMA_F32;
+    if (dtype == SAMA_F32) return Launch<float, float>::run(args...);
+    if (dtype == SAMA_BF16) return wide ? Launch<__nv_bfloat16, float>::run(args...) : Launch<__nv_bfloat16, __nv_bfloat16>::run(args...);
+    return wide ? Launch<__half, float>::run(args...) : Launch<__half, __half>::run(args...);
+}
+
+// Once per context: shared-memory and cluster sizes, and the counters of embed_few.
+cudaError_t prepare_embed(sama_ctx* ctx) {
+    cudaError_t e;
+    if ((e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortSmem))) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1)) != cudaSuccess) return e;
+    if ((e = FewLaunch<float, float>::prepare()) != cudaSuccess) return e;
+    if ((e = FewLaunch<__nv_bfloat16, float>::prepare()) != cudaSuccess) return e;
+    if ((e = FewLaunch<__nv_bfloat16, __nv_bfloat16>::prepare()) != cudaSuccess) return e;
+    if ((e = FewLaunch<__half, float>::prepare()) != cudaSuccess) return e;
+    if ((e = FewLaunch<__half, __half>::prepare()) != cudaSuccess) return e;
+    if (!ctx->embed_counters && (e = cudaMalloc(&ctx->embed_counters, sizeof(int) * kFewCounters)) != cudaSuccess) return e;
+    if ((e = cudaMemset(ctx->embed_counters, 0, sizeof(int) * kFewCounters)) != cudaSuccess) return e;
+    if ((e = cudaDeviceSynchronize()) != cudaSuccess) return e;
+    ctx->embed_ready = 1;
+    return cudaSuccess;
 }
 
 }  // namespace
@@ -635,59 +847,19 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
                               const void* dout, float scale, int32_t skip_id, int grad_dtype, int accumulate, void* grad,
                               void* ws, cudaStream_t st) {
     const GradPlan g = make_plan(ctx, dtype, n, vocab, d, dout, grad_dtype, grad);
+    if (!ctx->embed_ready) {
+        const cudaError_t e = prepare_embed(ctx);
+        if (e != cudaSuccess) return e;
+    }
     uint8_t* w = static_cast<uint8_t*>(ws);
     auto take = [&](size_t bytes) {
         void* p = w;
         w += bytes;
         return p;
     };
-    SortArgs s;
-    s.ids = ids;
-    s.buf[0] = static_cast<int2*>(take(g.list));
-    s.buf[1] = static_cast<int2*>(take(g.list));
-    s.span = static_cast<int2*>(take(g.span));
-    s.arrived = static_cast<int*>(take(g.arrived));
-    s.fill.present = static_cast<uint32_t*>(take(g.present));
-    s.fill.progress = static_cast<int*>(take(g.progress));
-    s.fill.grad = accumulate ? nullptr : static_cast<uint8_t*>(grad);
-    s.fill.row_bytes = (int64_t)d * dtype_size(grad_dtype);
-    s.fill.share = g.share;
-    s.fill.vocab = (int32_t)vocab;
-    s.done = &ctx->scalars->embed_done;
-    // (replays of a captured call find the flag already set: then embed_reduce writes all the zeros)
-    s.epoch = ++ctx->embed_epoch;
-    s.n = (int)n;
-    s.counters = g.counters;
-    int bits = 1;   // of the largest key, which is `vocab` itself
-    while ((vocab >> bits) != 0) ++bits;
-    s.passes = (bits + kMaxBits - 1) / kMaxBits;
-    s.bits = (bits + s.passes - 1) / s.passes;
-    s.vocab = (int32_t)vocab;
-    s.skip_id = skip_id;
-    s.status = &ctx->scalars->status;
-    if (!ctx->embed_ready) {
-        cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortSmem));
-        if (e != cudaSuccess) return e;
-        e = cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-        ctx->embed_ready = 1;
-    }
-    {
-        const int ctas = accumulate ? kSortCtas : kSortCtas + kFillCtas;
-        KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
-        const cudaError_t e = launch_clustered(kSortCtas, embed_sort_kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortSmem), st, s);
-        if (e != cudaSuccess) return e;
-    }
     ReduceArgs a;
-    a.list = s.buf[(s.passes - 1) & 1];
-    a.span = s.span;
     a.dout = dout;
     a.grad = grad;
-    a.head = static_cast<float*>(take(g.parts));
-    a.tail = static_cast<float*>(take(g.parts));
-    a.fill = s.fill;
-    a.fill_blocks = accumulate ? 0 : ctx->sm_count;
-    a.arrived = s.arrived;
     a.n = (int)n;
     a.vocab = (int)vocab;
     a.d = d;
@@ -696,12 +868,67 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
     a.slabs = g.slabs;
     a.accumulate = accumulate;
     a.scale = scale;
-    const bool wide = grad_dtype == SAMA_F32;
-    if (dtype == SAMA_F32) return reduce_typed<float, float>(ctx, a, g.vec, st);
-    if (dtype == SAMA_BF16)
-        return wide ? reduce_typed<__nv_bfloat16, float>(ctx, a, g.vec, st)
-                    : reduce_typed<__nv_bfloat16, __nv_bfloat16>(ctx, a, g.vec, st);
-    return wide ? reduce_typed<__half, float>(ctx, a, g.vec, st) : reduce_typed<__half, __half>(ctx, a, g.vec, st);
+    int bits = 1;   // of the largest key, which is `vocab` itself
+    while ((vocab >> bits) != 0) ++bits;
+    const int most = g.few ? kFewBits : kMaxBits, passes = (bits + most - 1) / most, digit = (bits + passes - 1) / passes;
+    a.fill = {};
+    a.fill.grad = accumulate ? nullptr : static_cast<uint8_t*>(grad);
+    a.fill.row_bytes = (int64_t)d * dtype_size(grad_dtype);
+    a.fill.vocab = (int32_t)vocab;
+    if (g.few) {
+        a.list = a.span = nullptr;
+        a.arrived = ctx->embed_counters;
+        a.head = static_cast<float*>(take(g.parts));
+        a.tail = static_cast<float*>(take(g.parts));
+        a.fill_blocks = 0;
+        FewArgs f;
+        f.ids = ids;
+        f.passes = passes;
+        f.bits = digit;
+        f.skip_id = skip_id;
+        f.status = &ctx->scalars->status;
+        // enough CTAs for four pieces each, and for 32 KB of zeros
+        const int64_t units = (int64_t)g.pieces * g.slabs, by_fill = accumulate ? 0 : vocab * a.fill.row_bytes / 32768;
+        int64_t ctas = (units + 3) / 4 > by_fill ? (units + 3) / 4 : by_fill;
+        ctas = ctas < 1 ? 1 : ctas > ctx->sm_count ? ctx->sm_count : ctas;
+        // (so that the bits of a share fit, too)
+        if (vocab > ctas * (kFewShare / 2)) ctas = ctx->sm_count;
+        f.share = accumulate ? 0 : ((vocab + ctas - 1) / ctas + 31) & ~(int64_t)31;
+        return by_type<FewLaunch>(dtype, grad_dtype, ctx, a, f, g.vec, (int)ctas, st);
+    }
+    SortArgs s;
+    s.ids = ids;
+    s.buf[0] = static_cast<int2*>(take(g.list));
+    s.buf[1] = static_cast<int2*>(take(g.list));
+    s.span = static_cast<int2*>(take(g.span));
+    s.arrived = static_cast<int*>(take(g.arrived));
+    a.fill.present = static_cast<uint32_t*>(take(g.present));
+    a.fill.progress = static_cast<int*>(take(g.progress));
+    a.fill.share = g.share;
+    s.fill = a.fill;
+    s.done = &ctx->scalars->embed_done;
+    // (replays of a captured call find the flag already set: then embed_reduce writes all the zeros)
+    s.epoch = ++ctx->embed_epoch;
+    s.n = (int)n;
+    s.counters = g.counters;
+    s.passes = passes;
+    s.bits = digit;
+    s.vocab = (int32_t)vocab;
+    s.skip_id = skip_id;
+    s.status = &ctx->scalars->status;
+    {
+        const int ctas = accumulate ? kSortCtas : kSortCtas + kFillCtas;
+        KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
+        const cudaError_t e = launch_clustered(kSortCtas, embed_sort_kernel, dim3(ctas), dim3(kSortThreads), sizeof(SortSmem), st, s);
+        if (e != cudaSuccess) return e;
+    }
+    a.list = s.buf[(passes - 1) & 1];
+    a.span = s.span;
+    a.head = static_cast<float*>(take(g.parts));
+    a.tail = static_cast<float*>(take(g.parts));
+    a.arrived = s.arrived;
+    a.fill_blocks = accumulate ? 0 : ctx->sm_count;
+    return by_type<ReduceLaunch>(dtype, grad_dtype, ctx, a, g.vec, st);
 }
 
 }  // namespace sama

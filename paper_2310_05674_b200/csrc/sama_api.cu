@@ -461,6 +461,7 @@ int sama_destroy(sama_ctx* ctx) {
     cudaFree(ctx->mg_tc);
     cudaFree(ctx->stage);
     cudaFree(ctx->op_ws);
+    cudaFree(ctx->embed_counters);
     cudaFree(ctx->ffn_parts);
     cudaFree(ctx->ffn_arrived);
     cudaFree(ctx->pm_small);

@@ -129,7 +129,8 @@ struct sama_ctx {
     size_t stage_bytes;
     void* op_ws;                   // device: workspace of the text-model operators (allocated on first use, grows)
     size_t op_ws_bytes;
-    int embed_ready;               // the sort's shared-memory size is set on this device
+    int embed_ready;               // the embedding gradient's kernels are set up on this device
+    int* embed_counters;           // device: arrival counters, zero between launches
     int embed_epoch;               // number of the last such call
     int clip_ready;                // the small clipping kernel's cluster size is allowed on this device
     uint32_t ffn_ready;            // kernels of gated_ffn.cu whose shared-memory size is set on this device
