@@ -19,6 +19,8 @@
 //                  finish last add them up, in the order of the list.  The first blocks write the zeros still missing.
 // Up to 2048 tokens, where launches and round trips are what counts, one launch: every CTA sorts all tokens for itself in
 // shared memory, then takes its share of the pieces and of the rows to be zeroed.
+#include <type_traits>
+
 #include "num_types.h"
 #include "sama_internal.h"
 
@@ -30,8 +32,40 @@ namespace {
 
 constexpr int kEmbedThreads = 256;
 
-// VE consecutive columns per thread; `tpr` threads (a power of two) share a row, a thread takes ROWS of them at a time.
-template <typename T, int VE, int ROWS>
+// A thread's columns of a row: CH chunks of PW consecutive ones, `apart` columns from chunk to chunk, so that neighbouring
+// threads are on neighbouring chunks.  Rows of whole aligned 16-byte groups take one such group; others go in chunks of
+// what their alignment allows, four at a time.  Against one value at a time (us, lookup / gradient): 24,596 tokens, 638
+// rows of 2394 fp16 values in pairs 38 / 59 (53 / 163), of 2395 in single values 60 / 76 (53 / 163), of 2394 fp32 values
+// 57 / 77 (70 / 164); 131,072 tokens, rows of 33 bf16 values 12 / 59 (21 / 63).  Up to 32 columns the further chunks would
+// all lie beyond the row.
+template <int PW, int CH>
+struct Columns {
+    static constexpr int VE = PW * CH;
+    int first, apart, d;
+    __device__ __forceinline__ int at(int q) const { return first + q * apart; }
+    __device__ __forceinline__ bool on(int q) const { return at(q) < d; }
+};
+template <typename T, int PW>
+__device__ __forceinline__ void put_chunk(T* p, const float* v) {
+    if constexpr (PW == 2 && sizeof(T) == 4) __stcs(reinterpret_cast<float2*>(p), make_float2(v[0], v[1]));
+    else if constexpr (PW == 2) __stcs(reinterpret_cast<uint32_t*>(p), pack2<T>(v[0], v[1]));
+    else store_n<T, PW, true>(p, v);
+}
+template <typename T, int PW>
+__device__ __forceinline__ void get_chunk(const T* p, float* v) {
+    if constexpr (PW == 2 && sizeof(T) == 4) {
+        const float2 x = *reinterpret_cast<const float2*>(p);
+        v[0] = x.x; v[1] = x.y;
+    } else if constexpr (PW == 2) {
+        const float2 x = unpack2<T>(*reinterpret_cast<const uint32_t*>(p));
+        v[0] = x.x; v[1] = x.y;
+    } else {
+        load_n<T, PW, true>(p, v);
+    }
+}
+
+// `tpr` threads (a power of two) share a row, a thread takes ROWS of them at a time.
+template <typename T, int PW, int CH, int ROWS>
 __global__ void __launch_bounds__(kEmbedThreads)
 embed_kernel(int64_t n_tokens, int64_t vocab, int d, int tpr, const T* __restrict__ table,
              const int32_t* __restrict__ ids, float scale, T* __restrict__ out, int32_t* status) {
@@ -48,18 +82,24 @@ embed_kernel(int64_t n_tokens, int64_t vocab, int d, int tpr, const T* __restric
         good[r] = id[r] >= 0 && id[r] < vocab;
         if (!good[r] && tx == 0) atomicOr(status, (int)SAMA_DEV_BAD_INDEX);
     }
-    for (int c = tx * VE; c < d; c += tpr * VE) {
-        float v[ROWS][VE];
+    for (Columns<PW, CH> c{tx * PW, tpr * PW, d}; c.first < d; c.first += tpr * PW * CH) {
+        float v[ROWS][CH][PW];
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)  // (rows of frequent tokens are read again and again)
-            load_n<T, VE, true>(table + (good[r] ? (int64_t)id[r] : 0) * d + c, v[r]);
+#pragma unroll
+            for (int q = 0; q < CH; ++q)
+                if (CH == 1 || c.on(q)) get_chunk<T, PW>(table + (good[r] ? (int64_t)id[r] : 0) * d + c.at(q), v[r][q]);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const int64_t t = t0 + (int64_t)r * rows;
             if (t >= n_tokens) continue;
 #pragma unroll
-            for (int i = 0; i < VE; ++i) v[r][i] = good[r] ? v[r][i] * scale : 0.f;
-            store_n<T, VE, true>(out + t * d + c, v[r]);  // (not to push the table out of L2)
+            for (int q = 0; q < CH; ++q) {
+                if (CH > 1 && !c.on(q)) continue;
+#pragma unroll
+                for (int i = 0; i < PW; ++i) v[r][q][i] = good[r] ? v[r][q][i] * scale : 0.f;
+                put_chunk<T, PW>(out + t * d + c.at(q), v[r][q]);  // (not to push the table out of L2)
+            }
         }
     }
 }
@@ -365,68 +405,101 @@ struct ReduceArgs {
     float scale;
 };
 
-template <typename TG, int VE>
-__device__ __forceinline__ void put_row(const ReduceArgs& a, int row, int c, const float* acc) {
-    TG* g = static_cast<TG*>(a.grad) + (int64_t)row * a.d + c;
-    float v[VE];
+template <typename TG, int PW, int CH>
+__device__ __forceinline__ void put_row(const ReduceArgs& a, int row, const Columns<PW, CH>& c, const float* acc) {
 #pragma unroll
-    for (int i = 0; i < VE; ++i) v[i] = acc[i] * a.scale;
-    if (a.accumulate) {
-        float old[VE];
-        load_n<TG, VE>(g, old);
+    for (int q = 0; q < CH; ++q) {
+        if (!c.on(q)) continue;
+        TG* g = static_cast<TG*>(a.grad) + (int64_t)row * a.d + c.at(q);
+        float v[PW];
 #pragma unroll
-        for (int i = 0; i < VE; ++i) v[i] += old[i];
+        for (int i = 0; i < PW; ++i) v[i] = acc[q * PW + i] * a.scale;
+        if (a.accumulate) {
+            float old[PW];
+            if constexpr (PW <= 2) get_chunk<TG, PW>(g, old); else load_n<TG, PW>(g, old);
+#pragma unroll
+            for (int i = 0; i < PW; ++i) v[i] += old[i];
+        }
+        if constexpr (PW <= 2) put_chunk<TG, PW>(g, v); else store_n<TG, PW>(g, v);
     }
-    store_n<TG, VE>(g, v);
+}
+template <int PW, int CH>
+__device__ __forceinline__ void put_part(float* part, const Columns<PW, CH>& c, const float* acc) {
+#pragma unroll
+    for (int q = 0; q < CH; ++q) {
+        if (!c.on(q)) continue;
+        if constexpr (PW == 2) *reinterpret_cast<float2*>(part + c.at(q)) = make_float2(acc[2 * q], acc[2 * q + 1]);
+        else store_n<float, PW>(part + c.at(q), acc + q * PW);
+    }
 }
 
-// The thread's VE values as they lie in memory: 16 bytes, or one value.
-template <typename T, int VE> struct Raw {
-    uint4 r;
-    __device__ __forceinline__ void load(const T* p) { r = __ldcs(reinterpret_cast<const uint4*>(p)); }
-    __device__ __forceinline__ void add_to(float* acc) const {
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+// A thread's values of one row as they lie in memory.
+template <typename T, int PW, int CH> struct Raw {
+    using Chunk = std::conditional_t<PW == 1, T, std::conditional_t<PW == 2, uint32_t, uint4>>;
+    static_assert(sizeof(Chunk) == PW * sizeof(T), "a chunk is one access");
+    Chunk r[CH] = {};
+    __device__ __forceinline__ void load(const T* row, const Columns<PW, CH>& c) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (sizeof(T) == 4) {
-                acc[j] += __uint_as_float(w[j]);
+        for (int q = 0; q < CH; ++q)
+            if (c.on(q)) r[q] = __ldcs(reinterpret_cast<const Chunk*>(row + c.at(q)));
+    }
+    __device__ __forceinline__ void add_to(float* acc) const {
+#pragma unroll
+        for (int q = 0; q < CH; ++q) {
+            if constexpr (PW == 1) {
+                acc[q] += to_float(r[q]);
+            } else if constexpr (PW == 2) {
+                const float2 f = unpack2<T>(r[q]);
+                acc[2 * q] += f.x;
+                acc[2 * q + 1] += f.y;
             } else {
-                const float2 f = unpack2<T>(w[j]);
-                acc[2 * j] += f.x;
-                acc[2 * j + 1] += f.y;
+                const uint32_t w[4] = {r[q].x, r[q].y, r[q].z, r[q].w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (sizeof(T) == 4) {
+                        acc[j] += __uint_as_float(w[j]);
+                    } else {
+                        const float2 f = unpack2<T>(w[j]);
+                        acc[2 * j] += f.x;
+                        acc[2 * j + 1] += f.y;
+                    }
+                }
             }
         }
     }
 };
-template <typename T> struct Raw<T, 1> {
-    T r;
-    __device__ __forceinline__ void load(const T* p) { r = *p; }
-    __device__ __forceinline__ void add_to(float* acc) const { acc[0] += to_float(r); }
-};
 
-// VE fp32 values that another warp of this launch has stored.
-template <int VE>
-__device__ __forceinline__ void load_part(const float* p, float* v) {
-    if constexpr (VE == 1) {
-        v[0] = __ldcg(p);
-    } else {
+// A thread's fp32 values that another warp of this launch has stored.
+template <int PW, int CH>
+__device__ __forceinline__ void load_part(const float* part, const Columns<PW, CH>& c, float* v) {
 #pragma unroll
-        for (int i = 0; i < VE / 4; ++i) {
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(p) + i);
-            v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+    for (int q = 0; q < CH; ++q) {
+        const float* p = part + (c.on(q) ? c.at(q) : 0);
+        if constexpr (PW == 1) {
+            v[q] = __ldcg(p);
+        } else if constexpr (PW == 2) {
+            const float2 x = __ldcg(reinterpret_cast<const float2*>(p));
+            v[2 * q] = x.x; v[2 * q + 1] = x.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < PW / 4; ++i) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(p) + i);
+                v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+            }
         }
     }
 }
 
-// Adds the parts at base + (first + step j) d, j = 0 .. count - 1, to sum, in this order.
-template <int VE>
-__device__ __forceinline__ void add_parts(const float* base, int64_t first, int64_t step, int count, float* sum) {
-    constexpr int U = VE == 8 ? 4 : 8;  // (more would set the whole kernel's register count)
+// Adds the parts at base + first + step j, j = 0 .. count - 1, to sum, in this order.
+template <int PW, int CH>
+__device__ __forceinline__ void add_parts(const float* base, int64_t first, int64_t step, int count,
+                                          const Columns<PW, CH>& c, float* sum) {
+    constexpr int VE = PW * CH, U = VE == 8 ? 4 : 8;  // (more would set the whole kernel's register count)
     for (int j = 0; j < count; j += U) {
         float v[U][VE];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (j + u < count) load_part<VE>(base + first + (j + u) * step, v[u]);
+            if (j + u < count) load_part(base + first + (j + u) * step, c, v[u]);
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (j + u < count)
@@ -473,10 +546,8 @@ struct SharedList {
 // This warp has stored its part, in piece k, of a run over pieces k0 .. k1.  The parts are joined in groups of kJoin
 // pieces, then the groups: the last to store a part adds up its group, the last to store a group's sum (in the place of
 // its first part) adds up the groups.
-template <typename TG, int VE, typename List>
-__device__ __forceinline__ void join_run(const ReduceArgs& a, const List& list, int key, int k, int slab, int lane) {
-    const int c = (slab * 32 + lane) * VE;
-    const bool on = c < a.d;
+template <typename TG, int PW, int CH, typename List>
+__device__ __forceinline__ void join_run(const ReduceArgs& a, const List& list, const Columns<PW, CH>& c, int key, int k, int slab, int lane) {
     const int2 run = list.run(key);
     const int k0 = run.x / a.piece, k1 = (run.y - 1) / a.piece;
     const int g = k / kJoin, g0 = k0 / kJoin, g1 = k1 / kJoin;
@@ -485,28 +556,28 @@ __device__ __forceinline__ void join_run(const ReduceArgs& a, const List& list, 
     // counters: of the group a run begins in, by k0 (at most one such run per piece); of a later group, by the group
     int* in_group = g == g0 ? a.arrived + (int64_t)k0 * a.slabs + slab : a.arrived + 2 * parts + (int64_t)g * a.slabs + slab;
     if (!last_to_arrive(in_group, last - first + 1, lane)) return;
-    float sum[VE];
-    float* slot = (g == g0 ? a.tail : a.head) + (int64_t)first * a.d + (on ? c : 0);
-    const float* heads = a.head + (on ? c : 0);
-    load_part<VE>(slot, sum);
-    add_parts<VE>(heads, (int64_t)(first + 1) * a.d, a.d, last - first, sum);
+    float sum[PW * CH];
+    float* slot = (g == g0 ? a.tail : a.head) + (int64_t)first * a.d;
+    load_part(slot, c, sum);
+    add_parts(a.head, (int64_t)(first + 1) * a.d, a.d, last - first, c, sum);
     if (g0 != g1) {
         __syncwarp();
-        if (on) store_n<float, VE>(slot, sum);
+        put_part(slot, c, sum);
         if (!last_to_arrive(a.arrived + parts + (int64_t)k0 * a.slabs + slab, g1 - g0 + 1, lane)) return;
-        load_part<VE>(a.tail + (int64_t)k0 * a.d + (on ? c : 0), sum);
-        add_parts<VE>(heads, (int64_t)(g0 + 1) * kJoin * a.d, (int64_t)kJoin * a.d, g1 - g0, sum);
+        load_part(a.tail + (int64_t)k0 * a.d, c, sum);
+        add_parts(a.head, (int64_t)(g0 + 1) * kJoin * a.d, (int64_t)kJoin * a.d, g1 - g0, c, sum);
     }
-    if (on) put_row<TG, VE>(a, key, c, sum);
+    put_row<TG>(a, key, c, sum);
 }
 
 // One warp: piece k of the list, columns [32 VE slab, 32 VE (slab + 1)), U rows in flight per thread.
-template <typename T, typename TG, int VE, int U, typename List>
+template <typename T, typename TG, int PW, int CH, int U, typename List>
 __device__ __forceinline__ void reduce_piece(const ReduceArgs& a, const List& list, int k, int slab, int lane) {
     const int i0 = k * a.piece, count = min(a.n - i0, a.piece);
-    const int c = (slab * 32 + lane) * VE;
-    const bool on = c < a.d;   // (the other lanes of the last slab go along for the warp's sake)
-    const T* dout = static_cast<const T*>(a.dout) + (on ? c : 0);
+    constexpr int VE = PW * CH;
+    // (lanes beyond the last column go along for the warp's sake)
+    const Columns<PW, CH> c{slab * 32 * VE + lane * PW, 32 * PW, a.d};
+    const T* dout = static_cast<const T*>(a.dout);
     // the piece's entries, two per lane
     const int2 none = make_int2(a.vocab, 0);
     const int2 low = lane < count ? list.at(i0 + lane) : none, high = lane + 32 < count ? list.at(i0 + lane + 32) : none;
@@ -519,15 +590,15 @@ __device__ __forceinline__ void reduce_piece(const ReduceArgs& a, const List& li
 #pragma unroll
     for (int j = 0; j < VE; ++j) acc[j] = 0.f;
 
-    Raw<T, VE> v[U];
+    Raw<T, PW, CH> v[U];
     auto entry = [&](int i) {
         const int2 e = i < 32 ? low : high;
         return make_int2(__shfl_sync(0xffffffffu, e.x, i & 31), __shfl_sync(0xffffffffu, e.y, i & 31));
     };
-    auto fetch = [&](Raw<T, VE>& r, int i) {
+    auto fetch = [&](Raw<T, PW, CH>& r, int i) {
         if (i >= count) return;
         const int2 e = entry(i);
-        if (e.x < a.vocab) r.load(dout + (int64_t)e.y * a.d);
+        if (e.x < a.vocab) r.load(dout + (int64_t)e.y * a.d, c);
     };
 #pragma unroll
     for (int u = 0; u < U; ++u) fetch(v[u], u);
@@ -537,10 +608,8 @@ __device__ __forceinline__ void reduce_piece(const ReduceArgs& a, const List& li
             if (b + u >= count) break;
             const int id = entry(b + u).x;
             if (id != key) {
-                if (on) {
-                    if (in_head) store_n<float, VE>(a.head + (int64_t)k * a.d + c, acc);
-                    else put_row<TG, VE>(a, key, c, acc);
-                }
+                if (in_head) put_part(a.head + (int64_t)k * a.d, c, acc);
+                else put_row<TG>(a, key, c, acc);
                 in_head = false;
                 key = id;
                 if (key >= a.vocab) break;
@@ -552,20 +621,20 @@ __device__ __forceinline__ void reduce_piece(const ReduceArgs& a, const List& li
         }
     }
     const bool open_tail = key < a.vocab && after_key == key;
-    if (on && key < a.vocab) {
-        if (in_head) store_n<float, VE>(a.head + (int64_t)k * a.d + c, acc);
-        else if (open_tail) store_n<float, VE>(a.tail + (int64_t)k * a.d + c, acc);
-        else put_row<TG, VE>(a, key, c, acc);
+    if (key < a.vocab) {
+        if (in_head) put_part(a.head + (int64_t)k * a.d, c, acc);
+        else if (open_tail) put_part(a.tail + (int64_t)k * a.d, c, acc);
+        else put_row<TG>(a, key, c, acc);
     }
     // the run that came in, and the one that goes on where that is another
 #pragma unroll 1
     for (int j = 0; j < 2; ++j) {
         const int run = j == 0 ? first_key : key;
-        if (j == 0 ? open_head : (open_tail && !in_head)) join_run<TG, VE>(a, list, run, k, slab, lane);
+        if (j == 0 ? open_head : (open_tail && !in_head)) join_run<TG>(a, list, c, run, k, slab, lane);
     }
 }
 
-template <typename T, typename TG, int VE>
+template <typename T, typename TG, int PW, int CH>
 __global__ void __launch_bounds__(kEmbedThreads, 3)
 embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
     pdl_trigger();
@@ -583,7 +652,7 @@ embed_reduce_kernel(const __grid_constant__ ReduceArgs a) {
     const int64_t unit = (int64_t)(blockIdx.x - a.fill_blocks) * (kEmbedThreads / 32) + (threadIdx.x >> 5);
     const int k = (int)(unit / a.slabs), slab = (int)(unit - (int64_t)k * a.slabs);
     // (single values: twice the rows, for half as many bytes in flight or less)
-    if (k < a.pieces) reduce_piece<T, TG, VE, VE == 1 ? 16 : 8>(a, GlobalList{a.list, a.span}, k, slab, lane);
+    if (k < a.pieces) reduce_piece<T, TG, PW, CH, PW * CH == 1 ? 16 : 8>(a, GlobalList{a.list, a.span}, k, slab, lane);
 }
 
 // ------------------------------------------------------------------ few tokens
@@ -608,7 +677,7 @@ struct FewArgs {
     int32_t* status;
 };
 
-template <typename T, typename TG, int VE>
+template <typename T, typename TG, int PW, int CH>
 __global__ void __launch_bounds__(kFewThreads, 1)
 embed_few_kernel(const __grid_constant__ ReduceArgs a, const __grid_constant__ FewArgs f) {
     extern __shared__ uint8_t few_raw[];
@@ -699,7 +768,7 @@ embed_few_kernel(const __grid_constant__ ReduceArgs a, const __grid_constant__ F
     const int64_t units = (int64_t)a.pieces * a.slabs;
     for (int64_t unit = (int64_t)warp * gridDim.x + blockIdx.x; unit < units; unit += (int64_t)kFewWarps * gridDim.x) {
         const int k = (int)(unit / a.slabs), slab = (int)(unit - (int64_t)k * a.slabs);
-        reduce_piece<T, TG, VE, 4>(a, list, k, slab, lane);
+        reduce_piece<T, TG, PW, CH, 4>(a, list, k, slab, lane);
     }
     // zeros to the rows without a token, by the warps that have no piece (any more)
     for (;;) {
@@ -726,19 +795,40 @@ int threads_per_row(int d, int ve) {
     return best;
 }
 
+// How rows of d values are taken apart: the chunks of a thread (see Columns).
+enum Access { GROUPS, PAIRS, SINGLES, SINGLE };
+Access access_of(int d, int dtype, uintptr_t addresses, bool wide_output) {
+    const int es = (int)dtype_size(dtype);
+    if (d % (16 / es) == 0 && (addresses & 15u) == 0) return GROUPS;
+    if (d <= 32) return SINGLE;
+    return es == 2 && d % 2 == 0 && (addresses & (wide_output ? 7u : 3u)) == 0 ? PAIRS : SINGLES;
+}
+inline int columns_of(Access a, int dtype) { return a == GROUPS ? 16 / (int)dtype_size(dtype) : a == PAIRS ? 8 : a == SINGLES ? 4 : 1; }
+// fn<values per chunk, chunks>
+template <typename T, typename F>
+auto with_access(Access a, F&& fn) {
+    using std::integral_constant;
+    constexpr int GROUP = 16 / sizeof(T), PAIR = sizeof(T) == 2 ? 2 : 1;   // (fp32 has no pairs: its single values are as wide)
+    return a == GROUPS    ? fn(integral_constant<int, GROUP>(), integral_constant<int, 1>())
+           : a == PAIRS   ? fn(integral_constant<int, PAIR>(), integral_constant<int, 4>())
+           : a == SINGLES ? fn(integral_constant<int, 1>(), integral_constant<int, 4>())
+                          : fn(integral_constant<int, 1>(), integral_constant<int, 1>());
+}
+
 template <typename T>
-cudaError_t embed_typed(sama_ctx* ctx, int64_t n, int64_t vocab, int d, const void* table, const int32_t* ids, float scale,
-                        void* out, cudaStream_t st) {
-    constexpr int VE = 16 / sizeof(T);
-    const bool vec = d % VE == 0 && ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
-    const int tpr = threads_per_row(d, vec ? VE : 1), rows = kEmbedThreads / tpr;
+cudaError_t embed_typed(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* table, const int32_t* ids,
+                        float scale, void* out, cudaStream_t st) {
+    const Access access = access_of(d, dtype, reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(out), false);
+    const int tpr = threads_per_row(d, columns_of(access, dtype)), rows = kEmbedThreads / tpr;
     // four rows per thread once that still leaves every SM its full number of threads
     const bool deep = n * tpr >= (int64_t)ctx->sm_count * 2048 * 4;
     const int64_t per_block = (int64_t)rows * (deep ? 4 : 1);
     KernelScope scope(ctx, SAMA_K_EMBED, -1, st);
-    auto* kernel = vec ? (deep ? embed_kernel<T, VE, 4> : embed_kernel<T, VE, 1>) : (deep ? embed_kernel<T, 1, 4> : embed_kernel<T, 1, 1>);
-    return launch_dependent(kernel, dim3((unsigned)((n + per_block - 1) / per_block)), dim3(kEmbedThreads), 0, st, n, vocab,
-                            d, tpr, static_cast<const T*>(table), ids, scale, static_cast<T*>(out), &ctx->scalars->status);
+    return with_access<T>(access, [&](auto pw, auto ch) {
+        auto* kernel = deep ? embed_kernel<T, decltype(pw)::value, decltype(ch)::value, 4> : embed_kernel<T, decltype(pw)::value, decltype(ch)::value, 1>;
+        return launch_dependent(kernel, dim3((unsigned)((n + per_block - 1) / per_block)), dim3(kEmbedThreads), 0, st, n, vocab,
+                                d, tpr, static_cast<const T*>(table), ids, scale, static_cast<T*>(out), &ctx->scalars->status);
+    });
 }
 
 // Entries per piece: as many as still give every SM 24 warps, 8 to 64.
@@ -751,8 +841,9 @@ int piece_of(const sama_ctx* ctx, int64_t n, int slabs) {
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct GradPlan {
-    bool vec, few;
-    int ve, slabs, piece, pieces, counters;
+    bool few;
+    Access access;
+    int slabs, piece, pieces, counters;
     int64_t share;
     size_t list, span, arrived, present, progress, parts;  // bytes
     size_t total() const { return few ? 2 * parts : 2 * list + span + arrived + present + progress + 2 * parts; }
@@ -760,10 +851,9 @@ struct GradPlan {
 GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout, int grad_dtype,
                    const void* grad) {
     GradPlan g;
-    const int ve = 16 / (int)dtype_size(dtype);
-    g.vec = d % ve == 0 && ((reinterpret_cast<uintptr_t>(dout) | reinterpret_cast<uintptr_t>(grad)) & 15u) == 0;
-    g.ve = g.vec ? ve : 1;
-    g.slabs = (d + 32 * g.ve - 1) / (32 * g.ve);
+    g.access = access_of(d, dtype, reinterpret_cast<uintptr_t>(dout) | reinterpret_cast<uintptr_t>(grad), grad_dtype == SAMA_F32);
+    const int slab = 32 * columns_of(g.access, dtype);
+    g.slabs = (d + slab - 1) / slab;
     g.piece = piece_of(ctx, n, g.slabs);
     g.pieces = (int)((n + g.piece - 1) / g.piece);
     g.list = up256(sizeof(int2) * (size_t)n);
@@ -780,26 +870,33 @@ GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int
 
 template <typename T, typename TG>
 struct ReduceLaunch {
-    static cudaError_t run(sama_ctx* ctx, const ReduceArgs& a, bool vec, cudaStream_t st) {
-        constexpr int VE = 16 / sizeof(T);
+    static cudaError_t run(sama_ctx* ctx, const ReduceArgs& a, Access access, cudaStream_t st) {
         KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
-        auto* kernel = vec ? embed_reduce_kernel<T, TG, VE> : embed_reduce_kernel<T, TG, 1>;
         const int64_t units = (int64_t)a.pieces * a.slabs, per = kEmbedThreads / 32;
-        return launch_dependent(kernel, dim3((unsigned)(a.fill_blocks + (units + per - 1) / per)), dim3(kEmbedThreads), 0, st, a);
+        return with_access<T>(access, [&](auto pw, auto ch) {
+            return launch_dependent(embed_reduce_kernel<T, TG, decltype(pw)::value, decltype(ch)::value>,
+                                    dim3((unsigned)(a.fill_blocks + (units + per - 1) / per)), dim3(kEmbedThreads), 0, st, a);
+        });
     }
 };
 template <typename T, typename TG>
 struct FewLaunch {
-    static cudaError_t run(sama_ctx* ctx, const ReduceArgs& a, const FewArgs& f, bool vec, int ctas, cudaStream_t st) {
-        constexpr int VE = 16 / sizeof(T);
+    static cudaError_t run(sama_ctx* ctx, const ReduceArgs& a, const FewArgs& f, Access access, int ctas, cudaStream_t st) {
         KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
-        auto* kernel = vec ? embed_few_kernel<T, TG, VE> : embed_few_kernel<T, TG, 1>;
-        return launch_dependent(kernel, dim3((unsigned)ctas), dim3(kFewThreads), sizeof(FewSmem), st, a, f);
+        return with_access<T>(access, [&](auto pw, auto ch) {
+            return launch_dependent(embed_few_kernel<T, TG, decltype(pw)::value, decltype(ch)::value>, dim3((unsigned)ctas),
+                                    dim3(kFewThreads), sizeof(FewSmem), st, a, f);
+        });
     }
     static cudaError_t prepare() {
-        constexpr int VE = 16 / sizeof(T);
-        const cudaError_t e = cudaFuncSetAttribute(embed_few_kernel<T, TG, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewSmem));
-        return e != cudaSuccess ? e : cudaFuncSetAttribute(embed_few_kernel<T, TG, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewSmem));
+        cudaError_t e = cudaSuccess;
+        for (Access access : {GROUPS, PAIRS, SINGLES, SINGLE})
+            if (e == cudaSuccess)
+                e = with_access<T>(access, [&](auto pw, auto ch) {
+                    return cudaFuncSetAttribute(embed_few_kernel<T, TG, decltype(pw)::value, decltype(ch)::value>,
+                                                cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewSmem));
+                });
+        return e;
     }
 };
 // Launch<type of dOut, type of the gradient>::run(args)
@@ -832,9 +929,9 @@ cudaError_t prepare_embed(sama_ctx* ctx) {
 
 cudaError_t launch_embed(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* table, const int32_t* ids,
                          float scale, void* out, cudaStream_t st) {
-    if (dtype == SAMA_F32) return embed_typed<float>(ctx, n, vocab, d, table, ids, scale, out, st);
-    if (dtype == SAMA_BF16) return embed_typed<__nv_bfloat16>(ctx, n, vocab, d, table, ids, scale, out, st);
-    return embed_typed<__half>(ctx, n, vocab, d, table, ids, scale, out, st);
+    if (dtype == SAMA_F32) return embed_typed<float>(ctx, dtype, n, vocab, d, table, ids, scale, out, st);
+    if (dtype == SAMA_BF16) return embed_typed<__nv_bfloat16>(ctx, dtype, n, vocab, d, table, ids, scale, out, st);
+    return embed_typed<__half>(ctx, dtype, n, vocab, d, table, ids, scale, out, st);
 }
 
 // Workspace: two lists of (id, position), the rows' runs, arrival counters, and two parts per piece.
@@ -894,7 +991,7 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
         // (so that the bits of a share fit, too)
         if (vocab > ctas * (kFewShare / 2)) ctas = ctx->sm_count;
         f.share = accumulate ? 0 : ((vocab + ctas - 1) / ctas + 31) & ~(int64_t)31;
-        return by_type<FewLaunch>(dtype, grad_dtype, ctx, a, f, g.vec, (int)ctas, st);
+        return by_type<FewLaunch>(dtype, grad_dtype, ctx, a, f, g.access, (int)ctas, st);
     }
     SortArgs s;
     s.ids = ids;
@@ -928,7 +1025,7 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
     a.tail = static_cast<float*>(take(g.parts));
     a.arrived = s.arrived;
     a.fill_blocks = accumulate ? 0 : ctx->sm_count;
-    return by_type<ReduceLaunch>(dtype, grad_dtype, ctx, a, g.vec, st);
+    return by_type<ReduceLaunch>(dtype, grad_dtype, ctx, a, g.access, st);
 }
 
 }  // namespace sama
