@@ -40,7 +40,6 @@ constexpr int kEmbedThreads = 256;
 // all lie beyond the row.
 template <int PW, int CH>
 struct Columns {
-    static constexpr int VE = PW * CH;
     int first, apart, d;
     __device__ __forceinline__ int at(int q) const { return first + q * apart; }
     __device__ __forceinline__ bool on(int q) const { return at(q) < d; }
