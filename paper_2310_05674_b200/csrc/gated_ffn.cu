@@ -67,6 +67,7 @@ __host__ __device__ constexpr int smem_of(int mode, int unit) {
 
 struct Problem {
     CUtensorMap a[2], b[2];     // [1]: the second part of the contraction, or (gate-up) the second right operand
+    CUtensorMap o[3];           // outputs that can be written in aligned 16-byte groups
     int M, N;                   // rows and columns of the output (gate-up: features)
     int num_kb, kb_first;       // k-blocks, and how many of them the first maps cover
     int tiles_m, tiles_n, item0;
@@ -125,6 +126,19 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
     asm volatile(
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
         ::"r"(dst), "l"(map), "r"(leader_bar), "r"(x), "r"(y) : "memory");
+}
+
+// A block of rows from shared memory; what lies beyond the matrix is not written.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];\n\tcp.async.bulk.commit_group;"
+        ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+}
+// This thread's stores have read shared memory, or (ALL) have been made.
+template <bool ALL>
+__device__ __forceinline__ void tma_store_wait() {
+    if (ALL) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    else asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
 }
 
 // 16 accumulator columns of this warp's 32 rows, from and to tensor memory.
@@ -216,27 +230,23 @@ __device__ __forceinline__ void with_act(int act, F&& fn) {
 // ---------------------------------------------------------------- stores
 
 // Writes a block of 32 rows x CU columns that a warp holds as packed pairs, one row per lane, in whole row segments:
-// through `stg` with 16-byte chunks permuted by row, so that neither side has bank conflicts.
+// through `stg` with 16-byte chunks permuted by row, so that neither side has bank conflicts.  Rows of aligned 16-byte
+// groups are fetched from there by the copy engine (the permutation is its 128- or 64-byte swizzle).
 template <typename T, int CU>
-__device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, T* dst, int64_t ld, int row0, int rows,
-                                           int col0, int cols, bool vec, int lane) {
+__device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, const CUtensorMap* map, T* dst, int64_t ld,
+                                           int row0, int rows, int col0, int cols, bool vec, int lane) {
     constexpr int LPR = CU / 8;  // 16-byte chunks of a row
     auto at = [](int r, int c) { return r * LPR + (c ^ (LPR == 8 ? (r & 7) : ((r >> 1) & 3))); };
     static_assert(CU == 64 || CU == 32, "rows of 128 or 64 bytes");
+    if (lane == 0) tma_store_wait<false>();
     __syncwarp();
 #pragma unroll
     for (int c = 0; c < LPR; ++c)
         stg[at(lane, c)] = make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+    if (vec) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (vec) {
-        const int c = lane % LPR;
-        if (col0 + 8 * c < cols) {   // (a vector destination has whole groups of eight columns)
-#pragma unroll
-            for (int i = 0; i < LPR; ++i) {
-                const int r = lane / LPR + i * (32 / LPR);
-                if (r < rows) *reinterpret_cast<uint4*>(dst + (int64_t)(row0 + r) * ld + col0 + 8 * c) = stg[at(r, c)];
-            }
-        }
+        if (lane == 0 && rows > 0 && col0 < cols) tma_store_2d(map, smem_u32(stg), col0, row0);
     } else {
         // rows that start anywhere: neighbouring lanes take neighbouring elements
         // Four values per lane, stored as two words that start on a 4-byte boundary: in a row that starts between two
@@ -300,6 +310,12 @@ __device__ __forceinline__ uint4 load8(const T* p, int col, int cols, bool vec) 
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
+// x / y for x >= 0, y > 0 and a quotient below 2^20: that of floats is off by one at most.  (Every role makes two per tile.)
+__device__ __forceinline__ int quotient(int x, int y) {
+    const int q = (int)((float)x * fast_rcp((float)y)), r = x - q * y;
+    return r < 0 ? q - 1 : r >= y ? q + 1 : q;
+}
+
 // ---------------------------------------------------------------- the kernel
 
 template <typename T, int MODE, int UNIT, bool A_MN, bool B_MN, int G>
@@ -338,7 +354,7 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
         int tile = item;
         w.split_tile = -1;
         if (over >= 0) {
-            w.split_tile = over / P.split;
+            w.split_tile = quotient(over, P.split);
             w.part = over - w.split_tile * P.split;
             tile = P.whole + w.split_tile;
         }
@@ -350,13 +366,13 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
         w.kb0 = 0;
         w.kb1 = q.num_kb;
         if (over >= 0) {
-            w.kb0 = (int)((int64_t)q.num_kb * w.part / P.split);
-            w.kb1 = (int)((int64_t)q.num_kb * (w.part + 1) / P.split);
+            w.kb0 = quotient(q.num_kb * w.part, P.split);
+            w.kb1 = quotient(q.num_kb * (w.part + 1), P.split);
         }
-        const int t = tile - q.item0, per_group = P.group_m * q.tiles_n, group = t / per_group, rem = t - group * per_group;
+        const int t = tile - q.item0, per_group = P.group_m * q.tiles_n, group = quotient(t, per_group), rem = t - group * per_group;
         const int first = group * P.group_m, size = min(P.group_m, q.tiles_m - first);
-        w.tm = first + rem % size;
-        w.tn = rem / size;
+        w.tn = quotient(rem, size);
+        w.tm = first + rem - w.tn * size;
         return q;
     };
 
@@ -642,10 +658,10 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                 release();
                 const int col0 = tn * TN + share * CU;
                 if (q.out[0]) {
-                    store_rows<T, CU>(stg, pg, static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, col0, q.cols[0], q.vec_out & 1, lane);
-                    store_rows<T, CU>(stg, pu, static_cast<T*>(q.out[1]), q.ldo[1], row0, rows, col0, q.cols[1], q.vec_out & 2, lane);
+                    store_rows<T, CU>(stg, pg, &q.o[0], static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, col0, q.cols[0], q.vec_out & 1, lane);
+                    store_rows<T, CU>(stg, pu, &q.o[1], static_cast<T*>(q.out[1]), q.ldo[1], row0, rows, col0, q.cols[1], q.vec_out & 2, lane);
                 }
-                store_rows<T, CU>(stg, ph, static_cast<T*>(q.out[2]), q.ldo[2], row0, rows, col0, q.cols[2], q.vec_out & 4, lane);
+                store_rows<T, CU>(stg, ph, &q.o[2], static_cast<T*>(q.out[2]), q.ldo[2], row0, rows, col0, q.cols[2], q.vec_out & 4, lane);
             } else if constexpr (MODE == PLAIN) {
 #pragma unroll 1
                 for (int c = 0; c < CPW; c += 64) {
@@ -658,7 +674,7 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                         for (int j = 0; j < 16; ++j) packed[16 * i + j] = pack2<T>(v[2 * j], v[2 * j + 1]);
                     }
                     if (c + 64 == CPW) release();
-                    store_rows<T, 64>(stg, packed, static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, tn * TN + share * CPW + c,
+                    store_rows<T, 64>(stg, packed, &q.o[0], static_cast<T*>(q.out[0]), q.ldo[0], row0, rows, tn * TN + share * CPW + c,
                                       q.cols[0], q.vec_out & 1, lane);
                 }
             } else {
@@ -713,6 +729,7 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
             }
         }
     }
+    tma_store_wait<true>();   // (of threads that have made any)
     tc_fence_before();
     __syncthreads();
     if (PAIR) cluster_sync_relaxed();  // the leader's products use the other CTA's shared and tensor memory
@@ -903,14 +920,15 @@ struct Matrix {
 };
 
 // Box of box_cols x box_rows; columns and rows beyond the matrix read as zero.
-bool make_map2(CUtensorMap* map, const Matrix& m, int dtype, int box_cols, int box_rows) {
+bool make_map2(CUtensorMap* map, const Matrix& m, int dtype, int box_cols, int box_rows) {   // rows of 128 or 64 bytes
     EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
     cuuint64_t strides[1] = {(cuuint64_t)m.ld * 2};
     cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, estr[2] = {1, 1};
     return fn(map, dtype == SAMA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-              const_cast<void*>(m.p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              const_cast<void*>(m.p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // The tile of 128 rows (or columns, MN-major) that one CTA stages.
@@ -1037,11 +1055,14 @@ TilePlan plan_tiles(const sama_ctx* ctx, const Problem* p, int n, Mode mode, boo
     return best;
 }
 
-void set_output(Problem& q, int i, void* p, int ld, int cols) {
+// block: columns that a warp stores at a time, 0 where it does so without the copy engine.
+bool set_output(Problem& q, int i, void* p, int ld, int cols, int dtype, int block) {
     q.out[i] = p;
     q.ldo[i] = ld;
     q.cols[i] = cols;
-    if (vec_rows(p, ld) && cols % 8 == 0) q.vec_out |= 1 << i;
+    if (!p || !vec_rows(p, ld) || cols % 8 != 0) return true;
+    q.vec_out |= 1 << i;
+    return block == 0 || make_map2(&q.o[i], {p, q.M, cols, ld}, dtype, block, 32);
 }
 
 // What a call works on: operands as TMA can read them, copied to the workspace where they are not.
@@ -1143,9 +1164,9 @@ struct Block {
             const TilePlan plan = plan_tiles(ctx, &q, 1, GATE_UP);
             check(operand_map(&q.a[0], mx, f.dtype, false) && operand_map(&q.b[0], mg, f.dtype, false, plan.unit == PAIRED ? 128 : 64) &&
                   operand_map(&q.b[1], mu, f.dtype, false, plan.unit == PAIRED ? 128 : 64));
-            set_output(q, 0, gate, n, n);
-            set_output(q, 1, up, n, n);
-            set_output(q, 2, h, fp, fp);
+            const int block = plan.unit == PAIRED ? 64 : 32;
+            check(set_output(q, 0, gate, n, n, f.dtype, block) && set_output(q, 1, up, n, n, f.dtype, block) &&
+                  set_output(q, 2, h, fp, fp, f.dtype, block));
             P.act = f.act;
             run<GATE_UP, false, false, 1>(P, 0, plan);
         }
@@ -1155,7 +1176,7 @@ struct Block {
         q.M = M;
         q.N = d;
         q.num_kb = q.kb_first = blocks_of(n, BK);
-        set_output(q, 0, y, d, d);
+        check(set_output(q, 0, y, d, d, f.dtype, 64));
         run<PLAIN, false, false, 1>(P, 1);
     }
 
@@ -1178,7 +1199,7 @@ struct Block {
             q.N = n;
             q.num_kb = q.kb_first = blocks_of(d, BK);
             void* outs[3] = {dg, du, h};
-            for (int i = 0; i < 3; ++i) set_output(q, i, outs[i], fp, fp);
+            for (int i = 0; i < 3; ++i) check(set_output(q, i, outs[i], fp, fp, f.dtype, 0));
             q.in[0] = mgate.p;
             q.in[1] = mup.p;
             q.ldi[0] = mgate.ld;
@@ -1197,7 +1218,7 @@ struct Block {
             q.N = d;
             q.kb_first = blocks_of(n, BK);
             q.num_kb = 2 * q.kb_first;
-            set_output(q, 0, dx, d, d);
+            check(set_output(q, 0, dx, d, d, f.dtype, 64));
             plan_i = plan_tiles(ctx, &q, 1, PLAIN);
         }
         if (!dwg && !dwu && !dwd) {
@@ -1213,7 +1234,7 @@ struct Block {
             q.M = w[i].rows;
             q.N = w[i].cols;
             q.num_kb = q.kb_first = blocks_of(M, BK);
-            set_output(q, 0, w[i].out, w[i].cols, w[i].cols);
+            check(set_output(q, 0, w[i].out, w[i].cols, w[i].cols, f.dtype, 64));
         }
         // (planned for all three, so that a gradient's bits do not depend on which others are wanted)
         const TilePlan plan = plan_tiles(ctx, P.p, 3, PLAIN, false);
