@@ -21,10 +21,16 @@
 // described to the tensor core "MN-major" instead of being transposed by a pass of its own.
 //
 // Roles of the 10 warps: warp 0 copies (TMA, 128-byte swizzle, 32 KB stages), warp 1 issues products, warps 2..9 read
-// finished accumulators, and store them through a shared-memory transpose while the next tile is
-// multiplied (two accumulators in tensor memory).  A CTA pair works on a 256 x 256 tile with cta_group::2 products; shapes with too few
-// of those take 128 x 128 tiles on single CTAs.  Every wait is bounded: one that expires raises SAMA_DEV_TIMEOUT, stops
-// the CTA's work, lets its copies land and exits.
+// finished accumulators and bring them out through shared memory while the next tile is multiplied (two accumulators in
+// tensor memory).  A CTA pair works on a 256 x 256 tile with cta_group::2 products; shapes with too few of those take
+// 128 x 128 tiles on single CTAs, or share a tile's contraction.  Every wait is bounded: one that expires raises
+// SAMA_DEV_TIMEOUT, stops the CTA's work, lets its copies land and exits.
+//
+// What bounds it (us on one B200, bf16): long contractions the tensor cores and the power limit (2048 tokens, 2048 x 5504,
+// forward and backward 316, 1310 TFLOP/s; 4096 tokens, 4096 x 8192 1650 to 1950, by the card's temperature); short ones
+// reading tensor memory, 64 bytes per cycle and SM, 2000 cycles for a pair's tile (64 tokens, 4096 x 8192: the weight
+// gradients, 201 MB, 54); few tokens the weights' way from memory and the start and end of two launches (45 tokens, 4096 x
+// 8192: 49, of which the weights' 201 MB at copy speed are 31); small models the launches (1024 tokens, 1024 x 2736: 89).
 #include <type_traits>
 
 #include "num_types.h"
@@ -214,7 +220,8 @@ __device__ __forceinline__ float2 activate(float x) {
         // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
         const float z2 = 1.59576912f * x * fmaf(0.044715f * x, x, 1.f);
         const float p = fast_rcp(1.f + fast_exp2(-kLog2e * z2));
-        return make_float2(x * p, GRAD ? fmaf(x * p * (1.f - p), 1.59576912f * fmaf(0.134145f * x, x, 1.f), p) : 0.f);
+        // (the slope of z is bounded: where x^2 overflows, p (1 - p) is 0 and so is their product)
+        return make_float2(x * p, GRAD ? fmaf(x * p * (1.f - p), 1.59576912f * fminf(fmaf(0.134145f * x, x, 1.f), 1e30f), p) : 0.f);
     }
 }
 
@@ -748,6 +755,8 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
 // blocks; weights go from memory straight to the registers of m16n8k16 products, 16 bytes per load.  (A thread's 8
 // consecutive k are used as the k-indices that the instruction wants from it; the tokens' operand is read with the same
 // permutation, so the sum is over the same products.)  The warps' partial sums are added in a fixed order.
+// 1 token, 4096 x 8192: 37 us for 201 MB, 5.5 TB/s.  The limit: at 16 tokens this and the tiles take the same 48 us at 4096
+// x 8192, and 9 against 14 at 512 x 1376; at 17, with twice the products here, 91 against 48 and 20 against 18 (1024 x 2736).
 constexpr int kFewTokens = 16, kFewWarps = 8;
 
 struct FewArgs {
@@ -859,7 +868,7 @@ ffn_few_kernel(const __grid_constant__ FewArgs a) {
 }
 
 // Rows of `cols` values at any address -> rows of `ld` (a multiple of 8) at an aligned one: what TMA can read.  All
-// matrices of a call in one launch.
+// matrices of a call in one launch.  Memory-bound where it counts (21 tokens, 3148 x 7198: 272 MB read and written, 54 us).
 struct AlignJobs {
     static constexpr int kMost = 7;
     const void* src[kMost];

@@ -189,6 +189,22 @@ def test_values_that_are_not_finite_stay_in_their_rows(lib, M):
     assert torch.equal(y[keep], clean[keep]) and bool(torch.isnan(y[1]).all()) and not bool(torch.isfinite(y[2]).any())
 
 
+@pytest.mark.parametrize("kind", ACTS)
+def test_gates_whose_square_overflows(lib, kind):
+    # a' is 1 to the right and 0 to the left of them, exactly, so dG is dH (rounded once) or 0
+    M, d, f = 32, 64, 96
+    t = make(M, d, f, "bf16", 5)
+    t["gate"].copy_(torch.where(t["gate"] > 0, 2.0 ** 100, -2.0 ** 100))
+    t["up"].fill_(1.0)
+    _, dwg, _, _ = backward(lib, t, kind, want=(0, 1, 0, 0))
+    x, wd, dy, G = (t[k].double() for k in ("x", "wd", "dy", "gate"))
+    dH, eH = dy @ wd, d * ACC * (dy.abs() @ wd.abs())
+    on = (G > 0).double()
+    dG, eG = dH * on, (eH + U["bf16"] * (dH.abs() + eH)) * on
+    err = eG.T @ x.abs() + M * ACC * ((dG.abs() + eG).T @ x.abs())
+    within(dwg, dG.T @ x, err, "bf16")
+
+
 def test_no_tokens(lib):
     S, ctx = lib
     t = make(4, 16, 24, "bf16")
