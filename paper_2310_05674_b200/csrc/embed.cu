@@ -18,7 +18,12 @@
 //                  written out; the parts of a run that crosses pieces go to the workspace in fp32, and the warps that
 //                  finish last add them up, in the order of the list.  The first blocks write the zeros still missing.
 // Up to 2048 tokens, where launches and round trips are what counts, one launch: every CTA sorts all tokens for itself in
-// shared memory, then takes its share of the pieces and of the rows to be zeroed.
+// shared memory, then takes its share of the pieces and of the rows to be zeroed (lookup and gradient, 8191 rows of 256
+// fp32 values: 2048 tokens 20 us, 2049 tokens, the other way, 25).
+//
+// Measured, gradient alone: 16,384 tokens, 50,021 rows of 1024 (bf16 in, fp32 out, 239 MB) 60 us; 131,007 tokens, 65,536
+// rows of 2048 bf16 values (805 MB) 215 us, 3.8 TB/s.  The sort takes 20 to 33 us of it, its length in cluster barriers.
+// The lookup moves 5.4 and 6.8 TB/s at these sizes.
 #include <type_traits>
 
 #include "num_types.h"
@@ -434,7 +439,7 @@ __device__ __forceinline__ void put_part(float* part, const Columns<PW, CH>& c, 
 
 // A thread's values of one row as they lie in memory.
 template <typename T, int PW, int CH> struct Raw {
-    using Chunk = std::conditional_t<PW == 1, T, std::conditional_t<PW == 2, uint32_t, uint4>>;
+    using Chunk = std::conditional_t<PW == 1, T, std::conditional_t<PW * sizeof(T) == 4, uint32_t, std::conditional_t<PW * sizeof(T) == 8, uint2, uint4>>>;
     static_assert(sizeof(Chunk) == PW * sizeof(T), "a chunk is one access");
     Chunk r[CH] = {};
     __device__ __forceinline__ void load(const T* row, const Columns<PW, CH>& c) {
@@ -451,6 +456,12 @@ template <typename T, int PW, int CH> struct Raw {
                 const float2 f = unpack2<T>(r[q]);
                 acc[2 * q] += f.x;
                 acc[2 * q + 1] += f.y;
+            } else if constexpr (sizeof(Chunk) == 8) {
+                const float2 f = unpack2<T>(r[q].x), g = unpack2<T>(r[q].y);
+                acc[4 * q] += f.x;
+                acc[4 * q + 1] += f.y;
+                acc[4 * q + 2] += g.x;
+                acc[4 * q + 3] += g.y;
             } else {
                 const uint32_t w[4] = {r[q].x, r[q].y, r[q].z, r[q].w};
 #pragma unroll
@@ -483,7 +494,8 @@ __device__ __forceinline__ void load_part(const float* part, const Columns<PW, C
 #pragma unroll
             for (int i = 0; i < PW / 4; ++i) {
                 const float4 x = __ldcg(reinterpret_cast<const float4*>(p) + i);
-                v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
+                float* o = v + q * PW + 4 * i;
+                o[0] = x.x; o[1] = x.y; o[2] = x.z; o[3] = x.w;
             }
         }
     }
@@ -803,12 +815,13 @@ Access access_of(int d, int dtype, uintptr_t addresses, bool wide_output) {
     return es == 2 && d % 2 == 0 && (addresses & (wide_output ? 7u : 3u)) == 0 ? PAIRS : SINGLES;
 }
 inline int columns_of(Access a, int dtype) { return a == GROUPS ? 16 / (int)dtype_size(dtype) : a == PAIRS ? 8 : a == SINGLES ? 4 : 1; }
-// fn<values per chunk, chunks>
-template <typename T, typename F>
+// fn<values per chunk, chunks>.  Groups of 16 bytes on both sides, so half a group of 16-bit values where the results are
+// fp32: two stores of 16 bytes, each 32 bytes from its neighbour's, would write every sector of L2 twice.
+template <typename T, typename TO, typename F>
 auto with_access(Access a, F&& fn) {
     using std::integral_constant;
-    constexpr int GROUP = 16 / sizeof(T), PAIR = sizeof(T) == 2 ? 2 : 1;   // (fp32 has no pairs: its single values are as wide)
-    return a == GROUPS    ? fn(integral_constant<int, GROUP>(), integral_constant<int, 1>())
+    constexpr int GROUP = 16 / sizeof(TO), GROUPS_OF = 16 / sizeof(T) / GROUP, PAIR = sizeof(T) == 2 ? 2 : 1;   // (fp32 has no pairs: its single values are as wide)
+    return a == GROUPS    ? fn(integral_constant<int, GROUP>(), integral_constant<int, GROUPS_OF>())
            : a == PAIRS   ? fn(integral_constant<int, PAIR>(), integral_constant<int, 4>())
            : a == SINGLES ? fn(integral_constant<int, 1>(), integral_constant<int, 4>())
                           : fn(integral_constant<int, 1>(), integral_constant<int, 1>());
@@ -819,18 +832,23 @@ cudaError_t embed_typed(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int 
                         float scale, void* out, cudaStream_t st) {
     const Access access = access_of(d, dtype, reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(out), false);
     const int tpr = threads_per_row(d, columns_of(access, dtype)), rows = kEmbedThreads / tpr;
-    // four rows per thread once that still leaves every SM its full number of threads
-    const bool deep = n * tpr >= (int64_t)ctx->sm_count * 2048 * 4;
+    // Four rows per thread once one row each would be more threads than the SMs take at a time.  One row against four (us, rows
+    // of 1024 bf16 values): 2100 tokens 3.0 / 3.5, 4096 4.6 / 4.1, 8192 8.0 / 5.8, 16,384 15.9 / 12.1, 131,072 104 / 70.
+    // Rows in four chunks have four loads on their way as it is: not before three times as many (4821 rows of 2796 bf16 values
+    // 14.1 / 20.6, 32,768 of 100 5.0 / 6.5).
+    const bool chunks = access == PAIRS || access == SINGLES;
+    const bool deep = n * tpr >= (int64_t)ctx->sm_count * 2048 * 4 / (chunks ? 1 : 3);
     const int64_t per_block = (int64_t)rows * (deep ? 4 : 1);
     KernelScope scope(ctx, SAMA_K_EMBED, -1, st);
-    return with_access<T>(access, [&](auto pw, auto ch) {
+    return with_access<T, T>(access, [&](auto pw, auto ch) {
         auto* kernel = deep ? embed_kernel<T, decltype(pw)::value, decltype(ch)::value, 4> : embed_kernel<T, decltype(pw)::value, decltype(ch)::value, 1>;
         return launch_dependent(kernel, dim3((unsigned)((n + per_block - 1) / per_block)), dim3(kEmbedThreads), 0, st, n, vocab,
                                 d, tpr, static_cast<const T*>(table), ids, scale, static_cast<T*>(out), &ctx->scalars->status);
     });
 }
 
-// Entries per piece: as many as still give every SM 24 warps, 8 to 64.
+// Entries per piece: as many as still give every SM 24 warps, 8 to 64.  With 8, 16, 32 and 64 (us, rows of 1024 bf16
+// values): 4096 tokens 27.2, 29.0, 31.8, 41.5; 16,384 41.5, 40.1, 43.3, 50.1; 131,072 208, 145, 122, 113.
 int piece_of(const sama_ctx* ctx, int64_t n, int slabs) {
     int piece = 64;
     while (piece > 8 && (n + piece - 1) / piece * slabs < (int64_t)ctx->sm_count * 24) piece /= 2;
@@ -872,7 +890,7 @@ struct ReduceLaunch {
     static cudaError_t run(sama_ctx* ctx, const ReduceArgs& a, Access access, cudaStream_t st) {
         KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
         const int64_t units = (int64_t)a.pieces * a.slabs, per = kEmbedThreads / 32;
-        return with_access<T>(access, [&](auto pw, auto ch) {
+        return with_access<T, TG>(access, [&](auto pw, auto ch) {
             return launch_dependent(embed_reduce_kernel<T, TG, decltype(pw)::value, decltype(ch)::value>,
                                     dim3((unsigned)(a.fill_blocks + (units + per - 1) / per)), dim3(kEmbedThreads), 0, st, a);
         });
@@ -882,7 +900,7 @@ template <typename T, typename TG>
 struct FewLaunch {
     static cudaError_t run(sama_ctx* ctx, const ReduceArgs& a, const FewArgs& f, Access access, int ctas, cudaStream_t st) {
         KernelScope scope(ctx, SAMA_K_EMBED_GRAD, -1, st);
-        return with_access<T>(access, [&](auto pw, auto ch) {
+        return with_access<T, TG>(access, [&](auto pw, auto ch) {
             return launch_dependent(embed_few_kernel<T, TG, decltype(pw)::value, decltype(ch)::value>, dim3((unsigned)ctas),
                                     dim3(kFewThreads), sizeof(FewSmem), st, a, f);
         });
@@ -891,7 +909,7 @@ struct FewLaunch {
         cudaError_t e = cudaSuccess;
         for (Access access : {GROUPS, PAIRS, SINGLES, SINGLE})
             if (e == cudaSuccess)
-                e = with_access<T>(access, [&](auto pw, auto ch) {
+                e = with_access<T, TG>(access, [&](auto pw, auto ch) {
                     return cudaFuncSetAttribute(embed_few_kernel<T, TG, decltype(pw)::value, decltype(ch)::value>,
                                                 cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(FewSmem));
                 });
