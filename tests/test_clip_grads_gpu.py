@@ -79,6 +79,20 @@ def test_separate_outputs(lib, sizes, types, max_norm, shift):
     assert S.sama_device_status(ctx) == 0
 
 
+@pytest.mark.parametrize("count", [1, 100, 112, 113])
+@pytest.mark.parametrize("total", [2 ** 18 + 1, 2 ** 19, 2 ** 19 + 1])
+@pytest.mark.parametrize("types", [["f32"], ["bf16", "f32", "f16"]])
+def test_where_one_launch_ends(lib, count, total, types):
+    sizes = [total // count] * (count - 1)
+    sizes.append(total - sum(sizes))
+    ins = tensors(sizes, types, 4)
+    outs = [torch.full_like(x, 7.0) for x in ins]
+    norm, ref = plain(ins, 0.5)
+    assert abs(run(lib, ins, outs, 0.5) - norm) <= 1.1 * 2.0 ** -24 * norm
+    for y, r in zip(outs, ref):
+        close(y, r)
+
+
 @pytest.mark.parametrize("types", [["f32"], ["bf16"], ["f16", "f32"]])
 @pytest.mark.parametrize("sizes", ["small", "ragged", "many"])
 def test_into_the_flat_vector(lib, types, sizes):
