@@ -258,7 +258,7 @@ typedef enum sama_dtype { SAMA_F32 = 0, SAMA_BF16 = 1, SAMA_F16 = 2 } sama_dtype
 
 /* Token embedding: out[t][:] = scale * table[ids[t]][:], computed in fp32 and rounded once.
  * table: [vocab][d], out: [n_tokens][d], both of type `dtype`; ids: int32 [n_tokens].  0 <= n_tokens <= 2^30,
- * 1 <= vocab < 2^31 - 1, d >= 1.  An id outside [0, vocab) sets SAMA_DEV_BAD_INDEX and its row of out is 0. */
+ * 1 <= vocab < 2^31 - 1, 1 <= d <= 2^30.  An id outside [0, vocab) sets SAMA_DEV_BAD_INDEX and its row of out is 0. */
 int sama_embed(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t vocab, int32_t d, const void* table,
                const int32_t* ids, float scale, void* out, void* stream);
 

@@ -23,9 +23,11 @@ int need_workspace(sama_ctx* ctx, size_t bytes, cudaStream_t st) {
     return SAMA_OK;
 }
 
-// n_tokens * d and vocab * d elements of at most 4 bytes stay far from the end of 64 bits
+// The kernels step through a row's columns in 32 bits, up to 8192 beyond its end.  With this limit on d, n_tokens * d and
+// vocab * d elements of at most 4 bytes stay within 2^63 bytes, too.
+constexpr int32_t kMaxColumns = 1 << 30;
 bool embed_sizes_ok(int64_t n_tokens, int64_t vocab, int32_t d) {
-    return n_tokens >= 0 && n_tokens <= kMaxTokens && vocab >= 1 && vocab < 0x7fffffff && d >= 1;
+    return n_tokens >= 0 && n_tokens <= kMaxTokens && vocab >= 1 && vocab < 0x7fffffff && d >= 1 && d <= kMaxColumns;
 }
 
 struct Span {
