@@ -102,12 +102,13 @@ class TensorList:
         self.ins, self.outs = list(ins), list(ins if outs is None else outs)
         if len(self.ins) != len(self.outs):
             raise SamaError(SAMA_ERR_SIZE, "TensorList")
+        self.device = self.ins[0].get_device() if self.ins else None
         self._arr = (sama_tensor_t * max(1, len(self.ins)))()
         for e, x, y in zip(self._arr, self.ins, self.outs):
             e.n, e.dtype = x.numel(), _dtype_of(x)
-            e.in_ = _dense(x, e.dtype, 0, "TensorList")
+            e.in_ = _dense(self.device, x, e.dtype, 0, "TensorList")
             e.out_dtype = e.dtype if y is None else _dtype_of(y)
-            e.out = None if y is None else _dense(y, e.out_dtype, e.n, "TensorList")
+            e.out = None if y is None else _dense(self.device, y, e.out_dtype, e.n, "TensorList")
 
     def c(self):
         return self._arr
@@ -187,11 +188,18 @@ def _dtype_of(x) -> int:
     raise SamaError(SAMA_ERR_PARAM, "a tensor is of type %s" % x.dtype)
 
 
-def _dense(x, dtype: int, count: int, where: str) -> Optional[int]:
-    """Address of an operand of the text-model operators, which take several types: a tensor has to be contiguous, of
-    the type that the call names (ids: "i32") and hold at least ``count`` elements.  Ints and None pass through."""
+_device_of = {}   # context handle -> the GPU it was created for
+
+
+def _dense(device: Optional[int], x, dtype: int, count: int, where: str) -> Optional[int]:
+    """Address of an operand of the text-model operators, which take several types: a tensor has to be on GPU ``device``
+    (None: on some GPU), contiguous, of the type that the call names (ids: "i32") and hold at least ``count`` elements.
+    Ints and None pass through."""
     if x is None or isinstance(x, int):
         return x
+    at = x.get_device()   # -1: not on a GPU
+    if at < 0 or (device is not None and at != device):
+        raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is on %s, not on the context's GPU" % (where, x.device))
     if not _torch_dtypes:
         _fill_dtypes()
     if x.dtype is not _torch_dtypes.get(dtype) or not x.is_contiguous():
@@ -237,10 +245,12 @@ def sama_create(device: int, max_n: int, max_batch: int, mlp: Optional[MLP]) -> 
     out = _vp()
     _check(lib.sama_create(C.byref(out), int(device), int(max_n), int(max_batch), mlp.c() if mlp else None),
            "sama_create")
+    _device_of[out.value] = int(device)
     return out.value
 
 
 def sama_destroy(ctx: int) -> int:
+    _device_of.pop(ctx, None)
     return _check(lib.sama_destroy(ctx), "sama_destroy")
 
 
@@ -332,44 +342,46 @@ def sama_meta_grad(ctx, mlp: MLP, theta, X_meta, y_meta, B, g_meta_out, loss_out
 
 
 def sama_embed(ctx, dtype, n_tokens, vocab, d, table, ids, scale, out, stream=None) -> int:
-    w = "sama_embed"
-    return _check(lib.sama_embed(ctx, dtype, n_tokens, vocab, d, _dense(table, dtype, vocab * d, w),
-                                 _dense(ids, "i32", n_tokens, w), scale, _dense(out, dtype, n_tokens * d, w),
+    w, v = "sama_embed", _device_of.get(ctx)
+    return _check(lib.sama_embed(ctx, dtype, n_tokens, vocab, d, _dense(v, table, dtype, vocab * d, w),
+                                 _dense(v, ids, "i32", n_tokens, w), scale, _dense(v, out, dtype, n_tokens * d, w),
                                  _stream(stream)), w)
 
 
 def sama_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, grad_dtype, accumulate, grad,
                     stream=None) -> int:
-    w = "sama_embed_grad"
-    return _check(lib.sama_embed_grad(ctx, dtype, n_tokens, vocab, d, _dense(ids, "i32", n_tokens, w),
-                                      _dense(d_out, dtype, n_tokens * d, w), scale, skip_id, grad_dtype, accumulate,
-                                      _dense(grad, grad_dtype, vocab * d, w), _stream(stream)), w)
+    w, v = "sama_embed_grad", _device_of.get(ctx)
+    return _check(lib.sama_embed_grad(ctx, dtype, n_tokens, vocab, d, _dense(v, ids, "i32", n_tokens, w),
+                                      _dense(v, d_out, dtype, n_tokens * d, w), scale, skip_id, grad_dtype, accumulate,
+                                      _dense(v, grad, grad_dtype, vocab * d, w), _stream(stream)), w)
 
 
 def sama_gated_ffn(ctx, dtype, act, n_tokens, d, f, x, w_gate, w_up, w_down, y, gate_out=None, up_out=None,
                    stream=None) -> int:
-    w = "sama_gated_ffn"
-    return _check(lib.sama_gated_ffn(ctx, dtype, act, n_tokens, d, f, _dense(x, dtype, n_tokens * d, w),
-                                     _dense(w_gate, dtype, f * d, w), _dense(w_up, dtype, f * d, w),
-                                     _dense(w_down, dtype, d * f, w), _dense(y, dtype, n_tokens * d, w),
-                                     _dense(gate_out, dtype, n_tokens * f, w), _dense(up_out, dtype, n_tokens * f, w),
+    w, v = "sama_gated_ffn", _device_of.get(ctx)
+    return _check(lib.sama_gated_ffn(ctx, dtype, act, n_tokens, d, f, _dense(v, x, dtype, n_tokens * d, w),
+                                     _dense(v, w_gate, dtype, f * d, w), _dense(v, w_up, dtype, f * d, w),
+                                     _dense(v, w_down, dtype, d * f, w), _dense(v, y, dtype, n_tokens * d, w),
+                                     _dense(v, gate_out, dtype, n_tokens * f, w), _dense(v, up_out, dtype, n_tokens * f, w),
                                      _stream(stream)), w)
 
 
 def sama_gated_ffn_grad(ctx, dtype, act, n_tokens, d, f, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up,
                         dw_down, stream=None) -> int:
-    w = "sama_gated_ffn_grad"
+    w, v = "sama_gated_ffn_grad", _device_of.get(ctx)
     t, h, m = n_tokens * d, n_tokens * f, d * f
-    return _check(lib.sama_gated_ffn_grad(ctx, dtype, act, n_tokens, d, f, _dense(x, dtype, t, w),
-                                          _dense(w_gate, dtype, m, w), _dense(w_up, dtype, m, w),
-                                          _dense(w_down, dtype, m, w), _dense(gate, dtype, h, w), _dense(up, dtype, h, w),
-                                          _dense(dy, dtype, t, w), _dense(dx, dtype, t, w), _dense(dw_gate, dtype, m, w),
-                                          _dense(dw_up, dtype, m, w), _dense(dw_down, dtype, m, w), _stream(stream)), w)
+    return _check(lib.sama_gated_ffn_grad(ctx, dtype, act, n_tokens, d, f, _dense(v, x, dtype, t, w),
+                                          _dense(v, w_gate, dtype, m, w), _dense(v, w_up, dtype, m, w),
+                                          _dense(v, w_down, dtype, m, w), _dense(v, gate, dtype, h, w), _dense(v, up, dtype, h, w),
+                                          _dense(v, dy, dtype, t, w), _dense(v, dx, dtype, t, w), _dense(v, dw_gate, dtype, m, w),
+                                          _dense(v, dw_up, dtype, m, w), _dense(v, dw_down, dtype, m, w), _stream(stream)), w)
 
 
 def sama_clip_grads(ctx, tensors: TensorList, max_norm, norm_out=None, stream=None) -> int:
-    w = "sama_clip_grads"
-    return _check(lib.sama_clip_grads(ctx, tensors.c(), len(tensors.ins), max_norm, _dense(norm_out, SAMA_F32, 1, w),
+    w, v = "sama_clip_grads", _device_of.get(ctx)
+    if v is not None and tensors.device is not None and tensors.device != v:
+        raise SamaError(SAMA_ERR_PARAM, "%s: the tensors are not on the context's GPU" % w)
+    return _check(lib.sama_clip_grads(ctx, tensors.c(), len(tensors.ins), max_norm, _dense(v, norm_out, SAMA_F32, 1, w),
                                       _stream(stream)), w)
 
 
