@@ -12,7 +12,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
-from typing import Optional, Sequence
+from typing import Iterable, Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsama.so")
@@ -98,8 +98,9 @@ class TensorList:
     are.  ``outs``: one tensor per input (the input itself: in place; None: counted in the norm only), or None for all
     in place.  Holds references, so the addresses stay valid."""
 
-    def __init__(self, ins: Sequence, outs: Optional[Sequence] = None):
-        self.ins, self.outs = list(ins), list(ins if outs is None else outs)
+    def __init__(self, ins: Iterable, outs: Optional[Iterable] = None):
+        self.ins = list(ins)
+        self.outs = list(self.ins if outs is None else outs)
         if len(self.ins) != len(self.outs):
             raise SamaError(SAMA_ERR_SIZE, "TensorList")
         self.device = self.ins[0].get_device() if self.ins else None

@@ -79,3 +79,26 @@ def test_tensors_on_another_gpu_than_the_context_are_refused(S, monkeypatch):
     with pytest.raises(S.SamaError) as e:
         S.sama_clip_grads(4096, tensors, 1.0, stream=0)
     assert e.value.status == S.SAMA_ERR_PARAM
+
+
+def test_a_list_in_place_takes_any_iterable(S):
+    class OnGpu:
+        dtype = device = None
+
+        def numel(self):
+            return 8
+
+        def get_device(self):
+            return 0
+
+        def is_contiguous(self):
+            return True
+
+        def data_ptr(self):
+            return 4096
+
+    import torch
+    OnGpu.dtype = torch.float32
+    x = OnGpu()
+    tensors = S.TensorList(t for t in [x, x])
+    assert tensors.ins == tensors.outs == [x, x] and tensors.c()[1].out == tensors.c()[1].in_ == 4096
