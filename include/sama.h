@@ -252,8 +252,11 @@ int sama_biasreg_step(sama_ctx* ctx, int32_t d, int32_t n_val, const float* Xv, 
  * features and gradients next to the step: their gradients, clipped into one flat fp32 vector, are the g_base or
  * g_meta of sama_adapt and sama_step.  They need a context (any sama_create will do, mlp may be NULL) for its
  * status word and for a workspace that is allocated on first use and grows with the largest call (cudaMalloc;
- * synchronises the stream).  A stream capture must therefore be preceded by a call of at least its sizes, and a
- * captured graph must not be replayed after a larger call has made the workspace grow. */
+ * synchronises the stream).  What an operator reserves depends on a call's sizes alone and does not fall as they
+ * grow, except that the feed-forward block needs more where it has to copy operands (see there).  A stream capture
+ * must therefore be preceded by a call of the same operator of at least its sizes, with operands to copy if the
+ * captured one has them; and a captured graph must not be replayed after the workspace has grown, which a call of no
+ * larger sizes, and with no new need of copies, does not do. */
 typedef enum sama_dtype { SAMA_F32 = 0, SAMA_BF16 = 1, SAMA_F16 = 2 } sama_dtype;
 
 /* Token embedding: out[t][:] = scale * table[ids[t]][:], computed in fp32 and rounded once.

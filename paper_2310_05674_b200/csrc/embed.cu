@@ -857,6 +857,12 @@ int piece_of(const sama_ctx* ctx, int64_t n, int slabs) {
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Rows of the table per share of the zeroing, and the two areas of the workspace that belong to it.
+inline int64_t fill_share(int64_t vocab) { return ((vocab + kFillCtas - 1) / kFillCtas + 31) & ~(int64_t)31; }
+inline size_t present_bytes(int64_t vocab) { return up256((size_t)(fill_share(vocab) / 32) * kFillCtas * 4); }
+constexpr size_t kProgressBytes = sizeof(int) * kFillCtas * 32;
+static_assert(kProgressBytes % 256 == 0, "what follows it is aligned");
+
 struct GradPlan {
     bool few;
     Access access;
@@ -878,9 +884,9 @@ GradPlan make_plan(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int
     g.counters = (2 * g.pieces + (g.pieces + kJoin - 1) / kJoin) * g.slabs;
     g.few = n <= kFewTokens && g.counters <= kFewCounters && vocab <= (int64_t)ctx->sm_count * (kFewShare / 2);
     g.arrived = up256(sizeof(int) * (size_t)g.counters);
-    g.share = ((vocab + kFillCtas - 1) / kFillCtas + 31) & ~(int64_t)31;
-    g.present = up256((size_t)(g.share / 32) * kFillCtas * 4);
-    g.progress = up256(sizeof(int) * kFillCtas * 32);
+    g.share = fill_share(vocab);
+    g.present = present_bytes(vocab);
+    g.progress = kProgressBytes;
     g.parts = up256(sizeof(float) * (size_t)g.pieces * d);
     return g;
 }
@@ -952,15 +958,34 @@ cudaError_t launch_embed(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int
 }
 
 // Workspace: two lists of (id, position), the rows' runs, arrival counters, and two parts per piece.
-size_t embed_grad_workspace(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout,
-                            int grad_dtype, const void* grad) {
+size_t embed_grad_plan_bytes(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout,
+                             int grad_dtype, const void* grad) {
     return make_plan(ctx, dtype, n, vocab, d, dout, grad_dtype, grad).total();
+}
+
+// What is reserved: enough for every plan of at most these sizes, whatever its types and alignment, so that no smaller
+// call needs more.  (A plan's own need is not monotone: with more tokens the pieces get longer, and their parts fewer.)
+// A plan has pieces of 64 entries, or fewer than 48 pieces x slabs per SM (see piece_of), and never pieces of fewer than 8;
+// a slab has 128 to 256 columns, or all of up to 32.
+size_t embed_grad_workspace(const sama_ctx* ctx, int64_t n, int64_t vocab, int d) {
+    const int64_t busy = (int64_t)ctx->sm_count * 48, long_pieces = (n + 63) / 64, short_pieces = (n + 7) / 8;
+    const int64_t slabs = ((int64_t)d + 127) / 128;
+    auto larger = [](int64_t a, int64_t b) { return a > b ? a : b; };
+    int64_t part = larger(long_pieces * d, busy * 256);
+    if (part > short_pieces * d) part = short_pieces * d;
+    const int64_t counters = 2 * larger(long_pieces * slabs, busy) +
+                             larger((long_pieces + kJoin - 1) / kJoin * slabs, busy / kJoin + slabs);
+    const size_t parts = 2 * up256(sizeof(float) * (size_t)part);
+    if (n <= kFewTokens && counters <= kFewCounters && vocab <= (int64_t)ctx->sm_count * (kFewShare / 2)) return parts;
+    return 2 * up256(sizeof(int2) * (size_t)n) + up256(sizeof(int2) * (size_t)vocab) + up256(sizeof(int) * (size_t)counters) +
+           present_bytes(vocab) + kProgressBytes + parts;
 }
 
 cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const int32_t* ids,
                               const void* dout, float scale, int32_t skip_id, int grad_dtype, int accumulate, void* grad,
-                              void* ws, cudaStream_t st) {
+                              void* ws, size_t ws_bytes, cudaStream_t st) {
     const GradPlan g = make_plan(ctx, dtype, n, vocab, d, dout, grad_dtype, grad);
+    if (g.total() > ws_bytes) return cudaErrorInvalidValue;
     if (!ctx->embed_ready) {
         const cudaError_t e = prepare_embed(ctx);
         if (e != cudaSuccess) return e;

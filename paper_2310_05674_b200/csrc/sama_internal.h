@@ -332,11 +332,12 @@ cudaError_t run_meta_grad(sama_ctx* ctx, const sama_mlp_t* mlp, const float* the
 // embed.cu : token embedding and its gradient
 cudaError_t launch_embed(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* table, const int32_t* ids,
                          float scale, void* out, cudaStream_t st);
-size_t embed_grad_workspace(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout,
-                            int grad_dtype, const void* grad);
+size_t embed_grad_plan_bytes(const sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const void* dout,
+                             int grad_dtype, const void* grad);  // what this call needs
+size_t embed_grad_workspace(const sama_ctx* ctx, int64_t n, int64_t vocab, int d);  // what no call up to these sizes exceeds
 cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab, int d, const int32_t* ids,
                               const void* dout, float scale, int32_t skip_id, int grad_dtype, int accumulate, void* grad,
-                              void* ws, cudaStream_t st);
+                              void* ws, size_t ws_bytes, cudaStream_t st);
 
 // clip_grads.cu : global gradient norm and clipping
 cudaError_t launch_clip_grads(sama_ctx* ctx, const sama_tensor_t* t, int n, float max_norm, float* norm_out,

@@ -99,10 +99,10 @@ int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t voca
         if (!accumulate) SAMA_CUDA(ctx, cudaMemsetAsync(grad, 0, gb, st));
         return SAMA_OK;
     }
-    const int rc = need_workspace(ctx, embed_grad_workspace(ctx, dtype, n_tokens, vocab, d, d_out, grad_dtype, grad), st);
+    const int rc = need_workspace(ctx, embed_grad_workspace(ctx, n_tokens, vocab, d), st);
     if (rc != SAMA_OK) return rc;
     SAMA_CUDA(ctx, launch_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, grad_dtype, accumulate,
-                                     grad, ctx->op_ws, st));
+                                     grad, ctx->op_ws, ctx->op_ws_bytes, st));
     return SAMA_OK;
 }
 

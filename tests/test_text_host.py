@@ -1,7 +1,14 @@
 """Host side of the text-model operators: what is refused, and how, before anything is launched.  No kernel runs."""
 import ctypes
+import math
+import os
+import random
+import subprocess
 
 import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
 
 
 @pytest.fixture(scope="module")
@@ -10,6 +17,24 @@ def S():
     build.build()
     from paper_2310_05674_b200 import binding
     return binding
+
+
+@pytest.fixture(scope="module")
+def sizes(S, tmp_path_factory):
+    """Answers of text_sizes.cpp, a line of numbers for each line asked."""
+    from paper_2310_05674_b200 import build
+    cuda = os.path.dirname(os.path.dirname(build.NVCC))
+    exe = str(tmp_path_factory.mktemp("sizes") / "text_sizes")
+    subprocess.check_call(["g++", "-std=c++17", "-I", os.path.join(cuda, "include"), "-I", os.path.join(ROOT, "include"),
+                           "-I", build.CSRC, os.path.join(HERE, "text_sizes.cpp"), "-o", exe, S.LIB_PATH,
+                           "-Wl,-rpath," + os.path.dirname(S.LIB_PATH), "-L", os.path.join(cuda, "lib64"), "-lcudart"])
+
+    def ask(lines):
+        out = subprocess.run([exe], input="\n".join(lines), capture_output=True, text=True, check=True).stdout
+        rows = [[int(v) for v in line.split()] for line in out.splitlines()]
+        assert len(rows) == len(lines)
+        return rows
+    return ask
 
 
 @pytest.fixture
@@ -102,3 +127,34 @@ def test_a_list_in_place_takes_any_iterable(S):
     x = OnGpu()
     tensors = S.TensorList(t for t in [x, x])
     assert tensors.ins == tensors.outs == [x, x] and tensors.c()[1].out == tensors.c()[1].in_ == 4096
+
+
+def embed_line(n, vocab, d, dtype=1, grad_dtype=0, shift=0):
+    return "embed %d %d %d %d %d %d %d" % (dtype, n, vocab, d, 4096 + (4 if dtype == 0 else 2) * shift, grad_dtype, 8192)
+
+
+def test_no_smaller_embedding_gradient_needs_a_larger_workspace(sizes):
+    """What a call reserves covers every call of at most its sizes, of any type and alignment."""
+    # fewer tokens have shorter pieces, and more parts
+    at = {n: sizes([embed_line(n, 50021, 1024)])[0] for n in (14000, 14192, 16384, 28416)}
+    assert at[14192][1] > at[16384][1] > at[28416][1]          # (what the plans need)
+    assert at[14000][0] <= at[14192][0] <= at[16384][0] <= at[28416][0]
+    rng = random.Random(3)
+
+    def log(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    asked = []
+    for _ in range(4000):
+        n, vocab, d = log(1, 1 << 21), log(1, 1 << 25), log(1, 1 << 18 if rng.random() < 0.2 else 8192)
+        if rng.random() < 0.3:
+            n, d = rng.choice([n, 2047, 2048, 2049, 131072]), rng.choice([d, 8, 32, 33, 128, 256, 1024, 129152, 129153])
+        asked.append((n, vocab, d))
+        asked.append(tuple(max(1, v if rng.random() < 0.4 else int(v * rng.random())) for v in (n, vocab, d)))
+    kinds = [(dt, gt, shift) for dt, gt in ((0, 0), (1, 0), (1, 1), (2, 0), (2, 2)) for shift in (0, 1)]
+    rows = sizes([embed_line(*a, *k) for a in asked for k in kinds])
+    for i in range(0, len(asked), 2):
+        large, small = (rows[j * len(kinds):(j + 1) * len(kinds)] for j in (i, i + 1))
+        assert len({r[0] for r in large}) == 1                 # not by type, not by alignment
+        assert small[0][0] <= large[0][0], asked[i:i + 2]
+        assert all(need <= reserved for reserved, need in large + small), asked[i:i + 2]

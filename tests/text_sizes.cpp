@@ -1,0 +1,26 @@
+// Prints, for each line of the standard input, sizes that the text-model operators compute on the host for a GPU of 148 SMs.
+//   embed DTYPE N VOCAB D DOUT GRAD_DTYPE GRAD  ->  bytes that are reserved, bytes that this call's plan needs
+#include <cstdio>
+#include <cstring>
+
+#include "sama_internal.h"
+
+int main() {
+    static sama_ctx ctx;
+    std::memset(static_cast<void*>(&ctx), 0, sizeof ctx);
+    ctx.sm_count = 148;
+    char what[16];
+    while (std::scanf("%15s", what) == 1) {
+        long long n, vocab, dout, grad;
+        int dtype, d, grad_dtype;
+        if (std::strcmp(what, "embed") == 0 &&
+            std::scanf("%d %lld %lld %d %lld %d %lld", &dtype, &n, &vocab, &d, &dout, &grad_dtype, &grad) == 7) {
+            std::printf("%zu %zu\n", sama::embed_grad_workspace(&ctx, n, vocab, d),
+                        sama::embed_grad_plan_bytes(&ctx, dtype, n, vocab, d, reinterpret_cast<void*>(dout), grad_dtype,
+                                                    reinterpret_cast<void*>(grad)));
+        } else {
+            return 1;
+        }
+    }
+    return 0;
+}
