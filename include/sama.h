@@ -280,8 +280,8 @@ int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t voca
  * x, y: [n_tokens][d]; w_gate, w_up: [f][d]; w_down: [d][f], row-major, all of type `dtype` (SAMA_BF16 or SAMA_F16).
  * gate_out, up_out: [n_tokens][f], G and U as the backward pass wants them, or both NULL.  Products are summed in fp32;
  * H is rounded to `dtype` in between.  0 <= n_tokens <= 2^24, 1 <= d, f <= 2^20, any of them odd; 16-byte aligned
- * operands with d and f multiples of 8 are read in place, others are first copied to the workspace.
- * Outputs must not overlap the inputs or one another.
+ * operands with d and f multiples of 8 are read in place, others are first copied to the workspace (in the forward pass
+ * from 17 tokens on: up to 16 read them in place, too).  Outputs must not overlap the inputs or one another.
  *
  * sama_gated_ffn_grad, given the gradient dy of Y, G and U:
  *   dH = dY Wd,  dG = dH * U * a'(G),  dU = dH * a(G),

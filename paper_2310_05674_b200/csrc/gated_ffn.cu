@@ -1262,12 +1262,13 @@ struct Block {
 
 }  // namespace
 
-// `copies`: some operand starts at an odd address or has rows that do.
+// H (and dG and dU), then the copies of operands.  `copies`: some operand starts at an odd address or has rows that do.
 size_t ffn_workspace(const FfnShape& f, bool grad, bool copies) {
     const size_t M = (size_t)f.n_tokens, dp = up8(f.d), fp = up8(f.f);
-    size_t b = (grad ? 3 : 1) * up256(M * fp * 2);
-    if (copies) b += 2 * up256(M * dp * 2) + 2 * up256((size_t)f.f * dp * 2) + up256((size_t)f.d * fp * 2) + 2 * up256(M * fp * 2);
-    return b;
+    const size_t hidden = (grad ? 3 : 1) * up256(M * fp * 2);
+    if (!copies || (!grad && f.n_tokens <= kFewTokens)) return hidden;   // (ffn_few_kernel copies nothing)
+    const size_t x_and_weights = up256(M * dp * 2) + 2 * up256((size_t)f.f * dp * 2) + up256((size_t)f.d * fp * 2);
+    return hidden + x_and_weights + (grad ? up256(M * dp * 2) + 2 * up256(M * fp * 2) : 0);   // dY, G and U
 }
 
 cudaError_t launch_ffn_forward(sama_ctx* ctx, const FfnShape& f, const void* x, const void* wg, const void* wu,

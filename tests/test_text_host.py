@@ -158,3 +158,20 @@ def test_no_smaller_embedding_gradient_needs_a_larger_workspace(sizes):
         assert len({r[0] for r in large}) == 1                 # not by type, not by alignment
         assert small[0][0] <= large[0][0], asked[i:i + 2]
         assert all(need <= reserved for reserved, need in large + small), asked[i:i + 2]
+
+
+def test_the_feed_forward_block_reserves_what_it_uses(sizes):
+    """H (three such matrices for a backward pass), and the operands that are copied: rows of whole 16-byte groups."""
+    def group(x):
+        return -(-x // 8) * 8
+
+    def area(rows, cols):
+        return -(-rows * group(cols) * 2 // 256) * 256
+
+    d, f = 3429, 9421
+    weights = 2 * area(f, d) + area(d, f)
+    for n in (1, 16, 17, 700):
+        hidden, x = area(n, f), area(n, d)
+        got = [r[0] for r in sizes(["ffn %d %d %d %d %d" % (n, d, f, grad, copies) for grad in (0, 1) for copies in (0, 1)])]
+        # up to 16 tokens, the forward pass reads odd operands where they are
+        assert got == [hidden, hidden + (x + weights if n > 16 else 0), 3 * hidden, 5 * hidden + 2 * x + weights], n

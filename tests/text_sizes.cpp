@@ -1,5 +1,6 @@
 // Prints, for each line of the standard input, sizes that the text-model operators compute on the host for a GPU of 148 SMs.
 //   embed DTYPE N VOCAB D DOUT GRAD_DTYPE GRAD  ->  bytes that are reserved, bytes that this call's plan needs
+//   ffn N D F GRAD COPIES                       ->  bytes that are reserved
 #include <cstdio>
 #include <cstring>
 
@@ -12,12 +13,14 @@ int main() {
     char what[16];
     while (std::scanf("%15s", what) == 1) {
         long long n, vocab, dout, grad;
-        int dtype, d, grad_dtype;
+        int dtype, d, f, grad_dtype, copies;
         if (std::strcmp(what, "embed") == 0 &&
             std::scanf("%d %lld %lld %d %lld %d %lld", &dtype, &n, &vocab, &d, &dout, &grad_dtype, &grad) == 7) {
             std::printf("%zu %zu\n", sama::embed_grad_workspace(&ctx, n, vocab, d),
                         sama::embed_grad_plan_bytes(&ctx, dtype, n, vocab, d, reinterpret_cast<void*>(dout), grad_dtype,
                                                     reinterpret_cast<void*>(grad)));
+        } else if (std::strcmp(what, "ffn") == 0 && std::scanf("%lld %d %d %d %d", &n, &d, &f, &grad_dtype, &copies) == 5) {
+            std::printf("%zu\n", sama::ffn_workspace({n, d, f, SAMA_BF16, SAMA_ACT_SILU}, grad_dtype != 0, copies != 0));
         } else {
             return 1;
         }
