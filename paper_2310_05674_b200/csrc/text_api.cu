@@ -12,7 +12,13 @@ namespace {
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 
 // The operators' workspace, at least `bytes` large.  Growing it waits for the work that may still use the old one.
-int need_workspace(sama_ctx* ctx, size_t bytes, cudaStream_t st) {
+// `ready`: the operator's kernels are set up; the first call does that, and allocates for it.  Neither is possible while
+// the stream is being captured, and trying would break the capture: the call is refused before.
+int need_workspace(sama_ctx* ctx, size_t bytes, bool ready, cudaStream_t st) {
+    if (ready && ctx->op_ws_bytes >= bytes) return SAMA_OK;
+    cudaStreamCaptureStatus capture;
+    SAMA_CUDA(ctx, cudaStreamIsCapturing(st, &capture));
+    if (capture != cudaStreamCaptureStatusNone) return SAMA_ERR_NOMEM;
     if (ctx->op_ws_bytes >= bytes) return SAMA_OK;
     SAMA_CUDA(ctx, cudaStreamSynchronize(st));
     cudaFree(ctx->op_ws);
@@ -99,7 +105,7 @@ int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t voca
         if (!accumulate) SAMA_CUDA(ctx, cudaMemsetAsync(grad, 0, gb, st));
         return SAMA_OK;
     }
-    const int rc = need_workspace(ctx, embed_grad_workspace(ctx, n_tokens, vocab, d), st);
+    const int rc = need_workspace(ctx, embed_grad_workspace(ctx, n_tokens, vocab, d), ctx->embed_ready != 0, st);
     if (rc != SAMA_OK) return rc;
     SAMA_CUDA(ctx, launch_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, grad_dtype, accumulate,
                                      grad, ctx->op_ws, ctx->op_ws_bytes, st));
@@ -145,7 +151,7 @@ int sama_gated_ffn(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tokens, 
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SAMA_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)stream;
-    if ((rc = need_workspace(ctx, ffn_workspace(s, false, copies), st)) != SAMA_OK) return rc;
+    if ((rc = need_workspace(ctx, ffn_workspace(s, false, copies), ctx->ffn_pair_units > 0, st)) != SAMA_OK) return rc;
     SAMA_CUDA(ctx, launch_ffn_forward(ctx, s, x, w_gate, w_up, w_down, y, gate_out, up_out, ctx->op_ws, st));
     return SAMA_OK;
 }
@@ -170,7 +176,7 @@ int sama_gated_ffn_grad(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tok
             if (p) SAMA_CUDA(ctx, cudaMemsetAsync(p, 0, w, st));
         return SAMA_OK;
     }
-    if ((rc = need_workspace(ctx, ffn_workspace(s, true, copies), st)) != SAMA_OK) return rc;
+    if ((rc = need_workspace(ctx, ffn_workspace(s, true, copies), ctx->ffn_pair_units > 0, st)) != SAMA_OK) return rc;
     SAMA_CUDA(ctx, launch_ffn_backward(ctx, s, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down,
                                        ctx->op_ws, st));
     return SAMA_OK;
