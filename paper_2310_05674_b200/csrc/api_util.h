@@ -32,6 +32,19 @@ inline int cuda_fail(sama_ctx* ctx, cudaError_t e) {
         if (e__ != cudaSuccess) return cuda_fail((ctx), e__);  \
     } while (0)
 
+// For calls that set up an operator on first use: running out of memory there is what running out of it for the workspace is.
+inline int setup_fail(sama_ctx* ctx, cudaError_t e) {
+    cuda_fail(ctx, e);
+    if (e != cudaErrorMemoryAllocation) return SAMA_ERR_CUDA;
+    cudaGetLastError();   // (not an error that the next call should find)
+    return SAMA_ERR_NOMEM;
+}
+#define SAMA_SETUP(ctx, expr)                                   \
+    do {                                                        \
+        cudaError_t e__ = (expr);                               \
+        if (e__ != cudaSuccess) return setup_fail((ctx), e__);  \
+    } while (0)
+
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 // true if [a, a+na) and [b, b+nb) share a byte

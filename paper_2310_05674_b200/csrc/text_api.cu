@@ -107,8 +107,8 @@ int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t voca
     }
     const int rc = need_workspace(ctx, embed_grad_workspace(ctx, n_tokens, vocab, d), ctx->embed_ready != 0, st);
     if (rc != SAMA_OK) return rc;
-    SAMA_CUDA(ctx, launch_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, grad_dtype, accumulate,
-                                     grad, ctx->op_ws, ctx->op_ws_bytes, st));
+    SAMA_SETUP(ctx, launch_embed_grad(ctx, dtype, n_tokens, vocab, d, ids, d_out, scale, skip_id, grad_dtype, accumulate,
+                                      grad, ctx->op_ws, ctx->op_ws_bytes, st));
     return SAMA_OK;
 }
 
@@ -152,7 +152,7 @@ int sama_gated_ffn(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tokens, 
     if (!guard.ok) return SAMA_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)stream;
     if ((rc = need_workspace(ctx, ffn_workspace(s, false, copies), ctx->ffn_pair_units > 0, st)) != SAMA_OK) return rc;
-    SAMA_CUDA(ctx, launch_ffn_forward(ctx, s, x, w_gate, w_up, w_down, y, gate_out, up_out, ctx->op_ws, st));
+    SAMA_SETUP(ctx, launch_ffn_forward(ctx, s, x, w_gate, w_up, w_down, y, gate_out, up_out, ctx->op_ws, st));
     return SAMA_OK;
 }
 
@@ -177,8 +177,8 @@ int sama_gated_ffn_grad(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tok
         return SAMA_OK;
     }
     if ((rc = need_workspace(ctx, ffn_workspace(s, true, copies), ctx->ffn_pair_units > 0, st)) != SAMA_OK) return rc;
-    SAMA_CUDA(ctx, launch_ffn_backward(ctx, s, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down,
-                                       ctx->op_ws, st));
+    SAMA_SETUP(ctx, launch_ffn_backward(ctx, s, x, w_gate, w_up, w_down, gate, up, dy, dx, dw_gate, dw_up, dw_down,
+                                        ctx->op_ws, st));
     return SAMA_OK;
 }
 

@@ -175,3 +175,9 @@ def test_the_feed_forward_block_reserves_what_it_uses(sizes):
         got = [r[0] for r in sizes(["ffn %d %d %d %d %d" % (n, d, f, grad, copies) for grad in (0, 1) for copies in (0, 1)])]
         # up to 16 tokens, the forward pass reads odd operands where they are
         assert got == [hidden, hidden + (x + weights if n > 16 else 0), 3 * hidden, 5 * hidden + 2 * x + weights], n
+
+
+def test_no_memory_for_the_set_up_has_its_own_status(S, sizes):
+    """Error 2 is cudaErrorMemoryAllocation; 1, 719 and 900 are other errors (value, launch, capture)."""
+    assert sizes(["setup %d" % e for e in (2, 1, 719, 900)]) == [
+        [S.SAMA_ERR_NOMEM, 2], [S.SAMA_ERR_CUDA, 1], [S.SAMA_ERR_CUDA, 719], [S.SAMA_ERR_CUDA, 900]]
