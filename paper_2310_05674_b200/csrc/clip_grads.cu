@@ -119,9 +119,10 @@ __device__ __forceinline__ void sum_group(const uint4& x, double* acc, uint32_t&
 }
 
 // This thread's share of a chunk: sum of squares of n elements, THREADS threads, neighbouring threads on neighbouring
-// 16 bytes (or elements, where the tensor starts at an odd address).
+// 16 bytes (or elements, where the tensor starts at an odd address).  (Ordinary loads, not the read-only path: the one-cluster
+// kernel may write the same tensor afterwards.)
 template <typename T, int THREADS>
-__device__ __forceinline__ double chunk_sumsq(const T* __restrict__ p, int n, bool vec, int tid) {
+__device__ __forceinline__ double chunk_sumsq(const T* p, int n, bool vec, int tid) {
     constexpr int PER = kLane / sizeof(T), U = 4;
     double sum = 0.0;
     const int groups = vec ? n / PER : 0;
@@ -133,7 +134,7 @@ __device__ __forceinline__ double chunk_sumsq(const T* __restrict__ p, int n, bo
         for (int i = tid; i < groups; i += U * THREADS) {
             uint4 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = i + u * THREADS < groups ? __ldg(q + i + u * THREADS) : make_uint4(0, 0, 0, 0);
+            for (int u = 0; u < U; ++u) v[u] = i + u * THREADS < groups ? q[i + u * THREADS] : make_uint4(0, 0, 0, 0);
 #pragma unroll
             for (int u = 0; u < U; ++u) sum_group<T>(v[u], acc, any);
         }

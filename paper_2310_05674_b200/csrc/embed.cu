@@ -71,8 +71,8 @@ __device__ __forceinline__ void get_chunk(const T* p, float* v) {
 // `tpr` threads (a power of two) share a row, a thread takes ROWS of them at a time.
 template <typename T, int PW, int CH, int ROWS>
 __global__ void __launch_bounds__(kEmbedThreads)
-embed_kernel(int64_t n_tokens, int64_t vocab, int d, int tpr, const T* __restrict__ table,
-             const int32_t* __restrict__ ids, float scale, T* __restrict__ out, int32_t* status) {
+embed_kernel(int64_t n_tokens, int64_t vocab, int d, int tpr, const T* table,
+             const int32_t* ids, float scale, T* __restrict__ out, int32_t* status) {
     pdl_trigger();
     pdl_wait();
     const int rows = kEmbedThreads / tpr, tx = threadIdx.x & (tpr - 1);
@@ -216,7 +216,7 @@ __device__ void fill_absent_rows(const SortArgs& a, uint8_t* smem, int cta) {
             int4 id[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                id[u] = i + u * kSortThreads < n4 ? __ldg(reinterpret_cast<const int4*>(a.ids) + i + u * kSortThreads) : make_int4(-1, -1, -1, -1);
+                id[u] = i + u * kSortThreads < n4 ? reinterpret_cast<const int4*>(a.ids)[i + u * kSortThreads] : make_int4(-1, -1, -1, -1);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 mark(id[u].x);

@@ -291,19 +291,19 @@ __device__ __forceinline__ void store_rows(uint4* stg, const uint32_t* packed, c
 // Eight consecutive values of a row, zeros beyond `cols`.
 template <typename T>
 __device__ __forceinline__ uint4 load8(const T* p, int col, int cols, bool vec) {
-    if (vec) return __ldg(reinterpret_cast<const uint4*>(p + col));
+    if (vec) return *reinterpret_cast<const uint4*>(p + col);
     const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + col;
     uint32_t r[4];
     if (col + 8 <= cols) {
         if ((reinterpret_cast<uintptr_t>(q) & 2u) == 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r[j] = __ldg(reinterpret_cast<const uint32_t*>(q) + j);
+            for (int j = 0; j < 4; ++j) r[j] = reinterpret_cast<const uint32_t*>(q)[j];
         } else {   // the words around a value at an odd place, within the eight
             uint32_t w[5];
-            w[0] = (uint32_t)__ldg(q) << 16;
+            w[0] = (uint32_t)*q << 16;
 #pragma unroll
-            for (int j = 0; j < 3; ++j) w[j + 1] = __ldg(reinterpret_cast<const uint32_t*>(q + 1) + j);
-            w[4] = __ldg(q + 7);
+            for (int j = 0; j < 3; ++j) w[j + 1] = reinterpret_cast<const uint32_t*>(q + 1)[j];
+            w[4] = q[7];
 #pragma unroll
             for (int j = 0; j < 4; ++j) r[j] = __funnelshift_r(w[j], w[j + 1], 16);
         }
@@ -527,8 +527,8 @@ ffn_kernel(const __grid_constant__ Params<G> P) {
                     const int r = r0 + 4 * (i0 + i);
                     vg[i] = vu[i] = make_uint4(0, 0, 0, 0);
                     if (r < rows && col < q.N) {
-                        vg[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(q.in[0]) + (row0 + r) * q.ldi[0] + col));
-                        vu[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(q.in[1]) + (row0 + r) * q.ldi[1] + col));
+                        vg[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(q.in[0]) + (row0 + r) * q.ldi[0] + col);
+                        vu[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(q.in[1]) + (row0 + r) * q.ldi[1] + col);
                     }
                 }
             };
@@ -767,6 +767,7 @@ struct FewArgs {
     int M, N, K, act;
 };
 
+// (The read-only path: no launch of the block writes weights, and whatever wrote them has ended when gate-up goes on.)
 __device__ __forceinline__ uint4 load_weights(const void* p) {
     uint4 v;
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
@@ -895,7 +896,7 @@ align_rows_kernel(const __grid_constant__ AlignJobs a) {
         uint4 v;
         if (c + 8 <= a.cols[k] && block >= reinterpret_cast<uintptr_t>(a.src[k]) && block + 32 <= a.end[k]) {
             // eight values out of the two aligned 16-byte blocks they lie in, both within the matrix
-            const uint4 x = __ldg(reinterpret_cast<const uint4*>(block)), y = __ldg(reinterpret_cast<const uint4*>(block) + 1);
+            const uint4 x = reinterpret_cast<const uint4*>(block)[0], y = reinterpret_cast<const uint4*>(block)[1];
             uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
             const int shift = (int)(from & 15) >> 1;   // in values
             if (shift & 4)

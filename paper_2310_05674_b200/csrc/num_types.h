@@ -40,7 +40,8 @@ template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t v) {
     return __half22float2(*reinterpret_cast<const __half2*>(&v));
 }
 
-// N consecutive values as fp32 (N = 1, or a multiple of 16 bytes).  KEEP: read-only data that will be read again.
+// N consecutive values as fp32 (N = 1, or a multiple of 16 bytes).  KEEP: data that will be read again.  (Ordinary loads:
+// kernels start while the launch before them may still be writing what they will read, which is no case for the read-only path.)
 template <typename T, int N, bool KEEP = false>
 __device__ __forceinline__ void load_n(const T* p, float* v) {
     if constexpr (N == 1) {
@@ -49,14 +50,14 @@ __device__ __forceinline__ void load_n(const T* p, float* v) {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
             const float4* q = reinterpret_cast<const float4*>(p) + i;
-            const float4 x = KEEP ? __ldg(q) : __ldcs(q);
+            const float4 x = KEEP ? *q : __ldcs(q);
             v[4 * i] = x.x; v[4 * i + 1] = x.y; v[4 * i + 2] = x.z; v[4 * i + 3] = x.w;
         }
     } else {
 #pragma unroll
         for (int i = 0; i < N / 8; ++i) {
             const uint4* q = reinterpret_cast<const uint4*>(p) + i;
-            const uint4 x = KEEP ? __ldg(q) : __ldcs(q);
+            const uint4 x = KEEP ? *q : __ldcs(q);
             const uint32_t r[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

@@ -3,6 +3,7 @@ import ctypes
 import math
 import os
 import random
+import re
 import subprocess
 
 import pytest
@@ -181,3 +182,15 @@ def test_no_memory_for_the_set_up_has_its_own_status(S, sizes):
     """Error 2 is cudaErrorMemoryAllocation; 1, 719 and 900 are other errors (value, launch, capture)."""
     assert sizes(["setup %d" % e for e in (2, 1, 719, 900)]) == [
         [S.SAMA_ERR_NOMEM, 2], [S.SAMA_ERR_CUDA, 1], [S.SAMA_ERR_CUDA, 719], [S.SAMA_ERR_CUDA, 900]]
+
+
+def test_only_weights_are_read_through_the_read_only_path():
+    """A kernel of the text-model operators may start before the launch whose results it reads has ended, and may write
+    what it has read (clipping in place).  Neither goes with loads that promise that the data does not change while the
+    kernel runs: __ldg, ld.global.nc, and pointers to const that are declared to have no alias."""
+    csrc = os.path.join(ROOT, "paper_2310_05674_b200", "csrc")
+    found = {}
+    for f in ("clip_grads.cu", "embed.cu", "gated_ffn.cu", "num_types.h"):
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, f)).read())
+        found[f] = len(re.findall(r"__ldg\b|ld\.global\.nc|const\s+\w+\s*\*\s*__restrict__", text))
+    assert found == {"clip_grads.cu": 0, "embed.cu": 0, "gated_ffn.cu": 1, "num_types.h": 0}   # load_weights
