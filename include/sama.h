@@ -382,6 +382,12 @@ int sama_set_gemm_mode(sama_ctx* ctx, int mode);
  * which is several times slower; this query makes that visible. */
 int sama_last_forward_path(sama_ctx* ctx);
 
+/* How a launch of the gated feed-forward block was last worked on through this context: SAMA_FFN_* + 16 * the number of
+ * parts that the contraction of a tile was cut into (of the last tiles, for pairs), or 0 if there was none yet.  `launch`:
+ * 0 gate-up, 1 down, 2 d-hidden, 3 d-input, 4 d-weights.  The library chooses by the sizes and the device. */
+enum { SAMA_FFN_FEW_TOKENS = 1, SAMA_FFN_SINGLE = 2, SAMA_FFN_PAIRS = 3, SAMA_FFN_CLUSTERS = 4 };
+int sama_last_ffn_path(sama_ctx* ctx, int32_t launch);
+
 /* Number of kernels the library has launched through this context. */
 int64_t sama_launch_count(sama_ctx* ctx);
 

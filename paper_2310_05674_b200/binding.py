@@ -158,6 +158,7 @@ lib.sama_status_string.restype = C.c_char_p
 lib.sama_set_gemm_mode.argtypes = [_vp, C.c_int]
 lib.sama_launch_count.argtypes = [_vp]
 lib.sama_last_forward_path.argtypes = [_vp]
+lib.sama_last_ffn_path.argtypes = [_vp, C.c_int32]
 lib.sama_launch_count.restype = C.c_int64
 lib.sama_profile_enable.argtypes = [_vp, C.c_int32]
 lib.sama_profile_collect.argtypes = [_vp, C.POINTER(sama_kernel_time_t), C.c_int32, C.POINTER(C.c_int32)]
@@ -430,6 +431,15 @@ def sama_launch_count(ctx) -> int:
 
 def sama_last_forward_path(ctx) -> int:
     return int(lib.sama_last_forward_path(ctx))
+
+
+FFN_KERNELS = {1: "few tokens", 2: "single", 3: "pairs", 4: "clusters"}
+
+
+def sama_last_ffn_path(ctx, launch):
+    """("single" | "pairs" | "clusters" | "few tokens", parts of a tile's contraction), or None if there was none yet."""
+    path = int(lib.sama_last_ffn_path(ctx, launch))
+    return (FFN_KERNELS[path % 16], path // 16) if path else None
 
 
 def sama_profile_enable(ctx, on) -> int:

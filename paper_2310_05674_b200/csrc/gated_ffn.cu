@@ -983,6 +983,7 @@ cudaError_t launch_ffn(sama_ctx* ctx, Params<G>& P, int kind, const TilePlan& pl
     P.status = &ctx->scalars->status;
     const int max_units = PAIR ? ctx->ffn_pair_units : ctx->sm_count, items = P.n_items;
     const int units = UNIT == SHARED || items < max_units ? items : max_units;   // (shared: one tile per cluster)
+    ctx->ffn_path[kind] = 16 * plan.split + (PAIR ? SAMA_FFN_PAIRS : UNIT == SHARED ? SAMA_FFN_CLUSTERS : SAMA_FFN_SINGLE);
     KernelScope scope(ctx, SAMA_K_FFN, kind, st);
     return launch_clustered(PAIR ? 2 : UNIT == SHARED ? plan.split : 1, kernel, dim3(units * (PAIR ? 2 : 1)), dim3(THREADS),
                             (size_t)smem_of(MODE, UNIT), st, P);
@@ -1131,6 +1132,7 @@ struct Block {
         const bool wide = a.M > 8;
         auto* kernel = vec ? (wide ? ffn_few_kernel<T, GATE, true, true> : ffn_few_kernel<T, GATE, true, false>)
                            : (wide ? ffn_few_kernel<T, GATE, false, true> : ffn_few_kernel<T, GATE, false, false>);
+        ctx->ffn_path[GATE ? 0 : 1] = 16 + SAMA_FFN_FEW_TOKENS;
         KernelScope scope(ctx, SAMA_K_FFN, GATE ? 0 : 1, st);
         err = launch_dependent(kernel, dim3(blocks_of(a.N, 8)), dim3(32 * kFewWarps), 0, st, a);
     }

@@ -138,6 +138,7 @@ struct sama_ctx {
     int ffn_clusters[3];           // ... and clusters of 2, 4 and 8 CTAs
     float* ffn_parts;              // device: sums of tiles whose contraction several CTAs share
     int* ffn_arrived;              // device: arrival counters of such tiles, zero between launches
+    int ffn_path[5];               // how each of the block's launches was last worked on (sama_last_ffn_path)
     sama::Profiler* prof;          // host
 };
 

@@ -182,4 +182,6 @@ int sama_gated_ffn_grad(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tok
     return SAMA_OK;
 }
 
+int sama_last_ffn_path(sama_ctx* ctx, int32_t launch) { return ctx && launch >= 0 && launch < 5 ? ctx->ffn_path[launch] : 0; }
+
 }  // extern "C"
