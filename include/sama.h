@@ -280,14 +280,19 @@ int sama_embed_grad(sama_ctx* ctx, int32_t dtype, int64_t n_tokens, int64_t voca
  *   G = X Wg^T,   U = X Wu^T,   H = a(G) * U (elementwise),   Y = H Wd^T
  * x, y: [n_tokens][d]; w_gate, w_up: [f][d]; w_down: [d][f], row-major, all of type `dtype` (SAMA_BF16 or SAMA_F16).
  * gate_out, up_out: [n_tokens][f], G and U as the backward pass wants them, or both NULL.  Products are summed in fp32;
- * H is rounded to `dtype` in between.  0 <= n_tokens <= 2^24, 1 <= d, f <= 2^20, any of them odd; 16-byte aligned
+ * H is rounded to `dtype` in between (formed from the sums of G and U, before their own rounding).  0 <= n_tokens <= 2^24, 1 <= d, f <= 2^20, any of them odd; 16-byte aligned
  * operands with d and f multiples of 8 are read in place, others are first copied to the workspace (in the forward pass
  * from 17 tokens on: up to 16 read them in place, too).  Outputs must not overlap the inputs or one another.
  *
  * sama_gated_ffn_grad, given the gradient dy of Y, G and U:
  *   dH = dY Wd,  dG = dH * U * a'(G),  dU = dH * a(G),
  *   dx = dG Wg + dU Wu,  dw_gate = dG^T X,  dw_up = dU^T X,  dw_down = dY^T H
- * each of type `dtype`; an output that is NULL is not computed.  a' of the ReLU at 0 is 0.  With n_tokens = 0 the
+ * each of type `dtype`; an output that is NULL is not computed.  dG, dU and H, operands of the last four products, are
+ * rounded to `dtype`, and H is formed again from G and U as they were stored, so it may differ from the forward pass's in
+ * the last place.  Each of these roundings weighs as much as that of a result: against sums of unrounded values the
+ * gradients' relative error doubles (0.0035 for 0.0017 in bf16, 0.00043 for 0.00021 in fp16).  In SAMA_F16, values of G,
+ * U, H, dG and dU beyond 65504 become infinite, as conversions to fp16 do, and with them the results they enter; below
+ * 2^-14 they lose places, below 2^-25 they vanish.  A loss scaled so that dY is of the order of one avoids both.  a' of the ReLU at 0 is 0.  With n_tokens = 0 the
  * weight gradients are zeros. */
 enum { SAMA_ACT_SILU = 0, SAMA_ACT_GELU = 1, SAMA_ACT_GELU_TANH = 2, SAMA_ACT_RELU = 3 };
 int sama_gated_ffn(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tokens, int32_t d, int32_t f, const void* x,
