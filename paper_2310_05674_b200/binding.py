@@ -95,7 +95,8 @@ class MLP:
 
 class TensorList:
     """Host description of the tensors of one sama_clip_grads call, kept by a program whose gradients stay where they
-    are.  ``outs``: one tensor per input (the input itself: in place; None: counted in the norm only), or None for all
+    are (about 1.5 us per tensor and its output to make, so one whose gradients are new tensors in every step has that to
+    pay each time).  ``outs``: one tensor per input (the input itself: in place; None: counted in the norm only), or None for all
     in place.  Holds references, so the addresses stay valid."""
 
     def __init__(self, ins: Iterable, outs: Optional[Iterable] = None):

@@ -19,10 +19,13 @@
 //                  finish last add them up, in the order of the list.  The first blocks write the zeros still missing.
 // Up to 2048 tokens, where launches and round trips are what counts, one launch: every CTA sorts all tokens for itself in
 // shared memory, then takes its share of the pieces and of the rows to be zeroed (lookup and gradient, 8191 rows of 256
-// fp32 values: 2048 tokens 20 us, 2049 tokens, the other way, 25).
+// fp32 values: 2048 tokens 20 us, 2049 tokens, the other way, 25).  The limit is what a CTA's lists and a thread's four
+// entries hold; the two ways take the same time somewhere above it, where was not looked for.
 //
 // Measured, gradient alone: 16,384 tokens, 50,021 rows of 1024 (bf16 in, fp32 out, 239 MB) 60 us; 131,007 tokens, 65,536
 // rows of 2048 bf16 values (805 MB) 215 us, 3.8 TB/s.  The sort takes 20 to 33 us of it, its length in cluster barriers.
+// The reduction keeps eight rows per thread on their way in registers: 80 of them, three blocks per SM, a third of the warp
+// slots in use (32 %), and 60 to 250 bytes spilled where a thread has more than one value of a row.
 // The lookup moves 5.4 and 6.8 TB/s at these sizes.
 #include <type_traits>
 
@@ -42,7 +45,8 @@ constexpr int kEmbedThreads = 256;
 // what their alignment allows, four at a time.  Against one value at a time (us, lookup / gradient): 24,596 tokens, 638
 // rows of 2394 fp16 values in pairs 38 / 59 (53 / 163), of 2395 in single values 60 / 76 (53 / 163), of 2394 fp32 values
 // 57 / 77 (70 / 164); 131,072 tokens, rows of 33 bf16 values 12 / 59 (21 / 63).  Up to 32 columns the further chunks would
-// all lie beyond the row.
+// all lie beyond the row.  (The lookup of wide odd 16-bit rows is the one that lost, 53 to 60; the boundary is no simple one:
+// 65,536 rows of 101, 401, 641, 1031 and 2395 bf16 values 12.7, 46.5, 58.6, 89, 152 us in four, 19.7, 37.3, 68.2, 81, 133 in one.)
 template <int PW, int CH>
 struct Columns {
     int first, apart, d;

@@ -12,8 +12,10 @@
 //   d-hidden  dH = dY Wd, whose epilogue reads G and U and leaves dG, dU and H (formed again rather than kept)
 //   d-input   dX as one product over the concatenated contraction (dG, dU) x (Wg, Wu)
 //   d-weights the three weight gradients as one launch over the tiles of all three
-// H, dG and dU are rounded to the operands' type between launches, as any operand of a 16-bit product has to be; every
-// sum stays in fp32 until its one rounding on the way out.
+// H, dG and dU are rounded to the operands' type between launches, as any operand of a 16-bit product has to be, and so are
+// G and U where they are kept for the backward pass; every sum stays in fp32 until its one rounding on the way out.  The
+// forward pass forms H from the unrounded sums, the backward pass forms it again from the rounded G and U: a last place of
+// H against writing and reading another matrix of that size.  In fp16, what exceeds 65504 in any of them is infinite.
 //
 // Up to 16 tokens go another way, see ffn_few_kernel.
 //
@@ -30,7 +32,8 @@
 // forward and backward 316, 1310 TFLOP/s; 4096 tokens, 4096 x 8192 1650 to 1950, by the card's temperature); short ones
 // reading tensor memory, 64 bytes per cycle and SM, 2000 cycles for a pair's tile (64 tokens, 4096 x 8192: the weight
 // gradients, 201 MB, 54); few tokens the weights' way from memory and the start and end of two launches (45 tokens, 4096 x
-// 8192: 49, of which the weights' 201 MB at copy speed are 31); small models the launches (1024 tokens, 1024 x 2736: 89).
+// 8192: 49, of which the weights' 201 MB at copy speed are 31); small models the launches (1024 tokens, 1024 x 2736: 89) and
+// the host (128 tokens, 256 x 688: 29 on the device in a graph; the host takes 17 for its five launches and 25 tensor maps).
 #include <type_traits>
 
 #include "num_types.h"
@@ -869,7 +872,7 @@ ffn_few_kernel(const __grid_constant__ FewArgs a) {
 }
 
 // Rows of `cols` values at any address -> rows of `ld` (a multiple of 8) at an aligned one: what TMA can read.  All
-// matrices of a call in one launch.  Memory-bound where it counts (21 tokens, 3148 x 7198: 272 MB read and written, 54 us).
+// matrices of a call in one launch, weights too, in every call of more than 16 tokens and every backward pass.  Memory-bound where it counts (21 tokens, 3148 x 7198: 272 MB read and written, 54 us).
 struct AlignJobs {
     static constexpr int kMost = 7;
     const void* src[kMost];
