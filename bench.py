@@ -115,7 +115,7 @@ def source_hash(*names):
 
 KERNEL_SOURCES = {"fused_sweep": ("adapt_perturb.cu",), "adapt_sumsq": ("adapt_perturb.cu",), "perturb": ("adapt_perturb.cu",), "sumsq": ("adapt_perturb.cu",),
                   "perturb_split": ("adapt_perturb.cu",), "head_ce_fd": ("head_ce_fd.cu",),
-                  "gemm_ffma": ("gemm_ffma.cu",), "ce_fd": ("ce_fd.cu",), "gemm_tf32x3": ("gemm_tf32x3.cu",),
+                  "gemm_ffma": ("gemm_ffma.cu",), "ce_fd": ("ce_fd.cu",), "gemm_tf32x3": ("gemm_tf32x3.cu", "tc_ptx.h"),
                   "split_tf32": ("gemm_tf32x3.cu",)}
 
 
