@@ -256,8 +256,8 @@ int sama_biasreg_step(sama_ctx* ctx, int32_t d, int32_t n_val, const float* Xv, 
  * grow, except that the feed-forward block needs more where it has to copy operands (see there).  A stream capture
  * must therefore be preceded by a call of the same operator of at least its sizes, with operands to copy if the
  * captured one has them (a captured call that would have to allocate returns SAMA_ERR_NOMEM, launches nothing and
- * leaves the capture as it is); and a captured graph must not be replayed after the workspace has grown, which a call of no
- * larger sizes, and with no new need of copies, does not do. */
+ * leaves the capture as it is); and a captured graph must not be replayed after the workspace has grown.  A call of
+ * sizes that its operator has had before, or smaller ones, with no new need of copies, does not make it grow. */
 typedef enum sama_dtype { SAMA_F32 = 0, SAMA_BF16 = 1, SAMA_F16 = 2 } sama_dtype;
 
 /* Token embedding: out[t][:] = scale * table[ids[t]][:], computed in fp32 and rounded once.
