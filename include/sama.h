@@ -60,7 +60,8 @@ typedef enum sama_status {
 enum {
     SAMA_DEV_DEGENERATE_NORM = 1, /* ||p|| was 0 or not finite: eps_fd = 0, theta+- = theta, metagrad = 0 */
     SAMA_DEV_BAD_LABEL = 2,       /* a label outside [0, d_L): that sample's metagrad is 0 */
-    SAMA_DEV_BAD_INDEX = 8,       /* a token id outside [0, vocab): its output row is 0, it adds to no gradient */
+    SAMA_DEV_BAD_INDEX = 8,       /* a token id outside [0, vocab): its output row is 0, it adds to no gradient.  A start,
+                                     length or page out of range, see the operator */
     SAMA_DEV_NONFINITE_GRAD = 16, /* the norm of sama_clip_grads was not finite: every output is 0 */
     SAMA_DEV_TIMEOUT = 4          /* a bounded wait inside a kernel expired; outputs of that call are invalid, and the
                                      context's arrival counters may be left non-zero: destroy and recreate it */
@@ -323,6 +324,49 @@ typedef struct sama_tensor_t {
 int sama_clip_grads(sama_ctx* ctx, const sama_tensor_t* tensors, int32_t n_tensors, float max_norm, float* norm_out,
                     void* stream);
 
+/* ---- Attention ------------------------------------------------------------------------------------------------
+ * Scores of a query against a key, for head h and key head g = h / (heads / kv_heads):
+ *   x = scale * (q . k);   if cap > 0: x = cap * tanh(x / cap);   if slopes: x = x - slopes[h] * |pos_q - pos_k|
+ *   out = sum over the keys that the query sees of softmax(x) * v
+ * (the softmax and every sum in fp32; the weights, operands of the second product, are rounded to `dtype`).
+ *
+ * Texts lie packed behind one another: text t has the queries q_starts[t] .. q_starts[t+1] - 1 and the keys
+ * k_starts[t] .. k_starts[t+1] - 1, and its queries see its own keys only.  The last query has the position of the last
+ * key: with Lq queries and Lk keys, query i of a text is at position i + Lk - Lq, key j at j (so a prompt's next chunk is
+ * the case Lk > Lq).  causal: a query sees the keys up to its position, and those before prefix[t] (NULL: none).
+ * A query that sees no key has out = 0, lse = -infinity and no gradient.  Rows of no text (before the first start, from
+ * the last on) are neither read for any text nor written, and no value of one text, finite or not, reaches another's.
+ * Within a text a v that is not finite may reach queries that do not see it (as 0 * infinity does). */
+typedef struct sama_attn_t {
+    int32_t dtype;                       /* SAMA_BF16 or SAMA_F16: q, k, v, out and their gradients */
+    int32_t heads, kv_heads, head_dim;   /* kv_heads divides heads; head_dim a multiple of 8, 8 .. 128 */
+    int64_t n_q, n_k;                    /* rows of q and of k, v; 0 .. 2^30 */
+    int32_t n_texts;                     /* 0 .. 2^20 */
+    int32_t causal;                      /* 0: a query sees all keys of its text */
+    const int32_t* q_starts;             /* device [n_texts + 1], not falling, within 0 .. n_q (others: SAMA_DEV_BAD_INDEX) */
+    const int32_t* k_starts;             /* the same for keys, or NULL: the queries' (n_k == n_q) */
+    const int32_t* prefix;               /* device [n_texts], or NULL; without effect unless causal */
+    const float* slopes;                 /* device [heads], or NULL */
+    float scale, cap;                    /* scale > 0; cap 0: no cap */
+    int64_t q_stride, k_stride, v_stride; /* elements from a row to the next, multiples of 8; 0: heads (kv_heads) * head_dim */
+} sama_attn_t;
+
+/* q: row r, head h at q + r * q_stride + h * head_dim, likewise k and v with kv_heads: three parts of one projection's
+ * output may be passed as they lie.  out: [n_q][heads][head_dim].  lse_out: fp32 [heads][n_q], the logarithm of the sum
+ * of exp(x) as sama_attention_grad wants it, or NULL.  All 16-byte aligned (lse: 4).  Outputs must not overlap inputs.
+ *
+ * sama_attention_grad, given out, lse and the gradient d_out of out: dq, dk, dv, laid out as q, k, v (with their strides;
+ * the gaps between rows are left alone, so they may be parts of one buffer, too), of type `dtype`, each required:
+ *   dP = d_out . v,  dX = softmax * (dP - d_out . out) * (1 - tanh^2),  dq = scale * dX k,  dk = scale * dX^T q,
+ *   dv = softmax^T d_out
+ * dk and dv are summed over the heads that share them.  Sums are fp32, in a fixed order (bitwise reproducible); dX and the
+ * softmax are rounded to `dtype` as operands of the last products.  slopes get no gradient.  Uses 8 * heads * n_q bytes of
+ * the workspace. */
+int sama_attention(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, void* out,
+                   float* lse_out, void* stream);
+int sama_attention_grad(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, const void* out,
+                        const float* lse, const void* d_out, void* dq, void* dk, void* dv, void* stream);
+
 /* sama_step (Fig. 2) for callers whose data lives in HOST memory: every
  * pointer below is a host pointer (pinned memory makes the copies
  * asynchronous).  Copies the inputs to staging buffers owned by the context
@@ -420,7 +464,8 @@ enum {
     SAMA_K_EMBED = 15,        /* token embedding */
     SAMA_K_EMBED_GRAD = 16,   /* its gradient: sort, sums, joins */
     SAMA_K_CLIP = 17,         /* global gradient norm and clipping */
-    SAMA_K_FFN = 18           /* gated feed-forward block; layer: 0 gate-up, 1 down, 2 d-hidden, 3 d-input, 4 d-weights */
+    SAMA_K_FFN = 18,          /* gated feed-forward block; layer: 0 gate-up, 1 down, 2 d-hidden, 3 d-input, 4 d-weights */
+    SAMA_K_ATTN = 19          /* attention; layer: 0 forward, 1 d-queries, 2 d-keys and d-values */
 };
 typedef struct sama_kernel_time_t {
     int32_t kind;     /* SAMA_K_* */

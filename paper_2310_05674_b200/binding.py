@@ -54,7 +54,7 @@ class sama_kernel_time_t(C.Structure):
 KERNEL_KINDS = {0: "adapt_sumsq", 1: "sumsq", 2: "perturb", 3: "gemm_ffma", 4: "ce_fd", 5: "split_tf32",
                 6: "gemm_tf32x3", 7: "head_ce_fd", 8: "perturb_split", 9: "meta_gemm", 10: "meta_aux",
                 11: "reweight_fd", 12: "biasreg_grad", 13: "biasreg_fd", 14: "fused_sweep", 15: "embed",
-                16: "embed_grad", 17: "clip", 18: "ffn"}
+                16: "embed_grad", 17: "clip", 18: "ffn", 19: "attn"}
 
 
 class sama_mlp_t(C.Structure):
@@ -116,6 +116,56 @@ class TensorList:
         return self._arr
 
 
+class sama_attn_t(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("n_q", C.c_int64), ("n_k", C.c_int64), ("n_texts", C.c_int32), ("causal", C.c_int32),
+                ("q_starts", C.c_void_p), ("k_starts", C.c_void_p), ("prefix", C.c_void_p), ("slopes", C.c_void_p),
+                ("scale", C.c_float), ("cap", C.c_float),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
+class Attn:
+    """Host description of packed texts for sama_attention and its gradient, kept by a program that runs several layers
+    or steps on them.  ``q_starts``, ``k_starts``, ``prefix`` (int32) and ``slopes`` (fp32) are tensors on the GPU, whose
+    values may change between calls; the number of texts is that of ``q_starts`` less one.  Holds references to them."""
+
+    def __init__(self, dtype, heads, kv_heads, head_dim, n_q, n_k, q_starts, k_starts=None, causal=False, prefix=None,
+                 slopes=None, scale=None, cap=0.0, q_stride=0, k_stride=0, v_stride=0):
+        w = "Attn"
+        self.device = q_starts.get_device()
+        texts = q_starts.numel() - 1
+        if texts < 0:
+            raise SamaError(SAMA_ERR_SIZE, w)
+        self.held = (q_starts, k_starts, prefix, slopes)
+        self.a = sama_attn_t(dtype, heads, kv_heads, head_dim, n_q, n_k, texts, int(causal),
+                             _dense(self.device, q_starts, "i32", 0, w), _dense(self.device, k_starts, "i32", texts + 1, w),
+                             _dense(self.device, prefix, "i32", texts, w), _dense(self.device, slopes, SAMA_F32, heads, w),
+                             head_dim ** -0.5 if scale is None else scale, cap, q_stride, k_stride, v_stride)
+        self._ref = C.byref(self.a)
+        # (heads, rows, elements from row to row) of q, k and v
+        self.q = (heads, n_q, q_stride or heads * head_dim)
+        self.k = (kv_heads, n_k, k_stride or kv_heads * head_dim)
+        self.v = (kv_heads, n_k, v_stride or kv_heads * head_dim)
+
+    def rows(self, x, shape, where):
+        """Address of an operand [rows][heads][head_dim] whose rows may lie apart."""
+        if x is None or isinstance(x, int):
+            return x
+        a, (heads, n, stride) = self.a, shape
+        if x.get_device() != self.device:
+            raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is on %s, not on the texts' GPU" % (where, x.device))
+        if not _torch_dtypes:
+            _fill_dtypes()
+        if x.dtype is not _torch_dtypes.get(a.dtype):
+            raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is not of the type the call names" % where)
+        if x.dim() != 3 or x.shape[0] < n or x.shape[1] != heads or x.shape[2] != a.head_dim:
+            raise SamaError(SAMA_ERR_SIZE, where)
+        s = x.stride()
+        if (x.shape[0] > 1 and s[0] != stride) or (heads > 1 and s[1] != a.head_dim) or s[2] != 1:
+            raise SamaError(SAMA_ERR_PARAM, "%s: a tensor's strides are not the described ones" % where)
+        return x.data_ptr()
+
+
 _vp = C.c_void_p
 lib.sama_create.argtypes = [C.POINTER(_vp), C.c_int, C.c_int64, C.c_int32, C.POINTER(sama_mlp_t)]
 lib.sama_destroy.argtypes = [_vp]
@@ -145,6 +195,8 @@ lib.sama_embed_grad.argtypes = [_vp, C.c_int32, C.c_int64, C.c_int64, C.c_int32,
 lib.sama_gated_ffn.argtypes = [_vp, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int32] + [_vp] * 8
 lib.sama_gated_ffn_grad.argtypes = [_vp, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int32] + [_vp] * 12
 lib.sama_clip_grads.argtypes = [_vp, C.POINTER(sama_tensor_t), C.c_int32, C.c_float, _vp, _vp]
+lib.sama_attention.argtypes = [_vp, C.POINTER(sama_attn_t)] + [_vp] * 6
+lib.sama_attention_grad.argtypes = [_vp, C.POINTER(sama_attn_t)] + [_vp] * 10
 lib.sama_ctx_sumsq.argtypes = [_vp]
 lib.sama_ctx_sumsq.restype = _vp
 lib.sama_ctx_eps_fd.argtypes = [_vp]
@@ -386,6 +438,30 @@ def sama_clip_grads(ctx, tensors: TensorList, max_norm, norm_out=None, stream=No
         raise SamaError(SAMA_ERR_PARAM, "%s: the tensors are not on the context's GPU" % w)
     return _check(lib.sama_clip_grads(ctx, tensors.c(), len(tensors.ins), max_norm, _dense(v, norm_out, SAMA_F32, 1, w),
                                       _stream(stream)), w)
+
+
+def _on_device(ctx, at, where):
+    v = _device_of.get(ctx)
+    if v is not None and at != v:
+        raise SamaError(SAMA_ERR_PARAM, "%s: the tensors are not on the context's GPU" % where)
+
+
+def sama_attention(ctx, attn: Attn, q, k, v, out, lse_out=None, stream=None) -> int:
+    w, a = "sama_attention", attn.a
+    _on_device(ctx, attn.device, w)
+    return _check(lib.sama_attention(ctx, attn._ref, attn.rows(q, attn.q, w), attn.rows(k, attn.k, w), attn.rows(v, attn.v, w),
+                                     _dense(attn.device, out, a.dtype, a.n_q * a.heads * a.head_dim, w),
+                                     _dense(attn.device, lse_out, SAMA_F32, a.heads * a.n_q, w), _stream(stream)), w)
+
+
+def sama_attention_grad(ctx, attn: Attn, q, k, v, out, lse, d_out, dq, dk, dv, stream=None) -> int:
+    w, a = "sama_attention_grad", attn.a
+    _on_device(ctx, attn.device, w)
+    n = a.n_q * a.heads * a.head_dim
+    return _check(lib.sama_attention_grad(ctx, attn._ref, attn.rows(q, attn.q, w), attn.rows(k, attn.k, w), attn.rows(v, attn.v, w),
+                                          _dense(attn.device, out, a.dtype, n, w), _dense(attn.device, lse, SAMA_F32, a.heads * a.n_q, w),
+                                          _dense(attn.device, d_out, a.dtype, n, w), attn.rows(dq, attn.q, w),
+                                          attn.rows(dk, attn.k, w), attn.rows(dv, attn.v, w), _stream(stream)), w)
 
 
 def sama_step_host(ctx, mlp: MLP, n, theta_host, m_host, s_host, g_base_host, g_meta_host, adam: Adam, alpha,

@@ -54,4 +54,22 @@ inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
     return x < y + nb && y < x + na;
 }
 
+// The operators' workspace, at least `bytes` large.  Growing it waits for the work that may still use the old one.
+// `ready`: the operator's kernels are set up; the first call does that, and allocates for it.  Neither is possible while
+// the stream is being captured, and trying would break the capture: the call is refused before.
+inline int need_workspace(sama_ctx* ctx, size_t bytes, bool ready, cudaStream_t st) {
+    if (ready && ctx->op_ws_bytes >= bytes) return SAMA_OK;
+    cudaStreamCaptureStatus capture;
+    SAMA_CUDA(ctx, cudaStreamIsCapturing(st, &capture));
+    if (capture != cudaStreamCaptureStatusNone) return SAMA_ERR_NOMEM;
+    if (ctx->op_ws_bytes >= bytes) return SAMA_OK;
+    SAMA_CUDA(ctx, cudaStreamSynchronize(st));
+    cudaFree(ctx->op_ws);
+    ctx->op_ws = nullptr;
+    ctx->op_ws_bytes = 0;
+    if (cudaMalloc(&ctx->op_ws, bytes) != cudaSuccess) { cudaGetLastError(); return SAMA_ERR_NOMEM; }
+    ctx->op_ws_bytes = bytes;
+    return SAMA_OK;
+}
+
 }  // namespace sama

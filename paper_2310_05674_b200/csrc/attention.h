@@ -1,0 +1,148 @@
+// What the attention kernels share: the packed texts, how a block finds its own, what a query sees, and the scores.
+#pragma once
+#include "num_types.h"
+#include "sama_internal.h"
+#include "tc_ptx.h"
+
+namespace sama {
+
+constexpr int kAttnRows = 128;   // rows of a score tile: the lanes of tensor memory
+
+struct AttnShape {
+    const int32_t *q_starts, *k_starts, *prefix;
+    const float* slopes;
+    int32_t* status;
+    int n_texts, n_q, n_k, heads, kv_heads, group, dim, causal;   // group: heads per key head
+    float scale, cap;
+};
+
+struct AttnText {
+    int q0, lq, k0, lk, prefix;   // first row and number of queries and keys; prefix: keys that every query sees
+};
+
+struct AttnOperands {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    int dtype;
+};
+// attention_fwd.cu, attention_bwd.cu
+cudaError_t launch_attention(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, void* out, float* lse, cudaStream_t st);
+size_t attention_grad_workspace(const AttnShape& a);
+cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, const void* out, const float* lse,
+                                  const void* dout, void* dq, void* dk, void* dv, void* ws, cudaStream_t st);
+
+#ifdef __CUDACC__
+
+__device__ __forceinline__ int attn_start(const int32_t* starts, int i, int n) { return min(max(starts[i], 0), n); }
+
+// Tiles of TILE rows are counted so that a text's first is number starts[t] / TILE + t: texts leave gaps of at most one
+// tile, there are n / TILE + n_texts numbers in all, and a block finds the text of its number by search, without a pass
+// over the texts before it.  All lanes of a warp probe at a time.  Returns the text, or -1; `tile`: number within it.
+template <int TILE>
+__device__ __forceinline__ int attn_find(const int32_t* starts, int n_texts, int n, int slot, int* tile) {
+    const int lane = threadIdx.x & 31;
+    if (attn_start(starts, 0, n) / TILE > slot) return -1;
+    int lo = 0, hi = n_texts;
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 31) / 32, t = lo + lane * step;
+        const bool before = t < hi && attn_start(starts, t, n) / TILE + t <= slot;
+        const int last = 31 - __clz(__ballot_sync(0xffffffffu, before) | 1u);
+        lo += last * step;
+        hi = min(hi, lo + step);
+    }
+    *tile = slot - (attn_start(starts, lo, n) / TILE + lo);
+    return lo;
+}
+// Starts that fall or lie outside are clamped, here and wherever they are used, and reported.
+__device__ __forceinline__ AttnText attn_text(const AttnShape& a, int t) {
+    AttnText x;
+    x.q0 = attn_start(a.q_starts, t, a.n_q);
+    x.lq = max(attn_start(a.q_starts, t + 1, a.n_q) - x.q0, 0);
+    x.k0 = attn_start(a.k_starts, t, a.n_k);
+    x.lk = max(attn_start(a.k_starts, t + 1, a.n_k) - x.k0, 0);
+    x.prefix = a.prefix ? min(max(a.prefix[t], 0), x.lk) : 0;
+    return x;
+}
+__device__ __forceinline__ void attn_check_starts(const AttnShape& a) {
+    bool bad = false;
+    for (int i = threadIdx.x; i <= a.n_texts; i += blockDim.x) {
+        const int q = a.q_starts[i], k = a.k_starts[i];
+        bad |= q < 0 || q > a.n_q || k < 0 || k > a.n_k || (i > 0 && (a.q_starts[i - 1] > q || a.k_starts[i - 1] > k));
+    }
+    if (bad) atomicOr(a.status, (int)SAMA_DEV_BAD_INDEX);
+}
+// Query i sees keys 0 .. result - 1: more of them, never fewer, as i grows.
+__device__ __forceinline__ int attn_seen(const AttnShape& a, const AttnText& x, int i) {
+    return a.causal ? min(max(max(x.prefix, i + x.lk - x.lq + 1), 0), x.lk) : x.lk;
+}
+// Key j is seen by queries result .. lq - 1.
+__device__ __forceinline__ int attn_first_query(const AttnShape& a, const AttnText& x, int j) {
+    return !a.causal || j < x.prefix ? 0 : max(0, j - (x.lk - x.lq));
+}
+
+// tanh(z) = 1 - 2 / (1 + exp 2z): an absolute error of two units in the last place of 1, which is what a capped score
+// needs (the hardware's own approximation has 2^-11, a hundredth of a weight at a cap of 30).
+__device__ __forceinline__ float attn_tanh(float z) { return fmaf(-2.f, fast_rcp(1.f + fast_exp2(2.f * kLog2e * z)), 1.f); }
+
+// D (fp32) += A B^T with A, 128 rows of 16-bit values two to a column, in tensor memory.
+__device__ __forceinline__ void umma16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// As make_desc, for a tile whose rows run along the contraction (MN-major): 64 values of N per row of 128 bytes, 8 rows to
+// a swizzle block, the next 64 values of N `rows` rows further on.
+__device__ __forceinline__ uint64_t attn_desc_mn(uint32_t saddr, int rows) {
+    return (uint64_t)((saddr & 0x3FFFF) >> 4) | ((uint64_t)((rows * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+// 32 accumulator columns of this warp's 32 rows; tmem_wait_ld has to follow.
+__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, float* v) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 16 columns of this warp's 32 rows, to tensor memory; tmem_wait_st has to follow.
+__device__ __forceinline__ void tmem_st16_nowait(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr));
+}
+// Rows [from, rows) of a tile of COLS 64-column blocks become zeros: rows of another text, whose values must not meet
+// weights of 0 in a product.
+template <int COLS>
+__device__ __forceinline__ void attn_zero_rows(uint32_t tile, int from, int rows) {
+    const int n = (rows - from) * 8;   // 16-byte chunks of a block
+    for (int i = threadIdx.x & 31; i < n * COLS; i += 32) {
+        const int block = i / n, at = i - block * n;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + (uint32_t)(block * rows + from) * 128u + 16u * at), "r"(0) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+
+#endif  // __CUDACC__
+
+// Tensor map of [n][heads][dim] with rows `stride` elements apart: boxes of `rows` rows of one head's 64 columns.
+inline bool attn_map(CUtensorMap* map, const void* p, int dtype, int dim, int heads, int64_t n, int64_t stride, int rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)n};
+    const cuuint64_t strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, 1, (cuuint32_t)rows}, step[3] = {1, 1, 1};
+    return fn(map, dtype == SAMA_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(p),
+              dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace sama

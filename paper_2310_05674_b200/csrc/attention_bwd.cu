@@ -1,0 +1,387 @@
+// Attention over packed texts, backward, on the 5th-generation tensor cores:
+//   P = 2^(x log2 e - lse),  dP = dO V^T,  dX = P (dP - delta) (1 - tanh^2),  delta = dO . O
+//   dQ = scale dX K,   dK = scale dX^T Q,   dV = P^T dO
+//
+// Two launches of one kernel template.  Each CTA keeps 128 rows of two operands and streams tiles of 64 rows of the other
+// two past them: d-queries keeps (Q, dO) and streams (K, V); d-keys keeps (K, V) of a key head and streams (Q, dO) of every
+// head that shares it.  The products are formed with the kept rows as the lanes of tensor memory (S^T rather than S for
+// the keys), so that P and dX go back to tensor memory as the left operands of the last products and no tile is
+// transposed.  The sums of a row stay in one accumulator from its first tile to its last: no atomics, a fixed order.
+// Forming S and dP in both launches costs seven products in place of the five of one launch that adds to dQ in memory.
+//
+// Roles of the 10 warps: warp 0 copies, warp 1 issues products, warps 2..5 and 6..9 take the streamed tiles in turn, so
+// that the products of one tile run while the other's weights are formed.  Every wait is bounded.
+#include <type_traits>
+
+#include "attention.h"
+
+namespace sama {
+
+namespace {
+
+constexpr int THREADS = 320;
+constexpr int BT = 64;   // rows of a streamed tile
+
+template <int D> struct BwdTile {
+    static constexpr int STAGES = D == 64 ? 6 : 4;
+    static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2, STAGE = 2 * TILE;
+    static constexpr int STATS = BT * 8;      // (lse, delta) of a streamed tile's queries
+    static constexpr int SMEM = 2 * KEPT + STAGES * (STAGE + STATS) + 2 * kAttnRows * 4 + 256 + 1024;
+};
+
+struct alignas(64) BwdParams {
+    CUtensorMap kept[2], streamed[2];   // (Q, dO) and (K, V), or the other way round
+    AttnShape a;
+    const void *out, *dout;
+    const float* lse;
+    float2* stats;      // [heads][n_q]: lse log2 e (infinity for a query that sees nothing) and delta
+    void* grad[2];      // dQ, or dK and dV
+    int64_t ld[2];
+    int slots;
+};
+
+template <typename T, int D, bool CAP, bool BIAS, bool KEYS>
+__global__ void __launch_bounds__(THREADS, 1)
+attn_bwd_kernel(const __grid_constant__ BwdParams P) {
+    using C = BwdTile<D>;
+    constexpr int STAGES = C::STAGES;
+    constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr uint32_t IDESC_S = idesc16(BF16, false, false, kAttnRows, BT), IDESC_G = idesc16(BF16, false, true, kAttnRows, D);
+    constexpr uint32_t COLS = 512;
+    const AttnShape& a = P.a;
+
+    pdl_trigger();
+    pdl_wait();
+    if (!KEYS && blockIdx.x == 0) attn_check_starts(a);
+    // heavy tiles first: the first keys are seen by most queries, the last queries see most keys
+    const int per_slot = KEYS ? a.kv_heads : a.heads, head0 = (int)blockIdx.x % per_slot;
+    const int slot = KEYS ? (int)blockIdx.x / per_slot : P.slots - 1 - (int)blockIdx.x / per_slot;
+    int tile;
+    const int t = attn_find<kAttnRows>(KEYS ? a.k_starts : a.q_starts, a.n_texts, KEYS ? a.n_k : a.n_q, slot, &tile);
+    if (t < 0) return;
+    const AttnText x = attn_text(a, t);
+    const int first = tile * kAttnRows, kept_rows = KEYS ? x.lk : x.lq, streamed_rows = KEYS ? x.lq : x.lk;
+    if (first >= kept_rows) return;
+    const int kept_base = KEYS ? x.k0 : x.q0, streamed_base = KEYS ? x.q0 : x.k0;
+
+    // streamed tiles: those that the last query sees, or from the first that sees the first key on, for each head
+    int tile0 = 0, per_head;
+    if (KEYS) {
+        tile0 = attn_first_query(a, x, first) / BT;
+        per_head = max(0, (x.lq + BT - 1) / BT - tile0);
+    } else {
+        per_head = (attn_seen(a, x, min(first + kAttnRows, x.lq) - 1) + BT - 1) / BT;
+    }
+    const int n = per_head * (KEYS ? a.group : 1);
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    const uint32_t ring = base + 2 * C::KEPT, stats = ring + STAGES * C::STAGE, halves = stats + STAGES * C::STATS;
+    const uint32_t bars = halves + 2 * kAttnRows * 4;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
+    auto s_bar = [&](int w) { return bars + 8u * (2 * STAGES + w); };       // S and dP are there
+    auto p_bar = [&](int w) { return bars + 8u * (2 * STAGES + 2 + w); };   // P and dX are there
+    const uint32_t kept_bar = bars + 8u * (2 * STAGES + 4), done_bar = kept_bar + 8u;
+    const uint32_t tmem_slot = done_bar + 8u;
+    volatile uint32_t* tmem_ptr_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_slot - raw));
+    volatile uint32_t* abort_flag = tmem_ptr_slot + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(full_bar(s), KEYS ? 33 : 1);   // the copies, and (d-keys) each lane's share of the statistics
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(s_bar(w), 1);
+            mbar_init(p_bar(w), 4);
+        }
+        mbar_init(kept_bar, 1);
+        mbar_init(done_bar, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(tmem_slot, COLS);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_ptr_slot;
+    auto s_cols = [&](int w) { return tmem + (uint32_t)(w * BT); };
+    auto dp_cols = [&](int w) { return tmem + (uint32_t)(2 * BT + w * BT); };
+    auto g_cols = [&](int i) { return tmem + (uint32_t)(4 * BT + i * D); };
+
+    auto raise_timeout = [&]() {
+        *abort_flag = 1;
+        atomicOr(a.status, (int)SAMA_DEV_TIMEOUT);
+    };
+    // for all lanes of a warp together
+    auto wait = [&](uint32_t bar, int parity) {
+        const bool ok = mbar_wait(bar, (uint32_t)parity, abort_flag);
+        if (__all_sync(0xffffffffu, ok)) return true;
+        raise_timeout();
+        return false;
+    };
+
+    if (warp == 0) {
+        int i = 0;
+        bool ok = true;
+        if (n > 0 && lane == 0) {
+            mbar_expect_tx(kept_bar, 2 * C::KEPT);
+            for (int o = 0; o < 2; ++o)
+                for (int c = 0; c < D / 64; ++c)
+                    tma_load_3d(base + o * C::KEPT + c * kAttnRows * 128, &P.kept[o], kept_bar, 64 * c, head0, kept_base + first);
+        }
+        for (; i < n; ++i) {
+            const int s = i % STAGES;
+            if (i >= STAGES && !wait(empty_bar(s), (i / STAGES - 1) & 1)) { ok = false; break; }
+            const int h = KEYS ? head0 * a.group + i / per_head : head0 / a.group;
+            const int row = streamed_base + (tile0 + (KEYS ? i % per_head : i)) * BT;
+            if (lane == 0) {
+                mbar_expect_tx(full_bar(s), C::STAGE);
+                for (int o = 0; o < 2; ++o)
+                    for (int c = 0; c < D / 64; ++c)
+                        tma_load_3d(ring + s * C::STAGE + o * C::TILE + c * BT * 128, &P.streamed[o], full_bar(s), 64 * c, h, row);
+            }
+            if (KEYS) {
+                for (int r = lane; r < BT; r += 32)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(stats + s * C::STATS + 8 * r),
+                                 "l"(P.stats + (int64_t)h * a.n_q + min(row + r, a.n_q - 1)) : "memory");
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full_bar(s)) : "memory");
+            }
+        }
+        if (!ok || *abort_flag) {
+            // let the copies already issued land before the CTA's shared memory goes away
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (n > 0) mbar_wait(kept_bar, 0);
+            for (int k = max(0, i - STAGES); k < i; ++k) mbar_wait(full_bar(k % STAGES), (k / STAGES) & 1);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        bool ok = true;
+        auto products = [&](int i) {   // S = kept[0] streamed[0]^T, dP = kept[1] streamed[1]^T
+            const int s = i % STAGES, w = i & 1;
+            if (!(ok = wait(full_bar(s), (i / STAGES) & 1))) return;
+            tc_fence_after();
+            const int from = streamed_rows - (tile0 + (KEYS ? i % per_head : i)) * BT;
+            if (from < BT) {
+                attn_zero_rows<D / 64>(ring + s * C::STAGE, from, BT);
+                attn_zero_rows<D / 64>(ring + s * C::STAGE + C::TILE, from, BT);
+            }
+            if (lane == 0) {
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    const uint64_t da = make_desc(base + o * C::KEPT), db = make_desc(ring + s * C::STAGE + o * C::TILE);
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        umma16(o ? dp_cols(w) : s_cols(w), da + (uint64_t)((k / 4 * kAttnRows * 128 + k % 4 * 32) >> 4),
+                               db + (uint64_t)((k / 4 * BT * 128 + k % 4 * 32) >> 4), IDESC_S, k > 0);
+                }
+                umma_commit(s_bar(w));
+            }
+            __syncwarp();
+        };
+        if (n > 0) ok = wait(kept_bar, 0);
+        for (int i = 0; ok && i < 2 && i < n; ++i) products(i);
+        for (int i = 0; ok && i < n; ++i) {
+            const int s = i % STAGES, w = i & 1;
+            if (!(ok = wait(p_bar(w), (i >> 1) & 1))) break;
+            tc_fence_after();
+            if (lane == 0) {
+                const uint64_t d0 = attn_desc_mn(ring + s * C::STAGE, BT), d1 = attn_desc_mn(ring + s * C::STAGE + C::TILE, BT);
+#pragma unroll
+                for (int k = 0; k < BT / 16; ++k) {
+                    umma16_ta(g_cols(0), dp_cols(w) + 8u * k, d0 + (uint64_t)(k * 2048 >> 4), IDESC_G, i > 0 || k > 0);
+                    if (KEYS) umma16_ta(g_cols(1), s_cols(w) + 8u * k, d1 + (uint64_t)(k * 2048 >> 4), IDESC_G, i > 0 || k > 0);
+                }
+                if (i + STAGES < n) umma_commit(empty_bar(s));
+                if (i + 1 == n) umma_commit(done_bar);
+            }
+            __syncwarp();
+            // (products are executed in order: the next scores do not overtake the weights they replace)
+            if (i + 2 < n) products(i + 2);
+        }
+    } else {
+        const int w = (warp - 2) >> 2, quarter = warp & 3;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const int row0 = first + quarter * 32, row = row0 + lane;   // in the text
+        const bool real = row < kept_rows;
+        constexpr bool RAW = !CAP && !BIAS;
+        const float c = RAW ? a.scale * kLog2e : 1.f;
+        const float inv_cap = CAP ? a.scale / a.cap : 0.f, cap2 = CAP ? a.cap * kLog2e : 0.f;
+        bool ok = true;
+
+        float lse2 = 0.f, delta = 0.f;
+        if (!KEYS) {
+            // the two warps that share these rows add up half of the columns each
+            volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (halves - raw));
+            float sum = 0.f;
+            if (real) {
+                const int64_t at = ((int64_t)(x.q0 + row) * a.heads + head0) * a.dim;
+                const T *o = static_cast<const T*>(P.out) + at, *d = static_cast<const T*>(P.dout) + at;
+#pragma unroll
+                for (int k = 0; k < D / 2; k += 8) {
+                    const int col = w * (D / 2) + k;
+                    if (col < a.dim) {
+                        float u[8], v[8];
+                        load_n<T, 8, true>(o + col, u);
+                        load_n<T, 8, true>(d + col, v);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum = fmaf(u[e], v[e], sum);
+                    }
+                }
+                lse2 = P.lse[(int64_t)head0 * a.n_q + x.q0 + row] * kLog2e;
+                if (lse2 == -INFINITY) lse2 = INFINITY;
+            }
+            part[w * kAttnRows + quarter * 32 + lane] = sum;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            delta = part[quarter * 32 + lane] + part[kAttnRows + quarter * 32 + lane];
+            if (w == 0 && real) P.stats[(int64_t)head0 * a.n_q + x.q0 + row] = make_float2(lse2, delta);
+        }
+        // d-queries: the row sees keys below `edge`; d-keys: the row is seen by queries from `edge` on
+        const int edge = KEYS ? attn_first_query(a, x, row) : attn_seen(a, x, row);
+        const int edge_of_all = KEYS ? attn_first_query(a, x, row0 + 31) : attn_seen(a, x, row0);
+
+        for (int i = w; i < n; i += 2) {
+            const int at = (tile0 + (KEYS ? i % per_head : i)) * BT;   // first streamed row, in the text
+            const float slope = BIAS ? a.slopes[KEYS ? head0 * a.group + i / per_head : head0] * kLog2e : 0.f;
+            const float2* st = reinterpret_cast<const float2*>(smem_raw + (stats - raw) + i % STAGES * C::STATS);
+            if (KEYS && !(ok = wait(full_bar(i % STAGES), (i / STAGES) & 1))) break;
+            if (!(ok = wait(s_bar(w), (i >> 1) & 1))) break;
+            tc_fence_after();
+            const bool masked = KEYS ? at < edge_of_all || at + BT > x.lq : at + BT > edge_of_all;
+            const int lo = KEYS ? edge - at : 0, hi = KEYS ? x.lq - at : edge - at;   // visible columns
+            const float away = BIAS ? (float)(KEYS ? row - (x.lk - x.lq) - at : row + x.lk - x.lq - at) : 0.f;
+#pragma unroll
+            for (int h = 0; h < BT; h += 32) {
+                float s[32], dp[32];
+                tmem_ld32_nowait(s_cols(w) + lanes + h, s);
+                tmem_ld32_nowait(dp_cols(w) + lanes + h, dp);
+                tmem_wait_ld();
+                uint32_t rp[16], rx[16];
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) {
+                    float4 two = make_float4(lse2, delta, lse2, delta);
+                    if (KEYS) two = *reinterpret_cast<const float4*>(st + h + k);
+                    float p[2], g[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float v = s[k + e], slack = 1.f;
+                        if (CAP) {
+                            const float th = attn_tanh(v * inv_cap);
+                            v = cap2 * th;
+                            slack = fmaf(-th, th, 1.f);
+                        }
+                        if (BIAS) v = fmaf(-slope, fabsf(away - (float)(h + k + e)), CAP ? v : v * (a.scale * kLog2e));
+                        p[e] = fast_exp2(fmaf(v, c, -(e ? two.z : two.x)));
+                        g[e] = p[e] * (dp[k + e] - (e ? two.w : two.y));
+                        if (CAP) g[e] *= slack;
+                        if (masked && (h + k + e >= hi || (KEYS && h + k + e < lo))) p[e] = g[e] = 0.f;
+                    }
+                    rp[k / 2] = pack2<T>(p[0], p[1]);
+                    rx[k / 2] = pack2<T>(g[0], g[1]);
+                }
+                // over what this half's scores were, which no other thread reads
+                if (KEYS) tmem_st16_nowait(s_cols(w) + lanes + h / 2, rp);
+                tmem_st16_nowait(dp_cols(w) + lanes + h / 2, rx);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_bar(w));
+        }
+        if (ok && n > 0) ok = wait(done_bar, 0);
+        if (ok) {
+            tc_fence_after();
+            // d-queries: half of the columns for each four warps; d-keys: dK and dV
+            const int which = KEYS ? w : 0, k0 = KEYS ? 0 : w * (D / 2), k1 = KEYS ? D : k0 + D / 2;
+            const float f = which == 0 ? a.scale : 1.f;
+            T* g = static_cast<T*>(P.grad[which]) + (int64_t)(kept_base + row) * P.ld[which] + (int64_t)head0 * a.dim;
+#pragma unroll 1
+            for (int k = k0; k < k1; k += 32) {
+                float v[32];
+                if (n > 0) {
+                    tmem_ld32_nowait(g_cols(which) + lanes + k, v);
+                    tmem_wait_ld();
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = n > 0 ? v[e] * f : 0.f;
+#pragma unroll
+                for (int e = 0; e < 32; e += 8)
+                    if (real && k + e < a.dim) store_n<T, 8>(g + k + e, v + e);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, COLS);
+}
+
+template <typename T, int D, bool CAP, bool BIAS, bool KEYS>
+cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {
+    auto* kernel = attn_bwd_kernel<T, D, CAP, BIAS, KEYS>;
+    const uint32_t bit = 1u << ((KEYS ? 16 : 0) + (std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
+    if (!(ctx->attn_bwd_ready & bit)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdTile<D>::SMEM);
+        if (e != cudaSuccess) return e;
+        ctx->attn_bwd_ready |= bit;
+    }
+    KernelScope scope(ctx, SAMA_K_ATTN, KEYS ? 2 : 1, st);
+    const int64_t blocks = (int64_t)P.slots * (KEYS ? P.a.kv_heads : P.a.heads);
+    return launch_dependent(kernel, dim3((unsigned)blocks), dim3(THREADS), BwdTile<D>::SMEM, st, P);
+}
+template <typename T, int D, bool KEYS>
+cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {
+    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, true, true, KEYS>(ctx, P, st) : launch<T, D, true, false, KEYS>(ctx, P, st);
+    return P.a.slopes ? launch<T, D, false, true, KEYS>(ctx, P, st) : launch<T, D, false, false, KEYS>(ctx, P, st);
+}
+template <bool KEYS>
+cudaError_t launch(sama_ctx* ctx, int dtype, const BwdParams& P, cudaStream_t st) {
+    if (dtype == SAMA_BF16)
+        return P.a.dim <= 64 ? launch<__nv_bfloat16, 64, KEYS>(ctx, P, st) : launch<__nv_bfloat16, 128, KEYS>(ctx, P, st);
+    return P.a.dim <= 64 ? launch<__half, 64, KEYS>(ctx, P, st) : launch<__half, 128, KEYS>(ctx, P, st);
+}
+
+}  // namespace
+
+size_t attention_grad_workspace(const AttnShape& a) { return (size_t)a.heads * a.n_q * sizeof(float2); }
+
+cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, const void* out, const float* lse,
+                                  const void* dout, void* dq, void* dk, void* dv, void* ws, cudaStream_t st) {
+    BwdParams P;
+    P.a = a;
+    P.out = out;
+    P.dout = dout;
+    P.lse = lse;
+    P.stats = static_cast<float2*>(ws);
+    const int64_t dense = (int64_t)a.heads * a.dim;
+    auto query_maps = [&](CUtensorMap* m, int rows) {
+        return attn_map(&m[0], op.q, op.dtype, a.dim, a.heads, a.n_q, op.q_stride, rows) &&
+               attn_map(&m[1], dout, op.dtype, a.dim, a.heads, a.n_q, dense, rows);
+    };
+    auto key_maps = [&](CUtensorMap* m, int rows) {
+        return attn_map(&m[0], op.k, op.dtype, a.dim, a.kv_heads, a.n_k, op.k_stride, rows) &&
+               attn_map(&m[1], op.v, op.dtype, a.dim, a.kv_heads, a.n_k, op.v_stride, rows);
+    };
+    if (a.n_q > 0) {
+        // (without keys nothing is loaded, but a map has to describe something)
+        if (!query_maps(P.kept, kAttnRows) || !(a.n_k > 0 ? key_maps(P.streamed, BT) : query_maps(P.streamed, BT)))
+            return cudaErrorInvalidValue;
+        P.grad[0] = P.grad[1] = dq;
+        P.ld[0] = P.ld[1] = op.q_stride;
+        P.slots = a.n_q / kAttnRows + a.n_texts;
+        const cudaError_t e = launch<false>(ctx, op.dtype, P, st);
+        if (e != cudaSuccess) return e;
+    }
+    if (a.n_k == 0) return cudaSuccess;
+    if (!key_maps(P.kept, kAttnRows) || !(a.n_q > 0 ? query_maps(P.streamed, BT) : key_maps(P.streamed, BT))) return cudaErrorInvalidValue;
+    P.grad[0] = dk;
+    P.grad[1] = dv;
+    P.ld[0] = op.k_stride;
+    P.ld[1] = op.v_stride;
+    P.slots = a.n_k / kAttnRows + a.n_texts;
+    return launch<true>(ctx, op.dtype, P, st);
+}
+
+}  // namespace sama

@@ -1,0 +1,339 @@
+// Attention over packed texts, forward: out = softmax(scores) V in one pass over the keys, with the running maximum and
+// sum of the softmax, on the 5th-generation tensor cores.
+//
+// A CTA has 256 queries of one text and head, two tiles of 128, and streams the keys and values that they see.  A score
+// tile S = Q K^T is produced in tensor memory; four warps per tile, a thread per query, turn it into weights
+// P = 2^(x log2 e - m), which go back to tensor memory in 16 bits over the scores they came from, and O += P V takes them
+// from there.  While one tile's weights are formed the other's products run.  The maximum m that the weights refer to is
+// only raised when a score exceeds it by more than 8 binary orders (O and the sum are scaled then): the weights stay below
+// 2^8, far from the end of either type, and are rounded relative to their size whatever they refer to.
+//
+// Roles of the 10 warps: warp 0 copies (TMA, 128-byte swizzle), warp 1 issues products, warps 2..5 and 6..9 the softmax of
+// the two tiles.  Every wait is bounded: one that expires raises SAMA_DEV_TIMEOUT and ends the CTA's work.
+#include <type_traits>
+
+#include "attention.h"
+
+namespace sama {
+
+namespace {
+
+constexpr int THREADS = 320;
+constexpr float kRaise = 8.f;
+
+template <int D> struct FwdTile {
+    static constexpr int BK = D == 64 ? 64 : 128;        // keys of a tile
+    static constexpr int STAGES = D == 64 ? 6 : 4;       // tiles of keys or values in shared memory
+    static constexpr int Q_BYTES = kAttnRows * D * 2, KV_BYTES = BK * D * 2;
+    static constexpr int SMEM = 2 * Q_BYTES + STAGES * KV_BYTES + 256 + 1024;
+    static constexpr int COLS = D == 64 ? 256 : 512;     // of tensor memory: two score tiles, two outputs
+};
+
+struct alignas(64) FwdParams {
+    CUtensorMap q, k, v;
+    AttnShape a;
+    void* out;
+    float* lse;
+    int slots;
+};
+
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(THREADS, D == 64 ? 2 : 1)
+attn_fwd_kernel(const __grid_constant__ FwdParams P) {
+    using C = FwdTile<D>;
+    constexpr int BK = C::BK, STAGES = C::STAGES;
+    constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr uint32_t IDESC_S = idesc16(BF16, false, false, kAttnRows, BK), IDESC_O = idesc16(BF16, false, true, kAttnRows, D);
+    const AttnShape& a = P.a;
+
+    pdl_trigger();
+    pdl_wait();
+    if (blockIdx.x == 0) attn_check_starts(a);
+    // the last tiles of a text, which see the most keys, come first
+    const int slot = P.slots - 1 - (int)blockIdx.x / a.heads, head = (int)blockIdx.x % a.heads;
+    int tile;
+    const int t = attn_find<2 * kAttnRows>(a.q_starts, a.n_texts, a.n_q, slot, &tile);
+    if (t < 0) return;
+    const AttnText x = attn_text(a, t);
+    const int first = tile * 2 * kAttnRows;
+    if (first >= x.lq) return;
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t base = (raw + 1023u) & ~1023u;
+    const uint32_t ring = base + 2 * C::Q_BYTES, bars = ring + STAGES * C::KV_BYTES;
+    auto full_bar = [&](int s) { return bars + 8u * s; };
+    auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
+    auto q_bar = [&](int w) { return bars + 8u * (2 * STAGES + w); };
+    auto s_bar = [&](int w) { return bars + 8u * (2 * STAGES + 2 + w); };   // scores are there
+    auto p_bar = [&](int w) { return bars + 8u * (2 * STAGES + 4 + w); };   // weights are there
+    auto o_bar = [&](int w) { return bars + 8u * (2 * STAGES + 6 + w); };   // the output is complete
+    const uint32_t tmem_slot = bars + 8u * (2 * STAGES + 8);
+    volatile uint32_t* tmem_ptr_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_slot - raw));
+    volatile uint32_t* abort_flag = tmem_ptr_slot + 1;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(q_bar(w), 1);
+            mbar_init(s_bar(w), 1);
+            mbar_init(p_bar(w), 4);
+            mbar_init(o_bar(w), 1);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(tmem_slot, C::COLS);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_ptr_slot;
+    auto s_cols = [&](int w) { return tmem + (uint32_t)(w * BK); };
+    auto o_cols = [&](int w) { return tmem + (uint32_t)(2 * BK + w * D); };
+
+    // key tiles that the last query of each of the two tiles sees
+    int n_kt[2];
+    for (int w = 0; w < 2; ++w) {
+        const int i0 = first + w * kAttnRows;
+        n_kt[w] = i0 < x.lq ? (attn_seen(a, x, min(i0 + kAttnRows, x.lq) - 1) + BK - 1) / BK : 0;
+    }
+    const int n_all = max(n_kt[0], n_kt[1]), items = 2 * n_all;   // keys and values in turn
+    const int kv_head = head / a.group;
+
+    auto raise_timeout = [&]() {
+        *abort_flag = 1;
+        atomicOr(a.status, (int)SAMA_DEV_TIMEOUT);
+    };
+
+    // for all lanes of a warp together
+    auto wait = [&](uint32_t bar, int parity) {
+        const bool ok = mbar_wait(bar, (uint32_t)parity, abort_flag);
+        if (__all_sync(0xffffffffu, ok)) return true;
+        raise_timeout();
+        return false;
+    };
+
+    if (warp == 0) {
+        if (lane == 0 && n_all > 0) {
+            auto load_q = [&](int w) {
+                if (n_kt[w] == 0) return;
+                mbar_expect_tx(q_bar(w), C::Q_BYTES);
+                for (int c = 0; c < D / 64; ++c)
+                    tma_load_3d(base + w * C::Q_BYTES + c * kAttnRows * 128, &P.q, q_bar(w), 64 * c, head, x.q0 + first + w * kAttnRows);
+            };
+            load_q(0);
+            int item = 0;
+            for (; item < items; ++item) {
+                const int s = item % STAGES;
+                if (item >= STAGES && !mbar_wait(empty_bar(s), (item / STAGES - 1) & 1, abort_flag)) { raise_timeout(); break; }
+                mbar_expect_tx(full_bar(s), C::KV_BYTES);
+                for (int c = 0; c < D / 64; ++c)
+                    tma_load_3d(ring + s * C::KV_BYTES + c * BK * 128, item & 1 ? &P.v : &P.k, full_bar(s), 64 * c, kv_head, x.k0 + (item >> 1) * BK);
+                if (item == 0) load_q(1);
+            }
+            if (*abort_flag) {
+                // let the copies already issued land before the CTA's shared memory goes away
+                for (int w = 0; w < 2; ++w)
+                    if (n_kt[w] > 0) mbar_wait(q_bar(w), 0);
+                for (int i = max(0, item - STAGES); i < item; ++i) mbar_wait(full_bar(i % STAGES), (i / STAGES) & 1);
+            }
+        }
+    } else if (warp == 1) {
+        bool ok = true;
+        auto wait_item = [&](int item) {
+            ok = ok && wait(full_bar(item % STAGES), (item / STAGES) & 1);
+            tc_fence_after();
+        };
+        auto release = [&](int item) {
+            if (item + STAGES < items) umma_commit(empty_bar(item % STAGES));
+        };
+        auto scores = [&](int w, int j) {   // S_w = Q_w K_j^T
+            const uint64_t dq = make_desc(base + w * C::Q_BYTES), dk = make_desc(ring + (2 * j) % STAGES * C::KV_BYTES);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                umma16(s_cols(w), dq + (uint64_t)((k / 4 * kAttnRows * 128 + k % 4 * 32) >> 4),
+                       dk + (uint64_t)((k / 4 * BK * 128 + k % 4 * 32) >> 4), IDESC_S, k > 0);
+            umma_commit(s_bar(w));
+        };
+        if (n_all > 0) {
+            wait_item(0);
+            for (int w = 0; w < 2 && ok; ++w) {
+                if (n_kt[w] == 0) continue;
+                if (!(ok = wait(q_bar(w), 0))) break;
+                tc_fence_after();
+                if (lane == 0) scores(w, 0);
+            }
+            if (ok && lane == 0) release(0);
+        }
+        for (int j = 0; ok && j < n_all; ++j) {
+            const int vs = (2 * j + 1) % STAGES;
+            wait_item(2 * j + 1);
+            if (!ok) break;
+            if ((j + 1) * BK > x.lk) attn_zero_rows<D / 64>(ring + vs * C::KV_BYTES, x.lk - j * BK, BK);
+            if (j + 1 < n_all) wait_item(2 * j + 2);
+            for (int w = 0; w < 2 && ok; ++w) {
+                if (j >= n_kt[w]) continue;
+                if (!(ok = wait(p_bar(w), j & 1))) break;
+                tc_fence_after();
+                if (lane == 0) {
+                    const uint64_t dv = attn_desc_mn(ring + vs * C::KV_BYTES, BK);
+#pragma unroll
+                    for (int k = 0; k < BK / 16; ++k)
+                        umma16_ta(o_cols(w), s_cols(w) + 8u * k, dv + (uint64_t)(k * 2048 >> 4), IDESC_O, j > 0 || k > 0);
+                    // (products are executed in order: the next scores do not overtake the weights they replace)
+                    if (j + 1 < n_kt[w]) scores(w, j + 1); else umma_commit(o_bar(w));
+                }
+            }
+            if (ok && lane == 0) {
+                release(2 * j + 1);
+                if (j + 1 < n_all) release(2 * j + 2);
+            }
+            __syncwarp();
+        }
+    } else {
+        const int w = (warp - 2) >> 2, quarter = warp & 3;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const int row0 = first + w * kAttnRows + quarter * 32, row = row0 + lane;   // in the text
+        const int seen = attn_seen(a, x, row), seen_by_all = attn_seen(a, x, row0);
+        constexpr bool RAW = !CAP && !BIAS;     // scores as they come, the factor is applied in the exponent
+        const float c = RAW ? a.scale * kLog2e : 1.f;
+        const float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
+        const float inv_cap = CAP ? a.scale / a.cap : 0.f, cap2 = CAP ? a.cap * kLog2e : 0.f;
+        float m = -INFINITY, l = 0.f;
+        bool ok = true;
+        for (int j = 0; j < n_kt[w]; ++j) {
+            if (!(ok = wait(s_bar(w), j & 1))) break;
+            tc_fence_after();
+            float s[BK];
+#pragma unroll
+            for (int k = 0; k < BK; k += 32) tmem_ld32_nowait(s_cols(w) + lanes + k, s + k);
+            tmem_wait_ld();
+            if (CAP) {
+#pragma unroll
+                for (int k = 0; k < BK; ++k) s[k] = cap2 * attn_tanh(s[k] * inv_cap);
+            }
+            if (BIAS) {
+                const float away = (float)(row + x.lk - x.lq - j * BK);
+#pragma unroll
+                for (int k = 0; k < BK; ++k) s[k] = fmaf(-slope, fabsf(away - (float)k), CAP ? s[k] : s[k] * (a.scale * kLog2e));
+            }
+            if ((j + 1) * BK > seen_by_all) {
+                const int left = seen - j * BK;
+#pragma unroll
+                for (int k = 0; k < BK; ++k) s[k] = k < left ? s[k] : -INFINITY;
+            }
+            float top = s[0];
+#pragma unroll
+            for (int k = 1; k < BK; ++k) top = fmaxf(top, s[k]);
+            top *= c;
+            if (__any_sync(0xffffffffu, top > m + kRaise || (m == -INFINITY && top > m))) {
+                const float raised = fmaxf(m, top);
+                const float factor = raised == -INFINITY ? 1.f : fast_exp2(m - raised);
+                m = raised;
+                l *= factor;
+                if (j > 0) {
+#pragma unroll 1
+                    for (int k = 0; k < D; k += 32) {
+                        float o[32];
+                        tmem_ld32_nowait(o_cols(w) + lanes + k, o);
+                        tmem_wait_ld();
+                        uint32_t r[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i] * factor);
+                        tmem_st16_nowait(o_cols(w) + lanes + k, r);
+                        tmem_st16_nowait(o_cols(w) + lanes + k + 16, r + 16);
+                    }
+                }
+            }
+            const float from = m == -INFINITY ? 0.f : m;
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < BK; k += 32) {
+                uint32_t r[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float p0 = fast_exp2(fmaf(s[k + 2 * i], c, -from)), p1 = fast_exp2(fmaf(s[k + 2 * i + 1], c, -from));
+                    sum += p0 + p1;
+                    r[i] = pack2<T>(p0, p1);
+                }
+                tmem_st16_nowait(s_cols(w) + lanes + k / 2, r);
+            }
+            l += sum;
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_bar(w));
+        }
+        const bool real = row < x.lq;
+        if (n_kt[w] > 0 && ok) {
+            ok = wait(o_bar(w), 0);
+            tc_fence_after();
+        }
+        if (ok && row0 < x.lq) {
+            const bool empty = l == 0.f;
+            const float inv = 1.f / l;
+            if (real && P.lse) P.lse[(int64_t)head * a.n_q + x.q0 + row] = empty ? -INFINITY : (m + __log2f(l)) * 0.69314718f;
+            T* out = static_cast<T*>(P.out) + ((int64_t)(x.q0 + row) * a.heads + head) * a.dim;
+#pragma unroll 1
+            for (int k = 0; k < D; k += 32) {
+                float o[32];
+                if (n_kt[w] > 0) {
+                    tmem_ld32_nowait(o_cols(w) + lanes + k, o);
+                    tmem_wait_ld();
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = empty ? 0.f : o[i] * inv;
+#pragma unroll
+                for (int i = 0; i < 32; i += 8)
+                    if (real && k + i < a.dim) store_n<T, 8>(out + k + i, o + i);
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, C::COLS);
+}
+
+template <typename T, int D, bool CAP, bool BIAS>
+cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
+    auto* kernel = attn_fwd_kernel<T, D, CAP, BIAS>;
+    const uint32_t bit = 1u << ((std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
+    if (!(ctx->attn_fwd_ready & bit)) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdTile<D>::SMEM);
+        if (e != cudaSuccess) return e;
+        ctx->attn_fwd_ready |= bit;
+    }
+    KernelScope scope(ctx, SAMA_K_ATTN, 0, st);
+    return launch_dependent(kernel, dim3((unsigned)((int64_t)P.slots * P.a.heads)), dim3(THREADS), FwdTile<D>::SMEM, st, P);
+}
+template <typename T, int D>
+cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
+    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, true, true>(ctx, P, st) : launch<T, D, true, false>(ctx, P, st);
+    return P.a.slopes ? launch<T, D, false, true>(ctx, P, st) : launch<T, D, false, false>(ctx, P, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attention(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, void* out, float* lse, cudaStream_t st) {
+    FwdParams P;
+    const int bk = a.dim <= 64 ? FwdTile<64>::BK : FwdTile<128>::BK;
+    // (without keys nothing is loaded, but a map has to describe something)
+    const bool none = a.n_k == 0;
+    if (!attn_map(&P.q, op.q, op.dtype, a.dim, a.heads, a.n_q, op.q_stride, kAttnRows) ||
+        !attn_map(&P.k, none ? op.q : op.k, op.dtype, a.dim, none ? a.heads : a.kv_heads, none ? a.n_q : a.n_k, none ? op.q_stride : op.k_stride, bk) ||
+        !attn_map(&P.v, none ? op.q : op.v, op.dtype, a.dim, none ? a.heads : a.kv_heads, none ? a.n_q : a.n_k, none ? op.q_stride : op.v_stride, bk))
+        return cudaErrorInvalidValue;
+    P.a = a;
+    P.out = out;
+    P.lse = lse;
+    P.slots = a.n_q / (2 * kAttnRows) + a.n_texts;
+    if (op.dtype == SAMA_BF16)
+        return a.dim <= 64 ? launch<__nv_bfloat16, 64>(ctx, P, st) : launch<__nv_bfloat16, 128>(ctx, P, st);
+    return a.dim <= 64 ? launch<__half, 64>(ctx, P, st) : launch<__half, 128>(ctx, P, st);
+}
+
+}  // namespace sama
