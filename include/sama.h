@@ -367,6 +367,47 @@ int sama_attention(sama_ctx* ctx, const sama_attn_t* a, const void* q, const voi
 int sama_attention_grad(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, const void* out,
                         const float* lse, const void* d_out, void* dq, void* dk, void* dv, void* stream);
 
+/* One new token for each of n_seqs sequences over a cache in pages: key j of sequence s is row j % page_size of page
+ * page_table[s][j / page_size], j < lengths[s].  The new token is at position lengths[s] - 1: lengths count it. */
+typedef struct sama_paged_t {
+    int32_t dtype;                       /* SAMA_BF16 or SAMA_F16 */
+    int32_t heads, kv_heads, head_dim;   /* kv_heads divides heads; head_dim a multiple of 8, 8 .. 128 */
+    int32_t page_size;                   /* 1 .. 2^20 */
+    int32_t n_seqs, max_pages;           /* rows and columns of page_table; 0 .. 2^20, 1 .. 2^24 */
+    int64_t n_pages;                     /* pages of each cache, 1 .. 2^31 - 1 */
+    int64_t page_stride;                 /* elements from a page to the next, a multiple of 8; 0: page_size * kv_heads * head_dim */
+    const int32_t* page_table;           /* device [n_seqs][max_pages]; entries behind a sequence's last page are not read */
+    const int32_t* lengths;              /* device [n_seqs], 0 .. max_pages * page_size (others: SAMA_DEV_BAD_INDEX, taken as the nearest) */
+    const float* slopes;                 /* device [heads], or NULL */
+    float scale, cap;
+} sama_paged_t;
+
+/* q, out: [n_seqs][heads][head_dim]; k_cache, v_cache: [n_pages][page_size][kv_heads][head_dim]; k_new, v_new:
+ * [n_seqs][kv_heads][head_dim], the new token's own, which are written to the cache and used, or both NULL where the cache
+ * has them already.  Scores as in sama_attention.  A sequence of length 0 has out = 0 (and writes nothing to the cache).  A page
+ * outside [0, n_pages) sets SAMA_DEV_BAD_INDEX and its keys are left out.  No two sequences may have their new token in
+ * the same place.  The cache is split over its length when there are few sequences; partial results are joined in a fixed
+ * order (bitwise reproducible). */
+int sama_paged_attention(sama_ctx* ctx, const sama_paged_t* a, const void* q, const void* k_new, const void* v_new,
+                         void* k_cache, void* v_cache, void* out, void* stream);
+
+/* ---- Learning from a teacher's top logits ----------------------------------------------------------------------
+ * For row i of the student's logits z, with the teacher's k largest logits u_ij of the entries id_ij:
+ *   p_i = softmax over j of u_ij / T,    q_i = softmax over the whole vocabulary of z_i / T
+ *   loss[i] = T^2 * sum over j of p_ij * (log p_ij - log q_i,id_ij)
+ *   grad[i][v] = grad_scale * weight[i] * T * (q_iv - sum of the p_ij with id_ij = v)
+ * logits: [n_rows][vocab] of type `dtype` (any sama_dtype), rows `ld` elements apart (0: vocab); grad: the same type, rows
+ * `ld_grad` apart (0: vocab; what lies between rows is left alone), or NULL for losses alone; grad may be logits itself,
+ * with the same ld.  top_logits [n_rows][k] of type top_dtype; top_ids: int32 [n_rows][k], an id of -1 is an unused
+ * entry, other ids outside [0, vocab) are unused, too, and set SAMA_DEV_BAD_INDEX.  An entry whose u is -infinity has p = 0.
+ * A row without any entry (or none above -infinity) has loss = 0 and a zero gradient.  weight: fp32 [n_rows] or NULL (1);
+ * a row of weight 0 has a zero gradient, whatever its logits.  loss_out: fp32 [n_rows], not weighted (what the meta step's
+ * weights are learnt from), or NULL.  Sums are fp32 in a fixed order (bitwise reproducible).
+ * 0 <= n_rows <= 2^30, 1 <= vocab <= 2^24, 1 <= k <= 1024, T > 0. */
+int sama_distill(sama_ctx* ctx, int32_t dtype, int64_t n_rows, int32_t vocab, const void* logits, int64_t ld, int32_t k,
+                 int32_t top_dtype, const void* top_logits, const int32_t* top_ids, float temperature, const float* weight,
+                 float grad_scale, float* loss_out, void* grad, int64_t ld_grad, void* stream);
+
 /* sama_step (Fig. 2) for callers whose data lives in HOST memory: every
  * pointer below is a host pointer (pinned memory makes the copies
  * asynchronous).  Copies the inputs to staging buffers owned by the context
@@ -465,7 +506,9 @@ enum {
     SAMA_K_EMBED_GRAD = 16,   /* its gradient: sort, sums, joins */
     SAMA_K_CLIP = 17,         /* global gradient norm and clipping */
     SAMA_K_FFN = 18,          /* gated feed-forward block; layer: 0 gate-up, 1 down, 2 d-hidden, 3 d-input, 4 d-weights */
-    SAMA_K_ATTN = 19          /* attention; layer: 0 forward, 1 d-queries, 2 d-keys and d-values */
+    SAMA_K_ATTN = 19,         /* attention; layer: 0 forward, 1 d-queries, 2 d-keys and d-values */
+    SAMA_K_PAGED = 20,        /* attention over a paged cache */
+    SAMA_K_DISTILL = 21       /* distillation loss and gradient */
 };
 typedef struct sama_kernel_time_t {
     int32_t kind;     /* SAMA_K_* */

@@ -54,7 +54,7 @@ class sama_kernel_time_t(C.Structure):
 KERNEL_KINDS = {0: "adapt_sumsq", 1: "sumsq", 2: "perturb", 3: "gemm_ffma", 4: "ce_fd", 5: "split_tf32",
                 6: "gemm_tf32x3", 7: "head_ce_fd", 8: "perturb_split", 9: "meta_gemm", 10: "meta_aux",
                 11: "reweight_fd", 12: "biasreg_grad", 13: "biasreg_fd", 14: "fused_sweep", 15: "embed",
-                16: "embed_grad", 17: "clip", 18: "ffn", 19: "attn"}
+                16: "embed_grad", 17: "clip", 18: "ffn", 19: "attn", 20: "paged", 21: "distill"}
 
 
 class sama_mlp_t(C.Structure):
@@ -166,6 +166,52 @@ class Attn:
         return x.data_ptr()
 
 
+class sama_paged_t(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int64),
+                ("page_stride", C.c_int64), ("page_table", C.c_void_p), ("lengths", C.c_void_p), ("slopes", C.c_void_p),
+                ("scale", C.c_float), ("cap", C.c_float)]
+
+
+class Paged:
+    """Host description of a paged cache for sama_paged_attention, kept by a program that runs several layers or steps on
+    it.  ``page_table`` (int32, [sequences][pages]), ``lengths`` (int32) and ``slopes`` (fp32) are tensors on the GPU, whose
+    values may change between calls.  Holds references to them."""
+
+    def __init__(self, dtype, heads, kv_heads, head_dim, page_size, n_pages, page_table, lengths, slopes=None, scale=None,
+                 cap=0.0, page_stride=0):
+        w = "Paged"
+        self.device = page_table.get_device()
+        if page_table.dim() != 2:
+            raise SamaError(SAMA_ERR_SIZE, w)
+        n, columns = page_table.shape
+        self.held = (page_table, lengths, slopes)
+        self.a = sama_paged_t(dtype, heads, kv_heads, head_dim, page_size, n, columns, n_pages, page_stride,
+                              _dense(self.device, page_table, "i32", n * columns, w), _dense(self.device, lengths, "i32", n, w),
+                              _dense(self.device, slopes, SAMA_F32, heads, w),
+                              head_dim ** -0.5 if scale is None else scale, cap)
+        self._ref = C.byref(self.a)
+        self.page = page_size * kv_heads * head_dim
+
+    def cache(self, x, where):
+        """Address of a cache [n_pages][page_size][kv_heads][head_dim] whose pages may lie apart."""
+        if x is None or isinstance(x, int):
+            return x
+        a = self.a
+        if x.get_device() != self.device:
+            raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is on %s, not on the cache's GPU" % (where, x.device))
+        if not _torch_dtypes:
+            _fill_dtypes()
+        if x.dtype is not _torch_dtypes.get(a.dtype):
+            raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is not of the type the call names" % where)
+        if x.dim() != 4 or x.shape[0] < a.n_pages or tuple(x.shape[1:]) != (a.page_size, a.kv_heads, a.head_dim):
+            raise SamaError(SAMA_ERR_SIZE, where)
+        stride = a.page_stride or self.page
+        if (x.shape[0] > 1 and x.stride(0) != stride) or not x[0].is_contiguous():
+            raise SamaError(SAMA_ERR_PARAM, "%s: a tensor's strides are not the described ones" % where)
+        return x.data_ptr()
+
+
 _vp = C.c_void_p
 lib.sama_create.argtypes = [C.POINTER(_vp), C.c_int, C.c_int64, C.c_int32, C.POINTER(sama_mlp_t)]
 lib.sama_destroy.argtypes = [_vp]
@@ -197,6 +243,9 @@ lib.sama_gated_ffn_grad.argtypes = [_vp, C.c_int32, C.c_int32, C.c_int64, C.c_in
 lib.sama_clip_grads.argtypes = [_vp, C.POINTER(sama_tensor_t), C.c_int32, C.c_float, _vp, _vp]
 lib.sama_attention.argtypes = [_vp, C.POINTER(sama_attn_t)] + [_vp] * 6
 lib.sama_attention_grad.argtypes = [_vp, C.POINTER(sama_attn_t)] + [_vp] * 10
+lib.sama_paged_attention.argtypes = [_vp, C.POINTER(sama_paged_t)] + [_vp] * 7
+lib.sama_distill.argtypes = [_vp, C.c_int32, C.c_int64, C.c_int32, _vp, C.c_int64, C.c_int32, C.c_int32, _vp, _vp, C.c_float, _vp,
+                             C.c_float, _vp, _vp, C.c_int64, _vp]
 lib.sama_ctx_sumsq.argtypes = [_vp]
 lib.sama_ctx_sumsq.restype = _vp
 lib.sama_ctx_eps_fd.argtypes = [_vp]
@@ -462,6 +511,42 @@ def sama_attention_grad(ctx, attn: Attn, q, k, v, out, lse, d_out, dq, dk, dv, s
                                           _dense(attn.device, out, a.dtype, n, w), _dense(attn.device, lse, SAMA_F32, a.heads * a.n_q, w),
                                           _dense(attn.device, d_out, a.dtype, n, w), attn.rows(dq, attn.q, w),
                                           attn.rows(dk, attn.k, w), attn.rows(dv, attn.v, w), _stream(stream)), w)
+
+
+def sama_paged_attention(ctx, paged: Paged, q, k_new, v_new, k_cache, v_cache, out, stream=None) -> int:
+    w, a, at = "sama_paged_attention", paged.a, paged.device
+    _on_device(ctx, at, w)
+    n, m = a.n_seqs * a.heads * a.head_dim, a.n_seqs * a.kv_heads * a.head_dim
+    return _check(lib.sama_paged_attention(ctx, paged._ref, _dense(at, q, a.dtype, n, w), _dense(at, k_new, a.dtype, m, w),
+                                           _dense(at, v_new, a.dtype, m, w), paged.cache(k_cache, w), paged.cache(v_cache, w),
+                                           _dense(at, out, a.dtype, n, w), _stream(stream)), w)
+
+
+def _matrix(device, x, dtype, rows, cols, where):
+    """Address of a matrix whose rows may lie apart, and the elements from a row to the next."""
+    if x is None or isinstance(x, int):
+        return x, 0
+    if x.dim() != 2 or x.shape[0] < rows or x.shape[1] < cols:
+        raise SamaError(SAMA_ERR_SIZE, where)
+    at = x.get_device()
+    if at < 0 or (device is not None and at != device):
+        raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is on %s, not on the context's GPU" % (where, x.device))
+    if not _torch_dtypes:
+        _fill_dtypes()
+    if x.dtype is not _torch_dtypes.get(dtype) or (x.stride(1) != 1 and cols > 1):
+        raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is not of the type the call names, or its columns lie apart" % where)
+    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else 0
+
+
+def sama_distill(ctx, dtype, n_rows, vocab, logits, k, top_dtype, top_logits, top_ids, temperature, weight, grad_scale,
+                 loss_out=None, grad=None, ld=0, ld_grad=0, stream=None) -> int:
+    """``ld`` and ``ld_grad`` are for addresses; tensors of two dimensions bring their own."""
+    w, v = "sama_distill", _device_of.get(ctx)
+    z, z_ld = _matrix(v, logits, dtype, n_rows, vocab, w)
+    g, g_ld = _matrix(v, grad, dtype, n_rows, vocab, w)
+    return _check(lib.sama_distill(ctx, dtype, n_rows, vocab, z, z_ld or ld, k, top_dtype, _dense(v, top_logits, top_dtype, n_rows * k, w),
+                                   _dense(v, top_ids, "i32", n_rows * k, w), temperature, _dense(v, weight, SAMA_F32, n_rows, w),
+                                   grad_scale, _dense(v, loss_out, SAMA_F32, n_rows, w), g, g_ld or ld_grad, _stream(stream)), w)
 
 
 def sama_step_host(ctx, mlp: MLP, n, theta_host, m_host, s_host, g_base_host, g_meta_host, adam: Adam, alpha,

@@ -31,6 +31,20 @@ size_t attention_grad_workspace(const AttnShape& a);
 cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, const void* out, const float* lse,
                                   const void* dout, void* dq, void* dk, void* dv, void* ws, cudaStream_t st);
 
+
+struct PagedShape {
+    const int32_t *page_table, *lengths;
+    const float* slopes;
+    int32_t* status;
+    int64_t n_pages, page_stride;
+    int n_seqs, max_pages, page_size, heads, kv_heads, group, dim;
+    float scale, cap;
+};
+// attention_paged.cu
+size_t paged_workspace(const sama_ctx* ctx);
+cudaError_t launch_paged(sama_ctx* ctx, const PagedShape& a, int dtype, const void* q, const void* k_new, const void* v_new,
+                         void* k_cache, void* v_cache, void* out, void* ws, cudaStream_t st);
+
 #ifdef __CUDACC__
 
 __device__ __forceinline__ int attn_start(const int32_t* starts, int i, int n) { return min(max(starts[i], 0), n); }

@@ -144,4 +144,57 @@ int sama_attention_grad(sama_ctx* ctx, const sama_attn_t* a, const void* q, cons
     return SAMA_OK;
 }
 
+int sama_paged_attention(sama_ctx* ctx, const sama_paged_t* a, const void* q, const void* k_new, const void* v_new,
+                         void* k_cache, void* v_cache, void* out, void* stream) {
+    if (!ctx || !a) return SAMA_ERR_NULL;
+    int rc = check_heads(a->dtype, a->heads, a->kv_heads, a->head_dim, a->scale, a->cap);
+    if (rc != SAMA_OK) return rc;
+    if (a->n_seqs < 0 || a->n_seqs > (1 << 20) || a->max_pages < 1 || a->max_pages > (1 << 24) || a->page_size < 1 ||
+        a->page_size > (1 << 20) || a->n_pages < 1 || a->n_pages > 0x7fffffff)
+        return SAMA_ERR_SIZE;
+    const int64_t row = (int64_t)a->kv_heads * a->head_dim, page = row * a->page_size, stride = a->page_stride ? a->page_stride : page;
+    if (stride < page || stride % 8 != 0 || stride > ((int64_t)1 << 40)) return SAMA_ERR_SIZE;
+    if (a->n_seqs > 0 && (!q || !k_cache || !v_cache || !out || !a->page_table || !a->lengths)) return SAMA_ERR_NULL;
+    if ((k_new == nullptr) != (v_new == nullptr)) return SAMA_ERR_NULL;
+    const void* wide[6] = {q, k_new, v_new, k_cache, v_cache, out};
+    for (const void* p : wide)
+        if (!aligned(p, 16)) return SAMA_ERR_ALIGN;
+    if (!aligned(a->page_table, 4) || !aligned(a->lengths, 4) || !aligned(a->slopes, 4)) return SAMA_ERR_ALIGN;
+    const Rows rk = {k_cache, a->n_pages, (size_t)page * 2, (size_t)stride * 2}, rv = {v_cache, a->n_pages, (size_t)page * 2, (size_t)stride * 2};
+    const size_t nq = (size_t)a->n_seqs * a->heads * a->head_dim * 2, nn = (size_t)a->n_seqs * row * 2;
+    const Rows ro = {out, a->n_seqs > 0 ? 1 : 0, nq, nq};
+    const struct { const void* p; size_t bytes; } ins[6] = {{q, nq}, {k_new, nn}, {v_new, nn},
+        {a->page_table, (size_t)a->n_seqs * a->max_pages * 4}, {a->lengths, (size_t)a->n_seqs * 4}, {a->slopes, (size_t)a->heads * 4}};
+    for (const auto& in : ins) {
+        const Rows ri = {in.p, in.bytes > 0 ? 1 : 0, in.bytes, in.bytes};
+        if (rows_overlap(ro, ri)) return SAMA_ERR_OVERLAP;
+        // the caches are written where there are new tokens
+        if (k_new && (overlaps(in.p, in.bytes, k_cache, rk.span()) || overlaps(in.p, in.bytes, v_cache, rv.span()))) return SAMA_ERR_OVERLAP;
+    }
+    if (overlaps(out, nq, k_cache, rk.span()) || overlaps(out, nq, v_cache, rv.span()) || (k_new && rows_overlap(rk, rv))) return SAMA_ERR_OVERLAP;
+    if (a->n_seqs == 0) return SAMA_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SAMA_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    if ((rc = need_workspace(ctx, paged_workspace(ctx), ctx->paged_arrived != nullptr, st)) != SAMA_OK) return rc;
+    PagedShape s;
+    s.page_table = a->page_table;
+    s.lengths = a->lengths;
+    s.slopes = a->slopes;
+    s.status = &ctx->scalars->status;
+    s.n_pages = a->n_pages;
+    s.page_stride = stride;
+    s.n_seqs = a->n_seqs;
+    s.max_pages = a->max_pages;
+    s.page_size = a->page_size;
+    s.heads = a->heads;
+    s.kv_heads = a->kv_heads;
+    s.group = a->heads / a->kv_heads;
+    s.dim = a->head_dim;
+    s.scale = a->scale;
+    s.cap = a->cap;
+    SAMA_SETUP(ctx, launch_paged(ctx, s, a->dtype, q, k_new, v_new, k_cache, v_cache, out, ctx->op_ws, st));
+    return SAMA_OK;
+}
+
 }  // extern "C"

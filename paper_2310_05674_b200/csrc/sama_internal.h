@@ -141,6 +141,9 @@ struct sama_ctx {
     int ffn_path[5];               // how each of the block's launches was last worked on (sama_last_ffn_path)
     uint32_t attn_fwd_ready;       // kernels of attention_fwd.cu whose shared-memory size is set on this device
     uint32_t attn_bwd_ready;       // ... and of attention_bwd.cu
+    uint32_t paged_ready;          // ... and of attention_paged.cu
+    uint32_t distill_ready;        // ... and of distill.cu
+    int* paged_arrived;            // device: arrival counters of heads that several CTAs share, zero between launches
     sama::Profiler* prof;          // host
 };
 
@@ -345,6 +348,11 @@ cudaError_t launch_embed_grad(sama_ctx* ctx, int dtype, int64_t n, int64_t vocab
 // clip_grads.cu : global gradient norm and clipping
 cudaError_t launch_clip_grads(sama_ctx* ctx, const sama_tensor_t* t, int n, float max_norm, float* norm_out,
                               cudaStream_t st);
+
+// distill.cu : learning from a teacher's top logits
+cudaError_t launch_distill(sama_ctx* ctx, int dtype, int64_t n_rows, int vocab, const void* logits, int64_t ld, int k, int top_dtype,
+                           const void* top, const int32_t* ids, float temperature, const float* weight, float grad_scale, float* loss,
+                           void* grad, int64_t ld_grad, cudaStream_t st);
 
 // gated_ffn.cu : gated feed-forward block
 struct FfnShape {

@@ -164,6 +164,36 @@ int sama_gated_ffn_grad(sama_ctx* ctx, int32_t dtype, int32_t act, int64_t n_tok
     return SAMA_OK;
 }
 
+int sama_distill(sama_ctx* ctx, int32_t dtype, int64_t n_rows, int32_t vocab, const void* logits, int64_t ld, int32_t k,
+                 int32_t top_dtype, const void* top_logits, const int32_t* top_ids, float temperature, const float* weight,
+                 float grad_scale, float* loss_out, void* grad, int64_t ld_grad, void* stream) {
+    if (!ctx) return SAMA_ERR_NULL;
+    if (n_rows < 0 || n_rows > kMaxTokens || vocab < 1 || vocab > (1 << 24) || k < 1 || k > 1024) return SAMA_ERR_SIZE;
+    if (!dtype_valid(dtype) || !dtype_valid(top_dtype) || !std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(grad_scale))
+        return SAMA_ERR_PARAM;
+    if (ld == 0) ld = vocab;
+    if (ld_grad == 0) ld_grad = vocab;
+    if (ld < vocab || ld > ((int64_t)1 << 30) || ld_grad < vocab || ld_grad > ((int64_t)1 << 30)) return SAMA_ERR_SIZE;
+    if (n_rows > 0 && (!logits || !top_logits || !top_ids)) return SAMA_ERR_NULL;
+    const size_t es = dtype_size(dtype), ts = dtype_size(top_dtype);
+    if (!aligned(logits, es) || !aligned(grad, es) || !aligned(top_logits, ts) || !aligned(top_ids, 4) || !aligned(weight, 4) || !aligned(loss_out, 4))
+        return SAMA_ERR_ALIGN;
+    const size_t n = (size_t)n_rows;
+    const size_t zb = n ? ((n - 1) * (size_t)ld + vocab) * es : 0, gb = n ? ((n - 1) * (size_t)ld_grad + vocab) * es : 0;
+    const Span ins[4] = {{logits, zb}, {top_logits, n * k * ts}, {top_ids, n * k * 4}, {weight, n * 4}};
+    for (int i = 0; i < 4; ++i) {
+        const bool in_place = i == 0 && grad == logits && ld == ld_grad;
+        if ((!in_place && overlaps(grad, gb, ins[i].p, ins[i].bytes)) || overlaps(loss_out, n * 4, ins[i].p, ins[i].bytes)) return SAMA_ERR_OVERLAP;
+    }
+    if (overlaps(grad, gb, loss_out, n * 4)) return SAMA_ERR_OVERLAP;
+    if (n_rows == 0 || (!grad && !loss_out)) return SAMA_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SAMA_ERR_CUDA;
+    SAMA_CUDA(ctx, launch_distill(ctx, dtype, n_rows, vocab, logits, ld, k, top_dtype, top_logits, top_ids, temperature, weight, grad_scale,
+                                  loss_out, grad, ld_grad, (cudaStream_t)stream));
+    return SAMA_OK;
+}
+
 int sama_last_ffn_path(sama_ctx* ctx, int32_t launch) { return ctx && launch >= 0 && launch < 5 ? ctx->ffn_path[launch] : 0; }
 
 }  // extern "C"
