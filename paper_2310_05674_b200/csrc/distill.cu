@@ -3,14 +3,16 @@
 //   p = softmax(u / T) over the kept entries,  q = softmax(z / T) over the vocabulary,
 //   loss = T^2 sum p (log p - log q),  grad = coef (q - p),  coef = grad_scale weight T
 //
-// The logits are read once and the gradient is written once, which is the floor: a row stays on the chip between its sum and
-// its gradient.  A team works on a row: a warp (rows up to 4 KB), a CTA of 256 (32 KB), or a cluster of up to 8 CTAs of 256
-// or 512 threads (256 KB, 512 KB) that exchange maximum and sum through distributed shared memory, one cluster barrier per
-// row.  Rows come by bulk copies into a ring of three, two of them ahead; each thread holds 8 vectors of 16 bytes as
-// exponentials in registers (one exponential per logit: at 4 bytes moved per 16-bit logit, two would take most of what the
-// special-function units can do), writes the gradient over them in shared memory, and bulk copies take it out.  The
-// teacher's entries are put right in shared memory before that.  Rows that do not start on 16 bytes have the elements at
-// their two ends read and written one by one.  Longer rows are read twice.
+// The logits are read once and the gradient is written once, which is the floor: a row stays in shared memory between its
+// sum and its gradient.  A row is a CTA's, or that of a cluster of up to 8 CTAs with 64 KB each; rows follow one another
+// through a ring, and the groups of warps of a CTA work on different rows at the same time:
+//   producer   bulk copies of the rows to come; the elements at the ends of rows that do not start on 16 bytes one by one
+//   sums       maximum and sum of exponentials of its part, sent to all CTAs of the cluster (distributed shared memory)
+//   entries    the teacher's distribution, the loss, and the gradient's values at the teacher's entries
+//   gradient   q in place of z, the entries' values over that, and bulk copies back
+// so that no group's barriers and latencies are in another's way; nothing but the arrival of the sums is waited for across
+// the cluster.  (All threads on one row at a time, with a cluster barrier per row, took three times as long.)
+// Rows of up to 4 KB are a warp's each; rows that no cluster can hold are read twice.
 #include <type_traits>
 
 #include "num_types.h"
@@ -21,10 +23,16 @@ namespace sama {
 
 namespace {
 
-constexpr int VECS = 8;        // vectors of a thread
-constexpr int STAGES = 3;
-constexpr int ENTRIES = 4;     // of the teacher's, of a thread
+constexpr int VECS = 8;               // 16-byte vectors that a thread has in hand
 constexpr int kMaxEntries = 1024;
+// one row per cluster or CTA
+constexpr int SUMS = 256, GRADS = 256, TEACHER = 128, THREADS = 32 + TEACHER + SUMS + GRADS;   // groups of threads
+constexpr int RING = 192 * 1024, MAX_STAGES = 8, MIN_STAGES = 3, PART = RING / MIN_STAGES;     // a CTA's part of a row, at most
+constexpr int PER_THREAD = kMaxEntries / TEACHER;
+constexpr int SMEM = RING + 2 * kMaxEntries * 8 + kMaxEntries * 8;
+// one row per warp
+constexpr int FEW_TEAMS = 8, FEW_STAGES = 3, FEW_ENTRIES = 4, FEW_CHUNK = 32 * VECS * 16, FEW_MOST = 32 * FEW_ENTRIES;
+constexpr int FEW_SMEM = FEW_TEAMS * (FEW_STAGES * FEW_CHUNK + FEW_MOST * 8);
 
 struct DistillParams {
     const void* logits;
@@ -36,10 +44,10 @@ struct DistillParams {
     float* loss;
     int32_t* status;
     int vocab, k, top_dtype;
+    int stages, stage_bytes;      // of the ring
+    int in_place;                 // the gradient replaces the logits
     float c, temperature, coef;   // log2 e / T, T, grad_scale T
 };
-
-template <typename T> __device__ __forceinline__ T lowest() { return from_float<T>(-INFINITY); }
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -95,151 +103,487 @@ struct Reduce {
 __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float sum_of(float a, float b) { return a + b; }
 
-template <int THREADS> constexpr int distill_smem() { return THREADS * VECS * 16 * STAGES + kMaxEntries * 8; }
+// A row's vectors [v0, v1) that a CTA has, those of them that lie wholly within it, and bytes before the row in the first.
+struct Span { int head, v0, v1, in0, in1; };
+__device__ __forceinline__ Span span_of(const uint8_t* row, int row_bytes, int rank, int ctas) {
+    Span s;
+    s.head = (int)(reinterpret_cast<uintptr_t>(row) & 15u);
+    const int n = (s.head + row_bytes + 15) / 16, per = ctas == 1 ? n : (n + ctas - 1) / ctas;
+    s.v0 = min(rank * per, n);
+    s.v1 = min(s.v0 + per, n);
+    s.in0 = max(s.v0, s.head ? 1 : 0);
+    s.in1 = max(s.in0, min(s.v1, (s.head + row_bytes) / 16));
+    return s;
+}
+// The vectors at a row's two ends that are not whole: thread t < VE has a place in the first, VE <= t < 2 VE in the last.
+// `place` in the CTA's vectors (-1: none), `element` in the row (outside it: nothing is there).
+template <int VE>
+__device__ __forceinline__ void edge_of(const Span& s, int row_bytes, int size, int t, int* place, int* element) {
+    const int last = (s.head + row_bytes) / 16, v = t < VE ? 0 : last;
+    const bool partial = t < VE ? s.head != 0 : (s.head + row_bytes) % 16 != 0 && !(last == 0 && s.head != 0);
+    *element = v * VE + t % VE - s.head / size;
+    *place = t < 2 * VE && partial && v >= s.v0 && v < s.v1 ? (v - s.v0) * VE + t % VE : -1;
+}
 
-// TEAM threads per row, or (CLUSTER) all CTAs of a cluster.
-template <typename T, int TEAM, int THREADS, bool CLUSTER>
-__global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 1)
+template <int BAR, int N> __device__ __forceinline__ void group_sync() { asm volatile("bar.sync %0, %1;" ::"n"(BAR), "n"(N) : "memory"); }
+
+// The largest of a vector's values (NaN aside).
+template <typename T> __device__ __forceinline__ float vec_max(uint4 x) {
+    if constexpr (sizeof(T) == 4) {
+        return fmaxf(fmaxf(__uint_as_float(x.x), __uint_as_float(x.y)), fmaxf(__uint_as_float(x.z), __uint_as_float(x.w)));
+    } else if constexpr (std::is_same<T, __half>::value) {
+        const __half2* h = reinterpret_cast<const __half2*>(&x);
+        const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+        return fmaxf(f.x, f.y);
+    } else {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&x);
+        const float2 f = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+        return fmaxf(f.x, f.y);
+    }
+}
+template <typename T> __device__ __forceinline__ uint4 vec_lowest() {
+    const uint32_t w = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
+    return make_uint4(w, w, w, w);
+}
+// (m, l) of two parts, each a maximum and the sum of 2^(c (z - maximum)): l as seen from `top`.
+__device__ __forceinline__ float rebase(float l, float m, float top, float c) { return m == -INFINITY ? l : l * fast_exp2((m - top) * c); }
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS, 1)
 distill_kernel(const DistillParams P) {
-    constexpr int VE = 16 / (int)sizeof(T), TEAMS = THREADS / TEAM, CHUNK = TEAM * VECS * 16, TEAM_ENTRIES = kMaxEntries / TEAMS;
-    static_assert(ENTRIES * TEAM >= TEAM_ENTRIES, "entries of a thread");
+    constexpr int VE = 16 / (int)sizeof(T), SIZE = (int)sizeof(T);
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t bars[TEAMS][STAGES];
-    __shared__ float2 slots[2][THREADS / 32];
-    __shared__ float2 peers[2][8];        // (maximum, sum) of the cluster's CTAs, rows in turn
-    const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM;
-    uint8_t* ring = smem + team * STAGES * CHUNK;
-    int32_t* e_id = reinterpret_cast<int32_t*>(smem + TEAMS * STAGES * CHUNK) + team * TEAM_ENTRIES;
-    float* e_p = reinterpret_cast<float*>(e_id - team * TEAM_ENTRIES + kMaxEntries) + team * TEAM_ENTRIES;
-    Reduce<TEAM> reduce{&slots[0][0]};
-    auto bar = [&](int s) { return smem_u32(&bars[team][s]); };
+    __shared__ __align__(8) uint64_t full[MAX_STAGES], empty[MAX_STAGES], stats[2 * MAX_STAGES], entries[2], taken[2];
+    __shared__ float2 peers[2 * MAX_STAGES][8];       // (maximum, sum) of the cluster's CTAs, by row
+    __shared__ float2 warp_sums[2][SUMS / 32];
+    __shared__ float teacher_slots[2][TEACHER / 32], row_coef[2];
+    __shared__ uint32_t abort_word;
+    volatile uint32_t* abort_flag = &abort_word;
+    int32_t* e_place = reinterpret_cast<int32_t*>(smem + RING);                  // [2][kMaxEntries]
+    float* e_value = reinterpret_cast<float*>(e_place + 2 * kMaxEntries);
+    int32_t* e_id = reinterpret_cast<int32_t*>(e_value + 2 * kMaxEntries);       // [kMaxEntries]
+    float* e_p = reinterpret_cast<float*>(e_id + kMaxEntries);
 
-    unsigned ctas = 1;
-    if (CLUSTER) asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
-    const int rank = CLUSTER ? (int)cluster_ctarank() : 0;
-    const int64_t first = CLUSTER ? blockIdx.x / ctas : (int64_t)blockIdx.x * TEAMS + team;
-    const int64_t stride = CLUSTER ? gridDim.x / ctas : (int64_t)gridDim.x * TEAMS;
-
-    if (t == 0) {
-        for (int s = 0; s < STAGES; ++s) mbar_init(bar(s), 1);
+    unsigned ctas_u;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas_u));
+    const int ctas = (int)ctas_u, rank = ctas > 1 ? (int)cluster_ctarank() : 0, S = P.stages;
+    const int64_t first = blockIdx.x / ctas_u, stride = gridDim.x / ctas_u;
+    const int n_rows = first < P.n_rows ? (int)((P.n_rows - first + stride - 1) / stride) : 0;   // of this cluster
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&empty[s]), 1 + TEACHER);
+        }
+        // (in place, no CTA writes before the loss has the logits that it needs)
+        for (int s = 0; s < 2 * S; ++s) mbar_init(smem_u32(&stats[s]), ctas + P.in_place);
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&entries[b]), TEACHER);
+            mbar_init(smem_u32(&taken[b]), 1);
+        }
+        abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    reduce.sync();
-    if (CLUSTER) cluster_sync();   // the other CTAs run before their shared memory is written
+    __syncthreads();
+    if (ctas > 1) cluster_sync();   // the other CTAs run before their shared memory is written
     pdl_trigger();
     pdl_wait();
 
-    const int row_bytes = P.vocab * (int)sizeof(T);
-    // This CTA's vectors [v0, v1) of a row, those of them that lie wholly within it, and bytes before the row in the first.
-    struct Span { int head, v0, v1, in0, in1; };
-    auto span_of = [&](const void* base, int64_t ld, int64_t row, int head_of) {
-        Span s;
-        s.head = head_of >= 0 ? head_of : (int)((reinterpret_cast<uintptr_t>(base) + (uintptr_t)(row * ld * (int64_t)sizeof(T))) & 15u);
-        const int n = (s.head + row_bytes + 15) / 16, per = CLUSTER ? (n + (int)ctas - 1) / (int)ctas : n;
-        s.v0 = min(rank * per, n);
-        s.v1 = min(s.v0 + per, n);
-        s.in0 = max(s.v0, s.head ? 1 : 0);
-        s.in1 = max(s.in0, min(s.v1, (s.head + row_bytes) / 16));
-        return s;
-    };
+    const int row_bytes = P.vocab * SIZE;
     const uint8_t* z_bytes = static_cast<const uint8_t*>(P.logits);
-    uint8_t* g_bytes = static_cast<uint8_t*>(P.grad);
-    auto row_at = [&](int64_t row) { return row * P.ld * (int64_t)sizeof(T); };
-
-    // Elements of the first and the last vector that is not whole: thread t < VE has one of the first, VE <= t < 2 VE of the last.
-    auto edge_at = [&](const Span& s, int* element) {   // place in this CTA's vectors, or -1
-        const int last = (s.head + row_bytes) / 16;
-        const int v = t < VE ? 0 : last;
-        *element = v * VE + t % VE - s.head / (int)sizeof(T);
-        const bool mine = t < 2 * VE && v >= s.v0 && v < s.v1 && *element >= 0 && *element < P.vocab &&
-                          (t < VE ? s.head != 0 : (s.head + row_bytes) % 16 != 0 && !(last == 0 && s.head != 0));
-        return mine ? (v - s.v0) * VE + t % VE : -1;
+    auto z_row = [&](int i) { return z_bytes + (first + i * stride) * P.ld * SIZE; };
+    auto chunk_of = [&](int s) { return smem + s * P.stage_bytes; };
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, int parity) {
+        if (ok && !mbar_wait(smem_u32(bar), (uint32_t)parity & 1u, abort_flag)) {
+            ok = false;
+            *abort_flag = 1;
+            atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
+        }
     };
+    // A row's maximum and sum over all CTAs; the same bits in each.
+    auto wait_stats = [&](int i, float* most, float* total) {
+        if (ok && !mbar_wait_cluster(smem_u32(&stats[i % (2 * S)]), (uint32_t)(i / (2 * S)) & 1u, abort_flag)) {
+            ok = false;
+            *abort_flag = 1;
+            atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
+        }
+        const volatile float2* p = peers[i % (2 * S)];
+        float m = -INFINITY, l = 0.f;
+        for (int r = 0; r < ctas; ++r) m = fmaxf(m, p[r].x);
+        for (int r = 0; r < ctas; ++r) l += rebase(p[r].y, p[r].x, m, P.c);
+        *most = m;
+        *total = l;
+    };
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+    if (warp == 0) {
+        // ---------------------------------------------------------- producer
+        auto edge = [&](int i, int* place) {
+            const uint8_t* row = z_row(i);
+            int element;
+            edge_of<VE>(span_of(row, row_bytes, rank, ctas), row_bytes, SIZE, lane, place, &element);
+            return *place >= 0 && element >= 0 && element < P.vocab ? reinterpret_cast<const T*>(row)[element] : from_float<T>(-INFINITY);
+        };
+        int place = -1, next_place = -1, i = 0;
+        T at_edge = n_rows > 0 ? edge(0, &place) : from_float<T>(0.f);
+        for (; i < n_rows && __all_sync(0xffffffffu, ok); ++i) {
+            const int s = i % S;
+            const T next_edge = i + 1 < n_rows ? edge(i + 1, &next_place) : from_float<T>(0.f);
+            if (i >= S) wait(&empty[s], i / S - 1);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            uint8_t* chunk = chunk_of(s);
+            if (place >= 0) reinterpret_cast<T*>(chunk)[place] = at_edge;
+            __syncwarp();
+            if (lane == 0) {
+                const uint8_t* row = z_row(i);
+                const Span sp = span_of(row, row_bytes, rank, ctas);
+                const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u;
+                mbar_expect_tx(smem_u32(&full[s]), bytes);
+                if (bytes) bulk_load(smem_u32(chunk + (sp.in0 - sp.v0) * 16), row - sp.head + (int64_t)sp.in0 * 16, bytes, smem_u32(&full[s]));
+            }
+            at_edge = next_edge;
+            place = next_place;
+        }
+        if (*abort_flag && lane == 0)
+            // let the copies already issued land before the CTA's shared memory goes away
+            for (int k = max(0, i - S); k < i; ++k) mbar_wait(smem_u32(&full[k % S]), (uint32_t)(k / S) & 1u);
+        __syncwarp();
+    } else if (warp <= TEACHER / 32) {
+        // ---------------------------------------------------------- the teacher's entries
+        const int t = threadIdx.x - 32, w = t / 32;
+        int32_t id[PER_THREAD], next_id[PER_THREAD];
+        float u[PER_THREAD], z[PER_THREAD], next_u[PER_THREAD];
+        float weight = 1.f, next_weight = 1.f;
+        auto fetch = [&](int i) {
+            const int64_t row = first + i * stride;
+#pragma unroll
+            for (int e = 0; e < PER_THREAD; ++e) {
+                const int j = t + e * TEACHER;
+                next_id[e] = -1;
+                if (j < P.k) {
+                    next_id[e] = P.ids[row * P.k + j];
+                    next_u[e] = load_top(P, row * P.k + j);
+                }
+            }
+            if (P.weight) next_weight = P.weight[row];
+        };
+        auto take = [&](int i) {   // the entries fetched last become the current ones; their logits are fetched
+            const T* row = reinterpret_cast<const T*>(z_row(i));
+#pragma unroll
+            for (int e = 0; e < PER_THREAD; ++e) {
+                if (e * TEACHER >= P.k) continue;
+                id[e] = next_id[e];
+                if (id[e] < -1 || id[e] >= P.vocab) {
+                    atomicOr(P.status, (int)SAMA_DEV_BAD_INDEX);
+                    id[e] = -1;
+                }
+                u[e] = id[e] >= 0 ? next_u[e] : -INFINITY;
+                z[e] = id[e] >= 0 ? to_float(row[id[e]]) : 0.f;
+            }
+            weight = next_weight;
+        };
+        auto reduce = [&](float x, int slot, auto f) {   // a barrier lies between two uses of a slot
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) x = f(x, __shfl_xor_sync(0xffffffffu, x, o));
+            if (lane == 0) teacher_slots[slot][w] = x;
+            group_sync<1, TEACHER>();
+            x = teacher_slots[slot][0];
+#pragma unroll
+            for (int v = 1; v < TEACHER / 32; ++v) x = f(x, teacher_slots[slot][v]);
+            return x;
+        };
+        if (n_rows > 0) {
+            fetch(0);
+            take(0);
+        }
+        for (int i = 0; i < n_rows; ++i) {
+            const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
+            if (i + 1 < n_rows) fetch(i + 1);
+            float top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < PER_THREAD; ++e) {
+                if (e * TEACHER >= P.k) continue;
+                top = fmaxf(top, u[e]);
+                e_id[t + e * TEACHER] = id[e];
+            }
+            top = reduce(top, 0, max_of);
+            if (P.in_place && rank == 0 && t < ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&stats[i % (2 * S)]), (uint32_t)t));
+            const float from_u = top == -INFINITY ? 0.f : top * P.c;
+            float p[PER_THREAD], sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < PER_THREAD; ++e) {
+                if (e * TEACHER >= P.k) continue;
+                u[e] = fmaf(u[e], P.c, -from_u);   // log2 of p, up to the sum
+                p[e] = exp2f(u[e]);
+                sum += p[e];
+                e_p[t + e * TEACHER] = p[e];
+            }
+            sum = reduce(sum, 1, sum_of);
+            const bool none = sum == 0.f;
+            const float inv_u = none ? 0.f : 1.f / sum, log_u = log2f(sum), coef = P.coef * weight;
+            const bool zero = none || weight == 0.f;
+            // of several entries with one id the first takes them all
+            const int skip = sp.head / SIZE - sp.v0 * VE, places = (sp.v1 - sp.v0) * VE;
+            float all[PER_THREAD];
+            int place[PER_THREAD];
+#pragma unroll
+            for (int e = 0; e < PER_THREAD; ++e) {
+                if (e * TEACHER >= P.k) continue;
+                const int j = t + e * TEACHER;
+                place[e] = id[e] >= 0 ? id[e] + skip : -1;
+                if (place[e] >= places || zero || !P.grad) place[e] = -1;
+                all[e] = 0.f;
+                if (place[e] < 0) continue;
+                for (int x = 0; x < P.k; x += 4) {   // (what lies behind the last entry, up to a multiple of 128, has id -1)
+                    const int4 four = *reinterpret_cast<const int4*>(e_id + x);
+                    const int32_t ids[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        if (ids[y] == id[e]) {
+                            all[e] += e_p[x + y];
+                            if (x + y < j) place[e] = -1;
+                        }
+                }
+            }
+            float most, total;
+            wait_stats(i, &most, &total);
+            if (P.grad && i >= 2) wait(&taken[i & 1], i / 2 - 1);
+            const float whole = most == -INFINITY ? 0.f : most * P.c, inv = 1.f / total, log_total = log2f(total);
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < PER_THREAD; ++e) {
+                if (e * TEACHER >= P.k) continue;
+                const float log_q = fmaf(z[e], P.c, -whole);           // log2 of q, up to the sum
+                const float pe = p[e] * inv_u;
+                if (id[e] >= 0 && !(pe == 0.f)) part += pe * ((u[e] - log_u) - ((z[e] - (most == -INFINITY ? 0.f : most)) * P.c - log_total));
+                e_place[(i & 1) * kMaxEntries + t + e * TEACHER] = place[e];
+                e_value[(i & 1) * kMaxEntries + t + e * TEACHER] = coef * (fast_exp2(log_q) * inv - all[e] * inv_u);
+            }
+            if (t == 0) {
+                row_coef[i & 1] = coef * inv;
+                if (zero) e_place[(i & 1) * kMaxEntries] = -2;   // zeros, whatever the logits
+            }
+            mbar_arrive(smem_u32(&entries[i & 1]));
+            mbar_arrive(smem_u32(&empty[i % S]));
+            if (i + 1 < n_rows) take(i + 1);
+            if (P.loss && rank == 0) {
+                part = reduce(part, 0, sum_of);
+                if (t == 0) P.loss[first + i * stride] = none ? 0.f : P.temperature * P.temperature * 0.69314718f * part;
+            }
+            group_sync<1, TEACHER>();   // the entries may be written again
+        }
+    } else if (warp <= (TEACHER + SUMS) / 32) {
+        // ---------------------------------------------------------- maxima and sums
+        const int t = threadIdx.x - 32 - TEACHER;
+        for (int i = 0; i < n_rows; ++i) {
+            const int s = i % S;
+            const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
+            const int n = sp.v1 - sp.v0;
+            wait(&full[s], i / S);
+            const uint4* chunk = reinterpret_cast<const uint4*>(chunk_of(s));
+            float m = -INFINITY, l = 0.f;
+            for (int b = t; b < n; b += SUMS * VECS) {
+                uint4 x[VECS];
+                float top = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < VECS; ++v) x[v] = b + v * SUMS < n ? chunk[b + v * SUMS] : vec_lowest<T>();
+#pragma unroll
+                for (int v = 0; v < VECS; ++v) top = fmaxf(top, vec_max<T>(x[v]));
+                if (top > m) {
+                    l = m == -INFINITY ? l : l * fast_exp2((m - top) * P.c);
+                    m = top;
+                }
+                const float from = m == -INFINITY ? 0.f : m * P.c;
+#pragma unroll
+                for (int v = 0; v < VECS; ++v) {
+                    float f[VE], sum = 0.f;
+                    unpack_vec<T>(x[v], f);
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) sum += fast_exp2(fmaf(f[e], P.c, -from));
+                    l += sum;
+                }
+            }
+            float top = m;
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            l = rebase(l, m, top, P.c);
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) l += __shfl_xor_sync(0xffffffffu, l, o);
+            if (lane == 0) warp_sums[i & 1][t / 32] = make_float2(top, l);
+            group_sync<2, SUMS>();
+            if (t < ctas) {
+                float most = -INFINITY, total = 0.f;
+#pragma unroll
+                for (int w = 0; w < SUMS / 32; ++w) most = fmaxf(most, warp_sums[i & 1][w].x);
+#pragma unroll
+                for (int w = 0; w < SUMS / 32; ++w) total += rebase(warp_sums[i & 1][w].y, warp_sums[i & 1][w].x, most, P.c);
+                const int slot = i % (2 * S);
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_rank(smem_u32(&peers[slot][rank]), (uint32_t)t)), "f"(most), "f"(total) : "memory");
+                mbar_arrive_cluster(map_to_rank(smem_u32(&stats[slot]), (uint32_t)t));
+            }
+            if (!P.grad && t == 0) mbar_arrive(smem_u32(&empty[s]));
+        }
+    } else if (P.grad) {
+        // ---------------------------------------------------------- gradients
+        const int t = threadIdx.x - 32 - TEACHER - SUMS;
+        for (int i = 0; i < n_rows; ++i) {
+            const int s = i % S;
+            const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
+            const int n = sp.v1 - sp.v0;
+            uint8_t* chunk = chunk_of(s);
+            float most, total;
+            wait_stats(i, &most, &total);
+            wait(&entries[i & 1], i / 2);
+            const volatile int32_t* places = e_place + (i & 1) * kMaxEntries;
+            const bool zero = places[0] == -2;
+            const float f = row_coef[i & 1], whole = most == -INFINITY ? 0.f : most * P.c;
+#pragma unroll 4
+            for (int b = t; b < n; b += GRADS) {
+                float g[VE];
+                unpack_vec<T>(reinterpret_cast<const uint4*>(chunk)[b], g);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) g[e] = zero ? 0.f : fast_exp2(fmaf(g[e], P.c, -whole)) * f;
+                store_n<T, VE>(reinterpret_cast<T*>(chunk) + b * VE, g);
+            }
+            group_sync<3, GRADS>();
+            if (!zero)
+                for (int j = t; j < P.k; j += GRADS) {
+                    const int place = places[j];
+                    if (place >= 0) reinterpret_cast<T*>(chunk)[place] = from_float<T>(e_value[(i & 1) * kMaxEntries + j]);
+                }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            group_sync<3, GRADS>();
+            uint8_t* g_row = static_cast<uint8_t*>(P.grad) + (first + i * stride) * P.ld_grad * SIZE;
+            const bool alike = (int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == sp.head;
+            if (t == 0) {
+                mbar_arrive(smem_u32(&taken[i & 1]));
+                const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u;
+                if (alike && bytes) bulk_store(g_row - sp.head + (int64_t)sp.in0 * 16, smem_u32(chunk + (sp.in0 - sp.v0) * 16), bytes);
+                // the row before this has left its place
+                asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 1;" ::: "memory");
+                if (i > 0) mbar_arrive(smem_u32(&empty[(i - 1) % S]));
+            }
+            if (alike) {
+                int place, element;
+                edge_of<VE>(sp, row_bytes, SIZE, t, &place, &element);
+                if (place >= 0 && element >= 0 && element < P.vocab) reinterpret_cast<T*>(g_row)[element] = reinterpret_cast<const T*>(chunk)[place];
+            } else {
+                // rows of the gradient start elsewhere than those of the logits
+                const int skip = sp.head / SIZE - sp.v0 * VE, e0 = max(0, -skip), e1 = min(P.vocab, n * VE - skip);
+                for (int e = e0 + t; e < e1; e += GRADS) reinterpret_cast<T*>(g_row)[e] = reinterpret_cast<const T*>(chunk)[e + skip];
+            }
+        }
+        if (t == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncthreads();
+    if (ctas > 1) cluster_sync();   // no CTA leaves while another may write to it
+}
+
+// A row per warp: rows of up to 4 KB and teachers of up to 128 entries.  Each thread holds 8 vectors as exponentials.
+template <typename T>
+__global__ void __launch_bounds__(32 * FEW_TEAMS, 2)
+distill_few_kernel(const DistillParams P) {
+    constexpr int VE = 16 / (int)sizeof(T), SIZE = (int)sizeof(T);
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t bars[FEW_TEAMS][FEW_STAGES];
+    const int team = threadIdx.x / 32, t = threadIdx.x % 32;
+    uint8_t* ring = smem + team * FEW_STAGES * FEW_CHUNK;
+    int32_t* e_id = reinterpret_cast<int32_t*>(smem + FEW_TEAMS * FEW_STAGES * FEW_CHUNK) + team * FEW_MOST;
+    float* e_p = reinterpret_cast<float*>(smem + FEW_TEAMS * (FEW_STAGES * FEW_CHUNK + FEW_MOST * 4)) + team * FEW_MOST;
+    auto bar = [&](int s) { return smem_u32(&bars[team][s]); };
+    const int64_t first = (int64_t)blockIdx.x * FEW_TEAMS + team, stride = (int64_t)gridDim.x * FEW_TEAMS;
+    if (t == 0) {
+        for (int s = 0; s < FEW_STAGES; ++s) mbar_init(bar(s), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    pdl_trigger();
+    pdl_wait();
+    auto over = [](float x, auto f) {
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) x = f(x, __shfl_xor_sync(0xffffffffu, x, o));
+        return x;
+    };
+
+    const int row_bytes = P.vocab * SIZE;
+    const uint8_t* z_bytes = static_cast<const uint8_t*>(P.logits);
+    auto z_row = [&](int64_t row) { return z_bytes + row * P.ld * SIZE; };
     // What a thread has at hand of a row before its turn comes: an element at the row's end, and entries of the teacher.
-    float edge = 0.f;
-    int32_t id[ENTRIES];
-    float u[ENTRIES], z[ENTRIES];
+    T edge = from_float<T>(0.f);
+    int32_t id[FEW_ENTRIES];
+    float u[FEW_ENTRIES], z[FEW_ENTRIES], weight = 1.f;
     auto fetch_row = [&](int64_t row, int stage) {
-        const Span s = span_of(P.logits, P.ld, row, -1);
+        const Span s = span_of(z_row(row), row_bytes, 0, 1);
         if (t == 0) {
             const uint32_t bytes = (uint32_t)(s.in1 - s.in0) * 16u;
             mbar_expect_tx(bar(stage), bytes);
-            if (bytes) bulk_load(smem_u32(ring + stage * CHUNK + (s.in0 - s.v0) * 16), z_bytes + row_at(row) - s.head + (int64_t)s.in0 * 16, bytes, bar(stage));
+            if (bytes) bulk_load(smem_u32(ring + stage * FEW_CHUNK + s.in0 * 16), z_row(row) - s.head + s.in0 * 16, bytes, bar(stage));
         }
     };
     auto fetch_entries = [&](int64_t row) {
-        const Span s = span_of(P.logits, P.ld, row, -1);
-        int element;
-        if (edge_at(s, &element) >= 0) edge = to_float(reinterpret_cast<const T*>(z_bytes + row_at(row))[element]);
+        int place, element;
+        edge_of<VE>(span_of(z_row(row), row_bytes, 0, 1), row_bytes, SIZE, t, &place, &element);
+        edge = place >= 0 && element >= 0 && element < P.vocab ? reinterpret_cast<const T*>(z_row(row))[element] : from_float<T>(-INFINITY);
 #pragma unroll
-        for (int i = 0; i < ENTRIES; ++i) {
-            const int j = t + i * TEAM;
+        for (int i = 0; i < FEW_ENTRIES; ++i) {
+            const int j = t + i * 32;
             id[i] = j < P.k ? P.ids[row * P.k + j] : -1;
             u[i] = j < P.k ? load_top(P, row * P.k + j) : -INFINITY;
         }
+        if (P.weight) weight = P.weight[row];
     };
     auto fetch_targets = [&](int64_t row) {
 #pragma unroll
-        for (int i = 0; i < ENTRIES; ++i) {
+        for (int i = 0; i < FEW_ENTRIES; ++i) {
             if (id[i] < -1 || id[i] >= P.vocab) {
                 atomicOr(P.status, (int)SAMA_DEV_BAD_INDEX);
                 id[i] = -1;
             }
             if (id[i] < 0) u[i] = -INFINITY;
-            z[i] = id[i] >= 0 ? to_float(reinterpret_cast<const T*>(z_bytes + row_at(row))[id[i]]) : 0.f;
+            z[i] = id[i] >= 0 ? to_float(reinterpret_cast<const T*>(z_row(row))[id[i]]) : 0.f;
         }
     };
 
-    for (int i = 0; i < STAGES - 1; ++i)
+    for (int i = 0; i < FEW_STAGES - 1; ++i)
         if (first + i * stride < P.n_rows) fetch_row(first + i * stride, i);
     if (first < P.n_rows) {
         fetch_entries(first);
         fetch_targets(first);
     }
-    int stage = 0, parity = 0, turn = 0;
+    int stage = 0, parity = 0;
     bool timed_out = false;
     for (int64_t row = first; row < P.n_rows; row += stride) {
-        const Span s = span_of(P.logits, P.ld, row, -1);
-        uint8_t* chunk = ring + stage * CHUNK;
+        const Span s = span_of(z_row(row), row_bytes, 0, 1);
+        const int n = s.v1;
+        uint8_t* chunk = ring + stage * FEW_CHUNK;
         if (!mbar_wait(bar(stage), (uint32_t)parity)) timed_out = true;
-        // the row's ends: its own elements there, and nothing beside them
-        const int n = s.v1 - s.v0;
-        if (t < 2 * VE) {
-            const int last = (s.head + row_bytes) / 16, v = t < VE ? 0 : last;
-            const bool partial = t < VE ? s.head != 0 : (s.head + row_bytes) % 16 != 0 && !(last == 0 && s.head != 0);
-            int element;
-            const int place = edge_at(s, &element);
-            if (partial && v >= s.v0 && v < s.v1) reinterpret_cast<T*>(chunk)[(v - s.v0) * VE + t % VE] = place >= 0 ? from_float<T>(edge) : lowest<T>();
-        }
-        float my_u[ENTRIES], my_z[ENTRIES], top_u = -INFINITY;
-        int32_t my_id[ENTRIES];
+        int place, element;
+        edge_of<VE>(s, row_bytes, SIZE, t, &place, &element);
+        if (place >= 0) reinterpret_cast<T*>(chunk)[place] = edge;
+        float my_u[FEW_ENTRIES], my_z[FEW_ENTRIES], top_u = -INFINITY;
+        int32_t my_id[FEW_ENTRIES];
 #pragma unroll
-        for (int i = 0; i < ENTRIES; ++i) {
+        for (int i = 0; i < FEW_ENTRIES; ++i) {
             my_id[i] = id[i];
             my_u[i] = u[i];
             my_z[i] = z[i];
             top_u = fmaxf(top_u, u[i]);
         }
+        const float my_weight = weight;
         const bool more = row + stride < P.n_rows;
         if (more) fetch_entries(row + stride);
-        const float weight = P.weight ? P.weight[row] : 1.f;
-        reduce.sync();
+        __syncwarp();
 
         float v[VECS * VE], top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < VECS; ++i) {
-            const int at = t + i * TEAM;
-            if (at < n) {
-                unpack_vec<T>(reinterpret_cast<const uint4*>(chunk)[at], v + i * VE);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VE; ++e) v[i * VE + e] = -INFINITY;
-            }
+            const uint4 x = t + i * 32 < n ? reinterpret_cast<const uint4*>(chunk)[t + i * 32] : vec_lowest<T>();
+            top = fmaxf(top, vec_max<T>(x));
+            unpack_vec<T>(x, v + i * VE);
         }
-#pragma unroll
-        for (int i = 0; i < VECS * VE; ++i) top = fmaxf(top, v[i]);
-        const float2 tops = reduce(top, top_u, max_of);
-        const float from = tops.x == -INFINITY ? 0.f : tops.x * P.c, from_u = tops.y == -INFINITY ? 0.f : tops.y * P.c;
+        top = over(top, max_of);
+        top_u = over(top_u, max_of);
+        const float from = top == -INFINITY ? 0.f : top * P.c, from_u = top_u == -INFINITY ? 0.f : top_u * P.c;
         float sum = 0.f, sum_u = 0.f;
 #pragma unroll
         for (int i = 0; i < VECS * VE; ++i) {
@@ -247,71 +591,46 @@ distill_kernel(const DistillParams P) {
             sum += v[i];
         }
 #pragma unroll
-        for (int i = 0; i < ENTRIES; ++i) {
+        for (int i = 0; i < FEW_ENTRIES; ++i) {
             my_u[i] = fmaf(my_u[i], P.c, -from_u);       // log2 of p, up to the sum
             sum_u += exp2f(my_u[i]);
         }
-        const float2 sums = reduce(sum, sum_u, sum_of);
-        float most = tops.x, total = sums.x;
-        if (CLUSTER) {
-            const uint32_t mine = smem_u32(&peers[turn][rank]);
-            if (t < (int)ctas)
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_rank(mine, (uint32_t)t)), "f"(tops.x), "f"(sums.x) : "memory");
-            cluster_sync();
-            most = -INFINITY;
-            for (int r = 0; r < (int)ctas; ++r) most = fmaxf(most, peers[turn][r].x);
-            total = 0.f;
-            for (int r = 0; r < (int)ctas; ++r) {
-                const float2 ml = peers[turn][r];
-                total += ml.x == -INFINITY ? 0.f : ml.y * fast_exp2((ml.x - most) * P.c);
-            }
-            turn ^= 1;
-        }
-        const float whole = most == -INFINITY ? 0.f : most * P.c, inv = 1.f / total, inv_u = sums.y > 0.f ? 1.f / sums.y : 0.f;
-        const bool none = !(sums.y > 0.f) && sums.y == sums.y;      // no entry
-        const float log_total = logf(total), log_u = log2f(sums.y);
-        // the loss, by the first CTA
-        float part = 0.f;
-        const bool has_loss = P.loss && rank == 0;
-        if (has_loss) {
+        sum = over(sum, sum_of);
+        sum_u = over(sum_u, sum_of);
+        const bool none = sum_u == 0.f;                  // no entry
+        const float inv = 1.f / sum, inv_u = none ? 0.f : 1.f / sum_u, log_total = log2f(sum), log_u = log2f(sum_u);
+        if (P.loss) {
+            float part = 0.f;
 #pragma unroll
-            for (int i = 0; i < ENTRIES; ++i) {
+            for (int i = 0; i < FEW_ENTRIES; ++i) {
                 const float p = exp2f(my_u[i]) * inv_u;
-                const float log_q = (my_z[i] - (most == -INFINITY ? 0.f : most)) / P.temperature - log_total;
-                if (my_id[i] >= 0 && !(p == 0.f)) part += p * ((my_u[i] - log_u) * 0.69314718f - log_q);
+                if (my_id[i] >= 0 && !(p == 0.f)) part += p * ((my_u[i] - log_u) - ((my_z[i] - (top == -INFINITY ? 0.f : top)) * P.c - log_total));
             }
-            part = reduce(part, 0.f, sum_of).x;
-            if (t == 0) P.loss[row] = none ? 0.f : P.temperature * P.temperature * part;
+            part = over(part, sum_of);
+            if (t == 0) P.loss[row] = none ? 0.f : P.temperature * P.temperature * 0.69314718f * part;
         }
         if (P.grad) {
-            const float coef = none ? 0.f : P.coef * weight;
-            const bool zero = none || weight == 0.f;
-            const float f = coef * (CLUSTER && tops.x != -INFINITY ? fast_exp2((tops.x - most) * P.c) * inv : inv);
+            const float coef = P.coef * my_weight, f = coef * inv;
+            const bool zero = none || my_weight == 0.f;
 #pragma unroll
-            for (int i = 0; i < VECS; ++i) {
-                const int at = t + i * TEAM;
-                if (at < n) {
+            for (int i = 0; i < VECS; ++i)
+                if (t + i * 32 < n) {
                     float g[VE];
 #pragma unroll
                     for (int e = 0; e < VE; ++e) g[e] = zero ? 0.f : v[i * VE + e] * f;
-                    store_n<T, VE>(reinterpret_cast<T*>(chunk) + at * VE, g);
+                    store_n<T, VE>(reinterpret_cast<T*>(chunk) + (t + i * 32) * VE, g);
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < ENTRIES; ++i) {
-                const int j = t + i * TEAM;
-                if (j < TEAM_ENTRIES) {
-                    e_id[j] = my_id[i];
-                    e_p[j] = exp2f(my_u[i]) * inv_u;
-                }
+            for (int i = 0; i < FEW_ENTRIES; ++i) {
+                e_id[t + i * 32] = my_id[i];
+                e_p[t + i * 32] = exp2f(my_u[i]) * inv_u;
             }
-            reduce.sync();
+            __syncwarp();
             // the teacher's entries; of several with one id the first takes them all
 #pragma unroll
-            for (int i = 0; i < ENTRIES; ++i) {
-                const int place = my_id[i] + s.head / (int)sizeof(T) - s.v0 * VE;
-                if (zero || my_id[i] < 0 || place < 0 || place >= n * VE) continue;
-                const int j = t + i * TEAM;
+            for (int i = 0; i < FEW_ENTRIES; ++i) {
+                const int j = t + i * 32;
+                if (zero || my_id[i] < 0) continue;
                 float p = 0.f;
                 bool is_first = true;
                 for (int x = 0; x < P.k; x += 4) {
@@ -324,39 +643,32 @@ distill_kernel(const DistillParams P) {
                             is_first = is_first && x + e >= j;
                         }
                 }
-                if (is_first) reinterpret_cast<T*>(chunk)[place] = from_float<T>(coef * (fast_exp2(fmaf(my_z[i], P.c, -whole)) * inv - p));
+                if (is_first) reinterpret_cast<T*>(chunk)[my_id[i] + s.head / SIZE] = from_float<T>(coef * (fast_exp2(fmaf(my_z[i], P.c, -from)) * inv - p));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            reduce.sync();
-            uint8_t* g_row = g_bytes + row * P.ld_grad * (int64_t)sizeof(T);
+            __syncwarp();
+            uint8_t* g_row = static_cast<uint8_t*>(P.grad) + row * P.ld_grad * SIZE;
             if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == s.head) {
-                if (t == 0) {
-                    const uint32_t bytes = (uint32_t)(s.in1 - s.in0) * 16u;
-                    if (bytes) bulk_store(g_row - s.head + (int64_t)s.in0 * 16, smem_u32(chunk + (s.in0 - s.v0) * 16), bytes);
-                }
-                int element;
-                const int place = edge_at(s, &element);
-                if (place >= 0) reinterpret_cast<T*>(g_row)[element] = reinterpret_cast<const T*>(chunk)[place];
+                const uint32_t bytes = (uint32_t)(s.in1 - s.in0) * 16u;
+                if (t == 0 && bytes) bulk_store(g_row - s.head + s.in0 * 16, smem_u32(chunk + s.in0 * 16), bytes);
+                if (place >= 0 && element >= 0 && element < P.vocab) reinterpret_cast<T*>(g_row)[element] = reinterpret_cast<const T*>(chunk)[place];
             } else {
                 // rows of the gradient start elsewhere than those of the logits
-                const int skip = s.head / (int)sizeof(T) - s.v0 * VE;
-                const int e0 = max(0, -skip), e1 = min(P.vocab, n * VE - skip);
-                for (int e = e0 + t; e < e1; e += TEAM) reinterpret_cast<T*>(g_row)[e] = reinterpret_cast<const T*>(chunk)[e + skip];
-                reduce.sync();
+                for (int e = t; e < P.vocab; e += 32) reinterpret_cast<T*>(g_row)[e] = reinterpret_cast<const T*>(chunk)[e + s.head / SIZE];
+                __syncwarp();
             }
         }
         if (t == 0) asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 1;" ::: "memory");
         // the row after the next takes the place of the one before this, whose gradient has left it
-        const int64_t after = row + (STAGES - 1) * stride;
-        if (after < P.n_rows) fetch_row(after, (stage + STAGES - 1) % STAGES);
+        const int64_t after = row + (FEW_STAGES - 1) * stride;
+        if (after < P.n_rows) fetch_row(after, (stage + FEW_STAGES - 1) % FEW_STAGES);
         if (more) fetch_targets(row + stride);
-        if (++stage == STAGES) { stage = 0; parity ^= 1; }
+        if (++stage == FEW_STAGES) { stage = 0; parity ^= 1; }
     }
     if (t == 0) {
         if (timed_out) atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
-    if (CLUSTER) cluster_sync();   // no CTA leaves while another may write to it
 }
 
 // Rows that no cluster can hold: one CTA per row, read once for the sum and once for the gradient.
@@ -431,36 +743,61 @@ distill_long_kernel(const DistillParams P) {
     }
 }
 
-template <typename T, int TEAM, int THREADS, bool CLUSTER>
-cudaError_t launch(sama_ctx* ctx, const DistillParams& P, int cluster, cudaStream_t st) {
-    auto* kernel = distill_kernel<T, TEAM, THREADS, CLUSTER>;
-    constexpr int SMEM = distill_smem<THREADS>();
-    const uint32_t bit = 1u << ((std::is_same<T, float>::value ? 0 : std::is_same<T, __half>::value ? 4 : 8) +
-                                (TEAM == 32 ? 0 : !CLUSTER ? 1 : THREADS == 256 ? 2 : 3));
-    if (!(ctx->distill_ready & bit)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-        if (e != cudaSuccess) return e;
-        ctx->distill_ready |= bit;
+// Once per context: how many clusters of 2, 4 and 8 CTAs can be resident.
+cudaError_t prepare(sama_ctx* ctx) {
+    if (ctx->distill_clusters[0] > 0) return cudaSuccess;
+    void* kernels[3] = {(void*)distill_kernel<float>, (void*)distill_kernel<__half>, (void*)distill_kernel<__nv_bfloat16>};
+    void* few[3] = {(void*)distill_few_kernel<float>, (void*)distill_few_kernel<__half>, (void*)distill_few_kernel<__nv_bfloat16>};
+    cudaError_t e;
+    for (int i = 0; i < 3; ++i) {
+        if ((e = cudaFuncSetAttribute(kernels[i], cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM)) != cudaSuccess) return e;
+        if ((e = cudaFuncSetAttribute(few[i], cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM)) != cudaSuccess) return e;
     }
-    const int most = (THREADS == 256 ? 2 : 1) * ctx->sm_count / cluster;            // teams that are resident, or a little more
-    const int64_t wanted = CLUSTER ? P.n_rows : (P.n_rows + THREADS / TEAM - 1) / (THREADS / TEAM);
-    const int64_t teams = wanted < most ? wanted : most;
-    KernelScope scope(ctx, SAMA_K_DISTILL, -1, st);
-    return launch_clustered(CLUSTER ? cluster : 1, kernel, dim3((unsigned)(teams * cluster)), dim3(THREADS), SMEM, st, P);
+    int found[3];
+    for (int i = 0; i < 3; ++i) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = 2u << i;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3(ctx->sm_count / (2 << i) * (2 << i));
+        cfg.blockDim = dim3(THREADS);
+        cfg.dynamicSmemBytes = SMEM;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if ((e = cudaOccupancyMaxActiveClusters(&found[i], distill_kernel<__nv_bfloat16>, &cfg)) != cudaSuccess) return e;
+        if (found[i] < 1) return cudaErrorLaunchOutOfResources;
+    }
+    for (int i = 2; i >= 0; --i) ctx->distill_clusters[i] = found[i];
+    return cudaSuccess;
 }
 
 template <typename T>
-cudaError_t launch(sama_ctx* ctx, const DistillParams& P, cudaStream_t st) {
-    // vectors of a row, wherever it starts
-    const int64_t vecs = ((int64_t)P.vocab * (int)sizeof(T) + 15 + 15) / 16;
-    if (vecs <= 32 * VECS && P.k <= kMaxEntries / 8) return launch<T, 32, 256, false>(ctx, P, 1, st);
-    if (vecs <= 256 * VECS) return launch<T, 256, 256, false>(ctx, P, 1, st);
-    for (int n = 2; n <= 8; n *= 2)
-        if (vecs <= (int64_t)256 * VECS * n) return launch<T, 256, 256, true>(ctx, P, n, st);
-    if (vecs <= (int64_t)512 * VECS * 8) return launch<T, 512, 512, true>(ctx, P, 8, st);
+cudaError_t launch(sama_ctx* ctx, DistillParams& P, cudaStream_t st) {
+    constexpr int SIZE = (int)sizeof(T);
+    // vectors of a row: one more where rows do not all start on 16 bytes
+    const bool whole = reinterpret_cast<uintptr_t>(P.logits) % 16 == 0 && (P.n_rows == 1 || P.ld * SIZE % 16 == 0);
+    const int64_t vecs = ((int64_t)P.vocab * SIZE + (whole ? 0 : 16 - SIZE) + 15) / 16;
     KernelScope scope(ctx, SAMA_K_DISTILL, -1, st);
-    const int64_t most = 2 * ctx->sm_count;
-    return launch_dependent(distill_long_kernel<T>, dim3((unsigned)(P.n_rows < most ? P.n_rows : most)), dim3(1024), 0, st, P);
+    if (vecs * 16 <= FEW_CHUNK && P.k <= FEW_MOST) {
+        const int64_t wanted = (P.n_rows + FEW_TEAMS - 1) / FEW_TEAMS, most = 2 * ctx->sm_count;
+        return launch_dependent(distill_few_kernel<T>, dim3((unsigned)(wanted < most ? wanted : most)), dim3(32 * FEW_TEAMS), FEW_SMEM, st, P);
+    }
+    if (vecs * 16 > 8 * PART) {
+        const int64_t most = 2 * ctx->sm_count;
+        return launch_dependent(distill_long_kernel<T>, dim3((unsigned)(P.n_rows < most ? P.n_rows : most)), dim3(1024), 0, st, P);
+    }
+    // The fewest CTAs that can hold a row, since each of them has a row's fixed costs to bear; more where rows are too few to
+    // fill the device.
+    int ctas = 1;
+    while (vecs * 16 > (int64_t)ctas * PART || (ctas < 8 && P.n_rows * ctas * 2 <= ctx->sm_count && vecs >= 2 * ctas * SUMS)) ctas *= 2;
+    P.stage_bytes = (int)((vecs + ctas - 1) / ctas) * 16;
+    P.stage_bytes = (P.stage_bytes + 127) / 128 * 128;
+    P.stages = RING / P.stage_bytes < MAX_STAGES ? RING / P.stage_bytes : MAX_STAGES;
+    const int64_t most = ctas == 1 ? ctx->sm_count : ctx->distill_clusters[ctas == 2 ? 0 : ctas == 4 ? 1 : 2];
+    const int64_t teams = P.n_rows < most ? P.n_rows : most;
+    return launch_clustered(ctas, distill_kernel<T>, dim3((unsigned)(teams * ctas)), dim3(THREADS), SMEM, st, P);
 }
 
 }  // namespace
@@ -468,9 +805,12 @@ cudaError_t launch(sama_ctx* ctx, const DistillParams& P, cudaStream_t st) {
 cudaError_t launch_distill(sama_ctx* ctx, int dtype, int64_t n_rows, int vocab, const void* logits, int64_t ld, int k, int top_dtype,
                            const void* top, const int32_t* ids, float temperature, const float* weight, float grad_scale, float* loss,
                            void* grad, int64_t ld_grad, cudaStream_t st) {
+    const cudaError_t e = prepare(ctx);
+    if (e != cudaSuccess) return e;
     DistillParams P;
     P.logits = logits;
     P.grad = grad;
+    P.in_place = grad == logits;
     P.n_rows = n_rows;
     P.ld = ld;
     P.ld_grad = ld_grad;
