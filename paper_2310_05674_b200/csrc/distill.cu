@@ -12,7 +12,7 @@
 //   gradient   q in place of z, the entries' values over that, and bulk copies back
 // so that no group's barriers and latencies are in another's way; nothing but the arrival of the sums is waited for across
 // the cluster.  (All threads on one row at a time, with a cluster barrier per row, took three times as long.)
-// Rows of up to 4 KB are a warp's each; rows that no cluster can hold are read twice.
+// Rows of up to 4 KB are a warp's each; rows that no cluster can hold, or with more than 512 entries, are read twice.
 #include <type_traits>
 
 #include "num_types.h"
@@ -28,8 +28,9 @@ constexpr int kMaxEntries = 1024;
 // one row per cluster or CTA
 constexpr int SUMS = 256, GRADS = 256, TEACHER = 128, THREADS = 32 + TEACHER + SUMS + GRADS;   // groups of threads
 constexpr int RING = 192 * 1024, MAX_STAGES = 8, MIN_STAGES = 3, PART = RING / MIN_STAGES;     // a CTA's part of a row, at most
-constexpr int PER_THREAD = kMaxEntries / TEACHER;
-constexpr int SMEM = RING + 2 * kMaxEntries * 8 + kMaxEntries * 8;
+constexpr int TEACHERS = TEACHER / 32, ENTRIES = 512, BITS = 8192;   // rows whose entries are worked on, entries at most
+constexpr int ENTRY_BYTES = ENTRIES * 12 + BITS / 8;                  // of a row
+constexpr int SMEM = RING + TEACHERS * ENTRY_BYTES;
 // one row per warp
 constexpr int FEW_TEAMS = 8, FEW_STAGES = 3, FEW_ENTRIES = 4, FEW_CHUNK = 32 * VECS * 16, FEW_MOST = 32 * FEW_ENTRIES;
 constexpr int FEW_SMEM = FEW_TEAMS * (FEW_STAGES * FEW_CHUNK + FEW_MOST * 8);
@@ -153,16 +154,15 @@ __global__ void __launch_bounds__(THREADS, 1)
 distill_kernel(const DistillParams P) {
     constexpr int VE = 16 / (int)sizeof(T), SIZE = (int)sizeof(T);
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t full[MAX_STAGES], empty[MAX_STAGES], stats[2 * MAX_STAGES], entries[2], taken[2];
+    __shared__ __align__(8) uint64_t full[MAX_STAGES], empty[MAX_STAGES], stats[2 * MAX_STAGES], entries[TEACHERS], taken[TEACHERS];
     __shared__ float2 peers[2 * MAX_STAGES][8];       // (maximum, sum) of the cluster's CTAs, by row
     __shared__ float2 warp_sums[2][SUMS / 32];
-    __shared__ float teacher_slots[2][TEACHER / 32], row_coef[2];
+    __shared__ float row_coef[TEACHERS];
     __shared__ uint32_t abort_word;
     volatile uint32_t* abort_flag = &abort_word;
-    int32_t* e_place = reinterpret_cast<int32_t*>(smem + RING);                  // [2][kMaxEntries]
-    float* e_value = reinterpret_cast<float*>(e_place + 2 * kMaxEntries);
-    int32_t* e_id = reinterpret_cast<int32_t*>(e_value + 2 * kMaxEntries);       // [kMaxEntries]
-    float* e_p = reinterpret_cast<float*>(e_id + kMaxEntries);
+    // of the teacher's entries of a row: id and then place in the part, weight and then gradient, logit
+    auto e_place = [&](int b) { return reinterpret_cast<int32_t*>(smem + RING + b * ENTRY_BYTES); };
+    auto e_value = [&](int b) { return reinterpret_cast<float*>(e_place(b) + ENTRIES); };
 
     unsigned ctas_u;
     asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas_u));
@@ -172,12 +172,12 @@ distill_kernel(const DistillParams P) {
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(smem_u32(&full[s]), 1);
-            mbar_init(smem_u32(&empty[s]), 1 + TEACHER);
+            mbar_init(smem_u32(&empty[s]), 2);   // (the gradient, or the sums if there is none, and the entries)
         }
         // (in place, no CTA writes before the loss has the logits that it needs)
         for (int s = 0; s < 2 * S; ++s) mbar_init(smem_u32(&stats[s]), ctas + P.in_place);
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(smem_u32(&entries[b]), TEACHER);
+        for (int b = 0; b < TEACHERS; ++b) {
+            mbar_init(smem_u32(&entries[b]), 1);
             mbar_init(smem_u32(&taken[b]), 1);
         }
         abort_word = 0;
@@ -250,127 +250,108 @@ distill_kernel(const DistillParams P) {
         __syncwarp();
     } else if (warp <= TEACHER / 32) {
         // ---------------------------------------------------------- the teacher's entries
-        const int t = threadIdx.x - 32, w = t / 32;
-        int32_t id[PER_THREAD], next_id[PER_THREAD];
-        float u[PER_THREAD], z[PER_THREAD], next_u[PER_THREAD];
-        float weight = 1.f, next_weight = 1.f;
-        auto fetch = [&](int i) {
-            const int64_t row = first + i * stride;
-#pragma unroll
-            for (int e = 0; e < PER_THREAD; ++e) {
-                const int j = t + e * TEACHER;
-                next_id[e] = -1;
-                if (j < P.k) {
-                    next_id[e] = P.ids[row * P.k + j];
-                    next_u[e] = load_top(P, row * P.k + j);
-                }
-            }
-            if (P.weight) next_weight = P.weight[row];
-        };
-        auto take = [&](int i) {   // the entries fetched last become the current ones; their logits are fetched
-            const T* row = reinterpret_cast<const T*>(z_row(i));
-#pragma unroll
-            for (int e = 0; e < PER_THREAD; ++e) {
-                if (e * TEACHER >= P.k) continue;
-                id[e] = next_id[e];
-                if (id[e] < -1 || id[e] >= P.vocab) {
-                    atomicOr(P.status, (int)SAMA_DEV_BAD_INDEX);
-                    id[e] = -1;
-                }
-                u[e] = id[e] >= 0 ? next_u[e] : -INFINITY;
-                z[e] = id[e] >= 0 ? to_float(row[id[e]]) : 0.f;
-            }
-            weight = next_weight;
-        };
-        auto reduce = [&](float x, int slot, auto f) {   // a barrier lies between two uses of a slot
+        // A warp has every fourth row to itself, so that its loads, which depend on one another, may take four rows' time.
+        const int b = warp - 1;
+        int32_t* place = e_place(b);
+        float *value = e_value(b), *logit = value + ENTRIES;
+        uint32_t* bits = reinterpret_cast<uint32_t*>(logit + ENTRIES);
+        auto over = [](float x, auto f) {
 #pragma unroll
             for (int o = 16; o > 0; o /= 2) x = f(x, __shfl_xor_sync(0xffffffffu, x, o));
-            if (lane == 0) teacher_slots[slot][w] = x;
-            group_sync<1, TEACHER>();
-            x = teacher_slots[slot][0];
-#pragma unroll
-            for (int v = 1; v < TEACHER / 32; ++v) x = f(x, teacher_slots[slot][v]);
             return x;
         };
-        if (n_rows > 0) {
-            fetch(0);
-            take(0);
-        }
-        for (int i = 0; i < n_rows; ++i) {
+        for (int i = b; i < n_rows; i += TEACHERS) {
+            const int64_t row = first + i * stride;
+            const T* z = reinterpret_cast<const T*>(z_row(i));
             const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
-            if (i + 1 < n_rows) fetch(i + 1);
-            float top = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < PER_THREAD; ++e) {
-                if (e * TEACHER >= P.k) continue;
-                top = fmaxf(top, u[e]);
-                e_id[t + e * TEACHER] = id[e];
-            }
-            top = reduce(top, 0, max_of);
-            if (P.in_place && rank == 0 && t < ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&stats[i % (2 * S)]), (uint32_t)t));
-            const float from_u = top == -INFINITY ? 0.f : top * P.c;
-            float p[PER_THREAD], sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < PER_THREAD; ++e) {
-                if (e * TEACHER >= P.k) continue;
-                u[e] = fmaf(u[e], P.c, -from_u);   // log2 of p, up to the sum
-                p[e] = exp2f(u[e]);
-                sum += p[e];
-                e_p[t + e * TEACHER] = p[e];
-            }
-            sum = reduce(sum, 1, sum_of);
-            const bool none = sum == 0.f;
-            const float inv_u = none ? 0.f : 1.f / sum, log_u = log2f(sum), coef = P.coef * weight;
-            const bool zero = none || weight == 0.f;
-            // of several entries with one id the first takes them all
             const int skip = sp.head / SIZE - sp.v0 * VE, places = (sp.v1 - sp.v0) * VE;
-            float all[PER_THREAD];
-            int place[PER_THREAD];
-#pragma unroll
-            for (int e = 0; e < PER_THREAD; ++e) {
-                if (e * TEACHER >= P.k) continue;
-                const int j = t + e * TEACHER;
-                place[e] = id[e] >= 0 ? id[e] + skip : -1;
-                if (place[e] >= places || zero || !P.grad) place[e] = -1;
-                all[e] = 0.f;
-                if (place[e] < 0) continue;
-                for (int x = 0; x < P.k; x += 4) {   // (what lies behind the last entry, up to a multiple of 128, has id -1)
-                    const int4 four = *reinterpret_cast<const int4*>(e_id + x);
-                    const int32_t ids[4] = {four.x, four.y, four.z, four.w};
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        if (ids[y] == id[e]) {
-                            all[e] += e_p[x + y];
-                            if (x + y < j) place[e] = -1;
-                        }
+            if (P.grad && i >= TEACHERS) wait(&taken[b], i / TEACHERS - 1);
+            const float weight = P.weight ? P.weight[row] : 1.f;
+            float top = -INFINITY;
+            for (int w = lane; w < BITS / 32; w += 32) bits[w] = 0;
+#pragma unroll 4
+            for (int j = lane; j < P.k; j += 32) {
+                int32_t id = P.ids[row * P.k + j];
+                float u = load_top(P, row * P.k + j);
+                if (id < 0 || id >= P.vocab) {
+                    if (id != -1) atomicOr(P.status, (int)SAMA_DEV_BAD_INDEX);
+                    id = -1;
+                    u = -INFINITY;
+                }
+                place[j] = id;
+                value[j] = u;
+                top = fmaxf(top, u);
+            }
+#pragma unroll 4
+            for (int j = lane; j < P.k; j += 32)
+                if (place[j] >= 0) logit[j] = to_float(z[place[j]]);
+            top = over(top, max_of);
+            if (P.in_place && rank == 0 && lane < ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&stats[i % (2 * S)]), (uint32_t)lane));
+            const float from_u = top == -INFINITY ? 0.f : top * P.c;
+            float sum = 0.f, entropy = 0.f;
+            for (int j = lane; j < P.k; j += 32) {
+                const float lp = fmaf(value[j], P.c, -from_u), p = exp2f(lp);   // log2 of p, up to the sum
+                sum += p;
+                if (p > 0.f) entropy += p * lp;
+                value[j] = p;
+            }
+            sum = over(sum, sum_of);
+            const bool none = sum == 0.f, zero = none || weight == 0.f;
+            const float inv_u = none ? 0.f : 1.f / sum, coef = P.coef * weight;
+            // Several entries with one id: the first takes them all.  An id that finds its bit set may be one of those.
+            {
+                __syncwarp();
+                for (int j0 = 0; j0 < P.k; j0 += 32) {
+                    const int j = j0 + lane;
+                    const int32_t id = j < P.k ? place[j] : -1;
+                    const uint32_t h = ((uint32_t)id * 2654435761u) >> 19, bit = 1u << (h & 31u);
+                    uint32_t again = __ballot_sync(0xffffffffu, id >= 0 && (atomicOr(bits + h / 32, bit) & bit) != 0);
+                    for (; again; again &= again - 1) {
+                        const int32_t it = __shfl_sync(0xffffffffu, id, __ffs(again) - 1);
+                        float all = 0.f;
+                        int leader = ENTRIES;
+                        for (int x = lane; x < P.k; x += 32)
+                            if (place[x] == it) {
+                                all += value[x];
+                                leader = min(leader, x);
+                            }
+                        all = over(all, sum_of);
+                        leader = __reduce_min_sync(0xffffffffu, leader);
+                        __syncwarp();
+                        for (int x = lane; x < P.k; x += 32)
+                            if (place[x] == it) value[x] = x == leader ? all : 0.f;
+                        __syncwarp();
+                    }
                 }
             }
             float most, total;
             wait_stats(i, &most, &total);
-            if (P.grad && i >= 2) wait(&taken[i & 1], i / 2 - 1);
-            const float whole = most == -INFINITY ? 0.f : most * P.c, inv = 1.f / total, log_total = log2f(total);
-            float part = 0.f;
-#pragma unroll
-            for (int e = 0; e < PER_THREAD; ++e) {
-                if (e * TEACHER >= P.k) continue;
-                const float log_q = fmaf(z[e], P.c, -whole);           // log2 of q, up to the sum
-                const float pe = p[e] * inv_u;
-                if (id[e] >= 0 && !(pe == 0.f)) part += pe * ((u[e] - log_u) - ((z[e] - (most == -INFINITY ? 0.f : most)) * P.c - log_total));
-                e_place[(i & 1) * kMaxEntries + t + e * TEACHER] = place[e];
-                e_value[(i & 1) * kMaxEntries + t + e * TEACHER] = coef * (fast_exp2(log_q) * inv - all[e] * inv_u);
+            const float base = most == -INFINITY ? 0.f : most, whole = base * P.c, inv = 1.f / total;
+            float cross = 0.f;
+            for (int j = lane; j < P.k; j += 32) {
+                const int32_t id = place[j];
+                const float p = value[j] * inv_u, ze = logit[j];
+                if (id >= 0 && !(p == 0.f)) cross += p * ((ze - base) * P.c);
+                int at = id >= 0 ? id + skip : -1;
+                if (at >= places || p == 0.f) at = -1;   // (without weight the gradient is q's own)
+                value[j] = coef * (fast_exp2(fmaf(ze, P.c, -whole)) * inv - p);
+                place[j] = at;
             }
-            if (t == 0) {
-                row_coef[i & 1] = coef * inv;
-                if (zero) e_place[(i & 1) * kMaxEntries] = -2;   // zeros, whatever the logits
+            if (lane == 0) {
+                row_coef[b] = coef * inv;
+                if (zero) place[0] = -2;                 // zeros, whatever the logits
             }
-            mbar_arrive(smem_u32(&entries[i & 1]));
-            mbar_arrive(smem_u32(&empty[i % S]));
-            if (i + 1 < n_rows) take(i + 1);
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&entries[b]));
+                mbar_arrive(smem_u32(&empty[i % S]));
+            }
             if (P.loss && rank == 0) {
-                part = reduce(part, 0, sum_of);
-                if (t == 0) P.loss[first + i * stride] = none ? 0.f : P.temperature * P.temperature * 0.69314718f * part;
+                // sum p (log2 p - log2 q), of which sum p = 1
+                entropy = over(entropy, sum_of) * inv_u - log2f(sum);
+                cross = over(cross, sum_of) - log2f(total);
+                if (lane == 0) P.loss[row] = none ? 0.f : P.temperature * P.temperature * 0.69314718f * (entropy - cross);
             }
-            group_sync<1, TEACHER>();   // the entries may be written again
         }
     } else if (warp <= (TEACHER + SUMS) / 32) {
         // ---------------------------------------------------------- maxima and sums
@@ -433,10 +414,10 @@ distill_kernel(const DistillParams P) {
             uint8_t* chunk = chunk_of(s);
             float most, total;
             wait_stats(i, &most, &total);
-            wait(&entries[i & 1], i / 2);
-            const volatile int32_t* places = e_place + (i & 1) * kMaxEntries;
+            wait(&entries[i % TEACHERS], i / TEACHERS);
+            const volatile int32_t* places = e_place(i % TEACHERS);
             const bool zero = places[0] == -2;
-            const float f = row_coef[i & 1], whole = most == -INFINITY ? 0.f : most * P.c;
+            const float f = *const_cast<volatile float*>(&row_coef[i % TEACHERS]), whole = most == -INFINITY ? 0.f : most * P.c;
 #pragma unroll 4
             for (int b = t; b < n; b += GRADS) {
                 float g[VE];
@@ -449,14 +430,14 @@ distill_kernel(const DistillParams P) {
             if (!zero)
                 for (int j = t; j < P.k; j += GRADS) {
                     const int place = places[j];
-                    if (place >= 0) reinterpret_cast<T*>(chunk)[place] = from_float<T>(e_value[(i & 1) * kMaxEntries + j]);
+                    if (place >= 0) reinterpret_cast<T*>(chunk)[place] = from_float<T>(e_value(i % TEACHERS)[j]);
                 }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             group_sync<3, GRADS>();
             uint8_t* g_row = static_cast<uint8_t*>(P.grad) + (first + i * stride) * P.ld_grad * SIZE;
             const bool alike = (int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == sp.head;
             if (t == 0) {
-                mbar_arrive(smem_u32(&taken[i & 1]));
+                mbar_arrive(smem_u32(&taken[i % TEACHERS]));
                 const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u;
                 if (alike && bytes) bulk_store(g_row - sp.head + (int64_t)sp.in0 * 16, smem_u32(chunk + (sp.in0 - sp.v0) * 16), bytes);
                 // the row before this has left its place
@@ -784,7 +765,7 @@ cudaError_t launch(sama_ctx* ctx, DistillParams& P, cudaStream_t st) {
         const int64_t wanted = (P.n_rows + FEW_TEAMS - 1) / FEW_TEAMS, most = 2 * ctx->sm_count;
         return launch_dependent(distill_few_kernel<T>, dim3((unsigned)(wanted < most ? wanted : most)), dim3(32 * FEW_TEAMS), FEW_SMEM, st, P);
     }
-    if (vecs * 16 > 8 * PART) {
+    if (vecs * 16 > 8 * PART || P.k > ENTRIES) {
         const int64_t most = 2 * ctx->sm_count;
         return launch_dependent(distill_long_kernel<T>, dim3((unsigned)(P.n_rows < most ? P.n_rows : most)), dim3(1024), 0, st, P);
     }
