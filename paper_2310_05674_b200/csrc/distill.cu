@@ -7,9 +7,11 @@
 // sum and its gradient.  A row is a CTA's, or that of a cluster of up to 8 CTAs with 64 KB each; rows follow one another
 // through a ring, and the groups of warps of a CTA work on different rows at the same time:
 //   producer   bulk copies of the rows to come; the elements at the ends of rows that do not start on 16 bytes one by one
-//   sums       maximum and sum of exponentials of its part, sent to all CTAs of the cluster (distributed shared memory)
+//   sums       maximum and sum of exponentials of its part
+//   send       which go to all CTAs of the cluster (distributed shared memory)
 //   entries    the teacher's distribution, the loss, and the gradient's values at the teacher's entries
-//   gradient   q in place of z, the entries' values over that, and bulk copies back
+//   gradient   q in place of z, and the entries' values over that
+//   store      bulk copies back, after which the row's place is free
 // so that no group's barriers and latencies are in another's way; nothing but the arrival of the sums is waited for across
 // the cluster.  (All threads on one row at a time, with a cluster barrier per row, took three times as long.)
 // Rows of up to 4 KB are a warp's each; rows that no cluster can hold, or with more than 512 entries, are read twice.
@@ -26,7 +28,8 @@ namespace {
 constexpr int VECS = 8;               // 16-byte vectors that a thread has in hand
 constexpr int kMaxEntries = 1024;
 // one row per cluster or CTA
-constexpr int SUMS = 256, GRADS = 256, TEACHER = 128, THREADS = 32 + TEACHER + SUMS + GRADS;   // groups of threads
+constexpr int SUMS = 384, GRADS = 384, TEACHER = 128, THREADS = 32 + TEACHER + 64 + SUMS + GRADS;   // groups of threads
+constexpr int STORE0 = 32 + TEACHER, SEND0 = STORE0 + 32, SUMS0 = SEND0 + 32, GRADS0 = SUMS0 + SUMS; // their first threads
 constexpr int RING = 192 * 1024, MAX_STAGES = 8, MIN_STAGES = 3, PART = RING / MIN_STAGES;     // a CTA's part of a row, at most
 constexpr int TEACHERS = TEACHER / 32, ENTRIES = 512, BITS = 8192;   // rows whose entries are worked on, entries at most
 constexpr int ENTRY_BYTES = ENTRIES * 12 + BITS / 8;                  // of a row
@@ -154,9 +157,9 @@ __global__ void __launch_bounds__(THREADS, 1)
 distill_kernel(const DistillParams P) {
     constexpr int VE = 16 / (int)sizeof(T), SIZE = (int)sizeof(T);
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t full[MAX_STAGES], empty[MAX_STAGES], stats[2 * MAX_STAGES], entries[TEACHERS], taken[TEACHERS];
+    __shared__ __align__(8) uint64_t full[MAX_STAGES], empty[MAX_STAGES], stats[2 * MAX_STAGES], entries[TEACHERS], taken[TEACHERS], done[2], summed[MAX_STAGES];
     __shared__ float2 peers[2 * MAX_STAGES][8];       // (maximum, sum) of the cluster's CTAs, by row
-    __shared__ float2 warp_sums[2][SUMS / 32];
+    __shared__ float2 warp_sums[MAX_STAGES][SUMS / 32];
     __shared__ float row_coef[TEACHERS];
     __shared__ uint32_t abort_word;
     volatile uint32_t* abort_flag = &abort_word;
@@ -172,6 +175,7 @@ distill_kernel(const DistillParams P) {
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(smem_u32(&full[s]), 1);
+            mbar_init(smem_u32(&summed[s]), SUMS / 32);
             mbar_init(smem_u32(&empty[s]), 2);   // (the gradient, or the sums if there is none, and the entries)
         }
         // (in place, no CTA writes before the loss has the logits that it needs)
@@ -180,6 +184,7 @@ distill_kernel(const DistillParams P) {
             mbar_init(smem_u32(&entries[b]), 1);
             mbar_init(smem_u32(&taken[b]), 1);
         }
+        for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&done[b]), GRADS / 32);
         abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -353,9 +358,51 @@ distill_kernel(const DistillParams P) {
                 if (lane == 0) P.loss[row] = none ? 0.f : P.temperature * P.temperature * 0.69314718f * (entropy - cross);
             }
         }
-    } else if (warp <= (TEACHER + SUMS) / 32) {
+    } else if (warp == STORE0 / 32) {
+        // ---------------------------------------------------------- stores
+        for (int i = 0; i < n_rows && P.grad; ++i) {
+            const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
+            uint8_t* chunk = chunk_of(i % S);
+            uint8_t* g_row = static_cast<uint8_t*>(P.grad) + (first + i * stride) * P.ld_grad * SIZE;
+            wait(&done[i & 1], i / 2);
+            if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == sp.head) {
+                const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u;
+                if (lane == 0 && bytes) bulk_store(g_row - sp.head + (int64_t)sp.in0 * 16, smem_u32(chunk + (sp.in0 - sp.v0) * 16), bytes);
+                int place, element;
+                edge_of<VE>(sp, row_bytes, SIZE, lane, &place, &element);
+                if (place >= 0 && element >= 0 && element < P.vocab) reinterpret_cast<T*>(g_row)[element] = reinterpret_cast<const T*>(chunk)[place];
+            }
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&taken[i % TEACHERS]));
+                asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 0;" ::: "memory");
+                mbar_arrive(smem_u32(&empty[i % S]));
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    } else if (warp == SEND0 / 32) {
+        // ---------------------------------------------------------- the warps' sums, to the cluster's CTAs
+        for (int i = 0; i < n_rows; ++i) {
+            const int s = i % S, slot = i % (2 * S);
+            wait(&summed[s], i / S);
+            const volatile float2* w = warp_sums[s];
+            const float m = lane < SUMS / 32 ? w[lane].x : -INFINITY;
+            float most = m, total = lane < SUMS / 32 ? w[lane].y : 0.f;
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            total = rebase(total, m, most, P.c);
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
+            if (lane < ctas) {
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_rank(smem_u32(&peers[slot][rank]), (uint32_t)lane)), "f"(most), "f"(total) : "memory");
+                mbar_arrive_cluster(map_to_rank(smem_u32(&stats[slot]), (uint32_t)lane));
+            }
+            if (!P.grad && lane == 0) mbar_arrive(smem_u32(&empty[s]));
+            __syncwarp();
+        }
+    } else if (warp < GRADS0 / 32) {
         // ---------------------------------------------------------- maxima and sums
-        const int t = threadIdx.x - 32 - TEACHER;
+        const int t = threadIdx.x - SUMS0;
         for (int i = 0; i < n_rows; ++i) {
             const int s = i % S;
             const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
@@ -390,23 +437,14 @@ distill_kernel(const DistillParams P) {
             l = rebase(l, m, top, P.c);
 #pragma unroll
             for (int o = 16; o > 0; o /= 2) l += __shfl_xor_sync(0xffffffffu, l, o);
-            if (lane == 0) warp_sums[i & 1][t / 32] = make_float2(top, l);
-            group_sync<2, SUMS>();
-            if (t < ctas) {
-                float most = -INFINITY, total = 0.f;
-#pragma unroll
-                for (int w = 0; w < SUMS / 32; ++w) most = fmaxf(most, warp_sums[i & 1][w].x);
-#pragma unroll
-                for (int w = 0; w < SUMS / 32; ++w) total += rebase(warp_sums[i & 1][w].y, warp_sums[i & 1][w].x, most, P.c);
-                const int slot = i % (2 * S);
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_rank(smem_u32(&peers[slot][rank]), (uint32_t)t)), "f"(most), "f"(total) : "memory");
-                mbar_arrive_cluster(map_to_rank(smem_u32(&stats[slot]), (uint32_t)t));
+            if (lane == 0) {
+                warp_sums[s][t / 32] = make_float2(top, l);
+                mbar_arrive(smem_u32(&summed[s]));
             }
-            if (!P.grad && t == 0) mbar_arrive(smem_u32(&empty[s]));
         }
     } else if (P.grad) {
         // ---------------------------------------------------------- gradients
-        const int t = threadIdx.x - 32 - TEACHER - SUMS;
+        const int t = threadIdx.x - GRADS0;
         for (int i = 0; i < n_rows; ++i) {
             const int s = i % S;
             const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
@@ -418,13 +456,17 @@ distill_kernel(const DistillParams P) {
             const volatile int32_t* places = e_place(i % TEACHERS);
             const bool zero = places[0] == -2;
             const float f = *const_cast<volatile float*>(&row_coef[i % TEACHERS]), whole = most == -INFINITY ? 0.f : most * P.c;
+            if (zero) {
+                for (int b = t; b < n; b += GRADS) reinterpret_cast<uint4*>(chunk)[b] = make_uint4(0u, 0u, 0u, 0u);
+            } else {
 #pragma unroll 4
-            for (int b = t; b < n; b += GRADS) {
-                float g[VE];
-                unpack_vec<T>(reinterpret_cast<const uint4*>(chunk)[b], g);
+                for (int b = t; b < n; b += GRADS) {
+                    float g[VE];
+                    unpack_vec<T>(reinterpret_cast<const uint4*>(chunk)[b], g);
 #pragma unroll
-                for (int e = 0; e < VE; ++e) g[e] = zero ? 0.f : fast_exp2(fmaf(g[e], P.c, -whole)) * f;
-                store_n<T, VE>(reinterpret_cast<T*>(chunk) + b * VE, g);
+                    for (int e = 0; e < VE; ++e) g[e] = fast_exp2(fmaf(g[e], P.c, -whole)) * f;
+                    store_n<T, VE>(reinterpret_cast<T*>(chunk) + b * VE, g);
+                }
             }
             group_sync<3, GRADS>();
             if (!zero)
@@ -432,29 +474,17 @@ distill_kernel(const DistillParams P) {
                     const int place = places[j];
                     if (place >= 0) reinterpret_cast<T*>(chunk)[place] = from_float<T>(e_value(i % TEACHERS)[j]);
                 }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            group_sync<3, GRADS>();
             uint8_t* g_row = static_cast<uint8_t*>(P.grad) + (first + i * stride) * P.ld_grad * SIZE;
-            const bool alike = (int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == sp.head;
-            if (t == 0) {
-                mbar_arrive(smem_u32(&taken[i % TEACHERS]));
-                const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u;
-                if (alike && bytes) bulk_store(g_row - sp.head + (int64_t)sp.in0 * 16, smem_u32(chunk + (sp.in0 - sp.v0) * 16), bytes);
-                // the row before this has left its place
-                asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 1;" ::: "memory");
-                if (i > 0) mbar_arrive(smem_u32(&empty[(i - 1) % S]));
-            }
-            if (alike) {
-                int place, element;
-                edge_of<VE>(sp, row_bytes, SIZE, t, &place, &element);
-                if (place >= 0 && element >= 0 && element < P.vocab) reinterpret_cast<T*>(g_row)[element] = reinterpret_cast<const T*>(chunk)[place];
-            } else {
+            if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) != sp.head) {
                 // rows of the gradient start elsewhere than those of the logits
+                group_sync<3, GRADS>();
                 const int skip = sp.head / SIZE - sp.v0 * VE, e0 = max(0, -skip), e1 = min(P.vocab, n * VE - skip);
                 for (int e = e0 + t; e < e1; e += GRADS) reinterpret_cast<T*>(g_row)[e] = reinterpret_cast<const T*>(chunk)[e + skip];
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&done[i & 1]));
         }
-        if (t == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncthreads();
     if (ctas > 1) cluster_sync();   // no CTA leaves while another may write to it
