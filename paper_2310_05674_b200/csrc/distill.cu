@@ -25,7 +25,7 @@ namespace sama {
 
 namespace {
 
-constexpr int VECS = 8;               // 16-byte vectors that a thread has in hand
+constexpr int VECS = 8, BATCH = 4;    // 16-byte vectors that a thread has in hand
 constexpr int kMaxEntries = 1024;
 // one row per cluster or CTA
 constexpr int SUMS = 384, GRADS = 384, TEACHER = 128, THREADS = 32 + TEACHER + 64 + SUMS + GRADS;   // groups of threads
@@ -149,6 +149,13 @@ template <typename T> __device__ __forceinline__ uint4 vec_lowest() {
     const uint32_t w = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
     return make_uint4(w, w, w, w);
 }
+// Where a group is in a ring: `at` counts through `size` places, `round` the times it has gone through them.
+struct Turn {
+    int at = 0, round = 0;
+    __device__ __forceinline__ void next(int size) {
+        if (++at == size) { at = 0; ++round; }
+    }
+};
 // (m, l) of two parts, each a maximum and the sum of 2^(c (z - maximum)): l as seen from `top`.
 __device__ __forceinline__ float rebase(float l, float m, float top, float c) { return m == -INFINITY ? l : l * fast_exp2((m - top) * c); }
 
@@ -161,6 +168,7 @@ distill_kernel(const DistillParams P) {
     __shared__ float2 peers[2 * MAX_STAGES][8];       // (maximum, sum) of the cluster's CTAs, by row
     __shared__ float2 warp_sums[MAX_STAGES][SUMS / 32];
     __shared__ float row_coef[TEACHERS];
+    __shared__ int4 parts[MAX_STAGES];                // of the row in a place: bytes before it, vectors, whole ones from and to
     __shared__ uint32_t abort_word;
     volatile uint32_t* abort_flag = &abort_word;
     // of the teacher's entries of a row: id and then place in the part, weight and then gradient, logit
@@ -206,16 +214,18 @@ distill_kernel(const DistillParams P) {
         }
     };
     // A row's maximum and sum over all CTAs; the same bits in each.
-    auto wait_stats = [&](int i, float* most, float* total) {
-        if (ok && !mbar_wait_cluster(smem_u32(&stats[i % (2 * S)]), (uint32_t)(i / (2 * S)) & 1u, abort_flag)) {
+    auto wait_stats = [&](const Turn& r, float* most, float* total) {
+        if (ok && !mbar_wait_cluster(smem_u32(&stats[r.at]), (uint32_t)r.round & 1u, abort_flag)) {
             ok = false;
             *abort_flag = 1;
             atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
         }
-        const volatile float2* p = peers[i % (2 * S)];
+        const volatile float2* p = peers[r.at];
         float m = -INFINITY, l = 0.f;
-        for (int r = 0; r < ctas; ++r) m = fmaxf(m, p[r].x);
-        for (int r = 0; r < ctas; ++r) l += rebase(p[r].y, p[r].x, m, P.c);
+#pragma unroll 1
+        for (int c = 0; c < ctas; ++c) m = fmaxf(m, p[c].x);
+#pragma unroll 1
+        for (int c = 0; c < ctas; ++c) l += rebase(p[c].y, p[c].x, m, P.c);
         *most = m;
         *total = l;
     };
@@ -231,20 +241,21 @@ distill_kernel(const DistillParams P) {
         };
         int place = -1, next_place = -1, i = 0;
         T at_edge = n_rows > 0 ? edge(0, &place) : from_float<T>(0.f);
-        for (; i < n_rows && __all_sync(0xffffffffu, ok); ++i) {
-            const int s = i % S;
+        Turn turn;
+        for (; i < n_rows; ++i, turn.next(S)) {
             const T next_edge = i + 1 < n_rows ? edge(i + 1, &next_place) : from_float<T>(0.f);
-            if (i >= S) wait(&empty[s], i / S - 1);
+            if (turn.round > 0) wait(&empty[turn.at], turn.round - 1);
             if (!__all_sync(0xffffffffu, ok)) break;
-            uint8_t* chunk = chunk_of(s);
+            uint8_t* chunk = chunk_of(turn.at);
             if (place >= 0) reinterpret_cast<T*>(chunk)[place] = at_edge;
             __syncwarp();
             if (lane == 0) {
                 const uint8_t* row = z_row(i);
                 const Span sp = span_of(row, row_bytes, rank, ctas);
-                const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u;
-                mbar_expect_tx(smem_u32(&full[s]), bytes);
-                if (bytes) bulk_load(smem_u32(chunk + (sp.in0 - sp.v0) * 16), row - sp.head + (int64_t)sp.in0 * 16, bytes, smem_u32(&full[s]));
+                const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u, bar = smem_u32(&full[turn.at]);
+                parts[turn.at] = make_int4(sp.head, sp.v1 - sp.v0, sp.in0 - sp.v0, sp.in1 - sp.v0);
+                mbar_expect_tx(bar, bytes);
+                if (bytes) bulk_load(smem_u32(chunk + (sp.in0 - sp.v0) * 16), row - sp.head + (int64_t)sp.in0 * 16, bytes, bar);
             }
             at_edge = next_edge;
             place = next_place;
@@ -265,12 +276,14 @@ distill_kernel(const DistillParams P) {
             for (int o = 16; o > 0; o /= 2) x = f(x, __shfl_xor_sync(0xffffffffu, x, o));
             return x;
         };
-        for (int i = b; i < n_rows; i += TEACHERS) {
+        int round = 0;
+        for (int i = b; i < n_rows; i += TEACHERS, ++round) {
+            const Turn seat{i % S, i / S}, sums{i % (2 * S), i / (2 * S)};
             const int64_t row = first + i * stride;
             const T* z = reinterpret_cast<const T*>(z_row(i));
             const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
             const int skip = sp.head / SIZE - sp.v0 * VE, places = (sp.v1 - sp.v0) * VE;
-            if (P.grad && i >= TEACHERS) wait(&taken[b], i / TEACHERS - 1);
+            if (P.grad && round > 0) wait(&taken[b], round - 1);
             const float weight = P.weight ? P.weight[row] : 1.f;
             float top = -INFINITY;
             for (int w = lane; w < BITS / 32; w += 32) bits[w] = 0;
@@ -291,7 +304,7 @@ distill_kernel(const DistillParams P) {
             for (int j = lane; j < P.k; j += 32)
                 if (place[j] >= 0) logit[j] = to_float(z[place[j]]);
             top = over(top, max_of);
-            if (P.in_place && rank == 0 && lane < ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&stats[i % (2 * S)]), (uint32_t)lane));
+            if (P.in_place && rank == 0 && lane < ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&stats[sums.at]), (uint32_t)lane));
             const float from_u = top == -INFINITY ? 0.f : top * P.c;
             float sum = 0.f, entropy = 0.f;
             for (int j = lane; j < P.k; j += 32) {
@@ -330,7 +343,7 @@ distill_kernel(const DistillParams P) {
                 }
             }
             float most, total;
-            wait_stats(i, &most, &total);
+            wait_stats(sums, &most, &total);
             const float base = most == -INFINITY ? 0.f : most, whole = base * P.c, inv = 1.f / total;
             float cross = 0.f;
             for (int j = lane; j < P.k; j += 32) {
@@ -349,7 +362,7 @@ distill_kernel(const DistillParams P) {
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(smem_u32(&entries[b]));
-                mbar_arrive(smem_u32(&empty[i % S]));
+                mbar_arrive(smem_u32(&empty[seat.at]));
             }
             if (P.loss && rank == 0) {
                 // sum p (log2 p - log2 q), of which sum p = 1
@@ -360,14 +373,16 @@ distill_kernel(const DistillParams P) {
         }
     } else if (warp == STORE0 / 32) {
         // ---------------------------------------------------------- stores
-        for (int i = 0; i < n_rows && P.grad; ++i) {
-            const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
-            uint8_t* chunk = chunk_of(i % S);
+        Turn turn;
+        for (int i = 0; i < n_rows && P.grad; ++i, turn.next(S)) {
+            uint8_t* chunk = chunk_of(turn.at);
             uint8_t* g_row = static_cast<uint8_t*>(P.grad) + (first + i * stride) * P.ld_grad * SIZE;
             wait(&done[i & 1], i / 2);
-            if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == sp.head) {
-                const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u;
-                if (lane == 0 && bytes) bulk_store(g_row - sp.head + (int64_t)sp.in0 * 16, smem_u32(chunk + (sp.in0 - sp.v0) * 16), bytes);
+            const int4 part = parts[turn.at];
+            if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == part.x) {
+                const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
+                const uint32_t bytes = (uint32_t)(part.w - part.z) * 16u;
+                if (lane == 0 && bytes) bulk_store(g_row - sp.head + (int64_t)sp.in0 * 16, smem_u32(chunk + part.z * 16), bytes);
                 int place, element;
                 edge_of<VE>(sp, row_bytes, SIZE, lane, &place, &element);
                 if (place >= 0 && element >= 0 && element < P.vocab) reinterpret_cast<T*>(g_row)[element] = reinterpret_cast<const T*>(chunk)[place];
@@ -376,15 +391,16 @@ distill_kernel(const DistillParams P) {
             if (lane == 0) {
                 mbar_arrive(smem_u32(&taken[i % TEACHERS]));
                 asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 0;" ::: "memory");
-                mbar_arrive(smem_u32(&empty[i % S]));
+                mbar_arrive(smem_u32(&empty[turn.at]));
             }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     } else if (warp == SEND0 / 32) {
         // ---------------------------------------------------------- the warps' sums, to the cluster's CTAs
-        for (int i = 0; i < n_rows; ++i) {
-            const int s = i % S, slot = i % (2 * S);
-            wait(&summed[s], i / S);
+        Turn turn, sums;
+        for (int i = 0; i < n_rows; ++i, turn.next(S), sums.next(2 * S)) {
+            const int s = turn.at, slot = sums.at;
+            wait(&summed[s], turn.round);
             const volatile float2* w = warp_sums[s];
             const float m = lane < SUMS / 32 ? w[lane].x : -INFINITY;
             float most = m, total = lane < SUMS / 32 ? w[lane].y : 0.f;
@@ -403,27 +419,27 @@ distill_kernel(const DistillParams P) {
     } else if (warp < GRADS0 / 32) {
         // ---------------------------------------------------------- maxima and sums
         const int t = threadIdx.x - SUMS0;
-        for (int i = 0; i < n_rows; ++i) {
-            const int s = i % S;
-            const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
-            const int n = sp.v1 - sp.v0;
-            wait(&full[s], i / S);
+        Turn turn;
+        for (int i = 0; i < n_rows; ++i, turn.next(S)) {
+            const int s = turn.at;
+            wait(&full[s], turn.round);
             const uint4* chunk = reinterpret_cast<const uint4*>(chunk_of(s));
+            const int n = parts[s].y;
             float m = -INFINITY, l = 0.f;
-            for (int b = t; b < n; b += SUMS * VECS) {
-                uint4 x[VECS];
+            for (int b = t; b < n; b += SUMS * BATCH) {
+                uint4 x[BATCH];
                 float top = -INFINITY;
 #pragma unroll
-                for (int v = 0; v < VECS; ++v) x[v] = b + v * SUMS < n ? chunk[b + v * SUMS] : vec_lowest<T>();
+                for (int v = 0; v < BATCH; ++v) x[v] = b + v * SUMS < n ? chunk[b + v * SUMS] : vec_lowest<T>();
 #pragma unroll
-                for (int v = 0; v < VECS; ++v) top = fmaxf(top, vec_max<T>(x[v]));
+                for (int v = 0; v < BATCH; ++v) top = fmaxf(top, vec_max<T>(x[v]));
                 if (top > m) {
                     l = m == -INFINITY ? l : l * fast_exp2((m - top) * P.c);
                     m = top;
                 }
                 const float from = m == -INFINITY ? 0.f : m * P.c;
 #pragma unroll
-                for (int v = 0; v < VECS; ++v) {
+                for (int v = 0; v < BATCH; ++v) {
                     float f[VE], sum = 0.f;
                     unpack_vec<T>(x[v], f);
 #pragma unroll
@@ -445,13 +461,13 @@ distill_kernel(const DistillParams P) {
     } else if (P.grad) {
         // ---------------------------------------------------------- gradients
         const int t = threadIdx.x - GRADS0;
-        for (int i = 0; i < n_rows; ++i) {
-            const int s = i % S;
-            const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
-            const int n = sp.v1 - sp.v0;
+        Turn turn, sums;
+        for (int i = 0; i < n_rows; ++i, turn.next(S), sums.next(2 * S)) {
+            const int s = turn.at;
             uint8_t* chunk = chunk_of(s);
             float most, total;
-            wait_stats(i, &most, &total);
+            wait_stats(sums, &most, &total);
+            const int head = parts[s].x, n = parts[s].y;
             wait(&entries[i % TEACHERS], i / TEACHERS);
             const volatile int32_t* places = e_place(i % TEACHERS);
             const bool zero = places[0] == -2;
@@ -475,10 +491,10 @@ distill_kernel(const DistillParams P) {
                     if (place >= 0) reinterpret_cast<T*>(chunk)[place] = from_float<T>(e_value(i % TEACHERS)[j]);
                 }
             uint8_t* g_row = static_cast<uint8_t*>(P.grad) + (first + i * stride) * P.ld_grad * SIZE;
-            if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) != sp.head) {
+            if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) != head) {
                 // rows of the gradient start elsewhere than those of the logits
                 group_sync<3, GRADS>();
-                const int skip = sp.head / SIZE - sp.v0 * VE, e0 = max(0, -skip), e1 = min(P.vocab, n * VE - skip);
+                const int skip = head / SIZE - span_of(z_row(i), row_bytes, rank, ctas).v0 * VE, e0 = max(0, -skip), e1 = min(P.vocab, n * VE - skip);
                 for (int e = e0 + t; e < e1; e += GRADS) reinterpret_cast<T*>(g_row)[e] = reinterpret_cast<const T*>(chunk)[e + skip];
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
