@@ -4,16 +4,13 @@
 //   loss = T^2 sum p (log p - log q),  grad = coef (q - p),  coef = grad_scale weight T
 //
 // The logits are read once and the gradient is written once, which is the floor: a row stays in shared memory between its
-// sum and its gradient.  A row is a CTA's, or that of a cluster of up to 8 CTAs with 64 KB each; rows follow one another
-// through a ring, and the groups of warps of a CTA work on different rows at the same time:
-//   producer   bulk copies of the rows to come; the elements at the ends of rows that do not start on 16 bytes one by one
-//   sums       maximum and sum of exponentials of its part
-//   send       which go to all CTAs of the cluster (distributed shared memory)
-//   entries    the teacher's distribution, the loss, and the gradient's values at the teacher's entries
-//   gradient   q in place of z, and the entries' values over that
-//   store      bulk copies back, after which the row's place is free
-// so that no group's barriers and latencies are in another's way; nothing but the arrival of the sums is waited for across
-// the cluster.  (All threads on one row at a time, with a cluster barrier per row, took three times as long.)
+// sum and its gradient.  A row is a CTA's, or that of a cluster of up to 8 CTAs with 64 KB each, which exchange maximum and
+// sum through distributed shared memory.  A bulk copy brings the part in; the threads take maximum and sum of it, meet, and
+// write q from registers straight to memory, while a warp of its own works out the teacher's distribution, the loss and the
+// gradient's values at the teacher's entries, which go over q at the end.  A CTA does one thing after the other, and three
+// or more of them per SM keep memory busy meanwhile.  (A persistent CTA whose groups of warps work on different rows of a
+// ring was slower, 174 for 127 us at 4096 rows of 50,021 bf16 logits: it had a single copy in flight per SM most of the
+// time, and its groups' waits took issue slots.)
 // Rows of up to 4 KB are a warp's each; rows that no cluster can hold, or with more than 512 entries, are read twice.
 #include <type_traits>
 
@@ -28,12 +25,9 @@ namespace {
 constexpr int VECS = 8, BATCH = 4;    // 16-byte vectors that a thread has in hand
 constexpr int kMaxEntries = 1024;
 // one row per cluster or CTA
-constexpr int SUMS = 384, GRADS = 384, TEACHER = 128, THREADS = 32 + TEACHER + 64 + SUMS + GRADS;   // groups of threads
-constexpr int STORE0 = 32 + TEACHER, SEND0 = STORE0 + 32, SUMS0 = SEND0 + 32, GRADS0 = SUMS0 + SUMS; // their first threads
-constexpr int RING = 192 * 1024, MAX_STAGES = 8, MIN_STAGES = 3, PART = RING / MIN_STAGES;     // a CTA's part of a row, at most
-constexpr int TEACHERS = TEACHER / 32, ENTRIES = 512, BITS = 8192;   // rows whose entries are worked on, entries at most
-constexpr int ENTRY_BYTES = ENTRIES * 12 + BITS / 8;                  // of a row
-constexpr int SMEM = RING + TEACHERS * ENTRY_BYTES;
+constexpr int PART = 64 * 1024;                            // bytes of a row in a CTA, at most
+constexpr int ENTRIES = 512, BITS = 8192;                  // of the teacher's, at most; of the table that finds an id twice
+constexpr int entry_bytes(int k) { return (k + 31) / 32 * 32 * 12 + BITS / 8; }
 // one row per warp
 constexpr int FEW_TEAMS = 8, FEW_STAGES = 3, FEW_ENTRIES = 4, FEW_CHUNK = 32 * VECS * 16, FEW_MOST = 32 * FEW_ENTRIES;
 constexpr int FEW_SMEM = FEW_TEAMS * (FEW_STAGES * FEW_CHUNK + FEW_MOST * 8);
@@ -48,7 +42,7 @@ struct DistillParams {
     float* loss;
     int32_t* status;
     int vocab, k, top_dtype;
-    int stages, stage_bytes;      // of the ring
+    int part_bytes;               // shared memory for a CTA's part of a row
     int in_place;                 // the gradient replaces the logits
     float c, temperature, coef;   // log2 e / T, T, grad_scale T
 };
@@ -129,8 +123,6 @@ __device__ __forceinline__ void edge_of(const Span& s, int row_bytes, int size, 
     *place = t < 2 * VE && partial && v >= s.v0 && v < s.v1 ? (v - s.v0) * VE + t % VE : -1;
 }
 
-template <int BAR, int N> __device__ __forceinline__ void group_sync() { asm volatile("bar.sync %0, %1;" ::"n"(BAR), "n"(N) : "memory"); }
-
 // The largest of a vector's values (NaN aside).
 template <typename T> __device__ __forceinline__ float vec_max(uint4 x) {
     if constexpr (sizeof(T) == 4) {
@@ -149,361 +141,260 @@ template <typename T> __device__ __forceinline__ uint4 vec_lowest() {
     const uint32_t w = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
     return make_uint4(w, w, w, w);
 }
-// Where a group is in a ring: `at` counts through `size` places, `round` the times it has gone through them.
-struct Turn {
-    int at = 0, round = 0;
-    __device__ __forceinline__ void next(int size) {
-        if (++at == size) { at = 0; ++round; }
-    }
-};
 // (m, l) of two parts, each a maximum and the sum of 2^(c (z - maximum)): l as seen from `top`.
 __device__ __forceinline__ float rebase(float l, float m, float top, float c) { return m == -INFINITY ? l : l * fast_exp2((m - top) * c); }
 
-template <typename T>
-__global__ void __launch_bounds__(THREADS, 1)
+// MAIN threads for the row and a warp for its entries.
+template <typename T, int MAIN>
+__global__ void __launch_bounds__(MAIN + 32, MAIN == 256 ? 4 : MAIN == 128 ? 7 : 11)
 distill_kernel(const DistillParams P) {
-    constexpr int VE = 16 / (int)sizeof(T), SIZE = (int)sizeof(T);
+    constexpr int VE = 16 / (int)sizeof(T), SIZE = (int)sizeof(T), WARPS = MAIN / 32;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t full[MAX_STAGES], empty[MAX_STAGES], stats[2 * MAX_STAGES], entries[TEACHERS], taken[TEACHERS], done[2], summed[MAX_STAGES];
-    __shared__ float2 peers[2 * MAX_STAGES][8];       // (maximum, sum) of the cluster's CTAs, by row
-    __shared__ float2 warp_sums[MAX_STAGES][SUMS / 32];
-    __shared__ float row_coef[TEACHERS];
-    __shared__ int4 parts[MAX_STAGES];                // of the row in a place: bytes before it, vectors, whole ones from and to
-    __shared__ uint32_t abort_word;
-    volatile uint32_t* abort_flag = &abort_word;
-    // of the teacher's entries of a row: id and then place in the part, weight and then gradient, logit
-    auto e_place = [&](int b) { return reinterpret_cast<int32_t*>(smem + RING + b * ENTRY_BYTES); };
-    auto e_value = [&](int b) { return reinterpret_cast<float*>(e_place(b) + ENTRIES); };
+    __shared__ __align__(8) uint64_t full;
+    __shared__ float2 peers[8], warp_sums[WARPS];     // (maximum, sum) of the cluster's CTAs, of this one's warps
+    __shared__ int no_entry;
+    const int kp = (P.k + 31) / 32 * 32;
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem + P.part_bytes);
+    int32_t* place = reinterpret_cast<int32_t*>(bits + BITS / 32);   // of the teacher's entries: id (in the end, of those in this part),
+    float *value = reinterpret_cast<float*>(place + kp), *logit = value + kp;   // weight and then gradient, logit
 
     unsigned ctas_u;
     asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas_u));
-    const int ctas = (int)ctas_u, rank = ctas > 1 ? (int)cluster_ctarank() : 0, S = P.stages;
-    const int64_t first = blockIdx.x / ctas_u, stride = gridDim.x / ctas_u;
-    const int n_rows = first < P.n_rows ? (int)((P.n_rows - first + stride - 1) / stride) : 0;   // of this cluster
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < S; ++s) {
-            mbar_init(smem_u32(&full[s]), 1);
-            mbar_init(smem_u32(&summed[s]), SUMS / 32);
-            mbar_init(smem_u32(&empty[s]), 2);   // (the gradient, or the sums if there is none, and the entries)
-        }
-        // (in place, no CTA writes before the loss has the logits that it needs)
-        for (int s = 0; s < 2 * S; ++s) mbar_init(smem_u32(&stats[s]), ctas + P.in_place);
-        for (int b = 0; b < TEACHERS; ++b) {
-            mbar_init(smem_u32(&entries[b]), 1);
-            mbar_init(smem_u32(&taken[b]), 1);
-        }
-        for (int b = 0; b < 2; ++b) mbar_init(smem_u32(&done[b]), GRADS / 32);
-        abort_word = 0;
+    const int ctas = (int)ctas_u, rank = ctas > 1 ? (int)cluster_ctarank() : 0;
+    const int64_t row = blockIdx.x / ctas_u;
+    const int t = threadIdx.x, warp = t / 32, lane = t % 32;
+    const int row_bytes = P.vocab * SIZE;
+    const uint8_t* z_row = static_cast<const uint8_t*>(P.logits) + row * P.ld * SIZE;
+    const Span sp = span_of(z_row, row_bytes, rank, ctas);
+    const int n = sp.v1 - sp.v0;
+    const uint32_t bar = smem_u32(&full);
+    if (t == 0) {
+        mbar_init(bar, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncthreads();
-    if (ctas > 1) cluster_sync();   // the other CTAs run before their shared memory is written
     pdl_trigger();
     pdl_wait();
-
-    const int row_bytes = P.vocab * SIZE;
-    const uint8_t* z_bytes = static_cast<const uint8_t*>(P.logits);
-    auto z_row = [&](int i) { return z_bytes + (first + i * stride) * P.ld * SIZE; };
-    auto chunk_of = [&](int s) { return smem + s * P.stage_bytes; };
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, int parity) {
-        if (ok && !mbar_wait(smem_u32(bar), (uint32_t)parity & 1u, abort_flag)) {
-            ok = false;
-            *abort_flag = 1;
-            atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
-        }
-    };
-    // A row's maximum and sum over all CTAs; the same bits in each.
-    auto wait_stats = [&](const Turn& r, float* most, float* total) {
-        if (ok && !mbar_wait_cluster(smem_u32(&stats[r.at]), (uint32_t)r.round & 1u, abort_flag)) {
-            ok = false;
-            *abort_flag = 1;
-            atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
-        }
-        const volatile float2* p = peers[r.at];
-        float m = -INFINITY, l = 0.f;
-#pragma unroll 1
-        for (int c = 0; c < ctas; ++c) m = fmaxf(m, p[c].x);
-#pragma unroll 1
-        for (int c = 0; c < ctas; ++c) l += rebase(p[c].y, p[c].x, m, P.c);
-        *most = m;
-        *total = l;
-    };
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-
     if (warp == 0) {
-        // ---------------------------------------------------------- producer
-        auto edge = [&](int i, int* place) {
-            const uint8_t* row = z_row(i);
-            int element;
-            edge_of<VE>(span_of(row, row_bytes, rank, ctas), row_bytes, SIZE, lane, place, &element);
-            return *place >= 0 && element >= 0 && element < P.vocab ? reinterpret_cast<const T*>(row)[element] : from_float<T>(-INFINITY);
-        };
-        int place = -1, next_place = -1, i = 0;
-        T at_edge = n_rows > 0 ? edge(0, &place) : from_float<T>(0.f);
-        Turn turn;
-        for (; i < n_rows; ++i, turn.next(S)) {
-            const T next_edge = i + 1 < n_rows ? edge(i + 1, &next_place) : from_float<T>(0.f);
-            if (turn.round > 0) wait(&empty[turn.at], turn.round - 1);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            uint8_t* chunk = chunk_of(turn.at);
-            if (place >= 0) reinterpret_cast<T*>(chunk)[place] = at_edge;
-            __syncwarp();
-            if (lane == 0) {
-                const uint8_t* row = z_row(i);
-                const Span sp = span_of(row, row_bytes, rank, ctas);
-                const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u, bar = smem_u32(&full[turn.at]);
-                parts[turn.at] = make_int4(sp.head, sp.v1 - sp.v0, sp.in0 - sp.v0, sp.in1 - sp.v0);
-                mbar_expect_tx(bar, bytes);
-                if (bytes) bulk_load(smem_u32(chunk + (sp.in0 - sp.v0) * 16), row - sp.head + (int64_t)sp.in0 * 16, bytes, bar);
-            }
-            at_edge = next_edge;
-            place = next_place;
-        }
-        if (*abort_flag && lane == 0)
-            // let the copies already issued land before the CTA's shared memory goes away
-            for (int k = max(0, i - S); k < i; ++k) mbar_wait(smem_u32(&full[k % S]), (uint32_t)(k / S) & 1u);
+        int at, element;
+        edge_of<VE>(sp, row_bytes, SIZE, lane, &at, &element);
+        if (at >= 0) reinterpret_cast<T*>(smem)[at] = element >= 0 && element < P.vocab ? reinterpret_cast<const T*>(z_row)[element] : from_float<T>(-INFINITY);
         __syncwarp();
-    } else if (warp <= TEACHER / 32) {
-        // ---------------------------------------------------------- the teacher's entries
-        // A warp has every fourth row to itself, so that its loads, which depend on one another, may take four rows' time.
-        const int b = warp - 1;
-        int32_t* place = e_place(b);
-        float *value = e_value(b), *logit = value + ENTRIES;
-        uint32_t* bits = reinterpret_cast<uint32_t*>(logit + ENTRIES);
-        auto over = [](float x, auto f) {
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) x = f(x, __shfl_xor_sync(0xffffffffu, x, o));
-            return x;
-        };
-        int round = 0;
-        for (int i = b; i < n_rows; i += TEACHERS, ++round) {
-            const Turn seat{i % S, i / S}, sums{i % (2 * S), i / (2 * S)};
-            const int64_t row = first + i * stride;
-            const T* z = reinterpret_cast<const T*>(z_row(i));
-            const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
-            const int skip = sp.head / SIZE - sp.v0 * VE, places = (sp.v1 - sp.v0) * VE;
-            if (P.grad && round > 0) wait(&taken[b], round - 1);
-            const float weight = P.weight ? P.weight[row] : 1.f;
-            float top = -INFINITY;
-            for (int w = lane; w < BITS / 32; w += 32) bits[w] = 0;
-#pragma unroll 4
-            for (int j = lane; j < P.k; j += 32) {
-                int32_t id = P.ids[row * P.k + j];
-                float u = load_top(P, row * P.k + j);
-                if (id < 0 || id >= P.vocab) {
-                    if (id != -1) atomicOr(P.status, (int)SAMA_DEV_BAD_INDEX);
-                    id = -1;
-                    u = -INFINITY;
-                }
-                place[j] = id;
-                value[j] = u;
-                top = fmaxf(top, u);
-            }
-#pragma unroll 4
-            for (int j = lane; j < P.k; j += 32)
-                if (place[j] >= 0) logit[j] = to_float(z[place[j]]);
-            top = over(top, max_of);
-            if (P.in_place && rank == 0 && lane < ctas) mbar_arrive_cluster(map_to_rank(smem_u32(&stats[sums.at]), (uint32_t)lane));
-            const float from_u = top == -INFINITY ? 0.f : top * P.c;
-            float sum = 0.f, entropy = 0.f;
-            for (int j = lane; j < P.k; j += 32) {
-                const float lp = fmaf(value[j], P.c, -from_u), p = exp2f(lp);   // log2 of p, up to the sum
-                sum += p;
-                if (p > 0.f) entropy += p * lp;
-                value[j] = p;
-            }
-            sum = over(sum, sum_of);
-            const bool none = sum == 0.f, zero = none || weight == 0.f;
-            const float inv_u = none ? 0.f : 1.f / sum, coef = P.coef * weight;
-            // Several entries with one id: the first takes them all.  An id that finds its bit set may be one of those.
-            {
-                __syncwarp();
-                for (int j0 = 0; j0 < P.k; j0 += 32) {
-                    const int j = j0 + lane;
-                    const int32_t id = j < P.k ? place[j] : -1;
-                    const uint32_t h = ((uint32_t)id * 2654435761u) >> 19, bit = 1u << (h & 31u);
-                    uint32_t again = __ballot_sync(0xffffffffu, id >= 0 && (atomicOr(bits + h / 32, bit) & bit) != 0);
-                    for (; again; again &= again - 1) {
-                        const int32_t it = __shfl_sync(0xffffffffu, id, __ffs(again) - 1);
-                        float all = 0.f;
-                        int leader = ENTRIES;
-                        for (int x = lane; x < P.k; x += 32)
-                            if (place[x] == it) {
-                                all += value[x];
-                                leader = min(leader, x);
-                            }
-                        all = over(all, sum_of);
-                        leader = __reduce_min_sync(0xffffffffu, leader);
-                        __syncwarp();
-                        for (int x = lane; x < P.k; x += 32)
-                            if (place[x] == it) value[x] = x == leader ? all : 0.f;
-                        __syncwarp();
-                    }
-                }
-            }
-            float most, total;
-            wait_stats(sums, &most, &total);
-            const float base = most == -INFINITY ? 0.f : most, whole = base * P.c, inv = 1.f / total;
-            float cross = 0.f;
-            for (int j = lane; j < P.k; j += 32) {
-                const int32_t id = place[j];
-                const float p = value[j] * inv_u, ze = logit[j];
-                if (id >= 0 && !(p == 0.f)) cross += p * ((ze - base) * P.c);
-                int at = id >= 0 ? id + skip : -1;
-                if (at >= places || p == 0.f) at = -1;   // (without weight the gradient is q's own)
-                value[j] = coef * (fast_exp2(fmaf(ze, P.c, -whole)) * inv - p);
-                place[j] = at;
-            }
-            if (lane == 0) {
-                row_coef[b] = coef * inv;
-                if (zero) place[0] = -2;                 // zeros, whatever the logits
-            }
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(smem_u32(&entries[b]));
-                mbar_arrive(smem_u32(&empty[seat.at]));
-            }
-            if (P.loss && rank == 0) {
-                // sum p (log2 p - log2 q), of which sum p = 1
-                entropy = over(entropy, sum_of) * inv_u - log2f(sum);
-                cross = over(cross, sum_of) - log2f(total);
-                if (lane == 0) P.loss[row] = none ? 0.f : P.temperature * P.temperature * 0.69314718f * (entropy - cross);
-            }
-        }
-    } else if (warp == STORE0 / 32) {
-        // ---------------------------------------------------------- stores
-        Turn turn;
-        for (int i = 0; i < n_rows && P.grad; ++i, turn.next(S)) {
-            uint8_t* chunk = chunk_of(turn.at);
-            uint8_t* g_row = static_cast<uint8_t*>(P.grad) + (first + i * stride) * P.ld_grad * SIZE;
-            wait(&done[i & 1], i / 2);
-            const int4 part = parts[turn.at];
-            if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == part.x) {
-                const Span sp = span_of(z_row(i), row_bytes, rank, ctas);
-                const uint32_t bytes = (uint32_t)(part.w - part.z) * 16u;
-                if (lane == 0 && bytes) bulk_store(g_row - sp.head + (int64_t)sp.in0 * 16, smem_u32(chunk + part.z * 16), bytes);
-                int place, element;
-                edge_of<VE>(sp, row_bytes, SIZE, lane, &place, &element);
-                if (place >= 0 && element >= 0 && element < P.vocab) reinterpret_cast<T*>(g_row)[element] = reinterpret_cast<const T*>(chunk)[place];
-            }
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(smem_u32(&taken[i % TEACHERS]));
-                asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 0;" ::: "memory");
-                mbar_arrive(smem_u32(&empty[turn.at]));
-            }
-        }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-    } else if (warp == SEND0 / 32) {
-        // ---------------------------------------------------------- the warps' sums, to the cluster's CTAs
-        Turn turn, sums;
-        for (int i = 0; i < n_rows; ++i, turn.next(S), sums.next(2 * S)) {
-            const int s = turn.at, slot = sums.at;
-            wait(&summed[s], turn.round);
-            const volatile float2* w = warp_sums[s];
-            const float m = lane < SUMS / 32 ? w[lane].x : -INFINITY;
-            float most = m, total = lane < SUMS / 32 ? w[lane].y : 0.f;
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-            total = rebase(total, m, most, P.c);
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
-            if (lane < ctas) {
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_rank(smem_u32(&peers[slot][rank]), (uint32_t)lane)), "f"(most), "f"(total) : "memory");
-                mbar_arrive_cluster(map_to_rank(smem_u32(&stats[slot]), (uint32_t)lane));
-            }
-            if (!P.grad && lane == 0) mbar_arrive(smem_u32(&empty[s]));
-            __syncwarp();
-        }
-    } else if (warp < GRADS0 / 32) {
-        // ---------------------------------------------------------- maxima and sums
-        const int t = threadIdx.x - SUMS0;
-        Turn turn;
-        for (int i = 0; i < n_rows; ++i, turn.next(S)) {
-            const int s = turn.at;
-            wait(&full[s], turn.round);
-            const uint4* chunk = reinterpret_cast<const uint4*>(chunk_of(s));
-            const int n = parts[s].y;
-            float m = -INFINITY, l = 0.f;
-            for (int b = t; b < n; b += SUMS * BATCH) {
-                uint4 x[BATCH];
-                float top = -INFINITY;
-#pragma unroll
-                for (int v = 0; v < BATCH; ++v) x[v] = b + v * SUMS < n ? chunk[b + v * SUMS] : vec_lowest<T>();
-#pragma unroll
-                for (int v = 0; v < BATCH; ++v) top = fmaxf(top, vec_max<T>(x[v]));
-                if (top > m) {
-                    l = m == -INFINITY ? l : l * fast_exp2((m - top) * P.c);
-                    m = top;
-                }
-                const float from = m == -INFINITY ? 0.f : m * P.c;
-#pragma unroll
-                for (int v = 0; v < BATCH; ++v) {
-                    float f[VE], sum = 0.f;
-                    unpack_vec<T>(x[v], f);
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) sum += fast_exp2(fmaf(f[e], P.c, -from));
-                    l += sum;
-                }
-            }
-            float top = m;
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            l = rebase(l, m, top, P.c);
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) l += __shfl_xor_sync(0xffffffffu, l, o);
-            if (lane == 0) {
-                warp_sums[s][t / 32] = make_float2(top, l);
-                mbar_arrive(smem_u32(&summed[s]));
-            }
-        }
-    } else if (P.grad) {
-        // ---------------------------------------------------------- gradients
-        const int t = threadIdx.x - GRADS0;
-        Turn turn, sums;
-        for (int i = 0; i < n_rows; ++i, turn.next(S), sums.next(2 * S)) {
-            const int s = turn.at;
-            uint8_t* chunk = chunk_of(s);
-            float most, total;
-            wait_stats(sums, &most, &total);
-            const int head = parts[s].x, n = parts[s].y;
-            wait(&entries[i % TEACHERS], i / TEACHERS);
-            const volatile int32_t* places = e_place(i % TEACHERS);
-            const bool zero = places[0] == -2;
-            const float f = *const_cast<volatile float*>(&row_coef[i % TEACHERS]), whole = most == -INFINITY ? 0.f : most * P.c;
-            if (zero) {
-                for (int b = t; b < n; b += GRADS) reinterpret_cast<uint4*>(chunk)[b] = make_uint4(0u, 0u, 0u, 0u);
-            } else {
-#pragma unroll 4
-                for (int b = t; b < n; b += GRADS) {
-                    float g[VE];
-                    unpack_vec<T>(reinterpret_cast<const uint4*>(chunk)[b], g);
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) g[e] = fast_exp2(fmaf(g[e], P.c, -whole)) * f;
-                    store_n<T, VE>(reinterpret_cast<T*>(chunk) + b * VE, g);
-                }
-            }
-            group_sync<3, GRADS>();
-            if (!zero)
-                for (int j = t; j < P.k; j += GRADS) {
-                    const int place = places[j];
-                    if (place >= 0) reinterpret_cast<T*>(chunk)[place] = from_float<T>(e_value(i % TEACHERS)[j]);
-                }
-            uint8_t* g_row = static_cast<uint8_t*>(P.grad) + (first + i * stride) * P.ld_grad * SIZE;
-            if ((int)(reinterpret_cast<uintptr_t>(g_row) & 15u) != head) {
-                // rows of the gradient start elsewhere than those of the logits
-                group_sync<3, GRADS>();
-                const int skip = head / SIZE - span_of(z_row(i), row_bytes, rank, ctas).v0 * VE, e0 = max(0, -skip), e1 = min(P.vocab, n * VE - skip);
-                for (int e = e0 + t; e < e1; e += GRADS) reinterpret_cast<T*>(g_row)[e] = reinterpret_cast<const T*>(chunk)[e + skip];
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&done[i & 1]));
+        if (lane == 0) {
+            const uint32_t bytes = (uint32_t)(sp.in1 - sp.in0) * 16u;
+            mbar_expect_tx(bar, bytes);
+            if (bytes) bulk_load(smem_u32(smem + (sp.in0 - sp.v0) * 16), z_row - sp.head + (int64_t)sp.in0 * 16, bytes, bar);
         }
     }
     __syncthreads();
-    if (ctas > 1) cluster_sync();   // no CTA leaves while another may write to it
+    // (the other CTAs run before their shared memory is written: waited for only then)
+    if (ctas > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+
+    const float weight = P.weight ? P.weight[row] : 1.f, coef = P.coef * weight;
+    float sum_u = 0.f, entropy = 0.f;
+    auto over = [](float x, auto f) {
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) x = f(x, __shfl_xor_sync(0xffffffffu, x, o));
+        return x;
+    };
+    if (warp == WARPS) {
+        const T* z = reinterpret_cast<const T*>(z_row);
+        if (ctas > 1) {
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (!P.in_place) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        }
+        float top = -INFINITY;
+        for (int w = lane; w < BITS / 32; w += 32) bits[w] = 0;
+#pragma unroll 4
+        for (int j = lane; j < P.k; j += 32) {
+            int32_t id = P.ids[row * P.k + j];
+            float u = load_top(P, row * P.k + j);
+            if (id < 0 || id >= P.vocab) {
+                if (id != -1) atomicOr(P.status, (int)SAMA_DEV_BAD_INDEX);
+                id = -1;
+                u = -INFINITY;
+            }
+            place[j] = id;
+            value[j] = u;
+            top = fmaxf(top, u);
+        }
+#pragma unroll 4
+        for (int j = lane; j < P.k; j += 32)
+            if (place[j] >= 0) logit[j] = to_float(z[place[j]]);
+        // (in place, no CTA writes before the loss has the logits that it needs)
+        if (ctas > 1 && P.in_place) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        top = over(top, max_of);
+        const float from_u = top == -INFINITY ? 0.f : top * P.c;
+        for (int j = lane; j < P.k; j += 32) {
+            const float lp = fmaf(value[j], P.c, -from_u), p = exp2f(lp);   // log2 of p, up to the sum
+            sum_u += p;
+            if (p > 0.f) entropy += p * lp;
+            value[j] = p;
+        }
+        sum_u = over(sum_u, sum_of);
+        entropy = over(entropy, sum_of);
+        if (lane == 0) no_entry = sum_u == 0.f;
+        // Several entries with one id: the first takes them all.  An id that finds its bit set may be one of those.
+        __syncwarp();
+        for (int j0 = 0; j0 < P.k; j0 += 32) {
+            const int j = j0 + lane;
+            const int32_t id = j < P.k ? place[j] : -1;
+            const uint32_t h = ((uint32_t)id * 2654435761u) >> 19, bit = 1u << (h & 31u);
+            uint32_t again = __ballot_sync(0xffffffffu, id >= 0 && (atomicOr(bits + h / 32, bit) & bit) != 0);
+            for (; again; again &= again - 1) {
+                const int32_t it = __shfl_sync(0xffffffffu, id, __ffs(again) - 1);
+                float all = 0.f;
+                int leader = ENTRIES;
+                for (int x = lane; x < P.k; x += 32)
+                    if (place[x] == it) {
+                        all += value[x];
+                        leader = min(leader, x);
+                    }
+                all = over(all, sum_of);
+                leader = __reduce_min_sync(0xffffffffu, leader);
+                __syncwarp();
+                for (int x = lane; x < P.k; x += 32)
+                    if (place[x] == it) value[x] = x == leader ? all : 0.f;
+                __syncwarp();
+            }
+        }
+    } else {
+        // (one warp asks for the copy, the others wait at a barrier: asking again and again takes issue slots)
+        if (warp == 0 && !mbar_wait(bar, 0)) atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
+        asm volatile("bar.sync 1, %0;" ::"n"(MAIN) : "memory");
+        const uint4* chunk = reinterpret_cast<const uint4*>(smem);
+        float m = -INFINITY, l = 0.f;
+        auto take = [&](auto count, int b) {   // vectors b, b + MAIN, ...
+            constexpr int N = decltype(count)::value;
+            uint4 x[N];
+            float top = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < N; ++v) x[v] = chunk[b + v * MAIN];
+#pragma unroll
+            for (int v = 0; v < N; ++v) top = fmaxf(top, vec_max<T>(x[v]));
+            if (top > m) {
+                l = m == -INFINITY ? l : l * fast_exp2((m - top) * P.c);
+                m = top;
+            }
+            const float from = m == -INFINITY ? 0.f : m * P.c;
+#pragma unroll
+            for (int v = 0; v < N; ++v) {
+                float f[VE], sum = 0.f;
+                unpack_vec<T>(x[v], f);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) sum += fast_exp2(fmaf(f[e], P.c, -from));
+                l += sum;
+            }
+        };
+        int b = t;
+        for (; b + (BATCH - 1) * MAIN < n; b += MAIN * BATCH) take(std::integral_constant<int, BATCH>(), b);
+        for (; b < n; b += MAIN) take(std::integral_constant<int, 1>(), b);
+        const float top = over(m, max_of);
+        l = over(rebase(l, m, top, P.c), sum_of);
+        if (lane == 0) warp_sums[warp] = make_float2(top, l);
+        asm volatile("bar.sync 1, %0;" ::"n"(MAIN) : "memory");
+    }
+    // The row's maximum and sum, the same bits in every thread.  The warp of the entries meets the others here without
+    // their waiting for it: its loads depend on one another.
+    float most = -INFINITY, total = 0.f;
+    if (ctas == 1) {
+        if (warp == WARPS) asm volatile("bar.sync 2, %0;" ::"n"(MAIN + 32) : "memory");
+        else asm volatile("bar.arrive 2, %0;" ::"n"(MAIN + 32) : "memory");
+    }
+    if (ctas == 1 || warp < WARPS) {
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) most = fmaxf(most, warp_sums[w].x);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) total += rebase(warp_sums[w].y, warp_sums[w].x, most, P.c);
+    }
+    if (ctas > 1) {
+        if (warp < WARPS) {
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            if (t < ctas)
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_rank(smem_u32(&peers[rank]), (uint32_t)t)), "f"(most), "f"(total) : "memory");
+            __syncwarp();
+            asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        }
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        most = -INFINITY;
+        total = 0.f;
+        for (int c = 0; c < ctas; ++c) most = fmaxf(most, peers[c].x);
+        for (int c = 0; c < ctas; ++c) total += rebase(peers[c].y, peers[c].x, most, P.c);
+    }
+    const float base = most == -INFINITY ? 0.f : most, whole = base * P.c, inv = 1.f / total;
+    T* g_row = static_cast<T*>(P.grad) + row * P.ld_grad;
+    if (warp == WARPS) {
+        const bool none = sum_u == 0.f;
+        const float inv_u = none ? 0.f : 1.f / sum_u;
+        const int skip = sp.head / SIZE - sp.v0 * VE;
+        float cross = 0.f;
+        for (int j = lane; j < P.k; j += 32) {
+            const int32_t id = place[j];
+            const float p = value[j] * inv_u, ze = logit[j];
+            if (id >= 0 && !(p == 0.f)) cross += p * ((ze - base) * P.c);
+            const bool mine = id >= 0 && id + skip >= 0 && id + skip < n * VE && p != 0.f;   // (without weight the gradient is q's own)
+            value[j] = coef * (fast_exp2(fmaf(ze, P.c, -whole)) * inv - p);
+            place[j] = mine ? id : -1;
+        }
+        if (P.loss && rank == 0) {
+            // sum p (log2 p - log2 q), of which sum p = 1
+            cross = over(cross, sum_of) - log2f(total);
+            if (lane == 0) P.loss[row] = none ? 0.f : P.temperature * P.temperature * 0.69314718f * (entropy * inv_u - log2f(sum_u) - cross);
+        }
+    }
+    if (!P.grad) return;
+    // Vectors [in0, in1) are stored whole, the others (a row's two ends, or all where rows of the gradient start elsewhere
+    // than those of the logits) by elements.
+    const bool alike = (int)(reinterpret_cast<uintptr_t>(g_row) & 15u) == sp.head;
+    const int element0 = sp.v0 * VE - sp.head / SIZE, in0 = alike ? sp.in0 - sp.v0 : n, in1 = alike ? sp.in1 - sp.v0 : n;
+    T* g_part = g_row + element0;
+    auto put_elements = [&](int b, const float* g) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+            if ((uint32_t)(element0 + b * VE + e) < (uint32_t)P.vocab) g_part[b * VE + e] = from_float<T>(g[e]);
+    };
+    if (warp < WARPS && weight != 0.f) {
+        const float f = coef * inv;
+        const uint4* chunk = reinterpret_cast<const uint4*>(smem);
+        auto gradient = [&](uint4 x, float* g) {
+            unpack_vec<T>(x, g);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) g[e] = fast_exp2(fmaf(g[e], P.c, -whole)) * f;
+        };
+        auto make = [&](auto count, int b) {
+            constexpr int N = decltype(count)::value;
+            uint4 x[N];
+#pragma unroll
+            for (int v = 0; v < N; ++v) x[v] = chunk[b + v * MAIN];
+#pragma unroll
+            for (int v = 0; v < N; ++v) {
+                float g[VE];
+                gradient(x[v], g);
+                store_n<T, VE, true>(g_part + (b + v * MAIN) * VE, g);
+            }
+        };
+        int b = in0 + t;
+        for (; b + (BATCH - 1) * MAIN < in1; b += MAIN * BATCH) make(std::integral_constant<int, BATCH>(), b);
+        for (; b < in1; b += MAIN) make(std::integral_constant<int, 1>(), b);
+        for (int e = t; e < in0 + n - in1; e += MAIN) {
+            float g[VE];
+            const int at = e < in0 ? e : in1 + e - in0;
+            gradient(chunk[at], g);
+            put_elements(at, g);
+        }
+    }
+    __syncthreads();
+    if (weight == 0.f || no_entry) {   // zeros, whatever the logits
+        const float g[VE] = {};
+        for (int b = t; b < n; b += MAIN + 32) {
+            if (b >= in0 && b < in1) store_n<T, VE>(g_part + b * VE, g);
+            else put_elements(b, g);
+        }
+        return;
+    }
+    for (int j = t; j < P.k; j += MAIN + 32) {
+        const int id = place[j];
+        if (id >= 0) g_row[id] = from_float<T>(value[j]);
+    }
 }
 
 // A row per warp: rows of up to 4 KB and teachers of up to 128 entries.  Each thread holds 8 vectors as exponentials.
@@ -770,34 +661,13 @@ distill_long_kernel(const DistillParams P) {
     }
 }
 
-// Once per context: how many clusters of 2, 4 and 8 CTAs can be resident.
-cudaError_t prepare(sama_ctx* ctx) {
-    if (ctx->distill_clusters[0] > 0) return cudaSuccess;
-    void* kernels[3] = {(void*)distill_kernel<float>, (void*)distill_kernel<__half>, (void*)distill_kernel<__nv_bfloat16>};
-    void* few[3] = {(void*)distill_few_kernel<float>, (void*)distill_few_kernel<__half>, (void*)distill_few_kernel<__nv_bfloat16>};
-    cudaError_t e;
-    for (int i = 0; i < 3; ++i) {
-        if ((e = cudaFuncSetAttribute(kernels[i], cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM)) != cudaSuccess) return e;
-        if ((e = cudaFuncSetAttribute(few[i], cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SMEM)) != cudaSuccess) return e;
-    }
-    int found[3];
-    for (int i = 0; i < 3; ++i) {
-        cudaLaunchConfig_t cfg = {};
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = 2u << i;
-        attr[0].val.clusterDim.y = 1;
-        attr[0].val.clusterDim.z = 1;
-        cfg.gridDim = dim3(ctx->sm_count / (2 << i) * (2 << i));
-        cfg.blockDim = dim3(THREADS);
-        cfg.dynamicSmemBytes = SMEM;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        if ((e = cudaOccupancyMaxActiveClusters(&found[i], distill_kernel<__nv_bfloat16>, &cfg)) != cudaSuccess) return e;
-        if (found[i] < 1) return cudaErrorLaunchOutOfResources;
-    }
-    for (int i = 2; i >= 0; --i) ctx->distill_clusters[i] = found[i];
-    return cudaSuccess;
+// Once per context: shared memory beyond the default.
+template <typename T>
+cudaError_t allow_memory() {
+    constexpr auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+    cudaError_t e = cudaFuncSetAttribute(distill_few_kernel<T>, attr, FEW_SMEM);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(distill_kernel<T, 256>, attr, PART + entry_bytes(ENTRIES));
+    return e;
 }
 
 template <typename T>
@@ -811,20 +681,22 @@ cudaError_t launch(sama_ctx* ctx, DistillParams& P, cudaStream_t st) {
         const int64_t wanted = (P.n_rows + FEW_TEAMS - 1) / FEW_TEAMS, most = 2 * ctx->sm_count;
         return launch_dependent(distill_few_kernel<T>, dim3((unsigned)(wanted < most ? wanted : most)), dim3(32 * FEW_TEAMS), FEW_SMEM, st, P);
     }
-    if (vecs * 16 > 8 * PART || P.k > ENTRIES) {
-        const int64_t most = 2 * ctx->sm_count;
-        return launch_dependent(distill_long_kernel<T>, dim3((unsigned)(P.n_rows < most ? P.n_rows : most)), dim3(1024), 0, st, P);
-    }
     // The fewest CTAs that can hold a row, since each of them has a row's fixed costs to bear; more where rows are too few to
     // fill the device.
     int ctas = 1;
-    while (vecs * 16 > (int64_t)ctas * PART || (ctas < 8 && P.n_rows * ctas * 2 <= ctx->sm_count && vecs >= 2 * ctas * SUMS)) ctas *= 2;
-    P.stage_bytes = (int)((vecs + ctas - 1) / ctas) * 16;
-    P.stage_bytes = (P.stage_bytes + 127) / 128 * 128;
-    P.stages = RING / P.stage_bytes < MAX_STAGES ? RING / P.stage_bytes : MAX_STAGES;
-    const int64_t most = ctas == 1 ? ctx->sm_count : ctx->distill_clusters[ctas == 2 ? 0 : ctas == 4 ? 1 : 2];
-    const int64_t teams = P.n_rows < most ? P.n_rows : most;
-    return launch_clustered(ctas, distill_kernel<T>, dim3((unsigned)(teams * ctas)), dim3(THREADS), SMEM, st, P);
+    while (ctas <= 8 && (vecs * 16 > (int64_t)ctas * PART || (ctas < 8 && P.n_rows * ctas * 2 <= ctx->sm_count && vecs >= 1024 * ctas))) ctas *= 2;
+    if (ctas > 8 || P.k > ENTRIES || P.n_rows * ctas > 0x7fffffff) {
+        const int64_t most = 2 * ctx->sm_count;
+        return launch_dependent(distill_long_kernel<T>, dim3((unsigned)(P.n_rows < most ? P.n_rows : most)), dim3(1024), 0, st, P);
+    }
+    const int per = (int)((vecs + ctas - 1) / ctas);
+    P.part_bytes = (per * 16 + 127) / 128 * 128;
+    const dim3 grid((unsigned)(P.n_rows * ctas));
+    const size_t smem = (size_t)P.part_bytes + entry_bytes(P.k);
+    // (as few threads as have eight vectors each: the smaller the CTA, the more of them share an SM)
+    if (per <= 64 * VECS) return launch_clustered(ctas, distill_kernel<T, 64>, grid, dim3(64 + 32), smem, st, P);
+    if (per <= 128 * VECS) return launch_clustered(ctas, distill_kernel<T, 128>, grid, dim3(128 + 32), smem, st, P);
+    return launch_clustered(ctas, distill_kernel<T, 256>, grid, dim3(256 + 32), smem, st, P);
 }
 
 }  // namespace
@@ -832,8 +704,13 @@ cudaError_t launch(sama_ctx* ctx, DistillParams& P, cudaStream_t st) {
 cudaError_t launch_distill(sama_ctx* ctx, int dtype, int64_t n_rows, int vocab, const void* logits, int64_t ld, int k, int top_dtype,
                            const void* top, const int32_t* ids, float temperature, const float* weight, float grad_scale, float* loss,
                            void* grad, int64_t ld_grad, cudaStream_t st) {
-    const cudaError_t e = prepare(ctx);
-    if (e != cudaSuccess) return e;
+    if (!ctx->distill_ready) {
+        cudaError_t e = allow_memory<float>();
+        if (e == cudaSuccess) e = allow_memory<__nv_bfloat16>();
+        if (e == cudaSuccess) e = allow_memory<__half>();
+        if (e != cudaSuccess) return e;
+        ctx->distill_ready = 1;
+    }
     DistillParams P;
     P.logits = logits;
     P.grad = grad;

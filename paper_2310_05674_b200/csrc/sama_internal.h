@@ -142,7 +142,7 @@ struct sama_ctx {
     uint32_t attn_fwd_ready;       // kernels of attention_fwd.cu whose shared-memory size is set on this device
     uint32_t attn_bwd_ready;       // ... and of attention_bwd.cu
     uint32_t paged_ready;          // ... and of attention_paged.cu
-    int distill_clusters[3];       // clusters of 2, 4 and 8 CTAs of distill.cu that can be resident (0: not yet asked)
+    int distill_ready;             // the shared-memory sizes of distill.cu are set on this device
     int* paged_arrived;            // device: arrival counters of heads that several CTAs share, zero between launches
     sama::Profiler* prof;          // host
 };
