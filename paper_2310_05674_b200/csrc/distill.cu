@@ -25,7 +25,7 @@ namespace {
 constexpr int VECS = 8, BATCH = 4;    // 16-byte vectors that a thread has in hand
 constexpr int kMaxEntries = 1024;
 // one row per cluster or CTA
-constexpr int PART = 64 * 1024;                            // bytes of a row in a CTA, at most
+constexpr int PART = 64 * 1024, ALONE = 104 * 1024;        // bytes of a row in a CTA of a cluster, and in one by itself
 constexpr int ENTRIES = 512, BITS = 8192;                  // of the teacher's, at most; of the table that finds an id twice
 constexpr int entry_bytes(int k) { return (k + 31) / 32 * 32 * 12 + BITS / 8; }
 // one row per warp
@@ -666,7 +666,7 @@ template <typename T>
 cudaError_t allow_memory() {
     constexpr auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
     cudaError_t e = cudaFuncSetAttribute(distill_few_kernel<T>, attr, FEW_SMEM);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(distill_kernel<T, 256>, attr, PART + entry_bytes(ENTRIES));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(distill_kernel<T, 256>, attr, ALONE + entry_bytes(ENTRIES));
     return e;
 }
 
@@ -681,10 +681,12 @@ cudaError_t launch(sama_ctx* ctx, DistillParams& P, cudaStream_t st) {
         const int64_t wanted = (P.n_rows + FEW_TEAMS - 1) / FEW_TEAMS, most = 2 * ctx->sm_count;
         return launch_dependent(distill_few_kernel<T>, dim3((unsigned)(wanted < most ? wanted : most)), dim3(32 * FEW_TEAMS), FEW_SMEM, st, P);
     }
-    // The fewest CTAs that can hold a row, since each of them has a row's fixed costs to bear; more where rows are too few to
-    // fill the device.
-    int ctas = 1;
-    while (ctas <= 8 && (vecs * 16 > (int64_t)ctas * PART || (ctas < 8 && P.n_rows * ctas * 2 <= ctx->sm_count && vecs >= 1024 * ctas))) ctas *= 2;
+    // One CTA, if two of them fit an SM with such rows: to meet the others of a cluster twice costs more than a third
+    // would give (100 KB: 155 us in one CTA, 185 in clusters of two, 4096 rows).  Beyond that as few as leave three per SM
+    // (256 KB, 4096 rows: clusters of 4 484 us, of 3 551, of 2 609, of 8 658).  More where rows are too few for the device.
+    const int64_t bytes = vecs * 16;
+    int64_t ctas = bytes <= ALONE ? 1 : (bytes + PART - 1) / PART;
+    while (ctas < 8 && P.n_rows * ctas * 2 <= ctx->sm_count && vecs >= 1024 * ctas) ++ctas;
     if (ctas > 8 || P.k > ENTRIES || P.n_rows * ctas > 0x7fffffff) {
         const int64_t most = 2 * ctx->sm_count;
         return launch_dependent(distill_long_kernel<T>, dim3((unsigned)(P.n_rows < most ? P.n_rows : most)), dim3(1024), 0, st, P);
@@ -694,9 +696,9 @@ cudaError_t launch(sama_ctx* ctx, DistillParams& P, cudaStream_t st) {
     const dim3 grid((unsigned)(P.n_rows * ctas));
     const size_t smem = (size_t)P.part_bytes + entry_bytes(P.k);
     // (as few threads as have eight vectors each: the smaller the CTA, the more of them share an SM)
-    if (per <= 64 * VECS) return launch_clustered(ctas, distill_kernel<T, 64>, grid, dim3(64 + 32), smem, st, P);
-    if (per <= 128 * VECS) return launch_clustered(ctas, distill_kernel<T, 128>, grid, dim3(128 + 32), smem, st, P);
-    return launch_clustered(ctas, distill_kernel<T, 256>, grid, dim3(256 + 32), smem, st, P);
+    if (per <= 64 * VECS) return launch_clustered((int)ctas, distill_kernel<T, 64>, grid, dim3(64 + 32), smem, st, P);
+    if (per <= 128 * VECS) return launch_clustered((int)ctas, distill_kernel<T, 128>, grid, dim3(128 + 32), smem, st, P);
+    return launch_clustered((int)ctas, distill_kernel<T, 256>, grid, dim3(256 + 32), smem, st, P);
 }
 
 }  // namespace
