@@ -1,5 +1,7 @@
 // What the attention kernels share: the packed texts, how a block finds its own, what a query sees, and the scores.
 #pragma once
+#include <type_traits>
+
 #include "num_types.h"
 #include "sama_internal.h"
 #include "tc_ptx.h"
@@ -95,8 +97,55 @@ __device__ __forceinline__ int attn_first_query(const AttnShape& a, const AttnTe
 }
 
 // tanh(z) = 1 - 2 / (1 + exp 2z): an absolute error of two units in the last place of 1, which is what a capped score
-// needs (the hardware's own approximation has 2^-11, a hundredth of a weight at a cap of 30).
+// needs (the hardware's own approximation has 2^-11, a hundredth of a weight at a cap of 30).  That takes two of the three
+// results of the special-function unit per score (16 a cycle and SM), so where no score of a warp's tile is beyond 0.75 caps
+// tanh is a polynomial, z p(z^2) with p of degree 4 through tanh(z) / z at the Chebyshev points of [0, 0.75^2]: 1.3e-7.
 __device__ __forceinline__ float attn_tanh(float z) { return fmaf(-2.f, fast_rcp(1.f + fast_exp2(2.f * kLog2e * z)), 1.f); }
+constexpr float kTanhNear = 0.75f;
+__device__ __forceinline__ float attn_tanh_near(float z) {
+    const float u = z * z;
+    float p = 0.0129166516f;
+    p = fmaf(p, u, -0.0500416085f);
+    p = fmaf(p, u, 0.132584617f);
+    p = fmaf(p, u, -0.333281934f);
+    p = fmaf(p, u, 0.999999404f);
+    return z * p;
+}
+// 2^x for x <= 2^20 on the multiply-add units: 2^n by the exponent, 2^f for |f| <= 1/2 by the polynomial of degree 4 through
+// it at the Chebyshev points of that interval (relative error 4e-6, a thousandth of the rounding that weights get).  At
+// least 2^-127: not for masked scores.
+__device__ __forceinline__ float poly_exp2(float x) {
+    x = fmaxf(x, -127.f);
+    const float shifted = x + 12582912.f, f = x - (shifted - 12582912.f);
+    float p = 0.00966636837f;
+    p = fmaf(p, f, 0.0559219755f);
+    p = fmaf(p, f, 0.240223497f);
+    p = fmaf(p, f, 0.693121016f);
+    p = fmaf(p, f, 1.0f);
+    return __uint_as_float(__float_as_uint(p) + (__float_as_uint(shifted) << 23));
+}
+// Two values rounded to T.  Conversions to bf16 run on the special-function unit, too, half as slow as an exponential;
+// adding half a unit in the last place (`half` = 0x8000: to nearest, ties away from zero) does not.  A NaN would not survive
+// that; `half` = 0 cuts off and keeps it.
+template <typename T> __device__ __forceinline__ uint32_t attn_pack(float a, float b, uint32_t half) {
+    if constexpr (std::is_same<T, __nv_bfloat16>::value)
+        return __byte_perm(__float_as_uint(a) + half, __float_as_uint(b) + half, 0x7632);
+    else
+        return pack2<T>(a, b);
+}
+
+// The largest of N values, in eight chains: one would wait for each result before the next.
+template <int N, typename F>
+__device__ __forceinline__ float attn_max(F&& value) {
+    float m[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = value(i);
+#pragma unroll
+    for (int k = 8; k < N; k += 8)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = fmaxf(m[i], value(k + i));
+    return fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), fmaxf(fmaxf(m[4], m[5]), fmaxf(m[6], m[7])));
+}
 
 // D (fp32) += A B^T with A, 128 rows of 16-bit values two to a column, in tensor memory.
 __device__ __forceinline__ void umma16_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {

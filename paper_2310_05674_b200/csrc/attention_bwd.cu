@@ -260,27 +260,38 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                 tmem_ld32_nowait(dp_cols(w) + lanes + h, dp);
                 tmem_wait_ld();
                 uint32_t rp[16], rx[16];
+                auto make = [&](auto near, auto some) {   // (some: scores are masked)
 #pragma unroll
-                for (int k = 0; k < 32; k += 2) {
-                    float4 two = make_float4(lse2, delta, lse2, delta);
-                    if (KEYS) two = *reinterpret_cast<const float4*>(st + h + k);
-                    float p[2], g[2];
+                    for (int k = 0; k < 32; k += 2) {
+                        float4 two = make_float4(lse2, delta, lse2, delta);
+                        if (KEYS) two = *reinterpret_cast<const float4*>(st + h + k);
+                        float p[2], g[2];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float v = s[k + e], slack = 1.f;
-                        if (CAP) {
-                            const float th = attn_tanh(v * inv_cap);
-                            v = cap2 * th;
-                            slack = fmaf(-th, th, 1.f);
+                        for (int e = 0; e < 2; ++e) {
+                            float v = s[k + e], slack = 1.f;
+                            if (CAP) {
+                                const float th = decltype(near)::value ? attn_tanh_near(v * inv_cap) : attn_tanh(v * inv_cap);
+                                v = cap2 * th;
+                                slack = fmaf(-th, th, 1.f);
+                            }
+                            if (BIAS) v = fmaf(-slope, fabsf(away - (float)(h + k + e)), CAP ? v : v * (a.scale * kLog2e));
+                            p[e] = fast_exp2(fmaf(v, c, -(e ? two.z : two.x)));
+                            g[e] = p[e] * (dp[k + e] - (e ? two.w : two.y));
+                            if (CAP) g[e] *= slack;
+                            if (decltype(some)::value && (h + k + e >= hi || (KEYS && h + k + e < lo))) p[e] = g[e] = 0.f;
                         }
-                        if (BIAS) v = fmaf(-slope, fabsf(away - (float)(h + k + e)), CAP ? v : v * (a.scale * kLog2e));
-                        p[e] = fast_exp2(fmaf(v, c, -(e ? two.z : two.x)));
-                        g[e] = p[e] * (dp[k + e] - (e ? two.w : two.y));
-                        if (CAP) g[e] *= slack;
-                        if (masked && (h + k + e >= hi || (KEYS && h + k + e < lo))) p[e] = g[e] = 0.f;
+                        if (KEYS) rp[k / 2] = pack2<T>(p[0], p[1]);
+                        rx[k / 2] = pack2<T>(g[0], g[1]);
                     }
-                    rp[k / 2] = pack2<T>(p[0], p[1]);
-                    rx[k / 2] = pack2<T>(g[0], g[1]);
+                };
+                if (CAP) {
+                    const float big = attn_max<32>([&](int k) { return fabsf(s[k]); });
+                    if (masked || !__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) make(std::false_type(), std::true_type());
+                    else make(std::true_type(), std::false_type());
+                } else if (masked) {
+                    make(std::false_type(), std::true_type());
+                } else {
+                    make(std::false_type(), std::false_type());
                 }
                 // over what this half's scores were, which no other thread reads
                 if (KEYS) tmem_st16_nowait(s_cols(w) + lanes + h / 2, rp);

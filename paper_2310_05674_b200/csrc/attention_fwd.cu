@@ -213,23 +213,27 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             for (int k = 0; k < BK; k += 32) tmem_ld32_nowait(s_cols(w) + lanes + k, s + k);
             tmem_wait_ld();
             if (CAP) {
+                const float big = attn_max<BK>([&](int k) { return fabsf(s[k]); });
+                if (__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) {
 #pragma unroll
-                for (int k = 0; k < BK; ++k) s[k] = cap2 * attn_tanh(s[k] * inv_cap);
+                    for (int k = 0; k < BK; ++k) s[k] = cap2 * attn_tanh_near(s[k] * inv_cap);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < BK; ++k) s[k] = cap2 * attn_tanh(s[k] * inv_cap);
+                }
             }
             if (BIAS) {
                 const float away = (float)(row + x.lk - x.lq - j * BK);
 #pragma unroll
                 for (int k = 0; k < BK; ++k) s[k] = fmaf(-slope, fabsf(away - (float)k), CAP ? s[k] : s[k] * (a.scale * kLog2e));
             }
-            if ((j + 1) * BK > seen_by_all) {
+            const bool masked = (j + 1) * BK > seen_by_all;
+            if (masked) {
                 const int left = seen - j * BK;
 #pragma unroll
                 for (int k = 0; k < BK; ++k) s[k] = k < left ? s[k] : -INFINITY;
             }
-            float top = s[0];
-#pragma unroll
-            for (int k = 1; k < BK; ++k) top = fmaxf(top, s[k]);
-            top *= c;
+            const float top = attn_max<BK>([&](int k) { return s[k]; }) * c;
             if (__any_sync(0xffffffffu, top > m + kRaise || (m == -INFINITY && top > m))) {
                 const float raised = fmaxf(m, top);
                 const float factor = raised == -INFINITY ? 1.f : fast_exp2(m - raised);
@@ -250,19 +254,25 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 }
             }
             const float from = m == -INFINITY ? 0.f : m;
-            float sum = 0.f;
+            // A quarter of the exponentials on the multiply-add units, where nothing is masked.  (A NaN is lost in a weight's
+            // rounding, but not in the sum by which the output is divided.)
+            float sums[4] = {0.f, 0.f, 0.f, 0.f};
+            auto weights = [&](auto some) {
 #pragma unroll
-            for (int k = 0; k < BK; k += 32) {
-                uint32_t r[16];
+                for (int k = 0; k < BK; k += 32) {
+                    uint32_t r[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float p0 = fast_exp2(fmaf(s[k + 2 * i], c, -from)), p1 = fast_exp2(fmaf(s[k + 2 * i + 1], c, -from));
-                    sum += p0 + p1;
-                    r[i] = pack2<T>(p0, p1);
+                    for (int i = 0; i < 16; ++i) {
+                        const float x0 = fmaf(s[k + 2 * i], c, -from), x1 = fmaf(s[k + 2 * i + 1], c, -from);
+                        const float p0 = fast_exp2(x0), p1 = decltype(some)::value && i % 2 == 1 ? poly_exp2(x1) : fast_exp2(x1);
+                        sums[i % 4] += p0 + p1;
+                        r[i] = pack2<T>(p0, p1);
+                    }
+                    tmem_st16_nowait(s_cols(w) + lanes + k / 2, r);
                 }
-                tmem_st16_nowait(s_cols(w) + lanes + k / 2, r);
-            }
-            l += sum;
+            };
+            weights(std::false_type());
+            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
