@@ -2,15 +2,21 @@
 //   P = 2^(x log2 e - lse),  dP = dO V^T,  dX = P (dP - delta) (1 - tanh^2),  delta = dO . O
 //   dQ = scale dX K,   dK = scale dX^T Q,   dV = P^T dO
 //
-// Two launches of one kernel template.  Each CTA keeps 128 rows of two operands and streams tiles of 64 rows of the other
+// Two launches of one kernel template.  Each CTA keeps 128 rows of two operands and streams tiles of 128 rows of the other
 // two past them: d-queries keeps (Q, dO) and streams (K, V); d-keys keeps (K, V) of a key head and streams (Q, dO) of every
 // head that shares it.  The products are formed with the kept rows as the lanes of tensor memory (S^T rather than S for
 // the keys), so that P and dX go back to tensor memory as the left operands of the last products and no tile is
 // transposed.  The sums of a row stay in one accumulator from its first tile to its last: no atomics, a fixed order.
 // Forming S and dP in both launches costs seven products in place of the five of one launch that adds to dQ in memory.
 //
-// Roles of the 10 warps: warp 0 copies, warp 1 issues products, warps 2..5 and 6..9 take the streamed tiles in turn, so
-// that the products of one tile run while the other's weights are formed.  Every wait is bounded.
+// The order of the products of tile i is  dP_i, dV (from P_i), S_i+1, dK (from dX_i), dP_i+1, ...:  P_i+1 is formed from
+// S_i+1 while dK and dP_i+1 run, dX_i from dP_i while dV and S_i+1 run.  S, dP and two accumulators of 128 columns fill tensor
+// memory.  (Tiles of 64 rows in two buffers, which the two halves of the warps took in turn, were half as fast: a product
+// 64 wide takes 48 cycles in place of 32, and each wait of the issuing thread leaves the tensor cores idle for some 200
+// cycles, since it can run ahead of them by a product or two only.)
+//
+// Roles of the 10 warps: warp 0 copies, warp 1 issues products, warps 2..9 form P and dX: two warps share 32 rows, each of
+// them has 64 of a tile's columns.  Every wait is bounded.
 #include <type_traits>
 
 #include "attention.h"
@@ -20,12 +26,12 @@ namespace sama {
 namespace {
 
 constexpr int THREADS = 320;
-constexpr int BT = 64;   // rows of a streamed tile
+constexpr int BT = 128;  // rows of a streamed tile
 
 template <int D> struct BwdTile {
-    static constexpr int STAGES = D == 64 ? 6 : 4;
+    static constexpr int STAGES = D == 64 ? 4 : 2;
     static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2, STAGE = 2 * TILE;
-    static constexpr int STATS = BT * 8;      // (lse, delta) of a streamed tile's queries
+    static constexpr int STATS = BT * 8;      // lse and delta of a streamed tile's queries
     static constexpr int SMEM = 2 * KEPT + STAGES * (STAGE + STATS) + 2 * kAttnRows * 4 + 256 + 1024;
 };
 
@@ -34,7 +40,7 @@ struct alignas(64) BwdParams {
     AttnShape a;
     const void *out, *dout;
     const float* lse;
-    float2* stats;      // [heads][n_q]: lse log2 e (infinity for a query that sees nothing) and delta
+    float *lse2, *delta;   // [heads][n_q]: lse log2 e (infinity for a query that sees nothing), and delta
     void* grad[2];      // dQ, or dK and dV
     int64_t ld[2];
     int slots;
@@ -81,9 +87,9 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     const uint32_t bars = halves + 2 * kAttnRows * 4;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
-    auto s_bar = [&](int w) { return bars + 8u * (2 * STAGES + w); };       // S and dP are there
-    auto p_bar = [&](int w) { return bars + 8u * (2 * STAGES + 2 + w); };   // P and dX are there
-    const uint32_t kept_bar = bars + 8u * (2 * STAGES + 4), done_bar = kept_bar + 8u;
+    const uint32_t s_bar = bars + 8u * (2 * STAGES), dp_bar = s_bar + 8u;   // S, dP are there
+    const uint32_t p_bar = dp_bar + 8u, x_bar = p_bar + 8u;                 // S may be overwritten and (d-keys) P is there; dX is there
+    const uint32_t kept_bar = x_bar + 8u, done_bar = kept_bar + 8u;
     const uint32_t tmem_slot = done_bar + 8u;
     volatile uint32_t* tmem_ptr_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_slot - raw));
     volatile uint32_t* abort_flag = tmem_ptr_slot + 1;
@@ -94,10 +100,10 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             mbar_init(full_bar(s), KEYS ? 33 : 1);   // the copies, and (d-keys) each lane's share of the statistics
             mbar_init(empty_bar(s), 1);
         }
-        for (int w = 0; w < 2; ++w) {
-            mbar_init(s_bar(w), 1);
-            mbar_init(p_bar(w), 4);
-        }
+        mbar_init(s_bar, 1);
+        mbar_init(dp_bar, 1);
+        mbar_init(p_bar, 8);
+        mbar_init(x_bar, 8);
         mbar_init(kept_bar, 1);
         mbar_init(done_bar, 1);
         *abort_flag = 0;
@@ -108,9 +114,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_ptr_slot;
-    auto s_cols = [&](int w) { return tmem + (uint32_t)(w * BT); };
-    auto dp_cols = [&](int w) { return tmem + (uint32_t)(2 * BT + w * BT); };
-    auto g_cols = [&](int i) { return tmem + (uint32_t)(4 * BT + i * D); };
+    const uint32_t s_cols = tmem, dp_cols = tmem + BT;
+    auto g_cols = [&](int i) { return tmem + (uint32_t)(2 * BT + i * D); };
 
     auto raise_timeout = [&]() {
         *abort_flag = 1;
@@ -145,9 +150,12 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                         tma_load_3d(ring + s * C::STAGE + o * C::TILE + c * BT * 128, &P.streamed[o], full_bar(s), 64 * c, h, row);
             }
             if (KEYS) {
-                for (int r = lane; r < BT; r += 32)
-                    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(stats + s * C::STATS + 8 * r),
-                                 "l"(P.stats + (int64_t)h * a.n_q + min(row + r, a.n_q - 1)) : "memory");
+                for (int r = lane; r < BT; r += 32) {
+                    const int64_t at = (int64_t)h * a.n_q + min(row + r, a.n_q - 1);
+                    const uint32_t to = stats + s * C::STATS + 4 * r;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(P.lse2 + at) : "memory");
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4 * BT), "l"(P.delta + at) : "memory");
+                }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full_bar(s)) : "memory");
             }
         }
@@ -159,48 +167,61 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         }
         __syncwarp();
     } else if (warp == 1) {
-        bool ok = true;
-        auto products = [&](int i) {   // S = kept[0] streamed[0]^T, dP = kept[1] streamed[1]^T
-            const int s = i % STAGES, w = i & 1;
-            if (!(ok = wait(full_bar(s), (i / STAGES) & 1))) return;
+        bool ok = n > 0 && wait(kept_bar, 0);
+        // S (o = 0) or dP (o = 1) of a tile: kept[o] streamed[o]^T
+        auto scores = [&](int o, int s) {
+            const uint64_t da = make_desc(base + o * C::KEPT), db = make_desc(ring + s * C::STAGE + o * C::TILE);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const uint64_t at = (uint64_t)((k / 4 * kAttnRows * 128 + k % 4 * 32) >> 4);
+                umma16(o ? dp_cols : s_cols, da + at, db + at, IDESC_S, k > 0);
+            }
+            umma_commit(o ? dp_bar : s_bar);
+        };
+        // dK or dQ (o = 0) from dX, dV (o = 1) from P.  Either warp of 32 rows has left its 64 columns, in 16 bits, in
+        // the first half of its 64 columns of fp32.
+        auto gradient = [&](int o, int s, bool add) {
+            const uint64_t db = attn_desc_mn(ring + s * C::STAGE + o * C::TILE, BT);
+#pragma unroll
+            for (int k = 0; k < BT / 16; ++k)
+                umma16_ta(g_cols(o), (o ? s_cols : dp_cols) + (uint32_t)(k / 4 * 64 + k % 4 * 8), db + (uint64_t)(k * 2048 >> 4), IDESC_G, add || k > 0);
+        };
+        auto arrived = [&](int tile_of_head, int s, int parity) {
+            if (!wait(full_bar(s), parity)) return false;
             tc_fence_after();
-            const int from = streamed_rows - (tile0 + (KEYS ? i % per_head : i)) * BT;
+            const int from = streamed_rows - tile_of_head * BT;
             if (from < BT) {
                 attn_zero_rows<D / 64>(ring + s * C::STAGE, from, BT);
                 attn_zero_rows<D / 64>(ring + s * C::STAGE + C::TILE, from, BT);
             }
-            if (lane == 0) {
-#pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                    const uint64_t da = make_desc(base + o * C::KEPT), db = make_desc(ring + s * C::STAGE + o * C::TILE);
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-                        umma16(o ? dp_cols(w) : s_cols(w), da + (uint64_t)((k / 4 * kAttnRows * 128 + k % 4 * 32) >> 4),
-                               db + (uint64_t)((k / 4 * BT * 128 + k % 4 * 32) >> 4), IDESC_S, k > 0);
-                }
-                umma_commit(s_bar(w));
-            }
-            __syncwarp();
+            return true;
         };
-        if (n > 0) ok = wait(kept_bar, 0);
-        for (int i = 0; ok && i < 2 && i < n; ++i) products(i);
+        if (ok && (ok = arrived(tile0, 0, 0)) && lane == 0) {
+            scores(0, 0);
+            scores(1, 0);
+        }
+        int s = 0, next = 1 % STAGES, parity = STAGES == 1 ? 1 : 0, next_tile = 1;
         for (int i = 0; ok && i < n; ++i) {
-            const int s = i % STAGES, w = i & 1;
-            if (!(ok = wait(p_bar(w), (i >> 1) & 1))) break;
+            if (next_tile == per_head) next_tile = 0;   // (d-keys: the next head's first tile)
+            if (!(ok = wait(p_bar, i & 1))) break;
+            tc_fence_after();
+            if (KEYS && lane == 0) gradient(1, s, i > 0);
+            // (products are executed in order: the next scores do not overtake the weights they replace)
+            if (i + 1 < n) {
+                if (!(ok = arrived(tile0 + next_tile, next, parity))) break;
+                if (lane == 0) scores(0, next);
+            }
+            if (!(ok = wait(x_bar, i & 1))) break;
             tc_fence_after();
             if (lane == 0) {
-                const uint64_t d0 = attn_desc_mn(ring + s * C::STAGE, BT), d1 = attn_desc_mn(ring + s * C::STAGE + C::TILE, BT);
-#pragma unroll
-                for (int k = 0; k < BT / 16; ++k) {
-                    umma16_ta(g_cols(0), dp_cols(w) + 8u * k, d0 + (uint64_t)(k * 2048 >> 4), IDESC_G, i > 0 || k > 0);
-                    if (KEYS) umma16_ta(g_cols(1), s_cols(w) + 8u * k, d1 + (uint64_t)(k * 2048 >> 4), IDESC_G, i > 0 || k > 0);
-                }
+                gradient(0, s, i > 0);
                 if (i + STAGES < n) umma_commit(empty_bar(s));
-                if (i + 1 == n) umma_commit(done_bar);
+                if (i + 1 < n) scores(1, next); else umma_commit(done_bar);
             }
             __syncwarp();
-            // (products are executed in order: the next scores do not overtake the weights they replace)
-            if (i + 2 < n) products(i + 2);
+            s = next;
+            ++next_tile;
+            if (++next == STAGES) { next = 0; parity ^= 1; }
         }
     } else {
         const int w = (warp - 2) >> 2, quarter = warp & 3;
@@ -237,70 +258,125 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             part[w * kAttnRows + quarter * 32 + lane] = sum;
             asm volatile("bar.sync 1, 256;" ::: "memory");
             delta = part[quarter * 32 + lane] + part[kAttnRows + quarter * 32 + lane];
-            if (w == 0 && real) P.stats[(int64_t)head0 * a.n_q + x.q0 + row] = make_float2(lse2, delta);
+            if (w == 0 && real) {
+                P.lse2[(int64_t)head0 * a.n_q + x.q0 + row] = lse2;
+                P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta;
+            }
         }
         // d-queries: the row sees keys below `edge`; d-keys: the row is seen by queries from `edge` on
         const int edge = KEYS ? attn_first_query(a, x, row) : attn_seen(a, x, row);
         const int edge_of_all = KEYS ? attn_first_query(a, x, row0 + 31) : attn_seen(a, x, row0);
 
-        for (int i = w; i < n; i += 2) {
-            const int at = (tile0 + (KEYS ? i % per_head : i)) * BT;   // first streamed row, in the text
-            const float slope = BIAS ? a.slopes[KEYS ? head0 * a.group + i / per_head : head0] * kLog2e : 0.f;
-            const float2* st = reinterpret_cast<const float2*>(smem_raw + (stats - raw) + i % STAGES * C::STATS);
-            if (KEYS && !(ok = wait(full_bar(i % STAGES), (i / STAGES) & 1))) break;
-            if (!(ok = wait(s_bar(w), (i >> 1) & 1))) break;
+        constexpr int MY = BT / 2;   // columns of a warp
+        int s = 0, parity = 0, tile_of_head = 0, head = KEYS ? head0 * a.group : head0;
+        float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
+        for (int i = 0; i < n; ++i) {
+            const int at = (tile0 + tile_of_head) * BT + w * MY;   // this warp's first streamed row, in the text
+            const float* lses = reinterpret_cast<const float*>(smem_raw + (stats - raw) + s * C::STATS) + w * MY;
+            const float* deltas = lses + BT;
+            if (KEYS && !(ok = wait(full_bar(s), parity))) break;
+            if (!(ok = wait(s_bar, i & 1))) break;
             tc_fence_after();
-            const bool masked = KEYS ? at < edge_of_all || at + BT > x.lq : at + BT > edge_of_all;
+            const bool masked = KEYS ? at < edge_of_all || at + MY > x.lq : at + MY > edge_of_all;
             const int lo = KEYS ? edge - at : 0, hi = KEYS ? x.lq - at : edge - at;   // visible columns
             const float away = BIAS ? (float)(KEYS ? row - (x.lk - x.lq) - at : row + x.lk - x.lq - at) : 0.f;
+            float p[MY];   // the weights, in the end times 1 - tanh^2
+            tmem_ld32_nowait(s_cols + lanes + w * MY, p);
+            tmem_ld32_nowait(s_cols + lanes + w * MY + 32, p + 32);
+            tmem_wait_ld();
+            if (!KEYS) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_bar);
+            }
+            auto weights = [&](auto near, auto some) {   // (some: scores are masked)
 #pragma unroll
-            for (int h = 0; h < BT; h += 32) {
-                float s[32], dp[32];
-                tmem_ld32_nowait(s_cols(w) + lanes + h, s);
-                tmem_ld32_nowait(dp_cols(w) + lanes + h, dp);
-                tmem_wait_ld();
-                uint32_t rp[16], rx[16];
-                auto make = [&](auto near, auto some) {   // (some: scores are masked)
+                for (int h = 0; h < MY; h += 32) {
+                    uint32_t r[16];
 #pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        float4 two = make_float4(lse2, delta, lse2, delta);
-                        if (KEYS) two = *reinterpret_cast<const float4*>(st + h + k);
-                        float p[2], g[2];
+                    for (int k = h; k < h + 32; k += 4) {
+                        float4 lse4 = make_float4(lse2, lse2, lse2, lse2);
+                        if (KEYS) lse4 = *reinterpret_cast<const float4*>(lses + k);
+                        const float l4[4] = {lse4.x, lse4.y, lse4.z, lse4.w};
+                        float slack[4];
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            float v = s[k + e], slack = 1.f;
+                        for (int e = 0; e < 4; ++e) {
+                            float v = p[k + e];
                             if (CAP) {
                                 const float th = decltype(near)::value ? attn_tanh_near(v * inv_cap) : attn_tanh(v * inv_cap);
                                 v = cap2 * th;
-                                slack = fmaf(-th, th, 1.f);
+                                slack[e] = fmaf(-th, th, 1.f);
                             }
-                            if (BIAS) v = fmaf(-slope, fabsf(away - (float)(h + k + e)), CAP ? v : v * (a.scale * kLog2e));
-                            p[e] = fast_exp2(fmaf(v, c, -(e ? two.z : two.x)));
-                            g[e] = p[e] * (dp[k + e] - (e ? two.w : two.y));
-                            if (CAP) g[e] *= slack;
-                            if (decltype(some)::value && (h + k + e >= hi || (KEYS && h + k + e < lo))) p[e] = g[e] = 0.f;
+                            if (BIAS) v = fmaf(-slope, fabsf(away - (float)(k + e)), CAP ? v : v * (a.scale * kLog2e));
+                            v = fast_exp2(fmaf(v, c, -l4[e]));
+                            if (decltype(some)::value && (k + e >= hi || (KEYS && k + e < lo))) v = 0.f;
+                            p[k + e] = v;
                         }
-                        if (KEYS) rp[k / 2] = pack2<T>(p[0], p[1]);
-                        rx[k / 2] = pack2<T>(g[0], g[1]);
+                        if (KEYS) {
+                            r[(k - h) / 2] = pack2<T>(p[k], p[k + 1]);
+                            r[(k - h) / 2 + 1] = pack2<T>(p[k + 2], p[k + 3]);
+                        }
+                        if (CAP) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) p[k + e] *= slack[e];
+                        }
                     }
-                };
-                if (CAP) {
-                    const float big = attn_max<32>([&](int k) { return fabsf(s[k]); });
-                    if (masked || !__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) make(std::false_type(), std::true_type());
-                    else make(std::true_type(), std::false_type());
-                } else if (masked) {
-                    make(std::false_type(), std::true_type());
-                } else {
-                    make(std::false_type(), std::false_type());
+                    // over the scores that this thread has read
+                    if (KEYS) tmem_st16_nowait(s_cols + lanes + w * MY + h / 2, r);
                 }
-                // over what this half's scores were, which no other thread reads
-                if (KEYS) tmem_st16_nowait(s_cols(w) + lanes + h / 2, rp);
-                tmem_st16_nowait(dp_cols(w) + lanes + h / 2, rx);
+            };
+            if (CAP) {
+                const float big = attn_max<MY>([&](int k) { return fabsf(p[k]); });
+                if (masked || !__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) weights(std::false_type(), std::true_type());
+                else weights(std::true_type(), std::false_type());
+            } else if (masked) {
+                weights(std::false_type(), std::true_type());
+            } else {
+                weights(std::false_type(), std::false_type());
             }
+            if (KEYS) {
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_bar);
+            }
+            if (!(ok = wait(dp_bar, i & 1))) break;
+            tc_fence_after();
+            auto slopes_of_scores = [&](auto some) {
+#pragma unroll
+                for (int h = 0; h < MY; h += 32) {
+                    float dp[32];
+                    uint32_t r[16];
+                    tmem_ld32_nowait(dp_cols + lanes + w * MY + h, dp);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) {
+                        float4 d4 = make_float4(delta, delta, delta, delta);
+                        if (KEYS) d4 = *reinterpret_cast<const float4*>(deltas + h + k);
+                        const float d[4] = {d4.x, d4.y, d4.z, d4.w};
+                        float g[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            g[e] = p[h + k + e] * (dp[k + e] - d[e]);
+                            if (decltype(some)::value && (h + k + e >= hi || (KEYS && h + k + e < lo))) g[e] = 0.f;
+                        }
+                        r[k / 2] = pack2<T>(g[0], g[1]);
+                        r[k / 2 + 1] = pack2<T>(g[2], g[3]);
+                    }
+                    tmem_st16_nowait(dp_cols + lanes + w * MY + h / 2, r);
+                }
+            };
+            if (masked) slopes_of_scores(std::true_type()); else slopes_of_scores(std::false_type());
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(p_bar(w));
+            if (lane == 0) mbar_arrive(x_bar);
+            if (++s == STAGES) { s = 0; parity ^= 1; }
+            if (++tile_of_head == per_head && KEYS && i + 1 < n) {
+                tile_of_head = 0;
+                ++head;
+                if (BIAS) slope = a.slopes[head] * kLog2e;
+            }
         }
         if (ok && n > 0) ok = wait(done_bar, 0);
         if (ok) {
@@ -356,7 +432,7 @@ cudaError_t launch(sama_ctx* ctx, int dtype, const BwdParams& P, cudaStream_t st
 
 }  // namespace
 
-size_t attention_grad_workspace(const AttnShape& a) { return (size_t)a.heads * a.n_q * sizeof(float2); }
+size_t attention_grad_workspace(const AttnShape& a) { return (size_t)a.heads * a.n_q * 2 * sizeof(float); }
 
 cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, const void* out, const float* lse,
                                   const void* dout, void* dq, void* dk, void* dv, void* ws, cudaStream_t st) {
@@ -365,7 +441,8 @@ cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnO
     P.out = out;
     P.dout = dout;
     P.lse = lse;
-    P.stats = static_cast<float2*>(ws);
+    P.lse2 = static_cast<float*>(ws);
+    P.delta = P.lse2 + (size_t)a.heads * a.n_q;
     const int64_t dense = (int64_t)a.heads * a.dim;
     auto query_maps = [&](CUtensorMap* m, int rows) {
         return attn_map(&m[0], op.q, op.dtype, a.dim, a.heads, a.n_q, op.q_stride, rows) &&
