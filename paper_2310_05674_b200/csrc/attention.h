@@ -102,38 +102,19 @@ __device__ __forceinline__ int attn_first_query(const AttnShape& a, const AttnTe
 // tanh is a polynomial, z p(z^2) with p of degree 4 through tanh(z) / z at the Chebyshev points of [0, 0.75^2]: 1.3e-7.
 __device__ __forceinline__ float attn_tanh(float z) { return fmaf(-2.f, fast_rcp(1.f + fast_exp2(2.f * kLog2e * z)), 1.f); }
 constexpr float kTanhNear = 0.75f;
-__device__ __forceinline__ float attn_tanh_near(float z) {
-    const float u = z * z;
-    float p = 0.0129166516f;
-    p = fmaf(p, u, -0.0500416085f);
-    p = fmaf(p, u, 0.132584617f);
-    p = fmaf(p, u, -0.333281934f);
-    p = fmaf(p, u, 0.999999404f);
-    return z * p;
-}
-// 2^x for x <= 2^20 on the multiply-add units: 2^n by the exponent, 2^f for |f| <= 1/2 by the polynomial of degree 4 through
-// it at the Chebyshev points of that interval (relative error 4e-6, a thousandth of the rounding that weights get).  At
-// least 2^-127: not for masked scores.
-__device__ __forceinline__ float poly_exp2(float x) {
-    x = fmaxf(x, -127.f);
-    const float shifted = x + 12582912.f, f = x - (shifted - 12582912.f);
-    float p = 0.00966636837f;
-    p = fmaf(p, f, 0.0559219755f);
-    p = fmaf(p, f, 0.240223497f);
-    p = fmaf(p, f, 0.693121016f);
-    p = fmaf(p, f, 1.0f);
-    return __uint_as_float(__float_as_uint(p) + (__float_as_uint(shifted) << 23));
-}
-// Two values rounded to T.  Conversions to bf16 run on the special-function unit, too, half as slow as an exponential;
-// adding half a unit in the last place (`half` = 0x8000: to nearest, ties away from zero) does not.  A NaN would not survive
-// that; `half` = 0 cuts off and keeps it.
-template <typename T> __device__ __forceinline__ uint32_t attn_pack(float a, float b, uint32_t half) {
-    if constexpr (std::is_same<T, __nv_bfloat16>::value)
-        return __byte_perm(__float_as_uint(a) + half, __float_as_uint(b) + half, 0x7632);
-    else
-        return pack2<T>(a, b);
-}
-
+struct AttnTanh {   // times `factor`, of `scale` times its argument
+    float k[5];
+    __device__ __forceinline__ AttnTanh(float scale, float factor) {
+        const float c[5] = {0.999999404f, -0.333281934f, 0.132584617f, -0.0500416085f, 0.0129166516f}, s2 = scale * scale;
+        float f = factor * scale;
+#pragma unroll
+        for (int i = 0; i < 5; ++i) { k[i] = c[i] * f; f *= s2; }
+    }
+    __device__ __forceinline__ float operator()(float x) const {
+        const float u = x * x;
+        return x * fmaf(fmaf(fmaf(fmaf(k[4], u, k[3]), u, k[2]), u, k[1]), u, k[0]);
+    }
+};
 // The largest of N values, in eight chains: one would wait for each result before the next.
 template <int N, typename F>
 __device__ __forceinline__ float attn_max(F&& value) {
@@ -145,6 +126,13 @@ __device__ __forceinline__ float attn_max(F&& value) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) m[i] = fmaxf(m[i], value(k + i));
     return fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), fmaxf(fmaxf(m[4], m[5]), fmaxf(m[6], m[7])));
+}
+
+// One lane of the warp, the same each time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
 }
 
 // D (fp32) += A B^T with A, 128 rows of 16-bit values two to a column, in tensor memory.

@@ -113,7 +113,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_ptr_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_ptr_slot, 0);
     const uint32_t s_cols = tmem, dp_cols = tmem + BT;
     auto g_cols = [&](int i) { return tmem + (uint32_t)(2 * BT + i * D); };
 
@@ -196,7 +196,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             }
             return true;
         };
-        if (ok && (ok = arrived(tile0, 0, 0)) && lane == 0) {
+        if (ok && (ok = arrived(tile0, 0, 0)) && elect_one()) {
             scores(0, 0);
             scores(1, 0);
         }
@@ -205,15 +205,15 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             if (next_tile == per_head) next_tile = 0;   // (d-keys: the next head's first tile)
             if (!(ok = wait(p_bar, i & 1))) break;
             tc_fence_after();
-            if (KEYS && lane == 0) gradient(1, s, i > 0);
+            if (KEYS && elect_one()) gradient(1, s, i > 0);
             // (products are executed in order: the next scores do not overtake the weights they replace)
             if (i + 1 < n) {
                 if (!(ok = arrived(tile0 + next_tile, next, parity))) break;
-                if (lane == 0) scores(0, next);
+                if (elect_one()) scores(0, next);
             }
             if (!(ok = wait(x_bar, i & 1))) break;
             tc_fence_after();
-            if (lane == 0) {
+            if (elect_one()) {
                 gradient(0, s, i > 0);
                 if (i + STAGES < n) umma_commit(empty_bar(s));
                 if (i + 1 < n) scores(1, next); else umma_commit(done_bar);
@@ -228,9 +228,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const int row0 = first + quarter * 32, row = row0 + lane;   // in the text
         const bool real = row < kept_rows;
-        constexpr bool RAW = !CAP && !BIAS;
-        const float c = RAW ? a.scale * kLog2e : 1.f;
-        const float inv_cap = CAP ? a.scale / a.cap : 0.f, cap2 = CAP ? a.cap * kLog2e : 0.f;
+        const float c = (CAP ? a.cap : a.scale) * kLog2e, inv_cap = CAP ? a.scale / a.cap : 0.f;
+        const AttnTanh tanh_near(inv_cap, 1.f);
         bool ok = true;
 
         float lse2 = 0.f, delta = 0.f;
@@ -303,12 +302,11 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                         for (int e = 0; e < 4; ++e) {
                             float v = p[k + e];
                             if (CAP) {
-                                const float th = decltype(near)::value ? attn_tanh_near(v * inv_cap) : attn_tanh(v * inv_cap);
-                                v = cap2 * th;
-                                slack[e] = fmaf(-th, th, 1.f);
+                                v = decltype(near)::value ? tanh_near(v) : attn_tanh(v * inv_cap);
+                                slack[e] = fmaf(-v, v, 1.f);
                             }
-                            if (BIAS) v = fmaf(-slope, fabsf(away - (float)(k + e)), CAP ? v : v * (a.scale * kLog2e));
-                            v = fast_exp2(fmaf(v, c, -l4[e]));
+                            if (BIAS) v = fmaf(-slope, fabsf(away - (float)(k + e)), v * c);
+                            v = fast_exp2(BIAS ? v - l4[e] : fmaf(v, c, -l4[e]));
                             if (decltype(some)::value && (k + e >= hi || (KEYS && k + e < lo))) v = 0.f;
                             p[k + e] = v;
                         }

@@ -91,7 +91,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_ptr_slot;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_ptr_slot, 0);
     auto s_cols = [&](int w) { return tmem + (uint32_t)(w * BK); };
     auto o_cols = [&](int w) { return tmem + (uint32_t)(2 * BK + w * D); };
 
@@ -165,9 +165,9 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 if (n_kt[w] == 0) continue;
                 if (!(ok = wait(q_bar(w), 0))) break;
                 tc_fence_after();
-                if (lane == 0) scores(w, 0);
+                if (elect_one()) scores(w, 0);
             }
-            if (ok && lane == 0) release(0);
+            if (ok && elect_one()) release(0);
         }
         for (int j = 0; ok && j < n_all; ++j) {
             const int vs = (2 * j + 1) % STAGES;
@@ -179,7 +179,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 if (j >= n_kt[w]) continue;
                 if (!(ok = wait(p_bar(w), j & 1))) break;
                 tc_fence_after();
-                if (lane == 0) {
+                if (elect_one()) {
                     const uint64_t dv = attn_desc_mn(ring + vs * C::KV_BYTES, BK);
 #pragma unroll
                     for (int k = 0; k < BK / 16; ++k)
@@ -188,7 +188,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                     if (j + 1 < n_kt[w]) scores(w, j + 1); else umma_commit(o_bar(w));
                 }
             }
-            if (ok && lane == 0) {
+            if (ok && elect_one()) {
                 release(2 * j + 1);
                 if (j + 1 < n_all) release(2 * j + 2);
             }
@@ -203,6 +203,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
         const float c = RAW ? a.scale * kLog2e : 1.f;
         const float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
         const float inv_cap = CAP ? a.scale / a.cap : 0.f, cap2 = CAP ? a.cap * kLog2e : 0.f;
+        const AttnTanh near(inv_cap, cap2);
         float m = -INFINITY, l = 0.f;
         bool ok = true;
         for (int j = 0; j < n_kt[w]; ++j) {
@@ -216,7 +217,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 const float big = attn_max<BK>([&](int k) { return fabsf(s[k]); });
                 if (__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) {
 #pragma unroll
-                    for (int k = 0; k < BK; ++k) s[k] = cap2 * attn_tanh_near(s[k] * inv_cap);
+                    for (int k = 0; k < BK; ++k) s[k] = near(s[k]);
                 } else {
 #pragma unroll
                     for (int k = 0; k < BK; ++k) s[k] = cap2 * attn_tanh(s[k] * inv_cap);
@@ -227,8 +228,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
 #pragma unroll
                 for (int k = 0; k < BK; ++k) s[k] = fmaf(-slope, fabsf(away - (float)k), CAP ? s[k] : s[k] * (a.scale * kLog2e));
             }
-            const bool masked = (j + 1) * BK > seen_by_all;
-            if (masked) {
+            if ((j + 1) * BK > seen_by_all) {
                 const int left = seen - j * BK;
 #pragma unroll
                 for (int k = 0; k < BK; ++k) s[k] = k < left ? s[k] : -INFINITY;
@@ -254,24 +254,18 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 }
             }
             const float from = m == -INFINITY ? 0.f : m;
-            // A quarter of the exponentials on the multiply-add units, where nothing is masked.  (A NaN is lost in a weight's
-            // rounding, but not in the sum by which the output is divided.)
             float sums[4] = {0.f, 0.f, 0.f, 0.f};
-            auto weights = [&](auto some) {
 #pragma unroll
-                for (int k = 0; k < BK; k += 32) {
-                    uint32_t r[16];
+            for (int k = 0; k < BK; k += 32) {
+                uint32_t r[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float x0 = fmaf(s[k + 2 * i], c, -from), x1 = fmaf(s[k + 2 * i + 1], c, -from);
-                        const float p0 = fast_exp2(x0), p1 = decltype(some)::value && i % 2 == 1 ? poly_exp2(x1) : fast_exp2(x1);
-                        sums[i % 4] += p0 + p1;
-                        r[i] = pack2<T>(p0, p1);
-                    }
-                    tmem_st16_nowait(s_cols(w) + lanes + k / 2, r);
+                for (int i = 0; i < 16; ++i) {
+                    const float p0 = fast_exp2(fmaf(s[k + 2 * i], c, -from)), p1 = fast_exp2(fmaf(s[k + 2 * i + 1], c, -from));
+                    sums[i % 4] += p0 + p1;
+                    r[i] = pack2<T>(p0, p1);
                 }
-            };
-            weights(std::false_type());
+                tmem_st16_nowait(s_cols(w) + lanes + k / 2, r);
+            }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             tmem_wait_st();
             tc_fence_before();
