@@ -171,10 +171,11 @@ __device__ __forceinline__ void tmem_st16_nowait(uint32_t taddr, const uint32_t*
 }
 // Rows [from, rows) of a tile of COLS 64-column blocks become zeros: rows of another text, whose values must not meet
 // weights of 0 in a product.
+// Shared out among `warps` warps, of which this is `warp`.
 template <int COLS>
-__device__ __forceinline__ void attn_zero_rows(uint32_t tile, int from, int rows) {
+__device__ __forceinline__ void attn_zero_rows(uint32_t tile, int from, int rows, int warp, int warps) {
     const int n = (rows - from) * 8;   // 16-byte chunks of a block
-    for (int i = threadIdx.x & 31; i < n * COLS; i += 32) {
+    for (int i = 32 * warp + (threadIdx.x & 31); i < n * COLS; i += 32 * warps) {
         const int block = i / n, at = i - block * n;
         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + (uint32_t)(block * rows + from) * 128u + 16u * at), "r"(0) : "memory");
     }

@@ -28,11 +28,13 @@ namespace {
 constexpr int THREADS = 320;
 constexpr int BT = 128;  // rows of a streamed tile
 
-template <int D> struct BwdTile {
-    static constexpr int STAGES = D == 64 ? 4 : 2;
-    static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2, STAGE = 2 * TILE;
-    static constexpr int STATS = BT * 8;      // lse and delta of a streamed tile's queries
-    static constexpr int SMEM = 2 * KEPT + STAGES * (STAGE + STATS) + 2 * kAttnRows * 4 + 256 + 1024;
+template <int D, bool KEYS> struct BwdTile {
+    // Places for tiles of the first streamed operand, which is needed until the last product of its tile, and of the second:
+    // what 227 KB hold.  (Waiting for the copies of 64 KB per tile was a third of d-queries' time with two places for each.)
+    static constexpr int FIRST = D == 64 ? 4 : KEYS ? 2 : 3, SECOND = D == 64 ? 4 : 2;
+    static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2;
+    static constexpr int STATS = KEYS ? BT * 8 : 0;      // lse and delta of a streamed tile's queries
+    static constexpr int SMEM = 2 * KEPT + (FIRST + SECOND) * TILE + FIRST * STATS + (KEYS ? 0 : 2 * kAttnRows * 4) + 256 + 1024;
 };
 
 struct alignas(64) BwdParams {
@@ -49,8 +51,8 @@ struct alignas(64) BwdParams {
 template <typename T, int D, bool CAP, bool BIAS, bool KEYS>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_bwd_kernel(const __grid_constant__ BwdParams P) {
-    using C = BwdTile<D>;
-    constexpr int STAGES = C::STAGES;
+    using C = BwdTile<D, KEYS>;
+    constexpr int N1 = C::FIRST, N2 = C::SECOND;
     constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr uint32_t IDESC_S = idesc16(BF16, false, false, kAttnRows, BT), IDESC_G = idesc16(BF16, false, true, kAttnRows, D);
     constexpr uint32_t COLS = 512;
@@ -83,11 +85,13 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
-    const uint32_t ring = base + 2 * C::KEPT, stats = ring + STAGES * C::STAGE, halves = stats + STAGES * C::STATS;
-    const uint32_t bars = halves + 2 * kAttnRows * 4;
-    auto full_bar = [&](int s) { return bars + 8u * s; };
-    auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
-    const uint32_t s_bar = bars + 8u * (2 * STAGES), dp_bar = s_bar + 8u;   // S, dP are there
+    const uint32_t ring1 = base + 2 * C::KEPT, ring2 = ring1 + N1 * C::TILE, stats = ring2 + N2 * C::TILE, halves = stats + N1 * C::STATS;
+    const uint32_t bars = halves + (KEYS ? 0 : 2 * kAttnRows * 4);
+    auto full1 = [&](int s) { return bars + 8u * s; };
+    auto empty1 = [&](int s) { return bars + 8u * (N1 + s); };
+    auto full2 = [&](int s) { return bars + 8u * (2 * N1 + s); };
+    auto empty2 = [&](int s) { return bars + 8u * (2 * N1 + N2 + s); };
+    const uint32_t s_bar = bars + 8u * (2 * N1 + 2 * N2), dp_bar = s_bar + 8u;   // S, dP are there
     const uint32_t p_bar = dp_bar + 8u, x_bar = p_bar + 8u;                 // S may be overwritten and (d-keys) P is there; dX is there
     const uint32_t kept_bar = x_bar + 8u, done_bar = kept_bar + 8u;
     const uint32_t tmem_slot = done_bar + 8u;
@@ -96,9 +100,13 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) {
-            mbar_init(full_bar(s), KEYS ? 33 : 1);   // the copies, and (d-keys) each lane's share of the statistics
-            mbar_init(empty_bar(s), 1);
+        for (int s = 0; s < N1; ++s) {
+            mbar_init(full1(s), KEYS ? 33 : 1);   // the copy, and (d-keys) each lane's share of the statistics
+            mbar_init(empty1(s), 1);
+        }
+        for (int s = 0; s < N2; ++s) {
+            mbar_init(full2(s), 1);
+            mbar_init(empty2(s), 1);
         }
         mbar_init(s_bar, 1);
         mbar_init(dp_bar, 1);
@@ -131,7 +139,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
 
     if (warp == 0) {
         int i = 0;
-        bool ok = true;
+        bool ok = true, one_ahead = false;   // (one_ahead: a tile's first copy is on its way, its second is not)
         if (n > 0 && lane == 0) {
             mbar_expect_tx(kept_bar, 2 * C::KEPT);
             for (int o = 0; o < 2; ++o)
@@ -139,38 +147,43 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                     tma_load_3d(base + o * C::KEPT + c * kAttnRows * 128, &P.kept[o], kept_bar, 64 * c, head0, kept_base + first);
         }
         for (; i < n; ++i) {
-            const int s = i % STAGES;
-            if (i >= STAGES && !wait(empty_bar(s), (i / STAGES - 1) & 1)) { ok = false; break; }
+            const int s1 = i % N1, s2 = i % N2;
             const int h = KEYS ? head0 * a.group + i / per_head : head0 / a.group;
             const int row = streamed_base + (tile0 + (KEYS ? i % per_head : i)) * BT;
-            if (lane == 0) {
-                mbar_expect_tx(full_bar(s), C::STAGE);
-                for (int o = 0; o < 2; ++o)
-                    for (int c = 0; c < D / 64; ++c)
-                        tma_load_3d(ring + s * C::STAGE + o * C::TILE + c * BT * 128, &P.streamed[o], full_bar(s), 64 * c, h, row);
-            }
+            auto load = [&](int o, uint32_t to, uint32_t bar) {
+                mbar_expect_tx(bar, C::TILE);
+                for (int c = 0; c < D / 64; ++c) tma_load_3d(to + c * BT * 128, &P.streamed[o], bar, 64 * c, h, row);
+            };
+            if (i >= N1 && !wait(empty1(s1), (i / N1 - 1) & 1)) { ok = false; break; }
+            if (lane == 0) load(0, ring1 + s1 * C::TILE, full1(s1));
             if (KEYS) {
                 for (int r = lane; r < BT; r += 32) {
                     const int64_t at = (int64_t)h * a.n_q + min(row + r, a.n_q - 1);
-                    const uint32_t to = stats + s * C::STATS + 4 * r;
+                    const uint32_t to = stats + s1 * C::STATS + 4 * r;
                     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(P.lse2 + at) : "memory");
                     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + 4 * BT), "l"(P.delta + at) : "memory");
                 }
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full_bar(s)) : "memory");
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full1(s1)) : "memory");
             }
+            one_ahead = true;
+            if (i >= N2 && !wait(empty2(s2), (i / N2 - 1) & 1)) { ok = false; break; }
+            if (lane == 0) load(1, ring2 + s2 * C::TILE, full2(s2));
+            one_ahead = false;
         }
         if (!ok || *abort_flag) {
             // let the copies already issued land before the CTA's shared memory goes away
             asm volatile("cp.async.wait_all;" ::: "memory");
             if (n > 0) mbar_wait(kept_bar, 0);
-            for (int k = max(0, i - STAGES); k < i; ++k) mbar_wait(full_bar(k % STAGES), (k / STAGES) & 1);
+            const int i1 = i + (one_ahead ? 1 : 0);
+            for (int k = max(0, i1 - N1); k < i1; ++k) mbar_wait(full1(k % N1), (k / N1) & 1);
+            for (int k = max(0, i - N2); k < i; ++k) mbar_wait(full2(k % N2), (k / N2) & 1);
         }
         __syncwarp();
     } else if (warp == 1) {
         bool ok = n > 0 && wait(kept_bar, 0);
         // S (o = 0) or dP (o = 1) of a tile: kept[o] streamed[o]^T
         auto scores = [&](int o, int s) {
-            const uint64_t da = make_desc(base + o * C::KEPT), db = make_desc(ring + s * C::STAGE + o * C::TILE);
+            const uint64_t da = make_desc(base + o * C::KEPT), db = make_desc((o ? ring2 : ring1) + s * C::TILE);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 const uint64_t at = (uint64_t)((k / 4 * kAttnRows * 128 + k % 4 * 32) >> 4);
@@ -181,47 +194,54 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         // dK or dQ (o = 0) from dX, dV (o = 1) from P.  Either warp of 32 rows has left its 64 columns, in 16 bits, in
         // the first half of its 64 columns of fp32.
         auto gradient = [&](int o, int s, bool add) {
-            const uint64_t db = attn_desc_mn(ring + s * C::STAGE + o * C::TILE, BT);
+            const uint64_t db = attn_desc_mn((o ? ring2 : ring1) + s * C::TILE, BT);
 #pragma unroll
             for (int k = 0; k < BT / 16; ++k)
                 umma16_ta(g_cols(o), (o ? s_cols : dp_cols) + (uint32_t)(k / 4 * 64 + k % 4 * 8), db + (uint64_t)(k * 2048 >> 4), IDESC_G, add || k > 0);
         };
-        auto arrived = [&](int tile_of_head, int s, int parity) {
-            if (!wait(full_bar(s), parity)) return false;
+        // The first tile; for the others the warps that allow its products have seen to it that it is there.
+        if (ok && (ok = wait(full1(0), 0) && wait(full2(0), 0))) {
             tc_fence_after();
-            const int from = streamed_rows - tile_of_head * BT;
-            if (from < BT) {
-                attn_zero_rows<D / 64>(ring + s * C::STAGE, from, BT);
-                attn_zero_rows<D / 64>(ring + s * C::STAGE + C::TILE, from, BT);
+            if (streamed_rows - tile0 * BT < BT) {
+                attn_zero_rows<D / 64>(ring1, streamed_rows - tile0 * BT, BT, 0, 1);
+                attn_zero_rows<D / 64>(ring2, streamed_rows - tile0 * BT, BT, 0, 1);
             }
-            return true;
-        };
-        if (ok && (ok = arrived(tile0, 0, 0)) && elect_one()) {
-            scores(0, 0);
-            scores(1, 0);
+            if (elect_one()) {
+                scores(0, 0);
+                scores(1, 0);
+                if (!KEYS && N2 < n) umma_commit(empty2(0));
+            }
         }
-        int s = 0, next = 1 % STAGES, parity = STAGES == 1 ? 1 : 0, next_tile = 1;
+        int s1 = 0, s2 = 0, next1 = 1 % N1, next2 = 1 % N2;
         for (int i = 0; ok && i < n; ++i) {
-            if (next_tile == per_head) next_tile = 0;   // (d-keys: the next head's first tile)
             if (!(ok = wait(p_bar, i & 1))) break;
             tc_fence_after();
-            if (KEYS && elect_one()) gradient(1, s, i > 0);
-            // (products are executed in order: the next scores do not overtake the weights they replace)
-            if (i + 1 < n) {
-                if (!(ok = arrived(tile0 + next_tile, next, parity))) break;
-                if (elect_one()) scores(0, next);
+            if (elect_one()) {
+                if (KEYS) {
+                    gradient(1, s2, i > 0);
+                    if (i + N2 < n) umma_commit(empty2(s2));
+                }
+                // (products are executed in order: the next scores do not overtake the weights they replace)
+                if (i + 1 < n) scores(0, next1);
             }
+            __syncwarp();
             if (!(ok = wait(x_bar, i & 1))) break;
             tc_fence_after();
             if (elect_one()) {
-                gradient(0, s, i > 0);
-                if (i + STAGES < n) umma_commit(empty_bar(s));
-                if (i + 1 < n) scores(1, next); else umma_commit(done_bar);
+                gradient(0, s1, i > 0);
+                if (i + N1 < n) umma_commit(empty1(s1));
+                if (i + 1 < n) {
+                    scores(1, next2);
+                    if (!KEYS && i + 1 + N2 < n) umma_commit(empty2(next2));
+                } else {
+                    umma_commit(done_bar);
+                }
             }
             __syncwarp();
-            s = next;
-            ++next_tile;
-            if (++next == STAGES) { next = 0; parity ^= 1; }
+            s1 = next1;
+            s2 = next2;
+            if (++next1 == N1) next1 = 0;
+            if (++next2 == N2) next2 = 0;
         }
     } else {
         const int w = (warp - 2) >> 2, quarter = warp & 3;
@@ -267,13 +287,22 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         const int edge_of_all = KEYS ? attn_first_query(a, x, row0 + 31) : attn_seen(a, x, row0);
 
         constexpr int MY = BT / 2;   // columns of a warp
-        int s = 0, parity = 0, tile_of_head = 0, head = KEYS ? head0 * a.group : head0;
+        int s1 = 0, next1 = 1 % N1, parity1 = N1 == 1, next2 = 1 % N2, parity2 = N2 == 1, tile_of_head = 0, head = KEYS ? head0 * a.group : head0;
         float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
-        for (int i = 0; i < n; ++i) {
+        // The products of the next tile are allowed once it is there, and holds zeros beyond its text.  (The waits are here
+        // because each one of the issuing thread's leaves the tensor cores idle.)
+        auto ready = [&](int o, int i) {
+            if (i + 1 >= n) return true;
+            if (!wait(o ? full2(next2) : full1(next1), o ? parity2 : parity1)) return false;
+            const int next_tile = tile_of_head + 1 == per_head ? 0 : tile_of_head + 1, from = streamed_rows - (tile0 + next_tile) * BT;
+            if (from < BT) attn_zero_rows<D / 64>(o ? ring2 + next2 * C::TILE : ring1 + next1 * C::TILE, from, BT, warp - 2, 8);
+            return true;
+        };
+        if (KEYS && n > 0) ok = wait(full1(0), 0);
+        for (int i = 0; ok && i < n; ++i) {
             const int at = (tile0 + tile_of_head) * BT + w * MY;   // this warp's first streamed row, in the text
-            const float* lses = reinterpret_cast<const float*>(smem_raw + (stats - raw) + s * C::STATS) + w * MY;
+            const float* lses = reinterpret_cast<const float*>(smem_raw + (stats - raw) + s1 * C::STATS) + w * MY;
             const float* deltas = lses + BT;
-            if (KEYS && !(ok = wait(full_bar(s), parity))) break;
             if (!(ok = wait(s_bar, i & 1))) break;
             tc_fence_after();
             const bool masked = KEYS ? at < edge_of_all || at + MY > x.lq : at + MY > edge_of_all;
@@ -285,6 +314,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             tmem_wait_ld();
             if (!KEYS) {
                 tc_fence_before();
+                if (!(ok = ready(0, i))) break;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_bar);
             }
@@ -335,6 +365,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             if (KEYS) {
                 tmem_wait_st();
                 tc_fence_before();
+                if (!(ok = ready(0, i))) break;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_bar);
             }
@@ -367,9 +398,12 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             if (masked) slopes_of_scores(std::true_type()); else slopes_of_scores(std::false_type());
             tmem_wait_st();
             tc_fence_before();
+            if (!(ok = ready(1, i))) break;
             __syncwarp();
             if (lane == 0) mbar_arrive(x_bar);
-            if (++s == STAGES) { s = 0; parity ^= 1; }
+            s1 = next1;
+            if (++next1 == N1) { next1 = 0; parity1 ^= 1; }
+            if (++next2 == N2) { next2 = 0; parity2 ^= 1; }
             if (++tile_of_head == per_head && KEYS && i + 1 < n) {
                 tile_of_head = 0;
                 ++head;
@@ -408,13 +442,13 @@ cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {
     auto* kernel = attn_bwd_kernel<T, D, CAP, BIAS, KEYS>;
     const uint32_t bit = 1u << ((KEYS ? 16 : 0) + (std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
     if (!(ctx->attn_bwd_ready & bit)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BwdTile<D>::SMEM);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (BwdTile<D, KEYS>::SMEM));
         if (e != cudaSuccess) return e;
         ctx->attn_bwd_ready |= bit;
     }
     KernelScope scope(ctx, SAMA_K_ATTN, KEYS ? 2 : 1, st);
     const int64_t blocks = (int64_t)P.slots * (KEYS ? P.a.kv_heads : P.a.heads);
-    return launch_dependent(kernel, dim3((unsigned)blocks), dim3(THREADS), BwdTile<D>::SMEM, st, P);
+    return launch_dependent(kernel, dim3((unsigned)blocks), dim3(THREADS), (BwdTile<D, KEYS>::SMEM), st, P);
 }
 template <typename T, int D, bool KEYS>
 cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {

@@ -173,7 +173,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             const int vs = (2 * j + 1) % STAGES;
             wait_item(2 * j + 1);
             if (!ok) break;
-            if ((j + 1) * BK > x.lk) attn_zero_rows<D / 64>(ring + vs * C::KV_BYTES, x.lk - j * BK, BK);
+            if ((j + 1) * BK > x.lk) attn_zero_rows<D / 64>(ring + vs * C::KV_BYTES, x.lk - j * BK, BK, 0, 1);
             if (j + 1 < n_all) wait_item(2 * j + 2);
             for (int w = 0; w < 2 && ok; ++w) {
                 if (j >= n_kt[w]) continue;
