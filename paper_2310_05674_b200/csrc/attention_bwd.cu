@@ -15,8 +15,8 @@
 // 64 wide takes 48 cycles in place of 32, and each wait of the issuing thread leaves the tensor cores idle for some 200
 // cycles, since it can run ahead of them by a product or two only.)
 //
-// Roles of the 10 warps: warp 0 copies, warp 1 issues products, warps 2..9 form P and dX: two warps share 32 rows, each of
-// them has 64 of a tile's columns.  Every wait is bounded.
+// Roles of the 18 warps: warp 0 copies, warp 1 issues products, warps 2..17 form P and dX: four warps share 32 rows, each of
+// them has 32 of a tile's columns.  Every wait is bounded.
 #include <type_traits>
 
 #include "attention.h"
@@ -25,8 +25,9 @@ namespace sama {
 
 namespace {
 
-constexpr int THREADS = 320;
-constexpr int BT = 128;  // rows of a streamed tile
+constexpr int FORMING = 16, THREADS = 64 + 32 * FORMING;   // warps that form P and dX
+constexpr int BT = 128;              // rows of a streamed tile
+constexpr int MY = BT / (FORMING / 4);   // of them, a warp's columns of P and dX
 
 template <int D, bool KEYS> struct BwdTile {
     // Places for tiles of the first streamed operand, which is needed until the last product of its tile, and of the second:
@@ -110,8 +111,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         }
         mbar_init(s_bar, 1);
         mbar_init(dp_bar, 1);
-        mbar_init(p_bar, 8);
-        mbar_init(x_bar, 8);
+        mbar_init(p_bar, FORMING);
+        mbar_init(x_bar, FORMING);
         mbar_init(kept_bar, 1);
         mbar_init(done_bar, 1);
         *abort_flag = 0;
@@ -191,13 +192,13 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             }
             umma_commit(o ? dp_bar : s_bar);
         };
-        // dK or dQ (o = 0) from dX, dV (o = 1) from P.  Either warp of 32 rows has left its 64 columns, in 16 bits, in
-        // the first half of its 64 columns of fp32.
+        // dK or dQ (o = 0) from dX, dV (o = 1) from P.  Each warp has left its columns, in 16 bits, in the first half of
+        // its columns of fp32.
         auto gradient = [&](int o, int s, bool add) {
             const uint64_t db = attn_desc_mn((o ? ring2 : ring1) + s * C::TILE, BT);
 #pragma unroll
             for (int k = 0; k < BT / 16; ++k)
-                umma16_ta(g_cols(o), (o ? s_cols : dp_cols) + (uint32_t)(k / 4 * 64 + k % 4 * 8), db + (uint64_t)(k * 2048 >> 4), IDESC_G, add || k > 0);
+                umma16_ta(g_cols(o), (o ? s_cols : dp_cols) + (uint32_t)(k / (MY / 16) * MY + k % (MY / 16) * 8), db + (uint64_t)(k * 2048 >> 4), IDESC_G, add || k > 0);
         };
         // The first tile; for the others the warps that allow its products have seen to it that it is there.
         if (ok && (ok = wait(full1(0), 0) && wait(full2(0), 0))) {
@@ -254,10 +255,10 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
 
         float lse2 = 0.f, delta = 0.f;
         if (!KEYS) {
-            // the two warps that share these rows add up half of the columns each
+            // two of the warps that share these rows add up half of the columns each
             volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (halves - raw));
             float sum = 0.f;
-            if (real) {
+            if (real && w < 2) {
                 const int64_t at = ((int64_t)(x.q0 + row) * a.heads + head0) * a.dim;
                 const T *o = static_cast<const T*>(P.out) + at, *d = static_cast<const T*>(P.dout) + at;
 #pragma unroll
@@ -271,11 +272,13 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                         for (int e = 0; e < 8; ++e) sum = fmaf(u[e], v[e], sum);
                     }
                 }
+            }
+            if (real) {
                 lse2 = P.lse[(int64_t)head0 * a.n_q + x.q0 + row] * kLog2e;
                 if (lse2 == -INFINITY) lse2 = INFINITY;
             }
-            part[w * kAttnRows + quarter * 32 + lane] = sum;
-            asm volatile("bar.sync 1, 256;" ::: "memory");
+            if (w < 2) part[w * kAttnRows + quarter * 32 + lane] = sum;
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
             delta = part[quarter * 32 + lane] + part[kAttnRows + quarter * 32 + lane];
             if (w == 0 && real) {
                 P.lse2[(int64_t)head0 * a.n_q + x.q0 + row] = lse2;
@@ -286,7 +289,6 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         const int edge = KEYS ? attn_first_query(a, x, row) : attn_seen(a, x, row);
         const int edge_of_all = KEYS ? attn_first_query(a, x, row0 + 31) : attn_seen(a, x, row0);
 
-        constexpr int MY = BT / 2;   // columns of a warp
         int s1 = 0, next1 = 1 % N1, parity1 = N1 == 1, next2 = 1 % N2, parity2 = N2 == 1, tile_of_head = 0, head = KEYS ? head0 * a.group : head0;
         float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
         // The products of the next tile are allowed once it is there, and holds zeros beyond its text.  (The waits are here
@@ -295,7 +297,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             if (i + 1 >= n) return true;
             if (!wait(o ? full2(next2) : full1(next1), o ? parity2 : parity1)) return false;
             const int next_tile = tile_of_head + 1 == per_head ? 0 : tile_of_head + 1, from = streamed_rows - (tile0 + next_tile) * BT;
-            if (from < BT) attn_zero_rows<D / 64>(o ? ring2 + next2 * C::TILE : ring1 + next1 * C::TILE, from, BT, warp - 2, 8);
+            if (from < BT) attn_zero_rows<D / 64>(o ? ring2 + next2 * C::TILE : ring1 + next1 * C::TILE, from, BT, warp - 2, FORMING);
             return true;
         };
         if (KEYS && n > 0) ok = wait(full1(0), 0);
@@ -309,8 +311,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             const int lo = KEYS ? edge - at : 0, hi = KEYS ? x.lq - at : edge - at;   // visible columns
             const float away = BIAS ? (float)(KEYS ? row - (x.lk - x.lq) - at : row + x.lk - x.lq - at) : 0.f;
             float p[MY];   // the weights, in the end times 1 - tanh^2
-            tmem_ld32_nowait(s_cols + lanes + w * MY, p);
-            tmem_ld32_nowait(s_cols + lanes + w * MY + 32, p + 32);
+#pragma unroll
+            for (int k = 0; k < MY; k += 32) tmem_ld32_nowait(s_cols + lanes + w * MY + k, p + k);
             tmem_wait_ld();
             if (!KEYS) {
                 tc_fence_before();
@@ -413,12 +415,13 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         if (ok && n > 0) ok = wait(done_bar, 0);
         if (ok) {
             tc_fence_after();
-            // d-queries: half of the columns for each four warps; d-keys: dK and dV
-            const int which = KEYS ? w : 0, k0 = KEYS ? 0 : w * (D / 2), k1 = KEYS ? D : k0 + D / 2;
+            // 32 columns at a time: d-keys' warps have dK or dV
+            constexpr int SHARES = FORMING / 4;
+            const int which = KEYS ? w % 2 : 0, k0 = 32 * (KEYS ? w / 2 : w);
             const float f = which == 0 ? a.scale : 1.f;
             T* g = static_cast<T*>(P.grad[which]) + (int64_t)(kept_base + row) * P.ld[which] + (int64_t)head0 * a.dim;
 #pragma unroll 1
-            for (int k = k0; k < k1; k += 32) {
+            for (int k = k0; k < D; k += 32 * (KEYS ? SHARES / 2 : SHARES)) {
                 float v[32];
                 if (n > 0) {
                     tmem_ld32_nowait(g_cols(which) + lanes + k, v);
