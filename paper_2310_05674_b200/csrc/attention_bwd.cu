@@ -25,14 +25,16 @@ namespace sama {
 
 namespace {
 
-constexpr int FORMING = 16, THREADS = 64 + 32 * FORMING;   // warps that form P and dX
-constexpr int BT = 128;              // rows of a streamed tile
-constexpr int MY = BT / (FORMING / 4);   // of them, a warp's columns of P and dX
-
-template <int D, bool KEYS> struct BwdTile {
+// BT rows of a streamed tile: 128, or for heads of up to 64 columns 64, which leaves room for a second CTA.
+template <int D, int BT, bool KEYS> struct BwdTile {
+    static constexpr int CTAS = BT == 64 ? 2 : 1;                 // per SM
+    static constexpr int FORMING = BT == 64 ? 8 : 16;             // warps that form P and dX
+    static constexpr int THREADS = 64 + 32 * FORMING;
+    static constexpr int COLS = BT == 64 ? 256 : 512;             // of tensor memory
     // Places for tiles of the first streamed operand, which is needed until the last product of its tile, and of the second:
     // what 227 KB hold.  (Waiting for the copies of 64 KB per tile was a third of d-queries' time with two places for each.)
     static constexpr int FIRST = D == 64 ? 4 : KEYS ? 2 : 3, SECOND = D == 64 ? 4 : 2;
+    static_assert(BT == 128 || D == 64, "two CTAs' accumulators");
     static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2;
     static constexpr int STATS = KEYS ? BT * 8 : 0;      // lse and delta of a streamed tile's queries
     static constexpr int SMEM = 2 * KEPT + (FIRST + SECOND) * TILE + FIRST * STATS + (KEYS ? 0 : 2 * kAttnRows * 4) + 256 + 1024;
@@ -49,14 +51,15 @@ struct alignas(64) BwdParams {
     int slots;
 };
 
-template <typename T, int D, bool CAP, bool BIAS, bool KEYS>
-__global__ void __launch_bounds__(THREADS, 1)
+template <typename T, int D, int BT, bool CAP, bool BIAS, bool KEYS>
+__global__ void __launch_bounds__(BwdTile<D, BT, KEYS>::THREADS, BwdTile<D, BT, KEYS>::CTAS)
 attn_bwd_kernel(const __grid_constant__ BwdParams P) {
-    using C = BwdTile<D, KEYS>;
+    using C = BwdTile<D, BT, KEYS>;
+    constexpr int FORMING = C::FORMING, MY = BT / (FORMING / 4);   // streamed rows, which are columns of P and dX, of a warp
     constexpr int N1 = C::FIRST, N2 = C::SECOND;
     constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr uint32_t IDESC_S = idesc16(BF16, false, false, kAttnRows, BT), IDESC_G = idesc16(BF16, false, true, kAttnRows, D);
-    constexpr uint32_t COLS = 512;
+    constexpr uint32_t COLS = C::COLS;
     const AttnShape& a = P.a;
 
     pdl_trigger();
@@ -440,29 +443,33 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     if (warp == 1) tmem_dealloc(tmem, COLS);
 }
 
-template <typename T, int D, bool CAP, bool BIAS, bool KEYS>
+template <typename T, int D, int BT, bool CAP, bool BIAS, bool KEYS>
 cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {
-    auto* kernel = attn_bwd_kernel<T, D, CAP, BIAS, KEYS>;
-    const uint32_t bit = 1u << ((KEYS ? 16 : 0) + (std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
+    using C = BwdTile<D, BT, KEYS>;
+    auto* kernel = attn_bwd_kernel<T, D, BT, CAP, BIAS, KEYS>;
+    const uint64_t bit = 1ull << ((BT == 64 ? 32 : 0) + (KEYS ? 16 : 0) + (std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
     if (!(ctx->attn_bwd_ready & bit)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (BwdTile<D, KEYS>::SMEM));
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         if (e != cudaSuccess) return e;
         ctx->attn_bwd_ready |= bit;
     }
     KernelScope scope(ctx, SAMA_K_ATTN, KEYS ? 2 : 1, st);
     const int64_t blocks = (int64_t)P.slots * (KEYS ? P.a.kv_heads : P.a.heads);
-    return launch_dependent(kernel, dim3((unsigned)blocks), dim3(THREADS), (BwdTile<D, KEYS>::SMEM), st, P);
+    return launch_dependent(kernel, dim3((unsigned)blocks), dim3(C::THREADS), C::SMEM, st, P);
 }
-template <typename T, int D, bool KEYS>
+template <typename T, int D, int BT, bool KEYS>
 cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {
-    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, true, true, KEYS>(ctx, P, st) : launch<T, D, true, false, KEYS>(ctx, P, st);
-    return P.a.slopes ? launch<T, D, false, true, KEYS>(ctx, P, st) : launch<T, D, false, false, KEYS>(ctx, P, st);
+    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, BT, true, true, KEYS>(ctx, P, st) : launch<T, D, BT, true, false, KEYS>(ctx, P, st);
+    return P.a.slopes ? launch<T, D, BT, false, true, KEYS>(ctx, P, st) : launch<T, D, BT, false, false, KEYS>(ctx, P, st);
+}
+template <typename T, bool KEYS>
+cudaError_t launch(sama_ctx* ctx, int bt, const BwdParams& P, cudaStream_t st) {
+    if (P.a.dim > 64) return launch<T, 128, 128, KEYS>(ctx, P, st);
+    return bt == 64 ? launch<T, 64, 64, KEYS>(ctx, P, st) : launch<T, 64, 128, KEYS>(ctx, P, st);
 }
 template <bool KEYS>
-cudaError_t launch(sama_ctx* ctx, int dtype, const BwdParams& P, cudaStream_t st) {
-    if (dtype == SAMA_BF16)
-        return P.a.dim <= 64 ? launch<__nv_bfloat16, 64, KEYS>(ctx, P, st) : launch<__nv_bfloat16, 128, KEYS>(ctx, P, st);
-    return P.a.dim <= 64 ? launch<__half, 64, KEYS>(ctx, P, st) : launch<__half, 128, KEYS>(ctx, P, st);
+cudaError_t launch(sama_ctx* ctx, int dtype, int bt, const BwdParams& P, cudaStream_t st) {
+    return dtype == SAMA_BF16 ? launch<__nv_bfloat16, KEYS>(ctx, bt, P, st) : launch<__half, KEYS>(ctx, bt, P, st);
 }
 
 }  // namespace
@@ -479,6 +486,11 @@ cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnO
     P.lse2 = static_cast<float*>(ws);
     P.delta = P.lse2 + (size_t)a.heads * a.n_q;
     const int64_t dense = (int64_t)a.heads * a.dim;
+    // Small tiles, two CTAs per SM, unless capped scores, whose arithmetic bounds them, are many (us for d-queries and d-keys,
+    // 16 heads of 64: 16 texts of 512 39 and 42, with the large ones 45 and 52; 64 of 128 44 and 48, 60 and 68; one of 8192,
+    // causal, 277 and 344, 310 and 379; but 4 of 2048, causal, capped and biased, 100 and 117, 85 and 97).  Lengths are on the
+    // device, but their mean is known.
+    const int bt = a.dim <= 64 && (a.cap == 0.f || a.n_q <= 256 * (int64_t)a.n_texts) ? 64 : 128;
     auto query_maps = [&](CUtensorMap* m, int rows) {
         return attn_map(&m[0], op.q, op.dtype, a.dim, a.heads, a.n_q, op.q_stride, rows) &&
                attn_map(&m[1], dout, op.dtype, a.dim, a.heads, a.n_q, dense, rows);
@@ -489,22 +501,22 @@ cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnO
     };
     if (a.n_q > 0) {
         // (without keys nothing is loaded, but a map has to describe something)
-        if (!query_maps(P.kept, kAttnRows) || !(a.n_k > 0 ? key_maps(P.streamed, BT) : query_maps(P.streamed, BT)))
+        if (!query_maps(P.kept, kAttnRows) || !(a.n_k > 0 ? key_maps(P.streamed, bt) : query_maps(P.streamed, bt)))
             return cudaErrorInvalidValue;
         P.grad[0] = P.grad[1] = dq;
         P.ld[0] = P.ld[1] = op.q_stride;
         P.slots = a.n_q / kAttnRows + a.n_texts;
-        const cudaError_t e = launch<false>(ctx, op.dtype, P, st);
+        const cudaError_t e = launch<false>(ctx, op.dtype, bt, P, st);
         if (e != cudaSuccess) return e;
     }
     if (a.n_k == 0) return cudaSuccess;
-    if (!key_maps(P.kept, kAttnRows) || !(a.n_q > 0 ? query_maps(P.streamed, BT) : key_maps(P.streamed, BT))) return cudaErrorInvalidValue;
+    if (!key_maps(P.kept, kAttnRows) || !(a.n_q > 0 ? query_maps(P.streamed, bt) : key_maps(P.streamed, bt))) return cudaErrorInvalidValue;
     P.grad[0] = dk;
     P.grad[1] = dv;
     P.ld[0] = op.k_stride;
     P.ld[1] = op.v_stride;
     P.slots = a.n_k / kAttnRows + a.n_texts;
-    return launch<true>(ctx, op.dtype, P, st);
+    return launch<true>(ctx, op.dtype, bt, P, st);
 }
 
 }  // namespace sama
