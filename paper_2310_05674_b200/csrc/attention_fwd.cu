@@ -1,15 +1,17 @@
 // Attention over packed texts, forward: out = softmax(scores) V in one pass over the keys, with the running maximum and
 // sum of the softmax, on the 5th-generation tensor cores.
 //
-// A CTA has 256 queries of one text and head, two tiles of 128, and streams the keys and values that they see.  A score
-// tile S = Q K^T is produced in tensor memory; four warps per tile, a thread per query, turn it into weights
+// A CTA has 128 or 256 queries of one text and head, one or two tiles of 128, and streams the keys and values that they see.
+// A score tile S = Q K^T is produced in tensor memory; four warps per tile, a thread per query, turn it into weights
 // P = 2^(x log2 e - m), which go back to tensor memory in 16 bits over the scores they came from, and O += P V takes them
-// from there.  While one tile's weights are formed the other's products run.  The maximum m that the weights refer to is
-// only raised when a score exceeds it by more than 8 binary orders (O and the sum are scaled then): the weights stay below
-// 2^8, far from the end of either type, and are rounded relative to their size whatever they refer to.
+// from there.  While one tile's weights are formed the other's products run: two tiles in a CTA for heads of more than 64
+// columns, which share the keys and values (64 KB per 128 of them, more than L2 delivers twice in that time), and three
+// CTAs of one tile per SM for others, whose arithmetic bounds them.  The maximum m that the weights refer to is only raised
+// when a score exceeds it by more than 8 binary orders (O and the sum are scaled then): the weights stay below 2^8, far from
+// the end of either type, and are rounded relative to their size whatever they refer to.
 //
-// Roles of the 10 warps: warp 0 copies (TMA, 128-byte swizzle), warp 1 issues products, warps 2..5 and 6..9 the softmax of
-// the two tiles.  Every wait is bounded: one that expires raises SAMA_DEV_TIMEOUT and ends the CTA's work.
+// Roles of the warps: warp 0 copies (TMA, 128-byte swizzle), warp 1 issues products, the others the softmax.  Every wait is
+// bounded: one that expires raises SAMA_DEV_TIMEOUT and ends the CTA's work.
 #include <type_traits>
 
 #include "attention.h"
@@ -18,15 +20,17 @@ namespace sama {
 
 namespace {
 
-constexpr int THREADS = 320;
 constexpr float kRaise = 8.f;
 
 template <int D> struct FwdTile {
+    static constexpr int NW = D == 64 ? 1 : 2;           // tiles of queries, of four warps each
+    static constexpr int THREADS = 64 + 128 * NW;
+    static constexpr int CTAS = D == 64 ? 3 : 1;         // per SM
     static constexpr int BK = D == 64 ? 64 : 128;        // keys of a tile
-    static constexpr int STAGES = D == 64 ? 6 : 4;       // tiles of keys or values in shared memory
+    static constexpr int STAGES = 4;                     // tiles of keys or values in shared memory
     static constexpr int Q_BYTES = kAttnRows * D * 2, KV_BYTES = BK * D * 2;
-    static constexpr int SMEM = 2 * Q_BYTES + STAGES * KV_BYTES + 256 + 1024;
-    static constexpr int COLS = D == 64 ? 256 : 512;     // of tensor memory: two score tiles, two outputs
+    static constexpr int SMEM = NW * Q_BYTES + STAGES * KV_BYTES + 256 + 1024;
+    static constexpr int COLS = NW * (BK + D);           // of tensor memory: a score tile and an output for each tile of queries
 };
 
 struct alignas(64) FwdParams {
@@ -38,10 +42,10 @@ struct alignas(64) FwdParams {
 };
 
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(THREADS, D == 64 ? 2 : 1)
+__global__ void __launch_bounds__(FwdTile<D>::THREADS, FwdTile<D>::CTAS)
 attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     using C = FwdTile<D>;
-    constexpr int BK = C::BK, STAGES = C::STAGES;
+    constexpr int BK = C::BK, STAGES = C::STAGES, NW = C::NW;
     constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr uint32_t IDESC_S = idesc16(BF16, false, false, kAttnRows, BK), IDESC_O = idesc16(BF16, false, true, kAttnRows, D);
     const AttnShape& a = P.a;
@@ -52,16 +56,16 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     // the last tiles of a text, which see the most keys, come first
     const int slot = P.slots - 1 - (int)blockIdx.x / a.heads, head = (int)blockIdx.x % a.heads;
     int tile;
-    const int t = attn_find<2 * kAttnRows>(a.q_starts, a.n_texts, a.n_q, slot, &tile);
+    const int t = attn_find<NW * kAttnRows>(a.q_starts, a.n_texts, a.n_q, slot, &tile);
     if (t < 0) return;
     const AttnText x = attn_text(a, t);
-    const int first = tile * 2 * kAttnRows;
+    const int first = tile * NW * kAttnRows;
     if (first >= x.lq) return;
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
-    const uint32_t ring = base + 2 * C::Q_BYTES, bars = ring + STAGES * C::KV_BYTES;
+    const uint32_t ring = base + NW * C::Q_BYTES, bars = ring + STAGES * C::KV_BYTES;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
     auto q_bar = [&](int w) { return bars + 8u * (2 * STAGES + w); };
@@ -78,7 +82,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             mbar_init(full_bar(s), 1);
             mbar_init(empty_bar(s), 1);
         }
-        for (int w = 0; w < 2; ++w) {
+        for (int w = 0; w < NW; ++w) {
             mbar_init(q_bar(w), 1);
             mbar_init(s_bar(w), 1);
             mbar_init(p_bar(w), 4);
@@ -93,15 +97,16 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_ptr_slot, 0);
     auto s_cols = [&](int w) { return tmem + (uint32_t)(w * BK); };
-    auto o_cols = [&](int w) { return tmem + (uint32_t)(2 * BK + w * D); };
+    auto o_cols = [&](int w) { return tmem + (uint32_t)(NW * BK + w * D); };
 
     // key tiles that the last query of each of the two tiles sees
-    int n_kt[2];
-    for (int w = 0; w < 2; ++w) {
+    int n_kt[NW], n_all = 0;
+    for (int w = 0; w < NW; ++w) {
         const int i0 = first + w * kAttnRows;
         n_kt[w] = i0 < x.lq ? (attn_seen(a, x, min(i0 + kAttnRows, x.lq) - 1) + BK - 1) / BK : 0;
+        n_all = max(n_all, n_kt[w]);
     }
-    const int n_all = max(n_kt[0], n_kt[1]), items = 2 * n_all;   // keys and values in turn
+    const int items = 2 * n_all;   // keys and values in turn
     const int kv_head = head / a.group;
 
     auto raise_timeout = [&]() {
@@ -133,11 +138,11 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 mbar_expect_tx(full_bar(s), C::KV_BYTES);
                 for (int c = 0; c < D / 64; ++c)
                     tma_load_3d(ring + s * C::KV_BYTES + c * BK * 128, item & 1 ? &P.v : &P.k, full_bar(s), 64 * c, kv_head, x.k0 + (item >> 1) * BK);
-                if (item == 0) load_q(1);
+                if (item == 0 && NW > 1) load_q(1);
             }
             if (*abort_flag) {
                 // let the copies already issued land before the CTA's shared memory goes away
-                for (int w = 0; w < 2; ++w)
+                for (int w = 0; w < NW; ++w)
                     if (n_kt[w] > 0) mbar_wait(q_bar(w), 0);
                 for (int i = max(0, item - STAGES); i < item; ++i) mbar_wait(full_bar(i % STAGES), (i / STAGES) & 1);
             }
@@ -161,7 +166,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
         };
         if (n_all > 0) {
             wait_item(0);
-            for (int w = 0; w < 2 && ok; ++w) {
+            for (int w = 0; w < NW && ok; ++w) {
                 if (n_kt[w] == 0) continue;
                 if (!(ok = wait(q_bar(w), 0))) break;
                 tc_fence_after();
@@ -175,7 +180,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             if (!ok) break;
             if ((j + 1) * BK > x.lk) attn_zero_rows<D / 64>(ring + vs * C::KV_BYTES, x.lk - j * BK, BK, 0, 1);
             if (j + 1 < n_all) wait_item(2 * j + 2);
-            for (int w = 0; w < 2 && ok; ++w) {
+            for (int w = 0; w < NW && ok; ++w) {
                 if (j >= n_kt[w]) continue;
                 if (!(ok = wait(p_bar(w), j & 1))) break;
                 tc_fence_after();
@@ -312,7 +317,7 @@ cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
         ctx->attn_fwd_ready |= bit;
     }
     KernelScope scope(ctx, SAMA_K_ATTN, 0, st);
-    return launch_dependent(kernel, dim3((unsigned)((int64_t)P.slots * P.a.heads)), dim3(THREADS), FwdTile<D>::SMEM, st, P);
+    return launch_dependent(kernel, dim3((unsigned)((int64_t)P.slots * P.a.heads)), dim3(FwdTile<D>::THREADS), FwdTile<D>::SMEM, st, P);
 }
 template <typename T, int D>
 cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
@@ -324,7 +329,7 @@ cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
 
 cudaError_t launch_attention(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, void* out, float* lse, cudaStream_t st) {
     FwdParams P;
-    const int bk = a.dim <= 64 ? FwdTile<64>::BK : FwdTile<128>::BK;
+    const int bk = a.dim <= 64 ? FwdTile<64>::BK : FwdTile<128>::BK, rows = kAttnRows * (a.dim <= 64 ? FwdTile<64>::NW : FwdTile<128>::NW);
     // (without keys nothing is loaded, but a map has to describe something)
     const bool none = a.n_k == 0;
     if (!attn_map(&P.q, op.q, op.dtype, a.dim, a.heads, a.n_q, op.q_stride, kAttnRows) ||
@@ -334,7 +339,7 @@ cudaError_t launch_attention(sama_ctx* ctx, const AttnShape& a, const AttnOperan
     P.a = a;
     P.out = out;
     P.lse = lse;
-    P.slots = a.n_q / (2 * kAttnRows) + a.n_texts;
+    P.slots = a.n_q / rows + a.n_texts;
     if (op.dtype == SAMA_BF16)
         return a.dim <= 64 ? launch<__nv_bfloat16, 64>(ctx, P, st) : launch<__nv_bfloat16, 128>(ctx, P, st);
     return a.dim <= 64 ? launch<__half, 64>(ctx, P, st) : launch<__half, 128>(ctx, P, st);
