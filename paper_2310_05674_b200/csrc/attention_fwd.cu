@@ -246,15 +246,13 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 l *= factor;
                 if (j > 0) {
 #pragma unroll 1
-                    for (int k = 0; k < D; k += 32) {
-                        float o[32];
-                        tmem_ld32_nowait(o_cols(w) + lanes + k, o);
+                    for (int k = 0; k < D; k += 16) {   // (few at a time: the scores are in registers, too)
+                        uint32_t r[16];
+                        tmem_ld16_nowait(o_cols(w) + lanes + k, r);
                         tmem_wait_ld();
-                        uint32_t r[32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(o[i] * factor);
+                        for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * factor);
                         tmem_st16_nowait(o_cols(w) + lanes + k, r);
-                        tmem_st16_nowait(o_cols(w) + lanes + k + 16, r + 16);
                     }
                 }
             }
