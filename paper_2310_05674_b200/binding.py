@@ -191,7 +191,8 @@ class Paged:
                               _dense(self.device, slopes, SAMA_F32, heads, w),
                               head_dim ** -0.5 if scale is None else scale, cap)
         self._ref = C.byref(self.a)
-        self.page = page_size * kv_heads * head_dim
+        self.shape = (page_size, kv_heads, head_dim)
+        self.strides = (page_stride or page_size * kv_heads * head_dim, kv_heads * head_dim, head_dim, 1)
 
     def cache(self, x, where):
         """Address of a cache [n_pages][page_size][kv_heads][head_dim] whose pages may lie apart."""
@@ -204,10 +205,9 @@ class Paged:
             _fill_dtypes()
         if x.dtype is not _torch_dtypes.get(a.dtype):
             raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is not of the type the call names" % where)
-        if x.dim() != 4 or x.shape[0] < a.n_pages or tuple(x.shape[1:]) != (a.page_size, a.kv_heads, a.head_dim):
+        if x.dim() != 4 or x.shape[0] < a.n_pages or tuple(x.shape[1:]) != self.shape:
             raise SamaError(SAMA_ERR_SIZE, where)
-        stride = a.page_stride or self.page
-        if (x.shape[0] > 1 and x.stride(0) != stride) or not x[0].is_contiguous():
+        if any(s != want and n > 1 for n, s, want in zip(x.shape, x.stride(), self.strides)):
             raise SamaError(SAMA_ERR_PARAM, "%s: a tensor's strides are not the described ones" % where)
         return x.data_ptr()
 
