@@ -26,8 +26,7 @@ constexpr int STAGES = 3;
 constexpr int kMinSteps = 2;             // a CTA's share, at least: 128 keys
 
 template <int D> struct PagedTile {
-    static constexpr int TILE = KEYS * D * 2, RING = STAGES * 2 * TILE, LD = D + 2;   // LD: a row's sums, maximum and weight
-    static constexpr int SMEM = WARPS * RING + WARPS * ROWS * LD * 4;
+    static constexpr int TILE = KEYS * D * 2, RING = STAGES * 2 * TILE, LD = D + 4;   // LD: a row's sums, maximum and weight
 };
 
 struct PagedParams {
@@ -75,10 +74,11 @@ paged_kernel(const PagedParams P) {
     constexpr int LD = C::LD;
     const PagedShape& a = P.a;
     extern __shared__ __align__(128) uint8_t smem_raw[];
-    float* sums = reinterpret_cast<float*>(smem_raw + WARPS * C::RING);
+    float* sums = reinterpret_cast<float*>(smem_raw + WARPS * C::RING);   // [WARPS][ROWS][LD], or a factor for each part and row
     __shared__ int64_t scan[WARPS];
     __shared__ int64_t start_before;
     __shared__ int start_s, last_to_arrive;
+    __shared__ float row_weight[ROWS];
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t ring = smem_u32(smem_raw) + warp * C::RING;
@@ -349,26 +349,6 @@ paged_kernel(const PagedParams P) {
         const bool shared = !unit_ends || first_step > 0;
         float* part = P.parts + (int64_t)(2 * cta + (first_step > 0 ? 0 : 1)) * ROWS * LD;
         T* out = static_cast<T*>(P.out) + ((int64_t)at.s * a.heads + g * a.group + row0) * a.dim;
-        // joined sums of column pairs; `get(i, row)` is the i-th of the parts' rows
-        auto join = [&](int parts, auto&& get, auto&& put) {
-            for (int e = threadIdx.x; e < rows * (D / 2); e += THREADS) {
-                const int r = e / (D / 2), col = 2 * (e - r * (D / 2));
-                float top = -INFINITY;
-                for (int p = 0; p < parts; ++p) top = fmaxf(top, __ldcg(get(p, r) + D));
-                const float from = top == -INFINITY ? 0.f : top;
-                float x = 0.f, y = 0.f, w = 0.f;
-                for (int p = 0; p < parts; ++p) {
-                    const float* row = get(p, r);
-                    const float2 ml = __ldcg(reinterpret_cast<const float2*>(row + D)), v = __ldcg(reinterpret_cast<const float2*>(row + col));
-                    const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - from);
-                    // (sums of nothing are 0; a maximum that is not finite makes them NaN, as it should)
-                    x += v.x * f;
-                    y += v.y * f;
-                    w += ml.y * f;
-                }
-                put(r, col, x, y, w);
-            }
-        };
         auto finish = [&](int r, int col, float x, float y, float w) {
             const float inv = 1.f / w;
             if (col < a.dim)
@@ -415,8 +395,48 @@ paged_kernel(const PagedParams P) {
             __syncthreads();
             if (last_to_arrive) {
                 __threadfence();
-                join(h1 - h0 + 1, [&](int p, int r) -> const float* { return P.parts + ((int64_t)(2 * (h0 + p) + (p == 0 ? 1 : 0)) * ROWS + r) * LD; },
-                     finish);
+                // Each part's factor, by the threads of a row together; then four columns per thread, several parts in flight.
+                const int parts = h1 - h0 + 1;
+                auto row_of = [&](int p, int r) { return P.parts + ((int64_t)(2 * (h0 + p) + (p == 0 ? 1 : 0)) * ROWS + r) * LD; };
+                constexpr int SHARE = THREADS / ROWS;
+                const int r0 = threadIdx.x / SHARE, q0 = threadIdx.x % SHARE;
+                float top = -INFINITY, weight = 0.f;
+                if (r0 < rows) {
+#pragma unroll 4
+                    for (int p = q0; p < parts; p += SHARE) top = fmaxf(top, __ldcg(row_of(p, r0) + D));
+                }
+#pragma unroll
+                for (int x = 1; x < SHARE; x *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                const float from = top == -INFINITY ? 0.f : top;
+                if (r0 < rows) {
+#pragma unroll 4
+                    for (int p = q0; p < parts; p += SHARE) {
+                        // (sums of nothing are 0; a maximum that is not finite makes them NaN, as it should)
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(row_of(p, r0) + D));
+                        const float f = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - from);
+                        sums[p * ROWS + r0] = f;
+                        weight += ml.y * f;
+                    }
+                }
+#pragma unroll
+                for (int x = 1; x < SHARE; x *= 2) weight += __shfl_xor_sync(0xffffffffu, weight, x);
+                if (q0 == 0) row_weight[r0] = weight;
+                __syncthreads();
+                for (int e = threadIdx.x; e < rows * (D / 4); e += THREADS) {
+                    const int r = e / (D / 4), col = 4 * (e - r * (D / 4));
+                    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+                    for (int p = 0; p < parts; ++p) {
+                        const float4 v = __ldcg(reinterpret_cast<const float4*>(row_of(p, r) + col));
+                        const float f = sums[p * ROWS + r];
+                        x.x += v.x * f;
+                        x.y += v.y * f;
+                        x.z += v.z * f;
+                        x.w += v.w * f;
+                    }
+                    finish(r, col, x.x, x.y, row_weight[r]);
+                    finish(r, col + 2, x.z, x.w, row_weight[r]);
+                }
             }
         }
         __syncthreads();   // the sums may be written again
@@ -424,17 +444,23 @@ paged_kernel(const PagedParams P) {
     }
 }
 
+// Two CTAs per SM.
+int most_ctas(const sama_ctx* ctx) { return 2 * ctx->sm_count; }
+
 template <typename T, int D, bool CAP, bool BIAS>
 cudaError_t launch(sama_ctx* ctx, const PagedParams& P, int ctas, cudaStream_t st) {
     auto* kernel = paged_kernel<T, D, CAP, BIAS>;
+    // the ring, and what is the larger of the warps' sums and the factors of all parts
+    using C = PagedTile<D>;
+    const int sums = WARPS * ROWS * C::LD * 4, factors = most_ctas(ctx) * ROWS * 4, smem = WARPS * C::RING + (sums > factors ? sums : factors);
     const uint32_t bit = 1u << ((std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
     if (!(ctx->paged_ready & bit)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PagedTile<D>::SMEM);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
         ctx->paged_ready |= bit;
     }
     KernelScope scope(ctx, SAMA_K_PAGED, -1, st);
-    return launch_dependent(kernel, dim3((unsigned)ctas), dim3(THREADS), PagedTile<D>::SMEM, st, P);
+    return launch_dependent(kernel, dim3((unsigned)ctas), dim3(THREADS), (size_t)smem, st, P);
 }
 template <typename T, int D>
 cudaError_t launch(sama_ctx* ctx, const PagedParams& P, int ctas, cudaStream_t st) {
@@ -442,8 +468,6 @@ cudaError_t launch(sama_ctx* ctx, const PagedParams& P, int ctas, cudaStream_t s
     return P.a.slopes ? launch<T, D, false, true>(ctx, P, ctas, st) : launch<T, D, false, false>(ctx, P, ctas, st);
 }
 
-// Two CTAs per SM.
-int most_ctas(const sama_ctx* ctx) { return 2 * ctx->sm_count; }
 
 }  // namespace
 
