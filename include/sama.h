@@ -334,7 +334,7 @@ int sama_clip_grads(sama_ctx* ctx, const sama_tensor_t* tensors, int32_t n_tenso
  * k_starts[t] .. k_starts[t+1] - 1, and its queries see its own keys only.  The last query has the position of the last
  * key: with Lq queries and Lk keys, query i of a text is at position i + Lk - Lq, key j at j (so a prompt's next chunk is
  * the case Lk > Lq).  causal: a query sees the keys up to its position, and those before prefix[t] (NULL: none).
- * A query that sees no key has out = 0, lse = -infinity and no gradient.  Rows of no text (before the first start, from
+ * A query that sees no key (or none whose score is above -infinity) has out = 0, lse = -infinity and no gradient.  Rows of no text (before the first start, from
  * the last on) are neither read for any text nor written, and no value of one text, finite or not, reaches another's.
  * Within a text a v that is not finite may reach queries that do not see it (as 0 * infinity does). */
 typedef struct sama_attn_t {
@@ -359,8 +359,10 @@ typedef struct sama_attn_t {
  * the gaps between rows are left alone, so they may be parts of one buffer, too), of type `dtype`, each required:
  *   dP = d_out . v,  dX = softmax * (dP - d_out . out) * (1 - tanh^2),  dq = scale * dX k,  dk = scale * dX^T q,
  *   dv = softmax^T d_out
- * dk and dv are summed over the heads that share them.  Sums are fp32, in a fixed order (bitwise reproducible); dX and the
- * softmax are rounded to `dtype` as operands of the last products.  slopes get no gradient.  Uses 8 * heads * n_q bytes of
+ * dk and dv are summed over the heads that share them.  Sums are fp32, in a fixed order (bitwise reproducible).  dX and the
+ * softmax are rounded to `dtype` as operands of the last products, and d_out . out takes out as it was stored: against sums of
+ * unrounded values the gradients' relative error grows from 0.0017 to 0.0025 .. 0.003 in bf16, 0.0002 to 0.00035 .. 0.0004 in
+ * fp16 (out's to 0.0018 .. 0.0022, 0.0003).  slopes get no gradient.  Uses 8 * heads * n_q bytes of
  * the workspace. */
 int sama_attention(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, void* out,
                    float* lse_out, void* stream);

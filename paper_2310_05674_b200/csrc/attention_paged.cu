@@ -106,7 +106,7 @@ paged_kernel(const PagedParams P) {
         total += scan[w];
     }
     const int ctas = (int)min((int64_t)gridDim.x, max((int64_t)1, total / kMinSteps)), cta = (int)blockIdx.x;
-    auto first_of = [&](int c) { return total * c / ctas; };
+    auto first_of = [&](int c) { return total / ctas * c + total % ctas * c / ctas; };   // (total * c might pass 64 bits)
     const int64_t begin = cta < ctas ? first_of(cta) : total, end = cta < ctas ? first_of(cta + 1) : total;
     if (begin < end && begin >= upto - mine && begin < upto) {
         int64_t before = upto - mine;
@@ -380,7 +380,7 @@ paged_kernel(const PagedParams P) {
             // the CTAs that hold this unit's first and last steps
             const int64_t unit0 = begin + i - at.step, unit1 = unit0 + at.steps - 1;
             auto holder = [&](int64_t step) {
-                int h = (int)(step * ctas / total);
+                int h = min((int)((double)step * ctas / (double)total), ctas - 1);
                 while (first_of(h) > step) --h;
                 while (first_of(h + 1) <= step) ++h;
                 return h;
@@ -497,7 +497,8 @@ cudaError_t launch_paged(sama_ctx* ctx, const PagedShape& a, int dtype, const vo
     P.parts = static_cast<float*>(ws);
     P.arrived = ctx->paged_arrived;
     // no more CTAs than there can be shares
-    const int64_t steps = ((int64_t)a.max_pages * a.page_size + STEP - 1) / STEP * a.n_seqs * a.kv_heads * ((a.group + ROWS - 1) / ROWS);
+    const int64_t most_keys = (int64_t)a.max_pages * a.page_size < 0x7fffffff ? (int64_t)a.max_pages * a.page_size : 0x7fffffff;
+    const int64_t steps = (most_keys + STEP - 1) / STEP * a.n_seqs * a.kv_heads * ((a.group + ROWS - 1) / ROWS);
     const int64_t shares = steps / kMinSteps > 1 ? steps / kMinSteps : 1;
     const int ctas = shares < most_ctas(ctx) ? (int)shares : most_ctas(ctx);
     if (dtype == SAMA_BF16)

@@ -297,7 +297,8 @@ distill_kernel(const DistillParams P) {
     // their waiting for it: its loads depend on one another.
     float most = -INFINITY, total = 0.f;
     if (ctas == 1) {
-        if (warp == WARPS) asm volatile("bar.sync 2, %0;" ::"n"(MAIN + 32) : "memory");
+        // (in place they do: nothing is written before the loss has the logits that it needs)
+        if (warp == WARPS || P.in_place) asm volatile("bar.sync 2, %0;" ::"n"(MAIN + 32) : "memory");
         else asm volatile("bar.arrive 2, %0;" ::"n"(MAIN + 32) : "memory");
     }
     if (ctas == 1 || warp < WARPS) {
