@@ -57,16 +57,18 @@ __device__ __forceinline__ int attn_start(const int32_t* starts, int i, int n) {
 template <int TILE>
 __device__ __forceinline__ int attn_find(const int32_t* starts, int n_texts, int n, int slot, int* tile) {
     const int lane = threadIdx.x & 31;
-    if (attn_start(starts, 0, n) / TILE > slot) return -1;
-    int lo = 0, hi = n_texts;
-    while (hi - lo > 1) {
+    int lo = 0, hi = n_texts, first = 0;
+    do {
         const int step = (hi - lo + 31) / 32, t = lo + lane * step;
-        const bool before = t < hi && attn_start(starts, t, n) / TILE + t <= slot;
-        const int last = 31 - __clz(__ballot_sync(0xffffffffu, before) | 1u);
+        const int at = t < hi ? attn_start(starts, t, n) / TILE + t : 0x7fffffff;
+        const uint32_t before = __ballot_sync(0xffffffffu, at <= slot);
+        if (!(before & 1u)) return -1;   // (before the first text; or starts that fall)
+        const int last = 31 - __clz(before);
+        first = __shfl_sync(0xffffffffu, at, last);
         lo += last * step;
         hi = min(hi, lo + step);
-    }
-    *tile = slot - (attn_start(starts, lo, n) / TILE + lo);
+    } while (hi - lo > 1);
+    *tile = slot - first;
     return lo;
 }
 // Starts that fall or lie outside are clamped, here and wherever they are used, and reported.

@@ -62,7 +62,6 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     constexpr uint32_t COLS = C::COLS;
     const AttnShape& a = P.a;
 
-    pdl_trigger();
     pdl_wait();
     if (!KEYS && blockIdx.x == 0) attn_check_starts(a);
     // heavy tiles first: the first keys are seen by most queries, the last queries see most keys
@@ -125,6 +124,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // (not before tensor memory is had: a kernel that starts early may take it and wait for this one)
+    pdl_trigger();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_ptr_slot, 0);
     const uint32_t s_cols = tmem, dp_cols = tmem + BT;
     auto g_cols = [&](int i) { return tmem + (uint32_t)(2 * BT + i * D); };

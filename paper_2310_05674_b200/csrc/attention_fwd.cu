@@ -50,7 +50,6 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     constexpr uint32_t IDESC_S = idesc16(BF16, false, false, kAttnRows, BK), IDESC_O = idesc16(BF16, false, true, kAttnRows, D);
     const AttnShape& a = P.a;
 
-    pdl_trigger();
     pdl_wait();
     if (blockIdx.x == 0) attn_check_starts(a);
     // the last tiles of a text, which see the most keys, come first
@@ -95,6 +94,8 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // (not before tensor memory is had: a kernel that starts early may take it and wait for this one)
+    pdl_trigger();
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_ptr_slot, 0);
     auto s_cols = [&](int w) { return tmem + (uint32_t)(w * BK); };
     auto o_cols = [&](int w) { return tmem + (uint32_t)(NW * BK + w * D); };
