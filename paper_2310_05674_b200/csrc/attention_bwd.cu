@@ -11,12 +11,17 @@
 //
 // The order of the products of tile i is  dP_i, dV (from P_i), S_i+1, dK (from dX_i), dP_i+1, ...:  P_i+1 is formed from
 // S_i+1 while dK and dP_i+1 run, dX_i from dP_i while dV and S_i+1 run.  S, dP and two accumulators of 128 columns fill tensor
-// memory.  (Tiles of 64 rows in two buffers, which the two halves of the warps took in turn, were half as fast: a product
-// 64 wide takes 48 cycles in place of 32, and each wait of the issuing thread leaves the tensor cores idle for some 200
-// cycles, since it can run ahead of them by a product or two only.)
+// memory.  (Tiles of 64 rows in two buffers, which the two halves of the warps took in turn, were slower, 1452 for 1148 us:
+// a product 64 wide takes 48 cycles in place of 32, and each wait of the issuing thread leaves the tensor cores idle for some
+// 200 cycles, since it can run ahead of them by a product or two only.)  Heads of up to 64 columns have tiles of 64 rows
+// and two CTAs per SM, which overlap each other.
 //
-// Roles of the 18 warps: warp 0 copies, warp 1 issues products, warps 2..17 form P and dX: four warps share 32 rows, each of
-// them has 32 of a tile's columns.  Every wait is bounded.
+// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 1010, d-keys
+// 1160, 620 TFLOP/s of the five products that the definition needs, 870 of the seven: forming P and dX (13 instructions per
+// score with a cap, 8 without) between products that wait for them.  48 texts of up to 512, 16 heads of 64: 139 and 150.
+//
+// Roles of the warps: warp 0 copies, warp 1 issues products, the other 16 (or 8) form P and dX: several share 32 rows, each
+// of them has 32 of a tile's columns.  Every wait is bounded.
 #include <type_traits>
 
 #include "attention.h"

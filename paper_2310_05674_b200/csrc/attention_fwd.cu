@@ -2,13 +2,20 @@
 // sum of the softmax, on the 5th-generation tensor cores.
 //
 // A CTA has 128 or 256 queries of one text and head, one or two tiles of 128, and streams the keys and values that they see.
-// A score tile S = Q K^T is produced in tensor memory; four warps per tile, a thread per query, turn it into weights
+// A score tile S = Q K^T is produced in tensor memory; four warps, or eight that share its columns, turn it into weights
 // P = 2^(x log2 e - m), which go back to tensor memory in 16 bits over the scores they came from, and O += P V takes them
-// from there.  While one tile's weights are formed the other's products run: two tiles in a CTA for heads of more than 64
-// columns, which share the keys and values (64 KB per 128 of them, more than L2 delivers twice in that time), and three
-// CTAs of one tile per SM for others, whose arithmetic bounds them.  The maximum m that the weights refer to is only raised
-// when a score exceeds it by more than 8 binary orders (O and the sum are scaled then): the weights stay below 2^8, far from
-// the end of either type, and are rounded relative to their size whatever they refer to.
+// from there.  While one tile's weights are formed the other's products run: the other tile of the CTA, which shares the
+// keys and values, or that of another CTA of the SM (heads of more than 64 columns: two CTAs; others: three).  The maximum m
+// that the weights refer to is only raised when a score exceeds it by more than 8 binary orders (O and the sum are scaled
+// then): the weights stay below 2^8, far from the end of either type, and are rounded relative to their size whatever they
+// refer to.
+//
+// What bounds it (one B200, bf16): the chain from a tile's scores to its weights and their products; one text of 8192, 32
+// heads of 128 over 8, causal: 484 us, 1130 TFLOP/s of the pairs that are seen (0.69 of the measured rate), 745 with a cap;
+// 48 texts of up to 512, 16 heads of 64: 94, where ragged tiles and the start and end of short CTAs weigh as much.  Tensor
+// cores, special-function units and issue slots are each in use for 50 to 57 % of the time (two prompts' next 1000 tokens
+// behind 7000, 250 us, a third of it the last round of CTAs).  Exponentials by a polynomial for a quarter of the scores, and
+// rounding to bf16 by integer addition, were slower (275, 254): more instructions in the chain.
 //
 // Roles of the warps: warp 0 copies (TMA, 128-byte swizzle), warp 1 issues products, the others the softmax.  Every wait is
 // bounded: one that expires raises SAMA_DEV_TIMEOUT and ends the CTA's work.
@@ -22,14 +29,16 @@ namespace {
 
 constexpr float kRaise = 8.f;
 
-template <int D> struct FwdTile {
-    static constexpr int NW = D == 64 ? 1 : 2;           // tiles of queries, of four warps each
-    static constexpr int THREADS = 64 + 128 * NW;
-    static constexpr int CTAS = D == 64 ? 3 : 1;         // per SM
+// NW: tiles of queries of a CTA.
+template <int D, int NW> struct FwdTile {
+    static constexpr int HALVES = NW;                    // warps that share 32 rows of a tile, and the columns of its scores
+    static constexpr int THREADS = 64 + 128 * NW * HALVES;
+    static constexpr int CTAS = D == 64 ? 3 : 3 - NW;    // per SM
     static constexpr int BK = D == 64 ? 64 : 128;        // keys of a tile
-    static constexpr int STAGES = 4;                     // tiles of keys or values in shared memory
+    static constexpr int STAGES = D == 64 ? 4 : 2 * NW;  // tiles of keys or values in shared memory
     static constexpr int Q_BYTES = kAttnRows * D * 2, KV_BYTES = BK * D * 2;
-    static constexpr int SMEM = NW * Q_BYTES + STAGES * KV_BYTES + 256 + 1024;
+    static constexpr int SHARED = HALVES == 1 ? 0 : 2 * NW * HALVES * kAttnRows * 4;
+    static constexpr int SMEM = NW * Q_BYTES + STAGES * KV_BYTES + SHARED + 256 + 1024;
     static constexpr int COLS = NW * (BK + D);           // of tensor memory: a score tile and an output for each tile of queries
 };
 
@@ -41,11 +50,11 @@ struct alignas(64) FwdParams {
     int slots;
 };
 
-template <typename T, int D, bool CAP, bool BIAS>
-__global__ void __launch_bounds__(FwdTile<D>::THREADS, FwdTile<D>::CTAS)
+template <typename T, int D, int NW, bool CAP, bool BIAS>
+__global__ void __launch_bounds__((FwdTile<D, NW>::THREADS), (FwdTile<D, NW>::CTAS))
 attn_fwd_kernel(const __grid_constant__ FwdParams P) {
-    using C = FwdTile<D>;
-    constexpr int BK = C::BK, STAGES = C::STAGES, NW = C::NW;
+    using C = FwdTile<D, NW>;
+    constexpr int BK = C::BK, STAGES = C::STAGES, HALVES = C::HALVES, MY = BK / HALVES;   // MY: columns of a warp
     constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr uint32_t IDESC_S = idesc16(BF16, false, false, kAttnRows, BK), IDESC_O = idesc16(BF16, false, true, kAttnRows, D);
     const AttnShape& a = P.a;
@@ -64,7 +73,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
-    const uint32_t ring = base + NW * C::Q_BYTES, bars = ring + STAGES * C::KV_BYTES;
+    const uint32_t ring = base + NW * C::Q_BYTES, shared = ring + STAGES * C::KV_BYTES, bars = shared + C::SHARED;
     auto full_bar = [&](int s) { return bars + 8u * s; };
     auto empty_bar = [&](int s) { return bars + 8u * (STAGES + s); };
     auto q_bar = [&](int w) { return bars + 8u * (2 * STAGES + w); };
@@ -84,7 +93,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
         for (int w = 0; w < NW; ++w) {
             mbar_init(q_bar(w), 1);
             mbar_init(s_bar(w), 1);
-            mbar_init(p_bar(w), 4);
+            mbar_init(p_bar(w), 4 * HALVES);
             mbar_init(o_bar(w), 1);
         }
         *abort_flag = 0;
@@ -189,7 +198,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                     const uint64_t dv = attn_desc_mn(ring + vs * C::KV_BYTES, BK);
 #pragma unroll
                     for (int k = 0; k < BK / 16; ++k)
-                        umma16_ta(o_cols(w), s_cols(w) + 8u * k, dv + (uint64_t)(k * 2048 >> 4), IDESC_O, j > 0 || k > 0);
+                        umma16_ta(o_cols(w), s_cols(w) + (uint32_t)(k / (MY / 16) * MY + k % (MY / 16) * 8), dv + (uint64_t)(k * 2048 >> 4), IDESC_O, j > 0 || k > 0);
                     // (products are executed in order: the next scores do not overtake the weights they replace)
                     if (j + 1 < n_kt[w]) scores(w, j + 1); else umma_commit(o_bar(w));
                 }
@@ -201,7 +210,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             __syncwarp();
         }
     } else {
-        const int w = (warp - 2) >> 2, quarter = warp & 3;
+        const int w = (warp - 2) / (4 * HALVES), half = (warp - 2) / 4 % HALVES, quarter = warp & 3;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const int row0 = first + w * kAttnRows + quarter * 32, row = row0 + lane;   // in the text
         const int seen = attn_seen(a, x, row), seen_by_all = attn_seen(a, x, row0);
@@ -210,36 +219,46 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
         const float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
         const float inv_cap = CAP ? a.scale / a.cap : 0.f, cap2 = CAP ? a.cap * kLog2e : 0.f;
         const AttnTanh near(inv_cap, cap2);
+        // What the other half of a row's columns has: by turns in two places, so that one barrier per exchange is enough.
+        volatile float* mine = reinterpret_cast<volatile float*>(smem_raw + (shared - raw)) + (w * HALVES + half) * kAttnRows + quarter * 32 + lane;
+        volatile float* other = mine + (half ? -kAttnRows : kAttnRows);
+        auto exchange = [&](float v, int turn) {
+            constexpr int TURN = NW * HALVES * kAttnRows;
+            mine[turn * TURN] = v;
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + w * 4 + quarter) : "memory");
+            return other[turn * TURN];
+        };
         float m = -INFINITY, l = 0.f;
         bool ok = true;
         for (int j = 0; j < n_kt[w]; ++j) {
             if (!(ok = wait(s_bar(w), j & 1))) break;
             tc_fence_after();
-            float s[BK];
+            float s[MY];
 #pragma unroll
-            for (int k = 0; k < BK; k += 32) tmem_ld32_nowait(s_cols(w) + lanes + k, s + k);
+            for (int k = 0; k < MY; k += 32) tmem_ld32_nowait(s_cols(w) + lanes + half * MY + k, s + k);
             tmem_wait_ld();
             if (CAP) {
-                const float big = attn_max<BK>([&](int k) { return fabsf(s[k]); });
+                const float big = attn_max<MY>([&](int k) { return fabsf(s[k]); });
                 if (__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) {
 #pragma unroll
-                    for (int k = 0; k < BK; ++k) s[k] = near(s[k]);
+                    for (int k = 0; k < MY; ++k) s[k] = near(s[k]);
                 } else {
 #pragma unroll
-                    for (int k = 0; k < BK; ++k) s[k] = cap2 * attn_tanh(s[k] * inv_cap);
+                    for (int k = 0; k < MY; ++k) s[k] = cap2 * attn_tanh(s[k] * inv_cap);
                 }
             }
             if (BIAS) {
-                const float away = (float)(row + x.lk - x.lq - j * BK);
+                const float away = (float)(row + x.lk - x.lq - j * BK - half * MY);
 #pragma unroll
-                for (int k = 0; k < BK; ++k) s[k] = fmaf(-slope, fabsf(away - (float)k), CAP ? s[k] : s[k] * (a.scale * kLog2e));
+                for (int k = 0; k < MY; ++k) s[k] = fmaf(-slope, fabsf(away - (float)k), CAP ? s[k] : s[k] * (a.scale * kLog2e));
             }
             if ((j + 1) * BK > seen_by_all) {
-                const int left = seen - j * BK;
+                const int left = seen - j * BK - half * MY;
 #pragma unroll
-                for (int k = 0; k < BK; ++k) s[k] = k < left ? s[k] : -INFINITY;
+                for (int k = 0; k < MY; ++k) s[k] = k < left ? s[k] : -INFINITY;
             }
-            const float top = attn_max<BK>([&](int k) { return s[k]; }) * c;
+            float top = attn_max<MY>([&](int k) { return s[k]; }) * c;
+            if (HALVES == 2) top = fmaxf(top, exchange(top, j & 1));
             if (__any_sync(0xffffffffu, top > m + kRaise || (m == -INFINITY && top > m))) {
                 const float raised = fmaxf(m, top);
                 const float factor = raised == -INFINITY ? 1.f : fast_exp2(m - raised);
@@ -247,7 +266,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 l *= factor;
                 if (j > 0) {
 #pragma unroll 1
-                    for (int k = 0; k < D; k += 16) {   // (few at a time: the scores are in registers, too)
+                    for (int k = half * (D / HALVES); k < (half + 1) * (D / HALVES); k += 16) {   // (few at a time: the scores are in registers, too)
                         uint32_t r[16];
                         tmem_ld16_nowait(o_cols(w) + lanes + k, r);
                         tmem_wait_ld();
@@ -260,7 +279,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             const float from = m == -INFINITY ? 0.f : m;
             float sums[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < BK; k += 32) {
+            for (int k = 0; k < MY; k += 32) {
                 uint32_t r[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -268,7 +287,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                     sums[i % 4] += p0 + p1;
                     r[i] = pack2<T>(p0, p1);
                 }
-                tmem_st16_nowait(s_cols(w) + lanes + k / 2, r);
+                tmem_st16_nowait(s_cols(w) + lanes + half * MY + k / 2, r);
             }
             l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             tmem_wait_st();
@@ -282,12 +301,13 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             tc_fence_after();
         }
         if (ok && row0 < x.lq) {
+            if (HALVES == 2) l += exchange(l, n_kt[w] & 1);
             const bool empty = l == 0.f;
             const float inv = 1.f / l;
-            if (real && P.lse) P.lse[(int64_t)head * a.n_q + x.q0 + row] = empty ? -INFINITY : (m + __log2f(l)) * 0.69314718f;
+            if (real && P.lse && half == 0) P.lse[(int64_t)head * a.n_q + x.q0 + row] = empty ? -INFINITY : (m + __log2f(l)) * 0.69314718f;
             T* out = static_cast<T*>(P.out) + ((int64_t)(x.q0 + row) * a.heads + head) * a.dim;
 #pragma unroll 1
-            for (int k = 0; k < D; k += 32) {
+            for (int k = half * (D / HALVES); k < (half + 1) * (D / HALVES); k += 32) {
                 float o[32];
                 if (n_kt[w] > 0) {
                     tmem_ld32_nowait(o_cols(w) + lanes + k, o);
@@ -306,29 +326,39 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     if (warp == 1) tmem_dealloc(tmem, C::COLS);
 }
 
-template <typename T, int D, bool CAP, bool BIAS>
+template <typename T, int D, int NW, bool CAP, bool BIAS>
 cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
-    auto* kernel = attn_fwd_kernel<T, D, CAP, BIAS>;
-    const uint32_t bit = 1u << ((std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
+    using C = FwdTile<D, NW>;
+    auto* kernel = attn_fwd_kernel<T, D, NW, CAP, BIAS>;
+    const uint32_t bit = 1u << ((NW == 2 ? 16 : 0) + (std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
     if (!(ctx->attn_fwd_ready & bit)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdTile<D>::SMEM);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         if (e != cudaSuccess) return e;
         ctx->attn_fwd_ready |= bit;
     }
     KernelScope scope(ctx, SAMA_K_ATTN, 0, st);
-    return launch_dependent(kernel, dim3((unsigned)((int64_t)P.slots * P.a.heads)), dim3(FwdTile<D>::THREADS), FwdTile<D>::SMEM, st, P);
+    return launch_dependent(kernel, dim3((unsigned)((int64_t)P.slots * P.a.heads)), dim3(C::THREADS), C::SMEM, st, P);
 }
-template <typename T, int D>
+template <typename T, int D, int NW>
 cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
-    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, true, true>(ctx, P, st) : launch<T, D, true, false>(ctx, P, st);
-    return P.a.slopes ? launch<T, D, false, true>(ctx, P, st) : launch<T, D, false, false>(ctx, P, st);
+    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, NW, true, true>(ctx, P, st) : launch<T, D, NW, true, false>(ctx, P, st);
+    return P.a.slopes ? launch<T, D, NW, false, true>(ctx, P, st) : launch<T, D, NW, false, false>(ctx, P, st);
+}
+template <typename T>
+cudaError_t launch(sama_ctx* ctx, int nw, const FwdParams& P, cudaStream_t st) {
+    if (P.a.dim <= 64) return launch<T, 64, 1>(ctx, P, st);
+    return nw == 1 ? launch<T, 128, 1>(ctx, P, st) : launch<T, 128, 2>(ctx, P, st);
 }
 
 }  // namespace
 
 cudaError_t launch_attention(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, void* out, float* lse, cudaStream_t st) {
     FwdParams P;
-    const int bk = a.dim <= 64 ? FwdTile<64>::BK : FwdTile<128>::BK, rows = kAttnRows * (a.dim <= 64 ? FwdTile<64>::NW : FwdTile<128>::NW);
+    const int bk = a.dim <= 64 ? FwdTile<64, 1>::BK : FwdTile<128, 2>::BK;
+    // Two tiles per CTA, unless that makes so few CTAs that SMs are left without (us with two and with one, 32 heads of 128:
+    // one text of 512 21 and 17, of 1024 29 and 25, of 4096 150 and 148, of 8192, capped, 745 and 812; 32 of 300 99 and 80).
+    const int64_t pairs = ((int64_t)a.n_q / (2 * kAttnRows) + a.n_texts) * a.heads;
+    const int nw = a.dim <= 64 || pairs < 4 * (int64_t)ctx->sm_count ? 1 : 2;
     // (without keys nothing is loaded, but a map has to describe something)
     const bool none = a.n_k == 0;
     if (!attn_map(&P.q, op.q, op.dtype, a.dim, a.heads, a.n_q, op.q_stride, kAttnRows) ||
@@ -338,10 +368,8 @@ cudaError_t launch_attention(sama_ctx* ctx, const AttnShape& a, const AttnOperan
     P.a = a;
     P.out = out;
     P.lse = lse;
-    P.slots = a.n_q / rows + a.n_texts;
-    if (op.dtype == SAMA_BF16)
-        return a.dim <= 64 ? launch<__nv_bfloat16, 64>(ctx, P, st) : launch<__nv_bfloat16, 128>(ctx, P, st);
-    return a.dim <= 64 ? launch<__half, 64>(ctx, P, st) : launch<__half, 128>(ctx, P, st);
+    P.slots = a.n_q / (nw * kAttnRows) + a.n_texts;
+    return op.dtype == SAMA_BF16 ? launch<__nv_bfloat16>(ctx, nw, P, st) : launch<__half>(ctx, nw, P, st);
 }
 
 }  // namespace sama
