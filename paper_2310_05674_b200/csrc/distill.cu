@@ -142,6 +142,10 @@ template <typename T> __device__ __forceinline__ uint4 vec_lowest() {
     const uint32_t w = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
     return make_uint4(w, w, w, w);
 }
+// 2^(c (z - m)).  One operation less takes c z - (c m), whose second product is rounded: an error of 2^-15 at most up to the
+// c m that `beyond` names, of anything for a row of nothing but masked values (-1e9, or the type's lowest).
+__device__ __forceinline__ float power_of(float z, float m, float c) { return fast_exp2((z - m) * c); }
+__device__ __forceinline__ bool beyond(float cm) { return fabsf(cm) > 1024.f; }
 // (m, l) of two parts, each a maximum and the sum of 2^(c (z - maximum)): l as seen from `top`.
 __device__ __forceinline__ float rebase(float l, float m, float top, float c) { return m == -INFINITY ? l : l * fast_exp2((m - top) * c); }
 
@@ -224,9 +228,9 @@ distill_kernel(const DistillParams P) {
         // (in place, no CTA writes before the loss has the logits that it needs)
         if (ctas > 1 && P.in_place) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
         top = over(top, max_of);
-        const float from_u = top == -INFINITY ? 0.f : top * P.c;
+        const float from_u = top == -INFINITY ? 0.f : top;
         for (int j = lane; j < P.k; j += 32) {
-            const float lp = fmaf(value[j], P.c, -from_u), p = exp2f(lp);   // log2 of p, up to the sum
+            const float lp = (value[j] - from_u) * P.c, p = exp2f(lp);   // log2 of p, up to the sum
             sum_u += p;
             if (p > 0.f) entropy += p * lp;
             value[j] = p;
@@ -260,7 +264,10 @@ distill_kernel(const DistillParams P) {
         }
     } else {
         // (one warp asks for the copy, the others wait at a barrier: asking again and again takes issue slots)
-        if (warp == 0 && !mbar_wait(bar, 0)) atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
+        if (warp == 0 && !mbar_wait(bar, 0)) {
+            atomicOr(P.status, (int)SAMA_DEV_TIMEOUT);
+            mbar_wait(bar, 0);   // (the copy should land before the CTA's memory goes away)
+        }
         asm volatile("bar.sync 1, %0;" ::"n"(MAIN) : "memory");
         const uint4* chunk = reinterpret_cast<const uint4*>(smem);
         float m = -INFINITY, l = 0.f;
@@ -289,6 +296,16 @@ distill_kernel(const DistillParams P) {
         int b = t;
         for (; b + (BATCH - 1) * MAIN < n; b += MAIN * BATCH) take(std::integral_constant<int, BATCH>(), b);
         for (; b < n; b += MAIN) take(std::integral_constant<int, 1>(), b);
+        if (beyond(m * P.c) && m != -INFINITY) {   // once more (in the loop it would cost ordinary rows a tenth of their time)
+            l = 0.f;
+#pragma unroll 1
+            for (b = t; b < n; b += MAIN) {
+                float f[VE];
+                unpack_vec<T>(chunk[b], f);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) l += power_of(f[e], m, P.c);
+            }
+        }
         const float top = over(m, max_of);
         l = over(rebase(l, m, top, P.c), sum_of);
         if (lane == 0) warp_sums[warp] = make_float2(top, l);
@@ -334,7 +351,7 @@ distill_kernel(const DistillParams P) {
             const float p = value[j] * inv_u, ze = logit[j];
             if (id >= 0 && !(p == 0.f)) cross += p * ((ze - base) * P.c);
             const bool mine = id >= 0 && id + skip >= 0 && id + skip < n * VE && p != 0.f;   // (without weight the gradient is q's own)
-            value[j] = coef * (fast_exp2(fmaf(ze, P.c, -whole)) * inv - p);
+            value[j] = coef * (power_of(ze, base, P.c) * inv - p);
             place[j] = mine ? id : -1;
         }
         if (P.loss && rank == 0) {
@@ -374,14 +391,25 @@ distill_kernel(const DistillParams P) {
                 store_n<T, VE, true>(g_part + (b + v * MAIN) * VE, g);
             }
         };
-        int b = in0 + t;
-        for (; b + (BATCH - 1) * MAIN < in1; b += MAIN * BATCH) make(std::integral_constant<int, BATCH>(), b);
-        for (; b < in1; b += MAIN) make(std::integral_constant<int, 1>(), b);
-        for (int e = t; e < in0 + n - in1; e += MAIN) {
-            float g[VE];
-            const int at = e < in0 ? e : in1 + e - in0;
-            gradient(chunk[at], g);
-            put_elements(at, g);
+        if (!beyond(whole)) {
+            int b = in0 + t;
+            for (; b + (BATCH - 1) * MAIN < in1; b += MAIN * BATCH) make(std::integral_constant<int, BATCH>(), b);
+            for (; b < in1; b += MAIN) make(std::integral_constant<int, 1>(), b);
+            for (int e = t; e < in0 + n - in1; e += MAIN) {
+                float g[VE];
+                const int at = e < in0 ? e : in1 + e - in0;
+                gradient(chunk[at], g);
+                put_elements(at, g);
+            }
+        } else {
+#pragma unroll 1
+            for (int b = t; b < n; b += MAIN) {
+                float g[VE];
+                unpack_vec<T>(chunk[b], g);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) g[e] = power_of(g[e], base, P.c) * f;
+                put_elements(b, g);
+            }
         }
     }
     __syncthreads();
@@ -476,7 +504,10 @@ distill_few_kernel(const DistillParams P) {
         const Span s = span_of(z_row(row), row_bytes, 0, 1);
         const int n = s.v1;
         uint8_t* chunk = ring + stage * FEW_CHUNK;
-        if (!mbar_wait(bar(stage), (uint32_t)parity)) timed_out = true;
+        if (!mbar_wait(bar(stage), (uint32_t)parity)) {
+            timed_out = true;
+            mbar_wait(bar(stage), (uint32_t)parity);   // (the copy should land before the CTA's memory goes away)
+        }
         int place, element;
         edge_of<VE>(s, row_bytes, SIZE, t, &place, &element);
         if (place >= 0) reinterpret_cast<T*>(chunk)[place] = edge;
@@ -503,16 +534,16 @@ distill_few_kernel(const DistillParams P) {
         }
         top = over(top, max_of);
         top_u = over(top_u, max_of);
-        const float from = top == -INFINITY ? 0.f : top * P.c, from_u = top_u == -INFINITY ? 0.f : top_u * P.c;
+        const float from = top == -INFINITY ? 0.f : top, from_u = top_u == -INFINITY ? 0.f : top_u;
         float sum = 0.f, sum_u = 0.f;
 #pragma unroll
         for (int i = 0; i < VECS * VE; ++i) {
-            v[i] = fast_exp2(fmaf(v[i], P.c, -from));
+            v[i] = power_of(v[i], from, P.c);
             sum += v[i];
         }
 #pragma unroll
         for (int i = 0; i < FEW_ENTRIES; ++i) {
-            my_u[i] = fmaf(my_u[i], P.c, -from_u);       // log2 of p, up to the sum
+            my_u[i] = (my_u[i] - from_u) * P.c;          // log2 of p, up to the sum
             sum_u += exp2f(my_u[i]);
         }
         sum = over(sum, sum_of);
@@ -524,7 +555,7 @@ distill_few_kernel(const DistillParams P) {
 #pragma unroll
             for (int i = 0; i < FEW_ENTRIES; ++i) {
                 const float p = exp2f(my_u[i]) * inv_u;
-                if (my_id[i] >= 0 && !(p == 0.f)) part += p * ((my_u[i] - log_u) - ((my_z[i] - (top == -INFINITY ? 0.f : top)) * P.c - log_total));
+                if (my_id[i] >= 0 && !(p == 0.f)) part += p * ((my_u[i] - log_u) - ((my_z[i] - from) * P.c - log_total));
             }
             part = over(part, sum_of);
             if (t == 0) P.loss[row] = none ? 0.f : P.temperature * P.temperature * 0.69314718f * part;
@@ -563,7 +594,7 @@ distill_few_kernel(const DistillParams P) {
                             is_first = is_first && x + e >= j;
                         }
                 }
-                if (is_first) reinterpret_cast<T*>(chunk)[my_id[i] + s.head / SIZE] = from_float<T>(coef * (fast_exp2(fmaf(my_z[i], P.c, -from)) * inv - p));
+                if (is_first) reinterpret_cast<T*>(chunk)[my_id[i] + s.head / SIZE] = from_float<T>(coef * (power_of(my_z[i], from, P.c) * inv - p));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
@@ -621,22 +652,22 @@ distill_long_kernel(const DistillParams P) {
                 v[i] = e < P.vocab ? to_float(z[e]) : -INFINITY;
                 top = fmaxf(top, v[i]);
             }
-            const float from = top == -INFINITY ? 0.f : top * P.c;
+            const float from = top == -INFINITY ? 0.f : top;
             l *= m == -INFINITY ? 0.f : fast_exp2((m - top) * P.c);
             m = top;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) l += fast_exp2(fmaf(v[i], P.c, -from));
+            for (int i = 0; i < 8; ++i) l += power_of(v[i], from, P.c);
         }
         const float2 tops = reduce(m, u, max_of);
-        const float from = tops.x == -INFINITY ? 0.f : tops.x * P.c, from_u = tops.y == -INFINITY ? 0.f : tops.y * P.c;
-        u = fmaf(u, P.c, -from_u);
+        const float from = tops.x == -INFINITY ? 0.f : tops.x, from_u = tops.y == -INFINITY ? 0.f : tops.y;
+        u = (u - from_u) * P.c;
         // (a part of nothing but -infinity has a sum of 0, one with a NaN a sum of NaN)
         const float2 sums = reduce(m == -INFINITY ? l : l * fast_exp2((m - tops.x) * P.c), exp2f(u), sum_of);
         const float inv = 1.f / sums.x, inv_u = sums.y > 0.f ? 1.f / sums.y : 0.f;
         const bool none = !(sums.y > 0.f) && sums.y == sums.y;
         const float p = exp2f(u) * inv_u;
         if (P.loss) {
-            const float log_q = (target - (tops.x == -INFINITY ? 0.f : tops.x)) / P.temperature - logf(sums.x);
+            const float log_q = (target - from) / P.temperature - logf(sums.x);
             const float part = reduce(id >= 0 && !(p == 0.f) ? p * ((u - log2f(sums.y)) * 0.69314718f - log_q) : 0.f, 0.f, sum_of).x;
             if (t == 0) P.loss[row] = none ? 0.f : P.temperature * P.temperature * part;
         }
@@ -645,7 +676,7 @@ distill_long_kernel(const DistillParams P) {
         const bool zero = none || weight == 0.f;
         T* g = static_cast<T*>(P.grad) + row * P.ld_grad;
         for (int e = t; e < P.vocab; e += TEAM)
-            g[e] = from_float<T>(zero ? 0.f : coef * (fast_exp2(fmaf(to_float(z[e]), P.c, -from)) * inv));
+            g[e] = from_float<T>(zero ? 0.f : coef * (power_of(to_float(z[e]), from, P.c) * inv));
         e_id[t] = id;
         e_p[t] = p;
         __syncthreads();
@@ -657,7 +688,7 @@ distill_long_kernel(const DistillParams P) {
                     all += e_p[x];
                     is_first = is_first && x >= t;
                 }
-            if (is_first) g[id] = from_float<T>(coef * (fast_exp2(fmaf(target, P.c, -from)) * inv - all));
+            if (is_first) g[id] = from_float<T>(coef * (power_of(target, from, P.c) * inv - all));
         }
         __syncthreads();   // the entries may be written again
     }

@@ -188,6 +188,32 @@ def test_masked_logits(lib, vocab):
     assert bool(((c.grad.double() - g).abs()[keep] <= 2.0 ** -8 * g.abs()[keep] + 1e-5).all())
 
 
+@pytest.mark.parametrize("vocab", [300, 2500, 9000, 70000, 300001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T", [0.25, 1.0])
+def test_rows_of_the_lowest_and_the_largest_value(lib, vocab, dtype, T):
+    """Logits whose products with log2 e / T are beyond fp32, or have no digits left behind the point.  A row of one value is a row of zeros, and next to the largest
+    value the lowest has no weight."""
+    c = Case(lib, 4, vocab, 8, dtype, T=T, seed=9)
+    low, high = torch.finfo(c.z.dtype).min, torch.finfo(c.z.dtype).max
+    few = torch.arange(vocab, device="cuda") % 4 == 0
+    c.ids.copy_(c.ids - c.ids % 4)           # targets among the few
+    stand_in = torch.zeros_like(c.z)
+    stand_in[2, ~few] = -200.0 * T           # (a weight below any fp32 value)
+    c.z[0], c.z[1], c.z[2], c.z[3] = low, high, torch.where(few, high, low), -high / 2
+    c.top[0], c.top[1] = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+    c.run()
+    z, top = c.z.clone(), c.top.clone()
+    c.z.copy_(stand_in)
+    c.top[:2] = 0.0
+    want, bound, g, bg = c.reference()
+    assert bool(((c.loss.double() - want).abs() <= bound).all())
+    assert bool(((c.grad.double() - g).abs() <= bg).all())
+    c.z.copy_(z)
+    c.top.copy_(top)
+    assert c.S.sama_device_status(c.ctx) == 0
+
+
 def test_ids_out_of_range_are_reported(lib):
     for vocab in (300, 9000, 70000, 300000):
         c = Case(lib, 4, vocab, 6, "f32", seed=7)
