@@ -375,7 +375,7 @@ typedef struct sama_paged_t {
     int32_t dtype;                       /* SAMA_BF16 or SAMA_F16 */
     int32_t heads, kv_heads, head_dim;   /* kv_heads divides heads; head_dim a multiple of 8, 8 .. 128 */
     int32_t page_size;                   /* 1 .. 2^20 */
-    int32_t n_seqs, max_pages;           /* rows and columns of page_table; 0 .. 2^20, 1 .. 2^24 */
+    int32_t n_seqs, max_pages;           /* rows and columns of page_table; 0 .. 2^20, 1 .. 2^24 (heads * n_seqs * the keys of max_pages: 2^44) */
     int64_t n_pages;                     /* pages of each cache, 1 .. 2^31 - 1 */
     int64_t page_stride;                 /* elements from a page to the next, a multiple of 8; 0: page_size * kv_heads * head_dim */
     const int32_t* page_table;           /* device [n_seqs][max_pages]; entries behind a sequence's last page are not read */

@@ -300,6 +300,8 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             ok = wait(o_bar(w), 0);
             tc_fence_after();
         }
+        // (a warp that gives up does not come to the next exchange, where its partner may already be)
+        if (HALVES == 2 && !ok) asm volatile("bar.arrive %0, 64;" ::"r"(1 + w * 4 + quarter) : "memory");
         if (ok && row0 < x.lq) {
             if (HALVES == 2) l += exchange(l, n_kt[w] & 1);
             const bool empty = l == 0.f;
@@ -355,10 +357,11 @@ cudaError_t launch(sama_ctx* ctx, int nw, const FwdParams& P, cudaStream_t st) {
 cudaError_t launch_attention(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, void* out, float* lse, cudaStream_t st) {
     FwdParams P;
     const int bk = a.dim <= 64 ? FwdTile<64, 1>::BK : FwdTile<128, 2>::BK;
-    // Two tiles per CTA, unless that makes so few CTAs that SMs are left without (us with two and with one, 32 heads of 128:
-    // one text of 512 21 and 17, of 1024 29 and 25, of 4096 150 and 148, of 8192, capped, 745 and 812; 32 of 300 99 and 80).
-    const int64_t pairs = ((int64_t)a.n_q / (2 * kAttnRows) + a.n_texts) * a.heads;
-    const int nw = a.dim <= 64 || pairs < 4 * (int64_t)ctx->sm_count ? 1 : 2;
+    // Two tiles per CTA, which read the keys once, for long texts; for shorter ones a CTA's start and end and the tiles that
+    // a text does not fill weigh more (us with two and with one, 32 heads of 128 over 8: one text of 512 21 and 17, of 2048 53.6
+    // and 53.7, of 4096, causal, 150 and 148, of 8192, causal, 484 and 488, capped 745 and 812; 8 of 1024 76 and 70, 32 of 300
+    // 99 and 80; 2 of 4096, all heads with their own keys, 314 and 329).  Lengths are on the device, but their mean is known.
+    const int nw = a.dim <= 64 || a.n_q < 2048 * (int64_t)a.n_texts ? 1 : 2;
     // (without keys nothing is loaded, but a map has to describe something)
     const bool none = a.n_k == 0;
     if (!attn_map(&P.q, op.q, op.dtype, a.dim, a.heads, a.n_q, op.q_stride, kAttnRows) ||

@@ -116,6 +116,61 @@ def test_lengths(lib, lens, dim, dtype, causal):
     assert c.S.sama_device_status(c.ctx) == 0
 
 
+# How a call is worked on depends on its mean number of rows per text, those of no text among them: with many of them, texts
+# of any length are worked on as long ones are.
+MANY = 1024     # rows of no text, before and behind, per text
+
+
+@pytest.mark.parametrize("lens", LENGTHS + [[2305]], ids=lambda v: "-".join(map(str, v)))
+@pytest.mark.parametrize("dim,dtype", [(128, "bf16"), (128, "f16")])
+@pytest.mark.parametrize("causal", [False, True])
+def test_lengths_among_many_rows(lib, lens, dim, dtype, causal):
+    c = Case(lib, lens, dim=dim, dtype=dtype, causal=causal, edge=MANY * len(lens), seed=len(lens))
+    c.run()
+    c.check()
+    assert c.S.sama_device_status(c.ctx) == 0
+
+
+@pytest.mark.parametrize("dim", [40, 64, 72, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("cap", [0.0, 2.0, 30.0])
+def test_capped_and_biased_scores_among_many_rows(lib, dim, dtype, bias, cap):
+    for causal, fused in ((False, True), (True, False)):
+        c = Case(lib, [300, 1, 77], heads=4, kv=2, dim=dim, dtype=dtype, causal=causal, bias=bias, cap=cap, fused=fused,
+                 edge=3 * MANY, seed=3)
+        c.run()
+        c.check()
+
+
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_masks_among_many_rows(lib, cap, dim):
+    lq, lk, prefix = [3, 0, 200, 130, 1, 5, 300], [0, 40, 500, 30, 700, 5, 299], [5, 5, 0, 20, 3, 0, 2]
+    for causal, prefix in ((False, None), (True, None), (True, prefix)):
+        c = Case(lib, lq, lk, heads=4, kv=2, dim=dim, causal=causal, prefix=prefix, cap=cap, edge=7 * MANY, seed=5)
+        c.run()
+        c.check()
+    for bad in (NAN, math.inf):
+        plain, other = (Case(lib, [70, 61, 200], heads=2, kv=1, dim=dim, causal=True, edge=3 * MANY, seed=7) for _ in range(2))
+        for x in (other.q, other.k, other.v, other.dout):
+            x[other.qs[1]:other.qs[2]] = bad
+        plain.run()
+        other.run()
+        for x, y in zip((plain.out, *plain.grads), (other.out, *other.grads)):
+            for t in (0, 2):
+                at = slice(plain.qs[t], plain.qs[t + 1])
+                assert torch.equal(x[at], y[at]) and bool(torch.isfinite(x[at]).all())
+
+
+def test_large_scores_among_many_rows(lib):
+    c = Case(lib, [400, 130], heads=2, kv=2, dim=128, edge=2 * MANY, seed=8, size=60.0, scale=1.0)
+    ramp = torch.linspace(0.1, 20.0, c.nk, device="cuda")[:, None, None]
+    c.k.copy_((c.k.float() * ramp).to(c.k.dtype))
+    c.run()
+    c.check()
+
+
 @pytest.mark.parametrize("dim", [8, 16, 24, 40, 56, 72, 80, 96, 104, 120])
 @pytest.mark.parametrize("heads,kv", [(1, 1), (3, 3), (6, 2), (7, 1)])
 def test_head_sizes_and_shared_heads(lib, dim, heads, kv):

@@ -111,7 +111,7 @@ def decode(S, ctx, a, q=Q, k_new=G[0], v_new=G[1], k=K, v=V, out=O):
 @pytest.mark.parametrize("status,change", [w for w in WRONG if set(w[1]) <= {"heads", "kv_heads", "head_dim", "dtype", "scale", "cap"}] + [
     ("SIZE", dict(page_size=0)), ("SIZE", dict(page_size=2 ** 20 + 1)), ("SIZE", dict(n_seqs=-1)), ("SIZE", dict(n_seqs=2 ** 20 + 1)),
     ("SIZE", dict(max_pages=0)), ("SIZE", dict(max_pages=2 ** 24 + 1)), ("SIZE", dict(n_pages=0)), ("SIZE", dict(n_pages=2 ** 31)),
-    ("SIZE", dict(page_stride=2040)), ("SIZE", dict(page_stride=2052)), ("NULL", dict(page_table=None)), ("NULL", dict(lengths=None)),
+    ("SIZE", dict(n_seqs=2 ** 20, max_pages=2 ** 20, page_size=64)), ("SIZE", dict(page_stride=2040)), ("SIZE", dict(page_stride=2052)), ("NULL", dict(page_table=None)), ("NULL", dict(lengths=None)),
     ("ALIGN", dict(page_table=A + 2)), ("ALIGN", dict(lengths=B + 1)), ("ALIGN", dict(slopes=D + 3))],
     ids=lambda v: v if isinstance(v, str) else "-".join("%s=%s" % i for i in v.items()))
 def test_paged_arguments(S, blank, status, change):
