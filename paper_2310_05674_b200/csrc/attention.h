@@ -98,6 +98,28 @@ __device__ __forceinline__ int attn_first_query(const AttnShape& a, const AttnTe
     return !a.causal || j < x.prefix ? 0 : max(0, j - (x.lk - x.lq));
 }
 
+// Two fp32 operations in one instruction: the scores' arithmetic takes most of the issue slots.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
 // tanh(z) = 1 - 2 / (1 + exp 2z): an absolute error of two units in the last place of 1, which is what a capped score
 // needs (the hardware's own approximation has 2^-11, a hundredth of a weight at a cap of 30).  That takes two of the three
 // results of the special-function unit per score (16 a cycle and SM), so where no score of a warp's tile is beyond 0.75 caps
@@ -112,9 +134,9 @@ struct AttnTanh {   // times `factor`, of `scale` times its argument
 #pragma unroll
         for (int i = 0; i < 5; ++i) { k[i] = c[i] * f; f *= s2; }
     }
-    __device__ __forceinline__ float operator()(float x) const {
-        const float u = x * x;
-        return x * fmaf(fmaf(fmaf(fmaf(k[4], u, k[3]), u, k[2]), u, k[1]), u, k[0]);
+    __device__ __forceinline__ float2 operator()(float2 x) const {
+        const float2 u = mul2(x, x);
+        return mul2(x, fma2(fma2(fma2(fma2(both(k[4]), u, both(k[3])), u, both(k[2])), u, both(k[1])), u, both(k[0])));
     }
 };
 // The largest of N values, in eight chains: one would wait for each result before the next.

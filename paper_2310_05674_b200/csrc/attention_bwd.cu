@@ -50,7 +50,7 @@ struct alignas(64) BwdParams {
     AttnShape a;
     const void *out, *dout;
     const float* lse;
-    float *lse2, *delta;   // [heads][n_q]: lse log2 e (infinity for a query that sees nothing), and delta
+    float *lse2, *delta;   // [heads][n_q]: -lse log2 e (-infinity for a query that sees nothing), and -delta
     void* grad[2];      // dQ, or dK and dV
     int64_t ld[2];
     int slots;
@@ -262,7 +262,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         const AttnTanh tanh_near(inv_cap, 1.f);
         bool ok = true;
 
-        float lse2 = 0.f, delta = 0.f;
+        float lse2 = 0.f, delta = 0.f;   // (both negated)
         if (!KEYS) {
             // two of the warps that share these rows add up half of the columns each
             volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (halves - raw));
@@ -283,12 +283,12 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                 }
             }
             if (real) {
-                lse2 = P.lse[(int64_t)head0 * a.n_q + x.q0 + row] * kLog2e;
-                if (lse2 == -INFINITY) lse2 = INFINITY;
+                lse2 = P.lse[(int64_t)head0 * a.n_q + x.q0 + row] * -kLog2e;
+                if (lse2 == INFINITY) lse2 = -INFINITY;
             }
             if (w < 2) part[w * kAttnRows + quarter * 32 + lane] = sum;
             asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
-            delta = part[quarter * 32 + lane] + part[kAttnRows + quarter * 32 + lane];
+            delta = -part[quarter * 32 + lane] - part[kAttnRows + quarter * 32 + lane];
             if (w == 0 && real) {
                 P.lse2[(int64_t)head0 * a.n_q + x.q0 + row] = lse2;
                 P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta;
@@ -338,26 +338,22 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                         float4 lse4 = make_float4(lse2, lse2, lse2, lse2);
                         if (KEYS) lse4 = *reinterpret_cast<const float4*>(lses + k);
                         const float l4[4] = {lse4.x, lse4.y, lse4.z, lse4.w};
-                        float slack[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float v = p[k + e];
+                        for (int e = 0; e < 4; e += 2) {
+                            float2 v = make_float2(p[k + e], p[k + e + 1]), l2 = make_float2(l4[e], l4[e + 1]), slack;
                             if (CAP) {
-                                v = decltype(near)::value ? tanh_near(v) : attn_tanh(v * inv_cap);
-                                slack[e] = fmaf(-v, v, 1.f);
+                                v = decltype(near)::value ? tanh_near(v) : make_float2(attn_tanh(v.x * inv_cap), attn_tanh(v.y * inv_cap));
+                                slack = fma2(mul2(v, both(-1.f)), v, both(1.f));
                             }
-                            if (BIAS) v = fmaf(-slope, fabsf(away - (float)(k + e)), v * c);
-                            v = fast_exp2(BIAS ? v - l4[e] : fmaf(v, c, -l4[e]));
-                            if (decltype(some)::value && (k + e >= hi || (KEYS && k + e < lo))) v = 0.f;
-                            p[k + e] = v;
-                        }
-                        if (KEYS) {
-                            r[(k - h) / 2] = pack2<T>(p[k], p[k + 1]);
-                            r[(k - h) / 2 + 1] = pack2<T>(p[k + 2], p[k + 3]);
-                        }
-                        if (CAP) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) p[k + e] *= slack[e];
+                            if (BIAS) l2 = fma2(make_float2(fabsf(away - (float)(k + e)), fabsf(away - (float)(k + e + 1))), both(-slope), l2);
+                            v = fma2(v, both(c), l2);
+                            v = make_float2(fast_exp2(v.x), fast_exp2(v.y));
+                            if (decltype(some)::value && (k + e >= hi || (KEYS && k + e < lo))) v.x = 0.f;
+                            if (decltype(some)::value && (k + e + 1 >= hi || (KEYS && k + e + 1 < lo))) v.y = 0.f;
+                            if (KEYS) r[(k + e - h) / 2] = pack2<T>(v.x, v.y);
+                            if (CAP) v = mul2(v, slack);
+                            p[k + e] = v.x;
+                            p[k + e + 1] = v.y;
                         }
                     }
                     // over the scores that this thread has read
@@ -394,14 +390,14 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                         float4 d4 = make_float4(delta, delta, delta, delta);
                         if (KEYS) d4 = *reinterpret_cast<const float4*>(deltas + h + k);
                         const float d[4] = {d4.x, d4.y, d4.z, d4.w};
-                        float g[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            g[e] = p[h + k + e] * (dp[k + e] - d[e]);
-                            if (decltype(some)::value && (h + k + e >= hi || (KEYS && h + k + e < lo))) g[e] = 0.f;
+                        for (int e = 0; e < 4; e += 2) {
+                            const int at = h + k + e;
+                            float2 g = mul2(make_float2(p[at], p[at + 1]), add2(make_float2(dp[k + e], dp[k + e + 1]), make_float2(d[e], d[e + 1])));
+                            if (decltype(some)::value && (at >= hi || (KEYS && at < lo))) g.x = 0.f;
+                            if (decltype(some)::value && (at + 1 >= hi || (KEYS && at + 1 < lo))) g.y = 0.f;
+                            r[(k + e) / 2] = pack2<T>(g.x, g.y);
                         }
-                        r[k / 2] = pack2<T>(g[0], g[1]);
-                        r[k / 2 + 1] = pack2<T>(g[2], g[3]);
                     }
                     tmem_st16_nowait(dp_cols + lanes + w * MY + h / 2, r);
                 }

@@ -241,16 +241,32 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 const float big = attn_max<MY>([&](int k) { return fabsf(s[k]); });
                 if (__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) {
 #pragma unroll
-                    for (int k = 0; k < MY; ++k) s[k] = near(s[k]);
+                    for (int k = 0; k < MY; k += 2) {
+                        const float2 v = near(make_float2(s[k], s[k + 1]));
+                        s[k] = v.x;
+                        s[k + 1] = v.y;
+                    }
                 } else {
 #pragma unroll
                     for (int k = 0; k < MY; ++k) s[k] = cap2 * attn_tanh(s[k] * inv_cap);
                 }
             }
             if (BIAS) {
-                const float away = (float)(row + x.lk - x.lq - j * BK - half * MY);
+                const int ahead = row0 + x.lk - x.lq - j * BK - half * MY;   // of this warp's first row, over the first column
+                const float away = (float)(ahead + lane);
+                auto bias = [&](auto of) {
 #pragma unroll
-                for (int k = 0; k < MY; ++k) s[k] = fmaf(-slope, fabsf(away - (float)k), CAP ? s[k] : s[k] * (a.scale * kLog2e));
+                    for (int k = 0; k < MY; k += 2) {
+                        const float2 b = make_float2(of(k), of(k + 1)), v = make_float2(s[k], s[k + 1]);
+                        const float2 y = CAP ? add2(v, b) : fma2(v, both(a.scale * kLog2e), b);
+                        s[k] = y.x;
+                        s[k + 1] = y.y;
+                    }
+                };
+                // (one operation less where all columns lie on one side of all rows)
+                const float sign = ahead >= MY - 1 ? slope : -slope, from = -sign * away;
+                if (ahead >= MY - 1 || ahead + 31 <= 0) bias([&](int k) { return fmaf(sign, (float)k, from); });
+                else bias([&](int k) { return -slope * fabsf(away - (float)k); });
             }
             if ((j + 1) * BK > seen_by_all) {
                 const int left = seen - j * BK - half * MY;
@@ -277,19 +293,21 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 }
             }
             const float from = m == -INFINITY ? 0.f : m;
-            float sums[4] = {0.f, 0.f, 0.f, 0.f};
+            const float2 c2 = both(c), from2 = both(-from);
+            float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int k = 0; k < MY; k += 32) {
                 uint32_t r[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const float p0 = fast_exp2(fmaf(s[k + 2 * i], c, -from)), p1 = fast_exp2(fmaf(s[k + 2 * i + 1], c, -from));
-                    sums[i % 4] += p0 + p1;
-                    r[i] = pack2<T>(p0, p1);
+                    const float2 e = RAW ? fma2(make_float2(s[k + 2 * i], s[k + 2 * i + 1]), c2, from2) : add2(make_float2(s[k + 2 * i], s[k + 2 * i + 1]), from2);
+                    const float2 p = make_float2(fast_exp2(e.x), fast_exp2(e.y));
+                    sums[i % 2] = add2(sums[i % 2], p);
+                    r[i] = pack2<T>(p.x, p.y);
                 }
                 tmem_st16_nowait(s_cols(w) + lanes + half * MY + k / 2, r);
             }
-            l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            l += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
