@@ -40,6 +40,7 @@ template <int D, int BT, bool KEYS> struct BwdTile {
     // what 227 KB hold.  (Waiting for the copies of 64 KB per tile was a third of d-queries' time with two places for each.)
     static constexpr int FIRST = D == 64 ? 4 : KEYS ? 2 : 3, SECOND = D == 64 ? 4 : 2;
     static_assert(BT == 128 || D == 64, "two CTAs' accumulators");
+    static_assert(COLS >= 2 * BT + (KEYS ? 2 : 1) * D, "scores, their gradients and the sums");
     static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2;
     static constexpr int STATS = KEYS ? BT * 8 : 0;      // lse and delta of a streamed tile's queries
     static constexpr int SMEM = 2 * KEPT + (FIRST + SECOND) * TILE + FIRST * STATS + (KEYS ? 0 : 2 * kAttnRows * 4) + 256 + 1024;
@@ -488,11 +489,11 @@ cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnO
     P.lse2 = static_cast<float*>(ws);
     P.delta = P.lse2 + (size_t)a.heads * a.n_q;
     const int64_t dense = (int64_t)a.heads * a.dim;
-    // Small tiles, two CTAs per SM, unless capped scores, whose arithmetic bounds them, are many (us for d-queries and d-keys,
-    // 16 heads of 64: 16 texts of 512 39 and 42, with the large ones 45 and 52; 64 of 128 44 and 48, 60 and 68; one of 8192,
-    // causal, 277 and 344, 310 and 379; but 4 of 2048, causal, capped and biased, 100 and 117, 85 and 97).  Lengths are on the
-    // device, but their mean is known.
-    const int bt = a.dim <= 64 && (a.cap == 0.f || a.n_q <= 256 * (int64_t)a.n_texts) ? 64 : 128;
+    // Small tiles, two CTAs per SM, unless capped scores, whose arithmetic weighs more, are many (us for d-queries and d-keys,
+    // 16 heads of 64: 16 texts of 512 39 and 42, with the large ones 45 and 52, capped 56 and 56, 60 and 66; one of 8192,
+    // causal, 277 and 344, 310 and 379; but 4 of 2048, causal and capped, 86 and 99, 76 and 88).  Lengths are on the device, but
+    // their mean is known.
+    const int bt = a.dim <= 64 && (a.cap == 0.f || a.n_q <= 512 * (int64_t)a.n_texts) ? 64 : 128;
     auto query_maps = [&](CUtensorMap* m, int rows) {
         return attn_map(&m[0], op.q, op.dtype, a.dim, a.heads, a.n_q, op.q_stride, rows) &&
                attn_map(&m[1], dout, op.dtype, a.dim, a.heads, a.n_q, dense, rows);

@@ -40,6 +40,7 @@ template <int D, int NW> struct FwdTile {
     static constexpr int SHARED = HALVES == 1 ? 0 : 2 * NW * HALVES * kAttnRows * 4;
     static constexpr int SMEM = NW * Q_BYTES + STAGES * KV_BYTES + SHARED + 256 + 1024;
     static constexpr int COLS = NW * (BK + D);           // of tensor memory: a score tile and an output for each tile of queries
+    static_assert((COLS & (COLS - 1)) == 0 && COLS * CTAS <= 512, "tensor memory is had in powers of two");
 };
 
 struct alignas(64) FwdParams {
