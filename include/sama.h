@@ -360,9 +360,10 @@ typedef struct sama_attn_t {
  *   dP = d_out . v,  dX = softmax * (dP - d_out . out) * (1 - tanh^2),  dq = scale * dX k,  dk = scale * dX^T q,
  *   dv = softmax^T d_out
  * dk and dv are summed over the heads that share them.  Sums are fp32, in a fixed order (bitwise reproducible).  dX and the
- * softmax are rounded to `dtype` as operands of the last products, and d_out . out takes out as it was stored: against sums of
- * unrounded values the gradients' relative error grows from 0.0017 to 0.0025 .. 0.003 in bf16, 0.0002 to 0.00035 .. 0.0004 in
- * fp16 (out's to 0.0018 .. 0.0022, 0.0003).  slopes get no gradient.  Uses 8 * heads * n_q bytes of
+ * softmax are rounded to `dtype` as operands of the last products: against sums of unrounded values the gradients' relative
+ * error grows from 0.0017 to 0.0024 in bf16, 0.0002 to 0.0003 in fp16 (out's to 0.0018 .. 0.0022, 0.0003).  For dq, d_out . out
+ * takes out as it was stored (dq's error: up to 0.0034, 0.0004, where a few keys have most of the weight); for dk it is
+ * put right by the sum of softmax * (dP - d_out . out).  slopes get no gradient.  Uses 8 * heads * n_q bytes of
  * the workspace. */
 int sama_attention(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, void* out,
                    float* lse_out, void* stream);

@@ -16,9 +16,13 @@
 // 200 cycles, since it can run ahead of them by a product or two only.)  Heads of up to 64 columns have tiles of 64 rows
 // and two CTAs per SM, which overlap each other.
 //
-// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 1010, d-keys
-// 1160, 620 TFLOP/s of the five products that the definition needs, 870 of the seven: forming P and dX (13 instructions per
-// score with a cap, 8 without) between products that wait for them.  48 texts of up to 512, 16 heads of 64: 139 and 150.
+// delta comes from out as the forward pass rounded it; d-queries adds up what it is off by, so that d-keys has it exactly.
+//
+// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 950, d-keys
+// 1140 (without a cap 700 and 880), 660 TFLOP/s of the five products that the definition needs, 920 of the seven: forming P
+// and dX between products that wait for them; tensor cores are busy 45 % of the time, as are the issue slots, although the
+// arithmetic is done two scores per instruction (one: 1010 and 1160).  48 texts of up to 512, 16 heads of 64, biased: 137
+// and 143, the start and end of CTAs that have five tiles each and the latency of a tile's way.
 //
 // Roles of the warps: warp 0 copies, warp 1 issues products, the other 16 (or 8) form P and dX: several share 32 rows, each
 // of them has 32 of a tile's columns.  Every wait is bounded.
@@ -264,6 +268,9 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         bool ok = true;
 
         float lse2 = 0.f, delta = 0.f;   // (both negated)
+        // sum P (dP - delta), which is what delta is off by for out's rounding.  dQ's own part in it, off sum P K, would take
+        // another product and is left (a relative 0.002 of dQ in bf16, beside as much by the roundings of dX and dQ).
+        float2 off[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         if (!KEYS) {
             // two of the warps that share these rows add up half of the columns each
             volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (halves - raw));
@@ -290,10 +297,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             if (w < 2) part[w * kAttnRows + quarter * 32 + lane] = sum;
             asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
             delta = -part[quarter * 32 + lane] - part[kAttnRows + quarter * 32 + lane];
-            if (w == 0 && real) {
-                P.lse2[(int64_t)head0 * a.n_q + x.q0 + row] = lse2;
-                P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta;
-            }
+            if (w == 0 && real) P.lse2[(int64_t)head0 * a.n_q + x.q0 + row] = lse2;
         }
         // d-queries: the row sees keys below `edge`; d-keys: the row is seen by queries from `edge` on
         const int edge = KEYS ? attn_first_query(a, x, row) : attn_seen(a, x, row);
@@ -320,7 +324,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             const bool masked = KEYS ? at < edge_of_all || at + MY > x.lq : at + MY > edge_of_all;
             const int lo = KEYS ? edge - at : 0, hi = KEYS ? x.lq - at : edge - at;   // visible columns
             const float away = BIAS ? (float)(KEYS ? row - (x.lk - x.lq) - at : row + x.lk - x.lq - at) : 0.f;
-            float p[MY];   // the weights, in the end times 1 - tanh^2
+            float p[MY];   // the weights, d-keys': in the end times 1 - tanh^2
+            float slack_of[CAP && !KEYS ? MY : 1];
 #pragma unroll
             for (int k = 0; k < MY; k += 32) tmem_ld32_nowait(s_cols + lanes + w * MY + k, p + k);
             tmem_wait_ld();
@@ -352,7 +357,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                             if (decltype(some)::value && (k + e >= hi || (KEYS && k + e < lo))) v.x = 0.f;
                             if (decltype(some)::value && (k + e + 1 >= hi || (KEYS && k + e + 1 < lo))) v.y = 0.f;
                             if (KEYS) r[(k + e - h) / 2] = pack2<T>(v.x, v.y);
-                            if (CAP) v = mul2(v, slack);
+                            if (CAP && KEYS) v = mul2(v, slack);
+                            if (CAP && !KEYS) { slack_of[k + e] = slack.x; slack_of[k + e + 1] = slack.y; }
                             p[k + e] = v.x;
                             p[k + e + 1] = v.y;
                         }
@@ -382,12 +388,16 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             auto slopes_of_scores = [&](auto some) {
 #pragma unroll
                 for (int h = 0; h < MY; h += 32) {
+                    constexpr int PIECE = CAP && !KEYS ? 16 : 32;   // (16: what registers hold beside the slacks)
                     float dp[32];
                     uint32_t r[16];
-                    tmem_ld32_nowait(dp_cols + lanes + w * MY + h, dp);
-                    tmem_wait_ld();
 #pragma unroll
                     for (int k = 0; k < 32; k += 4) {
+                        if (k % PIECE == 0) {
+                            if (PIECE == 16) tmem_ld16_nowait(dp_cols + lanes + w * MY + h + k, reinterpret_cast<uint32_t*>(dp) + k);
+                            else tmem_ld32_nowait(dp_cols + lanes + w * MY + h, dp);
+                            tmem_wait_ld();
+                        }
                         float4 d4 = make_float4(delta, delta, delta, delta);
                         if (KEYS) d4 = *reinterpret_cast<const float4*>(deltas + h + k);
                         const float d[4] = {d4.x, d4.y, d4.z, d4.w};
@@ -397,6 +407,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                             float2 g = mul2(make_float2(p[at], p[at + 1]), add2(make_float2(dp[k + e], dp[k + e + 1]), make_float2(d[e], d[e + 1])));
                             if (decltype(some)::value && (at >= hi || (KEYS && at < lo))) g.x = 0.f;
                             if (decltype(some)::value && (at + 1 >= hi || (KEYS && at + 1 < lo))) g.y = 0.f;
+                            if (!KEYS) off[e / 2] = add2(off[e / 2], g);
+                            if (CAP && !KEYS) g = mul2(g, make_float2(slack_of[at], slack_of[at + 1]));
                             r[(k + e) / 2] = pack2<T>(g.x, g.y);
                         }
                     }
@@ -419,6 +431,17 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             }
         }
         if (ok && n > 0) ok = wait(done_bar, 0);
+        if (!KEYS) {
+            // d-keys gets the exact delta.  (The kept operands' place is free now.)
+            volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (base - raw)) + quarter * 32 + lane;
+            part[w * kAttnRows] = (off[0].x + off[0].y) + (off[1].x + off[1].y);
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
+            if (w == 0 && real) {
+#pragma unroll
+                for (int i = 0; i < FORMING / 4; ++i) delta -= part[i * kAttnRows];
+                P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta;
+            }
+        }
         if (ok) {
             tc_fence_after();
             // 32 columns at a time: d-keys' warps have dK or dV

@@ -11,11 +11,12 @@
 // refer to.
 //
 // What bounds it (one B200, bf16): the chain from a tile's scores to its weights and their products; one text of 8192, 32
-// heads of 128 over 8, causal: 484 us, 1130 TFLOP/s of the pairs that are seen (0.69 of the measured rate), 745 with a cap;
-// 48 texts of up to 512, 16 heads of 64: 94, where ragged tiles and the start and end of short CTAs weigh as much.  Tensor
-// cores, special-function units and issue slots are each in use for 50 to 57 % of the time (two prompts' next 1000 tokens
-// behind 7000, 250 us, a third of it the last round of CTAs).  Exponentials by a polynomial for a quarter of the scores, and
-// rounding to bf16 by integer addition, were slower (275, 254): more instructions in the chain.
+// heads of 128 over 8, causal: 469 us, 1170 TFLOP/s of the pairs that are seen (0.72 of the measured rate), 650 with a cap;
+// 48 texts of up to 512, 16 heads of 64, biased: 90, where ragged tiles and the start and end of short CTAs weigh as much.
+// Two prompts' next 1000 tokens behind 7000: 250 us; tensor cores and special-function units are in use for 57 % of the time,
+// issue slots for 31, and 512 CTAs fill 296 places less than twice.  Exponentials by a polynomial for a quarter of the scores,
+// and rounding to bf16 by integer addition, were slower (275, 254): more instructions in the chain.  For heads of 64, four
+// CTAs per SM (spilled registers, 102 us for 90) and two warps per 32 rows (97) were slower.
 //
 // Roles of the warps: warp 0 copies (TMA, 128-byte swizzle), warp 1 issues products, the others the softmax.  Every wait is
 // bounded: one that expires raises SAMA_DEV_TIMEOUT and ends the CTA's work.
