@@ -193,6 +193,30 @@ __device__ __forceinline__ void tmem_st16_nowait(uint32_t taddr, const uint32_t*
         ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
           "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr));
 }
+// 32 lanes' rows of a tile in shared memory, 16 bytes at a time: a lane writes its own row (`mine`, in the tile) from column
+// `col`, 8 values.  Swizzled: the lanes of a warp write to different banks, here and where whole rows are read.
+template <int D>
+__device__ __forceinline__ uint32_t attn_chunk(uint32_t tile, int row, int chunk) { return tile + (uint32_t)row * (D * 2) + (uint32_t)((chunk ^ (row & 7)) << 4); }
+template <typename T, int D>
+__device__ __forceinline__ void attn_stage(uint32_t tile, int mine, int col, const float* v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(attn_chunk<D>(tile, mine, col / 8)), "r"(pack2<T>(v[0], v[1])),
+                 "r"(pack2<T>(v[2], v[3])), "r"(pack2<T>(v[4], v[5])), "r"(pack2<T>(v[6], v[7])) : "memory");
+}
+// The tile's first `rows` rows go to memory, rows `ld` elements apart, by warps of which this is `warp`: a row's columns by
+// lanes next to one another.  (With each lane storing its own row, 2 KB from the next, the stores of an encoder's dK and dV
+// took 3500 of a CTA's 28,000 cycles.)
+template <typename T, int D, int WARPS>
+__device__ __forceinline__ void attn_unstage(uint32_t tile, int rows, int dim, T* to, int64_t ld, int warp) {
+    constexpr int LANES = D / 8, AT_ONCE = 32 / LANES, EACH = kAttnRows / WARPS;
+    const int chunk = (int)(threadIdx.x & 31) % LANES, r0 = warp * EACH + (int)(threadIdx.x & 31) / LANES;
+#pragma unroll
+    for (int i = 0; i < EACH; i += AT_ONCE) {
+        const int r = r0 + i;
+        uint4 v;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(attn_chunk<D>(tile, r, chunk)) : "memory");
+        if (r < rows && 8 * chunk < dim) *reinterpret_cast<uint4*>(to + r * ld + 8 * chunk) = v;
+    }
+}
 // Rows [from, rows) of a tile of COLS 64-column blocks become zeros: rows of another text, whose values must not meet
 // weights of 0 in a product.
 // Shared out among `warps` warps, of which this is `warp`.

@@ -47,7 +47,7 @@ template <int D, int BT, bool KEYS> struct BwdTile {
     static_assert(COLS >= 2 * BT + (KEYS ? 2 : 1) * D, "scores, their gradients and the sums");
     static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2;
     static constexpr int STATS = KEYS ? BT * 8 : 0;      // lse and delta of a streamed tile's queries
-    static constexpr int SMEM = 2 * KEPT + (FIRST + SECOND) * TILE + FIRST * STATS + (KEYS ? 0 : 2 * kAttnRows * 4) + 256 + 1024;
+    static constexpr int SMEM = 2 * KEPT + (FIRST + SECOND) * TILE + FIRST * STATS + (KEYS ? 0 : kAttnRows * 4) + 256 + 1024;
 };
 
 struct alignas(64) BwdParams {
@@ -98,8 +98,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
-    const uint32_t ring1 = base + 2 * C::KEPT, ring2 = ring1 + N1 * C::TILE, stats = ring2 + N2 * C::TILE, halves = stats + N1 * C::STATS;
-    const uint32_t bars = halves + (KEYS ? 0 : 2 * kAttnRows * 4);
+    const uint32_t ring1 = base + 2 * C::KEPT, ring2 = ring1 + N1 * C::TILE, stats = ring2 + N2 * C::TILE, sums = stats + N1 * C::STATS;
+    const uint32_t bars = sums + (KEYS ? 0 : kAttnRows * 4);
     auto full1 = [&](int s) { return bars + 8u * s; };
     auto empty1 = [&](int s) { return bars + 8u * (N1 + s); };
     auto full2 = [&](int s) { return bars + 8u * (2 * N1 + s); };
@@ -272,31 +272,41 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         // another product and is left (a relative 0.002 of dQ in bf16, beside as much by the roundings of dX and dQ).
         float2 off[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         if (!KEYS) {
-            // two of the warps that share these rows add up half of the columns each
-            volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (halves - raw));
-            float sum = 0.f;
-            if (real && w < 2) {
-                const int64_t at = ((int64_t)(x.q0 + row) * a.heads + head0) * a.dim;
-                const T *o = static_cast<const T*>(P.out) + at, *d = static_cast<const T*>(P.dout) + at;
+            // each warp takes some rows, whose columns are added up by lanes next to one another (with a row per lane, the way
+            // to delta took 6500 of a CTA's 17,000 cycles for texts of a few hundred tokens)
+            volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (sums - raw));
+            constexpr int LANES = D / 8, AT_ONCE = 32 / LANES, EACH = kAttnRows / FORMING, N = EACH / AT_ONCE;
+            const int r0 = (warp - 2) * EACH + lane / LANES, col = lane % LANES * 8;
+            uint4 o[N], d[N];
 #pragma unroll
-                for (int k = 0; k < D / 2; k += 8) {
-                    const int col = w * (D / 2) + k;
-                    if (col < a.dim) {
-                        float u[8], v[8];
-                        load_n<T, 8, true>(o + col, u);
-                        load_n<T, 8, true>(d + col, v);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) sum = fmaf(u[e], v[e], sum);
-                    }
+            for (int i = 0; i < N; ++i) {
+                const int r = first + r0 + i * AT_ONCE;
+                o[i] = d[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (r < kept_rows && col < a.dim) {
+                    const int64_t at = ((int64_t)(x.q0 + r) * a.heads + head0) * a.dim + col;
+                    o[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(P.out) + at);
+                    d[i] = *reinterpret_cast<const uint4*>(static_cast<const T*>(P.dout) + at);
                 }
             }
             if (real) {
                 lse2 = P.lse[(int64_t)head0 * a.n_q + x.q0 + row] * -kLog2e;
                 if (lse2 == INFINITY) lse2 = -INFINITY;
             }
-            if (w < 2) part[w * kAttnRows + quarter * 32 + lane] = sum;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t u[4] = {o[i].x, o[i].y, o[i].z, o[i].w}, v[4] = {d[i].x, d[i].y, d[i].z, d[i].w};
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = unpack2<T>(u[e]), g = unpack2<T>(v[e]);
+                    sum = fmaf(f.x, g.x, fmaf(f.y, g.y, sum));
+                }
+#pragma unroll
+                for (int x = 1; x < LANES; x *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+                if (col == 0) part[r0 + i * AT_ONCE] = sum;
+            }
             asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
-            delta = -part[quarter * 32 + lane] - part[kAttnRows + quarter * 32 + lane];
+            delta = -part[quarter * 32 + lane];
             if (w == 0 && real) P.lse2[(int64_t)head0 * a.n_q + x.q0 + row] = lse2;
         }
         // d-queries: the row sees keys below `edge`; d-keys: the row is seen by queries from `edge` on
@@ -442,13 +452,14 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                 P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta;
             }
         }
+        // the kept operands' places, where all products are done (d-queries: the second's, the sums of `off` are in the first's)
+        auto stage_of = [&](int o) { return base + (KEYS ? o : 1) * C::KEPT; };
         if (ok) {
             tc_fence_after();
             // 32 columns at a time: d-keys' warps have dK or dV
             constexpr int SHARES = FORMING / 4;
             const int which = KEYS ? w % 2 : 0, k0 = 32 * (KEYS ? w / 2 : w);
             const float f = which == 0 ? a.scale : 1.f;
-            T* g = static_cast<T*>(P.grad[which]) + (int64_t)(kept_base + row) * P.ld[which] + (int64_t)head0 * a.dim;
 #pragma unroll 1
             for (int k = k0; k < D; k += 32 * (KEYS ? SHARES / 2 : SHARES)) {
                 float v[32];
@@ -459,9 +470,14 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] = n > 0 ? v[e] * f : 0.f;
 #pragma unroll
-                for (int e = 0; e < 32; e += 8)
-                    if (real && k + e < a.dim) store_n<T, 8>(g + k + e, v + e);
+                for (int e = 0; e < 32; e += 8) attn_stage<T, D>(stage_of(which), quarter * 32 + lane, k + e, v + e);
             }
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
+        if (ok) {
+            for (int o = 0; o < (KEYS ? 2 : 1); ++o)
+                attn_unstage<T, D, FORMING>(stage_of(o), kept_rows - first, a.dim, static_cast<T*>(P.grad[o]) + (int64_t)(kept_base + first) * P.ld[o] + (int64_t)head0 * a.dim,
+                                            P.ld[o], warp - 2);
         }
     }
     tc_fence_before();

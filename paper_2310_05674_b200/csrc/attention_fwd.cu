@@ -316,6 +316,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             if (lane == 0) mbar_arrive(p_bar(w));
         }
         const bool real = row < x.lq;
+        const uint32_t stage = base + w * C::Q_BYTES;   // the queries' place: their products are done
         if (n_kt[w] > 0 && ok) {
             ok = wait(o_bar(w), 0);
             tc_fence_after();
@@ -327,7 +328,6 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             const bool empty = l == 0.f;
             const float inv = 1.f / l;
             if (real && P.lse && half == 0) P.lse[(int64_t)head * a.n_q + x.q0 + row] = empty ? -INFINITY : (m + __log2f(l)) * 0.69314718f;
-            T* out = static_cast<T*>(P.out) + ((int64_t)(x.q0 + row) * a.heads + head) * a.dim;
 #pragma unroll 1
             for (int k = half * (D / HALVES); k < (half + 1) * (D / HALVES); k += 32) {
                 float o[32];
@@ -338,10 +338,14 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = empty ? 0.f : o[i] * inv;
 #pragma unroll
-                for (int i = 0; i < 32; i += 8)
-                    if (real && k + i < a.dim) store_n<T, 8>(out + k + i, o + i);
+                for (int i = 0; i < 32; i += 8) attn_stage<T, D>(stage, quarter * 32 + lane, k + i, o + i);
             }
         }
+        asm volatile("bar.sync %0, %1;" ::"r"(9 + w), "n"(128 * HALVES) : "memory");
+        const int i0 = first + w * kAttnRows;
+        if (ok && i0 < x.lq)
+            attn_unstage<T, D, 4 * HALVES>(stage, x.lq - i0, a.dim, static_cast<T*>(P.out) + ((int64_t)(x.q0 + i0) * a.heads + head) * a.dim,
+                                           (int64_t)a.heads * a.dim, (warp - 2) % (4 * HALVES));
     }
     tc_fence_before();
     __syncthreads();
