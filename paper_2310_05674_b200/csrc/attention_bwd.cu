@@ -18,11 +18,11 @@
 //
 // delta comes from out as the forward pass rounded it; d-queries adds up what it is off by, so that d-keys has it exactly.
 //
-// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 950, d-keys
-// 1140 (without a cap 700 and 880), 660 TFLOP/s of the five products that the definition needs, 920 of the seven: forming P
+// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 930, d-keys
+// 1160 (without a cap 700 and 880), 660 TFLOP/s of the five products that the definition needs, 920 of the seven: forming P
 // and dX between products that wait for them; tensor cores are busy 45 % of the time, as are the issue slots, although the
-// arithmetic is done two scores per instruction (one: 1010 and 1160).  48 texts of up to 512, 16 heads of 64, biased: 137
-// and 143, the start and end of CTAs that have five tiles each and the latency of a tile's way.
+// arithmetic is done two scores per instruction (one: 1010 and 1160).  48 texts of up to 512, 16 heads of 64, biased: 117
+// and 132, the start and end of CTAs that have three to eight tiles each and the latency of a tile's way.
 //
 // Roles of the warps: warp 0 copies, warp 1 issues products, the other 16 (or 8) form P and dX: several share 32 rows, each
 // of them has 32 of a tile's columns.  Every wait is bounded.
