@@ -535,7 +535,11 @@ def _matrix(device, x, dtype, rows, cols, where):
         _fill_dtypes()
     if x.dtype is not _torch_dtypes.get(dtype) or (x.stride(1) != 1 and cols > 1):
         raise SamaError(SAMA_ERR_PARAM, "%s: a tensor is not of the type the call names, or its columns lie apart" % where)
-    return x.data_ptr(), x.stride(0) if x.shape[0] > 1 else 0
+    if rows <= 1:
+        return x.data_ptr(), 0
+    if x.stride(0) < cols:   # (0, which the library takes as "without gaps", among them: a row that stands for many)
+        raise SamaError(SAMA_ERR_PARAM, "%s: a tensor's rows lie in one another" % where)
+    return x.data_ptr(), x.stride(0)
 
 
 def sama_distill(ctx, dtype, n_rows, vocab, logits, k, top_dtype, top_logits, top_ids, temperature, weight, grad_scale,
