@@ -380,7 +380,7 @@ typedef struct sama_paged_t {
     int64_t n_pages;                     /* pages of each cache, 1 .. 2^31 - 1 */
     int64_t page_stride;                 /* elements from a page to the next, a multiple of 8; 0: page_size * kv_heads * head_dim */
     const int32_t* page_table;           /* device [n_seqs][max_pages]; entries behind a sequence's last page are not read */
-    const int32_t* lengths;              /* device [n_seqs], 0 .. max_pages * page_size (others: SAMA_DEV_BAD_INDEX, taken as the nearest) */
+    const int32_t* lengths;              /* device [n_seqs], 0 .. max_pages * page_size, 2^31 - 64 at most (others: SAMA_DEV_BAD_INDEX, taken as the nearest) */
     const float* slopes;                 /* device [heads], or NULL */
     float scale, cap;
 } sama_paged_t;

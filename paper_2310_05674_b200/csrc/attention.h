@@ -2,6 +2,7 @@
 #pragma once
 #include <type_traits>
 
+#include "attention_sizes.h"
 #include "num_types.h"
 #include "sama_internal.h"
 #include "tc_ptx.h"

@@ -153,7 +153,7 @@ int sama_paged_attention(sama_ctx* ctx, const sama_paged_t* a, const void* q, co
         a->page_size > (1 << 20) || a->n_pages < 1 || a->n_pages > 0x7fffffff)
         return SAMA_ERR_SIZE;
     // (a CTA's steps of 64 keys are numbered in 31 bits)
-    const int64_t table = (int64_t)a->max_pages * a->page_size, longest = table < 0x7fffffff ? table : 0x7fffffff;
+    const int64_t longest = paged_most_keys(a->max_pages, a->page_size);
     if (longest * a->n_seqs > ((int64_t)1 << 44) / a->heads) return SAMA_ERR_SIZE;
     const int64_t row = (int64_t)a->kv_heads * a->head_dim, page = row * a->page_size, stride = a->page_stride ? a->page_stride : page;
     if (stride < page || stride % 8 != 0 || stride > ((int64_t)1 << 40)) return SAMA_ERR_SIZE;

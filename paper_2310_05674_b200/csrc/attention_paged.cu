@@ -22,7 +22,8 @@ namespace {
 
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int KEYS = 16;                 // of a warp's tile
-constexpr int STEP = KEYS * WARPS;       // of a CTA's step
+constexpr int STEP = kPagedStep;         // of a CTA's step
+static_assert(STEP == KEYS * WARPS, "a tile per warp");
 constexpr int ROWS = 8;                  // queries of a unit of work
 constexpr int STAGES = 3;
 constexpr int kMinSteps = 2;             // a CTA's share, at least: 128 keys
@@ -59,10 +60,7 @@ __device__ __forceinline__ void mma(float* c, uint32_t a0, uint32_t a2, uint32_t
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(0), "r"(a2), "r"(0), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ int paged_length(const PagedShape& a, int s) {
-    const int64_t most = min((int64_t)a.max_pages * a.page_size, (int64_t)0x7fffffff);
-    return (int)min(max((int64_t)a.lengths[s], (int64_t)0), most);
-}
+__device__ __forceinline__ int paged_length(const PagedShape& a, int s) { return paged_keys(a.lengths[s], a.max_pages, a.page_size); }
 
 // A place in the list of steps.
 struct Place {
@@ -91,7 +89,7 @@ paged_kernel(const PagedParams P) {
 
     // Steps of all sequences, and the sequence in which this CTA's share begins: each thread adds up a run of sequences.
     const int run = (a.n_seqs + THREADS - 1) / THREADS, s0 = min((int)threadIdx.x * run, a.n_seqs), s1 = min(s0 + run, a.n_seqs);
-    auto steps_of = [&](int s) { return (paged_length(a, s) + STEP - 1) / STEP; };
+    auto steps_of = [&](int s) { return paged_steps(paged_length(a, s)); };
     int64_t mine = 0;
     for (int s = s0; s < s1; ++s) mine += (int64_t)steps_of(s) * units;
     int64_t upto = mine;
@@ -137,7 +135,7 @@ paged_kernel(const PagedParams P) {
     Place at;   // of the next step to be worked on
     at.s = start_s;
     at.len = paged_length(a, at.s);
-    at.steps = (at.len + STEP - 1) / STEP;
+    at.steps = paged_steps(at.len);
     const int64_t inside = begin - start_before;
     at.unit = (int)(inside / at.steps);
     at.step = (int)(inside - (int64_t)at.unit * at.steps);
@@ -149,7 +147,7 @@ paged_kernel(const PagedParams P) {
         do {
             if (++p.s >= a.n_seqs) { p.steps = p.len = 0; return; }
             p.len = paged_length(a, p.s);
-            p.steps = (p.len + STEP - 1) / STEP;
+            p.steps = paged_steps(p.len);
         } while (p.steps == 0);
     };
 
@@ -499,8 +497,7 @@ cudaError_t launch_paged(sama_ctx* ctx, const PagedShape& a, int dtype, const vo
     P.parts = static_cast<float*>(ws);
     P.arrived = ctx->paged_arrived;
     // no more CTAs than there can be shares
-    const int64_t most_keys = (int64_t)a.max_pages * a.page_size < 0x7fffffff ? (int64_t)a.max_pages * a.page_size : 0x7fffffff;
-    const int64_t steps = (most_keys + STEP - 1) / STEP * a.n_seqs * a.kv_heads * ((a.group + ROWS - 1) / ROWS);
+    const int64_t steps = (int64_t)paged_steps((int)paged_most_keys(a.max_pages, a.page_size)) * a.n_seqs * a.kv_heads * ((a.group + ROWS - 1) / ROWS);
     const int64_t shares = steps / kMinSteps > 1 ? steps / kMinSteps : 1;
     const int ctas = shares < most_ctas(ctx) ? (int)shares : most_ctas(ctx);
     if (dtype == SAMA_BF16)
