@@ -19,10 +19,6 @@ struct AttnShape {
     float scale, cap;
 };
 
-struct AttnText {
-    int q0, lq, k0, lk, prefix;   // first row and number of queries and keys; prefix: keys that every query sees
-};
-
 struct AttnOperands {
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;
@@ -89,14 +85,6 @@ __device__ __forceinline__ void attn_check_starts(const AttnShape& a) {
         bad |= q < 0 || q > a.n_q || k < 0 || k > a.n_k || (i > 0 && (a.q_starts[i - 1] > q || a.k_starts[i - 1] > k));
     }
     if (bad) atomicOr(a.status, (int)SAMA_DEV_BAD_INDEX);
-}
-// Query i sees keys 0 .. result - 1: more of them, never fewer, as i grows.
-__device__ __forceinline__ int attn_seen(const AttnShape& a, const AttnText& x, int i) {
-    return a.causal ? min(max(max(x.prefix, i + x.lk - x.lq + 1), 0), x.lk) : x.lk;
-}
-// Key j is seen by queries result .. lq - 1.
-__device__ __forceinline__ int attn_first_query(const AttnShape& a, const AttnText& x, int j) {
-    return !a.causal || j < x.prefix ? 0 : max(0, j - (x.lk - x.lq));
 }
 
 // Two fp32 operations in one instruction: the scores' arithmetic takes most of the issue slots.

@@ -88,10 +88,10 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     // streamed tiles: those that the last query sees, or from the first that sees the first key on, for each head
     int tile0 = 0, per_head;
     if (KEYS) {
-        tile0 = attn_first_query(a, x, first) / BT;
+        tile0 = attn_first_query(a.causal, x, first) / BT;
         per_head = max(0, (x.lq + BT - 1) / BT - tile0);
     } else {
-        per_head = (attn_seen(a, x, min(first + kAttnRows, x.lq) - 1) + BT - 1) / BT;
+        per_head = (attn_seen(a.causal, x, min(first + kAttnRows, x.lq) - 1) + BT - 1) / BT;
     }
     const int n = per_head * (KEYS ? a.group : 1);
 
@@ -310,8 +310,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             if (w == 0 && real) P.lse2[(int64_t)head0 * a.n_q + x.q0 + row] = lse2;
         }
         // d-queries: the row sees keys below `edge`; d-keys: the row is seen by queries from `edge` on
-        const int edge = KEYS ? attn_first_query(a, x, row) : attn_seen(a, x, row);
-        const int edge_of_all = KEYS ? attn_first_query(a, x, row0 + 31) : attn_seen(a, x, row0);
+        const int edge = KEYS ? attn_first_query(a.causal, x, row) : attn_seen(a.causal, x, row);
+        const int edge_of_all = KEYS ? attn_first_query(a.causal, x, row0 + 31) : attn_seen(a.causal, x, row0);
 
         int s1 = 0, next1 = 1 % N1, parity1 = N1 == 1, next2 = 1 % N2, parity2 = N2 == 1, tile_of_head = 0, head = KEYS ? head0 * a.group : head0;
         float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
@@ -333,7 +333,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             tc_fence_after();
             const bool masked = KEYS ? at < edge_of_all || at + MY > x.lq : at + MY > edge_of_all;
             const int lo = KEYS ? edge - at : 0, hi = KEYS ? x.lq - at : edge - at;   // visible columns
-            const float away = BIAS ? (float)(KEYS ? row - (x.lk - x.lq) - at : row + x.lk - x.lq - at) : 0.f;
+            const float away = BIAS ? (float)(KEYS ? row - (x.lk - x.lq) - at : attn_position(x, row) - at) : 0.f;
             float p[MY];   // the weights, d-keys': in the end times 1 - tanh^2
             float slack_of[CAP && !KEYS ? MY : 1];
 #pragma unroll

@@ -115,7 +115,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     int n_kt[NW], n_all = 0;
     for (int w = 0; w < NW; ++w) {
         const int i0 = first + w * kAttnRows;
-        n_kt[w] = i0 < x.lq ? (attn_seen(a, x, min(i0 + kAttnRows, x.lq) - 1) + BK - 1) / BK : 0;
+        n_kt[w] = i0 < x.lq ? (attn_seen(a.causal, x, min(i0 + kAttnRows, x.lq) - 1) + BK - 1) / BK : 0;
         n_all = max(n_all, n_kt[w]);
     }
     const int items = 2 * n_all;   // keys and values in turn
@@ -215,7 +215,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
         const int w = (warp - 2) / (4 * HALVES), half = (warp - 2) / 4 % HALVES, quarter = warp & 3;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const int row0 = first + w * kAttnRows + quarter * 32, row = row0 + lane;   // in the text
-        const int seen = attn_seen(a, x, row), seen_by_all = attn_seen(a, x, row0);
+        const int seen = attn_seen(a.causal, x, row), seen_by_all = attn_seen(a.causal, x, row0);
         constexpr bool RAW = !CAP && !BIAS;     // scores as they come, the factor is applied in the exponent
         const float c = RAW ? a.scale * kLog2e : 1.f;
         const float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
@@ -254,7 +254,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 }
             }
             if (BIAS) {
-                const int ahead = row0 + x.lk - x.lq - j * BK - half * MY;   // of this warp's first row, over the first column
+                const int ahead = attn_position(x, row0) - j * BK - half * MY;   // of this warp's first row, over the first column
                 const float away = (float)(ahead + lane);
                 auto bias = [&](auto of) {
 #pragma unroll

@@ -10,6 +10,24 @@
 
 namespace sama {
 
+struct AttnText {
+    int q0, lq, k0, lk, prefix;   // first row and number of queries and keys; prefix: keys that every query sees
+};
+// The position of query i of a text, a tile's rows behind its last among them.  (i + lk might pass 31 bits.)
+SAMA_HD inline int attn_position(const AttnText& x, int i) { return i - (x.lq - x.lk); }
+// Query i sees keys 0 .. result - 1: more of them, never fewer, as i grows.
+SAMA_HD inline int attn_seen(int causal, const AttnText& x, int i) {
+    if (!causal) return x.lk;
+    const int past = attn_position(x, i) + 1, seen = past > x.prefix ? past : x.prefix;
+    return seen < 0 ? 0 : seen < x.lk ? seen : x.lk;
+}
+// Key j is seen by queries result .. lq - 1.
+SAMA_HD inline int attn_first_query(int causal, const AttnText& x, int j) {
+    if (!causal || j < x.prefix) return 0;
+    const int i = j - (x.lk - x.lq);
+    return i > 0 ? i : 0;
+}
+
 // A sequence's keys are counted in 31 bits, and worked on in steps of 64: the last step has to be countable, too.
 constexpr int kPagedStep = 64;
 constexpr int64_t kPagedMostKeys = 0x7fffffff / kPagedStep * kPagedStep;

@@ -36,3 +36,19 @@ def test_steps_of_a_paged_sequence(sizes, pages, page):
     for n, (keys, steps, last) in zip(lengths, sizes(["paged %d %d %d" % (n, pages, page) for n in lengths])):
         assert keys == max(0, min(n, most)), n
         assert steps == -(-keys // 64) and last == 64 * steps - 1, n
+
+
+@pytest.mark.parametrize("lq,lk", [(1, 1), (5, 5), (3, 9), (9, 3), (0, 4), (4, 0), (2 ** 30, 2 ** 30), (2 ** 30, 0), (0, 2 ** 30), (1, 2 ** 30),
+                                   (2 ** 30, 1), (2 ** 30, 2 ** 30 - 5)])
+def test_what_a_query_sees(sizes, lq, lk):
+    """At a text's ends, and for the rows of its last tile that lie behind it (up to 255 of queries, 127 of keys)."""
+    ends = {0, 1, 2, 5, lq - 1, lq, lq + 255, lk - 1, lk, lk + 127}
+    for causal in (0, 1):
+        for prefix in sorted({0, min(2, lk), lk}):
+            def ask(what, rows):
+                return zip(rows, sizes(["%s %d %d %d %d %d" % (what, causal, lq, lk, prefix, i) for i in rows]))
+            for i, (at, seen) in ask("query", sorted(i for i in ends if 0 <= i < lq + 256)):
+                assert at == i + lk - lq
+                assert seen == (max(0, min(lk, max(prefix, at + 1))) if causal else lk), (causal, prefix, i)
+            for i, (first,) in ask("key", sorted(i for i in ends if 0 <= i < lk + 128)):
+                assert first == (0 if not causal or i < prefix else max(0, i - (lk - lq))), (causal, prefix, i)
