@@ -608,6 +608,10 @@ distill_few_kernel(const DistillParams P) {
                 for (int e = t; e < P.vocab; e += 32) reinterpret_cast<T*>(g_row)[e] = reinterpret_cast<const T*>(chunk)[e + s.head / SIZE];
                 __syncwarp();
             }
+        } else {
+            // (the next copy into this place comes after the stores of the row's ends)
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
         }
         if (t == 0) asm volatile("cp.async.bulk.commit_group;\n\tcp.async.bulk.wait_group.read 1;" ::: "memory");
         // the row after the next takes the place of the one before this, whose gradient has left it

@@ -78,3 +78,24 @@ def test_other_rows_are_handed_on(distill):
     # a single row has no stride, whatever the tensor says of it
     assert distill(1, 1000, z=(0, 1), grad=(0, 1)) == (0, 0)
     assert distill(1, 1000, z=Matrix((4, 1000), distill.bf, (0, 1)), ld=2000) == (2000, 0)
+
+
+def test_a_ring_place_is_fenced_whatever_is_asked_for():
+    """Rows that a warp each works on: what a thread has stored into a place of the ring (a row's ends) has to be ordered before
+    the copy that takes the place next, for losses alone, too: once per row, after the stores, before that copy."""
+    import os
+    import re
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2310_05674_b200", "csrc", "distill.cu")
+    text = re.sub(r"//[^\n]*", "", open(path).read())
+    kernel = text[text.index("distill_few_kernel(const DistillParams P)"):text.index("distill_long_kernel(const DistillParams P)")]
+    loop = kernel[kernel.index("[place] = edge"):kernel.index("fetch_row(after")]
+    at = loop.index("if (P.grad) {")
+    depth, end = 0, at
+    for end in range(at, len(loop)):
+        depth += {"{": 1, "}": -1}.get(loop[end], 0)
+        if depth == 0 and loop[end] == "}":
+            break
+    with_gradient, without = loop[at:end], loop[:at] + loop[end:]
+    assert "fence.proxy.async" in without
+    last = max(m.start() for m in re.finditer(r"(chunk\)\[[^=]*\] = |store_n<)", with_gradient))
+    assert "fence.proxy.async" in with_gradient[last:] or "fence.proxy.async" in loop[end:]
