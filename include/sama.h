@@ -361,9 +361,9 @@ typedef struct sama_attn_t {
  *   dv = softmax^T d_out
  * dk and dv are summed over the heads that share them.  Sums are fp32, in a fixed order (bitwise reproducible).  dX and the
  * softmax are rounded to `dtype` as operands of the last products: against sums of unrounded values the gradients' relative
- * error grows from 0.0017 to 0.0024 in bf16, 0.0002 to 0.0003 in fp16 (out's to 0.0018 .. 0.0022, 0.0003).  For dq, d_out . out
- * takes out as it was stored (dq's error: up to 0.0034, 0.0004, where a few keys have most of the weight); for dk it is
- * put right by the sum of softmax * (dP - d_out . out).  slopes get no gradient.  Uses 8 * heads * n_q bytes of
+ * error grows from 0.0017 to 0.0024 in bf16, 0.0002 to 0.0003 in fp16 (out's to 0.0018 .. 0.0022, 0.0003).  d_out . out is
+ * put right for out's rounding by the sum of softmax * (dP - d_out . out).  Keys with a common offset have dq's error grow as
+ * their size does, which dq itself does not (0.007 in bf16, 0.0009 in fp16 where the offset is four times their spread).  slopes get no gradient.  Uses 8 * heads * n_q bytes of
  * the workspace. */
 int sama_attention(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, void* out,
                    float* lse_out, void* stream);

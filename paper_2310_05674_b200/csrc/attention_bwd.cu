@@ -7,21 +7,23 @@
 // head that shares it.  The products are formed with the kept rows as the lanes of tensor memory (S^T rather than S for
 // the keys), so that P and dX go back to tensor memory as the left operands of the last products and no tile is
 // transposed.  The sums of a row stay in one accumulator from its first tile to its last: no atomics, a fixed order.
-// Forming S and dP in both launches costs seven products in place of the five of one launch that adds to dQ in memory.
+// Forming S and dP in both launches costs seven products in place of the five of one launch that adds to dQ in memory; an
+// eighth, P K, puts right what out's rounding does to dQ.
 //
 // The order of the products of tile i is  dP_i, dV (from P_i), S_i+1, dK (from dX_i), dP_i+1, ...:  P_i+1 is formed from
-// S_i+1 while dK and dP_i+1 run, dX_i from dP_i while dV and S_i+1 run.  S, dP and two accumulators of 128 columns fill tensor
-// memory.  (Tiles of 64 rows in two buffers, which the two halves of the warps took in turn, were slower, 1452 for 1148 us:
+// S_i+1 while dK and dP_i+1 run, dX_i from dP_i while dV and S_i+1 run.  (d-queries: P K in dV's place, dQ in dK's.)  S, dP and
+// two accumulators of 128 columns fill tensor memory.  (Tiles of 64 rows in two buffers, which the two halves of the warps took in turn, were slower, 1452 for 1148 us:
 // a product 64 wide takes 48 cycles in place of 32, and each wait of the issuing thread leaves the tensor cores idle for some
 // 200 cycles, since it can run ahead of them by a product or two only.)  Heads of up to 64 columns have tiles of 64 rows
 // and two CTAs per SM, which overlap each other.
 //
-// delta comes from out as the forward pass rounded it; d-queries adds up what it is off by, so that d-keys has it exactly.
+// delta comes from out as the forward pass rounded it; d-queries adds up what it is off by, puts dQ right, and hands d-keys
+// the exact one.
 //
-// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 930, d-keys
-// 1160 (without a cap 700 and 880), 660 TFLOP/s of the five products that the definition needs, 920 of the seven: forming P
+// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 1050, d-keys
+// 1115, 635 TFLOP/s of the five products that the definition needs, 1015 of the eight: forming P
 // and dX between products that wait for them; tensor cores are busy 45 % of the time, as are the issue slots, although the
-// arithmetic is done two scores per instruction (one: 1010 and 1160).  48 texts of up to 512, 16 heads of 64, biased: 117
+// arithmetic is done two scores per instruction (one: 1010 and 1160).  48 texts of up to 512, 16 heads of 64, biased: 123
 // and 132, the start and end of CTAs that have three to eight tiles each and the latency of a tile's way.
 //
 // Roles of the warps: warp 0 copies, warp 1 issues products, the other 16 (or 8) form P and dX: several share 32 rows, each
@@ -44,7 +46,7 @@ template <int D, int BT, bool KEYS> struct BwdTile {
     // what 227 KB hold.  (Waiting for the copies of 64 KB per tile was a third of d-queries' time with two places for each.)
     static constexpr int FIRST = D == 64 ? 4 : KEYS ? 2 : 3, SECOND = D == 64 ? 4 : 2;
     static_assert(BT == 128 || D == 64, "two CTAs' accumulators");
-    static_assert(COLS >= 2 * BT + (KEYS ? 2 : 1) * D, "scores, their gradients and the sums");
+    static_assert(COLS >= 2 * BT + 2 * D, "scores, their gradients and the sums");
     static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2;
     static constexpr int STATS = KEYS ? BT * 8 : 0;      // lse and delta of a streamed tile's queries
     static constexpr int SMEM = 2 * KEPT + (FIRST + SECOND) * TILE + FIRST * STATS + (KEYS ? 0 : kAttnRows * 4) + 256 + 1024;
@@ -105,7 +107,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     auto full2 = [&](int s) { return bars + 8u * (2 * N1 + s); };
     auto empty2 = [&](int s) { return bars + 8u * (2 * N1 + N2 + s); };
     const uint32_t s_bar = bars + 8u * (2 * N1 + 2 * N2), dp_bar = s_bar + 8u;   // S, dP are there
-    const uint32_t p_bar = dp_bar + 8u, x_bar = p_bar + 8u;                 // S may be overwritten and (d-keys) P is there; dX is there
+    const uint32_t p_bar = dp_bar + 8u, x_bar = p_bar + 8u;                 // P is there, over S; dX is there, over dP
     const uint32_t kept_bar = x_bar + 8u, done_bar = kept_bar + 8u;
     const uint32_t tmem_slot = done_bar + 8u;
     volatile uint32_t* tmem_ptr_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_slot - raw));
@@ -206,10 +208,10 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             }
             umma_commit(o ? dp_bar : s_bar);
         };
-        // dK or dQ (o = 0) from dX, dV (o = 1) from P.  Each warp has left its columns, in 16 bits, in the first half of
-        // its columns of fp32.
+        // dK or dQ (o = 0) from dX, dV or d-queries' sum of P K (o = 1) from P.  Each warp has left its columns, in 16 bits, in
+        // the first half of its columns of fp32.
         auto gradient = [&](int o, int s, bool add) {
-            const uint64_t db = attn_desc_mn((o ? ring2 : ring1) + s * C::TILE, BT);
+            const uint64_t db = attn_desc_mn((o && KEYS ? ring2 : ring1) + s * C::TILE, BT);
 #pragma unroll
             for (int k = 0; k < BT / 16; ++k)
                 umma16_ta(g_cols(o), (o ? s_cols : dp_cols) + (uint32_t)(k / (MY / 16) * MY + k % (MY / 16) * 8), db + (uint64_t)(k * 2048 >> 4), IDESC_G, add || k > 0);
@@ -232,10 +234,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             if (!(ok = wait(p_bar, i & 1))) break;
             tc_fence_after();
             if (elect_one()) {
-                if (KEYS) {
-                    gradient(1, s2, i > 0);
-                    if (i + N2 < n) umma_commit(empty2(s2));
-                }
+                gradient(1, KEYS ? s2 : s1, i > 0);
+                if (KEYS && i + N2 < n) umma_commit(empty2(s2));
                 // (products are executed in order: the next scores do not overtake the weights they replace)
                 if (i + 1 < n) scores(0, next1);
             }
@@ -268,8 +268,10 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         bool ok = true;
 
         float lse2 = 0.f, delta = 0.f;   // (both negated)
-        // sum P (dP - delta), which is what delta is off by for out's rounding.  dQ's own part in it, off sum P K, would take
-        // another product and is left (a relative 0.002 of dQ in bf16, beside as much by the roundings of dX and dQ).
+        // sum P (dP - delta), which is what delta is off by for out's rounding: it is put right in dQ by off sum P (1 - tanh^2) K,
+        // which takes a product of its own, and in delta for d-keys.  (Without that, keys and values with a common offset of
+        // their spread have dQ off by 0.01 to 0.02 in bf16, of four times that by a third: dQ does not grow with the offset,
+        // out's rounding and the sum of P K do.)
         float2 off[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         if (!KEYS) {
             // each warp takes some rows, whose columns are added up by lanes next to one another (with a row per lane, the way
@@ -339,12 +341,6 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
 #pragma unroll
             for (int k = 0; k < MY; k += 32) tmem_ld32_nowait(s_cols + lanes + w * MY + k, p + k);
             tmem_wait_ld();
-            if (!KEYS) {
-                tc_fence_before();
-                if (!(ok = ready(0, i))) break;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_bar);
-            }
             auto weights = [&](auto near, auto some) {   // (some: scores are masked)
 #pragma unroll
                 for (int h = 0; h < MY; h += 32) {
@@ -366,15 +362,16 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                             v = make_float2(fast_exp2(v.x), fast_exp2(v.y));
                             if (decltype(some)::value && (k + e >= hi || (KEYS && k + e < lo))) v.x = 0.f;
                             if (decltype(some)::value && (k + e + 1 >= hi || (KEYS && k + e + 1 < lo))) v.y = 0.f;
-                            if (KEYS) r[(k + e - h) / 2] = pack2<T>(v.x, v.y);
-                            if (CAP && KEYS) v = mul2(v, slack);
+                            const float2 flat = CAP ? mul2(v, slack) : v, operand = KEYS ? v : flat;
+                            r[(k + e - h) / 2] = pack2<T>(operand.x, operand.y);
+                            if (KEYS) v = flat;
                             if (CAP && !KEYS) { slack_of[k + e] = slack.x; slack_of[k + e + 1] = slack.y; }
                             p[k + e] = v.x;
                             p[k + e + 1] = v.y;
                         }
                     }
                     // over the scores that this thread has read
-                    if (KEYS) tmem_st16_nowait(s_cols + lanes + w * MY + h / 2, r);
+                    tmem_st16_nowait(s_cols + lanes + w * MY + h / 2, r);
                 }
             };
             if (CAP) {
@@ -386,13 +383,11 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             } else {
                 weights(std::false_type(), std::false_type());
             }
-            if (KEYS) {
-                tmem_wait_st();
-                tc_fence_before();
-                if (!(ok = ready(0, i))) break;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(p_bar);
-            }
+            tmem_wait_st();
+            tc_fence_before();
+            if (!(ok = ready(0, i))) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_bar);
             if (!(ok = wait(dp_bar, i & 1))) break;
             tc_fence_after();
             auto slopes_of_scores = [&](auto some) {
@@ -441,16 +436,15 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             }
         }
         if (ok && n > 0) ok = wait(done_bar, 0);
+        float shift = 0.f;   // this row's, of all its warps
         if (!KEYS) {
             // d-keys gets the exact delta.  (The kept operands' place is free now.)
             volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (base - raw)) + quarter * 32 + lane;
             part[w * kAttnRows] = (off[0].x + off[0].y) + (off[1].x + off[1].y);
             asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
-            if (w == 0 && real) {
 #pragma unroll
-                for (int i = 0; i < FORMING / 4; ++i) delta -= part[i * kAttnRows];
-                P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta;
-            }
+            for (int i = 0; i < FORMING / 4; ++i) shift += part[i * kAttnRows];
+            if (w == 0 && real) P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta - shift;
         }
         // the kept operands' places, where all products are done (d-queries: the second's, the sums of `off` are in the first's)
         auto stage_of = [&](int o) { return base + (KEYS ? o : 1) * C::KEPT; };
@@ -466,6 +460,13 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                 if (n > 0) {
                     tmem_ld32_nowait(g_cols(which) + lanes + k, v);
                     tmem_wait_ld();
+                    if (!KEYS) {
+                        float pk[32];
+                        tmem_ld32_nowait(g_cols(1) + lanes + k, pk);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = fmaf(-shift, pk[e], v[e]);
+                    }
                 }
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] = n > 0 ? v[e] * f : 0.f;
