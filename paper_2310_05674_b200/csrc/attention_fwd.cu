@@ -277,9 +277,11 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             }
             float top = attn_max<MY>([&](int k) { return s[k]; }) * c;
             if (HALVES == 2) top = fmaxf(top, exchange(top, j & 1));
-            if (__any_sync(0xffffffffu, top > m + kRaise || (m == -INFINITY && top > m))) {
-                const float raised = fmaxf(m, top);
-                const float factor = raised == -INFINITY ? 1.f : fast_exp2(m - raised);
+            // (a row's own scores decide: others of its warp may be another text's)
+            const bool raise = top > m + kRaise || (m == -INFINITY && top > m);
+            if (__any_sync(0xffffffffu, raise)) {
+                const float raised = raise ? top : m;
+                const float factor = raise ? fast_exp2(m - raised) : 1.f;
                 m = raised;
                 l *= factor;
                 if (j > 0) {
