@@ -109,24 +109,30 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
 }
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
-// tanh(z) = 1 - 2 / (1 + exp 2z): an absolute error of two units in the last place of 1, which is what a capped score
-// needs (the hardware's own approximation has 2^-11, a hundredth of a weight at a cap of 30).  That takes two of the three
-// results of the special-function unit per score (16 a cycle and SM), so where no score of a warp's tile is beyond 0.75 caps
-// tanh is a polynomial, z p(z^2) with p of degree 4 through tanh(z) / z at the Chebyshev points of [0, 0.75^2]: 1.3e-7.
+// tanh(z) = 1 - 2 / (1 + exp 2z) has an absolute error of two units in the last place of 1 (the hardware's own approximation
+// 2^-11, a hundredth of a weight at a cap of 30), which is a relative one of 2.5e-7 beyond 0.75.  Below, tanh is a polynomial,
+// z p(z^2) with p of degree 4 through tanh(z) / z at the Chebyshev points of [0, 0.75^2]: 7e-7 of tanh(z).  The first takes two of
+// the three results of the special-function unit per score (16 a cycle and SM), so it is left out where all scores of a
+// warp's tile are within 0.75 caps (and, in the backward pass, seen).
 __device__ __forceinline__ float attn_tanh(float z) { return fmaf(-2.f, fast_rcp(1.f + fast_exp2(2.f * kLog2e * z)), 1.f); }
 constexpr float kTanhNear = 0.75f;
+enum { kNear, kFar };
 struct AttnTanh {   // times `factor`, of `scale` times its argument
-    float k[5];
-    __device__ __forceinline__ AttnTanh(float scale, float factor) {
+    float k[5], scale, factor;
+    __device__ __forceinline__ AttnTanh(float scale, float factor) : scale(scale), factor(factor) {
         const float c[5] = {0.999999404f, -0.333281934f, 0.132584617f, -0.0500416085f, 0.0129166516f}, s2 = scale * scale;
         float f = factor * scale;
 #pragma unroll
         for (int i = 0; i < 5; ++i) { k[i] = c[i] * f; f *= s2; }
     }
-    __device__ __forceinline__ float2 operator()(float2 x) const {
+    __device__ __forceinline__ bool is_near(float x) const { return fabsf(x) * scale <= kTanhNear; }
+    __device__ __forceinline__ float2 near(float2 x) const {
         const float2 u = mul2(x, x);
         return mul2(x, fma2(fma2(fma2(fma2(both(k[4]), u, both(k[3])), u, both(k[2])), u, both(k[1])), u, both(k[0])));
     }
+    // FORM: kNear, kFar
+    template <int FORM> __device__ __forceinline__ float2 of(float2 x) const { return FORM == kNear ? near(x) : far(x); }
+    __device__ __forceinline__ float2 far(float2 x) const { return make_float2(factor * attn_tanh(x.x * scale), factor * attn_tanh(x.y * scale)); }
 };
 // The largest of N values, in eight chains: one would wait for each result before the next.
 template <int N, typename F>

@@ -263,8 +263,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const int row0 = first + quarter * 32, row = row0 + lane;   // in the text
         const bool real = row < kept_rows;
-        const float c = (CAP ? a.cap : a.scale) * kLog2e, inv_cap = CAP ? a.scale / a.cap : 0.f;
-        const AttnTanh tanh_near(inv_cap, 1.f);
+        const float c = (CAP ? a.cap : a.scale) * kLog2e;
+        const AttnTanh capped(CAP ? a.scale / a.cap : 0.f, 1.f);
         bool ok = true;
 
         float lse2 = 0.f, delta = 0.f;   // (both negated)
@@ -341,7 +341,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
 #pragma unroll
             for (int k = 0; k < MY; k += 32) tmem_ld32_nowait(s_cols + lanes + w * MY + k, p + k);
             tmem_wait_ld();
-            auto weights = [&](auto near, auto some) {   // (some: scores are masked)
+            auto weights = [&](auto form, auto some) {   // (form: of tanh; some: scores are masked)
 #pragma unroll
                 for (int h = 0; h < MY; h += 32) {
                     uint32_t r[16];
@@ -352,16 +352,16 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                         const float l4[4] = {lse4.x, lse4.y, lse4.z, lse4.w};
 #pragma unroll
                         for (int e = 0; e < 4; e += 2) {
-                            float2 v = make_float2(p[k + e], p[k + e + 1]), l2 = make_float2(l4[e], l4[e + 1]), slack;
+                            float2 v = make_float2(p[k + e], p[k + e + 1]), l2 = make_float2(l4[e], l4[e + 1]), slack = both(1.f);
                             if (CAP) {
-                                v = decltype(near)::value ? tanh_near(v) : make_float2(attn_tanh(v.x * inv_cap), attn_tanh(v.y * inv_cap));
+                                v = capped.of<decltype(form)::value>(v);
                                 slack = fma2(mul2(v, both(-1.f)), v, both(1.f));
                             }
                             if (BIAS) l2 = fma2(make_float2(fabsf(away - (float)(k + e)), fabsf(away - (float)(k + e + 1))), both(-slope), l2);
                             v = fma2(v, both(c), l2);
                             v = make_float2(fast_exp2(v.x), fast_exp2(v.y));
-                            if (decltype(some)::value && (k + e >= hi || (KEYS && k + e < lo))) v.x = 0.f;
-                            if (decltype(some)::value && (k + e + 1 >= hi || (KEYS && k + e + 1 < lo))) v.y = 0.f;
+                            if (decltype(some)::value && (k + e >= hi || (KEYS && k + e < lo))) v.x = slack.x = 0.f;
+                            if (decltype(some)::value && (k + e + 1 >= hi || (KEYS && k + e + 1 < lo))) v.y = slack.y = 0.f;
                             const float2 flat = CAP ? mul2(v, slack) : v, operand = KEYS ? v : flat;
                             r[(k + e - h) / 2] = pack2<T>(operand.x, operand.y);
                             if (KEYS) v = flat;
@@ -374,14 +374,17 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                     tmem_st16_nowait(s_cols + lanes + w * MY + h / 2, r);
                 }
             };
-            if (CAP) {
-                const float big = attn_max<MY>([&](int k) { return fabsf(p[k]); });
-                if (masked || !__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) weights(std::false_type(), std::true_type());
-                else weights(std::true_type(), std::false_type());
+            constexpr std::integral_constant<int, kNear> near;
+            constexpr std::integral_constant<int, kFar> far;
+            if constexpr (CAP) {
+                // (what another text has in the tile decides nothing)
+                const float big = real ? attn_max<MY>([&](int k) { return fabsf(p[k]); }) : 0.f;
+                if (masked || !__all_sync(0xffffffffu, capped.is_near(big))) weights(far, std::true_type());
+                else weights(near, std::false_type());
             } else if (masked) {
-                weights(std::false_type(), std::true_type());
+                weights(far, std::true_type());
             } else {
-                weights(std::false_type(), std::false_type());
+                weights(far, std::false_type());
             }
             tmem_wait_st();
             tc_fence_before();

@@ -219,8 +219,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
         constexpr bool RAW = !CAP && !BIAS;     // scores as they come, the factor is applied in the exponent
         const float c = RAW ? a.scale * kLog2e : 1.f;
         const float slope = BIAS ? a.slopes[head] * kLog2e : 0.f;
-        const float inv_cap = CAP ? a.scale / a.cap : 0.f, cap2 = CAP ? a.cap * kLog2e : 0.f;
-        const AttnTanh near(inv_cap, cap2);
+        const AttnTanh capped(CAP ? a.scale / a.cap : 0.f, CAP ? a.cap * kLog2e : 0.f);
         // What the other half of a row's columns has: by turns in two places, so that one barrier per exchange is enough.
         volatile float* mine = reinterpret_cast<volatile float*>(smem_raw + (shared - raw)) + (w * HALVES + half) * kAttnRows + quarter * 32 + lane;
         volatile float* other = mine + (half ? -kAttnRows : kAttnRows);
@@ -239,19 +238,25 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
 #pragma unroll
             for (int k = 0; k < MY; k += 32) tmem_ld32_nowait(s_cols(w) + lanes + half * MY + k, s + k);
             tmem_wait_ld();
+            const bool masked = (j + 1) * BK > seen_by_all;
+            const int left = seen - j * BK - half * MY;   // columns that the row sees
             if (CAP) {
-                const float big = attn_max<MY>([&](int k) { return fabsf(s[k]); });
-                if (__all_sync(0xffffffffu, big * inv_cap <= kTanhNear)) {
+                auto cap_all = [&](auto form) {
 #pragma unroll
                     for (int k = 0; k < MY; k += 2) {
-                        const float2 v = near(make_float2(s[k], s[k + 1]));
+                        const float2 v = capped.of<decltype(form)::value>(make_float2(s[k], s[k + 1]));
                         s[k] = v.x;
                         s[k + 1] = v.y;
                     }
-                } else {
+                };
+                // (what another text has in the tile decides nothing)
+                if (masked) {
 #pragma unroll
-                    for (int k = 0; k < MY; ++k) s[k] = cap2 * attn_tanh(s[k] * inv_cap);
+                    for (int k = 0; k < MY; ++k) s[k] = k < left ? s[k] : 0.f;
                 }
+                const float big = row < x.lq ? attn_max<MY>([&](int k) { return fabsf(s[k]); }) : 0.f;
+                if (__all_sync(0xffffffffu, capped.is_near(big))) cap_all(std::integral_constant<int, kNear>());
+                else cap_all(std::integral_constant<int, kFar>());
             }
             if (BIAS) {
                 const int ahead = attn_position(x, row0) - j * BK - half * MY;   // of this warp's first row, over the first column
@@ -270,8 +275,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 if (ahead >= MY - 1 || ahead + 31 <= 0) bias([&](int k) { return fmaf(sign, (float)k, from); });
                 else bias([&](int k) { return -slope * fabsf(away - (float)k); });
             }
-            if ((j + 1) * BK > seen_by_all) {
-                const int left = seen - j * BK - half * MY;
+            if (masked) {
 #pragma unroll
                 for (int k = 0; k < MY; ++k) s[k] = k < left ? s[k] : -INFINITY;
             }

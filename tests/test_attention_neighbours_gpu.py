@@ -43,3 +43,14 @@ def same_bits(lib, lens, among=1, **kw):
 def test_neighbours_do_not_raise_a_maximum(lib, dtype, causal, bias, dim, among):
     for lens in ([300, 61, 400, 30], [70, 500, 140], [129, 1, 385, 2]):
         same_bits(lib, lens, among, dim=dim, dtype=dtype, causal=causal, bias=bias)
+
+
+@pytest.mark.parametrize("among", [1, MANY])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("causal,bias", [(False, False), (True, False), (False, True)])
+@pytest.mark.parametrize("cap", [20.0, 3.0])
+def test_neighbours_do_not_choose_how_scores_are_capped(lib, cap, causal, bias, dim, among):
+    """Scores within three quarters of a cap can do with less arithmetic than others.  (At a cap of 20 those of the texts
+    looked at are, and their neighbours' are not.)"""
+    for lens in ([300, 61, 400, 30], [70, 500, 140], [129, 1, 385, 2]):
+        same_bits(lib, lens, among, dim=dim, causal=causal, bias=bias, cap=cap)
