@@ -328,7 +328,7 @@ int sama_clip_grads(sama_ctx* ctx, const sama_tensor_t* tensors, int32_t n_tenso
  * Scores of a query against a key, for head h and key head g = h / (heads / kv_heads):
  *   x = scale * (q . k);   if cap > 0: x = cap * tanh(x / cap);   if slopes: x = x - slopes[h] * |pos_q - pos_k|
  *   out = sum over the keys that the query sees of softmax(x) * v
- * (the softmax and every sum in fp32; the weights, operands of the second product, are rounded to `dtype`).
+ * (a capped score is off by 7e-7 of itself, or up to a cap of 64 by 1e-5 at most; the softmax and every sum in fp32; the weights, operands of the second product, are rounded to `dtype`).
  *
  * Texts lie packed behind one another: text t has the queries q_starts[t] .. q_starts[t+1] - 1 and the keys
  * k_starts[t] .. k_starts[t+1] - 1, and its queries see its own keys only.  The last query has the position of the last

@@ -44,6 +44,9 @@ size_t paged_workspace(const sama_ctx* ctx);
 cudaError_t launch_paged(sama_ctx* ctx, const PagedShape& a, int dtype, const void* q, const void* k_new, const void* v_new,
                          void* k_cache, void* v_cache, void* out, void* ws, cudaStream_t st);
 
+enum AttnCap { kNoCap, kCap, kWideCap };
+inline AttnCap attn_cap(float cap) { return cap <= 0.f ? kNoCap : cap <= 64.f ? kCap : kWideCap; }
+
 #ifdef __CUDACC__
 
 __device__ __forceinline__ int attn_start(const int32_t* starts, int i, int n) { return min(max(starts[i], 0), n); }
@@ -113,10 +116,11 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 // 2^-11, a hundredth of a weight at a cap of 30), which is a relative one of 2.5e-7 beyond 0.75.  Below, tanh is a polynomial,
 // z p(z^2) with p of degree 4 through tanh(z) / z at the Chebyshev points of [0, 0.75^2]: 7e-7 of tanh(z).  The first takes two of
 // the three results of the special-function unit per score (16 a cycle and SM), so it is left out where all scores of a
-// warp's tile are within 0.75 caps (and, in the backward pass, seen).
+// warp's tile are within 0.75 caps (and, in the backward pass, seen).  Elsewhere it serves for all of them up to a cap of 64, where its error
+// is 1e-5 of a weight at most; with larger caps (kernels of their own) each score has the form that is good for it.
 __device__ __forceinline__ float attn_tanh(float z) { return fmaf(-2.f, fast_rcp(1.f + fast_exp2(2.f * kLog2e * z)), 1.f); }
 constexpr float kTanhNear = 0.75f;
-enum { kNear, kFar };
+enum { kNear, kFar, kAny };
 struct AttnTanh {   // times `factor`, of `scale` times its argument
     float k[5], scale, factor;
     __device__ __forceinline__ AttnTanh(float scale, float factor) : scale(scale), factor(factor) {
@@ -130,9 +134,13 @@ struct AttnTanh {   // times `factor`, of `scale` times its argument
         const float2 u = mul2(x, x);
         return mul2(x, fma2(fma2(fma2(fma2(both(k[4]), u, both(k[3])), u, both(k[2])), u, both(k[1])), u, both(k[0])));
     }
-    // FORM: kNear, kFar
-    template <int FORM> __device__ __forceinline__ float2 of(float2 x) const { return FORM == kNear ? near(x) : far(x); }
+    // FORM: kNear, kFar, kAny
+    template <int FORM> __device__ __forceinline__ float2 of(float2 x) const { return FORM == kNear ? near(x) : FORM == kFar ? far(x) : any(x); }
     __device__ __forceinline__ float2 far(float2 x) const { return make_float2(factor * attn_tanh(x.x * scale), factor * attn_tanh(x.y * scale)); }
+    __device__ __forceinline__ float2 any(float2 x) const {
+        const float2 y = near(x), z = far(x);
+        return make_float2(is_near(x.x) ? y.x : z.x, is_near(x.y) ? y.y : z.y);
+    }
 };
 // The largest of N values, in eight chains: one would wait for each result before the next.
 template <int N, typename F>

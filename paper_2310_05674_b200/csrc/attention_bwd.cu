@@ -63,7 +63,7 @@ struct alignas(64) BwdParams {
     int slots;
 };
 
-template <typename T, int D, int BT, bool CAP, bool BIAS, bool KEYS>
+template <typename T, int D, int BT, AttnCap CAP, bool BIAS, bool KEYS>
 __global__ void __launch_bounds__(BwdTile<D, BT, KEYS>::THREADS, BwdTile<D, BT, KEYS>::CTAS)
 attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     using C = BwdTile<D, BT, KEYS>;
@@ -375,8 +375,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                 }
             };
             constexpr std::integral_constant<int, kNear> near;
-            constexpr std::integral_constant<int, kFar> far;
-            if constexpr (CAP) {
+            constexpr std::integral_constant<int, CAP == kWideCap ? kAny : kFar> far;
+            if constexpr (CAP != kNoCap) {
                 // (what another text has in the tile decides nothing)
                 const float big = real ? attn_max<MY>([&](int k) { return fabsf(p[k]); }) : 0.f;
                 if (masked || !__all_sync(0xffffffffu, capped.is_near(big))) weights(far, std::true_type());
@@ -489,15 +489,15 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     if (warp == 1) tmem_dealloc(tmem, COLS);
 }
 
-template <typename T, int D, int BT, bool CAP, bool BIAS, bool KEYS>
+template <typename T, int D, int BT, AttnCap CAP, bool BIAS, bool KEYS>
 cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {
     using C = BwdTile<D, BT, KEYS>;
     auto* kernel = attn_bwd_kernel<T, D, BT, CAP, BIAS, KEYS>;
-    const uint64_t bit = 1ull << ((BT == 64 ? 32 : 0) + (KEYS ? 16 : 0) + (std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
-    if (!(ctx->attn_bwd_ready & bit)) {
+    const uint64_t bit = 1ull << ((BT == 64 ? 32 : 0) + (std::is_same<T, __half>::value ? 16 : 0) + (D == 64 ? 8 : 0) + 2 * CAP + (BIAS ? 1 : 0));
+    if (!(ctx->attn_bwd_ready[KEYS] & bit)) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         if (e != cudaSuccess) return e;
-        ctx->attn_bwd_ready |= bit;
+        ctx->attn_bwd_ready[KEYS] |= bit;
     }
     KernelScope scope(ctx, SAMA_K_ATTN, KEYS ? 2 : 1, st);
     const int64_t blocks = (int64_t)P.slots * (KEYS ? P.a.kv_heads : P.a.heads);
@@ -505,8 +505,11 @@ cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {
 }
 template <typename T, int D, int BT, bool KEYS>
 cudaError_t launch(sama_ctx* ctx, const BwdParams& P, cudaStream_t st) {
-    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, BT, true, true, KEYS>(ctx, P, st) : launch<T, D, BT, true, false, KEYS>(ctx, P, st);
-    return P.a.slopes ? launch<T, D, BT, false, true, KEYS>(ctx, P, st) : launch<T, D, BT, false, false, KEYS>(ctx, P, st);
+    switch (attn_cap(P.a.cap)) {
+        case kNoCap: return P.a.slopes ? launch<T, D, BT, kNoCap, true, KEYS>(ctx, P, st) : launch<T, D, BT, kNoCap, false, KEYS>(ctx, P, st);
+        case kCap: return P.a.slopes ? launch<T, D, BT, kCap, true, KEYS>(ctx, P, st) : launch<T, D, BT, kCap, false, KEYS>(ctx, P, st);
+        default: return P.a.slopes ? launch<T, D, BT, kWideCap, true, KEYS>(ctx, P, st) : launch<T, D, BT, kWideCap, false, KEYS>(ctx, P, st);
+    }
 }
 template <typename T, bool KEYS>
 cudaError_t launch(sama_ctx* ctx, int bt, const BwdParams& P, cudaStream_t st) {

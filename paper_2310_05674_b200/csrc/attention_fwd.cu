@@ -52,7 +52,7 @@ struct alignas(64) FwdParams {
     int slots;
 };
 
-template <typename T, int D, int NW, bool CAP, bool BIAS>
+template <typename T, int D, int NW, AttnCap CAP, bool BIAS>
 __global__ void __launch_bounds__((FwdTile<D, NW>::THREADS), (FwdTile<D, NW>::CTAS))
 attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     using C = FwdTile<D, NW>;
@@ -256,7 +256,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 }
                 const float big = row < x.lq ? attn_max<MY>([&](int k) { return fabsf(s[k]); }) : 0.f;
                 if (__all_sync(0xffffffffu, capped.is_near(big))) cap_all(std::integral_constant<int, kNear>());
-                else cap_all(std::integral_constant<int, kFar>());
+                else cap_all(std::integral_constant<int, CAP == kWideCap ? kAny : kFar>());
             }
             if (BIAS) {
                 const int ahead = attn_position(x, row0) - j * BK - half * MY;   // of this warp's first row, over the first column
@@ -358,11 +358,11 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
     if (warp == 1) tmem_dealloc(tmem, C::COLS);
 }
 
-template <typename T, int D, int NW, bool CAP, bool BIAS>
+template <typename T, int D, int NW, AttnCap CAP, bool BIAS>
 cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
     using C = FwdTile<D, NW>;
     auto* kernel = attn_fwd_kernel<T, D, NW, CAP, BIAS>;
-    const uint32_t bit = 1u << ((NW == 2 ? 16 : 0) + (std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
+    const uint64_t bit = 1ull << ((NW == 2 ? 32 : 0) + (std::is_same<T, __half>::value ? 16 : 0) + (D == 64 ? 8 : 0) + 2 * CAP + (BIAS ? 1 : 0));
     if (!(ctx->attn_fwd_ready & bit)) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
         if (e != cudaSuccess) return e;
@@ -373,8 +373,11 @@ cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
 }
 template <typename T, int D, int NW>
 cudaError_t launch(sama_ctx* ctx, const FwdParams& P, cudaStream_t st) {
-    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, NW, true, true>(ctx, P, st) : launch<T, D, NW, true, false>(ctx, P, st);
-    return P.a.slopes ? launch<T, D, NW, false, true>(ctx, P, st) : launch<T, D, NW, false, false>(ctx, P, st);
+    switch (attn_cap(P.a.cap)) {
+        case kNoCap: return P.a.slopes ? launch<T, D, NW, kNoCap, true>(ctx, P, st) : launch<T, D, NW, kNoCap, false>(ctx, P, st);
+        case kCap: return P.a.slopes ? launch<T, D, NW, kCap, true>(ctx, P, st) : launch<T, D, NW, kCap, false>(ctx, P, st);
+        default: return P.a.slopes ? launch<T, D, NW, kWideCap, true>(ctx, P, st) : launch<T, D, NW, kWideCap, false>(ctx, P, st);
+    }
 }
 template <typename T>
 cudaError_t launch(sama_ctx* ctx, int nw, const FwdParams& P, cudaStream_t st) {

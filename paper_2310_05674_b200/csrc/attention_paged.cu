@@ -67,7 +67,7 @@ struct Place {
     int s, unit, step, len, steps;   // sequence; key head and group of ROWS queries; step of the sequence, its length and number of steps
 };
 
-template <typename T, int D, bool CAP, bool BIAS>
+template <typename T, int D, AttnCap CAP, bool BIAS>
 __global__ void __launch_bounds__(THREADS, 2)
 paged_kernel(const PagedParams P) {
     using C = PagedTile<D>;
@@ -203,7 +203,7 @@ paged_kernel(const PagedParams P) {
 
     constexpr bool RAW = !CAP && !BIAS;
     const float c = RAW ? a.scale * kLog2e : 1.f;
-    const float inv_cap = CAP ? a.scale / a.cap : 0.f, cap2 = CAP ? a.cap * kLog2e : 0.f;
+    const AttnTanh capped(CAP ? a.scale / a.cap : 0.f, CAP ? a.cap * kLog2e : 0.f);
     uint32_t qf[D / 16][2];
     float o[D / 8][4], m = -INFINITY, l = 0.f, slope = 0.f;
     bool fresh_unit = true;
@@ -272,17 +272,18 @@ paged_kernel(const PagedParams P) {
             const int key0 = 2 * (lane & 3), pos0 = at.step * STEP + warp * KEYS;
             float top = -INFINITY;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
+                const float2 x = make_float2(s[t][0], s[t][1]), y = CAP == kNoCap ? x : CAP == kCap ? capped.far(x) : capped.any(x);
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int key = 8 * t + key0 + e;
-                    float v = s[t][e];
-                    if (CAP) v = cap2 * attn_tanh(v * inv_cap);
+                    float v = e ? y.y : y.x;
                     if (BIAS) v = fmaf(-slope, (float)(at.len - 1 - (pos0 + key)), CAP ? v : v * (a.scale * kLog2e));
                     v = (there >> key) & 1u ? v * c : -INFINITY;
                     s[t][e] = v;
                     top = fmaxf(top, v);
                 }
+            }
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             if (__any_sync(0xffffffffu, top > m)) {
@@ -447,13 +448,13 @@ paged_kernel(const PagedParams P) {
 // Two CTAs per SM.
 int most_ctas(const sama_ctx* ctx) { return 2 * ctx->sm_count; }
 
-template <typename T, int D, bool CAP, bool BIAS>
+template <typename T, int D, AttnCap CAP, bool BIAS>
 cudaError_t launch(sama_ctx* ctx, const PagedParams& P, int ctas, cudaStream_t st) {
     auto* kernel = paged_kernel<T, D, CAP, BIAS>;
     // the ring, and what is the larger of the warps' sums and the factors of all parts
     using C = PagedTile<D>;
     const int sums = WARPS * ROWS * C::LD * 4, factors = most_ctas(ctx) * ROWS * 4, smem = WARPS * C::RING + (sums > factors ? sums : factors);
-    const uint32_t bit = 1u << ((std::is_same<T, __half>::value ? 8 : 0) + (D == 64 ? 4 : 0) + (CAP ? 2 : 0) + (BIAS ? 1 : 0));
+    const uint32_t bit = 1u << ((std::is_same<T, __half>::value ? 16 : 0) + (D == 64 ? 8 : 0) + 2 * CAP + (BIAS ? 1 : 0));
     if (!(ctx->paged_ready & bit)) {
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
@@ -464,8 +465,11 @@ cudaError_t launch(sama_ctx* ctx, const PagedParams& P, int ctas, cudaStream_t s
 }
 template <typename T, int D>
 cudaError_t launch(sama_ctx* ctx, const PagedParams& P, int ctas, cudaStream_t st) {
-    if (P.a.cap > 0.f) return P.a.slopes ? launch<T, D, true, true>(ctx, P, ctas, st) : launch<T, D, true, false>(ctx, P, ctas, st);
-    return P.a.slopes ? launch<T, D, false, true>(ctx, P, ctas, st) : launch<T, D, false, false>(ctx, P, ctas, st);
+    switch (attn_cap(P.a.cap)) {
+        case kNoCap: return P.a.slopes ? launch<T, D, kNoCap, true>(ctx, P, ctas, st) : launch<T, D, kNoCap, false>(ctx, P, ctas, st);
+        case kCap: return P.a.slopes ? launch<T, D, kCap, true>(ctx, P, ctas, st) : launch<T, D, kCap, false>(ctx, P, ctas, st);
+        default: return P.a.slopes ? launch<T, D, kWideCap, true>(ctx, P, ctas, st) : launch<T, D, kWideCap, false>(ctx, P, ctas, st);
+    }
 }
 
 

@@ -139,8 +139,8 @@ struct sama_ctx {
     float* ffn_parts;              // device: sums of tiles whose contraction several CTAs share
     int* ffn_arrived;              // device: arrival counters of such tiles, zero between launches
     int ffn_path[5];               // how each of the block's launches was last worked on (sama_last_ffn_path)
-    uint32_t attn_fwd_ready;       // kernels of attention_fwd.cu whose shared-memory size is set on this device
-    uint64_t attn_bwd_ready;       // ... and of attention_bwd.cu
+    uint64_t attn_fwd_ready;       // kernels of attention_fwd.cu whose shared-memory size is set on this device
+    uint64_t attn_bwd_ready[2];    // ... and of attention_bwd.cu: d-queries, d-keys
     uint32_t paged_ready;          // ... and of attention_paged.cu
     int distill_ready;             // the shared-memory sizes of distill.cu are set on this device
     int* paged_arrived;            // device: arrival counters of heads that several CTAs share, zero between launches
