@@ -363,7 +363,11 @@ typedef struct sama_attn_t {
  * softmax are rounded to `dtype` as operands of the last products: against sums of unrounded values the gradients' relative
  * error grows from 0.0017 to 0.0024 in bf16, 0.0002 to 0.0003 in fp16 (out's to 0.0018 .. 0.0022, 0.0003).  d_out . out is
  * put right for out's rounding by the sum of softmax * (dP - d_out . out).  Keys with a common offset have dq's error grow as
- * their size does, which dq itself does not (0.007 in bf16, 0.0009 in fp16 where the offset is four times their spread).  slopes get no gradient.  Uses 8 * heads * n_q bytes of
+ * their size does, which dq itself does not (0.007 in bf16, 0.0009 in fp16 where the offset is four times their spread).  slopes get no gradient.  In
+ * SAMA_F16 the softmax and dX are scaled by powers of two on the way, dX by what takes the largest of d_out (for dq of its row, for
+ * dk of the queries from the first on that sees a key of the same 128) to 4 .. 8, so that a small or large d_out costs no
+ * places; results beyond 65504 are infinite, and dX beyond 8000 times the largest of d_out is, too.  Within a text a k, q or d_out
+ * that is not finite may reach gradients of rows that do not see it.  Uses (8 * n_q + 4 * (n_q / 128 + n_texts)) * heads bytes of
  * the workspace. */
 int sama_attention(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, void* out,
                    float* lse_out, void* stream);

@@ -49,7 +49,9 @@ template <int D, int BT, bool KEYS> struct BwdTile {
     static_assert(COLS >= 2 * BT + 2 * D, "scores, their gradients and the sums");
     static constexpr int KEPT = kAttnRows * D * 2, TILE = BT * D * 2;
     static constexpr int STATS = KEYS ? BT * 8 : 0;      // lse and delta of a streamed tile's queries
-    static constexpr int SMEM = 2 * KEPT + (FIRST + SECOND) * TILE + FIRST * STATS + (KEYS ? 0 : kAttnRows * 4) + 256 + 1024;
+    static constexpr int SUMS = 2 * kAttnRows * 4;       // d-queries: rows of d_out . out, and of d_out's largest; d-keys: warps of the latter
+    static constexpr int SMEM = 2 * KEPT + (FIRST + SECOND) * TILE + FIRST * STATS + SUMS + 256 + 1024;
+    static_assert(SMEM * CTAS + 1024 * CTAS <= 228 * 1024, "an SM's shared memory");
 };
 
 struct alignas(64) BwdParams {
@@ -57,10 +59,26 @@ struct alignas(64) BwdParams {
     AttnShape a;
     const void *out, *dout;
     const float* lse;
-    float *lse2, *delta;   // [heads][n_q]: -lse log2 e (-infinity for a query that sees nothing), and -delta
+    float *lse2, *delta;   // [heads][n_q]: -lse log2 e (-infinity for a query that sees nothing; fp16: lifted), and -delta
+    float* largest;        // fp16: [tile of queries][heads], the largest of d_out
     void* grad[2];      // dQ, or dK and dV
     int64_t ld[2];
     int slots;
+};
+
+// What fp16 holds in full is 2^-14 to 65504.  P is lifted by 2^14, and dX by a power of two that takes d_out's largest value to
+// 4 .. 8: a row's own for dQ, for dK that of the queries from the first on that sees a key of the tile.  Gradients are as exact
+// for any size of d_out (without that, dQ of 2048 keys is off by 0.003 at a d_out of 1e-3, where storing it costs 0.0005).
+template <typename T> constexpr float kLift = std::is_same<T, __half>::value ? 14.f : 0.f;
+constexpr float kUnlift = 1.f / (1 << 14);
+struct BwdPower {
+    int e = 0;
+    __device__ __forceinline__ BwdPower() {}
+    __device__ __forceinline__ explicit BwdPower(float largest) {
+        if (largest > 0.f && largest < INFINITY) e = 129 - (int)(__float_as_uint(largest) >> 23);   // (normal: 2^-24 at least)
+    }
+    __device__ __forceinline__ float up() const { return __uint_as_float((uint32_t)(127 + e) << 23); }
+    __device__ __forceinline__ float down() const { return __uint_as_float((uint32_t)(127 - e) << 23); }
 };
 
 template <typename T, int D, int BT, AttnCap CAP, bool BIAS, bool KEYS>
@@ -69,7 +87,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     using C = BwdTile<D, BT, KEYS>;
     constexpr int FORMING = C::FORMING, MY = BT / (FORMING / 4);   // streamed rows, which are columns of P and dX, of a warp
     constexpr int N1 = C::FIRST, N2 = C::SECOND;
-    constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value;
+    constexpr bool BF16 = std::is_same<T, __nv_bfloat16>::value, HALF = !BF16;
     constexpr uint32_t IDESC_S = idesc16(BF16, false, false, kAttnRows, BT), IDESC_G = idesc16(BF16, false, true, kAttnRows, D);
     constexpr uint32_t COLS = C::COLS;
     const AttnShape& a = P.a;
@@ -101,7 +119,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t base = (raw + 1023u) & ~1023u;
     const uint32_t ring1 = base + 2 * C::KEPT, ring2 = ring1 + N1 * C::TILE, stats = ring2 + N2 * C::TILE, sums = stats + N1 * C::STATS;
-    const uint32_t bars = sums + (KEYS ? 0 : kAttnRows * 4);
+    const uint32_t bars = sums + C::SUMS;
     auto full1 = [&](int s) { return bars + 8u * s; };
     auto empty1 = [&](int s) { return bars + 8u * (N1 + s); };
     auto full2 = [&](int s) { return bars + 8u * (2 * N1 + s); };
@@ -268,6 +286,8 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         bool ok = true;
 
         float lse2 = 0.f, delta = 0.f;   // (both negated)
+        BwdPower power;                  // of dX
+        volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (sums - raw));
         // sum P (dP - delta), which is what delta is off by for out's rounding: it is put right in dQ by off sum P (1 - tanh^2) K,
         // which takes a product of its own, and in delta for d-keys.  (Without that, keys and values with a common offset of
         // their spread have dQ off by 0.01 to 0.02 in bf16, of four times that by a third: dQ does not grow with the offset,
@@ -276,7 +296,6 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         if (!KEYS) {
             // each warp takes some rows, whose columns are added up by lanes next to one another (with a row per lane, the way
             // to delta took 6500 of a CTA's 17,000 cycles for texts of a few hundred tokens)
-            volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (sums - raw));
             constexpr int LANES = D / 8, AT_ONCE = 32 / LANES, EACH = kAttnRows / FORMING, N = EACH / AT_ONCE;
             const int r0 = (warp - 2) * EACH + lane / LANES, col = lane % LANES * 8;
             uint4 o[N], d[N];
@@ -292,25 +311,55 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             }
             if (real) {
                 lse2 = P.lse[(int64_t)head0 * a.n_q + x.q0 + row] * -kLog2e;
-                if (lse2 == INFINITY) lse2 = -INFINITY;
+                lse2 = lse2 == INFINITY ? -INFINITY : lse2 + kLift<T>;
             }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const uint32_t u[4] = {o[i].x, o[i].y, o[i].z, o[i].w}, v[4] = {d[i].x, d[i].y, d[i].z, d[i].w};
-                float sum = 0.f;
+                float sum = 0.f, most = 0.f;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 f = unpack2<T>(u[e]), g = unpack2<T>(v[e]);
                     sum = fmaf(f.x, g.x, fmaf(f.y, g.y, sum));
+                    if (HALF) most = fmaxf(most, fmaxf(fabsf(g.x), fabsf(g.y)));
                 }
 #pragma unroll
-                for (int x = 1; x < LANES; x *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-                if (col == 0) part[r0 + i * AT_ONCE] = sum;
+                for (int x = 1; x < LANES; x *= 2) {
+                    sum += __shfl_xor_sync(0xffffffffu, sum, x);
+                    if (HALF) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+                }
+                if (col == 0) {
+                    part[r0 + i * AT_ONCE] = sum;
+                    if (HALF) part[kAttnRows + r0 + i * AT_ONCE] = most;
+                }
             }
             asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
             delta = -part[quarter * 32 + lane];
+            if (HALF) {
+                power = BwdPower(part[kAttnRows + quarter * 32 + lane]);
+                if (warp == 2) {
+                    float most = 0.f;
+                    for (int r = lane; r < kAttnRows; r += 32) most = fmaxf(most, part[kAttnRows + r]);
+#pragma unroll
+                    for (int x = 16; x > 0; x /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+                    if (lane == 0) P.largest[(int64_t)slot * a.heads + head0] = most;
+                }
+            }
             if (w == 0 && real) P.lse2[(int64_t)head0 * a.n_q + x.q0 + row] = lse2;
         }
+        if (KEYS && HALF) {
+            const int from = tile0 * BT / kAttnRows, tiles = max((x.lq + kAttnRows - 1) / kAttnRows - from, 0), all = tiles * a.group;
+            const float* largest = P.largest + (int64_t)(x.q0 / kAttnRows + t + from) * a.heads + head0 * a.group;
+            float most = 0.f;
+            for (int i = threadIdx.x - 64; i < all; i += 32 * FORMING) most = fmaxf(most, largest[(int64_t)(i / a.group) * a.heads + i % a.group]);
+#pragma unroll
+            for (int x = 16; x > 0; x /= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, x));
+            if (lane == 0) part[warp - 2] = most;
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
+            for (int i = 0; i < FORMING; ++i) most = fmaxf(most, part[i]);
+            power = BwdPower(most);
+        }
+        const float raise = HALF ? power.up() * kUnlift : 1.f, lower = HALF ? power.down() : 1.f;   // of dP, and of what comes of dX
         // d-queries: the row sees keys below `edge`; d-keys: the row is seen by queries from `edge` on
         const int edge = KEYS ? attn_first_query(a.causal, x, row) : attn_seen(a.causal, x, row);
         const int edge_of_all = KEYS ? attn_first_query(a.causal, x, row0 + 31) : attn_seen(a.causal, x, row0);
@@ -326,6 +375,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             if (from < BT) attn_zero_rows<D / 64>(o ? ring2 + next2 * C::TILE : ring1 + next1 * C::TILE, from, BT, warp - 2, FORMING);
             return true;
         };
+        const float raised_delta = delta * raise;
         if (KEYS && n > 0) ok = wait(full1(0), 0);
         for (int i = 0; ok && i < n; ++i) {
             const int at = (tile0 + tile_of_head) * BT + w * MY;   // this warp's first streamed row, in the text
@@ -406,13 +456,15 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
                             else tmem_ld32_nowait(dp_cols + lanes + w * MY + h, dp);
                             tmem_wait_ld();
                         }
-                        float4 d4 = make_float4(delta, delta, delta, delta);
+                        float4 d4 = make_float4(raised_delta, raised_delta, raised_delta, raised_delta);
                         if (KEYS) d4 = *reinterpret_cast<const float4*>(deltas + h + k);
                         const float d[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
                         for (int e = 0; e < 4; e += 2) {
                             const int at = h + k + e;
-                            float2 g = mul2(make_float2(p[at], p[at + 1]), add2(make_float2(dp[k + e], dp[k + e + 1]), make_float2(d[e], d[e + 1])));
+                            float2 g = make_float2(dp[k + e], dp[k + e + 1]), d2 = make_float2(d[e], d[e + 1]);
+                            if (HALF && KEYS) d2 = mul2(d2, both(raise));
+                            g = mul2(make_float2(p[at], p[at + 1]), HALF ? fma2(g, both(raise), d2) : add2(g, d2));
                             if (decltype(some)::value && (at >= hi || (KEYS && at < lo))) g.x = 0.f;
                             if (decltype(some)::value && (at + 1 >= hi || (KEYS && at + 1 < lo))) g.y = 0.f;
                             if (!KEYS) off[e / 2] = add2(off[e / 2], g);
@@ -442,12 +494,13 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
         float shift = 0.f;   // this row's, of all its warps
         if (!KEYS) {
             // d-keys gets the exact delta.  (The kept operands' place is free now.)
-            volatile float* part = reinterpret_cast<volatile float*>(smem_raw + (base - raw)) + quarter * 32 + lane;
-            part[w * kAttnRows] = (off[0].x + off[0].y) + (off[1].x + off[1].y);
+            volatile float* all = reinterpret_cast<volatile float*>(smem_raw + (base - raw)) + quarter * 32 + lane;
+            all[w * kAttnRows] = (off[0].x + off[0].y) + (off[1].x + off[1].y);
             asm volatile("bar.sync 1, %0;" ::"n"(32 * FORMING) : "memory");
 #pragma unroll
-            for (int i = 0; i < FORMING / 4; ++i) shift += part[i * kAttnRows];
-            if (w == 0 && real) P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta - shift;
+            for (int i = 0; i < FORMING / 4; ++i) shift += all[i * kAttnRows];
+            if (w == 0 && real) P.delta[(int64_t)head0 * a.n_q + x.q0 + row] = delta - shift * lower;
+            if (HALF) shift *= kUnlift;
         }
         // the kept operands' places, where all products are done (d-queries: the second's, the sums of `off` are in the first's)
         auto stage_of = [&](int o) { return base + (KEYS ? o : 1) * C::KEPT; };
@@ -456,7 +509,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
             // 32 columns at a time: d-keys' warps have dK or dV
             constexpr int SHARES = FORMING / 4;
             const int which = KEYS ? w % 2 : 0, k0 = 32 * (KEYS ? w / 2 : w);
-            const float f = which == 0 ? a.scale : 1.f;
+            const float f = which == 0 ? a.scale * lower : HALF ? kUnlift : 1.f;
 #pragma unroll 1
             for (int k = k0; k < D; k += 32 * (KEYS ? SHARES / 2 : SHARES)) {
                 float v[32];
@@ -523,7 +576,9 @@ cudaError_t launch(sama_ctx* ctx, int dtype, int bt, const BwdParams& P, cudaStr
 
 }  // namespace
 
-size_t attention_grad_workspace(const AttnShape& a) { return (size_t)a.heads * a.n_q * 2 * sizeof(float); }
+size_t attention_grad_workspace(const AttnShape& a) {
+    return a.n_q == 0 ? 0 : (size_t)a.heads * ((size_t)a.n_q * 2 + a.n_q / kAttnRows + a.n_texts) * sizeof(float);
+}
 
 cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnOperands& op, const void* out, const float* lse,
                                   const void* dout, void* dq, void* dk, void* dv, void* ws, cudaStream_t st) {
@@ -534,6 +589,7 @@ cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnO
     P.lse = lse;
     P.lse2 = static_cast<float*>(ws);
     P.delta = P.lse2 + (size_t)a.heads * a.n_q;
+    P.largest = P.delta + (size_t)a.heads * a.n_q;
     const int64_t dense = (int64_t)a.heads * a.dim;
     // Small tiles, two CTAs per SM, unless capped scores, whose arithmetic weighs more, are many (us for d-queries and d-keys,
     // 16 heads of 64: 16 texts of 512 39 and 42, with the large ones 45 and 52, capped 56 and 56, 60 and 66; one of 8192,

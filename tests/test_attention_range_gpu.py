@@ -1,0 +1,94 @@
+"""fp16 holds 2^-14 to 65504 in full: gradients are as exact for small and large d_out, and many keys, as anywhere.
+
+Bound: test_attention_offsets_gpu.py's, a relative one on the whole gradient, and what storing it in fp16 costs: half of the
+smallest step, 2^-25, per element."""
+import math
+
+import pytest
+import torch
+
+import attention_reference as ref
+from test_attention_offsets_gpu import run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2310_05674_b200 import binding
+    ctx = binding.sama_create(0, 1024, 0, None)
+    yield binding, ctx
+    torch.cuda.synchronize()
+    binding.sama_destroy(ctx)
+
+
+@pytest.mark.parametrize("dout", [1e-6, 1e-4, 1e-3, 1.0, 1e3])
+@pytest.mark.parametrize("dim,lens,heads,kv", [(64, [2048], 2, 1), (64, [300, 1, 900], 4, 2), (128, [8192], 1, 1), (40, [700, 333], 2, 2)])
+def test_size_of_the_incoming_gradient(lib, dout, dim, lens, heads, kv):
+    for causal, cap in ((False, 0.0), (True, 20.0)):
+        wrong, allowed, size = run(lib, lens, heads, kv, dim, "f16", causal, cap, False, 0.0, 0.0, dout_size=dout, seed=dim)
+        for name, h, a, b, c in zip(("dq", "dk", "dv"), (heads, kv, kv), wrong, allowed, size):
+            stored = math.sqrt(sum(lens) * h * dim) * 2.0 ** -25
+            assert a <= math.sqrt(b * b + stored * stored), (name, causal, a / c, b / c, stored / c)
+
+
+def gradients(lib, q, k, v, dout, causal):
+    """For each gradient of one text of one head: the norm of what it is off by, and what it may be."""
+    S, ctx = lib
+    (n, _, dim), m = q.shape, k.shape[0]
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    a = S.Attn(S.SAMA_F16, 1, 1, dim, n, m, i32(0, n), i32(0, m), causal=causal)
+    out, lse = torch.empty_like(q), torch.empty(1, n, device="cuda")
+    grads = [torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)]
+    S.sama_attention(ctx, a, q, k, v, out, lse)
+    S.sama_attention_grad(ctx, a, q, k, v, out, lse, dout, *grads)
+    Q, K, V, D = (x[:, 0].double() for x in (q, k, v, dout))
+    x = Q @ K.T * dim ** -0.5
+    p = torch.softmax(torch.where(ref.visible(n, m, causal, 0, "cuda"), x, -math.inf), -1)
+    o = p @ V
+    dx = p * (D @ V.T - (D * o).sum(-1, keepdim=True)) * dim ** -0.5
+    want = [dx @ K, dx.T @ Q, p.T @ D]
+    # each rounded operand, and the result
+    allowed = [(dx.square() @ K.square().sum(-1)).sum(), (dx.T.square() @ Q.square().sum(-1)).sum(), (p.T.square() @ D.square().sum(-1)).sum()]
+    # beyond 65504 the right value is infinite (the values next to it, which rounding may take to either side, are left out)
+    errors = []
+    for g, w, e in zip(grads, want, allowed):
+        g = g[:, 0].double()
+        over, fits = w.abs() > 65504 * 1.01, w.abs() < 65504 * 0.99
+        assert torch.equal(g[over], math.inf * w[over].sign())
+        errors.append((float((g - w)[fits].norm()), math.sqrt(float(e + w.square().sum()) * 2.0 ** -22 + w.numel() * 2.0 ** -50)))
+    return errors
+
+
+def test_many_keys(lib):
+    """Weights of 2^-18."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    r = lambda n: torch.randn(n, 1, 64, generator=g, device="cuda").half()  # noqa: E731
+    errors = gradients(lib, r(70), r(200000), r(200000), (100 * r(70).float()).half(), False)
+    for name, (wrong, allowed) in zip(("dq", "dk", "dv"), errors):
+        assert wrong <= allowed, (name, wrong, allowed)
+
+
+def test_queries_of_different_sizes(lib):
+    """A gradient that comes to a text's last rows alone, or is far smaller there, as a weight per token makes it."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda n: torch.randn(n, 1, 64, generator=g, device="cuda").half()  # noqa: E731
+    q, k, v, d = r(1000), r(1000), r(1000), r(1000)
+    for factor in (1e-4, 0.0, 1e4):
+        dout = d.clone()
+        dout[:700] = (dout[:700].float() * factor).half()
+        for causal in (False, True):
+            for name, (wrong, allowed) in zip(("dq", "dk", "dv"), gradients(lib, q, k, v, dout, causal)):
+                assert wrong <= allowed, (name, factor, causal, wrong, allowed)
+
+
+def test_values_that_make_large_products(lib):
+    """dX beyond 65504 (a few keys, which share the weights), of which dQ is not."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    r = lambda n, s=1.0: (s * torch.randn(n, 1, 128, generator=g, device="cuda")).half()  # noqa: E731
+    k = r(500, 0.02)
+    errors = gradients(lib, r(300, 50.0), k, r(500, 4.0), r(300, 8000.0), False)
+    more = gradients(lib, r(300, 0.1), r(500, 0.1), r(500, 4.0), r(300, 8000.0), False)
+    few = gradients(lib, r(300), r(4), r(4, 4.0), r(300, 8000.0), False)
+    for name, (wrong, allowed) in zip(("dq", "dk", "dv") * 3, errors + more + few):
+        assert wrong <= allowed, (name, wrong, allowed)
