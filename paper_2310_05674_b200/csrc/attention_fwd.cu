@@ -7,8 +7,8 @@
 // from there.  While one tile's weights are formed the other's products run: the other tile of the CTA, which shares the
 // keys and values, or that of another CTA of the SM (heads of more than 64 columns: two CTAs; others: three).  The maximum m
 // that the weights refer to is only raised when a score exceeds it by more than 8 binary orders (O and the sum are scaled
-// then): the weights stay below 2^8, far from the end of either type, and are rounded relative to their size whatever they
-// refer to.
+// then): the weights stay below 2^8.  bf16 rounds them relative to their size whatever they refer to; fp16, which has fewer places
+// below 2^-14, gets them lifted by 2^7, so that those from 2^-21 of the largest on keep all of theirs.
 //
 // What bounds it (one B200, bf16): the chain from a tile's scores to its weights and their products; one text of 8192, 32
 // heads of 128 over 8, causal: 469 us, 1170 TFLOP/s of the pairs that are seen (0.72 of the measured rate), 650 with a cap;
@@ -29,6 +29,7 @@ namespace sama {
 namespace {
 
 constexpr float kRaise = 8.f;
+template <typename T> constexpr float kLift = std::is_same<T, __half>::value ? 7.f : 0.f;   // (2^(8 + 7) fits)
 
 // NW: tiles of queries of a CTA.
 template <int D, int NW> struct FwdTile {
@@ -301,7 +302,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 }
             }
             const float from = m == -INFINITY ? 0.f : m;
-            const float2 c2 = both(c), from2 = both(-from);
+            const float2 c2 = both(c), from2 = both(kLift<T> - from);
             float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int k = 0; k < MY; k += 32) {
@@ -333,7 +334,7 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
             if (HALVES == 2) l += exchange(l, n_kt[w] & 1);
             const bool empty = l == 0.f;
             const float inv = 1.f / l;
-            if (real && P.lse && half == 0) P.lse[(int64_t)head * a.n_q + x.q0 + row] = empty ? -INFINITY : (m + __log2f(l)) * 0.69314718f;
+            if (real && P.lse && half == 0) P.lse[(int64_t)head * a.n_q + x.q0 + row] = empty ? -INFINITY : (m - kLift<T> + __log2f(l)) * 0.69314718f;
 #pragma unroll 1
             for (int k = half * (D / HALVES); k < (half + 1) * (D / HALVES); k += 32) {
                 float o[32];

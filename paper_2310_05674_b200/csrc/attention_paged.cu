@@ -32,6 +32,9 @@ template <int D> struct PagedTile {
     static constexpr int TILE = KEYS * D * 2, RING = STAGES * 2 * TILE, LD = D + 4;   // LD: a row's sums, maximum and weight
 };
 
+// fp16 has fewer places below 2^-14: weights, which are 1 at most, are lifted there as operands.
+template <typename T> constexpr float kLift = std::is_same<T, __half>::value ? 32768.f : 1.f;
+
 struct PagedParams {
     PagedShape a;
     const void *q, *k_new, *v_new;
@@ -299,7 +302,7 @@ paged_kernel(const PagedParams P) {
             for (int t = 0; t < 2; ++t) {
                 const float p0 = fast_exp2(s[t][0] - from), p1 = fast_exp2(s[t][1] - from);
                 l += p0 + p1;
-                p[t] = pack2<T>(p0, p1);
+                p[t] = pack2<T>(p0 * kLift<T>, p1 * kLift<T>);
             }
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
@@ -351,7 +354,7 @@ paged_kernel(const PagedParams P) {
         float* part = P.parts + (int64_t)(2 * cta + (first_step > 0 ? 0 : 1)) * ROWS * LD;
         T* out = static_cast<T*>(P.out) + ((int64_t)at.s * a.heads + g * a.group + row0) * a.dim;
         auto finish = [&](int r, int col, float x, float y, float w) {
-            const float inv = 1.f / w;
+            const float inv = 1.f / (w * kLift<T>);
             if (col < a.dim)
                 *reinterpret_cast<uint32_t*>(out + (int64_t)r * a.dim + col) = w == 0.f ? 0u : pack2<T>(x * inv, y * inv);
         };

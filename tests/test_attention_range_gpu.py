@@ -92,3 +92,54 @@ def test_values_that_make_large_products(lib):
     few = gradients(lib, r(300), r(4), r(4, 4.0), r(300, 8000.0), False)
     for name, (wrong, allowed) in zip(("dq", "dk", "dv") * 3, errors + more + few):
         assert wrong <= allowed, (name, wrong, allowed)
+
+
+# Four keys with most of the weight (of each 16 that are worked on together among the first 64, one), whose values are zeros, and some
+# 100,000 of one kind: each of those has 128.5 / 2^24 of a weight, which fp16 as it stands rounds by half a step of 2^-24, all of
+# them to the same side.
+KEYS, HEAVY, WEIGHT = 100001, [0, 16, 32, 48], 128.5 * 2.0 ** -24
+
+
+def few_and_many(dim):
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    k = torch.zeros(KEYS, 1, dim, dtype=torch.float16, device="cuda")
+    k[HEAVY, 0, 0] = 1.0
+    v = (1 + torch.rand(dim, generator=g, device="cuda").half()).repeat(KEYS, 1, 1)
+    v[HEAVY] = 0.0
+    total = (KEYS - 4) * WEIGHT
+    return k, v, -math.log(WEIGHT), v[1, 0].double() * total / (4 + total)
+
+
+def close(out, want):
+    """A weight's rounding and the result's, 2^-11 each.  fp32: the score 12 is off by 2^-21.  The products of a row are added in
+    order, 16 keys at a time, 6251 times, and the tensor core cuts the sum off, by 2^-23 of it at most; the weights' sum, by
+    threads that add up 64 keys or more of each tile, is rounded 2 * 1563 + 64 times by 2^-24."""
+    bound = 2.0 ** -10 + 2.0 ** -20 + 6251 * 2.0 ** -23 + 3190 * 2.0 ** -24
+    assert bool(((out.double() - want).abs() <= bound * want).all()), float((out.double() / want - 1).abs().max())
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_small_weights_packed(lib, dim):
+    S, ctx = lib
+    k, v, scale, want = few_and_many(dim)
+    q = torch.zeros(130, 1, dim, dtype=torch.float16, device="cuda")
+    q[:, :, 0] = 1.0
+    out, i32 = torch.empty_like(q), lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    S.sama_attention(ctx, S.Attn(S.SAMA_F16, 1, 1, dim, 130, len(k), i32(0, 130), i32(0, len(k)), scale=scale), q, k, v, out)
+    close(out, want)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_many_small_weights_cached(lib, dim):
+    S, ctx = lib
+    k, v, scale, want = few_and_many(dim)
+    page = 11
+    pages = len(k) // page                                            # (100,001 = 11 * 9091)
+    seqs = 300                                                        # (so many that a CTA has a whole one)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(seqs, 1)
+    q = torch.zeros(seqs, 1, dim, dtype=torch.float16, device="cuda")
+    q[..., 0] = 1.0
+    out, length = torch.empty_like(q), torch.full((seqs,), len(k), dtype=torch.int32, device="cuda")
+    p = S.Paged(S.SAMA_F16, 1, 1, dim, page, pages, table, length, scale=scale)
+    S.sama_paged_attention(ctx, p, q, None, None, k.view(pages, page, 1, dim), v.view(pages, page, 1, dim), out)
+    close(out, want)
