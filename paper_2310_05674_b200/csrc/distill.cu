@@ -142,9 +142,11 @@ template <typename T> __device__ __forceinline__ uint4 vec_lowest() {
     const uint32_t w = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __half>::value ? 0xfc00fc00u : 0xff80ff80u;
     return make_uint4(w, w, w, w);
 }
-// 2^(c (z - m)).  One operation less takes c z - (c m), whose second product is rounded: an error of 2^-15 at most up to the
-// c m that `beyond` names, of anything for a row of nothing but masked values (-1e9, or the type's lowest).
+// 2^(c (z - m)).  One operation less takes c z - (c m), whose second product is rounded: by up to 2^-14 up to the c m that
+// `beyond` names, the same for all z, and taken back by `unrounded`; by anything for a row of nothing but masked values (-1e9, or
+// the type's lowest).
 __device__ __forceinline__ float power_of(float z, float m, float c) { return fast_exp2((z - m) * c); }
+__device__ __forceinline__ float unrounded(float m, float c, float cm) { return fast_exp2(-fmaf(m, c, -cm)); }
 __device__ __forceinline__ bool beyond(float cm) { return fabsf(cm) > 1024.f; }
 // (m, l) of two parts, each a maximum and the sum of 2^(c (z - maximum)): l as seen from `top`.
 __device__ __forceinline__ float rebase(float l, float m, float top, float c) { return m == -INFINITY ? l : l * fast_exp2((m - top) * c); }
@@ -270,7 +272,7 @@ distill_kernel(const DistillParams P) {
         }
         asm volatile("bar.sync 1, %0;" ::"n"(MAIN) : "memory");
         const uint4* chunk = reinterpret_cast<const uint4*>(smem);
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f, from = 0.f;   // from: c m as it was rounded
         auto take = [&](auto count, int b) {   // vectors b, b + MAIN, ...
             constexpr int N = decltype(count)::value;
             uint4 x[N];
@@ -280,10 +282,11 @@ distill_kernel(const DistillParams P) {
 #pragma unroll
             for (int v = 0; v < N; ++v) top = fmaxf(top, vec_max<T>(x[v]));
             if (top > m) {
-                l = m == -INFINITY ? l : l * fast_exp2((m - top) * P.c);
+                const float raised = top * P.c;
+                l = m == -INFINITY ? l : l * fast_exp2(from - raised);
                 m = top;
+                from = raised;
             }
-            const float from = m == -INFINITY ? 0.f : m * P.c;
 #pragma unroll
             for (int v = 0; v < N; ++v) {
                 float f[VE], sum = 0.f;
@@ -296,7 +299,9 @@ distill_kernel(const DistillParams P) {
         int b = t;
         for (; b + (BATCH - 1) * MAIN < n; b += MAIN * BATCH) take(std::integral_constant<int, BATCH>(), b);
         for (; b < n; b += MAIN) take(std::integral_constant<int, 1>(), b);
-        if (beyond(m * P.c) && m != -INFINITY) {   // once more (in the loop it would cost ordinary rows a tenth of their time)
+        if (m != -INFINITY && !beyond(from)) {
+            l *= unrounded(m, P.c, from);
+        } else if (m != -INFINITY) {   // once more (in the loop it would cost ordinary rows a tenth of their time)
             l = 0.f;
 #pragma unroll 1
             for (b = t; b < n; b += MAIN) {
@@ -372,12 +377,12 @@ distill_kernel(const DistillParams P) {
             if ((uint32_t)(element0 + b * VE + e) < (uint32_t)P.vocab) g_part[b * VE + e] = from_float<T>(g[e]);
     };
     if (warp < WARPS && weight != 0.f) {
-        const float f = coef * inv;
+        const float f = coef * inv, near = f * unrounded(base, P.c, whole);
         const uint4* chunk = reinterpret_cast<const uint4*>(smem);
         auto gradient = [&](uint4 x, float* g) {
             unpack_vec<T>(x, g);
 #pragma unroll
-            for (int e = 0; e < VE; ++e) g[e] = fast_exp2(fmaf(g[e], P.c, -whole)) * f;
+            for (int e = 0; e < VE; ++e) g[e] = fast_exp2(fmaf(g[e], P.c, -whole)) * near;
         };
         auto make = [&](auto count, int b) {
             constexpr int N = decltype(count)::value;
