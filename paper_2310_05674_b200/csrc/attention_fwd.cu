@@ -302,7 +302,17 @@ attn_fwd_kernel(const __grid_constant__ FwdParams P) {
                 }
             }
             const float from = m == -INFINITY ? 0.f : m;
-            const float2 c2 = both(c), from2 = both(kLift<T> - from);
+            // c s - m in one operation has m rounded and the product not, which is nothing up to 2^20 (2^-4 at most, the same for the
+            // whole row) and can be anything at 2^30: rows beyond are taken there in two.
+            float2 c2 = both(c), from2 = both(kLift<T> - from);
+            if (RAW && __any_sync(0xffffffffu, fabsf(from) > 1048576.f)) {
+                if (fabsf(from) > 1048576.f) {
+#pragma unroll
+                    for (int k = 0; k < MY; ++k) s[k] = __fadd_rn(__fmul_rn(s[k], c), -from);
+                    c2 = both(1.f);
+                    from2 = both(kLift<T>);
+                }
+            }
             float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int k = 0; k < MY; k += 32) {

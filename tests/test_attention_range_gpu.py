@@ -143,3 +143,33 @@ def test_many_small_weights_cached(lib, dim):
     p = S.Paged(S.SAMA_F16, 1, 1, dim, page, pages, table, length, scale=scale)
     S.sama_paged_attention(ctx, p, q, None, None, k.view(pages, page, 1, dim), v.view(pages, page, 1, dim), out)
     close(out, want)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("texts", [1, 40])
+def test_scores_without_places_behind_the_point(lib, dtype, dim, texts):
+    """Scores of up to 10^9, far enough apart that a row's largest has all of the weight, rising along the keys: out is its value
+    and lse, as far as 24 bits go, its score."""
+    S, ctx = lib
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    dt, n, m = ref.DT[dtype], 260, 400
+    q, k = torch.zeros(texts * n, 1, dim, dtype=dt, device="cuda"), torch.zeros(texts * m, 1, dim, dtype=dt, device="cuda")
+    q[:, 0, 0] = torch.exp(torch.rand(texts * n, generator=g, device="cuda") * 14 - 6).to(dt)
+    k[:, 0, 0] = (100 + torch.arange(texts * m, device="cuda") % m).to(dt)       # (bf16: 100 .. 500 in steps of 1 to 4, some alike)
+    v = torch.randn(texts * m, 1, dim, generator=g, device="cuda").to(dt)
+    for t in range(texts):                                                      # the last keys of a text are alike: one value
+        v[t * m:t * m + m] = v[t * m + m - 1]
+    v[:, 0, 1] = (k[:, 0, 0] == k[-1, 0, 0]).to(dt)                             # 1 for the largest score, else 0
+    i32 = lambda step: torch.arange(0, texts + 1, device="cuda", dtype=torch.int32) * step  # noqa: E731
+    out, lse = torch.empty_like(q), torch.empty(1, texts * n, device="cuda")
+    for scale in (1000.0, 500.123):
+        S.sama_attention(ctx, S.Attn(S.DTYPES[dtype], 1, 1, dim, texts * n, texts * m, i32(n), i32(m), scale=scale), q, k, v, out, lse)
+        x = scale * q[:, 0, 0].double() * float(k[-1, 0, 0])
+        sure = scale * q[:, 0, 0].double() > 100                                # (the next key's score is that much less)
+        assert int(sure.sum()) > 100 * texts and float(x.max()) > 5e8
+        # (the weight is rounded, as it refers to a maximum that may be up to 2^8 less, and so is the result)
+        off = (out[sure, 0, 1].double() - 1).abs()
+        assert bool((off <= 2 * ref.U[dtype]).all()) and bool(torch.isfinite(out).all()), (float(off.max()), int((off > 0.5).sum()))
+        alike = int((k[:m, 0, 0] == k[-1, 0, 0]).sum())
+        assert bool(((lse[0, sure].double() - x[sure] - math.log(alike)).abs() <= 2.0 ** -21 * (x[sure] + 4)).all())
