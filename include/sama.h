@@ -347,7 +347,7 @@ typedef struct sama_attn_t {
     const int32_t* k_starts;             /* the same for keys, or NULL: the queries' (n_k == n_q) */
     const int32_t* prefix;               /* device [n_texts], or NULL; without effect unless causal */
     const float* slopes;                 /* device [heads], or NULL */
-    float scale, cap;                    /* scale > 0; cap 0: no cap */
+    float scale, cap;                    /* scale within 2^-60 .. 2^60; cap 0: no cap, else as scale and at least scale / 8192 */
     int64_t q_stride, k_stride, v_stride; /* elements from a row to the next, multiples of 8; 0: heads (kv_heads) * head_dim */
 } sama_attn_t;
 
@@ -386,7 +386,7 @@ typedef struct sama_paged_t {
     const int32_t* page_table;           /* device [n_seqs][max_pages]; entries behind a sequence's last page are not read */
     const int32_t* lengths;              /* device [n_seqs], 0 .. max_pages * page_size, 2^31 - 64 at most (others: SAMA_DEV_BAD_INDEX, taken as the nearest) */
     const float* slopes;                 /* device [heads], or NULL */
-    float scale, cap;
+    float scale, cap;                    /* as in sama_attn_t */
 } sama_paged_t;
 
 /* q, out: [n_seqs][heads][head_dim]; k_cache, v_cache: [n_pages][page_size][kv_heads][head_dim]; k_new, v_new:
@@ -410,7 +410,7 @@ int sama_paged_attention(sama_ctx* ctx, const sama_paged_t* a, const void* q, co
  * A row without any entry (or none above -infinity) has loss = 0 and a zero gradient.  weight: fp32 [n_rows] or NULL (1);
  * a row of weight 0 has a zero gradient, whatever its logits.  loss_out: fp32 [n_rows], not weighted (what the meta step's
  * weights are learnt from), or NULL.  Sums are fp32 in a fixed order (bitwise reproducible).
- * 0 <= n_rows <= 2^30, 1 <= vocab <= 2^24, 1 <= k <= 1024, T > 0. */
+ * 0 <= n_rows <= 2^30, 1 <= vocab <= 2^24, 1 <= k <= 1024, T within 2^-60 .. 2^60, grad_scale * T finite. */
 int sama_distill(sama_ctx* ctx, int32_t dtype, int64_t n_rows, int32_t vocab, const void* logits, int64_t ld, int32_t k,
                  int32_t top_dtype, const void* top_logits, const int32_t* top_ids, float temperature, const float* weight,
                  float grad_scale, float* loss_out, void* grad, int64_t ld_grad, void* stream);

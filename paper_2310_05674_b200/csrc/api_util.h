@@ -54,6 +54,9 @@ inline bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
     return x < y + nb && y < x + na;
 }
 
+// A factor whose products with others of the kind, and squares, fp32 holds.
+inline bool moderate(float x) { return x >= 0x1p-60f && x <= 0x1p60f; }
+
 // The operators' workspace, at least `bytes` large.  Growing it waits for the work that may still use the old one.
 // `ready`: the operator's kernels are set up; the first call does that, and allocates for it.  Neither is possible while
 // the stream is being captured, and trying would break the capture: the call is refused before.

@@ -1,6 +1,4 @@
 // Host side of attention: argument checks, workspace, launch sequencing.
-#include <cmath>
-
 #include "api_util.h"
 #include "attention.h"
 
@@ -29,8 +27,9 @@ bool rows_overlap(const Rows& a, const Rows& b) {
 
 int check_heads(int32_t dtype, int32_t heads, int32_t kv_heads, int32_t dim, float scale, float cap) {
     if (heads < 1 || heads > 65535 || kv_heads < 1 || heads % kv_heads != 0 || dim < 8 || dim > 128 || dim % 8 != 0) return SAMA_ERR_SIZE;
-    if ((dtype != SAMA_BF16 && dtype != SAMA_F16) || !std::isfinite(scale) || !(scale > 0.f) || !std::isfinite(cap) || cap < 0.f)
-        return SAMA_ERR_PARAM;
+    if ((dtype != SAMA_BF16 && dtype != SAMA_F16) || !moderate(scale)) return SAMA_ERR_PARAM;
+    // (the polynomial of a capped score has (scale / cap)^9)
+    if (cap != 0.f && (!moderate(cap) || scale / cap > 8192.f)) return SAMA_ERR_PARAM;
     return SAMA_OK;
 }
 

@@ -169,7 +169,7 @@ int sama_distill(sama_ctx* ctx, int32_t dtype, int64_t n_rows, int32_t vocab, co
                  float grad_scale, float* loss_out, void* grad, int64_t ld_grad, void* stream) {
     if (!ctx) return SAMA_ERR_NULL;
     if (n_rows < 0 || n_rows > kMaxTokens || vocab < 1 || vocab > (1 << 24) || k < 1 || k > 1024) return SAMA_ERR_SIZE;
-    if (!dtype_valid(dtype) || !dtype_valid(top_dtype) || !std::isfinite(temperature) || !(temperature > 0.f) || !std::isfinite(grad_scale))
+    if (!dtype_valid(dtype) || !dtype_valid(top_dtype) || !moderate(temperature) || !std::isfinite(grad_scale * temperature))
         return SAMA_ERR_PARAM;
     if (ld == 0) ld = vocab;
     if (ld_grad == 0) ld_grad = vocab;

@@ -53,3 +53,24 @@ def test_cached(lib, cap, dim):
         want, _ = ref.text(c.q[s:s + 1], k, v, None, "f16", dim ** -0.5, cap, None, False, 0)
         _, bound = ref.text(c.q[s:s + 1], k, v, None, "f16", dim ** -0.5, 0.0, None, False, 0)
         within(s, c.out[s:s + 1], want["out"], bound["out"], dim)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("size", [0.0, 1e-4, 2.0])
+@pytest.mark.parametrize("scale,cap", [(1.0, 2.0 ** -13), (2.0 ** -60, 2.0 ** -60), (2.0 ** -60, 2.0 ** 60), (0.125, 2.0 ** 60)])
+def test_the_ends_of_the_range(lib, scale, cap, size, dim):
+    """Queries of zeros among them, whose scores are all exactly 0."""
+    for bias in (False, True):
+        c = Packed(lib, [300, 9], heads=2, kv=1, dim=dim, dtype="bf16", causal=True, cap=cap, scale=scale, size=size, bias=bias, seed=2)
+        c.run()
+        for lo, hi in zip(c.qs, c.qs[1:]):
+            at = slice(lo, hi)
+            # (a large cap as none: the bounds have nothing for it)
+            want, bound = ref.text(c.q[at], c.k[at], c.v[at], c.dout[at], "bf16", c.scale, 0.0 if cap > 1 else cap, c.slopes, True, 0)
+            for name, x in (("out", c.out), ("lse", c.lse.T), ("dq", c.grads[0]), ("dk", c.grads[1]), ("dv", c.grads[2])):
+                w, b = (r[name].T if name == "lse" else r[name] for r in (want, bound))
+                within(name, x[at], w, b, dim)
+    p = Cached(lib, [40, 3], heads=2, kv=1, dim=dim, cap=max(cap, dim ** -0.5 * 2.0 ** -13), seed=3)   # (its scale is dim ** -0.5)
+    p.q *= size
+    p.run()
+    p.check()
