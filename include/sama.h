@@ -392,8 +392,9 @@ typedef struct sama_paged_t {
 /* q, out: [n_seqs][heads][head_dim]; k_cache, v_cache: [n_pages][page_size][kv_heads][head_dim]; k_new, v_new:
  * [n_seqs][kv_heads][head_dim], the new token's own, which are written to the cache and used, or both NULL where the cache
  * has them already.  Scores as in sama_attention.  A sequence of length 0 has out = 0 (and writes nothing to the cache).  A page
- * outside [0, n_pages) sets SAMA_DEV_BAD_INDEX and its keys are left out.  No two sequences may have their new token in
- * the same place.  The cache is split over its length when there are few sequences; partial results are joined in a fixed
+ * outside [0, n_pages) sets SAMA_DEV_BAD_INDEX and its keys are left out; a new token whose place is on such a page is used, but
+ * not kept.  Sequences may share pages, but new tokens are written while other keys are read: no other key or new token, of any
+ * sequence, may lie in a new token's place (several new tokens of one sequence at once: write them first, pass NULL).  The cache is split over its length when there are few sequences; partial results are joined in a fixed
  * order (bitwise reproducible). */
 int sama_paged_attention(sama_ctx* ctx, const sama_paged_t* a, const void* q, const void* k_new, const void* v_new,
                          void* k_cache, void* v_cache, void* out, void* stream);

@@ -34,3 +34,40 @@ def test_the_longest_sequences(lib):
         assert S.sama_device_status(ctx) == status, n
         # 64 keys of 2^31 less than the mean is over; 296 parts; the result's own rounding
         assert bool(((out[0].double() - want).abs() <= (2.0 ** -8 + 296 * 2.0 ** -23 + 2.0 ** -20) * want).all()), n
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, "bf16"), (128, "f16")])
+def test_sequences_that_share_pages(lib, dim, dtype):
+    """A prompt's pages in several sequences, each with a last page of its own for its new token; and several tokens of one sequence
+    at once, which are in the cache already."""
+    import attention_reference as ref
+    S, ctx = lib
+    heads, kv, page, shared, n = 4, 2, 16, 9, 5
+    g = torch.Generator(device="cuda").manual_seed(dim)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(ref.DT[dtype])  # noqa: E731
+    k, v = r(shared + n, page, kv, dim), r(shared + n, page, kv, dim)
+    table = torch.empty(n, shared + 1, dtype=torch.int32, device="cuda")
+    table[:, :shared] = torch.arange(shared, device="cuda")
+    table[:, shared] = shared + torch.arange(n, device="cuda")
+    lengths = torch.tensor([shared * page + 1 + 3 * s for s in range(n)], dtype=torch.int32, device="cuda")
+    q, k_new, v_new = r(n, heads, dim), r(n, kv, dim), r(n, kv, dim)
+    out = torch.empty_like(q)
+
+    def check(lengths, table):
+        for s, length in enumerate(lengths.tolist()):
+            K, V = (x[table[s].long()].flatten(0, 1)[:length] for x in (k, v))
+            want, bound = ref.text(q[s:s + 1], K, V, None, dtype, dim ** -0.5, 0.0, None, False, 0)
+            assert bool(((out[s:s + 1].double() - want["out"]).abs() <= bound["out"]).all()), s
+
+    S.sama_paged_attention(ctx, S.Paged(S.DTYPES[dtype], heads, kv, dim, page, shared + n, table, lengths), q, k_new, v_new, k, v, out)
+    torch.cuda.synchronize()
+    check(lengths, table)
+    at = lengths.long() - 1
+    rows = (table[torch.arange(n, device="cuda"), at // page].long(), at % page)
+    assert torch.equal(k[rows], k_new) and torch.equal(v[rows], v_new)
+    # five tokens of the first sequence
+    one, five = table[:1].repeat(n, 1), (shared * page + 2 + torch.arange(n, device="cuda")).to(torch.int32)
+    S.sama_paged_attention(ctx, S.Paged(S.DTYPES[dtype], heads, kv, dim, page, shared + n, one, five), q, None, None, k, v, out)
+    torch.cuda.synchronize()
+    check(five, one)
+    assert S.sama_device_status(ctx) == 0
