@@ -93,7 +93,7 @@ attn_bwd_kernel(const __grid_constant__ BwdParams P) {
     const AttnShape& a = P.a;
 
     pdl_wait();
-    if (!KEYS && blockIdx.x == 0) attn_check_starts(a);
+    if ((!KEYS || a.n_q == 0) && blockIdx.x == 0) attn_check_starts(a);   // (without queries d-keys is the only launch)
     // heavy tiles first: the first keys are seen by most queries, the last queries see most keys
     const int per_slot = KEYS ? a.kv_heads : a.heads, head0 = (int)blockIdx.x % per_slot;
     const int slot = KEYS ? (int)blockIdx.x / per_slot : P.slots - 1 - (int)blockIdx.x / per_slot;
