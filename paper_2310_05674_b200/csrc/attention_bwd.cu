@@ -12,19 +12,18 @@
 //
 // The order of the products of tile i is  dP_i, dV (from P_i), S_i+1, dK (from dX_i), dP_i+1, ...:  P_i+1 is formed from
 // S_i+1 while dK and dP_i+1 run, dX_i from dP_i while dV and S_i+1 run.  (d-queries: P K in dV's place, dQ in dK's.)  S, dP and
-// two accumulators of 128 columns fill tensor memory.  (Tiles of 64 rows in two buffers, which the two halves of the warps took in turn, were slower, 1452 for 1148 us:
-// a product 64 wide takes 48 cycles in place of 32, and each wait of the issuing thread leaves the tensor cores idle for some
-// 200 cycles, since it can run ahead of them by a product or two only.)  Heads of up to 64 columns have tiles of 64 rows
-// and two CTAs per SM, which overlap each other.
+// two accumulators of 128 columns fill tensor memory.  (Tiles of 64 rows in two buffers, which the two halves of the warps took
+// in turn, were slower, 1452 for 1148 us: a product 64 wide takes 48 cycles in place of 32, and each wait of the issuing thread
+// leaves the tensor cores idle for some 200 cycles, since it can run ahead of them by a product or two only.)  Heads of up to 64
+// columns have tiles of 64 rows and two CTAs per SM, which overlap each other.
 //
 // delta comes from out as the forward pass rounded it; d-queries adds up what it is off by, puts dQ right, and hands d-keys
 // the exact one.
 //
-// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 1050, d-keys
-// 1115, 635 TFLOP/s of the five products that the definition needs, 1015 of the eight: forming P
-// and dX between products that wait for them; tensor cores are busy 45 % of the time, as are the issue slots, although the
-// arithmetic is done two scores per instruction (one: 1010 and 1160).  48 texts of up to 512, 16 heads of 64, biased: 123
-// and 132, the start and end of CTAs that have three to eight tiles each and the latency of a tile's way.
+// What bounds it (us on one B200, bf16): one text of 8192, 32 heads of 128 over 8, causal, capped: d-queries 1060, d-keys
+// 1150 in a short run (1200 and 1300 under the power limit), 620 TFLOP/s of the five products that the definition needs, 995 of
+// the eight: forming P and dX between products that wait for them; tensor cores are busy 47 % of the time, as are the issue
+// slots.  48 texts of up to 512, 16 heads of 64, biased: 121 and 131, the start and end of CTAs that have three to eight tiles each and the latency of a tile's way.
 //
 // Roles of the warps: warp 0 copies, warp 1 issues products, the other 16 (or 8) form P and dX: several share 32 rows, each
 // of them has 32 of a tile's columns.  Every wait is bounded.
@@ -592,8 +591,8 @@ cudaError_t launch_attention_grad(sama_ctx* ctx, const AttnShape& a, const AttnO
     P.largest = P.delta + (size_t)a.heads * a.n_q;
     const int64_t dense = (int64_t)a.heads * a.dim;
     // Small tiles, two CTAs per SM, unless capped scores, whose arithmetic weighs more, are many (us for d-queries and d-keys,
-    // 16 heads of 64: 16 texts of 512 39 and 42, with the large ones 45 and 52, capped 56 and 56, 60 and 66; one of 8192,
-    // causal, 277 and 344, 310 and 379; but 4 of 2048, causal and capped, 86 and 99, 76 and 88).  Lengths are on the device, but
+    // 16 heads of 64: 16 texts of up to 512 38 and 41, with the large ones 48 and 49, capped 54 and 52, 61 and 61; one of 8192,
+    // causal, 283 and 319, 320 and 356; but 4 of up to 2048, causal and capped, 92 and 94, 82 and 85).  Lengths are on the device, but
     // their mean is known.
     const int bt = a.dim <= 64 && (a.cap == 0.f || a.n_q <= 512 * (int64_t)a.n_texts) ? 64 : 128;
     auto query_maps = [&](CUtensorMap* m, int rows) {

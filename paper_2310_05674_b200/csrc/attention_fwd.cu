@@ -11,10 +11,10 @@
 // below 2^-14, gets them lifted by 2^7, so that those from 2^-21 of the largest on keep all of theirs.
 //
 // What bounds it (one B200, bf16): the chain from a tile's scores to its weights and their products; one text of 8192, 32
-// heads of 128 over 8, causal: 469 us, 1170 TFLOP/s of the pairs that are seen (0.72 of the measured rate), 650 with a cap;
+// heads of 128 over 8, causal: 466 us, 1180 TFLOP/s of the pairs that are seen (0.72 of the measured rate), 650 with a cap;
 // 48 texts of up to 512, 16 heads of 64, biased: 90, where ragged tiles and the start and end of short CTAs weigh as much.
-// Two prompts' next 1000 tokens behind 7000: 250 us; tensor cores and special-function units are in use for 57 % of the time,
-// issue slots for 31, and 512 CTAs fill 296 places less than twice.  Exponentials by a polynomial for a quarter of the scores,
+// Two prompts' next 1000 tokens behind 7000: 255 us; tensor cores and special-function units are in use for 52 % of the time,
+// issue slots for 30, and 512 CTAs fill 296 places less than twice.  Exponentials by a polynomial for a quarter of the scores,
 // and rounding to bf16 by integer addition, were slower (275, 254): more instructions in the chain.  For heads of 64, four
 // CTAs per SM (spilled registers, 102 us for 90) and two warps per 32 rows (97) were slower.
 //
@@ -402,9 +402,9 @@ cudaError_t launch_attention(sama_ctx* ctx, const AttnShape& a, const AttnOperan
     FwdParams P;
     const int bk = a.dim <= 64 ? FwdTile<64, 1>::BK : FwdTile<128, 2>::BK;
     // Two tiles per CTA, which read the keys once, for long texts; for shorter ones a CTA's start and end and the tiles that
-    // a text does not fill weigh more (us with two and with one, 32 heads of 128 over 8: one text of 512 21 and 17, of 2048 53.6
-    // and 53.7, of 4096, causal, 150 and 148, of 8192, causal, 484 and 488, capped 745 and 812; 8 of 1024 76 and 70, 32 of 300
-    // 99 and 80; 2 of 4096, all heads with their own keys, 314 and 329).  Lengths are on the device, but their mean is known.
+    // a text does not fill weigh more (us with two and with one, 32 heads of 128 over 8: one text of 512 17.7 and 15.6, of 2048 78.7
+    // and 78.7, of 4096, causal, 140 and 138, of 8192, causal, 466 and 476, capped 646 and 655; 8 of up to 1024 95 and 89, 32 of up
+    // to 300 103 and 87; 2 of up to 4096, all heads with their own keys, 304 and 322).  Lengths are on the device, but their mean is known.
     const int nw = a.dim <= 64 || a.n_q < 2048 * (int64_t)a.n_texts ? 1 : 2;
     // (without keys nothing is loaded, but a map has to describe something)
     const bool none = a.n_k == 0;

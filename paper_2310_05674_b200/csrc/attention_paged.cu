@@ -1,8 +1,8 @@
 // Attention of one new token per sequence over a cache in pages.
 //
-// Every key and value is read once and meets the few queries that share its head: 2 to 16 flops per byte, bound by memory
-// (96 sequences of up to 4096 keys, 32 heads of 128 over 8: 165 us, 5.8 TB/s, 0.88 of the copy rate; one of 60,001, capped:
-// 52 for 37 at that rate, the rest the way to the first keys, three loads that depend on one another, and the join).
+// Every key and value is read once for each 8 queries that share its head: 2 to 16 flops per byte, bound by memory
+// (96 sequences of up to 4096 keys, 32 heads of 128 over 8: 165 to 173 us, 5.5 to 5.8 TB/s, 0.84 to 0.88 of the copy rate; one of
+// 60,001, capped: 50 for 37 at that rate, the rest the way to the first keys, three loads that depend on one another, and the join).
 // What is needed is bytes in flight, so the cache streams through rings in shared memory, a ring per warp, by asynchronous
 // 16-byte copies that follow the page table; three tiles of 16 keys and values (8 KB each at 128 columns) are on their way per
 // warp, 8 warps per SM.  The products are small (8 queries by 16 keys) and go to the warp-level matrix instructions: the
