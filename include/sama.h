@@ -328,14 +328,16 @@ int sama_clip_grads(sama_ctx* ctx, const sama_tensor_t* tensors, int32_t n_tenso
  * Scores of a query against a key, for head h and key head g = h / (heads / kv_heads):
  *   x = scale * (q . k);   if cap > 0: x = cap * tanh(x / cap);   if slopes: x = x - slopes[h] * |pos_q - pos_k|
  *   out = sum over the keys that the query sees of softmax(x) * v
- * (a capped score is off by 7e-7 of itself, or up to a cap of 64 by 1e-5 at most; the softmax and every sum in fp32; the weights, operands of the second product, are rounded to `dtype`).
+ * (a capped score is off by 7e-7 of itself, or up to a cap of 64 by 1e-5 at most; the softmax and every sum in fp32; the
+ * weights, operands of the second product, are rounded to `dtype`).
  *
  * Texts lie packed behind one another: text t has the queries q_starts[t] .. q_starts[t+1] - 1 and the keys
  * k_starts[t] .. k_starts[t+1] - 1, and its queries see its own keys only.  The last query has the position of the last
  * key: with Lq queries and Lk keys, query i of a text is at position i + Lk - Lq, key j at j (so a prompt's next chunk is
  * the case Lk > Lq).  causal: a query sees the keys up to its position, and those before prefix[t] (NULL: none).
- * A query that sees no key (or none whose score is above -infinity) has out = 0, lse = -infinity and no gradient.  Rows of no text (before the first start, from
- * the last on) are neither read for any text nor written, and no value of one text, finite or not, reaches another's.
+ * A query that sees no key (or none whose score is above -infinity) has out = 0, lse = -infinity and no gradient.  Rows of
+ * no text (before the first start, from the last on) are neither read for any text nor written, and no value of one text,
+ * finite or not, reaches another's.
  * Within a text a v that is not finite may reach queries that do not see it (as 0 * infinity does). */
 typedef struct sama_attn_t {
     int32_t dtype;                       /* SAMA_BF16 or SAMA_F16: q, k, v, out and their gradients */
@@ -362,13 +364,14 @@ typedef struct sama_attn_t {
  * dk and dv are summed over the heads that share them.  Sums are fp32, in a fixed order (bitwise reproducible).  dX and the
  * softmax are rounded to `dtype` as operands of the last products: against sums of unrounded values the gradients' relative
  * error grows from 0.0017 to 0.0024 in bf16, 0.0002 to 0.0003 in fp16 (out's to 0.0018 .. 0.0022, 0.0003).  d_out . out is
- * put right for out's rounding by the sum of softmax * (dP - d_out . out).  Keys with a common offset have dq's error grow as
- * their size does, which dq itself does not (0.007 in bf16, 0.0009 in fp16 where the offset is four times their spread).  slopes get no gradient.  In
- * SAMA_F16 the softmax and dX are scaled by powers of two on the way, dX by what takes the largest of d_out (for dq of its row, for
- * dk of the queries from the first on that sees a key of the same 128) to 4 .. 8, so that a small or large d_out costs no
- * places; results beyond 65504 are infinite, and dX beyond 8000 times the largest of d_out is, too.  Within a text a k, q or d_out
- * that is not finite may reach gradients of rows that do not see it.  Uses (8 * n_q + 4 * (n_q / 128 + n_texts)) * heads bytes of
- * the workspace. */
+ * put right for out's rounding by the sum of softmax * (dP - d_out . out).  Keys with a common offset have dq's error grow
+ * as their size does, which dq itself does not (0.007 in bf16, 0.0009 in fp16 where the offset is four times their spread).
+ * The softmax is formed again from x - lse, off by some 2^-23 of the larger: scores of 10^6 leave gradients of one place.  In
+ * SAMA_F16 the softmax and dX are scaled by powers of two on the way, dX by what takes the largest of d_out (for dq of its
+ * row, for dk of the queries from the first on that sees a key of the same 128) to 4 .. 8, so that a small or large d_out
+ * costs no places; results beyond 65504 are infinite, and dX beyond 8000 times the largest of d_out is, too.  slopes get no
+ * gradient.  Within a text a k, q or d_out that is not finite may reach gradients of rows that do not see it.  Uses
+ * (8 * n_q + 4 * (n_q / 128 + n_texts)) * heads bytes of the workspace. */
 int sama_attention(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, void* out,
                    float* lse_out, void* stream);
 int sama_attention_grad(sama_ctx* ctx, const sama_attn_t* a, const void* q, const void* k, const void* v, const void* out,

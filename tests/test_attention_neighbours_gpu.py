@@ -54,3 +54,22 @@ def test_neighbours_do_not_choose_how_scores_are_capped(lib, cap, causal, bias, 
     looked at are, and their neighbours' are not.)"""
     for lens in ([300, 61, 400, 30], [70, 500, 140], [129, 1, 385, 2]):
         same_bits(lib, lens, among, dim=dim, causal=causal, bias=bias, cap=cap)
+
+
+@pytest.mark.parametrize("among", [1, MANY])
+@pytest.mark.parametrize("dim,dtype", [(64, "bf16"), (128, "f16"), (40, "f16")])
+@pytest.mark.parametrize("cap", [0.0, 20.0, 300.0])
+@pytest.mark.parametrize("causal,bias", [(True, False), (False, True)])
+def test_neighbours_that_are_not_finite(lib, causal, bias, cap, dim, dtype, among):
+    lens = [70, 61, 300]
+    for bad in (float("nan"), float("inf"), -float("inf")):
+        plain, other = (Case(lib, lens, heads=2, kv=1, dim=dim, dtype=dtype, causal=causal, bias=bias, cap=cap, seed=7,
+                             edge=MANY * len(lens) if among > 1 else 5) for _ in range(2))
+        for x in (other.q, other.k, other.v, other.dout):
+            x[other.qs[1]:other.qs[2]] = bad
+        plain.run()
+        other.run()
+        for x, y in zip((plain.out, plain.lse.T, *plain.grads), (other.out, other.lse.T, *other.grads)):
+            for t in (0, 2):
+                at = slice(plain.qs[t], plain.qs[t + 1])
+                assert torch.equal(x[at], y[at]) and bool(torch.isfinite(x[at]).all())
