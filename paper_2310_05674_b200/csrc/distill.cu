@@ -8,8 +8,8 @@
 // which exchange maximum and sum through distributed shared memory.  A bulk copy brings the part in; the threads take
 // maximum and sum of it, meet, and write q from registers straight to memory, while a warp of its own works out the teacher's
 // distribution, the loss and the gradient's values at the teacher's entries, which go over q at the end.  A CTA does one
-// thing after the other, and two or more of them per SM keep memory busy meanwhile.  4096 rows of 50,021 bf16 logits: 156 us,
-// 5.3 TB/s (0.81 of the copy rate); of 131,072 486 us, 4.4 TB/s (0.67), where a cluster meets twice per row and two
+// thing after the other, and two or more of them per SM keep memory busy meanwhile.  4096 rows of 50,021 bf16 logits: 156
+// to 162 us, 5.1 to 5.3 TB/s (0.77 to 0.80 of the copy rate); of 131,072 484 us, 4.4 TB/s (0.68), where a cluster meets twice per row and two
 // exponentials per logit take 60 % of the special-function units.  (A persistent CTA whose groups of warps work on different
 // rows of a ring was slower, 174 and 470 us at its best: it had a single copy in flight per SM most of the time.)
 // Rows of up to 4 KB are a warp's each; rows that no cluster can hold, or with more than 512 entries, are read twice.
