@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -24,3 +25,18 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+@pytest.fixture(autouse=True)
+def garbage_is_collected_between_gpu_tests(request):
+    """A CUDA graph that Python's garbage collector destroys while another is being captured invalidates that capture: what an
+    earlier test has left in cycles (an exception's traceback is enough) would end a later one, depending on the number of
+    objects made since."""
+    if "gpu" not in request.keywords:
+        yield
+        return
+    gc.collect()
+    gc.freeze()        # (what is left lives on: the next collection need not look at it)
+    gc.disable()
+    yield
+    gc.enable()
